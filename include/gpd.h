@@ -422,6 +422,56 @@ gpd_status coded_layer_step(gpd_plan_t plan, int32_t phases, void* W_shares_dev,
                             float* S_out_dev, float* Xnext_out_dev, float* CT_out_dev,
                             gpd_locate_result* results_dev, void* workspace_dev, void* stream);
 
+/*
+ * ---- Low-precision layer and output-head operators ------------------------------------------------
+ * What a language model's layers need next to the products above.  They follow the conventions at the
+ * top of this file, with these differences: a row is one token and matrices are row-major with a row
+ * stride in elements (ld*, at least the row length); tensors may be FP32, BF16 or FP16 (sums, norms and
+ * softmax statistics are FP32); 8-bit matrices are e4m3 or e5m2.  They need no plan, allocate nothing and
+ * may be captured into a CUDA graph.  Outputs must not overlap inputs unless the call says so.
+ *
+ * 8-bit blocks: 128 neighbours along a row (the last block may be shorter) share the scale 2^e, stored
+ * as the byte e + 127; e is the smallest integer >= -127 for which the block's largest magnitude is at
+ * most 448 * 2^e (e4m3) or 57344 * 2^e (e5m2), elements are rounded to nearest even.  A block of zeros
+ * has scale 1.  A block with a NaN or an infinity has the byte 255, which stands for NaN.
+ */
+typedef enum { GPD_DT_F32 = 0, GPD_DT_BF16 = 1, GPD_DT_F16 = 2, GPD_DT_E4M3 = 3, GPD_DT_E5M2 = 4 } gpd_dtype;
+
+#define GPD_RMSNORM_MAX_PARTS 512 /* gpd_rmsnorm_backward: partial rows of dweight in its workspace */
+
+/*
+ * gpd_rmsnorm_quant - root-mean-square norm with the residual's addition and an 8-bit output:
+ *   h = x + residual,  s = (mean_c h^2 + eps)^(-1/2),  y = h s weight      for T rows of H columns.
+ * h and y are FP32 inside and rounded once when stored; the norm is of the unrounded h.
+ * residual_dev may be NULL (h = x).  Outputs, each optional (NULL): h (residual_out_dev, may be x_dev or
+ * residual_dev with the same stride), y in the type of x (may be x_dev), y in 8 bits (q_dev of q_type with
+ * scales_dev [T][ceil(H/128)] bytes, row strides ldq and lds), s (rstd_dev, T floats).
+ * weight_type: `type` or GPD_DT_F32.
+ */
+gpd_status gpd_rmsnorm_quant(gpd_dtype type, const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr,
+                             gpd_dtype weight_type, const void* weight_dev, float eps, void* residual_out_dev,
+                             int64_t ldh, void* y_dev, int64_t ldy, gpd_dtype q_type, void* q_dev, int64_t ldq,
+                             uint8_t* scales_dev, int64_t lds, float* rstd_dev, int64_t T, int64_t H, void* stream);
+/*
+ * gpd_rmsnorm_backward - gradient of the norm, 8-bit rounding passed straight through:
+ *   dx = s (g - h s^2 mean_c(g h)) + dresidual  with g = dy weight;   dweight_c = sum_t dy h s  (floats)
+ * h: the stored sum of the forward call; s: its rstd.  dx is the gradient of x and of the residual alike;
+ * dx_dev may be dy_dev or dresidual_dev (NULL: none).  dweight is summed in a fixed order.
+ * workspace_dev: min(T, GPD_RMSNORM_MAX_PARTS) * H floats.
+ */
+gpd_status gpd_rmsnorm_backward(gpd_dtype type, const void* dy_dev, int64_t lddy, const void* h_dev, int64_t ldh,
+                                gpd_dtype weight_type, const void* weight_dev, const float* rstd_dev,
+                                const void* dresidual_dev, int64_t lddh, void* dx_dev, int64_t lddx, float* dweight_dev,
+                                int64_t T, int64_t H, void* workspace_dev, int64_t workspace_bytes, void* stream);
+/*
+ * gpd_quantize_blocks - cuts an M x K matrix into 8-bit blocks of block_rows x 128 (block_rows 1 or 128):
+ *   q_dev  [M][K] with scales_dev  [ceil(M/block_rows)][ceil(K/128)]   and/or, transposed,
+ *   qT_dev [K][M] with scalesT_dev [ceil(K/block_rows)][ceil(M/128)]   (blocks along the rows of src).
+ */
+gpd_status gpd_quantize_blocks(gpd_dtype type, const void* src_dev, int64_t ld, gpd_dtype q_type, int32_t block_rows,
+                               void* q_dev, int64_t ldq, uint8_t* scales_dev, int64_t lds, void* qT_dev, int64_t ldqT,
+                               uint8_t* scalesT_dev, int64_t ldsT, int64_t M, int64_t K, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,3 +6,4 @@ library; it fails loudly when the library has not been built (there is no CPU fa
 
 from .binding import *  # noqa: F401,F403
 from .binding import EXPORTED, Plan, GpdError, lib, new_results, read_results, result_slot  # noqa: F401
+from .lm import *  # noqa: F401,F403

@@ -1,0 +1,170 @@
+// Shared by the low-precision layer operators (rmsnorm.cu, quantize.cu, gemm_fp8.cu, logits.cu):
+// loads and stores of eight neighbouring elements of any of the storage types, the 8-bit conversions and
+// the power-of-two block scale.
+//
+// A block's scale is 2^e with the smallest e for which the block's largest magnitude is at most
+// top * 2^e, top = 448 (e4m3) or 57344 (e5m2), both 0.875 times a power of two.  A power of two makes the
+// division by the scale exact (one rounding per element, the conversion's), costs at most one step of an
+// 8-bit type's exponent range, and is the form the tensor cores apply by themselves; it is stored as its
+// biased exponent in one byte (e8m0).  A block of zeros has scale 1; a block holding a NaN or an infinity
+// has the scale byte 255, which stands for NaN, so that nothing computed from it looks like a number.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "gpd_internal.h"
+
+namespace gpd {
+namespace lm {
+
+constexpr int kBlock = 128;                            // elements that share a scale
+
+template <typename T> struct Raw8 { uint4 v; };        // eight 16-bit elements
+template <> struct Raw8<float> { uint4 v, w; };
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half) {
+    const __half2 p = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t u, __nv_bfloat16) {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t u, __half) {
+    return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+
+// Eight elements at p, of which n (may be <= 0 or >= 8) exist; the others read as zero.  VEC: p is
+// 16-byte aligned (the caller has checked base and row stride).
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> load8(const T* p, int64_t n) {
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 4) {
+        if (VEC && n >= 8) {
+            r.v = reinterpret_cast<const uint4*>(p)[0];
+            r.w = reinterpret_cast<const uint4*>(p)[1];
+        } else {
+            uint32_t u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = i < n ? __float_as_uint(p[i]) : 0u;
+            r.v = make_uint4(u[0], u[1], u[2], u[3]);
+            r.w = make_uint4(u[4], u[5], u[6], u[7]);
+        }
+    } else {
+        if (VEC && n >= 8) {
+            r.v = *reinterpret_cast<const uint4*>(p);
+        } else {
+            const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t lo = 2 * i < n ? s[2 * i] : 0u, hi = 2 * i + 1 < n ? s[2 * i + 1] : 0u;
+                u[i] = lo | (hi << 16);
+            }
+            r.v = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&f)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        f[0] = __uint_as_float(r.v.x); f[1] = __uint_as_float(r.v.y); f[2] = __uint_as_float(r.v.z); f[3] = __uint_as_float(r.v.w);
+        f[4] = __uint_as_float(r.w.x); f[5] = __uint_as_float(r.w.y); f[6] = __uint_as_float(r.w.z); f[7] = __uint_as_float(r.w.w);
+    } else {
+        const float2 a = unpack2(r.v.x, T()), b = unpack2(r.v.y, T()), c = unpack2(r.v.z, T()), d = unpack2(r.v.w, T());
+        f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T* p, const float (&f)[8], int64_t n) {
+    if (VEC && n >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+            reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+        } else {
+            *reinterpret_cast<uint4*>(p) = make_uint4(pack2(f[0], f[1], T()), pack2(f[2], f[3], T()),
+                                                      pack2(f[4], f[5], T()), pack2(f[6], f[7], T()));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = from_f32<T>(f[i]);
+    }
+}
+
+// ---- 8-bit blocks ----------------------------------------------------------------------------------
+// top = 0.875 * 2^kTopExp
+template <int Q> struct Fp8;
+template <> struct Fp8<GPD_DT_E4M3> { static constexpr int kTopExp = 9; };
+template <> struct Fp8<GPD_DT_E5M2> { static constexpr int kTopExp = 16; };
+
+// Magnitudes are compared as bit patterns: NaN is then the largest and cannot be lost in a maximum.
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Scale byte of a block whose largest magnitude has these bits.
+template <int Q>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
+    if (amax == 0u) return 127u;
+    if (amax >= 0x7f800000u) return 255u;
+    const int e = (int)(amax >> 23) + 1 - Fp8<Q>::kTopExp + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return (uint32_t)max(e, 0);
+}
+// 1 / scale = 2^(127 - byte); for the byte 255 any number will do.
+__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - min(byte, 253u)) << 23); }
+
+template <int Q>
+__device__ __forceinline__ uint32_t cvt_fp8x2(float lo, float hi) {
+    unsigned short r;
+    if constexpr (Q == GPD_DT_E4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <int Q>
+__device__ __forceinline__ uint32_t cvt_fp8x4(float a, float b, float c, float d) {
+    return cvt_fp8x2<Q>(a, b) | (cvt_fp8x2<Q>(c, d) << 16);
+}
+// Eight bytes at p, of which n exist; VEC: p is 8-byte aligned.
+template <bool VEC>
+__device__ __forceinline__ void store8_bytes(uint8_t* p, uint2 b, int64_t n) {
+    if (VEC && n >= 8) {
+        *reinterpret_cast<uint2*>(p) = b;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (uint8_t)((i < 4 ? b.x >> (8 * i) : b.y >> (8 * (i - 4))) & 0xffu);
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// ---- host side: argument checks ---------------------------------------------------------------------
+inline int dtype_size(int t) { return t == GPD_DT_F32 ? 4 : (t == GPD_DT_BF16 || t == GPD_DT_F16) ? 2 : 1; }
+inline bool is_float_type(int t) { return t == GPD_DT_F32 || t == GPD_DT_BF16 || t == GPD_DT_F16; }
+inline bool is_fp8_type(int t) { return t == GPD_DT_E4M3 || t == GPD_DT_E5M2; }
+inline bool aligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+// A matrix of `elem`-byte elements can be read in 16-byte pieces of every row (absent matrices can).
+inline bool rows_aligned(const void* p, int64_t ld, int elem, int bytes = 16) {
+    return !p || (aligned(p, bytes) && (ld * elem) % bytes == 0);
+}
+
+}  // namespace lm
+}  // namespace gpd

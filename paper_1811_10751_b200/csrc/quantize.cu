@@ -1,0 +1,185 @@
+// Cutting a matrix into 8-bit blocks with power-of-two scales, straight and transposed in one pass.
+//
+//   straight:    blocks of 1 x 128 (or 128 x 128) elements of src, q[r][c], scale[r / br][c / 128]
+//   transposed:  the same of src^T, qT[c][r], scaleT[c / br][r / 128]: the operand of a product that
+//                contracts over src's rows
+//
+// One CTA takes a 128 x 128 tile, which holds whole blocks of either kind, so the source is read once for
+// both: HBM bounds it (source bytes + one byte per element and output).  Thread (rg, cg) holds the 8 x 8
+// patch at rows 8 rg, columns 8 cg.  A row's sixteen column groups sit in sixteen adjacent lanes (maximum
+// by shuffles); the column maxima meet in shared memory.  A patch's column is eight bytes of a transposed
+// row, so the transposed tile goes through shared memory in 8-byte pieces and leaves in 16-byte ones.
+#include "lm_common.h"
+
+namespace gpd {
+
+namespace {
+
+using namespace lm;
+
+struct CutArgs {
+    const void* src; int64_t ld;
+    uint8_t* q; int64_t ldq;
+    uint8_t* s; int64_t lds;
+    uint8_t* qT; int64_t ldqT;
+    uint8_t* sT; int64_t ldsT;
+    int64_t M, K;
+};
+
+constexpr int kPitch = kBlock + 16;                    // bytes between transposed rows in shared memory (16-byte pieces stay aligned)
+
+template <typename T, int Q, bool SQUARE, bool VEC>
+__global__ void __launch_bounds__(256) cut_kernel(const CutArgs a, int tiles_k) {
+    __shared__ __align__(16) uint8_t tile[kBlock * kPitch];
+    __shared__ uint32_t colmax[16][kBlock];
+    const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
+    const int64_t bm = blockIdx.x / tiles_k, bk = blockIdx.x % tiles_k;
+    const int64_t r0 = bm * kBlock + 8 * rg, c0 = bk * kBlock + 8 * cg;
+    const int64_t nc = a.K - c0;
+
+    Raw8<T> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        raw[i] = r0 + i < a.M && nc > 0 ? load8<T, VEC>(static_cast<const T*>(a.src) + (r0 + i) * a.ld + c0, nc) : Raw8<T>{};
+
+    uint32_t cmax[8], rmax[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cmax[j] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float f[8];
+        unpack8<T>(raw[i], f);
+        rmax[i] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b = abs_bits(f[j]);
+            rmax[i] = max(rmax[i], b);
+            cmax[j] = max(cmax[j], b);
+        }
+    }
+    uint32_t byte = 0;                                 // SQUARE: the tile's scale
+    if (SQUARE) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, rmax[i]);
+        m = __reduce_max_sync(0xffffffffu, m);
+        if ((threadIdx.x & 31) == 0) colmax[0][threadIdx.x >> 5] = m;
+        __syncthreads();
+        m = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) m = max(m, colmax[0][w]);
+        byte = scale_byte<Q>(m);
+        if (threadIdx.x == 0) {
+            if (a.q) a.s[bm * a.lds + bk] = (uint8_t)byte;
+            if (a.qT) a.sT[bk * a.ldsT + bm] = (uint8_t)byte;
+        }
+    } else if (a.qT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) colmax[rg][8 * cg + j] = cmax[j];
+        __syncthreads();
+        if (threadIdx.x < kBlock) {                    // thread = column
+            uint32_t m = 0;
+#pragma unroll
+            for (int g = 0; g < 16; ++g) m = max(m, colmax[g][threadIdx.x]);
+            const uint32_t b = scale_byte<Q>(m);
+            colmax[0][threadIdx.x] = b;                // only this thread reads row 0 of its column
+            const int64_t c = bk * kBlock + threadIdx.x;
+            if (c < a.K) a.sT[c * a.ldsT + bm] = (uint8_t)b;
+        }
+        __syncthreads();
+    }
+
+    if (a.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t b = byte;
+            if (!SQUARE) {
+                uint32_t m = rmax[i];
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                b = scale_byte<Q>(m);
+                if (cg == 0 && r0 + i < a.M) a.s[(r0 + i) * a.lds + bk] = (uint8_t)b;
+            }
+            if (r0 + i < a.M && nc > 0) {
+                const float inv = scale_inverse(b);
+                float f[8];
+                unpack8<T>(raw[i], f);
+                store8_bytes<VEC>(a.q + (r0 + i) * a.ldq + c0,
+                                  make_uint2(cvt_fp8x4<Q>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                                             cvt_fp8x4<Q>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)), nc);
+            }
+        }
+    }
+    if (a.qT) {
+        float inv[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) inv[j] = scale_inverse(SQUARE ? byte : colmax[0][8 * cg + j]);
+        float f[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) unpack8<T>(raw[i], f[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint2*>(tile + (8 * cg + j) * kPitch + 8 * rg) =
+                make_uint2(cvt_fp8x4<Q>(f[0][j] * inv[j], f[1][j] * inv[j], f[2][j] * inv[j], f[3][j] * inv[j]),
+                           cvt_fp8x4<Q>(f[4][j] * inv[j], f[5][j] * inv[j], f[6][j] * inv[j], f[7][j] * inv[j]));
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {                  // 32 transposed rows per pass, 8 lanes of 16 bytes each
+            const int col = 32 * p + (threadIdx.x >> 3), piece = threadIdx.x & 7;
+            const int64_t c = bk * kBlock + col, r = bm * kBlock + 16 * piece, n = a.M - r;
+            if (c >= a.K || n <= 0) continue;
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + col * kPitch + 16 * piece);
+            uint8_t* dst = a.qT + c * a.ldqT + r;
+            if (VEC && n >= 16) {
+                *reinterpret_cast<uint4*>(dst) = v;
+            } else {
+                store8_bytes<false>(dst, make_uint2(v.x, v.y), n);
+                store8_bytes<false>(dst + 8, make_uint2(v.z, v.w), n - 8);
+            }
+        }
+    }
+}
+
+template <typename T, int Q>
+gpd_status launch_cut(const CutArgs& a, bool square, cudaStream_t st) {
+    const int64_t tk = (a.K + kBlock - 1) / kBlock, tm = (a.M + kBlock - 1) / kBlock;
+    if (tk * tm > 0x7fffffff) return GPD_ERR_SHAPE;
+    const unsigned grid = (unsigned)(tk * tm);
+    const bool vec = rows_aligned(a.src, a.ld, sizeof(T)) && rows_aligned(a.q, a.ldq, 1, 8) && rows_aligned(a.qT, a.ldqT, 1);
+    if (square) {
+        if (vec) cut_kernel<T, Q, true, true><<<grid, 256, 0, st>>>(a, (int)tk);
+        else cut_kernel<T, Q, true, false><<<grid, 256, 0, st>>>(a, (int)tk);
+    } else {
+        if (vec) cut_kernel<T, Q, false, true><<<grid, 256, 0, st>>>(a, (int)tk);
+        else cut_kernel<T, Q, false, false><<<grid, 256, 0, st>>>(a, (int)tk);
+    }
+    return launch_ok();
+}
+template <typename T>
+gpd_status launch_cut_q(const CutArgs& a, int q_type, bool square, cudaStream_t st) {
+    return q_type == GPD_DT_E4M3 ? launch_cut<T, GPD_DT_E4M3>(a, square, st) : launch_cut<T, GPD_DT_E5M2>(a, square, st);
+}
+
+}  // namespace
+
+}  // namespace gpd
+
+using namespace gpd;
+
+extern "C" gpd_status gpd_quantize_blocks(gpd_dtype type, const void* src_dev, int64_t ld, gpd_dtype q_type, int32_t block_rows,
+                                          void* q_dev, int64_t ldq, uint8_t* scales_dev, int64_t lds, void* qT_dev,
+                                          int64_t ldqT, uint8_t* scalesT_dev, int64_t ldsT, int64_t M, int64_t K, void* stream) {
+    if (!is_float_type(type) || !is_fp8_type(q_type) || (block_rows != 1 && block_rows != lm::kBlock)) return GPD_ERR_ARG;
+    if (M < 0 || K < 0) return GPD_ERR_SHAPE;
+    if (M == 0 || K == 0) return GPD_OK;               // empty buffers may have no address
+    if (!src_dev || (!q_dev && !qT_dev) || (q_dev && !scales_dev) || (qT_dev && !scalesT_dev)) return GPD_ERR_ARG;
+    const int64_t kb = (K + lm::kBlock - 1) / lm::kBlock, mb = (M + lm::kBlock - 1) / lm::kBlock;
+    if (ld < K || (q_dev && (ldq < K || lds < kb)) || (qT_dev && (ldqT < M || ldsT < mb))) return GPD_ERR_SHAPE;
+    const CutArgs a{src_dev, ld, static_cast<uint8_t*>(q_dev), ldq, scales_dev, lds, static_cast<uint8_t*>(qT_dev), ldqT,
+                    scalesT_dev, ldsT, M, K};
+    const bool square = block_rows != 1;
+    cudaStream_t st = as_stream(stream);
+    if (type == GPD_DT_F32) return launch_cut_q<float>(a, q_type, square, st);
+    if (type == GPD_DT_BF16) return launch_cut_q<__nv_bfloat16>(a, q_type, square, st);
+    return launch_cut_q<__half>(a, q_type, square, st);
+}

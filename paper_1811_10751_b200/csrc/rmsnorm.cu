@@ -1,0 +1,369 @@
+// Root-mean-square norm with the residual's addition and an 8-bit output, and its gradient.
+//
+//   h = x + r,   s = (mean_c h^2 + eps)^(-1/2),   y = h s w      (FP32 throughout; h is rounded once, when stored)
+//   q, scale = y cut into blocks of 128 columns (lm_common.h)
+//   dx = s (g - h s^2 mean_c(g h)) + dh  with g = dy w,   dw_c = sum_t dy h s
+//
+// Both directions move each element once and do a few operations on it, so HBM bounds them.  A row stays
+// in registers between the sum over its columns and its use: thread i of the row's G threads holds the
+// vectors i, i + G, ... of eight neighbouring elements, so that loads and stores are 16 bytes per lane and
+// the sixteen vectors of a scale block lie in sixteen adjacent lanes (four shuffles give the block's maximum).
+#include <algorithm>
+
+#include "lm_common.h"
+
+namespace gpd {
+
+namespace {
+
+using namespace lm;
+
+struct NormArgs {
+    const void* x; int64_t ldx;
+    const void* residual; int64_t ldr;
+    const void* weight;
+    void* h; int64_t ldh;
+    void* y; int64_t ldy;
+    uint8_t* q; int64_t ldq;
+    uint8_t* scales; int64_t lds;
+    float* rstd;
+    int64_t T, H;
+    float eps;
+};
+
+// Sum over the G threads of a row; every thread gets it.  G = 32: a warp of its own, no barrier.
+__device__ __forceinline__ float row_sum(float v, int G, float* scratch) {
+    v = warp_sum(v);
+    if (G == 32) return v;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = G >> 5;
+    if (lane == 0) scratch[warp] = v;
+    __syncthreads();
+    v = warp_sum(lane < n ? scratch[lane] : 0.f);
+    __syncthreads();                                   // scratch may be written again
+    return v;
+}
+
+// VPT vectors per thread are kept in registers; VPT = 0: rows too long for that are read twice.
+// blockDim = (G, rows per CTA), rows per CTA > 1 only with G = 32.
+template <typename T, typename W, int Q, int VPT, bool VEC>
+__global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const NormArgs a) {
+    __shared__ float scratch[32];
+    const int G = blockDim.x;
+    const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (t >= a.T) return;                              // a whole warp (G = 32) or, with one row per CTA, never
+    const T* x = static_cast<const T*>(a.x) + t * a.ldx;
+    const T* res = a.residual ? static_cast<const T*>(a.residual) + t * a.ldr : nullptr;
+    const W* wt = static_cast<const W*>(a.weight);
+    T* hout = a.h ? static_cast<T*>(a.h) + t * a.ldh : nullptr;
+    T* yout = a.y ? static_cast<T*>(a.y) + t * a.ldy : nullptr;
+    uint8_t* qout = a.q ? a.q + t * a.ldq : nullptr;
+    uint8_t* sout = a.q ? a.scales + t * a.lds : nullptr;
+
+    auto read = [&](int64_t c, float (&f)[8]) {
+        const int64_t n = a.H - c;
+        if (n <= 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = 0.f;
+            return;
+        }
+        unpack8<T>(load8<T, VEC>(x + c, n), f);
+        if (res) {
+            float r[8];
+            unpack8<T>(load8<T, VEC>(res + c, n), r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] += r[i];
+        }
+    };
+    // every lane of a warp gets here together (the shuffles need it)
+    auto finish = [&](int64_t c, const float (&h)[8], float s) {
+        const int64_t n = a.H - c;
+        float y[8];
+        if (n > 0) {
+            if (hout) store8<T, VEC>(hout + c, h, n);
+            float w[8];
+            unpack8<W>(load8<W, VEC>(wt + c, n), w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = h[i] * s * w[i];
+            if (yout) store8<T, VEC>(yout + c, y, n);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = 0.f;
+        }
+        if (!qout) return;
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(y[i]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const uint32_t b = scale_byte<Q>(m);
+        if (n > 0) {
+            const float inv = scale_inverse(b);
+            const uint2 v = make_uint2(cvt_fp8x4<Q>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
+                                       cvt_fp8x4<Q>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+            store8_bytes<VEC>(qout + c, v, n);
+            if ((c & (kBlock - 1)) == 0) sout[c / kBlock] = (uint8_t)b;
+        }
+    };
+
+    float sum = 0.f;
+    if constexpr (VPT > 0) {
+        float h[VPT][8];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) read(8 * ((int64_t)threadIdx.x + i * G), h[i]);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(h[i][j], h[i][j], sum);
+        sum = row_sum(sum, G, scratch);
+        const float s = rsqrtf(sum / (float)a.H + a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) finish(8 * ((int64_t)threadIdx.x + i * G), h[i], s);
+    } else {
+        // h may be stored over x or r: nothing is written before the second reading, and each element
+        // is read and written by the same thread
+        const int64_t step = 8 * (int64_t)G, end = (a.H + step - 1) / step * step;
+        for (int64_t c = 8 * threadIdx.x; c < end; c += step) {
+            float h[8];
+            read(c, h);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(h[j], h[j], sum);
+        }
+        sum = row_sum(sum, G, scratch);
+        const float s = rsqrtf(sum / (float)a.H + a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
+        for (int64_t c = 8 * threadIdx.x; c < end; c += step) {
+            float h[8];
+            read(c, h);
+            finish(c, h, s);
+        }
+    }
+}
+
+template <typename T, typename W, int Q, bool VEC>
+gpd_status launch_norm(const NormArgs& a, cudaStream_t st) {
+    const int64_t vecs = (a.H + 7) / 8;
+    auto threads = [&](int vpt) { return (int)(((vecs + vpt - 1) / vpt + 31) / 32 * 32); };
+    if (vecs <= 64) {                                  // a warp per row, four rows per CTA
+        const dim3 block(32, 4);
+        const unsigned grid = (unsigned)((a.T + 3) / 4);
+        if (vecs <= 32) rmsnorm_kernel<T, W, Q, 1, VEC><<<grid, block, 0, st>>>(a);
+        else rmsnorm_kernel<T, W, Q, 2, VEC><<<grid, block, 0, st>>>(a);
+    } else if (vecs <= 1024) {
+        rmsnorm_kernel<T, W, Q, 2, VEC><<<(unsigned)a.T, threads(2), 0, st>>>(a);
+    } else if (vecs <= 2048) {
+        rmsnorm_kernel<T, W, Q, 4, VEC><<<(unsigned)a.T, threads(4), 0, st>>>(a);
+    } else {
+        rmsnorm_kernel<T, W, Q, 0, VEC><<<(unsigned)a.T, 1024, 0, st>>>(a);
+    }
+    return launch_ok();
+}
+template <typename T, typename W, int Q>
+gpd_status launch_norm_q(const NormArgs& a, cudaStream_t st) {
+    const int e = sizeof(T);
+    const bool vec = rows_aligned(a.x, a.ldx, e) && rows_aligned(a.residual, a.ldr, e) && rows_aligned(a.h, a.ldh, e) &&
+                     rows_aligned(a.y, a.ldy, e) && rows_aligned(a.q, a.ldq, 1, 8) && aligned(a.weight, 16);
+    return vec ? launch_norm<T, W, Q, true>(a, st) : launch_norm<T, W, Q, false>(a, st);
+}
+template <typename T, typename W>
+gpd_status launch_norm_w(const NormArgs& a, int q_type, cudaStream_t st) {
+    return q_type == GPD_DT_E5M2 ? launch_norm_q<T, W, GPD_DT_E5M2>(a, st) : launch_norm_q<T, W, GPD_DT_E4M3>(a, st);
+}
+
+// ---- gradient ----------------------------------------------------------------------------------------
+struct NormBwdArgs {
+    const void* dy; int64_t lddy;
+    const void* h; int64_t ldh;
+    const void* dh; int64_t lddh;
+    const void* weight;
+    const float* rstd;
+    void* dx; int64_t lddx;
+    float* parts;                                      // [gridDim.x][H]
+    int64_t T, H;
+};
+
+// CTA p takes the rows p, p + gridDim.x, ... and adds up its share of dw: in registers, or (VPT = 0, long
+// rows) in its own row of `parts`, element by element by the thread that owns the column.
+template <typename T, typename W, int VPT, bool VEC>
+__global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(const NormBwdArgs a) {
+    __shared__ float scratch[32];
+    const int G = blockDim.x;
+    const W* wt = static_cast<const W*>(a.weight);
+    float* part = a.parts + (int64_t)blockIdx.x * a.H;
+    constexpr int N = VPT > 0 ? VPT : 1;
+    float dw[N][8];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
+    const int64_t step = 8 * (int64_t)G;
+
+    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const T* dy = static_cast<const T*>(a.dy) + t * a.lddy;
+        const T* h = static_cast<const T*>(a.h) + t * a.ldh;
+        const T* dh = a.dh ? static_cast<const T*>(a.dh) + t * a.lddh : nullptr;
+        T* dx = static_cast<T*>(a.dx) + t * a.lddx;
+        const float s = a.rstd[t];
+        auto write = [&](int64_t c, const Raw8<T>& rdy, const Raw8<T>& rh, const Raw8<T>& rdh, float k, float (&acc)[8]) {
+            const int64_t n = a.H - c;
+            float fy[8], fh[8], fd[8], w[8];
+            unpack8<T>(rdy, fy);
+            unpack8<T>(rh, fh);
+            unpack8<T>(rdh, fd);
+            unpack8<W>(load8<W, VEC>(wt + c, n), w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                acc[j] = fmaf(fy[j] * s, fh[j], acc[j]);
+                fd[j] = fmaf(s, fmaf(-fh[j], k, fy[j] * w[j]), fd[j]);
+            }
+            store8<T, VEC>(dx + c, fd, n);
+        };
+        float dot = 0.f;
+        if constexpr (VPT > 0) {
+            Raw8<T> rdy[VPT], rh[VPT], rdh[VPT];
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int64_t c = 8 * ((int64_t)threadIdx.x + i * G), n = a.H - c;
+                rdy[i] = n > 0 ? load8<T, VEC>(dy + c, n) : Raw8<T>{};
+                rh[i] = n > 0 ? load8<T, VEC>(h + c, n) : Raw8<T>{};
+                rdh[i] = n > 0 && dh ? load8<T, VEC>(dh + c, n) : Raw8<T>{};
+            }
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
+                if (c < a.H) {
+                    float fy[8], fh[8], w[8];
+                    unpack8<T>(rdy[i], fy);
+                    unpack8<T>(rh[i], fh);
+                    unpack8<W>(load8<W, VEC>(wt + c, a.H - c), w);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dot = fmaf(fy[j] * w[j], fh[j], dot);
+                }
+            }
+            dot = row_sum(dot, G, scratch);
+            const float k = s * s * (dot / (float)a.H);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
+                if (c < a.H) write(c, rdy[i], rh[i], rdh[i], k, dw[i]);
+            }
+        } else {
+            for (int64_t c = 8 * threadIdx.x; c < a.H; c += step) {
+                float fy[8], fh[8], w[8];
+                unpack8<T>(load8<T, VEC>(dy + c, a.H - c), fy);
+                unpack8<T>(load8<T, VEC>(h + c, a.H - c), fh);
+                unpack8<W>(load8<W, VEC>(wt + c, a.H - c), w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dot = fmaf(fy[j] * w[j], fh[j], dot);
+            }
+            dot = row_sum(dot, G, scratch);
+            const float k = s * s * (dot / (float)a.H);
+            for (int64_t c = 8 * threadIdx.x; c < a.H; c += step) {
+                const int64_t n = a.H - c;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dw[0][j] = j < n && t != blockIdx.x ? part[c + j] : 0.f;
+                write(c, load8<T, VEC>(dy + c, n), load8<T, VEC>(h + c, n), dh ? load8<T, VEC>(dh + c, n) : Raw8<T>{}, k, dw[0]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < n) part[c + j] = dw[0][j];
+            }
+        }
+    }
+    if constexpr (VPT > 0) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j < a.H) part[c + j] = dw[i][j];
+        }
+    }
+}
+
+// dw_c = sum over the partial rows, in a fixed order: eight threads per column, then their sums.
+__global__ void __launch_bounds__(256) rmsnorm_dweight_kernel(const float* parts, int n, int64_t H, float* dw) {
+    __shared__ float s[8][33];
+    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+    float v = 0.f;
+    if (c < H)
+        for (int p = threadIdx.y; p < n; p += 8) v += parts[(int64_t)p * H + c];
+    s[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.y == 0 && c < H) {
+        for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+        dw[c] = v;
+    }
+}
+
+template <typename T, typename W, bool VEC>
+gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
+    const int64_t vecs = (a.H + 7) / 8;
+    const int parts = (int)std::min<int64_t>(std::min<int64_t>(a.T, 3 * sm_count()), GPD_RMSNORM_MAX_PARTS);
+    if (parts > 0) {
+        constexpr int V = sizeof(T) == 4 ? 2 : 4;
+        if (vecs <= 512 * V)
+            rmsnorm_backward_kernel<T, W, V, VEC><<<parts, (int)(((vecs + V - 1) / V + 31) / 32 * 32), 0, st>>>(a);
+        else
+            rmsnorm_backward_kernel<T, W, 0, VEC><<<parts, 1024, 0, st>>>(a);
+    }
+    rmsnorm_dweight_kernel<<<(unsigned)((a.H + 31) / 32), dim3(32, 8), 0, st>>>(a.parts, parts, a.H, dweight);
+    return launch_ok();
+}
+template <typename T, typename W>
+gpd_status launch_bwd_w(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
+    const int e = sizeof(T);
+    const bool vec = rows_aligned(a.dy, a.lddy, e) && rows_aligned(a.h, a.ldh, e) && rows_aligned(a.dh, a.lddh, e) &&
+                     rows_aligned(a.dx, a.lddx, e) && aligned(a.weight, 16);
+    return vec ? launch_bwd<T, W, true>(a, dweight, st) : launch_bwd<T, W, false>(a, dweight, st);
+}
+
+}  // namespace
+
+}  // namespace gpd
+
+using namespace gpd;
+
+extern "C" gpd_status gpd_rmsnorm_quant(gpd_dtype type, const void* x_dev, int64_t ldx, const void* residual_dev,
+                                        int64_t ldr, gpd_dtype weight_type, const void* weight_dev, float eps,
+                                        void* residual_out_dev, int64_t ldh, void* y_dev, int64_t ldy, gpd_dtype q_type,
+                                        void* q_dev, int64_t ldq, uint8_t* scales_dev, int64_t lds, float* rstd_dev,
+                                        int64_t T, int64_t H, void* stream) {
+    if (!is_float_type(type) || (weight_type != type && weight_type != GPD_DT_F32)) return GPD_ERR_ARG;
+    if (T < 0 || H <= 0 || T > 0x7fffffff) return GPD_ERR_SHAPE;
+    if (T == 0) return GPD_OK;                         // empty buffers may have no address
+    if (!x_dev || !weight_dev || (q_dev && (!scales_dev || !is_fp8_type(q_type)))) return GPD_ERR_ARG;
+    if (ldx < H || (residual_dev && ldr < H) || (residual_out_dev && ldh < H) || (y_dev && ldy < H) ||
+        (q_dev && (ldq < H || lds < (H + lm::kBlock - 1) / lm::kBlock)))
+        return GPD_ERR_SHAPE;
+    const NormArgs a{x_dev, ldx, residual_dev, ldr, weight_dev, residual_out_dev, ldh, y_dev, ldy, static_cast<uint8_t*>(q_dev),
+                     ldq, scales_dev, lds, rstd_dev, T, H, eps};
+    cudaStream_t st = as_stream(stream);
+    if (type == GPD_DT_F32) return launch_norm_w<float, float>(a, q_type, st);
+    if (type == GPD_DT_BF16)
+        return weight_type == GPD_DT_F32 ? launch_norm_w<__nv_bfloat16, float>(a, q_type, st)
+                                         : launch_norm_w<__nv_bfloat16, __nv_bfloat16>(a, q_type, st);
+    return weight_type == GPD_DT_F32 ? launch_norm_w<__half, float>(a, q_type, st) : launch_norm_w<__half, __half>(a, q_type, st);
+}
+
+extern "C" gpd_status gpd_rmsnorm_backward(gpd_dtype type, const void* dy_dev, int64_t lddy, const void* h_dev, int64_t ldh,
+                                           gpd_dtype weight_type, const void* weight_dev, const float* rstd_dev,
+                                           const void* dresidual_dev, int64_t lddh, void* dx_dev, int64_t lddx,
+                                           float* dweight_dev, int64_t T, int64_t H, void* workspace_dev,
+                                           int64_t workspace_bytes, void* stream) {
+    if (!is_float_type(type) || (weight_type != type && weight_type != GPD_DT_F32)) return GPD_ERR_ARG;
+    if (T < 0 || H <= 0) return GPD_ERR_SHAPE;
+    if (!dweight_dev || (T > 0 && (!dy_dev || !h_dev || !weight_dev || !rstd_dev || !dx_dev))) return GPD_ERR_ARG;
+    if (T > 0 && (lddy < H || ldh < H || (dresidual_dev && lddh < H) || lddx < H)) return GPD_ERR_SHAPE;
+    if (T > 0 && (!workspace_dev || workspace_bytes < std::min<int64_t>(T, GPD_RMSNORM_MAX_PARTS) * H * (int64_t)sizeof(float) ||
+                  !aligned(workspace_dev, 4)))
+        return GPD_ERR_WORKSPACE;
+    const NormBwdArgs a{dy_dev, lddy, h_dev, ldh, dresidual_dev, lddh, weight_dev, rstd_dev, dx_dev, lddx,
+                        static_cast<float*>(workspace_dev), T, H};
+    cudaStream_t st = as_stream(stream);
+    if (type == GPD_DT_F32) return launch_bwd_w<float, float>(a, dweight_dev, st);
+    if (type == GPD_DT_BF16)
+        return weight_type == GPD_DT_F32 ? launch_bwd_w<__nv_bfloat16, float>(a, dweight_dev, st)
+                                         : launch_bwd_w<__nv_bfloat16, __nv_bfloat16>(a, dweight_dev, st);
+    return weight_type == GPD_DT_F32 ? launch_bwd_w<__half, float>(a, dweight_dev, st)
+                                     : launch_bwd_w<__half, __half>(a, dweight_dev, st);
+}

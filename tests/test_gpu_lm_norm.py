@@ -1,0 +1,225 @@
+"""RMS norm with residual and 8-bit output, its gradient, and the cutting of matrices into 8-bit blocks,
+against plain 64-bit forms.
+
+Bounds.  FP32 sums of n terms: at most (terms added one after another + depth of the tree) roundings of
+2^-24 each; the longest chain here is 64 per thread and 10 levels, so 74 * 2^-24 < 5e-6 for a sum of squares
+and half of that (plus 2^-22 for rsqrt) for its inverse root.  EPS_Y = 1e-5 covers y = h s w.  Stored values
+add the rounding of their type."""
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA device", allow_module_level=True)
+
+import paper_1811_10751_b200 as g                                           # noqa: E402
+from tests.lm_reference import check_close, check_cut, like, scale_values, strided   # noqa: E402
+
+EPS_Y = 1e-5
+E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def _rand(seed, *shape):
+    return torch.randn(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+def _ref_norm(x, res, w, eps):
+    h = x.double() + (0 if res is None else res.double())
+    s = (h.square().mean(1) + eps).rsqrt()
+    return h, s, h * s[:, None] * w.double()
+
+
+@pytest.mark.parametrize("T,H,pad,offset", [
+    (1, 1, 0, 0), (3, 7, 1, 1), (5, 128, 0, 0), (2, 130, 6, 8), (9, 256, 8, 0), (4, 264, 0, 0), (6, 512, 0, 1),
+    (7, 1000, 0, 0), (1, 4096, 0, 0), (33, 4104, 8, 0), (3, 8192, 0, 0), (2, 8199, 0, 3), (2, 16384, 0, 0),
+    (2, 16400, 0, 0), (1, 40000, 0, 0), (1, 33333, 1, 1)])
+@pytest.mark.parametrize("dtype,wtype,qtype", [(BF, BF, E4), (HF, F32, E5), (F32, F32, E4)])
+def test_norm_matches_64_bit_form(T, H, pad, offset, dtype, wtype, qtype):
+    x = like(_rand(1, T, H), dtype, pad, offset)
+    r = like(_rand(2, T, H) * 3, dtype, pad, offset)
+    w = (1 + 0.2 * _rand(3, H)).to(wtype)
+    h, y = strided(T, H, dtype, pad, offset), strided(T, H, dtype, pad, offset)
+    q, s = g.new_fp8(T, H, qtype)
+    rstd = torch.empty(T, device="cuda")
+    g.gpd_rmsnorm_quant(x, w, 1e-5, residual=r, residual_out=h, y=y, q=q, scales=s, rstd=rstd)
+    rh, rs, ry = _ref_norm(x, r, w, 1e-5)
+    check_close(h, rh, 2.0 ** -23)                              # the FP32 sum, then the stored type
+    check_close(rstd, rs, EPS_Y / 2)
+    check_close(y, ry, EPS_Y)
+    check_cut(q, s, ry, EPS_Y)
+
+
+def test_norm_without_residual_in_place_and_single_outputs():
+    T, H = 5, 1024
+    x, r, w = _rand(1, T, H).to(BF), _rand(2, T, H).to(BF), torch.ones(H, device="cuda", dtype=BF)
+    y = torch.empty_like(x)
+    g.gpd_rmsnorm_quant(x, w, 1e-6, y=y)                        # plain norm
+    check_close(y, _ref_norm(x, None, w, 1e-6)[2], EPS_Y)
+    rh, _, ry = _ref_norm(x, r, w, 1e-6)
+    x2, r2 = x.clone(), r.clone()
+    g.gpd_rmsnorm_quant(x2, w, 1e-6, residual=r2, residual_out=r2, y=x2)
+    check_close(r2, rh, 2.0 ** -23)
+    check_close(x2, ry, EPS_Y)
+    xl, rl, wl = _rand(4, 2, 20000).to(BF), _rand(5, 2, 20000).to(BF), torch.ones(20000, device="cuda")
+    rh, _, ry = _ref_norm(xl, rl, wl, 1e-6)                     # rows that are read twice, also in place
+    g.gpd_rmsnorm_quant(xl, wl, 1e-6, residual=rl, residual_out=rl, y=xl)
+    check_close(rl, rh, 2.0 ** -23)
+    check_close(xl, ry, EPS_Y)
+    scales_only = torch.full((T, 8), 7, dtype=torch.uint8, device="cuda")
+    q = torch.empty((T, H), dtype=E4, device="cuda")
+    g.gpd_rmsnorm_quant(x, w, 1e-6, q=q, scales=scales_only)    # uint8 holds the same bytes
+    check_cut(q, scales_only, _ref_norm(x, None, w, 1e-6)[2], EPS_Y)
+
+
+def test_norm_of_zero_and_non_finite_rows_and_of_no_rows():
+    H = 256
+    x = _rand(1, 4, H).to(BF)
+    x[1] = 0
+    x[2, 3], x[3, 200] = float("nan"), float("inf")
+    w = torch.ones(H, device="cuda", dtype=BF)
+    w[128:] = 0                                                 # a block of zeros in every row
+    q, s = g.new_fp8(4, H)
+    g.gpd_rmsnorm_quant(x, w, 1e-5, q=q, scales=s)
+    v = scale_values(s)
+    assert v[0, 1] == 1 and torch.equal(v[1].cpu(), torch.ones(2, dtype=torch.float64))
+    assert bool((q[0, 128:].double() == 0).all()) and bool((q[1].double() == 0).all())
+    assert bool(torch.isnan(v[2]).all()) and bool(torch.isnan(v[3, 1]))      # inf * 0: the row's scale is zero
+    e = torch.empty((0, H), device="cuda", dtype=BF)
+    g.gpd_rmsnorm_quant(e, w, 1e-5, y=e)
+
+
+@pytest.mark.parametrize("T,H,pad", [(1, 1, 0), (3, 129, 1), (2, 512, 0), (700, 264, 0), (1000, 96, 0), (5, 4096, 0), (450, 4100, 4),
+                                     (3, 8192, 0), (2, 8200, 0), (3, 16384, 0), (450, 16500, 4)])
+@pytest.mark.parametrize("dtype,wtype", [(BF, BF), (HF, F32), (F32, F32)])
+@pytest.mark.parametrize("has_dh", [True, False])
+def test_norm_gradient_matches_64_bit_form(T, H, pad, dtype, wtype, has_dh):
+    h, dy, dh = like(_rand(1, T, H) * 2, dtype, pad), like(_rand(2, T, H), dtype, pad), like(_rand(3, T, H), dtype, pad)
+    w = (1 + 0.2 * _rand(4, H)).to(wtype)
+    rstd = (h.float().square().mean(1) + 1e-5).rsqrt()
+    dx, dw = strided(T, H, dtype, pad), torch.full((H,), float("nan"), device="cuda")
+    ws = torch.full((min(T, g.GPD_RMSNORM_MAX_PARTS) * H,), float("nan"), device="cuda")
+    g.gpd_rmsnorm_backward(dy, h, w, rstd, dx, dw, ws, dresidual=dh if has_dh else None)
+    H64, dY, s, W = h.double(), dy.double(), rstd.double()[:, None], w.double()
+    gr = dY * W
+    mean = (gr * H64).mean(1, keepdim=True)
+    ref = s * (gr - H64 * s * s * mean) + (dh.double() if has_dh else 0)
+    # sum of three terms: each brings its own roundings; the mean's are those of a sum of H terms of either sign
+    size = s * (gr.abs() + H64.abs() * s * s * (gr * H64).abs().mean(1, keepdim=True)) + (dh.double().abs() if has_dh else 0)
+    check_close(dx, ref, EPS_Y, size)
+    # chains of T / parts rows in a thread, then at most 64 + 8 partial rows
+    n = -(-T // min(T, 148)) + 72
+    check_close(dw, (dY * H64 * s).sum(0), (n + 3) * 2.0 ** -24, (dY * H64 * s).abs().sum(0))
+
+
+def test_norm_gradient_against_differences_and_in_place():
+    T, H = 3, 300
+    x, r, w = _rand(1, T, H), _rand(2, T, H), 1 + 0.2 * _rand(3, H)
+    dy, dh = _rand(4, T, H), _rand(5, T, H)
+    h, rstd = torch.empty_like(x), torch.empty(T, device="cuda")
+    g.gpd_rmsnorm_quant(x, w, 1e-5, residual=r, residual_out=h, rstd=rstd)
+    dx, dw, ws = dy.clone(), torch.empty(H, device="cuda"), torch.empty(T * H, device="cuda")
+    g.gpd_rmsnorm_backward(dx, h, w, rstd, dx, dw, ws, dresidual=dh)          # dx over dy
+
+    def value(x, w):
+        hh, _, y = _ref_norm(x, r, w, 1e-5)
+        return (y * dy.double()).sum() + (hh * dh.double()).sum()
+    for seed in range(4):
+        vx, vw, e = _rand(10 + seed, T, H).double(), _rand(20 + seed, H).double(), 1e-4
+        num = (value(x.double() + e * vx, w.double()) - value(x.double() - e * vx, w.double())) / (2 * e)
+        assert abs(float((dx.double() * vx).sum() - num)) <= 1e-5 * float((dx.double() * vx).abs().sum())
+        num = (value(x.double(), w.double() + e * vw) - value(x.double(), w.double() - e * vw)) / (2 * e)
+        assert abs(float((dw.double() * vw).sum() - num)) <= 1e-5 * float((dw.double() * vw).abs().sum())
+
+
+def test_norm_gradient_of_no_rows_is_zero_and_repeats_exactly():
+    dw = torch.full((64,), 3.0, device="cuda")
+    e = torch.empty((0, 64), device="cuda")
+    g.gpd_rmsnorm_backward(e, e, torch.ones(64, device="cuda"), torch.empty(0, device="cuda"), e, dw, torch.empty(0, device="cuda"))
+    assert bool((dw == 0).all())
+    T, H = 2000, 640
+    h, dy, w = _rand(1, T, H).to(BF), _rand(2, T, H).to(BF), torch.ones(H, device="cuda")
+    rstd = (h.float().square().mean(1) + 1e-5).rsqrt()
+    outs = []
+    for _ in range(3):
+        dx, dw, ws = torch.empty_like(h), torch.empty(H, device="cuda"), torch.empty(512 * H, device="cuda")
+        g.gpd_rmsnorm_backward(dy, h, w, rstd, dx, dw, ws)
+        outs.append((dx, dw))
+    assert all(torch.equal(a, outs[0][0]) and torch.equal(b, outs[0][1]) for a, b in outs)
+
+
+@pytest.mark.parametrize("M,K,pad,offset", [(1, 1, 0, 0), (128, 128, 0, 0), (130, 257, 0, 0), (127, 129, 7, 0), (5, 1000, 0, 8),
+                                            (300, 64, 0, 1), (256, 384, 8, 0), (1, 4096, 0, 0), (777, 8, 0, 0), (16, 136, 0, 0)])
+@pytest.mark.parametrize("dtype,qtype", [(BF, E4), (HF, E5), (F32, E5), (F32, E4)])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_cut_matches_64_bit_form_straight_and_transposed(M, K, pad, offset, dtype, qtype, block_rows):
+    x = like(_rand(1, M, K) * torch.exp(_rand(2, M, 1)) * torch.exp(_rand(3, 1, K)), dtype, pad, offset)
+    q, s = g.new_fp8(M, K, qtype, block_rows)
+    qT, sT = g.new_fp8(K, M, qtype, block_rows)
+    g.gpd_quantize_blocks(x, q=q, scales=s, qT=qT, scalesT=sT, block_rows=block_rows)
+    check_cut(q, s, x.double(), 0.0, block_rows)
+    check_cut(qT, sT, x.double().t(), 0.0, block_rows)
+    q1, s1 = (torch.zeros((M, K), dtype=torch.uint8, device="cuda").view(qtype),
+              torch.zeros((-(-M // block_rows), -(-K // 128)), dtype=torch.uint8, device="cuda"))
+    g.gpd_quantize_blocks(x, q=q1, scales=s1, block_rows=block_rows)            # tight rows, straight alone
+    assert torch.equal(q1.view(torch.uint8), q.contiguous().view(torch.uint8))
+    assert torch.equal(s1, s.contiguous().view(torch.uint8))
+    qT.view(torch.uint8).zero_()
+    g.gpd_quantize_blocks(x, qT=qT, scalesT=sT, block_rows=block_rows)          # transposed alone
+    check_cut(qT, sT, x.double().t(), 0.0, block_rows)
+
+
+def test_cut_extremes():
+    # per row: zeros, the boundary 448 and just above it, subnormals, the largest FP32 values, NaN, infinity
+    x = torch.zeros((7, 256), device="cuda")
+    x[1, 0], x[1, 128] = 448.0, 448.0 * (1 + 2.0 ** -23)
+    x[2, 5], x[2, 130] = 1e-40, 2.0 ** -149
+    x[3, 9] = torch.finfo(torch.float32).max
+    x[4, 17], x[4, 18] = float("nan"), 1.0
+    x[5, 140] = float("-inf")
+    x[6, 0], x[6, 1] = 1e30, 1e-30
+    q, s = g.new_fp8(7, 256)
+    g.gpd_quantize_blocks(x, q=q, scales=s)
+    b = s.contiguous().view(torch.uint8).cpu().tolist()
+    assert b[0] == [127, 127] and b[1] == [127, 128] and b[2] == [0, 0]
+    assert b[3] == [127 + 120, 127] and b[4] == [255, 127] and b[5] == [127, 255]
+    check_cut(q[:4], s[:4], x[:4].double(), 0.0)
+    assert float(q[6, 1].double()) == 0.0
+    sq, ss = g.new_fp8(7, 256, block_rows=128)
+    g.gpd_quantize_blocks(x, q=sq, scales=ss, block_rows=128)
+    assert ss.contiguous().view(torch.uint8).cpu().tolist() == [[255, 255]]
+    for shape in ((0, 5), (5, 0)):                                              # nothing to cut
+        e = torch.empty(shape, device="cuda")
+        q, s = g.new_fp8(*shape)
+        g.gpd_quantize_blocks(e, q=q, scales=s)
+
+
+def test_refusals():
+    x, w = torch.zeros((4, 256), device="cuda", dtype=BF), torch.ones(256, device="cuda", dtype=BF)
+    q, s = g.new_fp8(4, 256)
+    for kw in (dict(residual=x.float()), dict(residual=x[:3]), dict(q=q), dict(q=q, scales=s[:, :1]), dict(y=x.cpu()),
+               dict(rstd=torch.empty(3, device="cuda")), dict(y=x.t()), dict(q=x, scales=s),
+               dict(residual=torch.zeros((1, 256), device="cuda", dtype=BF).expand(4, 256))):
+        with pytest.raises(ValueError):
+            g.gpd_rmsnorm_quant(x, w, 1e-5, **kw)
+    with pytest.raises(ValueError):
+        g.gpd_rmsnorm_quant(x, w.to(HF), 1e-5, y=x)
+    with pytest.raises(ValueError):
+        g.gpd_rmsnorm_quant(x.cpu(), w.cpu(), 1e-5)
+    with pytest.raises(g.GpdError) as e:
+        g.gpd_rmsnorm_backward(x, x, w, torch.ones(4, device="cuda"), x.clone(), torch.empty(256, device="cuda"),
+                               torch.empty(4 * 256 - 1, device="cuda"))
+    assert e.value.status == g.GPD_ERR_WORKSPACE
+    for kw in (dict(), dict(q=q), dict(q=q, scales=s, qT=g.new_fp8(256, 4, E5)[0], scalesT=g.new_fp8(256, 4)[1]),
+               dict(q=q, scales=s, block_rows=64)):
+        with pytest.raises(ValueError):
+            g.gpd_quantize_blocks(x, **kw)
+    L, p = g.lib, x.data_ptr()
+    assert L.gpd_rmsnorm_quant(3, p, 256, None, 0, 3, p, 1e-5, None, 0, None, 0, 3, None, 0, None, 0, None, 4, 256, None) == g.GPD_ERR_ARG
+    assert L.gpd_rmsnorm_quant(1, p, 255, None, 0, 1, p, 1e-5, None, 0, None, 0, 3, None, 0, None, 0, None, 4, 256, None) == g.GPD_ERR_SHAPE
+    assert L.gpd_rmsnorm_quant(1, p, 256, None, 0, 1, p, 1e-5, None, 0, None, 0, 3, None, 0, None, 0, None, 4, 0, None) == g.GPD_ERR_SHAPE
+    assert L.gpd_rmsnorm_quant(1, None, 256, None, 0, 1, p, 1e-5, None, 0, None, 0, 3, None, 0, None, 0, None, 4, 256, None) == g.GPD_ERR_ARG
+    assert L.gpd_quantize_blocks(1, p, 256, 1, 1, p, 256, p, 2, None, 0, None, 0, 4, 256, None) == g.GPD_ERR_ARG
+    assert L.gpd_quantize_blocks(1, p, 256, 3, 1, p, 256, p, 1, None, 0, None, 0, 4, 256, None) == g.GPD_ERR_SHAPE
