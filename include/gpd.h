@@ -472,6 +472,20 @@ gpd_status gpd_quantize_blocks(gpd_dtype type, const void* src_dev, int64_t ld, 
                                void* q_dev, int64_t ldq, uint8_t* scales_dev, int64_t lds, void* qT_dev, int64_t ldqT,
                                uint8_t* scalesT_dev, int64_t ldsT, int64_t M, int64_t K, void* stream);
 
+/*
+ * gpd_gemm_fp8 - out (M x N) = A B^T (+ out if accumulate), both operands in 8 bits with block scales:
+ *   out[i][j] = sum_k scaleA[i / a_block_rows][k / 128] A[i][k] * scaleB[j / b_block_rows][k / 128] B[j][k]
+ * A: M x K, B: N x K, each e4m3 or e5m2; block_rows 1 (scales per row) or 128; out FP32, BF16 or FP16,
+ * rounded once.  Products are exact, sums FP32.  Forward product of a layer: A = X, B = W; gradient of X:
+ * A = Delta, B = W transposed; gradient of W: A = Delta transposed, B = X transposed (gpd_quantize_blocks
+ * writes both forms).  A_dev and B_dev start on 16-byte boundaries, lda and ldb are multiples of 16
+ * (GPD_ERR_ARG otherwise); scales may have any stride.  A bounded wait that expires shows in gpd_device_status.
+ */
+gpd_status gpd_gemm_fp8(gpd_dtype a_type, const void* A_dev, int64_t lda, const uint8_t* a_scales_dev, int64_t ldsa,
+                        int32_t a_block_rows, gpd_dtype b_type, const void* B_dev, int64_t ldb,
+                        const uint8_t* b_scales_dev, int64_t ldsb, int32_t b_block_rows, gpd_dtype out_type,
+                        void* out_dev, int64_t ldd, int64_t M, int64_t N, int64_t K, int32_t accumulate, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

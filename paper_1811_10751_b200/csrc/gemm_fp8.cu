@@ -1,0 +1,572 @@
+// 8-bit matrix product with a power-of-two scale for each block of 128 along the contraction:
+//
+//   D[i][j] = sum_k 2^(ea[i][k/128] + eb[j][k/128]) A[i][k] B[j][k]   (+ D[i][j])
+//
+// A and B are rows of e4m3 or e5m2 numbers, contracted along the rows (both K-major).  The scales go to
+// the tensor cores as they are: tcgen05.mma.kind::mxf8f6f4 multiplies each row's 32 products of one
+// instruction by 2^(ea + eb), so a block of 128 is four instructions that name the same scale byte, and
+// scales per row, per 1 x 128 and per 128 x 128 block cost the same.
+//
+// One CTA computes 128 x BN output tiles.  Warp 0: one lane issues the TMA copies of the operands (k-blocks
+// of 128 bytes per row under the 128-byte swizzle, a ring that runs on across tiles).  Warp 2 gathers the
+// scales: a word holds one row's scales of four k-blocks; the words of 128 rows in the order tcgen05.cp
+// wants (lane i: rows i, i + 32, i + 64, i + 96) are one 16-byte store per lane.  Warp 1: one lane copies
+// them to tensor memory and issues the products.  Warps 4..11 read the accumulators back, two sets of
+// which alternate, and store.
+//
+// Accumulation.  tcgen05.mma adds into its FP32 accumulator with truncation.  16-bit results take one chain
+// over the whole contraction: the bias (about 2^-25 of the sum per instruction, 8e-6 at K = 8192) is far
+// below their own rounding.  FP32 results cut the chain every four k-blocks (16 instructions) and add the
+// pieces in registers, rounded to nearest.
+//
+// Few tiles (short A and B, long K): the CTAs of a cluster take a part of the contraction each; the parts
+// meet through distributed shared memory and are added in the order of the parts.
+//
+// Every mbarrier wait is bounded; on expiry the CTA raises a status word (gpd_device_status), drains its
+// copies, frees its tensor memory and returns.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "gemm_common.h"
+#include "lm_common.h"
+#include "tc_common.h"
+
+namespace gpd {
+
+namespace {
+
+using tc::mbar_arrive;
+using tc::mbar_expect_tx;
+using tc::mbar_init;
+using tc::mbar_try_wait;
+using tc::smem_u32;
+using tc::umma_commit;
+
+constexpr int BM = 128, BK = 128, UMMA_K = 32;
+constexpr int kEpiWarps = 8, kThreads = 128 + 32 * kEpiWarps;
+constexpr int kSfSlots = 2;                            // groups of four k-blocks whose scales are in flight
+__host__ __device__ constexpr int stage_bytes(int bn) { return (BM + bn) * BK; }
+__host__ __device__ constexpr int sfb_blocks(int bn) { return bn > 128 ? 2 : 1; }
+__host__ __device__ constexpr int sf_bytes(int bn) { return 512 * (1 + sfb_blocks(bn)); }
+__host__ __device__ constexpr int stages(int bn) {
+    const int n = (232448 - 1024 - 512 - kSfSlots * sf_bytes(bn)) / stage_bytes(bn);
+    return n > 10 ? 10 : n;
+}
+__host__ __device__ constexpr int smem_bytes(int bn) { return 1024 + stages(bn) * stage_bytes(bn) + kSfSlots * sf_bytes(bn); }
+__host__ __device__ constexpr int tmem_need(int bn) { return 2 * bn + kSfSlots * 4 * (1 + sfb_blocks(bn)); }
+__host__ __device__ constexpr int tmem_cols(int bn) {
+    return tmem_need(bn) <= 64 ? 64 : tmem_need(bn) <= 128 ? 128 : tmem_need(bn) <= 256 ? 256 : 512;
+}
+
+__device__ int g_fp8_status = 0;                       // GPD_ERR_TIMEOUT if a bounded wait expired
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    return tc::mbar_wait(bar, parity, abort_flag, &g_fp8_status);
+}
+
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1) : "memory");
+}
+// K-major tile with rows of 128 bytes under the 128-byte swizzle: 8-row groups 1024 bytes apart
+// (descriptor version 1, layout type 2).
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+// 32 rows of 16 bytes without swizzle: 8-row groups 128 bytes apart
+__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void umma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                        uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// FP32 accumulator, both operands K-major, M = 128, N = n, scales e8m0; types 0 = e4m3, 1 = e5m2; `sf` = byte of
+// the scale words that this instruction uses
+__device__ __forceinline__ uint32_t idesc_mx(int n, int a_type, int b_type, int sf) {
+    return ((uint32_t)sf << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
+           ((uint32_t)(BM >> 4) << 24) | ((uint32_t)sf << 29);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t* r, uint32_t taddr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+    uint32_t a;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+
+struct ScaleRows {
+    const uint8_t* p;
+    int64_t ld, rows;                                  // rows of the operand
+    int shift;                                         // log2 of the operand rows that share a scale row
+    bool words;                                        // every row starts on a 4-byte boundary
+};
+struct Fp8Params {
+    ScaleRows sa, sb;
+    void* out;
+    int64_t ldd, M, N;                                 // rows of A, rows of B
+    int kb, a_type, b_type, accumulate;
+    bool vec;                                          // 16-byte stores into the rows of out
+    int tiles_m, tiles_n, splits;
+};
+
+// Scales of the k-blocks 4 g .. 4 g + 3 of one operand row.  Rows and k-blocks that do not exist give any
+// valid scale: their products are zero or not stored.
+__device__ __forceinline__ uint32_t scale_word(const ScaleRows& s, int64_t row, int g, int kb) {
+    if (row >= s.rows) return 0x7f7f7f7fu;
+    const uint8_t* p = s.p + (row >> s.shift) * s.ld + 4 * g;
+    if (s.words && 4 * g + 4 <= kb) return __ldg(reinterpret_cast<const uint32_t*>(p));
+    uint32_t w = 0x7f7f7f7fu;
+    for (int i = 0; i < 4 && 4 * g + i < kb; ++i) w = (w & ~(0xffu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
+    return w;
+}
+
+// Tile order: columns of up to 16 row tiles, so that the tiles in flight share operands in L2.
+__device__ __forceinline__ void tile_origin(const Fp8Params& p, int tile, int bn, int64_t& m0, int64_t& n0) {
+    const int band = 16 * p.tiles_n, b = tile / band, r = tile - b * band;
+    const int h = min(16, p.tiles_m - 16 * b);
+    m0 = (int64_t)(16 * b + r % h) * BM;
+    n0 = (int64_t)(r / h) * bn;
+}
+
+// TRANS: D[i][j] is stored at out[j][i] (the caller swapped the operands); consecutive lanes hold consecutive i.
+template <int BN, typename T, bool TRANS>
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Fp8Params prm) {
+    constexpr int STAGES = stages(BN), STAGE = stage_bytes(BN), SFB = sfb_blocks(BN);
+    constexpr bool CHUNKED = sizeof(T) == 4;           // FP32 results: chains of four k-blocks
+    constexpr int CW = BN >= 64 ? BN / 2 : BN;         // columns of an epilogue warp (two warps share a lane quarter)
+    constexpr int COLS = tmem_cols(BN);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* sf_smem = smem + STAGES * STAGE;
+    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], sf_full[kSfSlots], sf_empty[kSfSlots],
+        acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&full_bar[s], 1);
+            mbar_init(&empty_bar[s], 1);
+        }
+        for (int s = 0; s < kSfSlots; ++s) {
+            mbar_init(&sf_full[s], 1);
+            mbar_init(&sf_empty[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&acc_full[s], 1);
+            mbar_init(&acc_empty[s], kEpiWarps);
+        }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot, tmem_sf = tmem + 2 * BN;
+    volatile int* abort_p = &abort_flag;
+
+    // this CTA's part of the contraction (whole k-blocks) and its tiles
+    const int S = prm.splits, rank = S > 1 ? (int)blockIdx.x % S : 0;
+    const int kb0 = (int)((int64_t)prm.kb * rank / S), kb1 = (int)((int64_t)prm.kb * (rank + 1) / S);
+    const int tile0 = (int)blockIdx.x / S, tile_step = (int)gridDim.x / S, tiles = prm.tiles_m * prm.tiles_n;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+                int64_t m0, n0;
+                tile_origin(prm, tile, BN, m0, n0);
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (!mbar_wait(&empty_bar[s], ((it / STAGES) & 1) ^ 1, abort_p)) { ok = false; break; }
+                    mbar_expect_tx(&full_bar[s], STAGE);
+                    tma_load_2d(smem + s * STAGE, &tmA, kb * BK, (int)m0, &full_bar[s]);
+                    tma_load_2d(smem + s * STAGE + BM * BK, &tmB, kb * BK, (int)n0, &full_bar[s]);
+                }
+            }
+            if (*abort_p) {                            // copies still in flight land before the CTA exits
+                for (int j = it > STAGES ? it - STAGES : 0; j < it; ++j) {
+                    const long long t0 = clock64();
+                    while (!mbar_try_wait(&full_bar[j % STAGES], (j / STAGES) & 1) && clock64() - t0 < tc::kWaitCycles) {}
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int it = 0, gi = 0, ac = 0;                // k-blocks, scale groups and accumulator chains so far
+            bool ok = true;
+            for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const bool new_group = kb == kb0 || (kb & 3) == 0;
+                    const bool new_chain = kb == kb0 || (CHUNKED && (kb & 3) == 0);
+                    if (new_chain && !mbar_wait(&acc_empty[ac & 1], ((ac >> 1) & 1) ^ 1, abort_p)) { ok = false; break; }
+                    if (new_group) {
+                        // the slot's previous scales are no longer in use: the gathering warp waited for that
+                        const int s = gi % kSfSlots;
+                        if (!mbar_wait(&sf_full[s], (gi / kSfSlots) & 1, abort_p)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t src = smem_u32(sf_smem + s * sf_bytes(BN)), dst = tmem_sf + s * 4 * (1 + SFB);
+#pragma unroll
+                        for (int b = 0; b < 1 + SFB; ++b) scales_to_tmem(dst + 4 * b, desc_scales(src + 512 * b));
+                    }
+                    const int s = it % STAGES;
+                    if (!mbar_wait(&full_bar[s], (it / STAGES) & 1, abort_p)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t a0 = smem_u32(smem + s * STAGE), b0 = a0 + BM * BK;
+                    const uint32_t sf = tmem_sf + (gi % kSfSlots) * 4 * (1 + SFB);
+                    const uint32_t idesc = idesc_mx(BN, prm.a_type, prm.b_type, kb & 3);
+#pragma unroll
+                    for (int k = 0; k < BK / UMMA_K; ++k)
+                        umma_mx(tmem + (ac & 1) * BN, desc_sw128(a0 + k * UMMA_K), desc_sw128(b0 + k * UMMA_K), idesc, sf,
+                                sf + 4, !(new_chain && k == 0));
+                    umma_commit(&empty_bar[s]);
+                    const bool last = kb + 1 == kb1;
+                    if (last || (kb & 3) == 3) {
+                        umma_commit(&sf_empty[gi % kSfSlots]);
+                        ++gi;
+                    }
+                    if (last || (CHUNKED && (kb & 3) == 3)) {
+                        umma_commit(&acc_full[ac & 1]);
+                        ++ac;
+                    }
+                }
+            }
+        }
+    } else if (warp == 2) {
+        int gi = 0;
+        bool ok = true;
+        for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+            int64_t m0, n0;
+            tile_origin(prm, tile, BN, m0, n0);
+            for (int g = kb0 >> 2; 4 * g < kb1; ++g, ++gi) {
+                uint4 v[1 + SFB];
+#pragma unroll
+                for (int b = 0; b < 1 + SFB; ++b) {
+                    const ScaleRows& s = b == 0 ? prm.sa : prm.sb;
+                    const int64_t r = (b == 0 ? m0 : n0 + 128 * (b - 1)) + lane;
+                    v[b] = make_uint4(scale_word(s, r, g, prm.kb), scale_word(s, r + 32, g, prm.kb),
+                                      scale_word(s, r + 64, g, prm.kb), scale_word(s, r + 96, g, prm.kb));
+                }
+                const int s = gi % kSfSlots;
+                ok = mbar_wait(&sf_empty[s], ((gi / kSfSlots) & 1) ^ 1, abort_p);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+#pragma unroll
+                for (int b = 0; b < 1 + SFB; ++b)
+                    *reinterpret_cast<uint4*>(sf_smem + s * sf_bytes(BN) + 512 * b + 16 * lane) = v[b];
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sf_full[s]);
+            }
+        }
+    } else if (warp >= 4) {
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        const int c0 = BN >= 64 ? half * CW : 0;
+        const bool idle = BN < 64 && half == 1;        // narrow tiles: four warps do it all
+        const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        float acc[CHUNKED ? CW : 1];
+        int ac = 0;
+        bool ok = true;
+        T* out = static_cast<T*>(prm.out);
+        float* part = reinterpret_cast<float*>(smem);  // split contraction: [BN][128], over the operand ring
+        for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+            int64_t m0, n0;
+            tile_origin(prm, tile, BN, m0, n0);
+            const int64_t row = m0 + q * 32 + lane;
+            // w columns from column c of the tile, in f
+            auto put = [&](int c, const float* f, int w) {
+                if (S > 1) {
+#pragma unroll
+                    for (int j = 0; j < w; ++j) part[(c + j) * BM + q * 32 + lane] = f[j];
+                    return;
+                }
+                if (row >= prm.M) return;
+                if (TRANS) {
+#pragma unroll
+                    for (int j = 0; j < w; ++j) {
+                        if (n0 + c + j >= prm.N) break;
+                        T* o = out + (n0 + c + j) * prm.ldd + row;
+                        *o = lm::from_f32<T>(prm.accumulate ? f[j] + lm::to_f32(*o) : f[j]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < w; j += 8) {
+                        const int64_t n = prm.N - (n0 + c + j);
+                        if (n <= 0) break;
+                        T* o = out + row * prm.ldd + n0 + c + j;
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = f[j + i];
+                        if (prm.accumulate) {
+                            float old[8];
+                            if (prm.vec) lm::unpack8<T>(lm::load8<T, true>(o, n), old);
+                            else lm::unpack8<T>(lm::load8<T, false>(o, n), old);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] += old[i];
+                        }
+                        if (prm.vec) lm::store8<T, true>(o, v, n);
+                        else lm::store8<T, false>(o, v, n);
+                    }
+                }
+            };
+            auto release = [&](int set) {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[set]);
+            };
+            auto ready = [&](int set, int n) {
+                const bool r = mbar_wait(&acc_full[set], (n >> 1) & 1, abort_p);
+                ok = __all_sync(0xffffffffu, r);       // tcgen05.ld is warp-collective: all lanes or none
+                if (ok) asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            };
+            if constexpr (CHUNKED) {
+#pragma unroll
+                for (int j = 0; j < CW; ++j) acc[j] = 0.f;
+                for (int g = kb0 >> 2; 4 * g < kb1 && ok; ++g, ++ac) {
+                    ready(ac & 1, ac);
+                    if (!ok) break;
+                    const uint32_t base = tmem + (ac & 1) * BN + lane_base + c0;
+                    if (!idle) {
+#pragma unroll
+                        for (int c = 0; c < CW; c += 16) {
+                            uint32_t r[16];
+                            tmem_ld16(r, base + c);
+                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) acc[c + j] += __uint_as_float(r[j]);
+                        }
+                    }
+                    release(ac & 1);
+                }
+                if (ok && !idle) {
+#pragma unroll
+                    for (int c = 0; c < CW; c += 16) put(c0 + c, acc + c, 16);
+                }
+            } else {
+                ready(ac & 1, ac);
+                if (!ok) break;
+                const uint32_t base = tmem + (ac & 1) * BN + lane_base + c0;
+                if (!idle) {
+#pragma unroll
+                    for (int c = 0; c < CW; c += 16) {
+                        uint32_t r[16];
+                        tmem_ld16(r, base + c);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        float f[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(r[j]);
+                        put(c0 + c, f, 16);
+                    }
+                }
+                release(ac & 1);
+                ++ac;
+            }
+        }
+    }
+    __syncwarp();
+    if (S > 1) {
+        // one tile per cluster: each CTA adds up its share of the tile's columns over all parts
+        cluster_sync();
+        int64_t m0, n0;
+        tile_origin(prm, tile0, BN, m0, n0);
+        const int j0 = BN * rank / S, j1 = BN * (rank + 1) / S;
+        const uint32_t base = smem_u32(smem);
+        T* out = static_cast<T*>(prm.out);
+        if (!abort_flag) {
+            for (int e = j0 * BM + threadIdx.x; e < j1 * BM; e += kThreads) {
+                const int64_t row = m0 + (e & (BM - 1)), col = n0 + e / BM;
+                if (row >= prm.M || col >= prm.N) continue;
+                float v = 0.f;
+                for (int s = 0; s < S; ++s) v += ld_cluster(base + 4 * e, s);
+                T* o = TRANS ? out + col * prm.ldd + row : out + row * prm.ldd + col;
+                *o = lm::from_f32<T>(prm.accumulate ? v + lm::to_f32(*o) : v);
+            }
+        }
+        cluster_sync();                                // shared memory of all parts stays until all have read it
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+bool make_map_2d(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    tc::EncodeTiledFn fn = tc::encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld};
+    cuuint32_t box[2] = {BK, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Operand {
+    const void* q;
+    int64_t ld, rows;
+    int type;
+    ScaleRows s;
+};
+struct Config { int bn, splits; bool trans; };
+
+template <int BN, typename T, bool TRANS>
+gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, int splits, cudaStream_t st) {
+    CUtensorMap tmA, tmB;
+    if (!make_map_2d(&tmA, a.q, a.rows, K, a.ld, BM) || !make_map_2d(&tmB, b.q, b.rows, K, b.ld, BN)) return GPD_ERR_CUDA;
+    auto kernel = gemm_fp8_kernel<BN, T, TRANS>;
+    constexpr int smem = smem_bytes(BN);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
+    prm.sa = a.s;
+    prm.sb = b.s;
+    prm.M = a.rows;
+    prm.N = b.rows;
+    prm.a_type = a.type == GPD_DT_E5M2;
+    prm.b_type = b.type == GPD_DT_E5M2;
+    prm.tiles_m = (int)((a.rows + BM - 1) / BM);
+    prm.tiles_n = (int)((b.rows + BN - 1) / BN);
+    prm.splits = splits;
+    const int64_t tiles = (int64_t)prm.tiles_m * prm.tiles_n;
+    if (tiles > 0x3fffffff) return GPD_ERR_SHAPE;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : std::min<int64_t>(tiles, sm_count())));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = splits > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, tmA, tmB, prm) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_ok();
+}
+
+// Tile width, orientation and split by the smallest estimated time.  A k-block of a 128 x BN tile takes the
+// tensor cores 2 BN cycles and its copies (128 + BN) * 128 bytes at about 48 bytes per cycle and SM; a tile
+// costs about 1500 cycles besides, a split tile twice that.
+Config choose(int64_t M, int64_t N, int kb, bool f32) {
+    static const int kWidths[] = {16, 32, 64, 128, 192, 224};
+    Config best{128, 1, true};
+    double best_t = 1e300;
+    const int sms = sm_count();
+    for (int t = 0; t < 2; ++t) {
+        const int64_t rows = t ? N : M, cols = t ? M : N;
+        for (int bn : kWidths) {
+            if (bn == 224 && f32) continue;            // FP32 results keep a tile's row in registers
+            const int64_t tiles = ((rows + BM - 1) / BM) * ((cols + bn - 1) / bn);
+            for (int s = 1; s <= 8; s *= 2) {
+                if (s > 1 && (s > kb || tiles * s > 2 * sms)) continue;
+                const double waves = (double)((tiles * s + sms - 1) / sms);
+                const double block = std::max(2.0 * bn, (BM + bn) * 128 / 48.0);
+                const double time = waves * (((kb + s - 1) / s) * block + (s > 1 ? 3000.0 : 1500.0));
+                if (time < best_t * 0.999) {
+                    best_t = time;
+                    best = Config{bn, s, t == 1};
+                }
+            }
+        }
+    }
+    return best;
+}
+
+template <typename T, bool TRANS>
+gpd_status launch_bn(const Operand& a, const Operand& b, const Fp8Params& prm, int64_t K, const Config& c, cudaStream_t st) {
+    switch (c.bn) {
+        case 16: return launch<16, T, TRANS>(a, b, prm, K, c.splits, st);
+        case 32: return launch<32, T, TRANS>(a, b, prm, K, c.splits, st);
+        case 64: return launch<64, T, TRANS>(a, b, prm, K, c.splits, st);
+        case 128: return launch<128, T, TRANS>(a, b, prm, K, c.splits, st);
+        case 192: return launch<192, T, TRANS>(a, b, prm, K, c.splits, st);
+        default: break;
+    }
+    if constexpr (sizeof(T) == 2) return launch<224, T, TRANS>(a, b, prm, K, c.splits, st);
+    return GPD_ERR_UNSUPPORTED;
+}
+template <typename T>
+gpd_status launch_type(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, cudaStream_t st) {
+    const Config c = choose(a.rows, b.rows, prm.kb, sizeof(T) == 4);
+    prm.vec = lm::rows_aligned(prm.out, prm.ldd, sizeof(T));
+    return c.trans ? launch_bn<T, true>(b, a, prm, K, c, st) : launch_bn<T, false>(a, b, prm, K, c, st);
+}
+
+}  // namespace
+
+int fp8_device_status_fetch_and_clear() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_fp8_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
+    if (v != 0) cudaMemcpyToSymbol(g_fp8_status, &zero, sizeof(int));
+    return v;
+}
+
+}  // namespace gpd
+
+using namespace gpd;
+
+extern "C" gpd_status gpd_gemm_fp8(gpd_dtype a_type, const void* A_dev, int64_t lda, const uint8_t* a_scales_dev, int64_t ldsa,
+                                   int32_t a_block_rows, gpd_dtype b_type, const void* B_dev, int64_t ldb,
+                                   const uint8_t* b_scales_dev, int64_t ldsb, int32_t b_block_rows, gpd_dtype out_type,
+                                   void* out_dev, int64_t ldd, int64_t M, int64_t N, int64_t K, int32_t accumulate,
+                                   void* stream) {
+    if (!lm::is_fp8_type(a_type) || !lm::is_fp8_type(b_type) || !lm::is_float_type(out_type)) return GPD_ERR_ARG;
+    if ((a_block_rows != 1 && a_block_rows != lm::kBlock) || (b_block_rows != 1 && b_block_rows != lm::kBlock)) return GPD_ERR_ARG;
+    const int64_t limit = 0x7fffffff - 256;            // row and column coordinates of a copy are 32-bit
+    if (M < 0 || N < 0 || K < 0 || M > limit || N > limit || K > limit) return GPD_ERR_SHAPE;
+    if (M == 0 || N == 0) return GPD_OK;               // empty buffers may have no address
+    if (!out_dev) return GPD_ERR_ARG;
+    if (ldd < N) return GPD_ERR_SHAPE;
+    cudaStream_t st = as_stream(stream);
+    if (K == 0) {
+        if (accumulate) return GPD_OK;
+        const int e = lm::dtype_size(out_type);
+        return cuda_ok(cudaMemset2DAsync(out_dev, (size_t)(ldd * e), 0, (size_t)(N * e), (size_t)M, st));
+    }
+    if (!A_dev || !B_dev || !a_scales_dev || !b_scales_dev) return GPD_ERR_ARG;
+    const int64_t kb = (K + BK - 1) / BK;
+    if (lda < K || ldb < K || ldsa < kb || ldsb < kb) return GPD_ERR_SHAPE;
+    if (!lm::aligned(A_dev, 16) || !lm::aligned(B_dev, 16) || lda % 16 || ldb % 16) return GPD_ERR_ARG;
+    auto scale_rows = [&](const uint8_t* p, int64_t ld, int64_t rows, int br) {
+        return ScaleRows{p, ld, rows, br == 1 ? 0 : 7, lm::aligned(p, 4) && ld % 4 == 0};
+    };
+    const Operand a{A_dev, lda, M, a_type, scale_rows(a_scales_dev, ldsa, M, a_block_rows)};
+    const Operand b{B_dev, ldb, N, b_type, scale_rows(b_scales_dev, ldsb, N, b_block_rows)};
+    Fp8Params prm{};
+    prm.out = out_dev;
+    prm.ldd = ldd;
+    prm.kb = (int)kb;
+    prm.accumulate = accumulate != 0;
+    if (out_type == GPD_DT_F32) return launch_type<float>(a, b, prm, K, st);
+    if (out_type == GPD_DT_BF16) return launch_type<__nv_bfloat16>(a, b, prm, K, st);
+    return launch_type<__half>(a, b, prm, K, st);
+}

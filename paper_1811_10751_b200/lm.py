@@ -31,7 +31,9 @@ lib.gpd_rmsnorm_quant.argtypes = [_e, _vp, _i64, _vp, _i64, _e, _vp, _f, _vp, _i
 lib.gpd_rmsnorm_backward.argtypes = [_e, _vp, _i64, _vp, _i64, _e, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _vp,
                                      _i64, _vp]
 lib.gpd_quantize_blocks.argtypes = [_e, _vp, _i64, _e, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp]
-_NAMES = ["gpd_rmsnorm_quant", "gpd_rmsnorm_backward", "gpd_quantize_blocks"]
+lib.gpd_gemm_fp8.argtypes = [_e, _vp, _i64, _vp, _i64, _i32, _e, _vp, _i64, _vp, _i64, _i32, _e, _vp, _i64, _i64, _i64,
+                             _i64, _i32, _vp]
+_NAMES = ["gpd_rmsnorm_quant", "gpd_rmsnorm_backward", "gpd_quantize_blocks", "gpd_gemm_fp8"]
 for _name in _NAMES:
     getattr(lib, _name).restype = C.c_int
 EXPORTED += _NAMES
@@ -161,3 +163,32 @@ def gpd_quantize_blocks(src, q=None, scales=None, qT=None, scalesT=None, block_r
     pts, ldts = _mat("scalesT", scalesT, dev, _SCALES, _blocks(K, block_rows), _blocks(M))
     _check(lib.gpd_quantize_blocks(_DT[src.dtype], ps, ld, _DT[(qT if q is None else q).dtype], block_rows, pq, ldq, pqs,
                                    lds, pt, ldt, pts, ldts, M, K, st), "gpd_quantize_blocks")
+
+
+def _scale_rows(name: str, s, rows: int) -> int:
+    """Operand rows that share a row of scales: 1 or 128, told from the number of scale rows."""
+    if s.dim() == 2 and s.shape[0] == rows:
+        return 1
+    if s.dim() == 2 and s.shape[0] == _blocks(rows):
+        return _BLOCK
+    raise ValueError(f"{name}: {rows} or {_blocks(rows)} rows of scales expected, got shape {tuple(s.shape)}")
+
+
+def gpd_gemm_fp8(A, a_scales, B, b_scales, out, accumulate: bool = False, stream=None):
+    """out (M x N) = A (M x K) B (N x K)^T with block scales; one scale row per operand row or per 128 of them."""
+    M, K = _rank2("A", A)
+    N = _rank2("B", B)[0]
+    dev = A.device
+    st = _where(dev, stream)
+    pa, lda = _mat("A", A, dev, _FP8, M, K)
+    pb, ldb = _mat("B", B, dev, _FP8, N, K)
+    ra, rb, kb = _scale_rows("a_scales", a_scales, M), _scale_rows("b_scales", b_scales, N), _blocks(K)
+    psa, ldsa = _mat("a_scales", a_scales, dev, _SCALES, a_scales.shape[0], kb)
+    psb, ldsb = _mat("b_scales", b_scales, dev, _SCALES, b_scales.shape[0], kb)
+    po, ldd = _mat("out", out, dev, _FLOATS, M, N)
+    if M == 1 and lda % 16:
+        lda = _blocks(lda, 16) * 16                    # a single row has no stride
+    if N == 1 and ldb % 16:
+        ldb = _blocks(ldb, 16) * 16
+    _check(lib.gpd_gemm_fp8(_DT[A.dtype], pa, lda, psa, ldsa, ra, _DT[B.dtype], pb, ldb, psb, ldsb, rb, _DT[out.dtype], po,
+                            ldd, M, N, K, accumulate, st), "gpd_gemm_fp8")
