@@ -486,6 +486,50 @@ gpd_status gpd_gemm_fp8(gpd_dtype a_type, const void* A_dev, int64_t lda, const 
                         const uint8_t* b_scales_dev, int64_t ldsb, int32_t b_block_rows, gpd_dtype out_type,
                         void* out_dev, int64_t ldd, int64_t M, int64_t N, int64_t K, int32_t accumulate, void* stream);
 
+#define GPD_LOGPROBS_MAX_TOP 32    /* alternatives per row of gpd_token_logprobs */
+#define GPD_LOGPROBS_MAX_TOKENS 64 /* given tokens per row */
+#define GPD_DISTILL_MAX_TOP 1024   /* teacher's entries per row of gpd_distill_topk */
+
+/*
+ * gpd_token_logprobs - for T rows of V logits x, with z = x / temperature and lse = log sum_v exp(z_v):
+ *   logprobs[t][g] = z[tokens[t][g]] - lse   for G given tokens per row (tokens [T][G], index_bytes 4 or 8);
+ *                    0 for a negative token (ignored), NaN for one >= V
+ *   lse[t];  entropy[t] = -sum_v p_v log p_v (optional);  top_ids [T][K] (int32) and top_logprobs [T][K]
+ *   (optional): the K largest entries, equal ones in the order of their index, a NaN before all numbers.
+ * -inf logits are masked entries; a row of them alone has lse and log probabilities -inf, entropy 0.  A NaN or
+ * +inf in a row makes its lse, log probabilities and entropy NaN.  K <= V.
+ */
+gpd_status gpd_token_logprobs(gpd_dtype type, const void* logits_dev, int64_t ld, int32_t index_bytes,
+                              const void* tokens_dev, int32_t G, float temperature, float* logprobs_dev, float* lse_dev,
+                              float* entropy_dev, int32_t K, int32_t* top_ids_dev, float* top_logprobs_dev, int64_t T,
+                              int64_t V, void* stream);
+/*
+ * gpd_token_logprobs_backward - gradient with respect to the logits of what gpd_token_logprobs returned:
+ *   dlogits_v = (1/temperature) [ sum_g dlogprobs_g (1[v = token_g] - p_v) - dentropy p_v (log p_v + entropy) ]
+ * dlogprobs [T][G] or NULL, dentropy [T] or NULL (entropy is needed with it), lse and entropy from the forward
+ * call.  dlogits has the type of the logits and may be their buffer.  Tokens outside 0 .. V-1 have no gradient;
+ * rows of -inf alone get 0.
+ */
+gpd_status gpd_token_logprobs_backward(gpd_dtype type, const void* logits_dev, int64_t ld, int32_t index_bytes,
+                                       const void* tokens_dev, int32_t G, float temperature, const float* lse_dev,
+                                       const float* entropy_dev, const float* dlogprobs_dev, const float* dentropy_dev,
+                                       void* dlogits_dev, int64_t ldd, int64_t T, int64_t V, void* stream);
+/*
+ * gpd_distill_topk - distillation from a teacher's K top logits per row, loss and gradient in one call:
+ *   q = softmax(teacher_logits / temperature) over the row's list,  p = softmax(logits / temperature) over V
+ *   loss[t] = w_t temperature^2 sum_k q_k (log q_k - log p[id_k])
+ *   dlogits = d(sum_t loss[t]) / d logits = w_t temperature (p - q)       (optional; may be the logits' buffer)
+ * w_t = weights[t] (NULL: 1): mask and reduction, 1/T for a mean.  A row of weight 0 is not read: its loss and
+ * gradient are 0, whatever its logits.  Entries of the list with a negative id or a logit of -inf do not count; a
+ * list without any gives loss and gradient 0.  An id named twice has the sum of its q.  An id >= V or a NaN in
+ * the list makes the loss NaN; a row of -inf logits alone has loss inf and gradient 0.
+ */
+gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, int64_t ld, int32_t index_bytes,
+                            const void* teacher_ids_dev, int64_t ldi, gpd_dtype teacher_type,
+                            const void* teacher_logits_dev, int64_t ldt, int32_t K, const float* weights_dev,
+                            float temperature, float* loss_dev, void* dlogits_dev, int64_t ldd, int64_t T, int64_t V,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,12 +17,15 @@ from .binding import EXPORTED, _check, lib
 
 GPD_DT_F32, GPD_DT_BF16, GPD_DT_F16, GPD_DT_E4M3, GPD_DT_E5M2 = range(5)
 GPD_RMSNORM_MAX_PARTS = 512
+GPD_LOGPROBS_MAX_TOP, GPD_LOGPROBS_MAX_TOKENS, GPD_DISTILL_MAX_TOP = 32, 64, 1024
 _DT = {torch.float32: GPD_DT_F32, torch.bfloat16: GPD_DT_BF16, torch.float16: GPD_DT_F16,
        torch.float8_e4m3fn: GPD_DT_E4M3, torch.float8_e5m2: GPD_DT_E5M2}
 _FLOATS = (torch.float32, torch.bfloat16, torch.float16)
 _FP8 = (torch.float8_e4m3fn, torch.float8_e5m2)
 _SCALES = (torch.float8_e8m0fnu, torch.uint8)
 _F32 = (torch.float32,)
+_I32 = (torch.int32,)
+_INDEX = (torch.int32, torch.int64)
 _BLOCK = 128
 
 _vp, _i32, _i64, _f, _e = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_int
@@ -33,7 +36,13 @@ lib.gpd_rmsnorm_backward.argtypes = [_e, _vp, _i64, _vp, _i64, _e, _vp, _vp, _vp
 lib.gpd_quantize_blocks.argtypes = [_e, _vp, _i64, _e, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp]
 lib.gpd_gemm_fp8.argtypes = [_e, _vp, _i64, _vp, _i64, _i32, _e, _vp, _i64, _vp, _i64, _i32, _e, _vp, _i64, _i64, _i64,
                              _i64, _i32, _vp]
-_NAMES = ["gpd_rmsnorm_quant", "gpd_rmsnorm_backward", "gpd_quantize_blocks", "gpd_gemm_fp8"]
+lib.gpd_token_logprobs.argtypes = [_e, _vp, _i64, _i32, _vp, _i32, _f, _vp, _vp, _vp, _i32, _vp, _vp, _i64, _i64, _vp]
+lib.gpd_token_logprobs_backward.argtypes = [_e, _vp, _i64, _i32, _vp, _i32, _f, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64,
+                                            _vp]
+lib.gpd_distill_topk.argtypes = [_e, _vp, _i64, _i32, _vp, _i64, _e, _vp, _i64, _i32, _vp, _f, _vp, _vp, _i64, _i64, _i64,
+                                 _vp]
+_NAMES = ["gpd_rmsnorm_quant", "gpd_rmsnorm_backward", "gpd_quantize_blocks", "gpd_gemm_fp8", "gpd_token_logprobs",
+          "gpd_token_logprobs_backward", "gpd_distill_topk"]
 for _name in _NAMES:
     getattr(lib, _name).restype = C.c_int
 EXPORTED += _NAMES
@@ -192,3 +201,76 @@ def gpd_gemm_fp8(A, a_scales, B, b_scales, out, accumulate: bool = False, stream
         ldb = _blocks(ldb, 16) * 16
     _check(lib.gpd_gemm_fp8(_DT[A.dtype], pa, lda, psa, ldsa, ra, _DT[B.dtype], pb, ldb, psb, ldsb, rb, _DT[out.dtype], po,
                             ldd, M, N, K, accumulate, st), "gpd_gemm_fp8")
+
+
+def _per_row(name: str, t, device, dtypes, T: int, G: int):
+    """Pointer of a contiguous [T] (G = 1) or [T, G] tensor."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: tensor of {' or '.join(map(str, dtypes))} expected, got {t.dtype}")
+    if t.device != device or t.dim() not in (1, 2) or t.numel() != T * G or t.shape[0] != T or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous ({T}, {G}) tensor on {device} expected, got {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _tokens_per_row(tokens, T: int) -> int:
+    if tokens.dim() == 1:
+        return 1
+    if tokens.dim() == 2:
+        return tokens.shape[1]
+    raise ValueError(f"tokens: [T] or [T, G] expected, got shape {tuple(tokens.shape)}")
+
+
+def gpd_token_logprobs(logits, tokens, logprobs, lse, entropy=None, top_ids=None, top_logprobs=None,
+                       temperature: float = 1.0, stream=None):
+    """tokens, logprobs: [T] or [T, G]; top_ids (int32), top_logprobs: [T, K]."""
+    T, V = _rank2("logits", logits)
+    dev = logits.device
+    st = _where(dev, stream)
+    px, ld = _mat("logits", logits, dev, _FLOATS, T, V)
+    G = _tokens_per_row(tokens, T)
+    K = 0
+    if top_ids is not None:
+        K = _rank2("top_ids", top_ids)[1]
+    elif top_logprobs is not None:
+        raise ValueError("top_ids: needed with top_logprobs")
+    if lse is None:
+        raise ValueError("lse: needed")
+    _check(lib.gpd_token_logprobs(_DT[logits.dtype], px, ld, tokens.element_size(),
+                                  _per_row("tokens", tokens, dev, _INDEX, T, G), G, temperature,
+                                  _per_row("logprobs", logprobs, dev, _F32, T, G), _vec("lse", lse, dev, _F32, T),
+                                  _vec("entropy", entropy, dev, _F32, T), K, _per_row("top_ids", top_ids, dev, _I32, T, K),
+                                  _per_row("top_logprobs", top_logprobs, dev, _F32, T, K), T, V, st), "gpd_token_logprobs")
+
+
+def gpd_token_logprobs_backward(logits, tokens, lse, entropy, dlogprobs, dentropy, dlogits, temperature: float = 1.0,
+                                stream=None):
+    """dlogprobs, dentropy: upstream gradients, either may be None; entropy is needed with dentropy."""
+    T, V = _rank2("logits", logits)
+    dev = logits.device
+    st = _where(dev, stream)
+    px, ld = _mat("logits", logits, dev, _FLOATS, T, V)
+    pd, ldd = _mat("dlogits", dlogits, dev, (logits.dtype,), T, V)
+    G = _tokens_per_row(tokens, T)
+    _check(lib.gpd_token_logprobs_backward(_DT[logits.dtype], px, ld, tokens.element_size(),
+                                           _per_row("tokens", tokens, dev, _INDEX, T, G), G, temperature,
+                                           _vec("lse", lse, dev, _F32, T), _vec("entropy", entropy, dev, _F32, T),
+                                           _per_row("dlogprobs", dlogprobs, dev, _F32, T, G),
+                                           _vec("dentropy", dentropy, dev, _F32, T), pd, ldd, T, V, st),
+           "gpd_token_logprobs_backward")
+
+
+def gpd_distill_topk(logits, teacher_ids, teacher_logits, weights, loss, dlogits=None, temperature: float = 1.0, stream=None):
+    """teacher_ids, teacher_logits: [T, K]; weights: [T] or None; dlogits: None for the loss alone."""
+    T, V = _rank2("logits", logits)
+    K = _rank2("teacher_ids", teacher_ids)[1]
+    dev = logits.device
+    st = _where(dev, stream)
+    px, ld = _mat("logits", logits, dev, _FLOATS, T, V)
+    pi, ldi = _mat("teacher_ids", teacher_ids, dev, _INDEX, T, K)
+    pt, ldt = _mat("teacher_logits", teacher_logits, dev, _FLOATS, T, K)
+    pd, ldd = _mat("dlogits", dlogits, dev, (logits.dtype,), T, V)
+    _check(lib.gpd_distill_topk(_DT[logits.dtype], px, ld, teacher_ids.element_size(), pi, ldi, _DT[teacher_logits.dtype], pt,
+                                ldt, K, _vec("weights", weights, dev, _F32, T), temperature, _vec("loss", loss, dev, _F32, T),
+                                pd, ldd, T, V, st), "gpd_distill_topk")
