@@ -90,6 +90,16 @@ __device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&f)[8]) {
         f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
     }
 }
+// Elements 2 i and 2 i + 1 of eight.
+template <typename T>
+__device__ __forceinline__ float2 pair_of(const Raw8<T>& r, int i) {
+    if constexpr (sizeof(T) == 4) {
+        const uint4& h = i < 2 ? r.v : r.w;
+        return i & 1 ? make_float2(__uint_as_float(h.z), __uint_as_float(h.w)) : make_float2(__uint_as_float(h.x), __uint_as_float(h.y));
+    } else {
+        return unpack2(i == 0 ? r.v.x : i == 1 ? r.v.y : i == 2 ? r.v.z : r.v.w, T());
+    }
+}
 template <typename T, bool VEC>
 __device__ __forceinline__ void store8(T* p, const float (&f)[8], int64_t n) {
     if (VEC && n >= 8) {

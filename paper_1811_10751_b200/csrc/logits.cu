@@ -71,24 +71,30 @@ __device__ __forceinline__ void for_pieces(const T* row, int v0, int v1, F each)
     };
     if (threadIdx.x == 0 && a0 > v0) some(v0, a0 - v0);
     if (threadIdx.x == blockDim.x - 1 && v1 > a1) some(a1, v1 - a1);
+    // the next UNROLL pieces are on their way while the present ones are worked on
     const uint4* p = reinterpret_cast<const uint4*>(row + a0);
     const int step = blockDim.x;
+    uint4 next[UNROLL];
     int i = threadIdx.x;
-    for (; i + (UNROLL - 1) * step < pieces; i += UNROLL * step) {
+#pragma unroll
+    for (int j = 0; j < UNROLL; ++j)
+        if (i + j * step < pieces) next[j] = p[i + j * step];
+    while (i < pieces) {
         uint4 r[UNROLL];
 #pragma unroll
-        for (int j = 0; j < UNROLL; ++j) r[j] = p[i + j * step];
+        for (int j = 0; j < UNROLL; ++j) r[j] = next[j];
+        const int n = i + UNROLL * step;
 #pragma unroll
-        for (int j = 0; j < UNROLL; ++j) {
-            float f[N];
-            unpack(r[j], f);
-            each(a0 + (i + j * step) * N, f, N);
-        }
-    }
-    for (; i < pieces; i += step) {
-        float f[N];
-        unpack(p[i], f);
-        each(a0 + i * N, f, N);
+        for (int j = 0; j < UNROLL; ++j)
+            if (n + j * step < pieces) next[j] = p[n + j * step];
+#pragma unroll
+        for (int j = 0; j < UNROLL; ++j)
+            if (i + j * step < pieces) {
+                float f[N];
+                unpack(r[j], f);
+                each(a0 + (i + j * step) * N, f, N);
+            }
+        i = n;
     }
 }
 
@@ -285,7 +291,7 @@ struct LogprobArgs {
 };
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kMaxThreads) logprobs_kernel(const LogprobArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogprobArgs a) {
     __shared__ Stats scratch[32];
     __shared__ Stats part;
     __shared__ typename std::conditional<TOP, TopShared, int>::type top;
@@ -347,7 +353,7 @@ struct LogprobBwdArgs {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kMaxThreads) logprobs_backward_kernel(const LogprobBwdArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 2) logprobs_backward_kernel(const LogprobBwdArgs a) {
     __shared__ float g[kMaxTokens], x_at[kMaxTokens];
     __shared__ int at[kMaxTokens];
     constexpr int N = 16 / sizeof(T);
@@ -433,7 +439,7 @@ __device__ __forceinline__ float block_reduce(float v, bool maximum, float* scra
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kMaxThreads) distill_kernel(const DistillArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillArgs a) {
     __shared__ Stats scratch[32];
     __shared__ Stats part;
     __shared__ float q[kMaxTeacher], x_at[kMaxTeacher], red[32];
@@ -558,7 +564,9 @@ gpd_status launch_logprobs(LogprobArgs a, int64_t rows, cudaStream_t st) {
 }
 template <typename T>
 gpd_status launch_logprobs_backward(LogprobBwdArgs a, int64_t rows, cudaStream_t st) {
-    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>((a.V + 16383) / 16384, 1024));   // no sums: any cut will do
+    // no sums over the row, so any cut will do: enough CTAs for the GPU, each with 8192 entries or more
+    const int64_t wanted = (4 * sm_count() + rows - 1) / rows;
+    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>((a.V + 8191) / 8192, wanted));
     return launch_rows(logprobs_backward_kernel<T>, a, rows * a.parts, 1, row_threads(a.V / a.parts), st);
 }
 template <typename T>

@@ -26,11 +26,57 @@ struct CutArgs {
     int64_t M, K;
 };
 
-constexpr int kPitch = kBlock + 16;                    // bytes between transposed rows in shared memory (16-byte pieces stay aligned)
+// Byte offset of the 8-byte chunk `chunk` of transposed row `col` in shared memory.  The chunks of a row are
+// permuted by the row's column group, so that the sixteen lanes that write one chunk column, 1024 bytes
+// apart, fall on all banks.
+__device__ __forceinline__ int chunk_at(int col, int chunk) { return col * kBlock + ((chunk ^ (col >> 3)) & 15) * 8; }
+
+// Magnitudes order like their bits without the sign, in every type: maxima of 16-bit elements are taken two at a
+// time, and only the final ones become FP32 bits.
+template <typename T>
+struct Maxima {
+    uint32_t w[4];                                     // columns 2 i (low half) and 2 i + 1
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ uint32_t take(const Raw8<T>& r) {       // returns the row's maximum
+        const uint32_t a[4] = {r.v.x & 0x7fff7fffu, r.v.y & 0x7fff7fffu, r.v.z & 0x7fff7fffu, r.v.w & 0x7fff7fffu};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __vmaxu2(w[i], a[i]);
+        const uint32_t m = __vmaxu2(__vmaxu2(a[0], a[1]), __vmaxu2(a[2], a[3]));
+        return max(m & 0xffffu, m >> 16);
+    }
+    __device__ __forceinline__ uint32_t column(int j) const { return j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu; }
+};
+template <>
+struct Maxima<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ uint32_t take(const Raw8<float>& r) {
+        const uint32_t a[8] = {r.v.x, r.v.y, r.v.z, r.v.w, r.w.x, r.w.y, r.w.z, r.w.w};
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = a[i] & 0x7fffffffu;
+            w[i] = max(w[i], b);
+            m = max(m, b);
+        }
+        return m;
+    }
+    __device__ __forceinline__ uint32_t column(int j) const { return w[j]; }
+};
+// FP32 bits of a magnitude given by its own bits
+template <typename T> __device__ __forceinline__ uint32_t magnitude(uint32_t b);
+template <> __device__ __forceinline__ uint32_t magnitude<float>(uint32_t b) { return b; }
+template <> __device__ __forceinline__ uint32_t magnitude<__nv_bfloat16>(uint32_t b) { return b << 16; }
+template <> __device__ __forceinline__ uint32_t magnitude<__half>(uint32_t b) {
+    return __float_as_uint(__half2float(__ushort_as_half((unsigned short)b)));
+}
 
 template <typename T, int Q, bool SQUARE, bool VEC>
-__global__ void __launch_bounds__(256) cut_kernel(const CutArgs a, int tiles_k) {
-    __shared__ __align__(16) uint8_t tile[kBlock * kPitch];
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const CutArgs a, int tiles_k) {
+    __shared__ __align__(16) uint8_t tile[kBlock * kBlock];
     __shared__ uint32_t colmax[16][kBlock];
     const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
     const int64_t bm = blockIdx.x / tiles_k, bk = blockIdx.x % tiles_k;
@@ -42,27 +88,17 @@ __global__ void __launch_bounds__(256) cut_kernel(const CutArgs a, int tiles_k) 
     for (int i = 0; i < 8; ++i)
         raw[i] = r0 + i < a.M && nc > 0 ? load8<T, VEC>(static_cast<const T*>(a.src) + (r0 + i) * a.ld + c0, nc) : Raw8<T>{};
 
-    uint32_t cmax[8], rmax[8];
+    Maxima<T> cm;                                      // of the patch's columns
+    uint32_t rmax[8];                                  // of its rows
+    cm.clear();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) cmax[j] = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float f[8];
-        unpack8<T>(raw[i], f);
-        rmax[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t b = abs_bits(f[j]);
-            rmax[i] = max(rmax[i], b);
-            cmax[j] = max(cmax[j], b);
-        }
-    }
+    for (int i = 0; i < 8; ++i) rmax[i] = cm.take(raw[i]);
     uint32_t byte = 0;                                 // SQUARE: the tile's scale
     if (SQUARE) {
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = max(m, rmax[i]);
-        m = __reduce_max_sync(0xffffffffu, m);
+        m = __reduce_max_sync(0xffffffffu, magnitude<T>(m));
         if ((threadIdx.x & 31) == 0) colmax[0][threadIdx.x >> 5] = m;
         __syncthreads();
         m = 0;
@@ -75,13 +111,13 @@ __global__ void __launch_bounds__(256) cut_kernel(const CutArgs a, int tiles_k) 
         }
     } else if (a.qT) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) colmax[rg][8 * cg + j] = cmax[j];
+        for (int j = 0; j < 8; ++j) colmax[rg][8 * cg + j] = cm.column(j);
         __syncthreads();
         if (threadIdx.x < kBlock) {                    // thread = column
             uint32_t m = 0;
 #pragma unroll
             for (int g = 0; g < 16; ++g) m = max(m, colmax[g][threadIdx.x]);
-            const uint32_t b = scale_byte<Q>(m);
+            const uint32_t b = scale_byte<Q>(magnitude<T>(m));
             colmax[0][threadIdx.x] = b;                // only this thread reads row 0 of its column
             const int64_t c = bk * kBlock + threadIdx.x;
             if (c < a.K) a.sT[c * a.ldsT + bm] = (uint8_t)b;
@@ -97,7 +133,7 @@ __global__ void __launch_bounds__(256) cut_kernel(const CutArgs a, int tiles_k) 
                 uint32_t m = rmax[i];
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                b = scale_byte<Q>(m);
+                b = scale_byte<Q>(magnitude<T>(m));
                 if (cg == 0 && r0 + i < a.M) a.s[(r0 + i) * a.lds + bk] = (uint8_t)b;
             }
             if (r0 + i < a.M && nc > 0) {
@@ -114,21 +150,29 @@ __global__ void __launch_bounds__(256) cut_kernel(const CutArgs a, int tiles_k) 
         float inv[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) inv[j] = scale_inverse(SQUARE ? byte : colmax[0][8 * cg + j]);
-        float f[8][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) unpack8<T>(raw[i], f[i]);
+        for (int j = 0; j < 8; j += 2) {
+            float lo[8], hi[8];                        // columns j and j + 1 of the patch
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<uint2*>(tile + (8 * cg + j) * kPitch + 8 * rg) =
-                make_uint2(cvt_fp8x4<Q>(f[0][j] * inv[j], f[1][j] * inv[j], f[2][j] * inv[j], f[3][j] * inv[j]),
-                           cvt_fp8x4<Q>(f[4][j] * inv[j], f[5][j] * inv[j], f[6][j] * inv[j], f[7][j] * inv[j]));
+            for (int i = 0; i < 8; ++i) {
+                const float2 f = pair_of<T>(raw[i], j >> 1);
+                lo[i] = f.x * inv[j];
+                hi[i] = f.y * inv[j + 1];
+            }
+            *reinterpret_cast<uint2*>(tile + chunk_at(8 * cg + j, rg)) =
+                make_uint2(cvt_fp8x4<Q>(lo[0], lo[1], lo[2], lo[3]), cvt_fp8x4<Q>(lo[4], lo[5], lo[6], lo[7]));
+            *reinterpret_cast<uint2*>(tile + chunk_at(8 * cg + j + 1, rg)) =
+                make_uint2(cvt_fp8x4<Q>(hi[0], hi[1], hi[2], hi[3]), cvt_fp8x4<Q>(hi[4], hi[5], hi[6], hi[7]));
+        }
         __syncthreads();
 #pragma unroll
         for (int p = 0; p < 4; ++p) {                  // 32 transposed rows per pass, 8 lanes of 16 bytes each
             const int col = 32 * p + (threadIdx.x >> 3), piece = threadIdx.x & 7;
             const int64_t c = bk * kBlock + col, r = bm * kBlock + 16 * piece, n = a.M - r;
             if (c >= a.K || n <= 0) continue;
-            const uint4 v = *reinterpret_cast<const uint4*>(tile + col * kPitch + 16 * piece);
+            // chunks 2 piece and 2 piece + 1 stay neighbours, in exchanged order for odd column groups
+            uint4 v = *reinterpret_cast<const uint4*>(tile + (chunk_at(col, 2 * piece) & ~15));
+            if ((col >> 3) & 1) v = make_uint4(v.z, v.w, v.x, v.y);
             uint8_t* dst = a.qT + c * a.ldqT + r;
             if (VEC && n >= 16) {
                 *reinterpret_cast<uint4*>(dst) = v;

@@ -31,16 +31,16 @@ struct NormArgs {
     float eps;
 };
 
-// Sum over the G threads of a row; every thread gets it.  G = 32: a warp of its own, no barrier.
-__device__ __forceinline__ float row_sum(float v, int G, float* scratch) {
+// Sum over the G threads of a row (a multiple of 32, threadIdx.x); every thread gets it.  G = 32: a warp of its
+// own, no barrier.  Otherwise row `g` of the CTA has named barrier g + 1 and two sets of 32 floats in
+// `scratch`, used in turn, so that one barrier per sum is enough.
+__device__ __forceinline__ float row_sum(float v, int G, int g, float* scratch) {
     v = warp_sum(v);
     if (G == 32) return v;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = G >> 5;
     if (lane == 0) scratch[warp] = v;
-    __syncthreads();
-    v = warp_sum(lane < n ? scratch[lane] : 0.f);
-    __syncthreads();                                   // scratch may be written again
-    return v;
+    asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(G) : "memory");
+    return warp_sum(lane < n ? scratch[lane] : 0.f);
 }
 
 // VPT vectors per thread are kept in registers; VPT = 0: rows too long for that are read twice.
@@ -59,17 +59,11 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
     uint8_t* qout = a.q ? a.q + t * a.ldq : nullptr;
     uint8_t* sout = a.q ? a.scales + t * a.lds : nullptr;
 
-    auto read = [&](int64_t c, float (&f)[8]) {
-        const int64_t n = a.H - c;
-        if (n <= 0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = 0.f;
-            return;
-        }
-        unpack8<T>(load8<T, VEC>(x + c, n), f);
+    auto add = [&](const Raw8<T>& rx, const Raw8<T>& rr, float (&f)[8]) {
+        unpack8<T>(rx, f);
         if (res) {
             float r[8];
-            unpack8<T>(load8<T, VEC>(res + c, n), r);
+            unpack8<T>(rr, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] += r[i];
         }
@@ -108,13 +102,20 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
     float sum = 0.f;
     if constexpr (VPT > 0) {
         float h[VPT][8];
+        Raw8<T> rx[VPT], rr[VPT];                      // all loads before the first use
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) read(8 * ((int64_t)threadIdx.x + i * G), h[i]);
+        for (int i = 0; i < VPT; ++i) {
+            const int64_t c = 8 * ((int64_t)threadIdx.x + i * G), n = a.H - c;
+            rx[i] = n > 0 ? load8<T, VEC>(x + c, n) : Raw8<T>{};
+            rr[i] = n > 0 && res ? load8<T, VEC>(res + c, n) : Raw8<T>{};
+        }
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
+        for (int i = 0; i < VPT; ++i) {
+            add(rx[i], rr[i], h[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = fmaf(h[i][j], h[i][j], sum);
-        sum = row_sum(sum, G, scratch);
+        }
+        sum = row_sum(sum, G, 0, scratch);
         const float s = rsqrtf(sum / (float)a.H + a.eps);
         if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
 #pragma unroll
@@ -123,13 +124,17 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
         // h may be stored over x or r: nothing is written before the second reading, and each element
         // is read and written by the same thread
         const int64_t step = 8 * (int64_t)G, end = (a.H + step - 1) / step * step;
+        auto read = [&](int64_t c, float (&f)[8]) {
+            const int64_t n = a.H - c;
+            add(n > 0 ? load8<T, VEC>(x + c, n) : Raw8<T>{}, n > 0 && res ? load8<T, VEC>(res + c, n) : Raw8<T>{}, f);
+        };
         for (int64_t c = 8 * threadIdx.x; c < end; c += step) {
             float h[8];
             read(c, h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = fmaf(h[j], h[j], sum);
         }
-        sum = row_sum(sum, G, scratch);
+        sum = row_sum(sum, G, 0, scratch);
         const float s = rsqrtf(sum / (float)a.H + a.eps);
         if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
         for (int64_t c = 8 * threadIdx.x; c < end; c += step) {
@@ -143,18 +148,25 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
 template <typename T, typename W, int Q, bool VEC>
 gpd_status launch_norm(const NormArgs& a, cudaStream_t st) {
     const int64_t vecs = (a.H + 7) / 8;
-    auto threads = [&](int vpt) { return (int)(((vecs + vpt - 1) / vpt + 31) / 32 * 32); };
-    if (vecs <= 64) {                                  // a warp per row, four rows per CTA
+    if (vecs <= 128) {                                 // a warp per row, four rows per CTA: no barrier
         const dim3 block(32, 4);
         const unsigned grid = (unsigned)((a.T + 3) / 4);
         if (vecs <= 32) rmsnorm_kernel<T, W, Q, 1, VEC><<<grid, block, 0, st>>>(a);
-        else rmsnorm_kernel<T, W, Q, 2, VEC><<<grid, block, 0, st>>>(a);
-    } else if (vecs <= 1024) {
-        rmsnorm_kernel<T, W, Q, 2, VEC><<<(unsigned)a.T, threads(2), 0, st>>>(a);
-    } else if (vecs <= 2048) {
-        rmsnorm_kernel<T, W, Q, 4, VEC><<<(unsigned)a.T, threads(4), 0, st>>>(a);
-    } else {
-        rmsnorm_kernel<T, W, Q, 0, VEC><<<(unsigned)a.T, 1024, 0, st>>>(a);
+        else if (vecs <= 64) rmsnorm_kernel<T, W, Q, 2, VEC><<<grid, block, 0, st>>>(a);
+        else rmsnorm_kernel<T, W, Q, 4, VEC><<<grid, block, 0, st>>>(a);
+        return launch_ok();
+    }
+    // Many rows: few threads with many vectors each, so that many rows are in flight on an SM and a barrier
+    // holds few warps.  Few rows: many threads, for the latency of one row.
+    constexpr int kMost = sizeof(T) == 4 ? 4 : 8;
+    const bool many = a.T >= 4 * sm_count();
+    const int vpt = vecs > 512 * kMost ? 0 : many || vecs > 2048 ? kMost : vecs > 1024 ? 4 : 2;
+    const int threads = vpt ? (int)(((vecs + vpt - 1) / vpt + 31) / 32 * 32) : 1024;
+    switch (vpt) {
+        case 2: rmsnorm_kernel<T, W, Q, 2, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
+        case 4: rmsnorm_kernel<T, W, Q, 4, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
+        case kMost == 8 ? 8 : -1: rmsnorm_kernel<T, W, Q, kMost, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
+        default: rmsnorm_kernel<T, W, Q, 0, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
     }
     return launch_ok();
 }
@@ -182,12 +194,16 @@ struct NormBwdArgs {
     int64_t T, H;
 };
 
-// CTA p takes the rows p, p + gridDim.x, ... and adds up its share of dw: in registers, or (VPT = 0, long
-// rows) in its own row of `parts`, element by element by the thread that owns the column.
+constexpr int kBwdThreads = 512;
+
+// blockDim = (G, R): R rows of the CTA at a time, G threads each.  A thread adds up its columns' share of dw over
+// its rows: in registers, met in shared memory at the end, one partial row per CTA; or (VPT = 0, long rows, R = 1)
+// in the CTA's row of `parts`, element by element by the thread that owns the column.
 template <typename T, typename W, int VPT, bool VEC>
-__global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(const NormBwdArgs a) {
-    __shared__ float scratch[32];
-    const int G = blockDim.x;
+__global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward_kernel(const NormBwdArgs a) {
+    __shared__ float scratch[16][2][32];
+    extern __shared__ float dw_rows[];                 // [R - 1][8 VPT G]
+    const int G = blockDim.x, g = threadIdx.y;
     const W* wt = static_cast<const W*>(a.weight);
     float* part = a.parts + (int64_t)blockIdx.x * a.H;
     constexpr int N = VPT > 0 ? VPT : 1;
@@ -197,8 +213,10 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
     const int64_t step = 8 * (int64_t)G;
+    const int64_t first = (int64_t)blockIdx.x * blockDim.y + g;
+    int turn = 0;
 
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    for (int64_t t = first; t < a.T; t += (int64_t)gridDim.x * blockDim.y, turn ^= 1) {
         const T* dy = static_cast<const T*>(a.dy) + t * a.lddy;
         const T* h = static_cast<const T*>(a.h) + t * a.ldh;
         const T* dh = a.dh ? static_cast<const T*>(a.dh) + t * a.lddh : nullptr;
@@ -240,7 +258,7 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(
                     for (int j = 0; j < 8; ++j) dot = fmaf(fy[j] * w[j], fh[j], dot);
                 }
             }
-            dot = row_sum(dot, G, scratch);
+            dot = row_sum(dot, G, g, scratch[g][turn]);
             const float k = s * s * (dot / (float)a.H);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
@@ -256,12 +274,12 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(
 #pragma unroll
                 for (int j = 0; j < 8; ++j) dot = fmaf(fy[j] * w[j], fh[j], dot);
             }
-            dot = row_sum(dot, G, scratch);
+            dot = row_sum(dot, G, g, scratch[g][turn]);
             const float k = s * s * (dot / (float)a.H);
             for (int64_t c = 8 * threadIdx.x; c < a.H; c += step) {
                 const int64_t n = a.H - c;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dw[0][j] = j < n && t != blockIdx.x ? part[c + j] : 0.f;
+                for (int j = 0; j < 8; ++j) dw[0][j] = j < n && t != first ? part[c + j] : 0.f;
                 write(c, load8<T, VEC>(dy + c, n), load8<T, VEC>(h + c, n), dh ? load8<T, VEC>(dh + c, n) : Raw8<T>{}, k, dw[0]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -270,6 +288,20 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(
         }
     }
     if constexpr (VPT > 0) {
+        // the R rows' shares in the order of the rows; [j][thread] keeps neighbouring threads in neighbouring banks
+        if (g > 0) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dw_rows[((g - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x] = dw[i][j];
+        }
+        __syncthreads();
+        if (g > 0) return;
+        for (int r = 1; r < (int)blockDim.y; ++r)
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dw[i][j] += dw_rows[((r - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
@@ -280,17 +312,18 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_backward_kernel(
     }
 }
 
-// dw_c = sum over the partial rows, in a fixed order: eight threads per column, then their sums.
-__global__ void __launch_bounds__(256) rmsnorm_dweight_kernel(const float* parts, int n, int64_t H, float* dw) {
-    __shared__ float s[8][33];
+// dw_c = sum over the partial rows, in a fixed order: sixteen threads per column, then their sums.
+__global__ void __launch_bounds__(512) rmsnorm_dweight_kernel(const float* parts, int n, int64_t H, float* dw) {
+    __shared__ float s[16][33];
     const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
     float v = 0.f;
     if (c < H)
-        for (int p = threadIdx.y; p < n; p += 8) v += parts[(int64_t)p * H + c];
+#pragma unroll 8
+        for (int p = threadIdx.y; p < n; p += 16) v += parts[(int64_t)p * H + c];
     s[threadIdx.y][threadIdx.x] = v;
     __syncthreads();
     if (threadIdx.y == 0 && c < H) {
-        for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+        for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
         dw[c] = v;
     }
 }
@@ -298,15 +331,25 @@ __global__ void __launch_bounds__(256) rmsnorm_dweight_kernel(const float* parts
 template <typename T, typename W, bool VEC>
 gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
     const int64_t vecs = (a.H + 7) / 8;
-    const int parts = (int)std::min<int64_t>(std::min<int64_t>(a.T, 3 * sm_count()), GPD_RMSNORM_MAX_PARTS);
+    constexpr int V = sizeof(T) == 4 ? 2 : 4;
+    // one CTA of up to 512 threads per SM: R rows of G threads at a time
+    const bool loop = vecs > kBwdThreads * V;
+    const int G = loop ? 1024 : (int)(((vecs + V - 1) / V + 31) / 32 * 32);
+    int R = loop ? 1 : std::max(1, std::min(kBwdThreads / G, 15));      // named barriers 1 .. 15
+    R = (int)std::max<int64_t>(1, std::min<int64_t>(R, (a.T + sm_count() - 1) / sm_count()));
+    const int parts = (int)std::min<int64_t>(std::min<int64_t>((a.T + R - 1) / R, sm_count()), GPD_RMSNORM_MAX_PARTS);
     if (parts > 0) {
-        constexpr int V = sizeof(T) == 4 ? 2 : 4;
-        if (vecs <= 512 * V)
-            rmsnorm_backward_kernel<T, W, V, VEC><<<parts, (int)(((vecs + V - 1) / V + 31) / 32 * 32), 0, st>>>(a);
-        else
+        const int smem = (R - 1) * 8 * V * G * (int)sizeof(float);      // at most 512 * 32 floats
+        if (loop) {
             rmsnorm_backward_kernel<T, W, 0, VEC><<<parts, 1024, 0, st>>>(a);
+        } else {
+            auto kernel = rmsnorm_backward_kernel<T, W, V, VEC>;
+            if (smem > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+                return GPD_ERR_CUDA;
+            kernel<<<parts, dim3(G, R), smem, st>>>(a);
+        }
     }
-    rmsnorm_dweight_kernel<<<(unsigned)((a.H + 31) / 32), dim3(32, 8), 0, st>>>(a.parts, parts, a.H, dweight);
+    rmsnorm_dweight_kernel<<<(unsigned)((a.H + 31) / 32), dim3(32, 16), 0, st>>>(a.parts, parts, a.H, dweight);
     return launch_ok();
 }
 template <typename T, typename W>
