@@ -1,4 +1,5 @@
-"""Builds libgpd.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Builds libgpd.so (the C-ABI CUDA library, nvcc for sm_100a) and _lm.so (the compiled part of the Python
+binding of its low-precision operators, host compiler and torch headers) in-tree.
 
 Usage:  python paper_1811_10751_b200/build.py [--force] [--verbose] [--ptxas]
 (run as a script so that the package, which needs the built library, is not imported)
@@ -18,6 +19,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libgpd.so")
+BINDING_SRC = os.path.join(CSRC, "lm_binding.cpp")
+BINDING_PATH = os.path.join(PKG_DIR, "_lm.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -42,6 +45,18 @@ def _headers_mtime() -> float:
     return max(os.path.getmtime(h) for h in hs)
 
 
+def _binding_cmd(out: str):
+    """Command that compiles and links _lm.so; torch and CUDA runtime libraries are the ones torch has loaded."""
+    import sysconfig
+    from torch.utils.cpp_extension import include_paths, library_paths
+    inc = [f for d in (INCLUDE, sysconfig.get_paths()["include"], *include_paths(device_type="cuda")) for f in ("-I", d)]
+    libs = [f for d in (PKG_DIR, *library_paths(device_type="cuda")) for f in ("-L", d)]
+    import torch
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *inc, BINDING_SRC, "-o", out, *libs,
+            "-lgpd", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     nvcc = _nvcc()
@@ -60,7 +75,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         if verbose or r.returncode != 0:
             sys.stderr.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
         if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed on {cmd[-3]}")
+            raise RuntimeError(f"{os.path.basename(cmd[0])} failed: {' '.join(cmd)}")
 
     with ThreadPoolExecutor(max_workers=min(8, max(1, len(jobs)))) as ex:
         list(ex.map(run, jobs))
@@ -68,6 +83,11 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         tmp = LIB_PATH + f".tmp{os.getpid()}"          # linked aside, then moved: readers never see half a file
         run([nvcc, "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
         os.replace(tmp, LIB_PATH)
+    newest = max(os.path.getmtime(BINDING_SRC), os.path.getmtime(os.path.join(INCLUDE, "gpd.h")))
+    if force or not os.path.exists(BINDING_PATH) or os.path.getmtime(BINDING_PATH) < newest:
+        tmp = BINDING_PATH + f".tmp{os.getpid()}"
+        run(_binding_cmd(tmp))
+        os.replace(tmp, BINDING_PATH)
     return LIB_PATH
 
 
