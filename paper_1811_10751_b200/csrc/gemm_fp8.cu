@@ -7,12 +7,19 @@
 // instruction by 2^(ea + eb), so a block of 128 is four instructions that name the same scale byte, and
 // scales per row, per 1 x 128 and per 128 x 128 block cost the same.
 //
-// One CTA computes 128 x BN output tiles.  Warp 0: one lane issues the TMA copies of the operands (k-blocks
-// of 128 bytes per row under the 128-byte swizzle, a ring that runs on across tiles).  Warp 2 gathers the
-// scales: a word holds one row's scales of four k-blocks; the words of 128 rows in the order tcgen05.cp
-// wants (lane i: rows i, i + 32, i + 64, i + 96) are one 16-byte store per lane.  Warp 1: one lane copies
-// them to tensor memory and issues the products.  Warps 4..11 read the accumulators back, two sets of
-// which alternate, and store.
+// Large products: two CTAs of a cluster (PAIR) compute a 256 x BN tile with cta_group::2 instructions, each
+// holding 128 rows of A and half of B's; a 128 x BN tile of one CTA moves every byte of B into twice as many
+// shared memories, and their bandwidth (operands coming in and going to the tensor cores) is what bounds it.
+// The even CTA issues; the odd one's copies and scales report to its barriers.
+//
+// Otherwise one CTA computes 128 x BN output tiles.  Warp 0: one lane issues the TMA copies of the operands (k-blocks
+// of 128 bytes per row under the 128-byte swizzle, a ring that runs on across tiles).  Warps 2..5 bring the
+// scales: a word holds one row's scales of four k-blocks, and the tensor cores want the words of rows
+// i, i + 32, i + 64, i + 96 in lane i of four columns of tensor memory, the same in each quarter of the lanes;
+// each warp writes one quarter (tcgen05.st), up to four groups of k-blocks ahead.  (Copies from shared memory
+// by the issuing lane, tcgen05.cp, stop the products around them: 850 instead of 450 cycles a k-block.)
+// Warp 1: one lane issues the products.  Warps 6..13 read the accumulators back, two sets of which alternate,
+// and store.
 //
 // Accumulation.  tcgen05.mma adds into its FP32 accumulator with truncation.  16-bit results take one chain
 // over the whole contraction: the bias (about 2^-25 of the sum per instruction, 8e-6 at K = 8192) is far
@@ -36,7 +43,6 @@ namespace gpd {
 
 namespace {
 
-using tc::mbar_arrive;
 using tc::mbar_expect_tx;
 using tc::mbar_init;
 using tc::mbar_try_wait;
@@ -44,17 +50,21 @@ using tc::smem_u32;
 using tc::umma_commit;
 
 constexpr int BM = 128, BK = 128, UMMA_K = 32;
-constexpr int kEpiWarps = 8, kThreads = 128 + 32 * kEpiWarps;
-constexpr int kSfSlots = 2;                            // groups of four k-blocks whose scales are in flight
-__host__ __device__ constexpr int stage_bytes(int bn) { return (BM + bn) * BK; }
+constexpr int kSfWarps = 4, kEpiWarps = 8, kThreads = 32 * (2 + kSfWarps + kEpiWarps);
+constexpr int kMaxSplits = 8;                          // parts of a split contraction (CTAs of a cluster)
+constexpr int kSfSlots = 4;                            // groups of four k-blocks whose scales are in flight
+__host__ __device__ constexpr int b_rows(int bn, bool pair) { return pair ? bn / 2 : bn; }
+__host__ __device__ constexpr int stage_bytes(int bn, bool pair) { return (BM + b_rows(bn, pair)) * BK; }
 __host__ __device__ constexpr int sfb_blocks(int bn) { return bn > 128 ? 2 : 1; }
-__host__ __device__ constexpr int sf_bytes(int bn) { return 512 * (1 + sfb_blocks(bn)); }
-__host__ __device__ constexpr int stages(int bn) {
-    const int n = (232448 - 1024 - 512 - kSfSlots * sf_bytes(bn)) / stage_bytes(bn);
+__host__ __device__ constexpr int sf_cols(int bn) { return 4 * (1 + sfb_blocks(bn)); }   // of tensor memory, per slot
+__host__ __device__ constexpr int stages(int bn, bool pair) {
+    const int n = (232448 - 1024 - 4096) / stage_bytes(bn, pair);
     return n > 10 ? 10 : n;
 }
-__host__ __device__ constexpr int smem_bytes(int bn) { return 1024 + stages(bn) * stage_bytes(bn) + kSfSlots * sf_bytes(bn); }
-__host__ __device__ constexpr int tmem_need(int bn) { return 2 * bn + kSfSlots * 4 * (1 + sfb_blocks(bn)); }
+__host__ __device__ constexpr int smem_bytes(int bn, bool pair) {
+    return 1024 + stages(bn, pair) * stage_bytes(bn, pair);
+}
+__host__ __device__ constexpr int tmem_need(int bn) { return 2 * bn + kSfSlots * sf_cols(bn); }
 __host__ __device__ constexpr int tmem_cols(int bn) {
     return tmem_need(bn) <= 64 ? 64 : tmem_need(bn) <= 128 ? 128 : tmem_need(bn) <= 256 ? 256 : 512;
 }
@@ -64,10 +74,58 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     return tc::mbar_wait(bar, parity, abort_flag, &g_fp8_status);
 }
 
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
+// Address of this CTA's `p` in the even CTA of the pair
+__device__ __forceinline__ uint32_t in_leader(const void* p) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(0));
+    return a;
+}
+// Arrivals (at a barrier of either CTA of a pair) and waits that order accesses to tensor memory alone, which
+// tcgen05.wait and tcgen05.fence before the arrival and tcgen05.fence after the wait take care of: a releasing
+// arrival would also wait for the thread's global loads and stores, 1000 cycles and more under load.
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_relaxed(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
     asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1) : "memory");
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_relaxed(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    if (mbar_try_wait_relaxed(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait_relaxed(bar, parity)) {
+        if (*abort_flag) return false;
+        if (clock64() - t0 > tc::kWaitCycles) {
+            *abort_flag = 1;
+            atomicExch(&g_fp8_status, (int)GPD_ERR_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
+// bar: shared::cluster address
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
+            ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+            ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+// Arrival, at the barrier of every CTA of the tile, once the tensor cores are done with what was issued so far
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(smem_u32(bar)), "h"((unsigned short)3) : "memory");
+    else
+        umma_commit(bar);
 }
 // K-major tile with rows of 128 bytes under the 128-byte swizzle: 8-row groups 1024 bytes apart
 // (descriptor version 1, layout type 2).
@@ -75,25 +133,29 @@ __device__ __forceinline__ uint64_t desc_sw128(uint32_t addr) {
     return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
            (uint64_t)2 << 61;
 }
-// 32 rows of 16 bytes without swizzle: 8-row groups 128 bytes apart
-__device__ __forceinline__ uint64_t desc_scales(uint32_t addr) {
-    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)1 << 16 | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+// Four columns of this warp's quarter of the lanes
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint4 v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
+template <bool PAIR>
 __device__ __forceinline__ void umma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
-// FP32 accumulator, both operands K-major, M = 128, N = n, scales e8m0; types 0 = e4m3, 1 = e5m2; `sf` = byte of
+// FP32 accumulator, both operands K-major, M = m, N = n, scales e8m0; types 0 = e4m3, 1 = e5m2; `sf` = byte of
 // the scale words that this instruction uses
-__device__ __forceinline__ uint32_t idesc_mx(int n, int a_type, int b_type, int sf) {
+__device__ __forceinline__ uint32_t idesc_mx(int m, int n, int a_type, int b_type, int sf) {
     return ((uint32_t)sf << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
-           ((uint32_t)(BM >> 4) << 24) | ((uint32_t)sf << 29);
+           ((uint32_t)(m >> 4) << 24) | ((uint32_t)sf << 29);
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t* r, uint32_t taddr) {
     asm volatile(
@@ -102,6 +164,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t* r, uint32_t taddr) {
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr));
+}
+// True in one lane of the (converged) warp
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -129,38 +197,39 @@ struct Fp8Params {
     int tiles_m, tiles_n, splits;
 };
 
-// Scales of the k-blocks 4 g .. 4 g + 3 of one operand row.  Rows and k-blocks that do not exist give any
-// valid scale: their products are zero or not stored.
-__device__ __forceinline__ uint32_t scale_word(const ScaleRows& s, int64_t row, int g, int kb) {
-    if (row >= s.rows) return 0x7f7f7f7fu;
-    const uint8_t* p = s.p + (row >> s.shift) * s.ld + 4 * g;
-    if (s.words && 4 * g + 4 <= kb) return __ldg(reinterpret_cast<const uint32_t*>(p));
+// Up to four scales of one row as a word.  Rows and k-blocks that do not exist get any valid scale (1): their
+// products are zero or not stored.
+__device__ __forceinline__ uint32_t scale_bytes(const uint8_t* p, int n) {
     uint32_t w = 0x7f7f7f7fu;
-    for (int i = 0; i < 4 && 4 * g + i < kb; ++i) w = (w & ~(0xffu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) w = (w & ~(0xffu << (8 * i))) | ((uint32_t)__ldg(p + i) << (8 * i));
     return w;
 }
 
-// Tile order: columns of up to 16 row tiles, so that the tiles in flight share operands in L2.
+// Tile order: columns of up to 2048 rows, so that the tiles in flight share operands in L2.
+template <bool PAIR>
 __device__ __forceinline__ void tile_origin(const Fp8Params& p, int tile, int bn, int64_t& m0, int64_t& n0) {
-    const int band = 16 * p.tiles_n, b = tile / band, r = tile - b * band;
-    const int h = min(16, p.tiles_m - 16 * b);
-    m0 = (int64_t)(16 * b + r % h) * BM;
+    constexpr int H = PAIR ? 8 : 16;
+    const int band = H * p.tiles_n, b = tile / band, r = tile - b * band;
+    const int h = min(H, p.tiles_m - H * b);
+    m0 = (int64_t)(H * b + r % h) * (PAIR ? 2 * BM : BM);
     n0 = (int64_t)(r / h) * bn;
 }
 
 // TRANS: D[i][j] is stored at out[j][i] (the caller swapped the operands); consecutive lanes hold consecutive i.
-template <int BN, typename T, bool TRANS>
+template <int BN, typename T, bool TRANS, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Fp8Params prm) {
-    constexpr int STAGES = stages(BN), STAGE = stage_bytes(BN), SFB = sfb_blocks(BN);
+    constexpr int STAGES = stages(BN, PAIR), STAGE = stage_bytes(BN, PAIR), SFB = sfb_blocks(BN);
     constexpr bool CHUNKED = sizeof(T) == 4;           // FP32 results: chains of four k-blocks
     constexpr int CW = BN >= 64 ? BN / 2 : BN;         // columns of an epilogue warp (two warps share a lane quarter)
     constexpr int COLS = tmem_cols(BN);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* sf_smem = smem + STAGES * STAGE;
     __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], sf_full[kSfSlots], sf_empty[kSfSlots],
         acc_full[2], acc_empty[2];
+    __shared__ __align__(16) uint4 sf_words[2][(1 + SFB) * 32];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -171,126 +240,196 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             mbar_init(&empty_bar[s], 1);
         }
         for (int s = 0; s < kSfSlots; ++s) {
-            mbar_init(&sf_full[s], 1);
+            mbar_init(&sf_full[s], PAIR ? 2 * kSfWarps : kSfWarps);
             mbar_init(&sf_empty[s], 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&acc_full[s], 1);
-            mbar_init(&acc_empty[s], kEpiWarps);
+            mbar_init(&acc_empty[s], PAIR ? 2 * kEpiWarps : kEpiWarps);
         }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync();                          // the pair's barriers exist before the other CTA uses them
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot, tmem_sf = tmem + 2 * BN;
     volatile int* abort_p = &abort_flag;
 
-    // this CTA's part of the contraction (whole k-blocks) and its tiles
-    const int S = prm.splits, rank = S > 1 ? (int)blockIdx.x % S : 0;
+    // this CTA's part of the contraction (whole k-blocks) and its tiles; its place in the pair
+    const int S = PAIR ? 1 : prm.splits, rank = S > 1 ? (int)blockIdx.x % S : 0, side = PAIR ? (int)blockIdx.x & 1 : 0;
     const int kb0 = (int)((int64_t)prm.kb * rank / S), kb1 = (int)((int64_t)prm.kb * (rank + 1) / S);
-    const int tile0 = (int)blockIdx.x / S, tile_step = (int)gridDim.x / S, tiles = prm.tiles_m * prm.tiles_n;
+    const int share = PAIR ? 2 : S;                    // CTAs that share a tile
+    const int tile0 = (int)blockIdx.x / share, tile_step = (int)gridDim.x / share, tiles = prm.tiles_m * prm.tiles_n;
 
+    // Warps 0 and 1 run their loops as a whole, with one elected lane issuing: what the instructions name is then the
+    // same for the warp and stays in uniform registers (issued by a lone lane, 4 products with their waits and
+    // bookkeeping took 1040 cycles a k-block, more than twice what the tensor cores need for them).
     if (warp == 0) {
-        if (lane == 0) {
-            int it = 0;
-            bool ok = true;
-            for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
-                int64_t m0, n0;
-                tile_origin(prm, tile, BN, m0, n0);
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (!mbar_wait(&empty_bar[s], ((it / STAGES) & 1) ^ 1, abort_p)) { ok = false; break; }
-                    mbar_expect_tx(&full_bar[s], STAGE);
-                    tma_load_2d(smem + s * STAGE, &tmA, kb * BK, (int)m0, &full_bar[s]);
-                    tma_load_2d(smem + s * STAGE + BM * BK, &tmB, kb * BK, (int)n0, &full_bar[s]);
+        const bool one = elect_one();
+        const uint32_t bar0 = PAIR ? in_leader(&full_bar[0]) : smem_u32(&full_bar[0]);
+        int s = 0, issued = 0;
+        uint32_t phase = 1;                            // of the empty barriers: the first round does not wait
+        bool live = true;                              // per lane; the loops run on without issuing when a wait expired
+        for (int tile = tile0; tile < tiles; tile += tile_step) {
+            int64_t m0, n0;
+            tile_origin<PAIR>(prm, tile, BN, m0, n0);
+            const int am = (int)m0 + side * BM, bn = (int)n0 + side * b_rows(BN, PAIR);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                live = live && mbar_wait(&empty_bar[s], phase, abort_p);
+                if (one && live) {
+                    ++issued;
+                    if (side == 0) mbar_expect_tx(&full_bar[s], (PAIR ? 2 : 1) * STAGE);
+                    tma_load_2d<PAIR>(smem + s * STAGE, &tmA, kb * BK, am, bar0 + 8 * s);
+                    tma_load_2d<PAIR>(smem + s * STAGE + BM * BK, &tmB, kb * BK, bn, bar0 + 8 * s);
+                }
+                if (++s == STAGES) {
+                    s = 0;
+                    phase ^= 1;
                 }
             }
-            if (*abort_p) {                            // copies still in flight land before the CTA exits
-                for (int j = it > STAGES ? it - STAGES : 0; j < it; ++j) {
-                    const long long t0 = clock64();
-                    while (!mbar_try_wait(&full_bar[j % STAGES], (j / STAGES) & 1) && clock64() - t0 < tc::kWaitCycles) {}
-                }
+        }
+        if (*abort_p && side == 0 && one) {            // copies still in flight, the pair's too, land before the CTA exits
+            for (int j = issued > STAGES ? issued - STAGES : 0; j < issued; ++j) {
+                const long long t0 = clock64();
+                while (!mbar_try_wait(&full_bar[j % STAGES], (j / STAGES) & 1) && clock64() - t0 < tc::kWaitCycles) {}
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int it = 0, gi = 0, ac = 0;                // k-blocks, scale groups and accumulator chains so far
-            bool ok = true;
-            for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const bool new_group = kb == kb0 || (kb & 3) == 0;
-                    const bool new_chain = kb == kb0 || (CHUNKED && (kb & 3) == 0);
-                    if (new_chain && !mbar_wait(&acc_empty[ac & 1], ((ac >> 1) & 1) ^ 1, abort_p)) { ok = false; break; }
-                    if (new_group) {
-                        // the slot's previous scales are no longer in use: the gathering warp waited for that
-                        const int s = gi % kSfSlots;
-                        if (!mbar_wait(&sf_full[s], (gi / kSfSlots) & 1, abort_p)) { ok = false; break; }
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t src = smem_u32(sf_smem + s * sf_bytes(BN)), dst = tmem_sf + s * 4 * (1 + SFB);
-#pragma unroll
-                        for (int b = 0; b < 1 + SFB; ++b) scales_to_tmem(dst + 4 * b, desc_scales(src + 512 * b));
-                    }
-                    const int s = it % STAGES;
-                    if (!mbar_wait(&full_bar[s], (it / STAGES) & 1, abort_p)) { ok = false; break; }
+        if (side == 0) {
+            const bool one = elect_one();
+            const uint64_t desc0 = desc_sw128(smem_u32(smem));
+            const uint32_t idesc0 = idesc_mx(PAIR ? 2 * BM : BM, BN, prm.a_type, prm.b_type, 0);
+            int s = 0, gs = 0, set = 0;                // stage, scale slot and accumulator set in turn, and their phases
+            uint32_t phase = 0, gphase = 0, aphase = 1;
+            bool live = true;
+            for (int tile = tile0; tile < tiles; tile += tile_step) {
+                bool fresh = true;                     // the next product starts a chain
+                for (int g = kb0 >> 2; 4 * g < kb1; ++g) {
+                    if (fresh) live = live && mbar_wait_relaxed(&acc_empty[set], aphase, abort_p);
+                    live = live && mbar_wait_relaxed(&sf_full[gs], gphase, abort_p);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a0 = smem_u32(smem + s * STAGE), b0 = a0 + BM * BK;
-                    const uint32_t sf = tmem_sf + (gi % kSfSlots) * 4 * (1 + SFB);
-                    const uint32_t idesc = idesc_mx(BN, prm.a_type, prm.b_type, kb & 3);
+                    const uint32_t sf = tmem_sf + gs * sf_cols(BN), d = tmem + set * BN;
 #pragma unroll
-                    for (int k = 0; k < BK / UMMA_K; ++k)
-                        umma_mx(tmem + (ac & 1) * BN, desc_sw128(a0 + k * UMMA_K), desc_sw128(b0 + k * UMMA_K), idesc, sf,
-                                sf + 4, !(new_chain && k == 0));
-                    umma_commit(&empty_bar[s]);
-                    const bool last = kb + 1 == kb1;
-                    if (last || (kb & 3) == 3) {
-                        umma_commit(&sf_empty[gi % kSfSlots]);
-                        ++gi;
+                    for (int i = 0; i < 4; ++i) {
+                        const int kb = 4 * g + i;
+                        if (kb < kb0 || kb >= kb1) continue;
+                        live = live && mbar_wait(&full_bar[s], phase, abort_p);
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t a = desc0 + (uint64_t)((s * STAGE) >> 4), b = a + (uint64_t)((BM * BK) >> 4);
+                        const uint32_t idesc = idesc0 | (uint32_t)i << 4 | (uint32_t)i << 29;      // byte i of the scale words
+                        if (one && live) {
+#pragma unroll
+                            for (int k = 0; k < BK / UMMA_K; ++k)
+                                umma_mx<PAIR>(d, a + k * (UMMA_K >> 4), b + k * (UMMA_K >> 4), idesc, sf, sf + 4, !(fresh && k == 0));
+                            commit<PAIR>(&empty_bar[s]);
+                        }
+                        fresh = false;
+                        if (++s == STAGES) {
+                            s = 0;
+                            phase ^= 1;
+                        }
                     }
-                    if (last || (CHUNKED && (kb & 3) == 3)) {
-                        umma_commit(&acc_full[ac & 1]);
-                        ++ac;
+                    const bool end = CHUNKED || 4 * g + 4 >= kb1;      // of the chain
+                    if (one && live) {
+                        commit<PAIR>(&sf_empty[gs]);
+                        if (end) commit<PAIR>(&acc_full[set]);
+                    }
+                    if (++gs == kSfSlots) {
+                        gs = 0;
+                        gphase ^= 1;
+                    }
+                    if (end) {
+                        fresh = true;
+                        if (set) aphase ^= 1;
+                        set ^= 1;
                     }
                 }
             }
         }
-    } else if (warp == 2) {
-        int gi = 0;
-        bool ok = true;
-        for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+        __syncwarp();
+    } else if (warp < 2 + kSfWarps) {
+        // Warp q of the four fetches the words of rows 32 q + lane of every block of 128; the warps exchange them
+        // through shared memory, and each writes all of them to its quarter.  Words are fetched kAhead groups before
+        // they are wanted.
+        constexpr int NB = 1 + SFB, kAhead = 4;
+        const int q = warp & 3;
+        const uint8_t* rows[NB];                       // this lane's scale rows of the tile being fetched; null: none
+        int tile = tile0, g = kb0 >> 2;                // the group to be fetched next
+        auto find_rows = [&]() {
             int64_t m0, n0;
-            tile_origin(prm, tile, BN, m0, n0);
-            for (int g = kb0 >> 2; 4 * g < kb1; ++g, ++gi) {
-                uint4 v[1 + SFB];
+            tile_origin<PAIR>(prm, tile, BN, m0, n0);
 #pragma unroll
-                for (int b = 0; b < 1 + SFB; ++b) {
-                    const ScaleRows& s = b == 0 ? prm.sa : prm.sb;
-                    const int64_t r = (b == 0 ? m0 : n0 + 128 * (b - 1)) + lane;
-                    v[b] = make_uint4(scale_word(s, r, g, prm.kb), scale_word(s, r + 32, g, prm.kb),
-                                      scale_word(s, r + 64, g, prm.kb), scale_word(s, r + 96, g, prm.kb));
+            for (int b = 0; b < NB; ++b) {
+                const ScaleRows& s = b == 0 ? prm.sa : prm.sb;
+                const int64_t r = (b == 0 ? m0 + side * BM : n0 + 128 * (b - 1)) + 32 * q + lane;
+                rows[b] = r < s.rows ? s.p + (r >> s.shift) * s.ld : nullptr;
+            }
+        };
+        auto fetch = [&](uint32_t (&v)[NB]) {
+            if (tile >= tiles) return;
+            const bool whole = 4 * g + 4 <= prm.kb;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                v[b] = 0x7f7f7f7fu;
+                if (rows[b]) {
+                    if (whole && (b == 0 ? prm.sa.words : prm.sb.words)) v[b] = __ldg(reinterpret_cast<const uint32_t*>(rows[b] + 4 * g));
+                    else v[b] = scale_bytes(rows[b] + 4 * g, prm.kb - 4 * g);
                 }
-                const int s = gi % kSfSlots;
-                ok = mbar_wait(&sf_empty[s], ((gi / kSfSlots) & 1) ^ 1, abort_p);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+            }
+            if (4 * (++g) >= kb1) {
+                g = kb0 >> 2;
+                tile += tile_step;
+                if (tile < tiles) find_rows();
+            }
+        };
+        const int groups = ((kb1 + 3) >> 2) - (kb0 >> 2);
+        const int total = tile0 < tiles ? groups * ((tiles - tile0 + tile_step - 1) / tile_step) : 0;
+        uint32_t ring[kAhead][NB];
+        if (total > 0) find_rows();
 #pragma unroll
-                for (int b = 0; b < 1 + SFB; ++b)
-                    *reinterpret_cast<uint4*>(sf_smem + s * sf_bytes(BN) + 512 * b + 16 * lane) = v[b];
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        for (int i = 0; i < kAhead; ++i) fetch(ring[i]);
+        const uint32_t sf_full0 = PAIR ? in_leader(&sf_full[0]) : smem_u32(&sf_full[0]);
+        bool live = true;
+        for (int g0 = 0; g0 < total; g0 += kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int gi = g0 + i;
+                if (gi >= total) break;
+                uint32_t* buf = reinterpret_cast<uint32_t*>(sf_words[i & 1]);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) buf[(b * 32 + lane) * 4 + q] = ring[i][b];
+                fetch(ring[i]);
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                const int s = gi % kSfSlots;
+                live = live && mbar_wait(&sf_empty[s], ((gi / kSfSlots) & 1) ^ 1, abort_p);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sf_full[s]);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    tmem_st4(tmem_sf + s * sf_cols(BN) + 4 * b + ((uint32_t)(q * 32) << 16), sf_words[i & 1][b * 32 + lane]);
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0 && live) mbar_arrive_relaxed(sf_full0 + 8 * s);
             }
         }
-    } else if (warp >= 4) {
-        const int q = warp & 3, half = (warp - 4) >> 2;
+    } else {
+        const int q = warp & 3, half = (warp - 2 - kSfWarps) >> 2;      // tcgen05.ld: a warp reads its quarter of the lanes
         const int c0 = BN >= 64 ? half * CW : 0;
         const bool idle = BN < 64 && half == 1;        // narrow tiles: four warps do it all
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        const uint32_t acc_empty0 = PAIR ? in_leader(&acc_empty[0]) : smem_u32(&acc_empty[0]);
         float acc[CHUNKED ? CW : 1];
         int ac = 0;
         bool ok = true;
@@ -298,8 +437,8 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         float* part = reinterpret_cast<float*>(smem);  // split contraction: [BN][128], over the operand ring
         for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
             int64_t m0, n0;
-            tile_origin(prm, tile, BN, m0, n0);
-            const int64_t row = m0 + q * 32 + lane;
+            tile_origin<PAIR>(prm, tile, BN, m0, n0);
+            const int64_t row = m0 + side * BM + q * 32 + lane;
             // w columns from column c of the tile, in f
             auto put = [&](int c, const float* f, int w) {
                 if (S > 1) {
@@ -339,7 +478,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             auto release = [&](int set) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[set]);
+                if (lane == 0) mbar_arrive_relaxed(acc_empty0 + 8 * set);
             };
             auto ready = [&](int set, int n) {
                 const bool r = mbar_wait(&acc_full[set], (n >> 1) & 1, abort_p);
@@ -395,7 +534,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         // one tile per cluster: each CTA adds up its share of the tile's columns over all parts
         cluster_sync();
         int64_t m0, n0;
-        tile_origin(prm, tile0, BN, m0, n0);
+        tile_origin<PAIR>(prm, tile0, BN, m0, n0);
         const int j0 = BN * rank / S, j1 = BN * (rank + 1) / S;
         const uint32_t base = smem_u32(smem);
         T* out = static_cast<T*>(prm.out);
@@ -403,8 +542,11 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             for (int e = j0 * BM + threadIdx.x; e < j1 * BM; e += kThreads) {
                 const int64_t row = m0 + (e & (BM - 1)), col = n0 + e / BM;
                 if (row >= prm.M || col >= prm.N) continue;
-                float v = 0.f;
-                for (int s = 0; s < S; ++s) v += ld_cluster(base + 4 * e, s);
+                float p[kMaxSplits], v = 0.f;          // all loads before the first sum
+#pragma unroll
+                for (int s = 0; s < kMaxSplits; ++s) p[s] = s < S ? ld_cluster(base + 4 * e, s) : 0.f;
+#pragma unroll
+                for (int s = 0; s < kMaxSplits; ++s) v += p[s];
                 T* o = TRANS ? out + col * prm.ldd + row : out + row * prm.ldd + col;
                 *o = lm::from_f32<T>(prm.accumulate ? v + lm::to_f32(*o) : v);
             }
@@ -413,9 +555,11 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync();                          // neither CTA's shared or tensor memory goes while the other may use it
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
     }
 }
 
@@ -438,14 +582,14 @@ struct Operand {
     int type;
     ScaleRows s;
 };
-struct Config { int bn, splits; bool trans; };
+struct Config { int bn, splits; bool trans, pair; };
 
-template <int BN, typename T, bool TRANS>
+template <int BN, typename T, bool TRANS, bool PAIR>
 gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, int splits, cudaStream_t st) {
     CUtensorMap tmA, tmB;
-    if (!make_map_2d(&tmA, a.q, a.rows, K, a.ld, BM) || !make_map_2d(&tmB, b.q, b.rows, K, b.ld, BN)) return GPD_ERR_CUDA;
-    auto kernel = gemm_fp8_kernel<BN, T, TRANS>;
-    constexpr int smem = smem_bytes(BN);
+    if (!make_map_2d(&tmA, a.q, a.rows, K, a.ld, BM) || !make_map_2d(&tmB, b.q, b.rows, K, b.ld, b_rows(BN, PAIR))) return GPD_ERR_CUDA;
+    auto kernel = gemm_fp8_kernel<BN, T, TRANS, PAIR>;
+    constexpr int smem = smem_bytes(BN, PAIR), rows = PAIR ? 2 * BM : BM;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
     prm.sa = a.s;
     prm.sb = b.s;
@@ -453,47 +597,51 @@ gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, 
     prm.N = b.rows;
     prm.a_type = a.type == GPD_DT_E5M2;
     prm.b_type = b.type == GPD_DT_E5M2;
-    prm.tiles_m = (int)((a.rows + BM - 1) / BM);
+    prm.tiles_m = (int)((a.rows + rows - 1) / rows);
     prm.tiles_n = (int)((b.rows + BN - 1) / BN);
     prm.splits = splits;
     const int64_t tiles = (int64_t)prm.tiles_m * prm.tiles_n;
     if (tiles > 0x3fffffff) return GPD_ERR_SHAPE;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : std::min<int64_t>(tiles, sm_count())));
+    const int cluster = PAIR ? 2 : splits;
+    cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : cluster * std::min<int64_t>(tiles, sm_count() / cluster)));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)splits;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = splits > 1 ? 1 : 0;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
     if (cudaLaunchKernelEx(&cfg, kernel, tmA, tmB, prm) != cudaSuccess) return GPD_ERR_CUDA;
     return launch_ok();
 }
 
-// Tile width, orientation and split by the smallest estimated time.  A k-block of a 128 x BN tile takes the
-// tensor cores 2 BN cycles and its copies (128 + BN) * 128 bytes at about 48 bytes per cycle and SM; a tile
-// costs about 1500 cycles besides, a split tile twice that.
+// Tile width, orientation, pairing and split by the smallest estimated time.  A k-block of a 128 x BN tile (per
+// CTA) takes the tensor cores 2 BN cycles and its copies (128 + BN, in a pair 128 + BN / 2) * 128 bytes at about 48
+// bytes per cycle and SM; a tile costs about 1500 cycles besides, a split tile twice that.
 Config choose(int64_t M, int64_t N, int kb, bool f32) {
     static const int kWidths[] = {16, 32, 64, 128, 192, 224};
-    Config best{128, 1, true};
+    Config best{128, 1, true, false};
     double best_t = 1e300;
     const int sms = sm_count();
     for (int t = 0; t < 2; ++t) {
         const int64_t rows = t ? N : M, cols = t ? M : N;
         for (int bn : kWidths) {
             if (bn == 224 && f32) continue;            // FP32 results keep a tile's row in registers
-            const int64_t tiles = ((rows + BM - 1) / BM) * ((cols + bn - 1) / bn);
-            for (int s = 1; s <= 8; s *= 2) {
-                if (s > 1 && (s > kb || tiles * s > 2 * sms)) continue;
-                const double waves = (double)((tiles * s + sms - 1) / sms);
-                const double block = std::max(2.0 * bn, (BM + bn) * 128 / 48.0);
-                const double time = waves * (((kb + s - 1) / s) * block + (s > 1 ? 3000.0 : 1500.0));
-                if (time < best_t * 0.999) {
-                    best_t = time;
-                    best = Config{bn, s, t == 1};
+            for (int pair = 0; pair <= (bn >= 128 ? 1 : 0); ++pair) {
+                const int height = pair ? 2 * BM : BM, slots = pair ? sms / 2 : sms;
+                const int64_t tiles = ((rows + height - 1) / height) * ((cols + bn - 1) / bn);
+                for (int s = 1; s <= (pair ? 1 : kMaxSplits); s *= 2) {
+                    if (s > 1 && (s > kb || tiles * s > 2 * sms)) continue;
+                    const double waves = (double)((tiles * s + slots - 1) / slots);
+                    const double block = std::max(2.0 * bn, (BM + b_rows(bn, pair)) * 128 / 48.0);
+                    const double time = waves * (((kb + s - 1) / s) * block + (s > 1 ? 3000.0 : 1500.0));
+                    if (time < best_t * 0.999) {
+                        best_t = time;
+                        best = Config{bn, s, t == 1, pair == 1};
+                    }
                 }
             }
         }
@@ -503,15 +651,20 @@ Config choose(int64_t M, int64_t N, int kb, bool f32) {
 
 template <typename T, bool TRANS>
 gpd_status launch_bn(const Operand& a, const Operand& b, const Fp8Params& prm, int64_t K, const Config& c, cudaStream_t st) {
-    switch (c.bn) {
-        case 16: return launch<16, T, TRANS>(a, b, prm, K, c.splits, st);
-        case 32: return launch<32, T, TRANS>(a, b, prm, K, c.splits, st);
-        case 64: return launch<64, T, TRANS>(a, b, prm, K, c.splits, st);
-        case 128: return launch<128, T, TRANS>(a, b, prm, K, c.splits, st);
-        case 192: return launch<192, T, TRANS>(a, b, prm, K, c.splits, st);
+    switch (c.pair ? -c.bn : c.bn) {
+        case 16: return launch<16, T, TRANS, false>(a, b, prm, K, c.splits, st);
+        case 32: return launch<32, T, TRANS, false>(a, b, prm, K, c.splits, st);
+        case 64: return launch<64, T, TRANS, false>(a, b, prm, K, c.splits, st);
+        case 128: return launch<128, T, TRANS, false>(a, b, prm, K, c.splits, st);
+        case 192: return launch<192, T, TRANS, false>(a, b, prm, K, c.splits, st);
+        case -128: return launch<128, T, TRANS, true>(a, b, prm, K, 1, st);
+        case -192: return launch<192, T, TRANS, true>(a, b, prm, K, 1, st);
         default: break;
     }
-    if constexpr (sizeof(T) == 2) return launch<224, T, TRANS>(a, b, prm, K, c.splits, st);
+    if constexpr (sizeof(T) == 2) {
+        if (c.pair) return launch<224, T, TRANS, true>(a, b, prm, K, 1, st);
+        return launch<224, T, TRANS, false>(a, b, prm, K, c.splits, st);
+    }
     return GPD_ERR_UNSUPPORTED;
 }
 template <typename T>
