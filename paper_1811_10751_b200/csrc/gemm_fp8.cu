@@ -57,12 +57,15 @@ __host__ __device__ constexpr int b_rows(int bn, bool pair) { return pair ? bn /
 __host__ __device__ constexpr int stage_bytes(int bn, bool pair) { return (BM + b_rows(bn, pair)) * BK; }
 __host__ __device__ constexpr int sfb_blocks(int bn) { return bn > 128 ? 2 : 1; }
 __host__ __device__ constexpr int sf_cols(int bn) { return 4 * (1 + sfb_blocks(bn)); }   // of tensor memory, per slot
-__host__ __device__ constexpr int stages(int bn, bool pair) {
-    const int n = (232448 - 1024 - 4096) / stage_bytes(bn, pair);
+// SPLIT: half an SM's shared memory and registers per CTA, so that two CTAs share an SM, and room for the other
+// parts' shares of this CTA's columns
+__host__ __device__ constexpr int part_bytes(int bn, bool split) { return split ? BM * bn * 4 : 0; }
+__host__ __device__ constexpr int stages(int bn, bool pair, bool split) {
+    const int n = ((split ? 113664 : 232448) - 1024 - 4096 - part_bytes(bn, split)) / stage_bytes(bn, pair);
     return n > 10 ? 10 : n;
 }
-__host__ __device__ constexpr int smem_bytes(int bn, bool pair) {
-    return 1024 + stages(bn, pair) * stage_bytes(bn, pair);
+__host__ __device__ constexpr int smem_bytes(int bn, bool pair, bool split) {
+    return 1024 + stages(bn, pair, split) * stage_bytes(bn, pair) + part_bytes(bn, split);
 }
 __host__ __device__ constexpr int tmem_need(int bn) { return 2 * bn + kSfSlots * sf_cols(bn); }
 __host__ __device__ constexpr int tmem_cols(int bn) {
@@ -174,12 +177,10 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t rank, float v) {
     uint32_t a;
-    float v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
 }
 
 struct ScaleRows {
@@ -194,7 +195,8 @@ struct Fp8Params {
     int64_t ldd, M, N;                                 // rows of A, rows of B
     int kb, a_type, b_type, accumulate;
     bool vec;                                          // 16-byte stores into the rows of out
-    int tiles_m, tiles_n, splits;
+    int tiles_m, tiles_n;
+    int part_kb, part_more;                            // SPLIT: k-blocks of a part; the first part_more have one more
 };
 
 // Up to four scales of one row as a word.  Rows and k-blocks that do not exist get any valid scale (1): their
@@ -218,10 +220,11 @@ __device__ __forceinline__ void tile_origin(const Fp8Params& p, int tile, int bn
 }
 
 // TRANS: D[i][j] is stored at out[j][i] (the caller swapped the operands); consecutive lanes hold consecutive i.
-template <int BN, typename T, bool TRANS, bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1)
+// SPLIT: gridDim = (parts, tiles), the parts of a tile are a cluster.  PAIR: gridDim = (2, pairs).
+template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, SPLIT ? 2 : 1)
 gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Fp8Params prm) {
-    constexpr int STAGES = stages(BN, PAIR), STAGE = stage_bytes(BN, PAIR), SFB = sfb_blocks(BN);
+    constexpr int STAGES = stages(BN, PAIR, SPLIT), STAGE = stage_bytes(BN, PAIR), SFB = sfb_blocks(BN);
     constexpr bool CHUNKED = sizeof(T) == 4;           // FP32 results: chains of four k-blocks
     constexpr int CW = BN >= 64 ? BN / 2 : BN;         // columns of an epilogue warp (two warps share a lane quarter)
     constexpr int COLS = tmem_cols(BN);
@@ -234,6 +237,10 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     __shared__ int abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmB) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&full_bar[s], 1);
@@ -261,16 +268,18 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (PAIR) cluster_sync();                          // the pair's barriers exist before the other CTA uses them
+    if (PAIR || SPLIT) cluster_sync();                 // the other CTAs of the cluster run, and their barriers exist
+    lm::after_previous();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot, tmem_sf = tmem + 2 * BN;
     volatile int* abort_p = &abort_flag;
 
     // this CTA's part of the contraction (whole k-blocks) and its tiles; its place in the pair
-    const int S = PAIR ? 1 : prm.splits, rank = S > 1 ? (int)blockIdx.x % S : 0, side = PAIR ? (int)blockIdx.x & 1 : 0;
-    const int kb0 = (int)((int64_t)prm.kb * rank / S), kb1 = (int)((int64_t)prm.kb * (rank + 1) / S);
-    const int share = PAIR ? 2 : S;                    // CTAs that share a tile
-    const int tile0 = (int)blockIdx.x / share, tile_step = (int)gridDim.x / share, tiles = prm.tiles_m * prm.tiles_n;
+    const int S = SPLIT ? (int)gridDim.x : 1, rank = SPLIT ? (int)blockIdx.x : 0, side = PAIR ? (int)blockIdx.x : 0;
+    const int kb0 = SPLIT ? rank * prm.part_kb + min(rank, prm.part_more) : 0;
+    const int kb1 = SPLIT ? kb0 + prm.part_kb + (rank < prm.part_more) : prm.kb;
+    const int tile0 = PAIR || SPLIT ? (int)blockIdx.y : (int)blockIdx.x, tiles = prm.tiles_m * prm.tiles_n;
+    const int tile_step = PAIR || SPLIT ? (int)gridDim.y : (int)gridDim.x;
 
     // Warps 0 and 1 run their loops as a whole, with one elected lane issuing: what the instructions name is then the
     // same for the warp and stays in uniform registers (issued by a lone lane, 4 products with their waits and
@@ -434,16 +443,19 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         int ac = 0;
         bool ok = true;
         T* out = static_cast<T*>(prm.out);
-        float* part = reinterpret_cast<float*>(smem);  // split contraction: [BN][128], over the operand ring
+        const uint32_t parts = smem_u32(smem + STAGES * STAGE);        // SPLIT: [part][column of the share][128]
+        const int own = SPLIT ? BN / S : 1;            // columns of a CTA's share
         for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
             int64_t m0, n0;
             tile_origin<PAIR>(prm, tile, BN, m0, n0);
             const int64_t row = m0 + side * BM + q * 32 + lane;
             // w columns from column c of the tile, in f
             auto put = [&](int c, const float* f, int w) {
-                if (S > 1) {
-#pragma unroll
-                    for (int j = 0; j < w; ++j) part[(c + j) * BM + q * 32 + lane] = f[j];
+                if (SPLIT) {
+                    for (int j = 0; j < w; ++j) {      // to the CTA that adds up this column
+                        const int to = (c + j) / own;
+                        st_cluster(parts + 4 * ((rank * own + (c + j) - to * own) * BM + q * 32 + lane), to, f[j]);
+                    }
                     return;
                 }
                 if (row >= prm.M) return;
@@ -530,28 +542,25 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         }
     }
     __syncwarp();
-    if (S > 1) {
-        // one tile per cluster: each CTA adds up its share of the tile's columns over all parts
+    if (SPLIT) {
+        // one tile per cluster: the parts of this CTA's columns are here once all have arrived, and nothing is
+        // written to or read from another CTA after that
         cluster_sync();
         int64_t m0, n0;
         tile_origin<PAIR>(prm, tile0, BN, m0, n0);
-        const int j0 = BN * rank / S, j1 = BN * (rank + 1) / S;
-        const uint32_t base = smem_u32(smem);
+        const int own = BN / S;
+        const float* part = reinterpret_cast<const float*>(smem + STAGES * STAGE);
         T* out = static_cast<T*>(prm.out);
         if (!abort_flag) {
-            for (int e = j0 * BM + threadIdx.x; e < j1 * BM; e += kThreads) {
-                const int64_t row = m0 + (e & (BM - 1)), col = n0 + e / BM;
+            for (int e = threadIdx.x; e < own * BM; e += kThreads) {
+                const int64_t row = m0 + (e & (BM - 1)), col = n0 + rank * own + e / BM;
                 if (row >= prm.M || col >= prm.N) continue;
-                float p[kMaxSplits], v = 0.f;          // all loads before the first sum
-#pragma unroll
-                for (int s = 0; s < kMaxSplits; ++s) p[s] = s < S ? ld_cluster(base + 4 * e, s) : 0.f;
-#pragma unroll
-                for (int s = 0; s < kMaxSplits; ++s) v += p[s];
+                float v = 0.f;
+                for (int s = 0; s < S; ++s) v += part[s * own * BM + e];
                 T* o = TRANS ? out + col * prm.ldd + row : out + row * prm.ldd + col;
                 *o = lm::from_f32<T>(prm.accumulate ? v + lm::to_f32(*o) : v);
             }
         }
-        cluster_sync();                                // shared memory of all parts stays until all have read it
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
@@ -584,12 +593,12 @@ struct Operand {
 };
 struct Config { int bn, splits; bool trans, pair; };
 
-template <int BN, typename T, bool TRANS, bool PAIR>
+template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT>
 gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, int splits, cudaStream_t st) {
     CUtensorMap tmA, tmB;
     if (!make_map_2d(&tmA, a.q, a.rows, K, a.ld, BM) || !make_map_2d(&tmB, b.q, b.rows, K, b.ld, b_rows(BN, PAIR))) return GPD_ERR_CUDA;
-    auto kernel = gemm_fp8_kernel<BN, T, TRANS, PAIR>;
-    constexpr int smem = smem_bytes(BN, PAIR), rows = PAIR ? 2 * BM : BM;
+    auto kernel = gemm_fp8_kernel<BN, T, TRANS, PAIR, SPLIT>;
+    constexpr int smem = smem_bytes(BN, PAIR, SPLIT), rows = PAIR ? 2 * BM : BM;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
     prm.sa = a.s;
     prm.sb = b.s;
@@ -599,23 +608,13 @@ gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, 
     prm.b_type = b.type == GPD_DT_E5M2;
     prm.tiles_m = (int)((a.rows + rows - 1) / rows);
     prm.tiles_n = (int)((b.rows + BN - 1) / BN);
-    prm.splits = splits;
+    prm.part_kb = prm.kb / splits;
+    prm.part_more = prm.kb % splits;
     const int64_t tiles = (int64_t)prm.tiles_m * prm.tiles_n;
     if (tiles > 0x3fffffff) return GPD_ERR_SHAPE;
-    cudaLaunchConfig_t cfg{};
     const int cluster = PAIR ? 2 : splits;
-    cfg.gridDim = dim3((unsigned)(splits > 1 ? tiles * splits : cluster * std::min<int64_t>(tiles, sm_count() / cluster)));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kernel, tmA, tmB, prm) != cudaSuccess) return GPD_ERR_CUDA;
-    return launch_ok();
+    const unsigned n = (unsigned)(SPLIT ? tiles : std::min<int64_t>(tiles, sm_count() / cluster));
+    return lm::launch_after(kernel, PAIR || SPLIT ? dim3(cluster, n) : dim3(n), dim3(kThreads), smem, cluster, st, tmA, tmB, prm);
 }
 
 // Tile width, orientation, pairing and split by the smallest estimated time.  A k-block of a 128 x BN tile (per
@@ -634,8 +633,9 @@ Config choose(int64_t M, int64_t N, int kb, bool f32) {
                 const int height = pair ? 2 * BM : BM, slots = pair ? sms / 2 : sms;
                 const int64_t tiles = ((rows + height - 1) / height) * ((cols + bn - 1) / bn);
                 for (int s = 1; s <= (pair ? 1 : kMaxSplits); s *= 2) {
-                    if (s > 1 && (s > kb || tiles * s > 2 * sms)) continue;
-                    const double waves = (double)((tiles * s + slots - 1) / slots);
+                    if (s > 1 && (bn > 64 || s > kb || tiles * s > 2 * sms)) continue;
+                    // two CTAs of a split product share an SM
+                    const double waves = s > 1 ? std::max(1.0, (double)(tiles * s) / sms) : (double)((tiles + slots - 1) / slots);
                     const double block = std::max(2.0 * bn, (BM + b_rows(bn, pair)) * 128 / 48.0);
                     const double time = waves * (((kb + s - 1) / s) * block + (s > 1 ? 3000.0 : 1500.0));
                     if (time < best_t * 0.999) {
@@ -652,18 +652,18 @@ Config choose(int64_t M, int64_t N, int kb, bool f32) {
 template <typename T, bool TRANS>
 gpd_status launch_bn(const Operand& a, const Operand& b, const Fp8Params& prm, int64_t K, const Config& c, cudaStream_t st) {
     switch (c.pair ? -c.bn : c.bn) {
-        case 16: return launch<16, T, TRANS, false>(a, b, prm, K, c.splits, st);
-        case 32: return launch<32, T, TRANS, false>(a, b, prm, K, c.splits, st);
-        case 64: return launch<64, T, TRANS, false>(a, b, prm, K, c.splits, st);
-        case 128: return launch<128, T, TRANS, false>(a, b, prm, K, c.splits, st);
-        case 192: return launch<192, T, TRANS, false>(a, b, prm, K, c.splits, st);
-        case -128: return launch<128, T, TRANS, true>(a, b, prm, K, 1, st);
-        case -192: return launch<192, T, TRANS, true>(a, b, prm, K, 1, st);
+        case 16: return c.splits > 1 ? launch<16, T, TRANS, false, true>(a, b, prm, K, c.splits, st) : launch<16, T, TRANS, false, false>(a, b, prm, K, 1, st);
+        case 32: return c.splits > 1 ? launch<32, T, TRANS, false, true>(a, b, prm, K, c.splits, st) : launch<32, T, TRANS, false, false>(a, b, prm, K, 1, st);
+        case 64: return c.splits > 1 ? launch<64, T, TRANS, false, true>(a, b, prm, K, c.splits, st) : launch<64, T, TRANS, false, false>(a, b, prm, K, 1, st);
+        case 128: return launch<128, T, TRANS, false, false>(a, b, prm, K, 1, st);
+        case 192: return launch<192, T, TRANS, false, false>(a, b, prm, K, 1, st);
+        case -128: return launch<128, T, TRANS, true, false>(a, b, prm, K, 1, st);
+        case -192: return launch<192, T, TRANS, true, false>(a, b, prm, K, 1, st);
         default: break;
     }
     if constexpr (sizeof(T) == 2) {
-        if (c.pair) return launch<224, T, TRANS, true>(a, b, prm, K, 1, st);
-        return launch<224, T, TRANS, false>(a, b, prm, K, c.splits, st);
+        if (c.pair) return launch<224, T, TRANS, true, false>(a, b, prm, K, 1, st);
+        return launch<224, T, TRANS, false, false>(a, b, prm, K, 1, st);
     }
     return GPD_ERR_UNSUPPORTED;
 }

@@ -166,6 +166,33 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// ---- launches ------------------------------------------------------------------------------------------
+// The operators' kernels are launched so that a kernel's start-up (its launch, barriers, tensor memory) overlaps
+// the end of the kernel before it in the stream: each calls `after_previous` before it touches memory, which waits
+// for that kernel's completion, and thereby lets the next one start.
+__device__ __forceinline__ void after_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+// cluster: CTAs per cluster along x (1: none)
+template <typename... P, typename... A>
+gpd_status launch_after(void (*kernel)(P...), dim3 grid, dim3 block, int smem, int cluster, cudaStream_t st, const A&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
+
 // ---- host side: argument checks ---------------------------------------------------------------------
 inline int dtype_size(int t) { return t == GPD_DT_F32 ? 4 : (t == GPD_DT_BF16 || t == GPD_DT_F16) ? 2 : 1; }
 inline bool is_float_type(int t) { return t == GPD_DT_F32 || t == GPD_DT_BF16 || t == GPD_DT_F16; }

@@ -295,6 +295,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogprobA
     __shared__ Stats scratch[32];
     __shared__ Stats part;
     __shared__ typename std::conditional<TOP, TopShared, int>::type top;
+    after_previous();
     const int C = a.C, rank = C > 1 ? blockIdx.x % C : 0;
     const int64_t t = blockIdx.x / C;
     const T* row = static_cast<const T*>(a.logits) + t * a.ld;
@@ -357,6 +358,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_backward_kernel(const
     __shared__ float g[kMaxTokens], x_at[kMaxTokens];
     __shared__ int at[kMaxTokens];
     constexpr int N = 16 / sizeof(T);
+    after_previous();
     const int64_t t = blockIdx.x / a.parts;
     const T* row = static_cast<const T*>(a.logits) + t * a.ld;
     T* d = static_cast<T*>(a.d) + t * a.ldd;
@@ -445,6 +447,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
     __shared__ float q[kMaxTeacher], x_at[kMaxTeacher], red[32];
     __shared__ int at[kMaxTeacher];
     constexpr int N = 16 / sizeof(T);
+    after_previous();
     const int C = a.C, rank = C > 1 ? blockIdx.x % C : 0;
     const int64_t t = blockIdx.x / C;
     const T* row = static_cast<const T*>(a.logits) + t * a.ld;
@@ -542,18 +545,7 @@ unsigned row_threads(int64_t entries) { return entries >= 8192 ? 512 : entries >
 template <typename... P, typename A>
 gpd_status launch_rows(void (*kernel)(P...), const A& a, int64_t T, int C, unsigned threads, cudaStream_t st) {
     if (T * C > 0x7fffffff) return GPD_ERR_SHAPE;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(T * C));
-    cfg.blockDim = dim3(threads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)C;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = C > 1 ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) return GPD_ERR_CUDA;
-    return launch_ok();
+    return launch_after(kernel, dim3((unsigned)(T * C)), dim3(threads), 0, C, st, a);
 }
 template <typename T>
 gpd_status launch_logprobs(LogprobArgs a, int64_t rows, cudaStream_t st) {

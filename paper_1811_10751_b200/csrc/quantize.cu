@@ -78,6 +78,7 @@ template <typename T, int Q, bool SQUARE, bool VEC>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const CutArgs a, int tiles_k) {
     __shared__ __align__(16) uint8_t tile[kBlock * kBlock];
     __shared__ uint32_t colmax[16][kBlock];
+    after_previous();
     const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
     const int64_t bm = blockIdx.x / tiles_k, bk = blockIdx.x % tiles_k;
     const int64_t r0 = bm * kBlock + 8 * rg, c0 = bk * kBlock + 8 * cg;
@@ -190,14 +191,9 @@ gpd_status launch_cut(const CutArgs& a, bool square, cudaStream_t st) {
     if (tk * tm > 0x7fffffff) return GPD_ERR_SHAPE;
     const unsigned grid = (unsigned)(tk * tm);
     const bool vec = rows_aligned(a.src, a.ld, sizeof(T)) && rows_aligned(a.q, a.ldq, 1, 8) && rows_aligned(a.qT, a.ldqT, 1);
-    if (square) {
-        if (vec) cut_kernel<T, Q, true, true><<<grid, 256, 0, st>>>(a, (int)tk);
-        else cut_kernel<T, Q, true, false><<<grid, 256, 0, st>>>(a, (int)tk);
-    } else {
-        if (vec) cut_kernel<T, Q, false, true><<<grid, 256, 0, st>>>(a, (int)tk);
-        else cut_kernel<T, Q, false, false><<<grid, 256, 0, st>>>(a, (int)tk);
-    }
-    return launch_ok();
+    auto kernel = square ? (vec ? cut_kernel<T, Q, true, true> : cut_kernel<T, Q, true, false>)
+                         : (vec ? cut_kernel<T, Q, false, true> : cut_kernel<T, Q, false, false>);
+    return launch_after(kernel, dim3(grid), dim3(256), 0, 1, st, a, (int)tk);
 }
 template <typename T>
 gpd_status launch_cut_q(const CutArgs& a, int q_type, bool square, cudaStream_t st) {

@@ -48,6 +48,7 @@ __device__ __forceinline__ float row_sum(float v, int G, int g, float* scratch) 
 template <typename T, typename W, int Q, int VPT, bool VEC>
 __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const NormArgs a) {
     __shared__ float scratch[32];
+    after_previous();
     const int G = blockDim.x;
     const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (t >= a.T) return;                              // a whole warp (G = 32) or, with one row per CTA, never
@@ -151,10 +152,9 @@ gpd_status launch_norm(const NormArgs& a, cudaStream_t st) {
     if (vecs <= 128) {                                 // a warp per row, four rows per CTA: no barrier
         const dim3 block(32, 4);
         const unsigned grid = (unsigned)((a.T + 3) / 4);
-        if (vecs <= 32) rmsnorm_kernel<T, W, Q, 1, VEC><<<grid, block, 0, st>>>(a);
-        else if (vecs <= 64) rmsnorm_kernel<T, W, Q, 2, VEC><<<grid, block, 0, st>>>(a);
-        else rmsnorm_kernel<T, W, Q, 4, VEC><<<grid, block, 0, st>>>(a);
-        return launch_ok();
+        if (vecs <= 32) return launch_after(rmsnorm_kernel<T, W, Q, 1, VEC>, dim3(grid), block, 0, 1, st, a);
+        if (vecs <= 64) return launch_after(rmsnorm_kernel<T, W, Q, 2, VEC>, dim3(grid), block, 0, 1, st, a);
+        return launch_after(rmsnorm_kernel<T, W, Q, 4, VEC>, dim3(grid), block, 0, 1, st, a);
     }
     // Many rows: few threads with many vectors each, so that many rows are in flight on an SM and a barrier
     // holds few warps.  Few rows: many threads, for the latency of one row.
@@ -163,12 +163,11 @@ gpd_status launch_norm(const NormArgs& a, cudaStream_t st) {
     const int vpt = vecs > 512 * kMost ? 0 : many || vecs > 2048 ? kMost : vecs > 1024 ? 4 : 2;
     const int threads = vpt ? (int)(((vecs + vpt - 1) / vpt + 31) / 32 * 32) : 1024;
     switch (vpt) {
-        case 2: rmsnorm_kernel<T, W, Q, 2, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
-        case 4: rmsnorm_kernel<T, W, Q, 4, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
-        case kMost == 8 ? 8 : -1: rmsnorm_kernel<T, W, Q, kMost, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
-        default: rmsnorm_kernel<T, W, Q, 0, VEC><<<(unsigned)a.T, threads, 0, st>>>(a); break;
+        case 2: return launch_after(rmsnorm_kernel<T, W, Q, 2, VEC>, dim3((unsigned)a.T), dim3(threads), 0, 1, st, a);
+        case 4: return launch_after(rmsnorm_kernel<T, W, Q, 4, VEC>, dim3((unsigned)a.T), dim3(threads), 0, 1, st, a);
+        case kMost == 8 ? 8 : -1: return launch_after(rmsnorm_kernel<T, W, Q, kMost, VEC>, dim3((unsigned)a.T), dim3(threads), 0, 1, st, a);
+        default: return launch_after(rmsnorm_kernel<T, W, Q, 0, VEC>, dim3((unsigned)a.T), dim3(threads), 0, 1, st, a);
     }
-    return launch_ok();
 }
 template <typename T, typename W, int Q>
 gpd_status launch_norm_q(const NormArgs& a, cudaStream_t st) {
@@ -203,6 +202,7 @@ template <typename T, typename W, int VPT, bool VEC>
 __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward_kernel(const NormBwdArgs a) {
     __shared__ float scratch[16][2][32];
     extern __shared__ float dw_rows[];                 // [R - 1][8 VPT G]
+    after_previous();
     const int G = blockDim.x, g = threadIdx.y;
     const W* wt = static_cast<const W*>(a.weight);
     float* part = a.parts + (int64_t)blockIdx.x * a.H;
@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
 // dw_c = sum over the partial rows, in a fixed order: sixteen threads per column, then their sums.
 __global__ void __launch_bounds__(512) rmsnorm_dweight_kernel(const float* parts, int n, int64_t H, float* dw) {
     __shared__ float s[16][33];
+    after_previous();
     const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
     float v = 0.f;
     if (c < H)
@@ -338,19 +339,21 @@ gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
     int R = loop ? 1 : std::max(1, std::min(kBwdThreads / G, 15));      // named barriers 1 .. 15
     R = (int)std::max<int64_t>(1, std::min<int64_t>(R, (a.T + sm_count() - 1) / sm_count()));
     const int parts = (int)std::min<int64_t>(std::min<int64_t>((a.T + R - 1) / R, sm_count()), GPD_RMSNORM_MAX_PARTS);
+    gpd_status rc = GPD_OK;
     if (parts > 0) {
         const int smem = (R - 1) * 8 * V * G * (int)sizeof(float);      // at most 512 * 32 floats
         if (loop) {
-            rmsnorm_backward_kernel<T, W, 0, VEC><<<parts, 1024, 0, st>>>(a);
+            rc = launch_after(rmsnorm_backward_kernel<T, W, 0, VEC>, dim3(parts), dim3(1024), 0, 1, st, a);
         } else {
             auto kernel = rmsnorm_backward_kernel<T, W, V, VEC>;
             if (smem > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
                 return GPD_ERR_CUDA;
-            kernel<<<parts, dim3(G, R), smem, st>>>(a);
+            rc = launch_after(kernel, dim3(parts), dim3(G, R), smem, 1, st, a);
         }
     }
-    rmsnorm_dweight_kernel<<<(unsigned)((a.H + 31) / 32), dim3(32, 16), 0, st>>>(a.parts, parts, a.H, dweight);
-    return launch_ok();
+    if (rc != GPD_OK) return rc;
+    const float* partial = a.parts;
+    return launch_after(rmsnorm_dweight_kernel, dim3((unsigned)((a.H + 31) / 32)), dim3(32, 16), 0, 1, st, partial, parts, a.H, dweight);
 }
 template <typename T, typename W>
 gpd_status launch_bwd_w(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
