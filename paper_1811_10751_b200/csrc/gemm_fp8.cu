@@ -16,15 +16,16 @@
 // of 128 bytes per row under the 128-byte swizzle, a ring that runs on across tiles).  Warps 2..5 bring the
 // scales: a word holds one row's scales of four k-blocks, and the tensor cores want the words of rows
 // i, i + 32, i + 64, i + 96 in lane i of four columns of tensor memory, the same in each quarter of the lanes;
-// each warp writes one quarter (tcgen05.st), up to four groups of k-blocks ahead.  (Copies from shared memory
+// each warp writes one quarter (tcgen05.st), up to two chunks of eight k-blocks ahead.  (Copies from shared memory
 // by the issuing lane, tcgen05.cp, stop the products around them: 850 instead of 450 cycles a k-block.)
 // Warp 1: one lane issues the products.  Warps 6..13 read the accumulators back, two sets of which alternate,
 // and store.
 //
 // Accumulation.  tcgen05.mma adds into its FP32 accumulator with truncation.  16-bit results take one chain
 // over the whole contraction: the bias (about 2^-25 of the sum per instruction, 8e-6 at K = 8192) is far
-// below their own rounding.  FP32 results cut the chain every four k-blocks (16 instructions) and add the
-// pieces in registers, rounded to nearest.
+// below their own rounding.  FP32 results cut the chain every eight k-blocks (32 instructions) and add the
+// pieces in registers, rounded to nearest: 4096 x 4096 x 4100 is then 1.0e-7 off the exact product, a plain FP32
+// product 1.0e-7.  (Pieces of four k-blocks: the reading of tensor memory holds the tensor cores up.)
 //
 // Few tiles (short A and B, long K): the CTAs of a cluster take a part of the contraction each; the parts
 // meet through distributed shared memory and are added in the order of the parts.
@@ -51,23 +52,30 @@ using tc::umma_commit;
 
 constexpr int BM = 128, BK = 128, UMMA_K = 32;
 constexpr int kSfWarps = 4, kEpiWarps = 8, kThreads = 32 * (2 + kSfWarps + kEpiWarps);
+constexpr int kChunk = 8;                              // k-blocks whose scales arrive together; FP32 results: added up in tensor memory
 constexpr int kMaxSplits = 8;                          // parts of a split contraction (CTAs of a cluster)
-constexpr int kSfSlots = 4;                            // groups of four k-blocks whose scales are in flight
+constexpr int kSfSlots = 2;                            // chunks whose scales are in flight
 __host__ __device__ constexpr int b_rows(int bn, bool pair) { return pair ? bn / 2 : bn; }
 __host__ __device__ constexpr int stage_bytes(int bn, bool pair) { return (BM + b_rows(bn, pair)) * BK; }
 __host__ __device__ constexpr int sfb_blocks(int bn) { return bn > 128 ? 2 : 1; }
-__host__ __device__ constexpr int sf_cols(int bn) { return 4 * (1 + sfb_blocks(bn)); }   // of tensor memory, per slot
+__host__ __device__ constexpr int sf_cols(int bn) { return 4 * (1 + sfb_blocks(bn)); }   // of tensor memory, per four k-blocks
 // SPLIT: half an SM's shared memory and registers per CTA, so that two CTAs share an SM, and room for the other
-// parts' shares of this CTA's columns
-__host__ __device__ constexpr int part_bytes(int bn, bool split) { return split ? BM * bn * 4 : 0; }
-__host__ __device__ constexpr int stages(int bn, bool pair, bool split) {
-    const int n = ((split ? 113664 : 232448) - 1024 - 4096 - part_bytes(bn, split)) / stage_bytes(bn, pair);
+// parts' shares of this CTA's columns.  Otherwise: room for 32 x 32 results per epilogue warp on their way out
+// (elem: bytes of one; 0: results are stored from registers alone).
+__host__ __device__ constexpr int extra_bytes(int bn, bool split, int elem) {
+    return split ? BM * bn * 4 : kEpiWarps * 32 * 32 * elem;
+}
+__host__ __device__ constexpr int stages(int bn, bool pair, bool split, int elem) {
+    const int n = ((split ? 113664 : 232448) - 1024 - 8192 - extra_bytes(bn, split, elem)) / stage_bytes(bn, pair);
     return n > 10 ? 10 : n;
 }
-__host__ __device__ constexpr int smem_bytes(int bn, bool pair, bool split) {
-    return 1024 + stages(bn, pair, split) * stage_bytes(bn, pair) + part_bytes(bn, split);
+__host__ __device__ constexpr int smem_bytes(int bn, bool pair, bool split, int elem) {
+    return 1024 + stages(bn, pair, split, elem) * stage_bytes(bn, pair) + extra_bytes(bn, split, elem);
 }
-__host__ __device__ constexpr int tmem_need(int bn) { return 2 * bn + kSfSlots * sf_cols(bn); }
+// Bytes of a result where they leave through shared memory and a copy engine (whole lines; stores from the
+// registers of a row's thread, 16 bytes of 32 rows at a time, held the copies of the next tile up)
+__host__ __device__ constexpr int staged_elem(int bn, bool trans, bool split, int elem) { return !trans && !split && bn >= 64 ? elem : 0; }
+__host__ __device__ constexpr int tmem_need(int bn) { return 2 * bn + kSfSlots * 2 * sf_cols(bn); }
 __host__ __device__ constexpr int tmem_cols(int bn) {
     return tmem_need(bn) <= 64 ? 64 : tmem_need(bn) <= 128 ? 128 : tmem_need(bn) <= 256 ? 256 : 512;
 }
@@ -120,6 +128,20 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, i
         asm volatile(
             "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
             ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+// 32 x 32 results from shared memory to (column, row) of the output; what lies beyond it is left out
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// Whether the phase is over, without waiting
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
 }
 // Arrival, at the barrier of every CTA of the tile, once the tensor cores are done with what was issued so far
 template <bool PAIR>
@@ -195,6 +217,7 @@ struct Fp8Params {
     int64_t ldd, M, N;                                 // rows of A, rows of B
     int kb, a_type, b_type, accumulate;
     bool vec;                                          // 16-byte stores into the rows of out
+    bool copy_out;                                     // results leave through shared memory (tmD)
     int tiles_m, tiles_n;
     int part_kb, part_more;                            // SPLIT: k-blocks of a part; the first part_more have one more
 };
@@ -223,16 +246,18 @@ __device__ __forceinline__ void tile_origin(const Fp8Params& p, int tile, int bn
 // SPLIT: gridDim = (parts, tiles), the parts of a tile are a cluster.  PAIR: gridDim = (2, pairs).
 template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, SPLIT ? 2 : 1)
-gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Fp8Params prm) {
-    constexpr int STAGES = stages(BN, PAIR, SPLIT), STAGE = stage_bytes(BN, PAIR), SFB = sfb_blocks(BN);
-    constexpr bool CHUNKED = sizeof(T) == 4;           // FP32 results: chains of four k-blocks
-    constexpr int CW = BN >= 64 ? BN / 2 : BN;         // columns of an epilogue warp (two warps share a lane quarter)
+gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                const __grid_constant__ CUtensorMap tmD, const Fp8Params prm) {
+    constexpr int STAGED = staged_elem(BN, TRANS, SPLIT, sizeof(T)), STAGES = stages(BN, PAIR, SPLIT, STAGED), STAGE = stage_bytes(BN, PAIR), SFB = sfb_blocks(BN);
+    constexpr bool CHUNKED = sizeof(T) == 4;           // FP32 results: one chain per chunk
+    // columns of an epilogue warp, in units of 32: two warps share a lane quarter, of narrow tiles one does it all
+    constexpr int W0 = BN >= 64 ? (BN / 32 + 1) / 2 * 32 : BN, W1 = BN - W0;
     constexpr int COLS = tmem_cols(BN);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], sf_full[kSfSlots], sf_empty[kSfSlots],
         acc_full[2], acc_empty[2];
-    __shared__ __align__(16) uint4 sf_words[2][(1 + SFB) * 32];
+    __shared__ __align__(16) uint4 sf_words[2][2 * (1 + SFB) * 32];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -321,35 +346,37 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             const uint32_t idesc0 = idesc_mx(PAIR ? 2 * BM : BM, BN, prm.a_type, prm.b_type, 0);
             int s = 0, gs = 0, set = 0;                // stage, scale slot and accumulator set in turn, and their phases
             uint32_t phase = 0, gphase = 0, aphase = 1;
-            bool live = true;
+            bool live = true, ready = false;           // ready: the stage's operands are known to be there
             for (int tile = tile0; tile < tiles; tile += tile_step) {
                 bool fresh = true;                     // the next product starts a chain
-                for (int g = kb0 >> 2; 4 * g < kb1; ++g) {
+                for (int c = kb0 / kChunk; kChunk * c < kb1; ++c) {
                     if (fresh) live = live && mbar_wait_relaxed(&acc_empty[set], aphase, abort_p);
                     live = live && mbar_wait_relaxed(&sf_full[gs], gphase, abort_p);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t sf = tmem_sf + gs * sf_cols(BN), d = tmem + set * BN;
+                    const uint32_t sf = tmem_sf + gs * 2 * sf_cols(BN), d = tmem + set * BN;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int kb = 4 * g + i;
-                        if (kb < kb0 || kb >= kb1) continue;
-                        live = live && mbar_wait(&full_bar[s], phase, abort_p);
+                    for (int i = 0; i < kChunk; ++i) {
+                        if (kChunk * c + i < kb0 || kChunk * c + i >= kb1) continue;
+                        if (!ready) live = live && mbar_wait(&full_bar[s], phase, abort_p);
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint64_t a = desc0 + (uint64_t)((s * STAGE) >> 4), b = a + (uint64_t)((BM * BK) >> 4);
-                        const uint32_t idesc = idesc0 | (uint32_t)i << 4 | (uint32_t)i << 29;      // byte i of the scale words
-                        if (one && live) {
-#pragma unroll
-                            for (int k = 0; k < BK / UMMA_K; ++k)
-                                umma_mx<PAIR>(d, a + k * (UMMA_K >> 4), b + k * (UMMA_K >> 4), idesc, sf, sf + 4, !(fresh && k == 0));
-                            commit<PAIR>(&empty_bar[s]);
-                        }
-                        fresh = false;
+                        // byte i % 4 of the scale words of the chunk's first or second half
+                        const uint32_t idesc = idesc0 | (uint32_t)(i & 3) << 4 | (uint32_t)(i & 3) << 29;
+                        const uint32_t w = sf + (i >> 2) * sf_cols(BN);
+                        uint64_t* done = &empty_bar[s];
                         if (++s == STAGES) {
                             s = 0;
                             phase ^= 1;
                         }
+                        ready = mbar_test(&full_bar[s], phase);        // the next stage, looked at while this one is issued
+                        if (one && live) {
+#pragma unroll
+                            for (int k = 0; k < BK / UMMA_K; ++k)
+                                umma_mx<PAIR>(d, a + k * (UMMA_K >> 4), b + k * (UMMA_K >> 4), idesc, w, w + 4, !(fresh && k == 0));
+                            commit<PAIR>(done);
+                        }
+                        fresh = false;
                     }
-                    const bool end = CHUNKED || 4 * g + 4 >= kb1;      // of the chain
+                    const bool end = CHUNKED || kChunk * (c + 1) >= kb1;       // of the chain
                     if (one && live) {
                         commit<PAIR>(&sf_empty[gs]);
                         if (end) commit<PAIR>(&acc_full[set]);
@@ -369,12 +396,12 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         __syncwarp();
     } else if (warp < 2 + kSfWarps) {
         // Warp q of the four fetches the words of rows 32 q + lane of every block of 128; the warps exchange them
-        // through shared memory, and each writes all of them to its quarter.  Words are fetched kAhead groups before
-        // they are wanted.
-        constexpr int NB = 1 + SFB, kAhead = 4;
+        // through shared memory, and each writes all of them to its quarter.  A chunk's words are fetched two chunks
+        // before they are wanted.
+        constexpr int NB = 1 + SFB;
         const int q = warp & 3;
         const uint8_t* rows[NB];                       // this lane's scale rows of the tile being fetched; null: none
-        int tile = tile0, g = kb0 >> 2;                // the group to be fetched next
+        int tile = tile0, c = kb0 / kChunk;            // the chunk to be fetched next
         auto find_rows = [&]() {
             int64_t m0, n0;
             tile_origin<PAIR>(prm, tile, BN, m0, n0);
@@ -385,61 +412,64 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 rows[b] = r < s.rows ? s.p + (r >> s.shift) * s.ld : nullptr;
             }
         };
-        auto fetch = [&](uint32_t (&v)[NB]) {
+        auto fetch = [&](uint32_t (&v)[2][NB]) {
             if (tile >= tiles) return;
-            const bool whole = 4 * g + 4 <= prm.kb;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                v[b] = 0x7f7f7f7fu;
-                if (rows[b]) {
-                    if (whole && (b == 0 ? prm.sa.words : prm.sb.words)) v[b] = __ldg(reinterpret_cast<const uint32_t*>(rows[b] + 4 * g));
-                    else v[b] = scale_bytes(rows[b] + 4 * g, prm.kb - 4 * g);
+            for (int h = 0; h < 2; ++h) {
+                const int kb = kChunk * c + 4 * h;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    v[h][b] = 0x7f7f7f7fu;
+                    if (rows[b] && kb < prm.kb) {
+                        if (kb + 4 <= prm.kb && (b == 0 ? prm.sa.words : prm.sb.words)) v[h][b] = __ldg(reinterpret_cast<const uint32_t*>(rows[b] + kb));
+                        else v[h][b] = scale_bytes(rows[b] + kb, prm.kb - kb);
+                    }
                 }
             }
-            if (4 * (++g) >= kb1) {
-                g = kb0 >> 2;
+            if (kChunk * (++c) >= kb1) {
+                c = kb0 / kChunk;
                 tile += tile_step;
                 if (tile < tiles) find_rows();
             }
         };
-        const int groups = ((kb1 + 3) >> 2) - (kb0 >> 2);
-        const int total = tile0 < tiles ? groups * ((tiles - tile0 + tile_step - 1) / tile_step) : 0;
-        uint32_t ring[kAhead][NB];
+        const int chunks = (kb1 + kChunk - 1) / kChunk - kb0 / kChunk;
+        const int total = tile0 < tiles ? chunks * ((tiles - tile0 + tile_step - 1) / tile_step) : 0;
+        uint32_t ring[2][2][NB];
         if (total > 0) find_rows();
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) fetch(ring[i]);
+        fetch(ring[0]);
+        fetch(ring[1]);
         const uint32_t sf_full0 = PAIR ? in_leader(&sf_full[0]) : smem_u32(&sf_full[0]);
         bool live = true;
-        for (int g0 = 0; g0 < total; g0 += kAhead) {
+        for (int i0 = 0; i0 < total; i0 += 2) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int gi = g0 + i;
-                if (gi >= total) break;
-                uint32_t* buf = reinterpret_cast<uint32_t*>(sf_words[i & 1]);
+            for (int i = 0; i < 2; ++i) {              // chunk i0 + i: ring, exchange buffer and slot i
+                if (i0 + i >= total) break;
+                uint32_t* buf = reinterpret_cast<uint32_t*>(sf_words[i]);
 #pragma unroll
-                for (int b = 0; b < NB; ++b) buf[(b * 32 + lane) * 4 + q] = ring[i][b];
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) buf[((h * NB + b) * 32 + lane) * 4 + q] = ring[i][h][b];
                 fetch(ring[i]);
                 asm volatile("bar.sync 1, 128;" ::: "memory");
-                const int s = gi % kSfSlots;
-                live = live && mbar_wait(&sf_empty[s], ((gi / kSfSlots) & 1) ^ 1, abort_p);
+                live = live && mbar_wait(&sf_empty[i], ((i0 >> 1) & 1) ^ 1, abort_p);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    tmem_st4(tmem_sf + s * sf_cols(BN) + 4 * b + ((uint32_t)(q * 32) << 16), sf_words[i & 1][b * 32 + lane]);
+                for (int b = 0; b < 2 * NB; ++b)
+                    tmem_st4(tmem_sf + i * 2 * sf_cols(BN) + 4 * b + ((uint32_t)(q * 32) << 16), sf_words[i][b * 32 + lane]);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0 && live) mbar_arrive_relaxed(sf_full0 + 8 * s);
+                if (lane == 0 && live) mbar_arrive_relaxed(sf_full0 + 8 * i);
             }
         }
     } else {
         const int q = warp & 3, half = (warp - 2 - kSfWarps) >> 2;      // tcgen05.ld: a warp reads its quarter of the lanes
-        const int c0 = BN >= 64 ? half * CW : 0;
-        const bool idle = BN < 64 && half == 1;        // narrow tiles: four warps do it all
+        const int c0 = half * W0, width = half ? W1 : W0;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         const uint32_t acc_empty0 = PAIR ? in_leader(&acc_empty[0]) : smem_u32(&acc_empty[0]);
-        float acc[CHUNKED ? CW : 1];
+        float acc[CHUNKED ? W0 : 1];                   // FP32: W0 = W1 or W1 = 0
+        uint8_t* staging = smem + STAGES * STAGE + (warp - 2 - kSfWarps) * 32 * 32 * STAGED;
         int ac = 0;
         bool ok = true;
         T* out = static_cast<T*>(prm.out);
@@ -487,6 +517,35 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                     }
                 }
             };
+            // 32 columns from column c of the tile, by way of shared memory
+            auto copy_out = [&](int c, const float* f) {
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // the last ones have left
+                __syncwarp();
+                if constexpr (STAGED == 4) {           // rows of 128 bytes under the 128-byte swizzle
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<float4*>(staging + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+                } else if constexpr (STAGED == 2) {    // rows of 64 bytes under the 64-byte swizzle
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<uint4*>(staging + lane * 64 + ((j ^ ((lane >> 1) & 3)) * 16)) =
+                            make_uint4(lm::pack2(f[8 * j], f[8 * j + 1], T()), lm::pack2(f[8 * j + 2], f[8 * j + 3], T()),
+                                       lm::pack2(f[8 * j + 4], f[8 * j + 5], T()), lm::pack2(f[8 * j + 6], f[8 * j + 7], T()));
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                const int64_t r0 = m0 + side * BM + q * 32, col = n0 + c;
+                if (lane == 0 && r0 < prm.M && col < prm.N) tma_store_2d(&tmD, smem_u32(staging), (int)col, (int)r0);
+            };
+            auto emit = [&](int c, const float* f) {
+                if constexpr (STAGED != 0) {
+                    if (prm.copy_out) {
+                        copy_out(c, f);
+                        return;
+                    }
+                }
+                put(c, f, BN < 32 ? 16 : 32);
+            };
             auto release = [&](int set) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -497,49 +556,52 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 ok = __all_sync(0xffffffffu, r);       // tcgen05.ld is warp-collective: all lanes or none
                 if (ok) asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             };
+            constexpr int STEP = BN < 32 ? 16 : 32;    // columns at a time
+            auto read = [&](uint32_t taddr, uint32_t (&r)[STEP]) {
+                tmem_ld16(r, taddr);
+                if constexpr (STEP == 32) tmem_ld16(r + 16, taddr + 16);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            };
             if constexpr (CHUNKED) {
 #pragma unroll
-                for (int j = 0; j < CW; ++j) acc[j] = 0.f;
-                for (int g = kb0 >> 2; 4 * g < kb1 && ok; ++g, ++ac) {
+                for (int j = 0; j < W0; ++j) acc[j] = 0.f;
+                for (int k = kb0 / kChunk; kChunk * k < kb1 && ok; ++k, ++ac) {
                     ready(ac & 1, ac);
                     if (!ok) break;
                     const uint32_t base = tmem + (ac & 1) * BN + lane_base + c0;
-                    if (!idle) {
+                    if (width) {
 #pragma unroll
-                        for (int c = 0; c < CW; c += 16) {
-                            uint32_t r[16];
-                            tmem_ld16(r, base + c);
-                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        for (int c = 0; c < W0; c += STEP) {
+                            uint32_t r[STEP];
+                            read(base + c, r);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) acc[c + j] += __uint_as_float(r[j]);
+                            for (int j = 0; j < STEP; ++j) acc[c + j] += __uint_as_float(r[j]);
                         }
                     }
                     release(ac & 1);
                 }
-                if (ok && !idle) {
+                if (ok && width) {
 #pragma unroll
-                    for (int c = 0; c < CW; c += 16) put(c0 + c, acc + c, 16);
+                    for (int c = 0; c < W0; c += STEP) emit(c0 + c, acc + c);
                 }
             } else {
                 ready(ac & 1, ac);
                 if (!ok) break;
                 const uint32_t base = tmem + (ac & 1) * BN + lane_base + c0;
-                if (!idle) {
+                for (int c = 0; c < width; c += STEP) {
+                    uint32_t r[STEP];
+                    read(base + c, r);
+                    if (c + STEP >= width) release(ac & 1);
+                    float f[STEP];
 #pragma unroll
-                    for (int c = 0; c < CW; c += 16) {
-                        uint32_t r[16];
-                        tmem_ld16(r, base + c);
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                        float f[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(r[j]);
-                        put(c0 + c, f, 16);
-                    }
+                    for (int j = 0; j < STEP; ++j) f[j] = __uint_as_float(r[j]);
+                    emit(c0 + c, f);
                 }
-                release(ac & 1);
+                if (width == 0) release(ac & 1);
                 ++ac;
             }
         }
+        if (STAGED && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // written before the CTA ends
     }
     __syncwarp();
     if (SPLIT) {
@@ -585,6 +647,19 @@ bool make_map_2d(CUtensorMap* map, const void* base, int64_t rows, int64_t cols,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Output of `elem`-byte elements, written in boxes of 32 x 32.
+bool make_out_map(CUtensorMap* map, void* base, int64_t rows, int64_t cols, int64_t ld, int elem) {
+    tc::EncodeTiledFn fn = tc::encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)(ld * elem)};
+    cuuint32_t box[2] = {32, 32};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, elem == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, elem == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Operand {
     const void* q;
     int64_t ld, rows;
@@ -595,10 +670,13 @@ struct Config { int bn, splits; bool trans, pair; };
 
 template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT>
 gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, int splits, cudaStream_t st) {
-    CUtensorMap tmA, tmB;
+    constexpr int STAGED = staged_elem(BN, TRANS, SPLIT, sizeof(T));
+    CUtensorMap tmA, tmB, tmD{};
+    prm.copy_out = STAGED != 0 && prm.vec && !prm.accumulate;
+    if (prm.copy_out && !make_out_map(&tmD, prm.out, a.rows, b.rows, prm.ldd, sizeof(T))) return GPD_ERR_CUDA;
     if (!make_map_2d(&tmA, a.q, a.rows, K, a.ld, BM) || !make_map_2d(&tmB, b.q, b.rows, K, b.ld, b_rows(BN, PAIR))) return GPD_ERR_CUDA;
     auto kernel = gemm_fp8_kernel<BN, T, TRANS, PAIR, SPLIT>;
-    constexpr int smem = smem_bytes(BN, PAIR, SPLIT), rows = PAIR ? 2 * BM : BM;
+    constexpr int smem = smem_bytes(BN, PAIR, SPLIT, STAGED), rows = PAIR ? 2 * BM : BM;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
     prm.sa = a.s;
     prm.sb = b.s;
@@ -614,7 +692,7 @@ gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, 
     if (tiles > 0x3fffffff) return GPD_ERR_SHAPE;
     const int cluster = PAIR ? 2 : splits;
     const unsigned n = (unsigned)(SPLIT ? tiles : std::min<int64_t>(tiles, sm_count() / cluster));
-    return lm::launch_after(kernel, PAIR || SPLIT ? dim3(cluster, n) : dim3(n), dim3(kThreads), smem, cluster, st, tmA, tmB, prm);
+    return lm::launch_after(kernel, PAIR || SPLIT ? dim3(cluster, n) : dim3(n), dim3(kThreads), smem, cluster, st, tmA, tmB, tmD, prm);
 }
 
 // Tile width, orientation, pairing and split by the smallest estimated time.  A k-block of a 128 x BN tile (per

@@ -4,7 +4,8 @@ Integer operands with small scale exponents make every partial sum an integer mu
 below 2^24 of it: the FP32 result has to be exact whatever the order.  For random operands the bound is the
 sum of magnitudes times 2^-23 (one truncation) for each instruction of 32 terms in a chain and for each
 addition of a chain, plus four for the alignment inside the instructions: 16-bit results have one chain of K / 32,
-FP32 results chains of 16 and K / 512 additions."""
+FP32 results chains of at
+most 32, held to the bound of chains of 16 with K / 512 additions."""
 
 import pytest
 
