@@ -695,9 +695,14 @@ gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, 
     return lm::launch_after(kernel, PAIR || SPLIT ? dim3(cluster, n) : dim3(n), dim3(kThreads), smem, cluster, st, tmA, tmB, tmD, prm);
 }
 
-// Tile width, orientation, pairing and split by the smallest estimated time.  A k-block of a 128 x BN tile (per
-// CTA) takes the tensor cores 2 BN cycles and its copies (128 + BN, in a pair 128 + BN / 2) * 128 bytes at about 48
-// bytes per cycle and SM; a tile costs about 1500 cycles besides, a split tile twice that.
+// Tile width, orientation, pairing and split by the smallest estimated time, in cycles.  A k-block of a tile takes the
+// tensor cores 2 BN (four dependent instructions: 344 at least) and its copies a cycle per 64 bytes; a tile costs about
+// 1500 besides.  A part of a split contraction has half an SM's stages, whose latency shows (about 3300 over their
+// number), and 3000 for the meeting of the parts.  Measured over 19 shapes from 1 x 4096 x 4096 to 4096^3 with every
+// configuration, the choice is within 6 % of the best but for 64 x 8192 x 8192 (18.2 us, in four parts 15.5) and
+// 16 x 50000 x 512 in FP32 (9.1, 128 x 16 tiles 8.1).  Examples:
+// 7 x 4096 x 4096: 6.7 us in four parts, 8.2 in two; 128 x 8192 x 8192: 17.6 us as 256 x 128 pairs, 30.1 split;
+// 512 x 8192 x 8192: 23.5 us as 256 x 224 pairs, 28.9 as 128 x 224 tiles, 30.9 as 256 x 128 pairs.
 Config choose(int64_t M, int64_t N, int kb, bool f32) {
     static const int kWidths[] = {16, 32, 64, 128, 192, 224};
     Config best{128, 1, true, false};
@@ -714,7 +719,8 @@ Config choose(int64_t M, int64_t N, int kb, bool f32) {
                     if (s > 1 && (bn > 64 || s > kb || tiles * s > 2 * sms)) continue;
                     // two CTAs of a split product share an SM
                     const double waves = s > 1 ? std::max(1.0, (double)(tiles * s) / sms) : (double)((tiles + slots - 1) / slots);
-                    const double block = std::max(2.0 * bn, (BM + b_rows(bn, pair)) * 128 / 48.0);
+                    double block = std::max(std::max(2.0 * bn, 344.0), stage_bytes(bn, pair) / 64.0);
+                    if (s > 1) block = std::max(block, 3300.0 / stages(bn, false, true, 0));
                     const double time = waves * (((kb + s - 1) / s) * block + (s > 1 ? 3000.0 : 1500.0));
                     if (time < best_t * 0.999) {
                         best_t = time;
