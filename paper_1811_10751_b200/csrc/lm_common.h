@@ -48,10 +48,38 @@ __device__ __forceinline__ float2 unpack2(uint32_t u, __half) {
     return __half22float2(*reinterpret_cast<const __half2*>(&u));
 }
 
+// Pairs of FP32 numbers, one instruction for both
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 f2(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // Eight elements at p, of which n (may be <= 0 or >= 8) exist; the others read as zero.  VEC: p is
 // 16-byte aligned (the caller has checked base and row stride).
 template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load8(const T* p, int64_t n) {
+__device__ __forceinline__ Raw8<T> load8(const T* p, int n) {
     Raw8<T> r;
     if constexpr (sizeof(T) == 4) {
         if (VEC && n >= 8) {
@@ -90,6 +118,38 @@ __device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&f)[8]) {
         f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y; f[4] = c.x; f[5] = c.y; f[6] = d.x; f[7] = d.y;
     }
 }
+// Eight elements as four pairs and back, and all of eight elements at a 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ void pairs8(const Raw8<T>& r, F2 (&p)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        p[0] = f2(__uint_as_float(r.v.x), __uint_as_float(r.v.y));
+        p[1] = f2(__uint_as_float(r.v.z), __uint_as_float(r.v.w));
+        p[2] = f2(__uint_as_float(r.w.x), __uint_as_float(r.w.y));
+        p[3] = f2(__uint_as_float(r.w.z), __uint_as_float(r.w.w));
+    } else {
+        const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2(w[i], T());
+            p[i] = f2(f.x, f.y);
+        }
+    }
+}
+__device__ __forceinline__ void floats8(const F2 (&p)[4], float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = f2(p[i]);
+        f[2 * i] = x.x;
+        f[2 * i + 1] = x.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8_all(const T* p) {
+    Raw8<T> r;
+    r.v = reinterpret_cast<const uint4*>(p)[0];
+    if constexpr (sizeof(T) == 4) r.w = reinterpret_cast<const uint4*>(p)[1];
+    return r;
+}
 // Elements 2 i and 2 i + 1 of eight.
 template <typename T>
 __device__ __forceinline__ float2 pair_of(const Raw8<T>& r, int i) {
@@ -101,7 +161,7 @@ __device__ __forceinline__ float2 pair_of(const Raw8<T>& r, int i) {
     }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float (&f)[8], int64_t n) {
+__device__ __forceinline__ void store8(T* p, const float (&f)[8], int n) {
     if (VEC && n >= 8) {
         if constexpr (sizeof(T) == 4) {
             reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
@@ -150,7 +210,7 @@ __device__ __forceinline__ uint32_t cvt_fp8x4(float a, float b, float c, float d
 }
 // Eight bytes at p, of which n exist; VEC: p is 8-byte aligned.
 template <bool VEC>
-__device__ __forceinline__ void store8_bytes(uint8_t* p, uint2 b, int64_t n) {
+__device__ __forceinline__ void store8_bytes(uint8_t* p, uint2 b, int n) {
     if (VEC && n >= 8) {
         *reinterpret_cast<uint2*>(p) = b;
     } else {
@@ -158,6 +218,25 @@ __device__ __forceinline__ void store8_bytes(uint8_t* p, uint2 b, int64_t n) {
         for (int i = 0; i < 8; ++i)
             if (i < n) p[i] = (uint8_t)((i < 4 ? b.x >> (8 * i) : b.y >> (8 * (i - 4))) & 0xffu);
     }
+}
+
+// Bits of the largest magnitude of eight numbers, a NaN above all
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t amax8(const float (&f)[8]) {
+    float m = max_nan(fabsf(f[0]), fabsf(f[1]));
+#pragma unroll
+    for (int i = 2; i < 8; ++i) m = max_nan(m, fabsf(f[i]));
+    return __float_as_uint(m);
+}
+// Eight numbers times `inv`, in 8 bits
+template <int Q>
+__device__ __forceinline__ uint2 to_fp8x8(const float (&f)[8], float inv) {
+    return make_uint2(cvt_fp8x4<Q>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                      cvt_fp8x4<Q>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

@@ -82,12 +82,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
     const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
     const int64_t bm = blockIdx.x / tiles_k, bk = blockIdx.x % tiles_k;
     const int64_t r0 = bm * kBlock + 8 * rg, c0 = bk * kBlock + 8 * cg;
-    const int64_t nc = a.K - c0;
+    const int nc = (int)min(a.K - c0, (int64_t)8), nr = (int)min(a.M - r0, (int64_t)8);      // of the patch, possibly <= 0
+    const T* src = static_cast<const T*>(a.src) + r0 * a.ld + c0;
 
     Raw8<T> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        raw[i] = r0 + i < a.M && nc > 0 ? load8<T, VEC>(static_cast<const T*>(a.src) + (r0 + i) * a.ld + c0, nc) : Raw8<T>{};
+        raw[i] = i < nr && nc > 0 ? (VEC && nc == 8 ? load8_all<T>(src + i * a.ld) : load8<T, false>(src + i * a.ld, nc)) : Raw8<T>{};
 
     Maxima<T> cm;                                      // of the patch's columns
     uint32_t rmax[8];                                  // of its rows
@@ -127,23 +128,27 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
     }
 
     if (a.q) {
+        uint8_t* q = a.q + r0 * a.ldq + c0;
+        uint8_t* sc = a.s + r0 * a.lds + bk;
+        const uint32_t half_mask = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint32_t b = byte;
             if (!SQUARE) {
-                uint32_t m = rmax[i];
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                b = scale_byte<Q>(magnitude<T>(m));
-                if (cg == 0 && r0 + i < a.M) a.s[(r0 + i) * a.lds + bk] = (uint8_t)b;
+                b = scale_byte<Q>(magnitude<T>(__reduce_max_sync(half_mask, rmax[i])));
+                if (cg == 0 && i < nr) sc[i * a.lds] = (uint8_t)b;
             }
-            if (r0 + i < a.M && nc > 0) {
+            if (i < nr && nc > 0) {
                 const float inv = scale_inverse(b);
+                F2 p[4];
+                pairs8<T>(raw[i], p);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = mul2(p[j], f2(inv, inv));
                 float f[8];
-                unpack8<T>(raw[i], f);
-                store8_bytes<VEC>(a.q + (r0 + i) * a.ldq + c0,
-                                  make_uint2(cvt_fp8x4<Q>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
-                                             cvt_fp8x4<Q>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)), nc);
+                floats8(p, f);
+                const uint2 v = make_uint2(cvt_fp8x4<Q>(f[0], f[1], f[2], f[3]), cvt_fp8x4<Q>(f[4], f[5], f[6], f[7]));
+                if (VEC && nc == 8) *reinterpret_cast<uint2*>(q + i * a.ldq) = v;
+                else store8_bytes<false>(q + i * a.ldq, v, nc);
             }
         }
     }
@@ -156,9 +161,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
             float lo[8], hi[8];                        // columns j and j + 1 of the patch
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float2 f = pair_of<T>(raw[i], j >> 1);
-                lo[i] = f.x * inv[j];
-                hi[i] = f.y * inv[j + 1];
+                const float2 x = pair_of<T>(raw[i], j >> 1), f = f2(mul2(f2(x.x, x.y), f2(inv[j], inv[j + 1])));
+                lo[i] = f.x;
+                hi[i] = f.y;
             }
             *reinterpret_cast<uint2*>(tile + chunk_at(8 * cg + j, rg)) =
                 make_uint2(cvt_fp8x4<Q>(lo[0], lo[1], lo[2], lo[3]), cvt_fp8x4<Q>(lo[4], lo[5], lo[6], lo[7]));
@@ -169,7 +174,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
 #pragma unroll
         for (int p = 0; p < 4; ++p) {                  // 32 transposed rows per pass, 8 lanes of 16 bytes each
             const int col = 32 * p + (threadIdx.x >> 3), piece = threadIdx.x & 7;
-            const int64_t c = bk * kBlock + col, r = bm * kBlock + 16 * piece, n = a.M - r;
+            const int64_t c = bk * kBlock + col, r = bm * kBlock + 16 * piece;
+            const int n = (int)min(a.M - r, (int64_t)16);
             if (c >= a.K || n <= 0) continue;
             // chunks 2 piece and 2 piece + 1 stay neighbours, in exchanged order for odd column groups
             uint4 v = *reinterpret_cast<const uint4*>(tile + (chunk_at(col, 2 * piece) & ~15));

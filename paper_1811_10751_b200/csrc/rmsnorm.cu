@@ -44,12 +44,12 @@ __device__ __forceinline__ float row_sum(float v, int G, int g, float* scratch) 
 }
 
 // VPT vectors per thread are kept in registers; VPT = 0: rows too long for that are read twice.
-// blockDim = (G, rows per CTA), rows per CTA > 1 only with G = 32.
+// blockDim = (G, rows per CTA), rows per CTA > 1 only with G = 32.  VEC: every vector is whole and on a 16-byte boundary.
 template <typename T, typename W, int Q, int VPT, bool VEC>
 __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const NormArgs a) {
     __shared__ float scratch[32];
     after_previous();
-    const int G = blockDim.x;
+    const int G = blockDim.x, H = (int)a.H;
     const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (t >= a.T) return;                              // a whole warp (G = 32) or, with one row per CTA, never
     const T* x = static_cast<const T*>(a.x) + t * a.ldx;
@@ -59,88 +59,92 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
     T* yout = a.y ? static_cast<T*>(a.y) + t * a.ldy : nullptr;
     uint8_t* qout = a.q ? a.q + t * a.ldq : nullptr;
     uint8_t* sout = a.q ? a.scales + t * a.lds : nullptr;
+    const uint32_t half_mask = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
 
-    auto add = [&](const Raw8<T>& rx, const Raw8<T>& rr, float (&f)[8]) {
-        unpack8<T>(rx, f);
+    auto load = [&](const T* p, int c) {
+        if (VEC) return c < H ? load8_all<T>(p + c) : Raw8<T>{};
+        return c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
+    };
+    auto add = [&](const Raw8<T>& rx, const Raw8<T>& rr, F2 (&h)[4]) {
+        pairs8<T>(rx, h);
         if (res) {
-            float r[8];
-            unpack8<T>(rr, r);
+            F2 r[4];
+            pairs8<T>(rr, r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] += r[i];
+            for (int i = 0; i < 4; ++i) h[i] = add2(h[i], r[i]);
         }
     };
-    // every lane of a warp gets here together (the shuffles need it)
-    auto finish = [&](int64_t c, const float (&h)[8], float s) {
-        const int64_t n = a.H - c;
+    // every lane of a warp gets here together (the maximum over a block needs it)
+    auto finish = [&](int c, const F2 (&h)[4], float s) {
+        const int n = H - c;
         float y[8];
         if (n > 0) {
-            if (hout) store8<T, VEC>(hout + c, h, n);
-            float w[8];
-            unpack8<W>(load8<W, VEC>(wt + c, n), w);
+            if (hout) {
+                float f[8];
+                floats8(h, f);
+                store8<T, VEC>(hout + c, f, VEC ? 8 : n);
+            }
+            F2 w[4];
+            pairs8<W>(VEC ? load8_all<W>(wt + c) : load8<W, false>(wt + c, n), w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = h[i] * s * w[i];
-            if (yout) store8<T, VEC>(yout + c, y, n);
+            for (int i = 0; i < 4; ++i) w[i] = mul2(mul2(h[i], f2(s, s)), w[i]);
+            floats8(w, y);
+            if (yout) store8<T, VEC>(yout + c, y, VEC ? 8 : n);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = 0.f;
         }
         if (!qout) return;
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(y[i]));
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const uint32_t b = scale_byte<Q>(m);
+        const uint32_t b = scale_byte<Q>(__reduce_max_sync(half_mask, amax8(y)));
         if (n > 0) {
-            const float inv = scale_inverse(b);
-            const uint2 v = make_uint2(cvt_fp8x4<Q>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
-                                       cvt_fp8x4<Q>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
-            store8_bytes<VEC>(qout + c, v, n);
+            store8_bytes<VEC>(qout + c, to_fp8x8<Q>(y, scale_inverse(b)), VEC ? 8 : n);
             if ((c & (kBlock - 1)) == 0) sout[c / kBlock] = (uint8_t)b;
         }
     };
+    auto square = [](const F2 (&h)[4], F2 sum) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = fma2(h[i], h[i], sum);
+        return sum;
+    };
+    auto inverse_root = [&](F2 squares) {
+        const float2 p = f2(squares);
+        const float s = rsqrtf(row_sum(p.x + p.y, G, 0, scratch) / (float)H + a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
+        return s;
+    };
 
-    float sum = 0.f;
+    F2 sum = f2(0.f, 0.f);
     if constexpr (VPT > 0) {
-        float h[VPT][8];
+        F2 h[VPT][4];
         Raw8<T> rx[VPT], rr[VPT];                      // all loads before the first use
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int64_t c = 8 * ((int64_t)threadIdx.x + i * G), n = a.H - c;
-            rx[i] = n > 0 ? load8<T, VEC>(x + c, n) : Raw8<T>{};
-            rr[i] = n > 0 && res ? load8<T, VEC>(res + c, n) : Raw8<T>{};
+            const int c = 8 * (threadIdx.x + i * G);
+            rx[i] = load(x, c);
+            rr[i] = res ? load(res, c) : Raw8<T>{};
         }
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             add(rx[i], rr[i], h[i]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(h[i][j], h[i][j], sum);
+            sum = square(h[i], sum);
         }
-        sum = row_sum(sum, G, 0, scratch);
-        const float s = rsqrtf(sum / (float)a.H + a.eps);
-        if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
+        const float s = inverse_root(sum);
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) finish(8 * ((int64_t)threadIdx.x + i * G), h[i], s);
+        for (int i = 0; i < VPT; ++i) finish(8 * (threadIdx.x + i * G), h[i], s);
     } else {
         // h may be stored over x or r: nothing is written before the second reading, and each element
         // is read and written by the same thread
-        const int64_t step = 8 * (int64_t)G, end = (a.H + step - 1) / step * step;
-        auto read = [&](int64_t c, float (&f)[8]) {
-            const int64_t n = a.H - c;
-            add(n > 0 ? load8<T, VEC>(x + c, n) : Raw8<T>{}, n > 0 && res ? load8<T, VEC>(res + c, n) : Raw8<T>{}, f);
-        };
-        for (int64_t c = 8 * threadIdx.x; c < end; c += step) {
-            float h[8];
-            read(c, h);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(h[j], h[j], sum);
+        const int step = 8 * G, rounds = (H + step - 1) / step;
+        F2 h[4];
+        for (int i = 0; i < rounds; ++i) {
+            const int c = 8 * threadIdx.x + i * step;
+            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h);
+            sum = square(h, sum);
         }
-        sum = row_sum(sum, G, 0, scratch);
-        const float s = rsqrtf(sum / (float)a.H + a.eps);
-        if (a.rstd && threadIdx.x == 0) a.rstd[t] = s;
-        for (int64_t c = 8 * threadIdx.x; c < end; c += step) {
-            float h[8];
-            read(c, h);
+        const float s = inverse_root(sum);
+        for (int i = 0; i < rounds; ++i) {
+            const int c = 8 * threadIdx.x + i * step;
+            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h);
             finish(c, h, s);
         }
     }
@@ -172,7 +176,7 @@ gpd_status launch_norm(const NormArgs& a, cudaStream_t st) {
 template <typename T, typename W, int Q>
 gpd_status launch_norm_q(const NormArgs& a, cudaStream_t st) {
     const int e = sizeof(T);
-    const bool vec = rows_aligned(a.x, a.ldx, e) && rows_aligned(a.residual, a.ldr, e) && rows_aligned(a.h, a.ldh, e) &&
+    const bool vec = a.H % 8 == 0 && rows_aligned(a.x, a.ldx, e) && rows_aligned(a.residual, a.ldr, e) && rows_aligned(a.h, a.ldh, e) &&
                      rows_aligned(a.y, a.ldy, e) && rows_aligned(a.q, a.ldq, 1, 8) && aligned(a.weight, 16);
     return vec ? launch_norm<T, W, Q, true>(a, st) : launch_norm<T, W, Q, false>(a, st);
 }
@@ -207,14 +211,22 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
     const W* wt = static_cast<const W*>(a.weight);
     float* part = a.parts + (int64_t)blockIdx.x * a.H;
     constexpr int N = VPT > 0 ? VPT : 1;
-    float dw[N][8];
+    F2 dw[N][4];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
-    const int64_t step = 8 * (int64_t)G;
+        for (int j = 0; j < 4; ++j) dw[i][j] = f2(0.f, 0.f);
+    const int H = (int)a.H, step = 8 * G;
     const int64_t first = (int64_t)blockIdx.x * blockDim.y + g;
     int turn = 0;
+    auto load = [&](const T* p, int c) {
+        if (VEC) return c < H ? load8_all<T>(p + c) : Raw8<T>{};
+        return c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
+    };
+    auto weights = [&](int c, F2 (&w)[4]) {
+        if (VEC) pairs8<W>(load8_all<W>(wt + c), w);
+        else pairs8<W>(load8<W, false>(wt + c, H - c), w);
+    };
 
     for (int64_t t = first; t < a.T; t += (int64_t)gridDim.x * blockDim.y, turn ^= 1) {
         const T* dy = static_cast<const T*>(a.dy) + t * a.lddy;
@@ -222,78 +234,81 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
         const T* dh = a.dh ? static_cast<const T*>(a.dh) + t * a.lddh : nullptr;
         T* dx = static_cast<T*>(a.dx) + t * a.lddx;
         const float s = a.rstd[t];
-        auto write = [&](int64_t c, const Raw8<T>& rdy, const Raw8<T>& rh, const Raw8<T>& rdh, float k, float (&acc)[8]) {
-            const int64_t n = a.H - c;
-            float fy[8], fh[8], fd[8], w[8];
-            unpack8<T>(rdy, fy);
-            unpack8<T>(rh, fh);
-            unpack8<T>(rdh, fd);
-            unpack8<W>(load8<W, VEC>(wt + c, n), w);
+        auto dot8 = [&](int c, const Raw8<T>& rdy, const Raw8<T>& rh, F2 sum) {
+            F2 fy[4], fh[4], w[4];
+            pairs8<T>(rdy, fy);
+            pairs8<T>(rh, fh);
+            weights(c, w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                acc[j] = fmaf(fy[j] * s, fh[j], acc[j]);
-                fd[j] = fmaf(s, fmaf(-fh[j], k, fy[j] * w[j]), fd[j]);
-            }
-            store8<T, VEC>(dx + c, fd, n);
+            for (int j = 0; j < 4; ++j) sum = fma2(mul2(fy[j], w[j]), fh[j], sum);
+            return sum;
         };
-        float dot = 0.f;
+        auto write = [&](int c, const Raw8<T>& rdy, const Raw8<T>& rh, const Raw8<T>& rdh, float k, F2 (&acc)[4]) {
+            F2 fy[4], fh[4], fd[4], w[4];
+            pairs8<T>(rdy, fy);
+            pairs8<T>(rh, fh);
+            pairs8<T>(rdh, fd);
+            weights(c, w);
+            const F2 ss = f2(s, s), mk = f2(-k, -k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[j] = fma2(mul2(fy[j], ss), fh[j], acc[j]);
+                fd[j] = fma2(ss, fma2(fh[j], mk, mul2(fy[j], w[j])), fd[j]);
+            }
+            float o[8];
+            floats8(fd, o);
+            store8<T, VEC>(dx + c, o, VEC ? 8 : H - c);
+        };
+        F2 sum = f2(0.f, 0.f);
         if constexpr (VPT > 0) {
             Raw8<T> rdy[VPT], rh[VPT], rdh[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int64_t c = 8 * ((int64_t)threadIdx.x + i * G), n = a.H - c;
-                rdy[i] = n > 0 ? load8<T, VEC>(dy + c, n) : Raw8<T>{};
-                rh[i] = n > 0 ? load8<T, VEC>(h + c, n) : Raw8<T>{};
-                rdh[i] = n > 0 && dh ? load8<T, VEC>(dh + c, n) : Raw8<T>{};
+                const int c = 8 * (threadIdx.x + i * G);
+                rdy[i] = load(dy, c);
+                rh[i] = load(h, c);
+                rdh[i] = dh ? load(dh, c) : Raw8<T>{};
             }
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
-                if (c < a.H) {
-                    float fy[8], fh[8], w[8];
-                    unpack8<T>(rdy[i], fy);
-                    unpack8<T>(rh[i], fh);
-                    unpack8<W>(load8<W, VEC>(wt + c, a.H - c), w);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) dot = fmaf(fy[j] * w[j], fh[j], dot);
-                }
+                const int c = 8 * (threadIdx.x + i * G);
+                if (c < H) sum = dot8(c, rdy[i], rh[i], sum);
             }
-            dot = row_sum(dot, G, g, scratch[g][turn]);
-            const float k = s * s * (dot / (float)a.H);
+            const float2 p = f2(sum);
+            const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
-                if (c < a.H) write(c, rdy[i], rh[i], rdh[i], k, dw[i]);
+                const int c = 8 * (threadIdx.x + i * G);
+                if (c < H) write(c, rdy[i], rh[i], rdh[i], k, dw[i]);
             }
         } else {
-            for (int64_t c = 8 * threadIdx.x; c < a.H; c += step) {
-                float fy[8], fh[8], w[8];
-                unpack8<T>(load8<T, VEC>(dy + c, a.H - c), fy);
-                unpack8<T>(load8<T, VEC>(h + c, a.H - c), fh);
-                unpack8<W>(load8<W, VEC>(wt + c, a.H - c), w);
+            for (int c = 8 * threadIdx.x; c < H; c += step) sum = dot8(c, load(dy, c), load(h, c), sum);
+            const float2 p = f2(sum);
+            const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
+            for (int c = 8 * threadIdx.x; c < H; c += step) {
+                float f[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dot = fmaf(fy[j] * w[j], fh[j], dot);
-            }
-            dot = row_sum(dot, G, g, scratch[g][turn]);
-            const float k = s * s * (dot / (float)a.H);
-            for (int64_t c = 8 * threadIdx.x; c < a.H; c += step) {
-                const int64_t n = a.H - c;
+                for (int j = 0; j < 8; ++j) f[j] = c + j < H && t != first ? part[c + j] : 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dw[0][j] = j < n && t != first ? part[c + j] : 0.f;
-                write(c, load8<T, VEC>(dy + c, n), load8<T, VEC>(h + c, n), dh ? load8<T, VEC>(dh + c, n) : Raw8<T>{}, k, dw[0]);
+                for (int j = 0; j < 4; ++j) dw[0][j] = f2(f[2 * j], f[2 * j + 1]);
+                write(c, load(dy, c), load(h, c), dh ? load(dh, c) : Raw8<T>{}, k, dw[0]);
+                floats8(dw[0], f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j < n) part[c + j] = dw[0][j];
+                    if (c + j < H) part[c + j] = f[j];
             }
         }
     }
     if constexpr (VPT > 0) {
         // the R rows' shares in the order of the rows; [j][thread] keeps neighbouring threads in neighbouring banks
+        float f[VPT][8];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) floats8(dw[i], f[i]);
         if (g > 0) {
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dw_rows[((g - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x] = dw[i][j];
+                for (int j = 0; j < 8; ++j) dw_rows[((g - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x] = f[i][j];
         }
         __syncthreads();
         if (g > 0) return;
@@ -301,13 +316,13 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dw[i][j] += dw_rows[((r - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x];
+                for (int j = 0; j < 8; ++j) f[i][j] += dw_rows[((r - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int64_t c = 8 * ((int64_t)threadIdx.x + i * G);
+            const int c = 8 * (threadIdx.x + i * G);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (c + j < a.H) part[c + j] = dw[i][j];
+                if (c + j < H) part[c + j] = f[i][j];
         }
     }
 }
@@ -358,7 +373,7 @@ gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
 template <typename T, typename W>
 gpd_status launch_bwd_w(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
     const int e = sizeof(T);
-    const bool vec = rows_aligned(a.dy, a.lddy, e) && rows_aligned(a.h, a.ldh, e) && rows_aligned(a.dh, a.lddh, e) &&
+    const bool vec = a.H % 8 == 0 && rows_aligned(a.dy, a.lddy, e) && rows_aligned(a.h, a.ldh, e) && rows_aligned(a.dh, a.lddh, e) &&
                      rows_aligned(a.dx, a.lddx, e) && aligned(a.weight, 16);
     return vec ? launch_bwd<T, W, true>(a, dweight, st) : launch_bwd<T, W, false>(a, dweight, st);
 }
@@ -375,7 +390,7 @@ extern "C" gpd_status gpd_rmsnorm_quant(gpd_dtype type, const void* x_dev, int64
                                         void* q_dev, int64_t ldq, uint8_t* scales_dev, int64_t lds, float* rstd_dev,
                                         int64_t T, int64_t H, void* stream) {
     if (!is_float_type(type) || (weight_type != type && weight_type != GPD_DT_F32)) return GPD_ERR_ARG;
-    if (T < 0 || H <= 0 || T > 0x7fffffff) return GPD_ERR_SHAPE;
+    if (T < 0 || H <= 0 || T > 0x7fffffff || H > 0x7ffffff0 / 2) return GPD_ERR_SHAPE;
     if (T == 0) return GPD_OK;                         // empty buffers may have no address
     if (!x_dev || !weight_dev || (q_dev && (!scales_dev || !is_fp8_type(q_type)))) return GPD_ERR_ARG;
     if (ldx < H || (residual_dev && ldr < H) || (residual_out_dev && ldh < H) || (y_dev && ldy < H) ||
@@ -397,7 +412,7 @@ extern "C" gpd_status gpd_rmsnorm_backward(gpd_dtype type, const void* dy_dev, i
                                            float* dweight_dev, int64_t T, int64_t H, void* workspace_dev,
                                            int64_t workspace_bytes, void* stream) {
     if (!is_float_type(type) || (weight_type != type && weight_type != GPD_DT_F32)) return GPD_ERR_ARG;
-    if (T < 0 || H <= 0) return GPD_ERR_SHAPE;
+    if (T < 0 || H <= 0 || H > 0x7ffffff0 / 2) return GPD_ERR_SHAPE;
     if (!dweight_dev || (T > 0 && (!dy_dev || !h_dev || !weight_dev || !rstd_dev || !dx_dev))) return GPD_ERR_ARG;
     if (T > 0 && (lddy < H || ldh < H || (dresidual_dev && lddh < H) || lddx < H)) return GPD_ERR_SHAPE;
     if (T > 0 && (!workspace_dev || workspace_bytes < std::min<int64_t>(T, GPD_RMSNORM_MAX_PARTS) * H * (int64_t)sizeof(float) ||
