@@ -283,30 +283,33 @@ __device__ __forceinline__ Stats block_merge(Stats st, float k, Stats* scratch) 
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_here() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_here() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ float peer_f32(const void* p, uint32_t rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(p, rank)) : "memory");
-    return v;
+__device__ __forceinline__ void to_peer(float* p, uint32_t rank, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(p, rank)), "f"(v) : "memory");
 }
-__device__ __forceinline__ uint64_t peer_u64(const void* p, uint32_t rank) {
-    uint64_t v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer_addr(p, rank)) : "memory");
-    return v;
+__device__ __forceinline__ void to_peer(uint64_t* p, uint32_t rank, uint64_t v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_addr(p, rank)), "l"(v) : "memory");
 }
-// Stats of the row from those of the cluster's CTAs (each in its own `mine`); a barrier comes first.
-__device__ __forceinline__ Stats cluster_merge(const Stats* mine, int C, float k) {
-    cluster_sync_all();
-    Stats st = no_stats();
-    for (int r = 0; r < C; ++r) {
-        const Stats b{peer_f32(&mine->m, r), peer_f32(&mine->s, r), peer_f32(&mine->u, r)};
-        st = merge(st, b, k);
+// Results of the C CTAs of a row meet: each writes its own into the others' shared memory, slot by rank, so that one
+// barrier is enough and nobody's shared memory is touched after it.  Before that all of them have to run: they arrive
+// at a barrier when they start and wait for it when the first pass is over.
+constexpr int kMaxSplit = 8;
+__device__ __forceinline__ void to_peers(Stats* slots, int C, int rank, const Stats& st) {
+    if ((int)threadIdx.x < C) {
+        to_peer(&slots[rank].m, threadIdx.x, st.m);
+        to_peer(&slots[rank].s, threadIdx.x, st.s);
+        to_peer(&slots[rank].u, threadIdx.x, st.u);
     }
-    return st;
+}
+__device__ __forceinline__ Stats from_peers(const Stats* slots, int C, float k) {
+    const int lane = threadIdx.x & 31;
+    return warp_merge(lane < C ? slots[lane] : no_stats(), k);
 }
 // Part `rank` of C of a row, cut at multiples of eight entries.
 __device__ __forceinline__ void slice(int V, int C, int rank, int& v0, int& v1) {
@@ -336,36 +339,70 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t key_of(float x, int v) { return (uint64_t)order_of(x) << 32 | (0xffffffffu - (uint32_t)v); }
 
-struct TopShared {
+struct __align__(16) TopShared {
     uint64_t cand[kCand];
     uint64_t top[kMaxTop];
-    float maxima[64];
+    uint64_t from[kMaxSplit * kMaxTop];                // the lists of a row's CTAs
+    int larger[kMaxSplit * kMaxTop];
+    float maxima[32];
     uint32_t threshold;
     int count;
 };
 
-// cand[0 .. n) -> the K largest in order in top (0: none); all threads.
-__device__ __forceinline__ void rank_top(TopShared& sh, int n, int K) {
+// The K largest of n <= kCand keys, in order, to sh.top (0: none); all threads.  A warp counts, for one key
+// after another, how many are larger.
+__device__ __forceinline__ void rank_top(TopShared& sh, const uint64_t* keys, int n, int K) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     if (threadIdx.x < K) sh.top[threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const uint64_t key = sh.cand[i];
-        int r = 0;
-        for (int j = 0; j < n; ++j) r += sh.cand[j] > key;
-        if (r < K && key) sh.top[r] = key;
+    const int rounds = (n + 31) >> 5;
+    for (int i = warp; i < n; i += warps) {
+        const uint64_t key = keys[i];
+        int larger = 0;
+#pragma unroll 2
+        for (int j = 0; j < rounds; ++j) larger += 32 * j + lane < n && keys[32 * j + lane] > key;
+        larger = __reduce_add_sync(0xffffffffu, larger);
+        if (lane == 0 && larger < K && key) sh.top[larger] = key;
     }
+    __syncthreads();
+}
+
+// The K largest of C ordered lists of K keys in sh.from (0: no key), in order, to sh.top; all threads.  A thread looks
+// for one key's place in one list.
+__device__ __forceinline__ void merge_top(TopShared& sh, int C, int K) {
+    const int n = C * K;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) sh.larger[i] = 0;
+    if (threadIdx.x < K) sh.top[threadIdx.x] = 0;
+    __syncthreads();
+    for (int task = threadIdx.x; task < n * C; task += blockDim.x) {
+        const int i = task / C;
+        const uint64_t key = sh.from[i], *list = sh.from + (task - i * C) * K;
+        int lo = 0, hi = K;                            // the first entry that is not larger
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (list[mid] > key) lo = mid + 1;
+            else hi = mid;
+        }
+        atomicAdd(&sh.larger[i], lo);                  // a count: any order will do
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x)
+        if (sh.from[i] && sh.larger[i] < K) sh.top[sh.larger[i]] = sh.from[i];
     __syncthreads();
 }
 
 // The K largest entries of [v0, v1), in order, to sh.top.  `mine`: this thread's largest entry (-FLT_MAX: none).
 // K entries are at least as large as the K-th largest of any set of entries, so the K-th largest among the
-// largest 64 / warps thread maxima of every warp bounds the answer from below; what reaches the bound is
+// largest 32 / warps thread maxima of every warp bounds the answer from below; what reaches the bound is
 // gathered and ranked.  Where more reaches it than there is room for (many equal entries), each warp keeps
 // a sorted list of 32 instead.
-template <typename T>
-__device__ void block_top(const T* row, int v0, int v1, float mine, int K, TopShared& sh) {
+// `in` has been through the slice once; where its first pieces were all of them, they are still in registers.
+template <typename T, int U>
+__device__ void block_top(Pieces<T, U>& in, float mine, int K, TopShared& sh) {
+    const T* row = in.row;
+    const int v0 = in.v0, v1 = in.v1;
     constexpr int N = 16 / sizeof(T);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, per = 64 / warps;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, per = 32 / warps;
     float v = mine;                                    // sorted over the warp, largest first
 #pragma unroll
     for (int size = 2; size <= 32; size <<= 1)
@@ -381,10 +418,14 @@ __device__ void block_top(const T* row, int v0, int v1, float mine, int K, TopSh
         sh.threshold = 0;
     }
     __syncthreads();
-    if (threadIdx.x < warps * per) {
-        const float x = sh.maxima[threadIdx.x];
+    if (warp == 0) {                                   // K <= 32 of 32
+        const float x = sh.maxima[lane];
         int r = 0;
-        for (int j = 0; j < warps * per; ++j) r += sh.maxima[j] > x || (sh.maxima[j] == x && j < (int)threadIdx.x);
+#pragma unroll 8
+        for (int j = 0; j < 32; ++j) {
+            const float y = __shfl_sync(0xffffffffu, x, j);
+            r += y > x || (y == x && j < lane);
+        }
         if (r == K - 1 && x > -FLT_MAX) sh.threshold = order_of(x);
     }
     __syncthreads();
@@ -402,12 +443,11 @@ __device__ void block_top(const T* row, int v0, int v1, float mine, int K, TopSh
             }
         }
     };
-    Pieces<T, 4> in;
-    in.template start<true>(row, v0, v1);
+    if (in.pieces > U * (int)blockDim.x) in.template start<true>(row, v0, v1);
     in.template run<true>(
-        [&](int b, int step, int n, const uint4 (&r)[4]) {
+        [&](int b, int step, int n, const uint4 (&r)[U]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < U; ++j)
                 if (j < n) keep(r[j], b + j * step, N);
         },
         [&](int b, const uint4& r, int n) { keep(r, b, n); });
@@ -431,7 +471,7 @@ __device__ void block_top(const T* row, int v0, int v1, float mine, int K, TopSh
         n = blockDim.x;
         __syncthreads();
     }
-    rank_top(sh, n, K);
+    rank_top(sh, sh.cand, n, K);
 }
 
 // ---- log probabilities -----------------------------------------------------------------------------------
@@ -448,8 +488,7 @@ struct LogprobArgs {
 // C CTAs per row (gridDim.x = C, a cluster); the rows blockIdx.y, blockIdx.y + gridDim.y, ...
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogprobArgs a) {
-    __shared__ Stats scratch[32];
-    __shared__ Stats part;
+    __shared__ Stats scratch[32], slots[kMaxSplit];
     __shared__ typename std::conditional<TOP, TopShared, int>::type top;
     after_previous();
     const int C = gridDim.x, rank = blockIdx.x;
@@ -460,45 +499,49 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogprobA
     for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
         const T* row = static_cast<const T*>(a.logits) + t * a.ld;
         in.template start<!TOP>(row, v0, v1);
+        if (C > 1) cluster_here();                     // one row per cluster then
+        // this thread's token and its logit arrive during the pass
+        int64_t token = -1;
+        float x_token = 0.f;
+        if (rank == 0 && (int)threadIdx.x < a.G) {
+            token = index_at(a.tokens, a.index_bytes, t * a.G + threadIdx.x);
+            if (token >= 0 && token < a.V) x_token = to_f32(row[token]);
+        }
         Stats st = thread_stats<T, true, !TOP>(in, k);
         const float mine = st.m;
         st = block_merge(st, k, scratch);
-        if constexpr (TOP) block_top<T>(row, v0, v1, mine, a.K, top);
+        if constexpr (TOP) block_top(in, mine, a.K, top);
         if (C > 1) {
-            if (threadIdx.x == 0) part = st;
-            st = cluster_merge(&part, C, k);
+            cluster_all_here();
+            to_peers(slots, C, rank, st);
             if constexpr (TOP) {
-                if (rank == 0) {
-                    for (int i = threadIdx.x; i < C * a.K; i += blockDim.x) top.cand[i] = peer_u64(&top.top[i % a.K], i / a.K);
-                    __syncthreads();
-                    rank_top(top, C * a.K, a.K);       // overwrites this CTA's own list, which has been copied
-                }
+                if ((int)threadIdx.x < a.K) to_peer(&top.from[rank * a.K + threadIdx.x], 0, top.top[threadIdx.x]);
+            }
+            cluster_sync_all();
+            if (rank != 0) return;
+            st = from_peers(slots, C, k);
+            if constexpr (TOP) merge_top(top, C, a.K);
+        }
+        const float lse = lse_of(st, a.inv_tau);
+        if (threadIdx.x == 0) {
+            a.lse[t] = lse;
+            if (a.entropy) a.entropy[t] = st.s == 0.f ? 0.f : logf(st.s) - st.u / st.s * a.inv_tau;
+        }
+        if ((int)threadIdx.x < a.G) {                  // at most 64, fewer than there are threads
+            float lp = 0.f;
+            if (token >= a.V) lp = __uint_as_float(0x7fc00000u);
+            else if (token >= 0) lp = st.s == 0.f ? -INFINITY : fmaf(x_token, a.inv_tau, -lse);
+            a.logprobs[t * a.G + threadIdx.x] = lp;
+        }
+        if constexpr (TOP) {
+            if (threadIdx.x < a.K) {
+                const uint64_t key = top.top[threadIdx.x];
+                a.top_ids[t * a.K + threadIdx.x] = (int32_t)(0xffffffffu - (uint32_t)key);
+                if (a.top_logprobs)
+                    a.top_logprobs[t * a.K + threadIdx.x] =
+                        st.s == 0.f ? -INFINITY : fmaf(value_of((uint32_t)(key >> 32)), a.inv_tau, -lse);
             }
         }
-        if (rank == 0) {
-            const float lse = lse_of(st, a.inv_tau);
-            if (threadIdx.x == 0) {
-                a.lse[t] = lse;
-                if (a.entropy) a.entropy[t] = st.s == 0.f ? 0.f : logf(st.s) - st.u / st.s * a.inv_tau;
-            }
-            for (int i = threadIdx.x; i < a.G; i += blockDim.x) {
-                const int64_t v = index_at(a.tokens, a.index_bytes, t * a.G + i);
-                float lp = 0.f;
-                if (v >= a.V) lp = __uint_as_float(0x7fc00000u);
-                else if (v >= 0) lp = st.s == 0.f ? -INFINITY : fmaf(to_f32(row[v]), a.inv_tau, -lse);
-                a.logprobs[t * a.G + i] = lp;
-            }
-            if constexpr (TOP) {
-                if (threadIdx.x < a.K) {
-                    const uint64_t key = top.top[threadIdx.x];
-                    a.top_ids[t * a.K + threadIdx.x] = (int32_t)(0xffffffffu - (uint32_t)key);
-                    if (a.top_logprobs)
-                        a.top_logprobs[t * a.K + threadIdx.x] =
-                            st.s == 0.f ? -INFINITY : fmaf(value_of((uint32_t)(key >> 32)), a.inv_tau, -lse);
-                }
-            }
-        }
-        if (C > 1) cluster_sync_all();                 // shared memory of all parts stays until it has been read
         if (TOP) __syncthreads();                      // `top` is taken up again
     }
 }
@@ -607,8 +650,7 @@ struct __align__(16) TeacherList {
 // to the first pass and from L2 to the second, which writes the gradient.
 template <typename T>
 __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillArgs a) {
-    __shared__ Stats scratch[32];
-    __shared__ Stats part;
+    __shared__ Stats scratch[32], slots[kMaxSplit];
     __shared__ TeacherList lists[2];                   // in turn, so that a row's last readers need no barrier
     after_previous();
     const int C = gridDim.x, rank = blockIdx.x, lane = threadIdx.x & 31;
@@ -621,6 +663,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
         const T* row = static_cast<const T*>(a.logits) + t * a.ld;
         T* d = a.d ? static_cast<T*>(a.d) + t * a.ldd : nullptr;
         in.template start<false>(row, v0, v1);
+        if (C > 1) cluster_here();                     // one row per cluster then
         const float wt = a.weights ? a.weights[t] : 1.f;
         // this thread's entry of the list arrives during the first pass
         int64_t id = 0;
@@ -636,6 +679,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
                 for (int v = v0 + threadIdx.x; v < v1; v += blockDim.x) d[v] = from_f32<T>(0.f);
         };
         if (wt == 0.f) {                               // the same in all parts
+            if (C > 1) cluster_all_here();
             nothing();
             continue;
         }
@@ -653,8 +697,10 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
         }
         st = block_merge(st, k, scratch);              // its barriers publish the list
         if (C > 1) {
-            if (threadIdx.x == 0) part = st;
-            st = cluster_merge(&part, C, k);
+            cluster_all_here();
+            to_peers(slots, C, rank, st);
+            cluster_sync_all();
+            st = from_peers(slots, C, k);
         }
         // the teacher's distribution, in every warp
         float tmax = -INFINITY, qs = 0.f;
@@ -668,7 +714,6 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
         tmax = warp_max(tmax);
         if (tmax == -INFINITY && !bad) {               // nothing in the list
             nothing();
-            if (C > 1) cluster_sync_all();
             continue;
         }
         for (int i = lane; i < a.K; i += 32) qs += list.t[i] == -INFINITY ? 0.f : ex2(k * (list.t[i] - tmax));
@@ -707,7 +752,6 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
                 if (first_at == i) d[v] = from_f32<T>(none ? 0.f : scale * ex2((list.x[i] - m) * k) - wt * a.tau * (s / qs));
             }
         }
-        if (C > 1) cluster_sync_all();                 // `part` stays until all have read it
     }
 }
 
@@ -715,7 +759,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
 // CTAs per row: as many (up to 8) as the GPU has SMs for, while each still has 4096 entries to read.
 int row_split(int64_t T, int64_t V) {
     int c = 1;
-    while (c < 8 && T * c * 2 <= 2 * sm_count() && V / (2 * c) >= 4096) c *= 2;
+    while (c < kMaxSplit && T * c * 2 <= 2 * sm_count() && V / (2 * c) >= 4096) c *= 2;
     return c;
 }
 unsigned row_threads(int64_t entries) { return entries >= 8192 ? 512 : entries >= 4096 ? 256 : 128; }
