@@ -198,15 +198,15 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
 __device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - min(byte, 253u)) << 23); }
 
 template <int Q>
-__device__ __forceinline__ uint32_t cvt_fp8x2(float lo, float hi) {
-    unsigned short r;
-    if constexpr (Q == GPD_DT_E4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-template <int Q>
 __device__ __forceinline__ uint32_t cvt_fp8x4(float a, float b, float c, float d) {
-    return cvt_fp8x2<Q>(a, b) | (cvt_fp8x2<Q>(c, d) << 16);
+    uint32_t r;
+    if constexpr (Q == GPD_DT_E4M3)
+        asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+            : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+    else
+        asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e5m2x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e5m2x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+            : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
 }
 // Eight bytes at p, of which n exist; VEC: p is 8-byte aligned.
 template <bool VEC>
@@ -237,6 +237,51 @@ template <int Q>
 __device__ __forceinline__ uint2 to_fp8x8(const float (&f)[8], float inv) {
     return make_uint2(cvt_fp8x4<Q>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
                       cvt_fp8x4<Q>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+}
+
+// Scale bytes of N (1, 2, 4 or 8) blocks, each spread over the sixteen lanes of a half-warp: amax[i] holds the bits of
+// this lane's largest magnitude in block i, `bits` turns the block's maximum into FP32 bits.  The lanes halve the blocks
+// among them while they exchange maxima, so that a lane ends with one block (`mine`, the same in 16 / N lanes) and its
+// byte is worked out once; then they hand the bytes back.  Every lane gets all N, packed; `first` in one lane per block.
+struct BlockScales { uint32_t lo, hi, byte; int mine; bool first; };
+__device__ __forceinline__ uint32_t packed_byte(const BlockScales& b, int i) { return (i < 4 ? b.lo >> (8 * i) : b.hi >> (8 * (i - 4))) & 0xffu; }
+template <int Q, int N, typename F>
+__device__ __forceinline__ BlockScales block_scales(const uint32_t (&amax)[N], F bits) {
+    const int cg = threadIdx.x & 15;
+    uint32_t r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = amax[i];
+    BlockScales b{0, 0, 0, 0, false};
+#pragma unroll
+    for (int n = N, o = 8; o > 0; n >>= 1, o >>= 1) {
+        if (n > 1) {
+            const bool up = cg & o;
+            b.mine = 2 * b.mine + up;
+#pragma unroll
+            for (int i = 0; i < n / 2; ++i) {
+                const uint32_t keep = up ? r[i + n / 2] : r[i], send = up ? r[i] : r[i + n / 2];
+                r[i] = max(keep, __shfl_xor_sync(0xffffffffu, send, o));
+            }
+        } else {
+            r[0] = max(r[0], __shfl_xor_sync(0xffffffffu, r[0], o));
+        }
+    }
+    b.byte = scale_byte<Q>(bits(r[0]));
+    b.first = (cg & (16 / N - 1)) == 0;
+    b.lo = b.byte;
+#pragma unroll
+    for (int have = 1, o = 16 / N; have < N; have *= 2, o *= 2) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, b.lo, o);
+        const bool up = cg & o;
+        const uint32_t low = up ? other : b.lo, high = up ? b.lo : other;
+        if (have < 4) {
+            b.lo = low | high << (8 * have);
+        } else {
+            b.lo = low;
+            b.hi = high;
+        }
+    }
+    return b;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

@@ -31,8 +31,15 @@ struct CutArgs {
 // apart, fall on all banks.
 __device__ __forceinline__ int chunk_at(int col, int chunk) { return col * kBlock + ((chunk ^ (col >> 3)) & 15) * 8; }
 
-// Magnitudes order like their bits without the sign, in every type: maxima of 16-bit elements are taken two at a
-// time, and only the final ones become FP32 bits.
+// Maxima of 16-bit magnitudes are taken two at a time (a NaN is above all), and only the final ones become FP32 bits.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, __nv_bfloat16) {
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b, __half) {
+    const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
 template <typename T>
 struct Maxima {
     uint32_t w[4];                                     // columns 2 i (low half) and 2 i + 1
@@ -40,8 +47,8 @@ struct Maxima {
     __device__ __forceinline__ uint32_t take(const Raw8<T>& r) {       // returns the row's maximum
         const uint32_t a[4] = {r.v.x & 0x7fff7fffu, r.v.y & 0x7fff7fffu, r.v.z & 0x7fff7fffu, r.v.w & 0x7fff7fffu};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __vmaxu2(w[i], a[i]);
-        const uint32_t m = __vmaxu2(__vmaxu2(a[0], a[1]), __vmaxu2(a[2], a[3]));
+        for (int i = 0; i < 4; ++i) w[i] = max_pair(w[i], a[i], T());
+        const uint32_t m = max_pair(max_pair(a[0], a[1], T()), max_pair(a[2], a[3], T()), T());
         return max(m & 0xffffu, m >> 16);
     }
     __device__ __forceinline__ uint32_t column(int j) const { return j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu; }
@@ -130,14 +137,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
     if (a.q) {
         uint8_t* q = a.q + r0 * a.ldq + c0;
         uint8_t* sc = a.s + r0 * a.lds + bk;
-        const uint32_t half_mask = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
+        BlockScales rows{};
+        if (!SQUARE) {
+            rows = block_scales<Q, 8>(rmax, [](uint32_t m) { return magnitude<T>(m); });
+            if (rows.first && rows.mine < nr) sc[rows.mine * a.lds] = (uint8_t)rows.byte;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            uint32_t b = byte;
-            if (!SQUARE) {
-                b = scale_byte<Q>(magnitude<T>(__reduce_max_sync(half_mask, rmax[i])));
-                if (cg == 0 && i < nr) sc[i * a.lds] = (uint8_t)b;
-            }
+            const uint32_t b = SQUARE ? byte : packed_byte(rows, i);
             if (i < nr && nc > 0) {
                 const float inv = scale_inverse(b);
                 F2 p[4];

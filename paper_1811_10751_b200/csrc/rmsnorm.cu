@@ -59,7 +59,6 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
     T* yout = a.y ? static_cast<T*>(a.y) + t * a.ldy : nullptr;
     uint8_t* qout = a.q ? a.q + t * a.ldq : nullptr;
     uint8_t* sout = a.q ? a.scales + t * a.lds : nullptr;
-    const uint32_t half_mask = threadIdx.x & 16 ? 0xffff0000u : 0x0000ffffu;
 
     auto load = [&](const T* p, int c) {
         if (VEC) return c < H ? load8_all<T>(p + c) : Raw8<T>{};
@@ -74,31 +73,43 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
             for (int i = 0; i < 4; ++i) h[i] = add2(h[i], r[i]);
         }
     };
-    // every lane of a warp gets here together (the maximum over a block needs it)
-    auto finish = [&](int c, const F2 (&h)[4], float s) {
+    // y of one vector, from h; h and y are stored where they are wanted
+    auto normed = [&](int c, const F2 (&h)[4], float s, float (&y)[8]) {
         const int n = H - c;
-        float y[8];
-        if (n > 0) {
-            if (hout) {
-                float f[8];
-                floats8(h, f);
-                store8<T, VEC>(hout + c, f, VEC ? 8 : n);
-            }
-            F2 w[4];
-            pairs8<W>(VEC ? load8_all<W>(wt + c) : load8<W, false>(wt + c, n), w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = mul2(mul2(h[i], f2(s, s)), w[i]);
-            floats8(w, y);
-            if (yout) store8<T, VEC>(yout + c, y, VEC ? 8 : n);
-        } else {
+        if (n <= 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = 0.f;
+            return;
+        }
+        if (hout) {
+            floats8(h, y);
+            store8<T, VEC>(hout + c, y, VEC ? 8 : n);
+        }
+        F2 w[4];
+        pairs8<W>(VEC ? load8_all<W>(wt + c) : load8<W, false>(wt + c, n), w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = mul2(mul2(h[i], f2(s, s)), w[i]);
+        floats8(w, y);
+        if (yout) store8<T, VEC>(yout + c, y, VEC ? 8 : n);
+    };
+    // N vectors of this thread, G vectors apart, in 8 bits; every lane of a warp gets here together
+    auto finish = [&](int c0, const auto& h, float s) {
+        constexpr int N = sizeof(h) / sizeof(h[0]);
+        float y[N][8];
+        uint32_t m[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            normed(c0 + 8 * i * G, h[i], s, y[i]);
+            m[i] = amax8(y[i]);
         }
         if (!qout) return;
-        const uint32_t b = scale_byte<Q>(__reduce_max_sync(half_mask, amax8(y)));
-        if (n > 0) {
-            store8_bytes<VEC>(qout + c, to_fp8x8<Q>(y, scale_inverse(b)), VEC ? 8 : n);
-            if ((c & (kBlock - 1)) == 0) sout[c / kBlock] = (uint8_t)b;
+        const BlockScales b = block_scales<Q, N>(m, [](uint32_t x) { return x; });
+        const int mine = (c0 + 8 * b.mine * G) / kBlock;
+        if (b.first && mine * kBlock < H) sout[mine] = (uint8_t)b.byte;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = c0 + 8 * i * G, n = H - c;
+            if (n > 0) store8_bytes<VEC>(qout + c, to_fp8x8<Q>(y[i], scale_inverse(packed_byte(b, i))), VEC ? 8 : n);
         }
     };
     auto square = [](const F2 (&h)[4], F2 sum) {
@@ -129,22 +140,24 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
             sum = square(h[i], sum);
         }
         const float s = inverse_root(sum);
+        // four vectors at a time: more would not fit in registers beside their y
+        constexpr int N = VPT < 4 ? VPT : 4;
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) finish(8 * (threadIdx.x + i * G), h[i], s);
+        for (int i = 0; i < VPT; i += N) finish(8 * (threadIdx.x + i * G), *reinterpret_cast<F2(*)[N][4]>(&h[i]), s);
     } else {
         // h may be stored over x or r: nothing is written before the second reading, and each element
         // is read and written by the same thread
         const int step = 8 * G, rounds = (H + step - 1) / step;
-        F2 h[4];
+        F2 h[1][4];
         for (int i = 0; i < rounds; ++i) {
             const int c = 8 * threadIdx.x + i * step;
-            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h);
-            sum = square(h, sum);
+            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h[0]);
+            sum = square(h[0], sum);
         }
         const float s = inverse_root(sum);
         for (int i = 0; i < rounds; ++i) {
             const int c = 8 * threadIdx.x + i * step;
-            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h);
+            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h[0]);
             finish(c, h, s);
         }
     }
