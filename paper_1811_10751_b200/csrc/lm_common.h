@@ -177,6 +177,89 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8], int n) {
     }
 }
 
+// ---- rows that do not start on 16-byte boundaries ----------------------------------------------------------
+// Four words from the `n` words w, starting `s` elements in.
+template <typename T, int N>
+__device__ __forceinline__ void shifted4(const uint32_t (&w)[N], int s, uint32_t (&o)[4]) {
+    constexpr int per = 4 / sizeof(T);                 // elements of a word
+    const int ws = s / per;
+    uint32_t a[6], b[5];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) a[i] = i + 2 < N ? (ws & 2 ? w[i + 2] : w[i]) : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) b[i] = ws & 1 ? a[i + 1] : a[i];
+    const uint32_t sel = per == 2 && (s & 1) ? 0x5432u : 0x3210u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = per == 2 ? __byte_perm(b[i], b[i + 1], sel) : b[i];
+}
+// Eight elements at p, anywhere, by 16-byte loads of what surrounds them.  [begin, end): the tensor; what would reach
+// beyond it is loaded element by element.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8_near(const T* p, const T* begin, const T* end) {
+    constexpr int N = 16 / sizeof(T);
+    const int mis = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    if (mis == 0) return load8_all<T>(p);
+    const T* q = p - mis;
+    if (q < begin || q + 8 + N > end) return load8<T, false>(p, 8);
+    const uint4* v = reinterpret_cast<const uint4*>(q);
+    const uint4 x = v[0], y = v[1];
+    uint32_t o[4];
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        shifted4<T>(w, mis, o);
+        r.v = make_uint4(o[0], o[1], o[2], o[3]);
+    } else {
+        const uint4 z = v[2];
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}, u[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+        shifted4<T>(w, mis, o);
+        r.v = make_uint4(o[0], o[1], o[2], o[3]);
+        shifted4<T>(u, mis, o);
+        r.w = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+    return r;
+}
+// The n (<= 8, possibly none) elements f to p, where the lanes of the warp hold consecutive eights of one row: a lane
+// stores the 16-byte piece that begins among its elements and ends among the next lane's.  All lanes call it.
+template <typename T>
+__device__ __forceinline__ void store8_near(T* p, const float (&f)[8], int n) {
+    constexpr int N = 16 / sizeof(T), W = 8 / (4 / sizeof(T));         // elements of a piece, words of eight elements
+    const int lane = threadIdx.x & 31, mis = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    if (mis == 0) {                                    // the same for all lanes of the warp
+        store8<T, true>(p, f, n);
+        return;
+    }
+    uint32_t w[W], next[W];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2(f[2 * i], f[2 * i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(f[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) next[i] = __shfl_down_sync(0xffffffffu, w[i], 1);
+    const uint32_t full = __ballot_sync(0xffffffffu, n >= 8);
+    const bool before = lane > 0 && full >> (lane - 1) & 1, after = lane < 31 && full >> (lane + 1) & 1;
+    const int head = N - mis, tail = 8 - mis;          // the first whole piece starts at `head`, the last one begun at `tail`
+    if (n >= 8) {
+        uint32_t o[4];
+        if constexpr (sizeof(T) == 4) {
+            const uint32_t own[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+            shifted4<T>(own, head, o);
+            *reinterpret_cast<uint4*>(p + head) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        if (after) {
+            const uint32_t both[8] = {w[W - 4], w[W - 3], w[W - 2], w[W - 1], next[0], next[1], next[2], next[3]};
+            shifted4<T>(both, head, o);
+            *reinterpret_cast<uint4*>(p + tail) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)                        // what no piece covers
+        if (i < n && (n < 8 || (i < head && !before) || (i >= tail && !after))) p[i] = from_f32<T>(f[i]);
+}
+
 // ---- 8-bit blocks ----------------------------------------------------------------------------------
 // top = 0.875 * 2^kTopExp
 template <int Q> struct Fp8;

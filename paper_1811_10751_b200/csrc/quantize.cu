@@ -24,6 +24,7 @@ struct CutArgs {
     uint8_t* qT; int64_t ldqT;
     uint8_t* sT; int64_t ldsT;
     int64_t M, K;
+    bool q_vec, qT_vec;                                // rows of q (qT) start on 8-byte (16-byte) boundaries
 };
 
 // Byte offset of the 8-byte chunk `chunk` of transposed row `col` in shared memory.  The chunks of a row are
@@ -90,12 +91,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
     const int64_t bm = blockIdx.x / tiles_k, bk = blockIdx.x % tiles_k;
     const int64_t r0 = bm * kBlock + 8 * rg, c0 = bk * kBlock + 8 * cg;
     const int nc = (int)min(a.K - c0, (int64_t)8), nr = (int)min(a.M - r0, (int64_t)8);      // of the patch, possibly <= 0
-    const T* src = static_cast<const T*>(a.src) + r0 * a.ld + c0;
+    const T *begin = static_cast<const T*>(a.src), *end = begin + (a.M - 1) * a.ld + a.K, *src = begin + r0 * a.ld + c0;
 
     Raw8<T> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        raw[i] = i < nr && nc > 0 ? (VEC && nc == 8 ? load8_all<T>(src + i * a.ld) : load8<T, false>(src + i * a.ld, nc)) : Raw8<T>{};
+        raw[i] = i < nr && nc > 0 ? (nc < 8 ? load8<T, false>(src + i * a.ld, nc) : VEC ? load8_all<T>(src + i * a.ld) : load8_near<T>(src + i * a.ld, begin, end)) : Raw8<T>{};
 
     Maxima<T> cm;                                      // of the patch's columns
     uint32_t rmax[8];                                  // of its rows
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
                 float f[8];
                 floats8(p, f);
                 const uint2 v = make_uint2(cvt_fp8x4<Q>(f[0], f[1], f[2], f[3]), cvt_fp8x4<Q>(f[4], f[5], f[6], f[7]));
-                if (VEC && nc == 8) *reinterpret_cast<uint2*>(q + i * a.ldq) = v;
+                if (a.q_vec && nc == 8) *reinterpret_cast<uint2*>(q + i * a.ldq) = v;
                 else store8_bytes<false>(q + i * a.ldq, v, nc);
             }
         }
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
             uint4 v = *reinterpret_cast<const uint4*>(tile + (chunk_at(col, 2 * piece) & ~15));
             if ((col >> 3) & 1) v = make_uint4(v.z, v.w, v.x, v.y);
             uint8_t* dst = a.qT + c * a.ldqT + r;
-            if (VEC && n >= 16) {
+            if (a.qT_vec && n >= 16) {
                 *reinterpret_cast<uint4*>(dst) = v;
             } else {
                 store8_bytes<false>(dst, make_uint2(v.x, v.y), n);
@@ -203,7 +204,7 @@ gpd_status launch_cut(const CutArgs& a, bool square, cudaStream_t st) {
     const int64_t tk = (a.K + kBlock - 1) / kBlock, tm = (a.M + kBlock - 1) / kBlock;
     if (tk * tm > 0x7fffffff) return GPD_ERR_SHAPE;
     const unsigned grid = (unsigned)(tk * tm);
-    const bool vec = rows_aligned(a.src, a.ld, sizeof(T)) && rows_aligned(a.q, a.ldq, 1, 8) && rows_aligned(a.qT, a.ldqT, 1);
+    const bool vec = rows_aligned(a.src, a.ld, sizeof(T));
     auto kernel = square ? (vec ? cut_kernel<T, Q, true, true> : cut_kernel<T, Q, true, false>)
                          : (vec ? cut_kernel<T, Q, false, true> : cut_kernel<T, Q, false, false>);
     return launch_after(kernel, dim3(grid), dim3(256), 0, 1, st, a, (int)tk);
@@ -229,7 +230,7 @@ extern "C" gpd_status gpd_quantize_blocks(gpd_dtype type, const void* src_dev, i
     const int64_t kb = (K + lm::kBlock - 1) / lm::kBlock, mb = (M + lm::kBlock - 1) / lm::kBlock;
     if (ld < K || (q_dev && (ldq < K || lds < kb)) || (qT_dev && (ldqT < M || ldsT < mb))) return GPD_ERR_SHAPE;
     const CutArgs a{src_dev, ld, static_cast<uint8_t*>(q_dev), ldq, scales_dev, lds, static_cast<uint8_t*>(qT_dev), ldqT,
-                    scalesT_dev, ldsT, M, K};
+                    scalesT_dev, ldsT, M, K, lm::rows_aligned(q_dev, ldq, 1, 8), lm::rows_aligned(qT_dev, ldqT, 1)};
     const bool square = block_rows != 1;
     cudaStream_t st = as_stream(stream);
     if (type == GPD_DT_F32) return launch_cut_q<float>(a, q_type, square, st);

@@ -29,7 +29,15 @@ struct NormArgs {
     float* rstd;
     int64_t T, H;
     float eps;
+    bool q_vec;                                        // rows of q start on 8-byte boundaries
 };
+
+// Eight weights from column c < H (VEC: all there, on a 16-byte boundary)
+template <typename W, bool VEC>
+__device__ __forceinline__ Raw8<W> weight_at(const W* w, int c, int H) {
+    if (VEC || (c + 8 <= H && (reinterpret_cast<uintptr_t>(w) & 15) == 0)) return load8_all<W>(w + c);
+    return load8<W, false>(w + c, H - c);
+}
 
 // Sum over the G threads of a row (a multiple of 32, threadIdx.x); every thread gets it.  G = 32: a warp of its
 // own, no barrier.  Otherwise row `g` of the CTA has named barrier g + 1 and two sets of 32 floats in
@@ -60,9 +68,14 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
     uint8_t* qout = a.q ? a.q + t * a.ldq : nullptr;
     uint8_t* sout = a.q ? a.scales + t * a.lds : nullptr;
 
-    auto load = [&](const T* p, int c) {
+    auto load = [&](const T* p, int c, const void* base, int64_t ld) {
         if (VEC) return c < H ? load8_all<T>(p + c) : Raw8<T>{};
-        return c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
+        const T* begin = static_cast<const T*>(base);
+        return c + 8 <= H ? load8_near<T>(p + c, begin, begin + (a.T - 1) * ld + H) : c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
+    };
+    auto store = [&](T* p, int c, const float (&f)[8]) {               // every lane of the warp calls it
+        if (!VEC) store8_near<T>(p + c, f, H - c);
+        else if (c < H) store8<T, true>(p + c, f, 8);
     };
     auto add = [&](const Raw8<T>& rx, const Raw8<T>& rr, F2 (&h)[4]) {
         pairs8<T>(rx, h);
@@ -75,22 +88,20 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
     };
     // y of one vector, from h; h and y are stored where they are wanted
     auto normed = [&](int c, const F2 (&h)[4], float s, float (&y)[8]) {
-        const int n = H - c;
-        if (n <= 0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = 0.f;
-            return;
-        }
         if (hout) {
             floats8(h, y);
-            store8<T, VEC>(hout + c, y, VEC ? 8 : n);
+            store(hout, c, y);
         }
-        F2 w[4];
-        pairs8<W>(VEC ? load8_all<W>(wt + c) : load8<W, false>(wt + c, n), w);
+        F2 w[4] = {0, 0, 0, 0};                        // columns that do not exist: y = 0
+        if (c < H) pairs8<W>(weight_at<W, VEC>(wt, c, H), w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = mul2(mul2(h[i], f2(s, s)), w[i]);
         floats8(w, y);
-        if (yout) store8<T, VEC>(yout + c, y, VEC ? 8 : n);
+        if (c >= H) {                                  // whatever s is
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = 0.f;
+        }
+        if (yout) store(yout, c, y);
     };
     // N vectors of this thread, G vectors apart, in 8 bits; every lane of a warp gets here together
     auto finish = [&](int c0, const auto& h, float s) {
@@ -109,7 +120,11 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = c0 + 8 * i * G, n = H - c;
-            if (n > 0) store8_bytes<VEC>(qout + c, to_fp8x8<Q>(y[i], scale_inverse(packed_byte(b, i))), VEC ? 8 : n);
+            if (n > 0) {
+                const uint2 v = to_fp8x8<Q>(y[i], scale_inverse(packed_byte(b, i)));
+                if (VEC || (a.q_vec && n >= 8)) *reinterpret_cast<uint2*>(qout + c) = v;
+                else store8_bytes<false>(qout + c, v, n);
+            }
         }
     };
     auto square = [](const F2 (&h)[4], F2 sum) {
@@ -131,8 +146,8 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int c = 8 * (threadIdx.x + i * G);
-            rx[i] = load(x, c);
-            rr[i] = res ? load(res, c) : Raw8<T>{};
+            rx[i] = load(x, c, a.x, a.ldx);
+            rr[i] = res ? load(res, c, a.residual, a.ldr) : Raw8<T>{};
         }
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -151,13 +166,13 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
         F2 h[1][4];
         for (int i = 0; i < rounds; ++i) {
             const int c = 8 * threadIdx.x + i * step;
-            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h[0]);
+            add(load(x, c, a.x, a.ldx), res ? load(res, c, a.residual, a.ldr) : Raw8<T>{}, h[0]);
             sum = square(h[0], sum);
         }
         const float s = inverse_root(sum);
         for (int i = 0; i < rounds; ++i) {
             const int c = 8 * threadIdx.x + i * step;
-            add(load(x, c), res ? load(res, c) : Raw8<T>{}, h[0]);
+            add(load(x, c, a.x, a.ldx), res ? load(res, c, a.residual, a.ldr) : Raw8<T>{}, h[0]);
             finish(c, h, s);
         }
     }
@@ -231,13 +246,14 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
     const int H = (int)a.H, step = 8 * G;
     const int64_t first = (int64_t)blockIdx.x * blockDim.y + g;
     int turn = 0;
-    auto load = [&](const T* p, int c) {
+    auto load = [&](const T* p, int c, const void* base, int64_t ld) {
         if (VEC) return c < H ? load8_all<T>(p + c) : Raw8<T>{};
-        return c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
+        const T* begin = static_cast<const T*>(base);
+        return c + 8 <= H ? load8_near<T>(p + c, begin, begin + (a.T - 1) * ld + H) : c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
     };
     auto weights = [&](int c, F2 (&w)[4]) {
-        if (VEC) pairs8<W>(load8_all<W>(wt + c), w);
-        else pairs8<W>(load8<W, false>(wt + c, H - c), w);
+        if (VEC || c < H) pairs8<W>(weight_at<W, VEC>(wt, c, H), w);
+        else w[0] = w[1] = w[2] = w[3] = 0;
     };
 
     for (int64_t t = first; t < a.T; t += (int64_t)gridDim.x * blockDim.y, turn ^= 1) {
@@ -269,7 +285,8 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
             }
             float o[8];
             floats8(fd, o);
-            store8<T, VEC>(dx + c, o, VEC ? 8 : H - c);
+            if (!VEC) store8_near<T>(dx + c, o, H - c);        // every lane of the warp gets here
+            else store8<T, true>(dx + c, o, 8);
         };
         F2 sum = f2(0.f, 0.f);
         if constexpr (VPT > 0) {
@@ -277,33 +294,38 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 const int c = 8 * (threadIdx.x + i * G);
-                rdy[i] = load(dy, c);
-                rh[i] = load(h, c);
-                rdh[i] = dh ? load(dh, c) : Raw8<T>{};
+                rdy[i] = load(dy, c, a.dy, a.lddy);
+                rh[i] = load(h, c, a.h, a.ldh);
+                rdh[i] = dh ? load(dh, c, a.dh, a.lddh) : Raw8<T>{};
             }
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 const int c = 8 * (threadIdx.x + i * G);
-                if (c < H) sum = dot8(c, rdy[i], rh[i], sum);
+                if (!VEC || c < H) sum = dot8(c, rdy[i], rh[i], sum);
             }
             const float2 p = f2(sum);
             const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 const int c = 8 * (threadIdx.x + i * G);
-                if (c < H) write(c, rdy[i], rh[i], rdh[i], k, dw[i]);
+                if (!VEC || c < H) write(c, rdy[i], rh[i], rdh[i], k, dw[i]);
             }
         } else {
-            for (int c = 8 * threadIdx.x; c < H; c += step) sum = dot8(c, load(dy, c), load(h, c), sum);
+            const int rounds = (H + step - 1) / step;
+            for (int i = 0; i < rounds; ++i) {
+                const int c = 8 * threadIdx.x + i * step;
+                if (!VEC || c < H) sum = dot8(c, load(dy, c, a.dy, a.lddy), load(h, c, a.h, a.ldh), sum);
+            }
             const float2 p = f2(sum);
             const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
-            for (int c = 8 * threadIdx.x; c < H; c += step) {
+            for (int i = 0; i < rounds; ++i) {
+                const int c = 8 * threadIdx.x + i * step;
                 float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = c + j < H && t != first ? part[c + j] : 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dw[0][j] = f2(f[2 * j], f[2 * j + 1]);
-                write(c, load(dy, c), load(h, c), dh ? load(dh, c) : Raw8<T>{}, k, dw[0]);
+                if (!VEC || c < H) write(c, load(dy, c, a.dy, a.lddy), load(h, c, a.h, a.ldh), dh ? load(dh, c, a.dh, a.lddh) : Raw8<T>{}, k, dw[0]);
                 floats8(dw[0], f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -359,7 +381,7 @@ __global__ void __launch_bounds__(512) rmsnorm_dweight_kernel(const float* parts
 template <typename T, typename W, bool VEC>
 gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
     const int64_t vecs = (a.H + 7) / 8;
-    constexpr int V = sizeof(T) == 4 ? 2 : 4;
+    constexpr int V = sizeof(T) == 4 ? 2 : 4;          // vectors per thread that fit in registers
     // one CTA of up to 512 threads per SM: R rows of G threads at a time
     const bool loop = vecs > kBwdThreads * V;
     const int G = loop ? 1024 : (int)(((vecs + V - 1) / V + 31) / 32 * 32);
@@ -409,7 +431,7 @@ extern "C" gpd_status gpd_rmsnorm_quant(gpd_dtype type, const void* x_dev, int64
         (q_dev && (ldq < H || lds < (H + lm::kBlock - 1) / lm::kBlock)))
         return GPD_ERR_SHAPE;
     const NormArgs a{x_dev, ldx, residual_dev, ldr, weight_dev, residual_out_dev, ldh, y_dev, ldy, static_cast<uint8_t*>(q_dev),
-                     ldq, scales_dev, lds, rstd_dev, T, H, eps};
+                     ldq, scales_dev, lds, rstd_dev, T, H, eps, lm::rows_aligned(q_dev, ldq, 1, 8)};
     cudaStream_t st = as_stream(stream);
     if (type == GPD_DT_F32) return launch_norm_w<float, float>(a, q_type, st);
     if (type == GPD_DT_BF16)
