@@ -216,7 +216,7 @@ extern "C" gpd_status gpd_device_status(int32_t* status_host) {
     if (!status_host) return GPD_ERR_ARG;
     if (cudaDeviceSynchronize() != cudaSuccess) return GPD_ERR_CUDA;
     const int a = tf32_device_status_fetch_and_clear(), b = i8_device_status_fetch_and_clear();
-    const int c = fp8_device_status_fetch_and_clear(), d = norm_device_status_fetch_and_clear();
-    *status_host = a != 0 ? a : b != 0 ? b : c != 0 ? c : d;
+    const int c = fp8_device_status_fetch_and_clear();
+    *status_host = a != 0 ? a : b != 0 ? b : c;
     return GPD_OK;
 }

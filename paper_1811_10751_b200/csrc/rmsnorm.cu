@@ -11,9 +11,7 @@
 // Measured: forward 8192 x 8192 BF16 with residual 78 us, 0.92 of the copy bandwidth.
 #include <algorithm>
 
-#include "gemm_common.h"
 #include "lm_common.h"
-#include "tc_common.h"
 
 namespace gpd {
 
@@ -232,54 +230,120 @@ constexpr int kBwdThreads = 512;
 // blockDim = (G, R): R rows of the CTA at a time, G threads each.  A thread adds up its columns' share of dw over
 // its rows: in registers, met in shared memory at the end, one partial row per CTA; or (VPT = 0, long rows, R = 1)
 // in the CTA's row of `parts`, element by element by the thread that owns the column.
-template <typename T, typename W, int VPT, bool VEC>
+// PIECES: the rows' 16-byte pieces are the threads' vectors.  A row that starts `shift` elements after a boundary has
+// its first vector begin that much before it; the tensors share their shifts, and a thread's rows are so many
+// apart that they have the same one, so that its columns stay its own.
+// AHEAD: the next row is loaded while the present one's sum is awaited and its results are written.
+template <typename T, typename W, int VPT, bool PIECES, bool AHEAD>
 __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward_kernel(const NormBwdArgs a) {
     __shared__ float scratch[16][2][32];
-    extern __shared__ float dw_rows[];                 // [R - 1][8 VPT G]
+    extern __shared__ __align__(16) float dw_rows[];   // the threads' weights; at the end [R][H], the rows' shares of dw
     after_previous();
-    const int G = blockDim.x, g = threadIdx.y;
+    const int G = blockDim.x, g = threadIdx.y, H = (int)a.H, step = 8 * G;
     const W* wt = static_cast<const W*>(a.weight);
     float* part = a.parts + (int64_t)blockIdx.x * a.H;
     constexpr int N = VPT > 0 ? VPT : 1;
+    const int64_t stride = (int64_t)gridDim.x * blockDim.y, first = (int64_t)blockIdx.x * blockDim.y + g;
+    const int shift = PIECES ? (int)((first * a.ldh) & (16 / sizeof(T) - 1)) : 0;
+    const int c0 = 8 * threadIdx.x - shift;            // first column of the thread's first vector
     F2 dw[N][4];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) dw[i][j] = f2(0.f, 0.f);
-    const int H = (int)a.H, step = 8 * G;
-    const int64_t first = (int64_t)blockIdx.x * blockDim.y + g;
     int turn = 0;
+    // eight columns from c, some of which may lie outside the row
+    auto whole = [&](int c) { return c >= 0 && c + 8 <= H; };
+    auto edge = [&](const auto* p, int c, float (&f)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = c + j >= 0 && c + j < H ? to_f32(p[c + j]) : 0.f;
+    };
     auto load = [&](const T* p, int c, const void* base, int64_t ld) {
-        if (VEC) return c < H ? load8_all<T>(p + c) : Raw8<T>{};
-        const T* begin = static_cast<const T*>(base);
-        return c + 8 <= H ? load8_near<T>(p + c, begin, begin + (a.T - 1) * ld + H) : c < H ? load8<T, false>(p + c, H - c) : Raw8<T>{};
+        if (whole(c)) {
+            if (PIECES) return load8_all<T>(p + c);
+            const T* begin = static_cast<const T*>(base);
+            return load8_near<T>(p + c, begin, begin + (a.T - 1) * ld + H);
+        }
+        Raw8<T> r{};
+        if (c > -8 && c < H) {
+            float f[8];
+            edge(p, c, f);
+            if constexpr (sizeof(T) == 4) {
+                r.v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                r.w = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+            } else {
+                r.v = make_uint4(pack2(f[0], f[1], T()), pack2(f[2], f[3], T()), pack2(f[4], f[5], T()), pack2(f[6], f[7], T()));
+            }
+        }
+        return r;
     };
-    auto weights = [&](int c, F2 (&w)[4]) {
-        if (VEC || c < H) pairs8<W>(weight_at<W, VEC>(wt, c, H), w);
-        else w[0] = w[1] = w[2] = w[3] = 0;
+    // the thread's weights, FP32, in places of its own in shared memory; long rows read them anew
+    float4* own_w = reinterpret_cast<float4*>(dw_rows) + (size_t)g * 2 * N * G + threadIdx.x;
+    if (VPT > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float f[8];
+            edge(wt, c0 + i * step, f);
+            own_w[(2 * i) * G] = make_float4(f[0], f[1], f[2], f[3]);
+            own_w[(2 * i + 1) * G] = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+    auto weights = [&](int i, F2 (&w)[4]) {
+        float f[8];
+        if (VPT > 0) {
+            const float4 lo = own_w[(2 * i) * G], hi = own_w[(2 * i + 1) * G];
+            w[0] = f2(lo.x, lo.y);
+            w[1] = f2(lo.z, lo.w);
+            w[2] = f2(hi.x, hi.y);
+            w[3] = f2(hi.z, hi.w);
+            return;
+        }
+        const int c = c0 + i * step;
+        if (whole(c) && ((reinterpret_cast<uintptr_t>(wt + c)) & 15) == 0) {
+            pairs8<W>(load8_all<W>(wt + c), w);
+            return;
+        }
+        edge(wt, c, f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = f2(f[2 * j], f[2 * j + 1]);
     };
-
-    for (int64_t t = first; t < a.T; t += (int64_t)gridDim.x * blockDim.y, turn ^= 1) {
+    Raw8<T> rdy[N], rh[N], rdh[N];
+    auto fetch = [&](int64_t t) {
+        const T* dy = static_cast<const T*>(a.dy) + t * a.lddy;
+        const T* h = static_cast<const T*>(a.h) + t * a.ldh;
+        const T* dh = a.dh ? static_cast<const T*>(a.dh) + t * a.lddh : nullptr;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int c = c0 + i * step;
+            rdy[i] = load(dy, c, a.dy, a.lddy);
+            rh[i] = load(h, c, a.h, a.ldh);
+            rdh[i] = dh ? load(dh, c, a.dh, a.lddh) : Raw8<T>{};
+        }
+    };
+    if (AHEAD && first < a.T) fetch(first);
+    for (int64_t t = first; t < a.T; t += stride, turn ^= 1) {
         const T* dy = static_cast<const T*>(a.dy) + t * a.lddy;
         const T* h = static_cast<const T*>(a.h) + t * a.ldh;
         const T* dh = a.dh ? static_cast<const T*>(a.dh) + t * a.lddh : nullptr;
         T* dx = static_cast<T*>(a.dx) + t * a.lddx;
         const float s = a.rstd[t];
-        auto dot8 = [&](int c, const Raw8<T>& rdy, const Raw8<T>& rh, F2 sum) {
+        auto dot8 = [&](int i, const Raw8<T>& qdy, const Raw8<T>& qh, F2 sum) {
             F2 fy[4], fh[4], w[4];
-            pairs8<T>(rdy, fy);
-            pairs8<T>(rh, fh);
-            weights(c, w);
+            pairs8<T>(qdy, fy);
+            pairs8<T>(qh, fh);
+            weights(i, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum = fma2(mul2(fy[j], w[j]), fh[j], sum);
             return sum;
         };
-        auto write = [&](int c, const Raw8<T>& rdy, const Raw8<T>& rh, const Raw8<T>& rdh, float k, F2 (&acc)[4]) {
+        // every lane of the warp gets here
+        auto write = [&](int i, const Raw8<T>& qdy, const Raw8<T>& qh, const Raw8<T>& qdh, float k, F2 (&acc)[4]) {
+            const int c = c0 + i * step;
             F2 fy[4], fh[4], fd[4], w[4];
-            pairs8<T>(rdy, fy);
-            pairs8<T>(rh, fh);
-            pairs8<T>(rdh, fd);
-            weights(c, w);
+            pairs8<T>(qdy, fy);
+            pairs8<T>(qh, fh);
+            pairs8<T>(qdh, fd);
+            weights(i, w);
             const F2 ss = f2(s, s), mk = f2(-k, -k);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -288,281 +352,75 @@ __global__ void __launch_bounds__(VPT > 0 ? kBwdThreads : 1024) rmsnorm_backward
             }
             float o[8];
             floats8(fd, o);
-            if (!VEC) store8_near<T>(dx + c, o, H - c);        // every lane of the warp gets here
-            else store8<T, true>(dx + c, o, 8);
+            if (!PIECES) {
+                store8_near<T>(dx + c, o, H - c);
+            } else if (whole(c)) {
+                store8<T, true>(dx + c, o, 8);
+            } else if (c > -8 && c < H) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j >= 0 && c + j < H) dx[c + j] = from_f32<T>(o[j]);
+            }
         };
         F2 sum = f2(0.f, 0.f);
         if constexpr (VPT > 0) {
-            Raw8<T> rdy[VPT], rh[VPT], rdh[VPT];
+            if (!AHEAD) fetch(t);
+            Raw8<T> cdy[VPT], ch[VPT], cdh[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int c = 8 * (threadIdx.x + i * G);
-                rdy[i] = load(dy, c, a.dy, a.lddy);
-                rh[i] = load(h, c, a.h, a.ldh);
-                rdh[i] = dh ? load(dh, c, a.dh, a.lddh) : Raw8<T>{};
+                cdy[i] = rdy[i];
+                ch[i] = rh[i];
+                cdh[i] = rdh[i];
             }
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int c = 8 * (threadIdx.x + i * G);
-                if (!VEC || c < H) sum = dot8(c, rdy[i], rh[i], sum);
-            }
+            for (int i = 0; i < VPT; ++i) sum = dot8(i, cdy[i], ch[i], sum);
+            if (AHEAD && t + stride < a.T) fetch(t + stride);
             const float2 p = f2(sum);
             const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int c = 8 * (threadIdx.x + i * G);
-                if (!VEC || c < H) write(c, rdy[i], rh[i], rdh[i], k, dw[i]);
-            }
+            for (int i = 0; i < VPT; ++i) write(i, cdy[i], ch[i], cdh[i], k, dw[i]);
         } else {
-            const int rounds = (H + step - 1) / step;
+            const int rounds = (H + shift + step - 1) / step;
             for (int i = 0; i < rounds; ++i) {
-                const int c = 8 * threadIdx.x + i * step;
-                if (!VEC || c < H) sum = dot8(c, load(dy, c, a.dy, a.lddy), load(h, c, a.h, a.ldh), sum);
+                const int c = c0 + i * step;
+                sum = dot8(i, load(dy, c, a.dy, a.lddy), load(h, c, a.h, a.ldh), sum);
             }
             const float2 p = f2(sum);
             const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
             for (int i = 0; i < rounds; ++i) {
-                const int c = 8 * threadIdx.x + i * step;
+                const int c = c0 + i * step;
                 float f[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = c + j < H && t != first ? part[c + j] : 0.f;
+                for (int j = 0; j < 8; ++j) f[j] = c + j >= 0 && c + j < H && t != first ? part[c + j] : 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dw[0][j] = f2(f[2 * j], f[2 * j + 1]);
-                if (!VEC || c < H) write(c, load(dy, c, a.dy, a.lddy), load(h, c, a.h, a.ldh), dh ? load(dh, c, a.dh, a.lddh) : Raw8<T>{}, k, dw[0]);
+                write(i, load(dy, c, a.dy, a.lddy), load(h, c, a.h, a.ldh), dh ? load(dh, c, a.dh, a.lddh) : Raw8<T>{}, k, dw[0]);
                 floats8(dw[0], f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (c + j < H) part[c + j] = f[j];
+                    if (c + j >= 0 && c + j < H) part[c + j] = f[j];
             }
         }
     }
     if constexpr (VPT > 0) {
-        // the R rows' shares in the order of the rows; [j][thread] keeps neighbouring threads in neighbouring banks
-        float f[VPT][8];
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) floats8(dw[i], f[i]);
-        if (g > 0) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) dw_rows[((g - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x] = f[i][j];
-        }
-        __syncthreads();
-        if (g > 0) return;
-        for (int r = 1; r < (int)blockDim.y; ++r)
-#pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[i][j] += dw_rows[((r - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x];
+        // the R rows' shares in the order of the rows; their shifts may differ, so each has all H columns
+        __syncthreads();                               // the weights have been read
+        float* mine = dw_rows + (int64_t)g * H;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int c = 8 * (threadIdx.x + i * G);
+            const int c = c0 + i * step;
+            float f[8];
+            floats8(dw[i], f);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (c + j < H) part[c + j] = f[i][j];
+                if (c + j >= 0 && c + j < H) mine[c + j] = f[j];
         }
-    }
-}
-
-// The same for rows off 16-byte boundaries, brought to shared memory by bulk copies, two rows ahead for each of the R rows
-// at a time.  A row is copied in whole
-// 16-byte pieces, from the boundary before its start to the one after its end, so its place may be any multiple of
-// an element; every tensor starts on a boundary, a row has 64 bytes or more (so that only the last row's last piece can
-// reach beyond the tensor), and what that piece would bring is loaded element by element.
-// The bounded waits raise a status word (gpd_device_status) and skip what is left.
-constexpr int kRing = 2, kRingThreads = 1024;
-__device__ int g_norm_status = 0;
-// room for a row from a boundary on, and for the last piece that a thread reads around its elements
-__host__ __device__ constexpr int span_bytes(int64_t H, int e) { return (int)((H * e + 15) / 16 + (e == 4 ? 2 : 1)) * 16; }
-
-template <typename T, typename W, int VPT>
-__global__ void __launch_bounds__(kRingThreads) rmsnorm_backward_ring_kernel(const NormBwdArgs a) {
-    __shared__ float scratch[16][2][32];
-    __shared__ __align__(8) uint64_t full[16][kRing];
-    __shared__ int abort_flag;
-    extern __shared__ __align__(16) uint8_t ring[];    // [R][kRing][3][span]; afterwards the rows' shares of dw
-    const int G = blockDim.x, g = threadIdx.y, H = (int)a.H, span = span_bytes(H, sizeof(T));
-    const W* wt = static_cast<const W*>(a.weight);
-    const int64_t stride = (int64_t)gridDim.x * blockDim.y, first = (int64_t)blockIdx.x * blockDim.y + g;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kRing; ++i) tc::mbar_init(&full[g][i], 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (threadIdx.x == 0 && g == 0) abort_flag = 0;
-    __syncthreads();
-    after_previous();
-
-    auto tensor = [&](int k) { return k == 0 ? a.dy : k == 1 ? a.h : a.dh; };
-    auto ld_of = [&](int k) { return k == 0 ? a.lddy : k == 1 ? a.ldh : a.lddh; };
-    auto buffer = [&](int i, int k) { return ring + ((size_t)((g * kRing + i) * 3 + k)) * span; };
-    // first byte of a row, and the bytes that whole pieces bring from the boundary before it
-    auto place = [&](int k, int64_t t, int& mis, int& bytes, bool& cut) {
-        const int64_t at = t * ld_of(k) * (int64_t)sizeof(T);
-        mis = (int)(at & 15);
-        bytes = (mis + H * (int)sizeof(T) + 15) & ~15;
-        cut = t == a.T - 1 && ((mis + H * (int)sizeof(T)) & 15) != 0;      // the last piece ends beyond the tensor
-        if (cut) bytes -= 16;
-        return static_cast<const uint8_t*>(tensor(k)) + at - mis;
-    };
-    auto send = [&](int64_t t, int i) {                // thread 0 of the row
-        int mis, bytes, sum = 0;
-        bool cut;
-        for (int k = 0; k < (a.dh ? 3 : 2); ++k) {
-            place(k, t, mis, bytes, cut);
-            sum += bytes;
+        __syncthreads();
+        for (int c = g * G + threadIdx.x; c < H; c += G * blockDim.y) {
+            float v = dw_rows[c];
+            for (int r = 1; r < (int)blockDim.y; ++r) v += dw_rows[(int64_t)r * H + c];
+            part[c] = v;
         }
-        tc::mbar_expect_tx(&full[g][i], sum);
-        for (int k = 0; k < (a.dh ? 3 : 2); ++k) {
-            const uint8_t* src = place(k, t, mis, bytes, cut);
-            if (bytes > 0)
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(tc::smem_u32(buffer(i, k))), "l"(src), "r"(bytes), "r"(tc::smem_u32(&full[g][i])) : "memory");
-        }
-    };
-    if (threadIdx.x == 0)
-        for (int i = 0; i < kRing; ++i)
-            if (first + i * stride < a.T) send(first + i * stride, i);
-
-    F2 dw[VPT][4];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dw[i][j] = f2(0.f, 0.f);
-    auto group_sync = [&]() {
-        if (G > 32) asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "r"(G) : "memory");
-        else __syncwarp();
-    };
-    int turn = 0, slot = 0;
-    uint32_t phase = 0;
-    bool live = true;
-    int rows = 0, lost = 0;                            // rows so far; the one whose copies did not come
-    for (int64_t t = first; t < a.T; t += stride, turn ^= 1, ++rows) {
-        if (live && !tc::mbar_wait(&full[g][slot], phase, &abort_flag, &g_norm_status)) {
-            live = false;
-            lost = rows;
-        }
-        const T* at[3];                                // the row's first elements
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            int mis = 0, bytes = 0;
-            bool cut = false;
-            const uint8_t* src = k < 2 || a.dh ? place(k, t, mis, bytes, cut) : nullptr;
-            at[k] = reinterpret_cast<const T*>(buffer(slot, k) + mis);
-            if (cut) {                                 // what is left of the row, by the elements
-                const int from = (bytes - mis) / (int)sizeof(T) > 0 ? (bytes - mis) / (int)sizeof(T) : 0;
-                const T* row = reinterpret_cast<const T*>(src + mis);
-                T* to = reinterpret_cast<T*>(buffer(slot, k) + mis);
-                for (int j = from + threadIdx.x; j < H; j += G) to[j] = row[j];
-            }
-        }
-        if (t == a.T - 1) group_sync();
-        const float s = a.rstd[t];
-        T* dx = static_cast<T*>(a.dx) + t * a.lddx;
-        // eight elements from column c of a row in shared memory; pieces that surround them are inside the ring
-        auto near = [&](const T* p, int c, F2 (&f)[4]) {
-            const int mis = (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
-            if (mis == 0) {
-                pairs8<T>(load8_all<T>(p + c), f);
-            } else {
-                const uint4* v = reinterpret_cast<const uint4*>(p + c - mis);
-                const uint4 x = v[0], y = v[1];
-                const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                uint32_t o[4];
-                Raw8<T> r;
-                shifted4<T>(w, mis, o);
-                r.v = make_uint4(o[0], o[1], o[2], o[3]);
-                if constexpr (sizeof(T) == 4) {
-                    const uint4 z = v[2];
-                    const uint32_t u[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
-                    shifted4<T>(u, mis, o);
-                    r.w = make_uint4(o[0], o[1], o[2], o[3]);
-                }
-                pairs8<T>(r, f);
-            }
-            if (c + 8 > H) {                           // columns beyond the row
-                float q[8];
-                floats8(f, q);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = c + j < H ? q[j] : 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = f2(q[2 * j], q[2 * j + 1]);
-            }
-        };
-        F2 sum = f2(0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int c = 8 * (threadIdx.x + i * G);
-            if (c < H) {
-                F2 fy[4], fh[4], w[4];
-                near(at[0], c, fy);
-                near(at[1], c, fh);
-                pairs8<W>(weight_at<W, false>(wt, c, H), w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum = fma2(mul2(fy[j], w[j]), fh[j], sum);
-            }
-        }
-        const float2 p = f2(sum);
-        const float k = s * s * (row_sum(p.x + p.y, G, g, scratch[g][turn]) / (float)H);
-        const F2 ss = f2(s, s), mk = f2(-k, -k);
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int c = 8 * (threadIdx.x + i * G);
-            float o[8];
-            if (c < H) {
-                F2 fy[4], fh[4], fd[4], w[4];
-                near(at[0], c, fy);
-                near(at[1], c, fh);
-                if (a.dh) near(at[2], c, fd);
-                else fd[0] = fd[1] = fd[2] = fd[3] = f2(0.f, 0.f);
-                pairs8<W>(weight_at<W, false>(wt, c, H), w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    dw[i][j] = fma2(mul2(fy[j], ss), fh[j], dw[i][j]);
-                    fd[j] = fma2(ss, fma2(fh[j], mk, mul2(fy[j], w[j])), fd[j]);
-                }
-                floats8(fd, o);
-            }
-            store8_near<T>(dx + c, o, H - c);          // every lane of the warp
-        }
-        group_sync();                                  // the slot has been read
-        if (threadIdx.x == 0 && live && t + kRing * stride < a.T) send(t + kRing * stride, slot);
-        if (++slot == kRing) {
-            slot = 0;
-            phase ^= 1;
-        }
-    }
-    if (!live && threadIdx.x == 0) {                   // copies still under way land before the CTA goes on, or time runs out
-        for (int i = lost; i < lost + kRing && first + i * stride < a.T; ++i) {
-            const long long t0 = clock64();
-            while (!tc::mbar_try_wait(&full[g][i % kRing], (i / kRing) & 1) && clock64() - t0 < tc::kWaitCycles) {}
-        }
-    }
-    // the R rows' shares in the order of the rows; [j][thread] keeps neighbouring threads in neighbouring banks
-    float f[VPT][8];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) floats8(dw[i], f[i]);
-    __syncthreads();                                   // every copy that was sent for has been waited for by its row
-    float* dw_rows = reinterpret_cast<float*>(ring);   // [R - 1][8 VPT G]
-    if (g > 0) {
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) dw_rows[((g - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x] = f[i][j];
-    }
-    __syncthreads();
-    if (g > 0) return;
-    float* part = a.parts + (int64_t)blockIdx.x * a.H;
-    for (int r = 1; r < (int)blockDim.y; ++r)
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] += dw_rows[((r - 1) * 8 * VPT + 8 * i + j) * G + threadIdx.x];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int c = 8 * (threadIdx.x + i * G);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c + j < H) part[c + j] = f[i][j];
     }
 }
 
@@ -585,36 +443,36 @@ __global__ void __launch_bounds__(512) rmsnorm_dweight_kernel(const float* parts
 
 template <typename T, typename W>
 gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
-    constexpr int e = sizeof(T), V = e == 4 ? 2 : 4;   // vectors per thread that fit in registers
-    const int64_t vecs = (a.H + 7) / 8;
-    constexpr int RV = V / 2;                          // of the ring kernel: twice the threads
-    const bool bases = aligned(a.dy, 16) && aligned(a.h, 16) && aligned(a.dh, 16);
-    // one CTA per SM: R rows of G threads at a time, as many as it takes for T rows
-    const int room = 220 * 1024 / (3 * kRing * span_bytes(std::min<int64_t>(a.H, 1 << 20), e));
-    const bool vec = a.H % 8 == 0 && rows_aligned(a.dy, a.lddy, e) && rows_aligned(a.h, a.ldh, e) && rows_aligned(a.dh, a.lddh, e) &&
-                     rows_aligned(a.dx, a.lddx, e) && aligned(a.weight, 16);
-    // rows on boundaries: registers (4000 x 4096 BF16: 37 us, through the ring 51); off them: the ring (4000 x 4133: 69 us,
-    // from registers 114), where it has room and is allowed; long rows: read twice
-    const bool ring = !vec && bases && a.H * e >= 64 && vecs <= kRingThreads * RV && room > 0, loop = !ring && vecs > kBwdThreads * V;
-    const int per = ring ? RV : V, G = loop ? 1024 : (int)(((vecs + per - 1) / per + 31) / 32 * 32);
-    int R = loop ? 1 : std::max(1, std::min((ring ? kRingThreads : kBwdThreads) / G, 15));      // named barriers 1 .. 15
-    if (ring) R = std::min(R, room);
+    constexpr int e = sizeof(T), per16 = 16 / e, V = e == 4 ? 2 : 4;   // vectors per thread that fit in registers
+    // whether the tensors' rows start equally far from 16-byte boundaries, and whether that differs from row to row
+    auto like_h = [&](const void* p, int64_t ld) { return !p || (aligned(p, 16) && (ld - a.ldh) % per16 == 0); };
+    const bool pieces = like_h(a.dy, a.lddy) && like_h(a.h, a.ldh) && like_h(a.dh, a.lddh) && like_h(a.dx, a.lddx);
+    const bool shifts = pieces && a.ldh % per16 != 0;
+    const int64_t vecs = (a.H + 7 + (shifts ? per16 - 1 : 0)) / 8;
+    // two vectors per thread leave room for the next row (4096 x 4096 BF16: 33 us, without it 37 from four vectors);
+    // FP32 rows do not gain from it (one vector 49.8 us, two without the next row 48.5)
+    // nor do rows for which it would leave more than a quarter of the CTA's 512 threads out
+    auto group = [&](int per) { return (int)(((vecs + per - 1) / per + 31) / 32 * 32); };
+    const bool ahead = e == 2 && pieces && vecs <= kBwdThreads * V / 2 && kBwdThreads / group(V / 2) * group(V / 2) >= kBwdThreads * 3 / 4;
+    const bool loop = !ahead && vecs > kBwdThreads * V;
+    const int per = ahead ? V / 2 : V, G = loop ? 1024 : group(per);
+    // one CTA per SM: R rows of G threads at a time, as many as it takes for T rows; named barriers 1 .. 15
+    int R = loop ? 1 : std::max(1, std::min(kBwdThreads / G, 15));
     R = (int)std::max<int64_t>(1, std::min<int64_t>(R, (a.T + sm_count() - 1) / sm_count()));
-    const int parts = (int)std::min<int64_t>(std::min<int64_t>((a.T + R - 1) / R, sm_count()), GPD_RMSNORM_MAX_PARTS);
+    int parts = (int)std::min<int64_t>(std::min<int64_t>((a.T + R - 1) / R, sm_count()), GPD_RMSNORM_MAX_PARTS);
+    // a thread's rows are a multiple of per16 apart where the shifts differ, unless it has one row only
+    if (shifts && (int64_t)parts * R < a.T) {
+        while (R > 1 && R % 2) --R;
+        while ((int64_t)parts * R % per16 != 0) --parts;
+    }
     if (parts > 0) {
-        const int shares = (R - 1) * 8 * per * G * (int)sizeof(float);  // at most 64 KB
-        gpd_status rc;
-        if (loop) {
-            rc = launch_after(vec ? rmsnorm_backward_kernel<T, W, 0, true> : rmsnorm_backward_kernel<T, W, 0, false>, dim3(parts),
-                              dim3(1024), 0, 1, st, a);
-        } else {
-            const int smem = ring ? std::max(shares, R * 3 * kRing * span_bytes(a.H, e)) : shares;
-            auto kernel = ring ? rmsnorm_backward_ring_kernel<T, W, RV>
-                          : vec ? rmsnorm_backward_kernel<T, W, V, true> : rmsnorm_backward_kernel<T, W, V, false>;
-            if (smem > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-                return GPD_ERR_CUDA;
-            rc = launch_after(kernel, dim3(parts), dim3(G, R), smem, 1, st, a);
-        }
+        auto kernel = loop    ? (pieces ? rmsnorm_backward_kernel<T, W, 0, true, false> : rmsnorm_backward_kernel<T, W, 0, false, false>)
+                      : ahead ? rmsnorm_backward_kernel<T, W, V / 2, true, e == 2>
+                              : (pieces ? rmsnorm_backward_kernel<T, W, V, true, false> : rmsnorm_backward_kernel<T, W, V, false, false>);
+        const int smem = loop ? 0 : R * G * per * 32;  // at most 64 KB; H <= 8 per G
+        if (smem > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+            return GPD_ERR_CUDA;
+        const gpd_status rc = launch_after(kernel, dim3(parts), dim3(G, R), smem, 1, st, a);
         if (rc != GPD_OK) return rc;
     }
     const float* partial = a.parts;
@@ -622,13 +480,6 @@ gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
 }
 
 }  // namespace
-
-int norm_device_status_fetch_and_clear() {
-    int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_norm_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
-    if (v != 0) cudaMemcpyToSymbol(g_norm_status, &zero, sizeof(int));
-    return v;
-}
 
 }  // namespace gpd
 

@@ -223,3 +223,31 @@ def test_refusals():
     assert L.gpd_rmsnorm_quant(1, None, 256, None, 0, 1, p, 1e-5, None, 0, None, 0, 3, None, 0, None, 0, None, 4, 256, None) == g.GPD_ERR_ARG
     assert L.gpd_quantize_blocks(1, p, 256, 1, 1, p, 256, p, 2, None, 0, None, 0, 4, 256, None) == g.GPD_ERR_ARG
     assert L.gpd_quantize_blocks(1, p, 256, 3, 1, p, 256, p, 1, None, 0, None, 0, 4, 256, None) == g.GPD_ERR_SHAPE
+
+
+@pytest.mark.parametrize("T,H", [(1, 5), (3, 129), (500, 264), (300, 1001), (7, 4133), (450, 4100), (2, 9001), (3, 16500)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("same_stride", [True, False])
+def test_norm_gradient_of_rows_off_boundaries(T, H, dtype, same_stride):
+    """Rows that start anywhere: tensors that share their distances from 16-byte boundaries (odd strides, aligned
+    buffers), and tensors that do not (other strides, buffers that start off a boundary)."""
+    pads, offs = ((3, 3, 3, 3), (0, 0, 0, 0)) if same_stride else ((1, 5, 2, 7), (0, 1, 3, 2))
+    h, dy, dh = (like(_rand(i, T, H) * 2, dtype, pads[i], offs[i]) for i in range(3))
+    dx = strided(T, H, dtype, pads[3], offs[3])
+    guard = dx._base.clone() if dx._base is not None else None
+    w = 1 + 0.2 * _rand(4, H)
+    rstd = (h.float().square().mean(1) + 1e-5).rsqrt()
+    dw, ws = torch.full((H,), float("nan"), device="cuda"), torch.full((min(T, 512) * H,), float("nan"), device="cuda")
+    g.gpd_rmsnorm_backward(dy, h, w, rstd, dx, dw, ws, dresidual=dh)
+    H64, dY, s, W = h.double(), dy.double(), rstd.double()[:, None], w.double()
+    gr = dY * W
+    mean = (gr * H64).mean(1, keepdim=True)
+    size = s * (gr.abs() + H64.abs() * s * s * (gr * H64).abs().mean(1, keepdim=True)) + dh.double().abs()
+    check_close(dx, s * (gr - H64 * s * s * mean) + dh.double(), EPS_Y, size)
+    n = -(-T // min(T, 128)) + 72
+    check_close(dw, (dY * H64 * s).sum(0), (n + 3) * 2.0 ** -24, (dY * H64 * s).abs().sum(0))
+    if guard is not None:                                        # nothing was written between the rows
+        now = dx._base.clone()
+        view = torch.as_strided(now, dx.shape, dx.stride(), dx.storage_offset())
+        view.copy_(torch.as_strided(guard, dx.shape, dx.stride(), dx.storage_offset()))
+        assert torch.equal(now.view(torch.uint8), guard.view(torch.uint8))
