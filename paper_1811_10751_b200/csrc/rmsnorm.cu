@@ -443,19 +443,19 @@ __global__ void __launch_bounds__(512) rmsnorm_dweight_kernel(const float* parts
 
 template <typename T, typename W>
 gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
-    constexpr int e = sizeof(T), per16 = 16 / e, V = e == 4 ? 2 : 4;   // vectors per thread that fit in registers
+    constexpr int e = sizeof(T), per16 = 16 / e, V = e == 4 ? 2 : 3, A = 2;   // vectors per thread that fit in registers, with the next row's (16-bit)
     // whether the tensors' rows start equally far from 16-byte boundaries, and whether that differs from row to row
     auto like_h = [&](const void* p, int64_t ld) { return !p || (aligned(p, 16) && (ld - a.ldh) % per16 == 0); };
     const bool pieces = like_h(a.dy, a.lddy) && like_h(a.h, a.ldh) && like_h(a.dh, a.lddh) && like_h(a.dx, a.lddx);
     const bool shifts = pieces && a.ldh % per16 != 0;
     const int64_t vecs = (a.H + 7 + (shifts ? per16 - 1 : 0)) / 8;
-    // two vectors per thread leave room for the next row (4096 x 4096 BF16: 33 us, without it 37 from four vectors);
+    // two vectors per thread leave room for the next row (4096 x 4096 BF16: 32 us, without it 37 from four vectors);
     // FP32 rows do not gain from it (one vector 49.8 us, two without the next row 48.5)
     // nor do rows for which it would leave more than a quarter of the CTA's 512 threads out
     auto group = [&](int per) { return (int)(((vecs + per - 1) / per + 31) / 32 * 32); };
-    const bool ahead = e == 2 && pieces && vecs <= kBwdThreads * V / 2 && kBwdThreads / group(V / 2) * group(V / 2) >= kBwdThreads * 3 / 4;
+    const bool ahead = e == 2 && pieces && vecs <= kBwdThreads * A && kBwdThreads / group(A) * group(A) >= kBwdThreads * 3 / 4;
     const bool loop = !ahead && vecs > kBwdThreads * V;
-    const int per = ahead ? V / 2 : V, G = loop ? 1024 : group(per);
+    const int per = ahead ? A : V, G = loop ? 1024 : group(per);
     // one CTA per SM: R rows of G threads at a time, as many as it takes for T rows; named barriers 1 .. 15
     int R = loop ? 1 : std::max(1, std::min(kBwdThreads / G, 15));
     R = (int)std::max<int64_t>(1, std::min<int64_t>(R, (a.T + sm_count() - 1) / sm_count()));
@@ -467,7 +467,7 @@ gpd_status launch_bwd(const NormBwdArgs& a, float* dweight, cudaStream_t st) {
     }
     if (parts > 0) {
         auto kernel = loop    ? (pieces ? rmsnorm_backward_kernel<T, W, 0, true, false> : rmsnorm_backward_kernel<T, W, 0, false, false>)
-                      : ahead ? rmsnorm_backward_kernel<T, W, V / 2, true, e == 2>
+                      : ahead ? rmsnorm_backward_kernel<T, W, A, true, e == 2>
                               : (pieces ? rmsnorm_backward_kernel<T, W, V, true, false> : rmsnorm_backward_kernel<T, W, V, false, false>);
         const int smem = loop ? 0 : R * G * per * 32;  // at most 64 KB; H <= 8 per G
         if (smem > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
