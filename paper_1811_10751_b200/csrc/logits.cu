@@ -789,7 +789,7 @@ gpd_status launch_distill(const DistillArgs& a, cudaStream_t st) {
     return launch_rows(distill_kernel<T>, a, a.T, C, row_threads(a.V / C), st);
 }
 
-bool bad_rows(int64_t T, int64_t V) { return T < 0 || V <= 0 || V > 0x7fffff00; }
+bool bad_rows(int64_t T, int64_t V) { return T < 0 || V <= 0 || V > 0x40000000; }
 
 }  // namespace
 
