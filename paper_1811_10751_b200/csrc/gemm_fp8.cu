@@ -30,6 +30,10 @@
 // Few tiles (short A and B, long K): the CTAs of a cluster take a part of the contraction each; the parts
 // meet through distributed shared memory and are added in the order of the parts.
 //
+// Measured: 8192^3 to BF16 391 us in a burst (2810 TFLOP/s), 444 sustained, at 455 of 448 cycles a k-block and the power
+// limit; 4096 x 4096 x 4100 to FP32 89 us with rows 4112 bytes apart, 62 on 128-byte boundaries to BF16;
+// 7 x 4096 x 4096 6.5 us.
+//
 // Every mbarrier wait is bounded; on expiry the CTA raises a status word (gpd_device_status), drains its
 // copies, frees its tensor memory and returns.
 #include <cuda.h>

@@ -9,6 +9,10 @@
 // patch at rows 8 rg, columns 8 cg.  A row's sixteen column groups sit in sixteen adjacent lanes (maximum
 // by shuffles); the column maxima meet in shared memory.  A patch's column is eight bytes of a transposed
 // row, so the transposed tile goes through shared memory in 8-byte pieces and leaves in 16-byte ones.
+//
+// Measured: 4096 x 8192 BF16 both ways 29.6 us, 0.70 of the copy bandwidth (issue slots 57 % busy: two conversions and
+// the maxima per element); 1000 x 4096 FP32 in 128 x 128 blocks 5.3 us.  A CTA per tile, three on an SM: tiles of other
+// shapes would hold parts of blocks of one kind or the other.
 #include "lm_common.h"
 
 namespace gpd {
