@@ -560,6 +560,10 @@ struct LogprobBwdArgs {
     float inv_tau;
 };
 
+// Log probabilities below this one are taken for it: 2^x of them is 0, and p (log p + H) g has to be 0 there for every g
+// in use, so log p g may not overflow (a masked entry's log p is -inf, or -3e38 under a mask of the lowest value).
+constexpr float kLeastLogp = -1024.f;
+
 template <typename T>
 __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_backward_kernel(const LogprobBwdArgs a) {
     __shared__ float g[kMaxTokens], x_at[kMaxTokens];
@@ -588,7 +592,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_backward_kernel(const
     const bool none = lse == -INFINITY;
     auto dp = [&](float x) {                           // at a token, without its own term
         const float logp = fmaf(x, a.inv_tau, -lse), p = ex2(logp * kLog2e);
-        return none ? 0.f : p * fmaf(-gh, fmaxf(logp, -FLT_MAX), c) * a.inv_tau;
+        return none ? 0.f : p * fmaf(-gh, fmaxf(logp, kLeastLogp), c) * a.inv_tau;
     };
     const F2 it = f2(a.inv_tau, a.inv_tau), ml = f2(-lse, -lse), l2e = f2(kLog2e, kLog2e), mg = f2(-gh * a.inv_tau, -gh * a.inv_tau),
              cc = f2(c * a.inv_tau, c * a.inv_tau);
@@ -598,7 +602,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_backward_kernel(const
         write_gradient(in, d, [&](F2 x) {
             const F2 logp = fma2(x, it, ml);
             const float2 l = f2(logp);
-            return mul2(ex2_pair(mul2(logp, l2e)), fma2(mg, f2(fmaxf(l.x, -FLT_MAX), fmaxf(l.y, -FLT_MAX)), cc));
+            return mul2(ex2_pair(mul2(logp, l2e)), fma2(mg, f2(fmaxf(l.x, kLeastLogp), fmaxf(l.y, kLeastLogp)), cc));
         });
     } else {
         write_gradient(in, d, [&](F2 x) { return mul2(ex2_pair(mul2(fma2(x, it, ml), l2e)), cc); });
