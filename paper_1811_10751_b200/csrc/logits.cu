@@ -659,7 +659,9 @@ struct __align__(16) TeacherList {
 template <typename T>
 __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillArgs a) {
     __shared__ Stats scratch[32], slots[kMaxSplit];
-    __shared__ TeacherList lists[2];                   // in turn, so that a row's last readers need no barrier
+    // In turn, so that a row's last readers need no barrier: the next row that fills a list takes the other one and passes
+    // block_merge, which all threads reach only after them.  Rows without weight pass no barrier and take no turn.
+    __shared__ TeacherList lists[2];
     after_previous();
     const int C = gridDim.x, rank = blockIdx.x, lane = threadIdx.x & 31;
     const float inv_tau = 1.f / a.tau, k = kLog2e * inv_tau;
@@ -667,7 +669,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
     slice(a.V, C, rank, v0, v1);
     Pieces<T, 4> in;
     int turn = 0;
-    for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y, turn ^= 1) {
+    for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
         const T* row = static_cast<const T*>(a.logits) + t * a.ld;
         T* d = a.d ? static_cast<T*>(a.d) + t * a.ldd : nullptr;
         in.template start<false>(row, v0, v1);
@@ -704,6 +706,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
             list.x[i] = ok ? to_f32(row[v]) : 0.f;     // before d, perhaps the same buffer, is written
         }
         st = block_merge(st, k, scratch);              // its barriers publish the list
+        turn ^= 1;
         if (C > 1) {
             cluster_all_here();
             to_peers(slots, C, rank, st);
