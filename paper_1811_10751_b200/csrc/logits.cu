@@ -715,10 +715,10 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
         }
         // the teacher's distribution, in every warp
         float tmax = -INFINITY, qs = 0.f;
-        bool bad = false;                              // an id beyond the row or a NaN
+        bool bad = false;                              // an id beyond the row, a NaN or +inf: the list's softmax is NaN
         for (int i = lane; i < a.K; i += 32) {
             const float x = list.t[i];
-            bad = bad || x != x || list.at[i] == kBeyond;
+            bad = bad || !(x < INFINITY) || list.at[i] == kBeyond;
             tmax = fmaxf(tmax, x);
         }
         bad = __any_sync(0xffffffffu, bad);
