@@ -521,9 +521,9 @@ gpd_status gpd_token_logprobs_backward(gpd_dtype type, const void* logits_dev, i
  *   dlogits = d(sum_t loss[t]) / d logits = w_t temperature (p - q)       (optional; may be the logits' buffer)
  * w_t = weights[t] (NULL: 1): mask and reduction, 1/T for a mean.  A row of weight 0 is not read: its loss and
  * gradient are 0, whatever its logits.  Entries of the list with a negative id or a logit of -inf do not count; a
- * list without any gives loss and gradient 0.  An id named twice has the sum of its q.  An id >= V, a NaN or +inf in
- * the list makes the loss NaN, NaN and +inf also the gradient at the list's ids; a row of -inf logits alone has
- * loss inf and gradient 0.
+ * list without any gives loss and gradient 0.  An id named twice has the sum of its q.  A NaN or +inf in the list
+ * makes the loss and the gradient at the list's ids NaN, an id >= V the loss and the row's whole gradient; a row of
+ * -inf logits alone has loss inf and gradient 0 (NaN where its list is such a one).
  */
 gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, int64_t ld, int32_t index_bytes,
                             const void* teacher_ids_dev, int64_t ldi, gpd_dtype teacher_type,

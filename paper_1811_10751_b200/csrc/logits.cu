@@ -715,13 +715,15 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
         }
         // the teacher's distribution, in every warp
         float tmax = -INFINITY, qs = 0.f;
-        bool bad = false;                              // an id beyond the row, a NaN or +inf: the list's softmax is NaN
+        bool bad = false, beyond = false;              // a NaN, +inf or an id beyond the row: no distribution; such an id
         for (int i = lane; i < a.K; i += 32) {
             const float x = list.t[i];
-            bad = bad || !(x < INFINITY) || list.at[i] == kBeyond;
+            beyond = beyond || list.at[i] == kBeyond;
+            bad = bad || !(x < INFINITY) || beyond;
             tmax = fmaxf(tmax, x);
         }
         bad = __any_sync(0xffffffffu, bad);
+        beyond = __any_sync(0xffffffffu, beyond);
         tmax = warp_max(tmax);
         if (tmax == -INFINITY && !bad) {               // nothing in the list
             nothing();
@@ -729,7 +731,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
         }
         for (int i = lane; i < a.K; i += 32) qs += list.t[i] == -INFINITY ? 0.f : ex2(k * (list.t[i] - tmax));
         qs = warp_sum(qs);
-        const bool none = st.s == 0.f;                 // every logit of the row is masked
+        const bool none = st.s == 0.f && !bad;         // every logit of the row is masked
         if (rank == 0 && threadIdx.x < 32) {
             const float log_s = logf(st.s), log_qs = logf(qs);
             float l = 0.f;
@@ -741,7 +743,8 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
             if (lane == 0) a.loss[t] = bad ? __uint_as_float(0x7fc00000u) : none ? INFINITY : wt * a.tau * a.tau * l;
         }
         if (d) {
-            const float scale = none ? 0.f : wt * a.tau / st.s, m = st.m;
+            // the share of an id beyond the row has no place in d: all of it is NaN, like the loss
+            const float scale = none ? 0.f : beyond ? __uint_as_float(0x7fc00000u) : wt * a.tau / st.s, m = st.m;
             const F2 mm = f2(-m, -m), kk = f2(k, k), sc = f2(scale, scale);
             write_gradient(in, d, [&](F2 x) { return mul2(sc, ex2_pair(mul2(add2(x, mm), kk))); });
             __syncthreads();

@@ -52,3 +52,33 @@ def test_teacher_logit_of_infinity(V, dtype, ttype, tau):
         check_close(d[r][~listed][None], p[r][~listed][None], REL)
     assert float(loss[3]) == 0 and bool((d[3] == 0).all())
     assert bool(torch.isfinite(loss[4:]).all()) and bool(torch.isfinite(d[4:]).all()) and torch.equal(loss[3:], alone[3:])
+
+
+@pytest.mark.parametrize("V", [300, 40000])
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_id_beyond_the_row_shows_in_the_gradient_too(V, index):
+    T, K = 5, 9
+    x, t, ids = _rand(1, T, V), _rand(2, T, K), _lists(T, V, K).to(index)
+    ids[0, 4] = V
+    ids[1, :] = V + 5
+    ids[2, 8] = 2 ** 31 - 1 if index == torch.int32 else 2 ** 40
+    x[2] = -math.inf
+    ids[3, 2], w = V, torch.ones(T, device="cuda")
+    w[3] = 0.0                                               # no weight: not read
+    loss, d = torch.full((T,), 5.0, device="cuda"), torch.full_like(x, 5.0)
+    g.gpd_distill_topk(x, ids, t, w, loss, dlogits=d)
+    for r in (0, 1, 2):
+        assert math.isnan(float(loss[r])) and bool(torch.isnan(d[r]).all()), r
+    assert float(loss[3]) == 0 and bool((d[3] == 0).all())
+    assert math.isfinite(float(loss[4])) and bool(torch.isfinite(d[4]).all())
+
+
+def test_masked_row_with_a_bad_list():
+    """Neither softmax exists: NaN, not the 0 that a masked row with a sound list gets."""
+    x, t, ids = torch.full((3, 500), -math.inf, device="cuda"), _rand(2, 3, 9), _lists(3, 500, 9)
+    t[0, 2], t[1, 2] = math.inf, math.nan
+    loss, d = torch.full((3,), 5.0, device="cuda"), torch.full_like(x, 5.0)
+    g.gpd_distill_topk(x, ids, t, None, loss, dlogits=d)
+    for r in (0, 1):
+        assert math.isnan(float(loss[r])) and bool(torch.isnan(d[r]).all())
+    assert float(loss[2]) == math.inf and bool((d[2] == 0).all())
