@@ -508,7 +508,8 @@ gpd_status gpd_token_logprobs(gpd_dtype type, const void* logits_dev, int64_t ld
  *   dlogits_v = (1/temperature) [ sum_g dlogprobs_g (1[v = token_g] - p_v) - dentropy p_v (log p_v + entropy) ]
  * dlogprobs [T][G] or NULL, dentropy [T] or NULL (entropy is needed with it), lse and entropy from the forward
  * call.  dlogits has the type of the logits and may be their buffer.  Tokens outside 0 .. V-1 have no gradient;
- * rows of -inf alone get 0.
+ * rows of -inf alone get 0.  p = exp(z - lse) takes lse as it was rounded: p is off by up to 2^-24 |lse| of itself,
+ * where a large offset of the logits or a low temperature makes |lse| large (the forward call's log probabilities are not).
  */
 gpd_status gpd_token_logprobs_backward(gpd_dtype type, const void* logits_dev, int64_t ld, int32_t index_bytes,
                                        const void* tokens_dev, int32_t G, float temperature, const float* lse_dev,

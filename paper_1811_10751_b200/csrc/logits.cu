@@ -3,7 +3,7 @@
 //
 // With z = x / tau, m = max x, k = log2(e) / tau:
 //   S = sum_v 2^(k (x_v - m)),   U = sum_v 2^(k (x_v - m)) (x_v - m)
-//   lse = m / tau + ln S,  log p_v = x_v / tau - lse,  entropy = ln S - U / (S tau)
+//   lse = m / tau + ln S,  log p_v = (x_v - m) / tau - ln S,  entropy = ln S - U / (S tau)
 // in one pass that keeps the running maximum and rescales S and U when it rises (FP32).  Partial results of
 // threads, warps and CTAs are merged by the same rule in a fixed order.
 //
@@ -326,9 +326,10 @@ __device__ __forceinline__ int64_t index_at(const void* p, int bytes, int64_t i)
     return bytes == 8 ? static_cast<const int64_t*>(p)[i] : (int64_t) static_cast<const int32_t*>(p)[i];
 }
 
-// lse in units of z; -inf where nothing is left
-__device__ __forceinline__ float lse_of(const Stats& st, float inv_tau) {
-    return st.s == 0.f ? -INFINITY : fmaf(st.m, inv_tau, logf(st.s));
+// Log probability of an entry x; -inf where nothing is left.  From its distance to the maximum and not from lse, whose
+// rounding goes by the size of the logits (3e-5 at 1000) and not of the result.
+__device__ __forceinline__ float logp_of(const Stats& st, float x, float inv_tau, float log_s) {
+    return st.s == 0.f ? -INFINITY : fmaf(x - st.m, inv_tau, -log_s);
 }
 
 // ---- top entries ---------------------------------------------------------------------------------------
@@ -526,15 +527,15 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogprobA
             st = from_peers(slots, C, k);
             if constexpr (TOP) merge_top(top, C, a.K);
         }
-        const float lse = lse_of(st, a.inv_tau);
+        const float log_s = logf(st.s);
         if (threadIdx.x == 0) {
-            a.lse[t] = lse;
-            if (a.entropy) a.entropy[t] = st.s == 0.f ? 0.f : logf(st.s) - st.u / st.s * a.inv_tau;
+            a.lse[t] = st.s == 0.f ? -INFINITY : fmaf(st.m, a.inv_tau, log_s);
+            if (a.entropy) a.entropy[t] = st.s == 0.f ? 0.f : log_s - st.u / st.s * a.inv_tau;
         }
         if ((int)threadIdx.x < a.G) {                  // at most 64, fewer than there are threads
             float lp = 0.f;
             if (token >= a.V) lp = __uint_as_float(0x7fc00000u);
-            else if (token >= 0) lp = st.s == 0.f ? -INFINITY : fmaf(x_token, a.inv_tau, -lse);
+            else if (token >= 0) lp = logp_of(st, x_token, a.inv_tau, log_s);
             a.logprobs[t * a.G + threadIdx.x] = lp;
         }
         if constexpr (TOP) {
@@ -542,8 +543,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) logprobs_kernel(const LogprobA
                 const uint64_t key = top.top[threadIdx.x];
                 a.top_ids[t * a.K + threadIdx.x] = (int32_t)(0xffffffffu - (uint32_t)key);
                 if (a.top_logprobs)
-                    a.top_logprobs[t * a.K + threadIdx.x] =
-                        st.s == 0.f ? -INFINITY : fmaf(value_of((uint32_t)(key >> 32)), a.inv_tau, -lse);
+                    a.top_logprobs[t * a.K + threadIdx.x] = logp_of(st, value_of((uint32_t)(key >> 32)), a.inv_tau, log_s);
             }
         }
         if (TOP) __syncthreads();                      // `top` is taken up again
