@@ -236,9 +236,9 @@ __device__ __forceinline__ Stats thread_stats(Pieces<T, U>& in, float k) {
             s = mul2(f2(f, f), s);
             m = top;
         }
-        // k (x - m), not k x - k m: differences stay finite for logits of any size
+        // k (x - m), not k x - k m, which is infinity less infinity for large logits
         const F2 mm = f2(-m, -m);
-        const bool masked = ENTROPY && bottom_of<T>(r) == -INFINITY;
+        const bool masked = ENTROPY && bottom_of<T>(r) - m == -INFINITY;       // -inf, or too far below m for FP32
 #pragma unroll
         for (int j = 0; j < (int)(sizeof(r) / sizeof(r[0])); ++j)
 #pragma unroll
