@@ -497,7 +497,8 @@ gpd_status gpd_gemm_fp8(gpd_dtype a_type, const void* A_dev, int64_t lda, const 
  *   lse[t];  entropy[t] = -sum_v p_v log p_v (optional);  top_ids [T][K] (int32) and top_logprobs [T][K]
  *   (optional): the K largest entries, equal ones in the order of their index, a NaN before all numbers.
  * -inf logits are masked entries; a row of them alone has lse and log probabilities -inf, entropy 0.  A NaN or
- * +inf in a row makes its lse, log probabilities and entropy NaN.  K <= V.
+ * +inf in a row makes its lse, log probabilities and entropy NaN.  K <= V.  Temperatures below
+ * 4.3e-39, whose reciprocals are no FP32 numbers, are refused, here and in the two calls below.
  */
 gpd_status gpd_token_logprobs(gpd_dtype type, const void* logits_dev, int64_t ld, int32_t index_bytes,
                               const void* tokens_dev, int32_t G, float temperature, float* logprobs_dev, float* lse_dev,

@@ -803,6 +803,8 @@ gpd_status launch_distill(const DistillArgs& a, cudaStream_t st) {
     return launch_rows(distill_kernel<T>, a, a.T, C, row_threads(a.V / C), st);
 }
 
+// log2(e) / tau multiplies differences of logits, 0 among them, so it has to be a number.
+bool bad_temperature(float t) { return !(t > 0.f) || isinf(t) || isinf(kLog2e * (1.f / t)); }
 bool bad_rows(int64_t T, int64_t V) { return T < 0 || V <= 0 || V > 0x40000000; }
 
 }  // namespace
@@ -815,7 +817,7 @@ extern "C" gpd_status gpd_token_logprobs(gpd_dtype type, const void* logits_dev,
                                          const void* tokens_dev, int32_t G, float temperature, float* logprobs_dev,
                                          float* lse_dev, float* entropy_dev, int32_t K, int32_t* top_ids_dev,
                                          float* top_logprobs_dev, int64_t T, int64_t V, void* stream) {
-    if (!is_float_type(type) || !(temperature > 0.f) || isinf(temperature)) return GPD_ERR_ARG;
+    if (!is_float_type(type) || bad_temperature(temperature)) return GPD_ERR_ARG;
     if (bad_rows(T, V) || G < 0 || G > kMaxTokens || K < 0 || K > kMaxTop || K > V) return GPD_ERR_SHAPE;
     if (T == 0) return GPD_OK;                         // empty buffers may have no address
     if (!logits_dev || !lse_dev || (G > 0 && (!tokens_dev || !logprobs_dev || (index_bytes != 4 && index_bytes != 8))) ||
@@ -835,7 +837,7 @@ extern "C" gpd_status gpd_token_logprobs_backward(gpd_dtype type, const void* lo
                                                   const float* entropy_dev, const float* dlogprobs_dev,
                                                   const float* dentropy_dev, void* dlogits_dev, int64_t ldd, int64_t T,
                                                   int64_t V, void* stream) {
-    if (!is_float_type(type) || !(temperature > 0.f) || isinf(temperature)) return GPD_ERR_ARG;
+    if (!is_float_type(type) || bad_temperature(temperature)) return GPD_ERR_ARG;
     if (bad_rows(T, V) || G < 0 || G > kMaxTokens) return GPD_ERR_SHAPE;
     if (T == 0) return GPD_OK;
     if (!logits_dev || !lse_dev || !dlogits_dev || (dentropy_dev && !entropy_dev) ||
@@ -855,7 +857,7 @@ extern "C" gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, i
                                        const void* teacher_logits_dev, int64_t ldt, int32_t K, const float* weights_dev,
                                        float temperature, float* loss_dev, void* dlogits_dev, int64_t ldd, int64_t T,
                                        int64_t V, void* stream) {
-    if (!is_float_type(type) || !is_float_type(teacher_type) || !(temperature > 0.f) || isinf(temperature)) return GPD_ERR_ARG;
+    if (!is_float_type(type) || !is_float_type(teacher_type) || bad_temperature(temperature)) return GPD_ERR_ARG;
     if (bad_rows(T, V) || K < 0 || K > kMaxTeacher) return GPD_ERR_SHAPE;
     if (T == 0) return GPD_OK;
     if (!logits_dev || !loss_dev || (K > 0 && (!teacher_ids_dev || !teacher_logits_dev || (index_bytes != 4 && index_bytes != 8))))
