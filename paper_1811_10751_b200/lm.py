@@ -16,7 +16,18 @@ from .binding import EXPORTED, _check, lib
 try:
     from . import _lm                                   # compiled from csrc/lm_binding.cpp
 except ImportError as e:
-    raise ImportError(f"{e}: build it with `python paper_1811_10751_b200/build.py`. This package has no CPU fallback.") from e
+    class _NotBuilt:
+        """Stands for the compiled part where it cannot be loaded: the coded products do not need it, every operator of
+        this file fails with the reason."""
+
+        def __init__(self, why):
+            self._why = why
+
+        def __getattr__(self, name):
+            raise ImportError(f"{self._why}: build it with `python paper_1811_10751_b200/build.py`. "
+                              "This package has no CPU fallback.")
+
+    _lm = _NotBuilt(str(e))
 
 GPD_DT_F32, GPD_DT_BF16, GPD_DT_F16, GPD_DT_E4M3, GPD_DT_E5M2 = range(5)
 GPD_RMSNORM_MAX_PARTS = 512
