@@ -45,6 +45,20 @@ def _headers_mtime() -> float:
     return max(os.path.getmtime(h) for h in hs)
 
 
+def _binding_for() -> str:
+    """What _lm.so is compiled against: its binary interface is that of one torch and one Python."""
+    from importlib import metadata
+    return f"torch {metadata.version('torch')} {sys.implementation.cache_tag}"
+
+
+def _recorded(path: str) -> str:
+    try:
+        with open(path) as f:
+            return f.read()
+    except OSError:
+        return ""
+
+
 def _binding_cmd(out: str):
     """Command that compiles and links _lm.so; torch and CUDA runtime libraries are the ones torch has loaded."""
     import sysconfig
@@ -84,10 +98,13 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         run([nvcc, "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
         os.replace(tmp, LIB_PATH)
     newest = max(os.path.getmtime(BINDING_SRC), os.path.getmtime(os.path.join(INCLUDE, "gpd.h")))
-    if force or not os.path.exists(BINDING_PATH) or os.path.getmtime(BINDING_PATH) < newest:
+    built_for, record = _binding_for(), os.path.join(BUILD_DIR, "_lm.built_for")
+    if (force or not os.path.exists(BINDING_PATH) or os.path.getmtime(BINDING_PATH) < newest or _recorded(record) != built_for):
         tmp = BINDING_PATH + f".tmp{os.getpid()}"
         run(_binding_cmd(tmp))
         os.replace(tmp, BINDING_PATH)
+        with open(record, "w") as f:
+            f.write(built_for)
     return LIB_PATH
 
 
