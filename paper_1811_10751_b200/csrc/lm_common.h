@@ -266,10 +266,8 @@ template <int Q> struct Fp8;
 template <> struct Fp8<GPD_DT_E4M3> { static constexpr int kTopExp = 9; };
 template <> struct Fp8<GPD_DT_E5M2> { static constexpr int kTopExp = 16; };
 
-// Magnitudes are compared as bit patterns: NaN is then the largest and cannot be lost in a maximum.
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// Scale byte of a block whose largest magnitude has these bits.
+// Scale byte of a block whose largest magnitude has these bits.  Magnitudes are compared as bit patterns: NaN is then the
+// largest and cannot be lost in a maximum.
 template <int Q>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
     if (amax == 0u) return 127u;
@@ -291,16 +289,11 @@ __device__ __forceinline__ uint32_t cvt_fp8x4(float a, float b, float c, float d
             : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
     return r;
 }
-// Eight bytes at p, of which n exist; VEC: p is 8-byte aligned.
-template <bool VEC>
+// Eight bytes at p, anywhere, of which n exist
 __device__ __forceinline__ void store8_bytes(uint8_t* p, uint2 b, int n) {
-    if (VEC && n >= 8) {
-        *reinterpret_cast<uint2*>(p) = b;
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = (uint8_t)((i < 4 ? b.x >> (8 * i) : b.y >> (8 * (i - 4))) & 0xffu);
-    }
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = (uint8_t)((i < 4 ? b.x >> (8 * i) : b.y >> (8 * (i - 4))) & 0xffu);
 }
 
 // Bits of the largest magnitude of eight numbers, a NaN above all

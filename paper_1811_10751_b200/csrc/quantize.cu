@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
                 floats8(p, f);
                 const uint2 v = make_uint2(cvt_fp8x4<Q>(f[0], f[1], f[2], f[3]), cvt_fp8x4<Q>(f[4], f[5], f[6], f[7]));
                 if (a.q_vec && nc == 8) *reinterpret_cast<uint2*>(q + i * a.ldq) = v;
-                else store8_bytes<false>(q + i * a.ldq, v, nc);
+                else store8_bytes(q + i * a.ldq, v, nc);
             }
         }
     }
@@ -196,8 +196,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) cut_kernel(const 
             if (a.qT_vec && n >= 16) {
                 *reinterpret_cast<uint4*>(dst) = v;
             } else {
-                store8_bytes<false>(dst, make_uint2(v.x, v.y), n);
-                store8_bytes<false>(dst + 8, make_uint2(v.z, v.w), n - 8);
+                store8_bytes(dst, make_uint2(v.x, v.y), n);
+                store8_bytes(dst + 8, make_uint2(v.z, v.w), n - 8);
             }
         }
     }

@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(VPT > 0 ? 512 : 1024) rmsnorm_kernel(const Nor
             if (n > 0) {
                 const uint2 v = to_fp8x8<Q>(y[i], scale_inverse(packed_byte(b, i)));
                 if (VEC || (a.q_vec && n >= 8)) *reinterpret_cast<uint2*>(qout + c) = v;
-                else store8_bytes<false>(qout + c, v, n);
+                else store8_bytes(qout + c, v, n);
             }
         }
     };
