@@ -476,7 +476,9 @@ gpd_status gpd_quantize_blocks(gpd_dtype type, const void* src_dev, int64_t ld, 
  * gpd_gemm_fp8 - out (M x N) = A B^T (+ out if accumulate), both operands in 8 bits with block scales:
  *   out[i][j] = sum_k scaleA[i / a_block_rows][k / 128] A[i][k] * scaleB[j / b_block_rows][k / 128] B[j][k]
  * A: M x K, B: N x K, each e4m3 or e5m2; block_rows 1 (scales per row) or 128; out FP32, BF16 or FP16,
- * rounded once.  Products are exact, sums FP32.  Forward product of a layer: A = X, B = W; gradient of X:
+ * rounded once.  Products are exact, sums FP32.  A 16-bit result of K <= 65536 is summed with truncation, which takes up
+ * to 6e-5 of a sum of numbers of one sign (an eighth of FP16's rounding); longer ones and FP32 results are added to
+ * nearest, 1024 terms at a time (1e-7 for those).  Forward product of a layer: A = X, B = W; gradient of X:
  * A = Delta, B = W transposed; gradient of W: A = Delta transposed, B = X transposed (gpd_quantize_blocks
  * writes both forms).  A_dev and B_dev start on 16-byte boundaries, lda and ldb are multiples of 16
  * (GPD_ERR_ARG otherwise); scales may have any stride.  A bounded wait that expires shows in gpd_device_status.

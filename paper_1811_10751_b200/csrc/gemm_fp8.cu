@@ -21,11 +21,13 @@
 // Warp 1: one lane issues the products.  Warps 6..13 read the accumulators back, two sets of which alternate,
 // and store.
 //
-// Accumulation.  tcgen05.mma adds into its FP32 accumulator with truncation.  16-bit results take one chain
-// over the whole contraction: the bias (about 2^-25 of the sum per instruction, 8e-6 at K = 8192) is far
-// below their own rounding.  FP32 results cut the chain every eight k-blocks (32 instructions) and add the
-// pieces in registers, rounded to nearest: 4096 x 4096 x 4100 is then 1.0e-7 off the exact product, a plain FP32
-// product 1.0e-7.  (Pieces of four k-blocks: the reading of tensor memory holds the tensor cores up.)
+// Accumulation.  tcgen05.mma adds into its FP32 accumulator with truncation, which takes up to an ulp of the sum each
+// time: of sums of positive products 4e-6 at K = 8192, 2.4e-5 at 32768, 6e-5 at 65536, 2.8e-4 at 524288.  16-bit results
+// take one chain over the whole contraction up to K = 65536, where that is an eighth of FP16's rounding.  Longer ones, and
+// FP32 results of any length, cut the chain every eight k-blocks (32 instructions) and add the pieces in registers, rounded
+// to nearest: 4096 x 4096 x 4100 is then 1.0e-7 off the exact product, a plain FP32 product 1.0e-7; a 16-bit result at
+// K = 524288 3e-7 before its rounding, for 7 % of the time (2048 x 2048: 1644 -> 1766 us).  (Pieces of four k-blocks: the
+// reading of tensor memory holds the tensor cores up.)
 //
 // Few tiles (short A and B, long K): the CTAs of a cluster take a part of the contraction each; the parts
 // meet through distributed shared memory and are added in the order of the parts.
@@ -248,12 +250,12 @@ __device__ __forceinline__ void tile_origin(const Fp8Params& p, int tile, int bn
 
 // TRANS: D[i][j] is stored at out[j][i] (the caller swapped the operands); consecutive lanes hold consecutive i.
 // SPLIT: gridDim = (parts, tiles), the parts of a tile are a cluster.  PAIR: gridDim = (2, pairs).
-template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT>
+// CHUNKED: one chain of additions in tensor memory per chunk, the chunks added up in registers.
+template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT, bool CHUNKED>
 __global__ void __launch_bounds__(kThreads, SPLIT ? 2 : 1)
 gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                 const __grid_constant__ CUtensorMap tmD, const Fp8Params prm) {
     constexpr int STAGED = staged_elem(BN, TRANS, SPLIT, sizeof(T)), STAGES = stages(BN, PAIR, SPLIT, STAGED), STAGE = stage_bytes(BN, PAIR), SFB = sfb_blocks(BN);
-    constexpr bool CHUNKED = sizeof(T) == 4;           // FP32 results: one chain per chunk
     // columns of an epilogue warp, in units of 32: two warps share a lane quarter, of narrow tiles one does it all
     constexpr int W0 = BN >= 64 ? (BN / 32 + 1) / 2 * 32 : BN, W1 = BN - W0;
     constexpr int COLS = tmem_cols(BN);
@@ -472,7 +474,7 @@ gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const int c0 = half * W0, width = half ? W1 : W0;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         const uint32_t acc_empty0 = PAIR ? in_leader(&acc_empty[0]) : smem_u32(&acc_empty[0]);
-        float acc[CHUNKED ? W0 : 1];                   // FP32: W0 = W1 or W1 = 0
+        float acc[CHUNKED ? W0 : 1];                   // CHUNKED: W0 = W1 or W1 = 0
         uint8_t* staging = smem + STAGES * STAGE + (warp - 2 - kSfWarps) * 32 * 32 * STAGED;
         int ac = 0;
         bool ok = true;
@@ -672,14 +674,14 @@ struct Operand {
 };
 struct Config { int bn, splits; bool trans, pair; };
 
-template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT>
+template <int BN, typename T, bool TRANS, bool PAIR, bool SPLIT, bool CHUNKED>
 gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, int splits, cudaStream_t st) {
     constexpr int STAGED = staged_elem(BN, TRANS, SPLIT, sizeof(T));
     CUtensorMap tmA, tmB, tmD{};
     prm.copy_out = STAGED != 0 && prm.vec && !prm.accumulate;
     if (prm.copy_out && !make_out_map(&tmD, prm.out, a.rows, b.rows, prm.ldd, sizeof(T))) return GPD_ERR_CUDA;
     if (!make_map_2d(&tmA, a.q, a.rows, K, a.ld, BM) || !make_map_2d(&tmB, b.q, b.rows, K, b.ld, b_rows(BN, PAIR))) return GPD_ERR_CUDA;
-    auto kernel = gemm_fp8_kernel<BN, T, TRANS, PAIR, SPLIT>;
+    auto kernel = gemm_fp8_kernel<BN, T, TRANS, PAIR, SPLIT, CHUNKED>;
     constexpr int smem = smem_bytes(BN, PAIR, SPLIT, STAGED), rows = PAIR ? 2 * BM : BM;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
     prm.sa = a.s;
@@ -707,7 +709,7 @@ gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, 
 // 16 x 50000 x 512 in FP32 (9.1, 128 x 16 tiles 8.1).  Examples:
 // 7 x 4096 x 4096: 6.7 us in four parts, 8.2 in two; 128 x 8192 x 8192: 17.6 us as 256 x 128 pairs, 30.1 split;
 // 512 x 8192 x 8192: 23.5 us as 256 x 224 pairs, 28.9 as 128 x 224 tiles, 30.9 as 256 x 128 pairs.
-Config choose(int64_t M, int64_t N, int kb, bool f32) {
+Config choose(int64_t M, int64_t N, int kb, bool chunked) {
     static const int kWidths[] = {16, 32, 64, 128, 192, 224};
     Config best{128, 1, true, false};
     double best_t = 1e300;
@@ -715,7 +717,7 @@ Config choose(int64_t M, int64_t N, int kb, bool f32) {
     for (int t = 0; t < 2; ++t) {
         const int64_t rows = t ? N : M, cols = t ? M : N;
         for (int bn : kWidths) {
-            if (bn == 224 && f32) continue;            // FP32 results keep a tile's row in registers
+            if (bn == 224 && chunked) continue;        // a tile's row is kept in registers
             for (int pair = 0; pair <= (bn >= 128 ? 1 : 0); ++pair) {
                 const int height = pair ? 2 * BM : BM, slots = pair ? sms / 2 : sms;
                 const int64_t tiles = ((rows + height - 1) / height) * ((cols + bn - 1) / bn);
@@ -737,29 +739,38 @@ Config choose(int64_t M, int64_t N, int kb, bool f32) {
     return best;
 }
 
-template <typename T, bool TRANS>
+template <typename T, bool TRANS, bool CHUNKED>
 gpd_status launch_bn(const Operand& a, const Operand& b, const Fp8Params& prm, int64_t K, const Config& c, cudaStream_t st) {
     switch (c.pair ? -c.bn : c.bn) {
-        case 16: return c.splits > 1 ? launch<16, T, TRANS, false, true>(a, b, prm, K, c.splits, st) : launch<16, T, TRANS, false, false>(a, b, prm, K, 1, st);
-        case 32: return c.splits > 1 ? launch<32, T, TRANS, false, true>(a, b, prm, K, c.splits, st) : launch<32, T, TRANS, false, false>(a, b, prm, K, 1, st);
-        case 64: return c.splits > 1 ? launch<64, T, TRANS, false, true>(a, b, prm, K, c.splits, st) : launch<64, T, TRANS, false, false>(a, b, prm, K, 1, st);
-        case 128: return launch<128, T, TRANS, false, false>(a, b, prm, K, 1, st);
-        case 192: return launch<192, T, TRANS, false, false>(a, b, prm, K, 1, st);
-        case -128: return launch<128, T, TRANS, true, false>(a, b, prm, K, 1, st);
-        case -192: return launch<192, T, TRANS, true, false>(a, b, prm, K, 1, st);
+        case 16: return c.splits > 1 ? launch<16, T, TRANS, false, true, CHUNKED>(a, b, prm, K, c.splits, st) : launch<16, T, TRANS, false, false, CHUNKED>(a, b, prm, K, 1, st);
+        case 32: return c.splits > 1 ? launch<32, T, TRANS, false, true, CHUNKED>(a, b, prm, K, c.splits, st) : launch<32, T, TRANS, false, false, CHUNKED>(a, b, prm, K, 1, st);
+        case 64: return c.splits > 1 ? launch<64, T, TRANS, false, true, CHUNKED>(a, b, prm, K, c.splits, st) : launch<64, T, TRANS, false, false, CHUNKED>(a, b, prm, K, 1, st);
+        case 128: return launch<128, T, TRANS, false, false, CHUNKED>(a, b, prm, K, 1, st);
+        case 192: return launch<192, T, TRANS, false, false, CHUNKED>(a, b, prm, K, 1, st);
+        case -128: return launch<128, T, TRANS, true, false, CHUNKED>(a, b, prm, K, 1, st);
+        case -192: return launch<192, T, TRANS, true, false, CHUNKED>(a, b, prm, K, 1, st);
         default: break;
     }
-    if constexpr (sizeof(T) == 2) {
-        if (c.pair) return launch<224, T, TRANS, true, false>(a, b, prm, K, 1, st);
-        return launch<224, T, TRANS, false, false>(a, b, prm, K, 1, st);
+    if constexpr (!CHUNKED) {
+        if (c.pair) return launch<224, T, TRANS, true, false, false>(a, b, prm, K, 1, st);
+        return launch<224, T, TRANS, false, false, false>(a, b, prm, K, 1, st);
     }
     return GPD_ERR_UNSUPPORTED;
 }
-template <typename T>
-gpd_status launch_type(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, cudaStream_t st) {
-    const Config c = choose(a.rows, b.rows, prm.kb, sizeof(T) == 4);
+template <typename T, bool CHUNKED>
+gpd_status launch_chain(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, cudaStream_t st) {
+    const Config c = choose(a.rows, b.rows, prm.kb, CHUNKED);
     prm.vec = lm::rows_aligned(prm.out, prm.ldd, sizeof(T));
-    return c.trans ? launch_bn<T, true>(b, a, prm, K, c, st) : launch_bn<T, false>(a, b, prm, K, c, st);
+    return c.trans ? launch_bn<T, true, CHUNKED>(b, a, prm, K, c, st) : launch_bn<T, false, CHUNKED>(a, b, prm, K, c, st);
+}
+// K-blocks in one chain of 16-bit results at most (K = 65536)
+constexpr int kLongChain = 512;
+template <typename T>
+gpd_status launch_type(const Operand& a, const Operand& b, const Fp8Params& prm, int64_t K, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (prm.kb <= kLongChain) return launch_chain<T, false>(a, b, prm, K, st);
+    }
+    return launch_chain<T, true>(a, b, prm, K, st);
 }
 
 }  // namespace
