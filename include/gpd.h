@@ -433,7 +433,8 @@ gpd_status coded_layer_step(gpd_plan_t plan, int32_t phases, void* W_shares_dev,
  * 8-bit blocks: 128 neighbours along a row (the last block may be shorter) share the scale 2^e, stored
  * as the byte e + 127; e is the smallest integer >= -127 for which the block's largest magnitude is at
  * most 448 * 2^e (e4m3) or 57344 * 2^e (e5m2), elements are rounded to nearest even.  A block of zeros
- * has scale 1.  A block with a NaN or an infinity has the byte 255, which stands for NaN.
+ * has scale 1.  A block with a NaN or an infinity has the byte 255, which stands for NaN.  No other scales are taken:
+ * a matrix with scales that are not powers of two has to be cut again.
  */
 typedef enum { GPD_DT_F32 = 0, GPD_DT_BF16 = 1, GPD_DT_F16 = 2, GPD_DT_E4M3 = 3, GPD_DT_E5M2 = 4 } gpd_dtype;
 
@@ -481,7 +482,8 @@ gpd_status gpd_quantize_blocks(gpd_dtype type, const void* src_dev, int64_t ld, 
  * nearest, 1024 terms at a time (1e-7 for those).  Forward product of a layer: A = X, B = W; gradient of X:
  * A = Delta, B = W transposed; gradient of W: A = Delta transposed, B = X transposed (gpd_quantize_blocks
  * writes both forms).  A_dev and B_dev start on 16-byte boundaries, lda and ldb are multiples of 16
- * (GPD_ERR_ARG otherwise); scales may have any stride.  A bounded wait that expires shows in gpd_device_status.
+ * (GPD_ERR_ARG otherwise); scales and out may have any stride, but rows of out on 16-byte boundaries are stored much
+ * faster.  A bounded wait that expires shows in gpd_device_status.
  */
 gpd_status gpd_gemm_fp8(gpd_dtype a_type, const void* A_dev, int64_t lda, const uint8_t* a_scales_dev, int64_t ldsa,
                         int32_t a_block_rows, gpd_dtype b_type, const void* B_dev, int64_t ldb,

@@ -33,8 +33,10 @@
 // meet through distributed shared memory and are added in the order of the parts.
 //
 // Measured: 8192^3 to BF16 391 us in a burst (2810 TFLOP/s), 444 sustained, at 455 of 448 cycles a k-block and the power
-// limit; 4096 x 4096 x 4100 to FP32 89 us with rows 4112 bytes apart, 62 on 128-byte boundaries to BF16;
-// 7 x 4096 x 4096 6.5 us.
+// limit; 4096 x 4096 x 4100 with rows 4112 bytes apart 75 us to FP32, 69 to BF16, with rows on 128-byte boundaries 64 and
+// 54; 7 x 4096 x 4096 6.5 us.  Results that cannot leave through shared memory are stored from the registers of their row's
+// thread, 32 rows at a time, and that time shows: rows of the output off 16-byte boundaries (8192 x 8191 x 1024 to BF16
+// 623 us, on boundaries 61; x 8192 848 and 403), accumulation (4096^3 to FP32 131 us, plain 63; to BF16 82 and 53).
 //
 // Every mbarrier wait is bounded; on expiry the CTA raises a status word (gpd_device_status), drains its
 // copies, frees its tensor memory and returns.
@@ -705,7 +707,8 @@ gpd_status launch(const Operand& a, const Operand& b, Fp8Params prm, int64_t K, 
 // tensor cores 2 BN (four dependent instructions: 344 at least) and its copies a cycle per 64 bytes; a tile costs about
 // 1500 besides.  A part of a split contraction has half an SM's stages, whose latency shows (about 3300 over their
 // number), and 3000 for the meeting of the parts.  Measured over 19 shapes from 1 x 4096 x 4096 to 4096^3 with every
-// configuration, the choice is within 6 % of the best but for 64 x 8192 x 8192 (18.2 us, in four parts 15.5) and
+// configuration, outputs on 16-byte boundaries and no accumulation (the others' stores are not in the estimate), the
+// choice is within 6 % of the best but for 64 x 8192 x 8192 (18.2 us, in four parts 15.5) and
 // 16 x 50000 x 512 in FP32 (9.1, 128 x 16 tiles 8.1).  Examples:
 // 7 x 4096 x 4096: 6.7 us in four parts, 8.2 in two; 128 x 8192 x 8192: 17.6 us as 256 x 128 pairs, 30.1 split;
 // 512 x 8192 x 8192: 23.5 us as 256 x 224 pairs, 28.9 as 128 x 224 tiles, 30.9 as 256 x 128 pairs.
