@@ -537,6 +537,70 @@ gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, int64_t ld, 
                             float temperature, float* loss_dev, void* dlogits_dev, int64_t ldd, int64_t T, int64_t V,
                             void* stream);
 
+#define GPD_HEAD_MAX_DIM 256          /* columns of a head */
+#define GPD_HEAD_MAX_HEADS 65536
+#define GPD_HEAD_MAX_AXES 4           /* axes that positions have */
+#define GPD_HEAD_NORM_MAX_PARTS 512   /* gpd_head_norm_rope_backward: partial rows of each weight's gradient */
+
+/*
+ * gpd_head_norm_rope - norms of queries and keys for each head and their rotation by position, in one pass:
+ *   s = (mean_d x^2 + eps)^(-1/2),  z = x s weight,  y = z with its first `rotated` columns turned,  for every head x
+ * q: T rows of q_heads * head_dim columns, k: of k_heads * head_dim; both may be parts of one wider matrix (ldq, ldk), and
+ * either may have no heads.  Weights have head_dim elements of weight_type (`type` or GPD_DT_F32), shared by the heads of q
+ * and of k; both NULL: no norm, rotation alone.  FP32 inside, y is rounded once.  q_out may be q and k_out may be k, with the
+ * same stride.  head_dim is even and at most GPD_HEAD_MAX_DIM.
+ * Rotation: with half = rotated / 2, pair j is (z_j, z_(j + half)), or (z_2j, z_(2j + 1)) where neighbours != 0, and becomes
+ *   (a c - b s, b c + a s)  with  c = table[pos][j], s = table[pos][half + j]
+ * table: `positions` rows of at least `rotated` floats, ldt apart (angles belong in 64 bits before their cosines are taken);
+ * pos: T rows of n_axes positions (index_bytes 4 or 8), ldp apart; axes: half bytes, which of them pair j turns by (not read
+ * if n_axes = 1).  A position outside the table, or an axis that there is none of, makes the pairs that it turns NaN.
+ * rotated = 0: no rotation; table, pos and axes are not looked at.  Rows on 16-byte boundaries and columns in multiples of 32
+ * bytes are much faster.
+ */
+gpd_status gpd_head_norm_rope(gpd_dtype type, const void* q_dev, int64_t ldq, int32_t q_heads, const void* k_dev, int64_t ldk,
+                              int32_t k_heads, int32_t head_dim, gpd_dtype weight_type, const void* q_weight_dev,
+                              const void* k_weight_dev, float eps, const float* table_dev, int64_t ldt, int64_t positions,
+                              int32_t rotated, int32_t neighbours, int32_t index_bytes, const void* pos_dev, int64_t ldp,
+                              int32_t n_axes, const uint8_t* axes_dev, void* q_out_dev, int64_t ldqo, void* k_out_dev,
+                              int64_t ldko, int64_t T, void* stream);
+/*
+ * gpd_head_norm_rope_backward - gradient of it: with g = dy turned back,
+ *   dx = s (g weight - x s^2 mean_d(g weight x)),   dweight_d = sum over tokens and heads of g x s   (floats, fixed order)
+ * q and k: the inputs of the forward call (not looked at without norm).  dq_in may be dq or q, dk_in dk or k, with the
+ * same stride.  dq_weight and dk_weight: head_dim floats each, needed with norm where there are heads.
+ * workspace_dev: 2 * GPD_HEAD_NORM_MAX_PARTS * head_dim floats, needed with norm.
+ */
+gpd_status gpd_head_norm_rope_backward(gpd_dtype type, const void* dq_dev, int64_t lddq, const void* dk_dev, int64_t lddk,
+                                       const void* q_dev, int64_t ldq, int32_t q_heads, const void* k_dev, int64_t ldk,
+                                       int32_t k_heads, int32_t head_dim, gpd_dtype weight_type, const void* q_weight_dev,
+                                       const void* k_weight_dev, float eps, const float* table_dev, int64_t ldt,
+                                       int64_t positions, int32_t rotated, int32_t neighbours, int32_t index_bytes,
+                                       const void* pos_dev, int64_t ldp, int32_t n_axes, const uint8_t* axes_dev,
+                                       void* dq_in_dev, int64_t lddqi, void* dk_in_dev, int64_t lddki, float* dq_weight_dev,
+                                       float* dk_weight_dev, int64_t T, void* workspace_dev, int64_t workspace_bytes,
+                                       void* stream);
+
+#define GPD_GRAD_NORM_WORKSPACE 16384 /* bytes */
+
+/*
+ * gpd_grad_norm - norm over n tensors together: (sum over all elements of all of them of g^2)^(1/2), one float.
+ * types, grads and counts are arrays in HOST memory, read during the call: a gpd_dtype (FP32, BF16 or FP16), the device
+ * address and the number of elements of every tensor (each contiguous; addresses on a boundary of the element's size).
+ * FP64 where FP32 would lose or overflow; sums are taken in a fixed order.  No tensors: 0.  A NaN or an infinity shows in
+ * the norm.  workspace_dev: GPD_GRAD_NORM_WORKSPACE bytes on an 8-byte boundary.  Ranks that hold parts of the gradients combine their norms
+ * (root of the sum of squares) between this call and the next.
+ */
+gpd_status gpd_grad_norm(int32_t n, const int32_t* types_host, const void* const* grads_host, const int64_t* counts_host,
+                         float* norm_dev, void* workspace_dev, int64_t workspace_bytes, void* stream);
+/*
+ * gpd_clip_grads - out = grad * min(1, max_norm / norm) for every one of n tensors, FP32 inside and rounded once.
+ * norm_dev: one float, as gpd_grad_norm leaves it; max_norm > 0.  out[i] may be grads[i] (of the same type; if all are,
+ * nothing is moved where the norm is within the bound); otherwise an output must not overlap any other tensor of the call
+ * (GPD_ERR_ARG).  An infinite norm gives 0 (NaN where the gradient is infinite), a norm that is NaN gives NaN.
+ */
+gpd_status gpd_clip_grads(int32_t n, const int32_t* types_host, const void* const* grads_host, const int32_t* out_types_host,
+                          void* const* out_host, const int64_t* counts_host, const float* norm_dev, float max_norm, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,588 @@
+// Norms of queries and keys for each head with the rotation by position in the same pass, and their gradient.
+//
+//   s = (mean_d x^2 + eps)^(-1/2),   z = x s w,   y = R z          (FP32 throughout, y rounded once)
+//   (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of the first R columns, the others stay
+//   g = R^T dy,   dw_d = sum g x s,   dx = s (g w - x s^2 mean_d(g w x))
+//
+// Every element is read once and written once, with a handful of operations: HBM bounds both directions.  A head of D
+// columns is cut into units of V pairs: the two vectors of V elements that hold them, so that a pair's halves are in one
+// thread's registers in either pairing and loads are 16 bytes (or 8) per lane.  G lanes hold a head, 32 / G heads are in a
+// warp; the norm is a butterfly over the G lanes, no shared memory and no barrier.  A warp stays with one token, whose
+// angles it loads once, for up to U steps of 32 / G heads, all of whose loads are issued before the first use.
+#include <algorithm>
+
+#include "lm_common.h"
+
+namespace gpd {
+
+namespace {
+
+using namespace lm;
+
+constexpr int kWarps = 4;                              // of a CTA
+constexpr int kMaxHead = GPD_HEAD_MAX_DIM;
+
+// Queries or keys
+struct Part {
+    const void* x; int64_t ldx;
+    const void* dy; int64_t lddy;                      // gradient only
+    void* out; int64_t ldo;
+    const void* w;                                     // null: no norm
+    int heads, chunks;                                 // a token's work: chunks of U * 32 / G heads
+};
+struct HeadArgs {
+    Part part[2];
+    unsigned split;                                    // CTAs of the first part
+    const float* table; int64_t ldt, P;
+    const void* pos; int64_t ldp;
+    const uint8_t* axes;
+    float* parts;                                      // gradient: [gridDim.x][D]
+    int64_t T;
+    int D, R, A, lanes;                                // lanes: G
+    float eps;
+    bool wide_pos, w_f32, neighbours, inverse, table_vec;
+};
+
+template <typename T, int V> struct Vec;               // V neighbouring elements
+template <> struct Vec<float, 4> { uint4 r; };
+template <> struct Vec<__nv_bfloat16, 8> { uint4 r; };
+template <> struct Vec<__half, 8> { uint4 r; };
+template <> struct Vec<__nv_bfloat16, 4> { uint2 r; };
+template <> struct Vec<__half, 4> { uint2 r; };
+template <typename T> struct Vec<T, 1> { T r; };
+
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> load_vec(const T* p) { return *reinterpret_cast<const Vec<T, V>*>(p); }
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Vec<T, V>& v, float (&f)[V]) {
+    if constexpr (V == 1) {
+        f[0] = to_f32(v.r);
+    } else if constexpr (sizeof(T) == 4) {
+        f[0] = __uint_as_float(v.r.x); f[1] = __uint_as_float(v.r.y); f[2] = __uint_as_float(v.r.z); f[3] = __uint_as_float(v.r.w);
+    } else {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(&v.r);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 x = unpack2(w[i], T());
+            f[2 * i] = x.x;
+            f[2 * i + 1] = x.y;
+        }
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[V]) {
+    Vec<T, V> v;
+    if constexpr (V == 1) {
+        v.r = from_f32<T>(f[0]);
+    } else if constexpr (sizeof(T) == 4) {
+        v.r = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    } else {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v.r);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) w[i] = pack2(f[2 * i], f[2 * i + 1], T());
+    }
+    *reinterpret_cast<Vec<T, V>*>(p) = v;
+}
+
+// Unit u of a head: columns c1 .. c1 + V - 1 and c2 .. c2 + V - 1; turned or not.
+template <int V>
+struct Unit {
+    int c1, c2;
+    bool there, turned;
+    __device__ __forceinline__ Unit(int u, const HeadArgs& a) {
+        const int nr = a.R / (2 * V);
+        there = u < a.D / (2 * V);
+        turned = u < nr;
+        if (a.neighbours) {
+            c1 = 2 * V * u;
+            c2 = c1 + V;
+        } else {
+            const int i = turned ? u : u - nr, from = turned ? 0 : a.R;
+            c1 = from + V * i;
+            c2 = c1 + (turned ? a.R : a.D - a.R) / 2;
+        }
+    }
+};
+// The two vectors of a unit as first and second halves of its pairs, and back.
+template <int V>
+__device__ __forceinline__ void to_pairs(const float (&x)[V], const float (&y)[V], bool neighbours, float (&a)[V], float (&b)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (V == 1) {
+            a[i] = x[i];
+            b[i] = y[i];
+        } else {
+            const float ea = 2 * i < V ? x[2 * i % V] : y[2 * i % V], eb = 2 * i < V ? x[(2 * i + 1) % V] : y[(2 * i + 1) % V];
+            a[i] = neighbours ? ea : x[i];
+            b[i] = neighbours ? eb : y[i];
+        }
+    }
+}
+template <int V>
+__device__ __forceinline__ void from_pairs(const float (&a)[V], const float (&b)[V], bool neighbours, float (&x)[V], float (&y)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (V == 1) {
+            x[i] = a[i];
+            y[i] = b[i];
+        } else {
+            const int lo = i / 2, hi = V / 2 + i / 2;
+            x[i] = neighbours ? (i & 1 ? b[lo] : a[lo]) : a[i];
+            y[i] = neighbours ? (i & 1 ? b[hi] : a[hi]) : b[i];
+        }
+    }
+}
+
+// V floats at p; vec: on a 16-byte boundary
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, bool vec, float (&f)[V]) {
+    if (V % 4 == 0 && vec) {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const float4 v = __ldg(reinterpret_cast<const float4*>(p) + i);
+            f[4 * i] = v.x; f[4 * i + 1 < V ? 4 * i + 1 : 0] = v.y; f[4 * i + 2 < V ? 4 * i + 2 : 0] = v.z; f[4 * i + 3 < V ? 4 * i + 3 : 0] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = __ldg(p + i);
+    }
+}
+
+// Cosines and sines of unit u for token t.  Several axes: the rows of all of them are loaded, and every pair takes its
+// axis's; positions outside the table, and axes that there are none of, give NaN.
+template <int V>
+__device__ __forceinline__ void angles(const HeadArgs& a, int64_t t, int u, float (&cs)[V], float (&sn)[V]) {
+    unsigned long long axis = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        cs[i] = sn[i] = __int_as_float(0x7fffffff);
+        if (a.axes) axis |= (unsigned long long)__ldg(a.axes + V * u + i) << (8 * i);
+    }
+    for (int x = 0; x < a.A; ++x) {
+        const int64_t i = t * a.ldp + x;
+        const int64_t at = a.wide_pos ? static_cast<const int64_t*>(a.pos)[i] : static_cast<const int32_t*>(a.pos)[i];
+        if (at < 0 || at >= a.P) continue;
+        const float* row = a.table + at * a.ldt + V * u;
+        float c[V], s[V];
+        load_floats<V>(row, a.table_vec, c);
+        load_floats<V>(row + a.R / 2, a.table_vec, s);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const bool mine = !a.axes || (int)(axis >> (8 * j) & 0xff) == x;
+            cs[j] = mine ? c[j] : cs[j];
+            sn[j] = mine ? (a.inverse ? -s[j] : s[j]) : sn[j];
+        }
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void weights(const HeadArgs& a, const void* w, const Unit<V>& u, float (&wa)[V], float (&wb)[V]) {
+    float x[V], y[V];
+    if (a.w_f32) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            x[i] = static_cast<const float*>(w)[u.c1 + i];
+            y[i] = static_cast<const float*>(w)[u.c2 + i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            x[i] = to_f32(static_cast<const T*>(w)[u.c1 + i]);
+            y[i] = to_f32(static_cast<const T*>(w)[u.c2 + i]);
+        }
+    }
+    to_pairs<V>(x, y, a.neighbours, wa, wb);
+}
+// Sum over the G lanes of a head
+__device__ __forceinline__ float lanes_sum(float v, int G) {
+    for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// N units per lane (N > 1 only with V = 1: rows that no vector fits)
+template <typename T, int V, int N, int U>
+__global__ void __launch_bounds__(32 * kWarps) heads_kernel(const __grid_constant__ HeadArgs a) {
+    after_previous();
+    const bool second = blockIdx.x >= a.split;
+    const Part& p = a.part[second];
+    const int64_t work = (int64_t)(blockIdx.x - (second ? a.split : 0)) * kWarps + (threadIdx.x >> 5);
+    const int64_t t = work / p.chunks;
+    if (t >= a.T) return;                              // whole warps
+    const int lane = threadIdx.x & 31, G = a.lanes, per = 32 / G;
+    const int h0 = (int)(work - t * p.chunks) * per * U + lane / G;
+    const T* x = static_cast<const T*>(p.x) + t * p.ldx;
+    T* y = static_cast<T*>(p.out) + t * p.ldo;
+
+    Vec<T, V> r1[U][N], r2[U][N];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const Unit<V> u(lane % G + n * G, a);
+            const int h = h0 + i * per;
+            r1[i][n] = r2[i][n] = Vec<T, V>{};
+            if (u.there && h < p.heads) {
+                r1[i][n] = load_vec<T, V>(x + (int64_t)h * a.D + u.c1);
+                r2[i][n] = load_vec<T, V>(x + (int64_t)h * a.D + u.c2);
+            }
+        }
+    float cs[N][V], sn[N][V], wa[N][V], wb[N][V];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Unit<V> u(lane % G + n * G, a);
+        if (u.there && u.turned) angles<V>(a, t, lane % G + n * G, cs[n], sn[n]);
+        if (u.there && p.w) weights<T, V>(a, p.w, u, wa[n], wb[n]);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int h = h0 + i * per;
+        float fa[N][V], fb[N][V];
+        float sum = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float f[V], g[V];
+            unpack<T, V>(r1[i][n], f);
+            unpack<T, V>(r2[i][n], g);
+            to_pairs<V>(f, g, a.neighbours, fa[n], fb[n]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum = fmaf(fa[n][j], fa[n][j], fmaf(fb[n][j], fb[n][j], sum));
+        }
+        const float s = p.w ? rsqrtf(lanes_sum(sum, G) / (float)a.D + a.eps) : 1.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const Unit<V> u(lane % G + n * G, a);
+            if (!u.there || h >= p.heads) continue;
+            if (p.w) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    fa[n][j] = fa[n][j] * s * wa[n][j];
+                    fb[n][j] = fb[n][j] * s * wb[n][j];
+                }
+            }
+            if (u.turned) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float c = fa[n][j], d = fb[n][j];
+                    fa[n][j] = c * cs[n][j] - d * sn[n][j];
+                    fb[n][j] = d * cs[n][j] + c * sn[n][j];
+                }
+            }
+            float f[V], g[V];
+            from_pairs<V>(fa[n], fb[n], a.neighbours, f, g);
+            store_vec<T, V>(y + (int64_t)h * a.D + u.c1, f);
+            store_vec<T, V>(y + (int64_t)h * a.D + u.c2, g);
+        }
+    }
+}
+
+// Gradient with norm: warps walk over the tokens and add up their lanes' share of dw in registers.
+template <typename T, int V, int N, int U>
+__global__ void __launch_bounds__(32 * kWarps) heads_backward_kernel(const __grid_constant__ HeadArgs a) {
+    __shared__ float shares[kWarps][kMaxHead];
+    after_previous();
+    const bool second = blockIdx.x >= a.split;
+    const Part& p = a.part[second];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.lanes, per = 32 / G;
+    const int64_t ctas = second ? gridDim.x - a.split : a.split, all = a.T * p.chunks;
+    float wa[N][V], wb[N][V], da[N][V], db[N][V];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Unit<V> u(lane % G + n * G, a);
+#pragma unroll
+        for (int j = 0; j < V; ++j) wa[n][j] = wb[n][j] = da[n][j] = db[n][j] = 0.f;
+        if (u.there) weights<T, V>(a, p.w, u, wa[n], wb[n]);
+    }
+    for (int64_t work = (int64_t)(blockIdx.x - (second ? a.split : 0)) * kWarps + warp; work < all; work += ctas * kWarps) {
+        const int64_t t = work / p.chunks;
+        const int h0 = (int)(work - t * p.chunks) * per * U + lane / G;
+        const T* x = static_cast<const T*>(p.x) + t * p.ldx;
+        const T* dy = static_cast<const T*>(p.dy) + t * p.lddy;
+        T* dx = static_cast<T*>(p.out) + t * p.ldo;
+        Vec<T, V> x1[U][N], x2[U][N], y1[U][N], y2[U][N];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const Unit<V> u(lane % G + n * G, a);
+                const int h = h0 + i * per;
+                x1[i][n] = x2[i][n] = y1[i][n] = y2[i][n] = Vec<T, V>{};
+                if (u.there && h < p.heads) {
+                    const int64_t at = (int64_t)h * a.D;
+                    x1[i][n] = load_vec<T, V>(x + at + u.c1);
+                    x2[i][n] = load_vec<T, V>(x + at + u.c2);
+                    y1[i][n] = load_vec<T, V>(dy + at + u.c1);
+                    y2[i][n] = load_vec<T, V>(dy + at + u.c2);
+                }
+            }
+        float cs[N][V], sn[N][V];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const Unit<V> u(lane % G + n * G, a);
+            if (u.there && u.turned) angles<V>(a, t, lane % G + n * G, cs[n], sn[n]);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int h = h0 + i * per;
+            float xa[N][V], xb[N][V], ga[N][V], gb[N][V];
+            float squares = 0.f, dot = 0.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const Unit<V> u(lane % G + n * G, a);
+                float f[V], g[V];
+                unpack<T, V>(x1[i][n], f);
+                unpack<T, V>(x2[i][n], g);
+                to_pairs<V>(f, g, a.neighbours, xa[n], xb[n]);
+                unpack<T, V>(y1[i][n], f);
+                unpack<T, V>(y2[i][n], g);
+                to_pairs<V>(f, g, a.neighbours, ga[n], gb[n]);
+                // heads and units that do not exist are zeros and stay so
+                if (u.there && u.turned && h < p.heads) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {      // a.inverse: the sines are negated
+                        const float c = ga[n][j], d = gb[n][j];
+                        ga[n][j] = c * cs[n][j] - d * sn[n][j];
+                        gb[n][j] = d * cs[n][j] + c * sn[n][j];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    squares = fmaf(xa[n][j], xa[n][j], fmaf(xb[n][j], xb[n][j], squares));
+                    dot = fmaf(ga[n][j] * wa[n][j], xa[n][j], fmaf(gb[n][j] * wb[n][j], xb[n][j], dot));
+                }
+            }
+            const float s = rsqrtf(lanes_sum(squares, G) / (float)a.D + a.eps);
+            const float k = s * s * (lanes_sum(dot, G) / (float)a.D);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const Unit<V> u(lane % G + n * G, a);
+                if (!u.there || h >= p.heads) continue;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    da[n][j] = fmaf(ga[n][j] * s, xa[n][j], da[n][j]);
+                    db[n][j] = fmaf(gb[n][j] * s, xb[n][j], db[n][j]);
+                    ga[n][j] = s * fmaf(xa[n][j], -k, ga[n][j] * wa[n][j]);
+                    gb[n][j] = s * fmaf(xb[n][j], -k, gb[n][j] * wb[n][j]);
+                }
+                float f[V], g[V];
+                from_pairs<V>(ga[n], gb[n], a.neighbours, f, g);
+                store_vec<T, V>(dx + (int64_t)h * a.D + u.c1, f);
+                store_vec<T, V>(dx + (int64_t)h * a.D + u.c2, g);
+            }
+        }
+    }
+    // the warp's heads, then the CTA's warps, in a fixed order
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const Unit<V> u(lane % G + n * G, a);
+        for (int o = G; o < 32; o <<= 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                da[n][j] += __shfl_xor_sync(0xffffffffu, da[n][j], o);
+                db[n][j] += __shfl_xor_sync(0xffffffffu, db[n][j], o);
+            }
+        }
+        if (u.there && lane < G) {
+            float f[V], g[V];
+            from_pairs<V>(da[n], db[n], a.neighbours, f, g);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                shares[warp][u.c1 + j] = f[j];
+                shares[warp][u.c2 + j] = g[j];
+            }
+        }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.D; c += 32 * kWarps) {
+        float v = shares[0][c];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) v += shares[w][c];
+        a.parts[(int64_t)blockIdx.x * a.D + c] = v;
+    }
+}
+
+// Both weights' gradients: sums over their CTAs' rows in a fixed order, 32 threads per column, then theirs.
+__global__ void __launch_bounds__(1024) heads_dweight_kernel(const float* parts, int split, int n, int D, float* dqw, float* dkw) {
+    __shared__ float s[32][33];
+    after_previous();
+    const int c = blockIdx.x * 32 + threadIdx.x, from = blockIdx.y ? split : 0, to = blockIdx.y ? n : split;
+    float* dw = blockIdx.y ? dkw : dqw;
+    float v = 0.f;
+    if (c < D)
+        for (int p = from + threadIdx.y; p < to; p += 32) v += parts[(int64_t)p * D + c];
+    s[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.y == 0 && c < D && dw) {
+        for (int i = 1; i < 32; ++i) v += s[i][threadIdx.x];
+        dw[c] = v;
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------
+// Largest vector that the layout allows: whole units (turned and not), and every row on a boundary of it.
+int vector_width(const HeadArgs& a, int elem) {
+    for (int V = 16 / elem; V >= 4; V /= 2) {
+        bool ok = a.D % (2 * V) == 0 && a.R % (2 * V) == 0;
+        for (const Part& p : a.part)
+            if (p.heads > 0)
+                ok = ok && rows_aligned(p.x, p.ldx, elem, V * elem) && rows_aligned(p.dy, p.lddy, elem, V * elem) &&
+                     rows_aligned(p.out, p.ldo, elem, V * elem);
+        if (ok) return V;
+    }
+    return 1;
+}
+int pow2_lanes(int units) {
+    int g = 1;
+    while (g < units && g < 32) g *= 2;
+    return g;
+}
+
+template <typename T, int V, int U>
+gpd_status launch_forward(HeadArgs a, cudaStream_t st) {
+    constexpr int N = V == 1 ? kMaxHead / 64 : 1;
+    int64_t ctas = 0;
+    for (int i = 0; i < 2; ++i) {
+        Part& p = a.part[i];
+        const int step = 32 / a.lanes * U;
+        p.chunks = std::max(1, (p.heads + step - 1) / step);
+        const int64_t n = p.heads > 0 ? (a.T * p.chunks + kWarps - 1) / kWarps : 0;
+        if (i == 0) a.split = (unsigned)n;
+        ctas += n;
+    }
+    if (ctas > 0x7fffffff) return GPD_ERR_SHAPE;
+    return launch_after(heads_kernel<T, V, N, U>, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, a);
+}
+template <typename T, int V>
+gpd_status launch_forward_steps(HeadArgs a, cudaStream_t st) {
+    a.lanes = pow2_lanes(a.D / (2 * V));
+    if (V == 1) return launch_forward<T, V, 1>(a, st);
+    // Few tokens: one step per warp, so that the heads are spread over the SMs.
+    const int64_t steps = a.T * ((a.part[0].heads + a.part[1].heads) / (32 / a.lanes) + 1);
+    return steps < 8 * (int64_t)sm_count() * kWarps ? launch_forward<T, V, 1>(a, st) : launch_forward<T, V, 4>(a, st);
+}
+template <typename T>
+gpd_status launch_heads(const HeadArgs& a, cudaStream_t st) {
+    switch (vector_width(a, sizeof(T))) {
+        case sizeof(T) == 2 ? 8 : -1: return launch_forward_steps<T, 16 / sizeof(T)>(a, st);
+        case 4: return launch_forward_steps<T, 4>(a, st);
+        default: return launch_forward_steps<T, 1>(a, st);
+    }
+}
+
+template <typename T, int V>
+gpd_status launch_backward(HeadArgs a, float* dqw, float* dkw, cudaStream_t st) {
+    constexpr int N = V == 1 ? kMaxHead / 64 : 1, U = V == 1 ? 1 : 2;
+    a.lanes = pow2_lanes(a.D / (2 * V));
+    const int step = 32 / a.lanes * U;
+    int64_t work[2];
+    for (int i = 0; i < 2; ++i) {
+        a.part[i].chunks = std::max(1, (a.part[i].heads + step - 1) / step);
+        work[i] = a.part[i].heads > 0 ? (a.T * a.part[i].chunks + kWarps - 1) / kWarps : 0;
+    }
+    // four CTAs per SM, shared out by the amount of work
+    const int64_t most = std::min<int64_t>(4 * sm_count(), 2 * GPD_HEAD_NORM_MAX_PARTS), sum = work[0] + work[1];
+    int64_t n[2];
+    for (int i = 0; i < 2; ++i)
+        n[i] = work[i] == 0 ? 0 : std::max<int64_t>(1, std::min({work[i], most * work[i] / sum, (int64_t)GPD_HEAD_NORM_MAX_PARTS}));
+    a.split = (unsigned)n[0];
+    const int split = (int)n[0], total = (int)(n[0] + n[1]);
+    if (total > 0) {
+        const gpd_status rc = launch_after(heads_backward_kernel<T, V, N, U>, dim3((unsigned)total), dim3(32 * kWarps), 0, 1, st, a);
+        if (rc != GPD_OK) return rc;
+    }
+    const float* parts = a.parts;
+    return launch_after(heads_dweight_kernel, dim3((unsigned)((a.D + 31) / 32), 2), dim3(32, 32), 0, 1, st, parts, split, total, a.D, dqw, dkw);
+}
+template <typename T>
+gpd_status launch_heads_backward(const HeadArgs& a, float* dqw, float* dkw, cudaStream_t st) {
+    switch (vector_width(a, sizeof(T))) {
+        case sizeof(T) == 2 ? 8 : -1: return launch_backward<T, 16 / sizeof(T)>(a, dqw, dkw, st);
+        case 4: return launch_backward<T, 4>(a, dqw, dkw, st);
+        default: return launch_backward<T, 1>(a, dqw, dkw, st);
+    }
+}
+
+// What both directions check.  GPD_OK with a.T = 0: nothing to do.
+gpd_status check_heads(int type, int weight_type, const HeadArgs& a, int index_bytes, bool norm) {
+    if (!is_float_type(type) || (norm && weight_type != type && weight_type != GPD_DT_F32)) return GPD_ERR_ARG;
+    if (a.T < 0 || a.T > 0x7fffffff || a.D <= 0 || a.D % 2 || a.D > kMaxHead || a.R < 0 || a.R % 2 || a.R > a.D) return GPD_ERR_SHAPE;
+    if (!norm && a.R == 0) return GPD_ERR_ARG;
+    const Part *q = &a.part[0], *k = &a.part[1];
+    if (q->heads < 0 || k->heads < 0 || q->heads > GPD_HEAD_MAX_HEADS || k->heads > GPD_HEAD_MAX_HEADS) return GPD_ERR_SHAPE;
+    if (a.R > 0) {
+        if (a.A < 1 || a.A > GPD_HEAD_MAX_AXES || a.P < 0 || (a.P > 1 && a.ldt < a.R) || (a.T > 1 && a.ldp < a.A)) return GPD_ERR_SHAPE;
+        if ((index_bytes != 4 && index_bytes != 8) || (a.A > 1 && !a.axes)) return GPD_ERR_ARG;
+        if ((a.P > 0 && !a.table) || (a.T > 0 && !a.pos)) return GPD_ERR_ARG;
+    }
+    for (const Part& p : a.part) {
+        if (p.heads == 0 || a.T == 0) continue;
+        const int64_t row = (int64_t)p.heads * a.D;
+        if (p.ldx < row || p.ldo < row) return GPD_ERR_SHAPE;
+        if (!p.out) return GPD_ERR_ARG;
+    }
+    return GPD_OK;
+}
+
+}  // namespace
+
+}  // namespace gpd
+
+using namespace gpd;
+
+extern "C" gpd_status gpd_head_norm_rope(gpd_dtype type, const void* q_dev, int64_t ldq, int32_t q_heads, const void* k_dev,
+                                         int64_t ldk, int32_t k_heads, int32_t head_dim, gpd_dtype weight_type,
+                                         const void* q_weight_dev, const void* k_weight_dev, float eps,
+                                         const float* table_dev, int64_t ldt, int64_t positions, int32_t rotated,
+                                         int32_t neighbours, int32_t index_bytes, const void* pos_dev, int64_t ldp,
+                                         int32_t n_axes, const uint8_t* axes_dev, void* q_out_dev, int64_t ldqo, void* k_out_dev,
+                                         int64_t ldko, int64_t T, void* stream) {
+    HeadArgs a{{{q_dev, ldq, nullptr, 0, q_out_dev, ldqo, q_weight_dev, q_heads, 0}, {k_dev, ldk, nullptr, 0, k_out_dev, ldko, k_weight_dev, k_heads, 0}},
+               0, table_dev, ldt, positions, pos_dev, ldp, n_axes > 1 ? axes_dev : nullptr, nullptr, T, head_dim, rotated, n_axes, 0, eps,
+               index_bytes == 8, weight_type == GPD_DT_F32, neighbours != 0, false, lm::rows_aligned(table_dev, ldt, 4)};
+    const bool norm = q_weight_dev || k_weight_dev;
+    const gpd_status rc = check_heads(type, weight_type, a, index_bytes, norm);
+    if (rc != GPD_OK) return rc;
+    if (T == 0 || q_heads + k_heads == 0) return GPD_OK;   // empty buffers may have no address
+    for (const Part& p : a.part)
+        if (p.heads > 0 && (!p.x || (norm && !p.w))) return GPD_ERR_ARG;
+    cudaStream_t st = as_stream(stream);
+    if (type == GPD_DT_F32) return launch_heads<float>(a, st);
+    return type == GPD_DT_BF16 ? launch_heads<__nv_bfloat16>(a, st) : launch_heads<__half>(a, st);
+}
+
+extern "C" gpd_status gpd_head_norm_rope_backward(gpd_dtype type, const void* dq_dev, int64_t lddq, const void* dk_dev, int64_t lddk,
+                                                  const void* q_dev, int64_t ldq, int32_t q_heads, const void* k_dev, int64_t ldk,
+                                                  int32_t k_heads, int32_t head_dim, gpd_dtype weight_type,
+                                                  const void* q_weight_dev, const void* k_weight_dev, float eps,
+                                                  const float* table_dev, int64_t ldt, int64_t positions, int32_t rotated,
+                                                  int32_t neighbours, int32_t index_bytes, const void* pos_dev, int64_t ldp,
+                                                  int32_t n_axes, const uint8_t* axes_dev, void* dq_in_dev, int64_t lddqi,
+                                                  void* dk_in_dev, int64_t lddki, float* dq_weight_dev, float* dk_weight_dev,
+                                                  int64_t T, void* workspace_dev, int64_t workspace_bytes, void* stream) {
+    const bool norm = q_weight_dev || k_weight_dev;
+    // without norm the gradient is the forward pass of dy with the angles negated
+    const void *xq = norm ? q_dev : dq_dev, *xk = norm ? k_dev : dk_dev;
+    HeadArgs a{{{xq, norm ? ldq : lddq, norm ? dq_dev : nullptr, lddq, dq_in_dev, lddqi, q_weight_dev, q_heads, 0},
+                {xk, norm ? ldk : lddk, norm ? dk_dev : nullptr, lddk, dk_in_dev, lddki, k_weight_dev, k_heads, 0}},
+               0, table_dev, ldt, positions, pos_dev, ldp, n_axes > 1 ? axes_dev : nullptr, static_cast<float*>(workspace_dev), T, head_dim,
+               rotated, n_axes, 0, eps, index_bytes == 8, weight_type == GPD_DT_F32, neighbours != 0, true,
+               lm::rows_aligned(table_dev, ldt, 4)};
+    const gpd_status rc = check_heads(type, weight_type, a, index_bytes, norm);
+    if (rc != GPD_OK) return rc;
+    cudaStream_t st = as_stream(stream);
+    if (!norm) {
+        if (T == 0 || q_heads + k_heads == 0) return GPD_OK;
+        for (const Part& p : a.part)
+            if (p.heads > 0 && !p.x) return GPD_ERR_ARG;
+        if (type == GPD_DT_F32) return launch_heads<float>(a, st);
+        return type == GPD_DT_BF16 ? launch_heads<__nv_bfloat16>(a, st) : launch_heads<__half>(a, st);
+    }
+    if (T > 0) {
+        for (const Part& p : a.part)
+            if (p.heads > 0 && (!p.x || !p.dy || !p.w || p.lddy < (int64_t)p.heads * head_dim)) return p.x && p.dy && p.w ? GPD_ERR_SHAPE : GPD_ERR_ARG;
+        if (q_heads + k_heads > 0 && (!workspace_dev || workspace_bytes < 2 * GPD_HEAD_NORM_MAX_PARTS * (int64_t)head_dim * 4 || !lm::aligned(workspace_dev, 4)))
+            return GPD_ERR_WORKSPACE;
+    }
+    if ((q_heads > 0 && !dq_weight_dev) || (k_heads > 0 && !dk_weight_dev)) return GPD_ERR_ARG;
+    if (type == GPD_DT_F32) return launch_heads_backward<float>(a, dq_weight_dev, dk_weight_dev, st);
+    return type == GPD_DT_BF16 ? launch_heads_backward<__nv_bfloat16>(a, dq_weight_dev, dk_weight_dev, st)
+                               : launch_heads_backward<__half>(a, dq_weight_dev, dk_weight_dev, st);
+}

@@ -14,6 +14,7 @@
 #include <cstdio>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
 #include "gpd.h"
 
@@ -84,14 +85,14 @@ public:
         return v;
     }
     // The leading tensor: fixes the device (the current one) and the shape.
-    const at::Tensor& lead(const char* name, int i, unsigned types) {
+    const at::Tensor& lead(const char* name, int i, unsigned types, int dims = 2) {
         const at::Tensor& t = tensor(name, i);
         if (!t.is_cuda()) refuse(name, "device tensor expected");
         device_ = t.device();
         const int current = c10::cuda::current_device();
         if (device_.index() != current)
             refuse(name, "tensor is on cuda:" + std::to_string(device_.index()) + ", the current device is cuda:" + std::to_string(current));
-        if (t.dim() != 2) refuse(name, "matrix expected, got shape " + shape_text(t));
+        if (t.dim() != dims) refuse(name, std::string(dims == 2 ? "matrix" : "vector") + " expected, got shape " + shape_text(t));
         check_type(name, t, types);
         return t;
     }
@@ -146,6 +147,15 @@ public:
         const bool shape = t.dim() == 2 ? t.size(0) == T && t.size(1) == G : t.dim() == 1 && G == 1 && t.size(0) == T;
         if (!shape || !t.is_contiguous())
             refuse(name, "contiguous (" + std::to_string(T) + ", " + std::to_string(G) + ") tensor expected, got shape " + shape_text(t));
+        return t.data_ptr();
+    }
+    // contiguous, of any type
+    void* buffer(const char* name, int i, int64_t* bytes) const {
+        if (absent(i)) refuse(name, "needed");
+        const at::Tensor& t = tensor(name, i);
+        check_device(name, t);
+        if (!t.is_contiguous()) refuse(name, "contiguous buffer expected");
+        *bytes = t.numel() * (int64_t)t.element_size();
         return t.data_ptr();
     }
     void check_device(const char* name, const at::Tensor& t) const {
@@ -316,6 +326,184 @@ gpd_status distill_topk(PyObject* const* args, Py_ssize_t n) {
                             (int32_t)K, w, (float)c.number(6), loss, md.p, md.ld, T, V, c.stream(7));
 }
 
+// Queries or keys and their head count: [T, heads * D], None for no heads.
+int32_t heads_of(const Call& c, const char* name, int i, int64_t T, int64_t D) {
+    if (c.absent(i)) return 0;
+    const at::Tensor& t = c.tensor(name, i);
+    if (t.dim() != 2 || t.size(0) != T || t.size(1) % D || t.size(1) / D > GPD_HEAD_MAX_HEADS)
+        refuse(name, "(" + std::to_string(T) + ", heads * " + std::to_string(D) + ") expected, got shape " + shape_text(t));
+    return (int32_t)(t.size(1) / D);
+}
+// Table of angles, positions and axes from argument `at` on (table, positions, axes).
+struct Angles {
+    const float* table = nullptr;
+    int64_t ldt = 0, P = 0, ldp = 0;
+    int32_t R = 0, index_bytes = 4, n = 1;
+    const void* pos = nullptr;
+    const uint8_t* axes = nullptr;
+    Angles(const Call& c, int at, int64_t T) {
+        if (c.absent(at)) {
+            if (!c.absent(at + 1) || !c.absent(at + 2)) throw Refusal("table: needed with positions or axes");
+            return;
+        }
+        const at::Tensor& t = c.tensor("table", at);
+        if (t.dim() != 2 || t.size(1) > GPD_HEAD_MAX_DIM || t.size(1) % 2) refuse("table", "[positions, columns] expected, got shape " + shape_text(t));
+        const auto m = c.mat("table", at, kF32, t.size(0), t.size(1));
+        table = static_cast<const float*>(m.p);
+        ldt = m.ld;
+        P = t.size(0);
+        R = (int32_t)t.size(1);
+        if (c.absent(at + 1)) refuse("positions", "needed");
+        const at::Tensor& p = c.tensor("positions", at + 1);
+        index_bytes = (int32_t)p.element_size();
+        if (p.dim() == 1) {
+            pos = c.vec("positions", at + 1, kIndex, T);
+            ldp = 1;
+        } else {
+            if (p.dim() != 2 || p.size(1) < 1 || p.size(1) > GPD_HEAD_MAX_AXES)
+                refuse("positions", "[T] or [T, axes] expected, got shape " + shape_text(p));
+            n = (int32_t)p.size(1);
+            const auto mp = c.mat("positions", at + 1, kIndex, T, n);
+            pos = mp.p;
+            ldp = mp.ld;
+        }
+        if (n > 1 && c.absent(at + 2)) refuse("axes", "needed with positions of several axes");
+        axes = static_cast<const uint8_t*>(c.vec("axes", at + 2, kU8, R / 2));
+    }
+};
+
+gpd_status head_norm_rope(PyObject* const* args, Py_ssize_t n) {
+    // q, k, table, positions, axes, q_out, k_out, head_dim, q_weight, k_weight, eps, neighbours, stream
+    Call c(args, n, 13);
+    const int first = c.absent(0) ? 1 : 0;
+    const at::Tensor& x = c.lead(first ? "k" : "q", first, kFloats);
+    const int64_t T = x.size(0), D = c.integer(7);
+    if (D <= 0 || D > GPD_HEAD_MAX_DIM) refuse("head_dim", "1 .. " + std::to_string(GPD_HEAD_MAX_DIM));
+    const unsigned same = type_bit(x.scalar_type());
+    const int32_t Hq = heads_of(c, "q", 0, T, D), Hk = heads_of(c, "k", 1, T, D);
+    const auto mq = c.mat("q", 0, same, T, Hq * D), mk = c.mat("k", 1, same, T, Hk * D);
+    const Angles an(c, 2, T);
+    if (c.absent(0) != c.absent(5)) throw Refusal("q and q_out go together");
+    if (c.absent(1) != c.absent(6)) throw Refusal("k and k_out go together");
+    const auto oq = c.mat("q_out", 5, same, T, Hq * D), ok = c.mat("k_out", 6, same, T, Hk * D);
+    unsigned wq = 0, wk = 0;
+    void *pq = c.vec("q_weight", 8, same | kF32, D, &wq), *pk = c.vec("k_weight", 9, same | kF32, D, &wk);
+    if (wq && wk && wq != wk) throw Refusal("q_weight and k_weight: one type expected");
+    const int near = PyObject_IsTrue(args[11]);
+    if (near < 0) throw PythonError();
+    return gpd_head_norm_rope(gpd_type(same), mq.p, mq.ld, Hq, mk.p, mk.ld, Hk, (int32_t)D, gpd_type(wq ? wq : wk ? wk : same), pq, pk,
+                              (float)c.number(10), an.table, an.ldt, an.P, an.R, near, an.index_bytes, an.pos, an.ldp, an.n, an.axes, oq.p,
+                              oq.ld, ok.p, ok.ld, T, c.stream(12));
+}
+
+gpd_status head_norm_rope_backward(PyObject* const* args, Py_ssize_t n) {
+    // dq, dk, table, positions, axes, q, k, dq_in, dk_in, head_dim, q_weight, k_weight, dq_weight, dk_weight, workspace, eps,
+    // neighbours, stream
+    Call c(args, n, 18);
+    const int first = c.absent(0) ? 1 : 0;
+    const at::Tensor& x = c.lead(first ? "dk" : "dq", first, kFloats);
+    const int64_t T = x.size(0), D = c.integer(9);
+    if (D <= 0 || D > GPD_HEAD_MAX_DIM) refuse("head_dim", "1 .. " + std::to_string(GPD_HEAD_MAX_DIM));
+    const unsigned same = type_bit(x.scalar_type());
+    const int32_t Hq = heads_of(c, "dq", 0, T, D), Hk = heads_of(c, "dk", 1, T, D);
+    const auto gq = c.mat("dq", 0, same, T, Hq * D), gk = c.mat("dk", 1, same, T, Hk * D);
+    const Angles an(c, 2, T);
+    if (c.absent(0) != c.absent(7)) throw Refusal("dq and dq_in go together");
+    if (c.absent(1) != c.absent(8)) throw Refusal("dk and dk_in go together");
+    const auto mq = c.mat("q", 5, same, T, Hq * D), mk = c.mat("k", 6, same, T, Hk * D), oq = c.mat("dq_in", 7, same, T, Hq * D),
+               ok = c.mat("dk_in", 8, same, T, Hk * D);
+    unsigned wq = 0, wk = 0;
+    void *pq = c.vec("q_weight", 10, same | kF32, D, &wq), *pk = c.vec("k_weight", 11, same | kF32, D, &wk);
+    if (wq && wk && wq != wk) throw Refusal("q_weight and k_weight: one type expected");
+    float *dwq = static_cast<float*>(c.vec("dq_weight", 12, kF32, D)), *dwk = static_cast<float*>(c.vec("dk_weight", 13, kF32, D));
+    void* ws = nullptr;
+    int64_t ws_bytes = 0;
+    if (!c.absent(14)) ws = c.buffer("workspace", 14, &ws_bytes);
+    const int near = PyObject_IsTrue(args[16]);
+    if (near < 0) throw PythonError();
+    return gpd_head_norm_rope_backward(gpd_type(same), gq.p, gq.ld, gk.p, gk.ld, mq.p, mq.ld, Hq, mk.p, mk.ld, Hk, (int32_t)D,
+                                       gpd_type(wq ? wq : wk ? wk : same), pq, pk, (float)c.number(15), an.table, an.ldt, an.P, an.R, near,
+                                       an.index_bytes, an.pos, an.ldp, an.n, an.axes, oq.p, oq.ld, ok.p, ok.ld, dwq, dwk, T, ws, ws_bytes,
+                                       c.stream(17));
+}
+
+// Tensors of a list: floating types, on the call's device, dense (in any order of their dimensions).
+struct TensorList {
+    std::vector<int32_t> types;
+    std::vector<void*> at;
+    std::vector<int64_t> counts;
+    std::vector<const at::Tensor*> tensors;            // borrowed from the list's items, which `items` keeps
+    PyObject* items = nullptr;
+    TensorList(const Call& c, const char* name, PyObject* list) {
+        if (THPVariable_Check(list)) refuse(name, "list of tensors expected");
+        items = PySequence_Tuple(list);
+        if (!items) throw PythonError();
+        try {
+            fill(c, name);
+        } catch (...) {
+            Py_DECREF(items);
+            throw;
+        }
+    }
+    ~TensorList() { Py_DECREF(items); }
+    TensorList(const TensorList&) = delete;
+    TensorList& operator=(const TensorList&) = delete;
+
+private:
+    void fill(const Call& c, const char* name) {
+        const Py_ssize_t n = PyTuple_GET_SIZE(items);
+        if (n > 0x7fffffff) refuse(name, "too many tensors");
+        types.reserve(n);
+        at.reserve(n);
+        counts.reserve(n);
+        tensors.reserve(n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            PyObject* o = PyTuple_GET_ITEM(items, i);
+            if (!THPVariable_Check(o)) refuse(name, "list of tensors expected");
+            const at::Tensor& t = THPVariable_Unpack(o);
+            types.push_back(gpd_type(c.check_type(name, t, kFloats)));
+            c.check_device(name, t);
+            if (!t.is_non_overlapping_and_dense()) refuse(name, "dense tensors expected, item " + std::to_string(i) + " is not");
+            at.push_back(t.numel() ? t.data_ptr() : nullptr);
+            counts.push_back(t.numel());
+            tensors.push_back(&t);
+        }
+    }
+};
+
+gpd_status grad_norm(PyObject* const* args, Py_ssize_t n) {
+    // grads, norm, workspace, stream
+    Call c(args, n, 4);
+    c.lead("norm", 1, kF32, 1);
+    float* norm = static_cast<float*>(c.need_vec("norm", 1, kF32, 1));
+    const TensorList g(c, "grads", args[0]);
+    int64_t ws_bytes = 0;
+    void* ws = c.buffer("workspace", 2, &ws_bytes);
+    return gpd_grad_norm((int32_t)g.at.size(), g.types.data(), g.at.data(), g.counts.data(), norm, ws, ws_bytes, c.stream(3));
+}
+
+gpd_status clip_grads(PyObject* const* args, Py_ssize_t n) {
+    // grads, norm, max_norm, out, stream
+    Call c(args, n, 5);
+    c.lead("norm", 1, kF32, 1);
+    const float* norm = static_cast<float*>(c.need_vec("norm", 1, kF32, 1));
+    const TensorList g(c, "grads", args[0]);
+    const float max_norm = (float)c.number(2);
+    if (c.absent(3))
+        return gpd_clip_grads((int32_t)g.at.size(), g.types.data(), g.at.data(), g.types.data(), g.at.data(), g.counts.data(), norm, max_norm,
+                              c.stream(4));
+    const TensorList o(c, "out", args[3]);
+    if (o.at.size() != g.at.size()) refuse("out", std::to_string(g.at.size()) + " tensors expected, got " + std::to_string(o.at.size()));
+    for (size_t i = 0; i < g.at.size(); ++i) {
+        const at::Tensor &a = *g.tensors[i], &b = *o.tensors[i];
+        if (a.sizes() != b.sizes()) refuse("out", "item " + std::to_string(i) + " has shape " + shape_text(b) + " for a gradient of shape " + shape_text(a));
+        if (a.strides() != b.strides() && !(a.is_contiguous() && b.is_contiguous()))
+            refuse("out", "item " + std::to_string(i) + " has its dimensions in another order than its gradient");
+    }
+    return gpd_clip_grads((int32_t)g.at.size(), g.types.data(), g.at.data(), o.types.data(), o.at.data(), g.counts.data(), norm, max_norm,
+                          c.stream(4));
+}
+
 // No C++ exception leaves for the interpreter.
 template <gpd_status (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -334,7 +522,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(rmsnorm_quant), ENTRY(rmsnorm_backward), ENTRY(quantize_blocks), ENTRY(gemm_fp8), ENTRY(token_logprobs),
-                         ENTRY(token_logprobs_backward), ENTRY(distill_topk), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(token_logprobs_backward), ENTRY(distill_topk), ENTRY(head_norm_rope), ENTRY(head_norm_rope_backward),
+                         ENTRY(grad_norm), ENTRY(clip_grads), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lm", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -32,6 +32,7 @@ except ImportError as e:
 GPD_DT_F32, GPD_DT_BF16, GPD_DT_F16, GPD_DT_E4M3, GPD_DT_E5M2 = range(5)
 GPD_RMSNORM_MAX_PARTS = 512
 GPD_LOGPROBS_MAX_TOP, GPD_LOGPROBS_MAX_TOKENS, GPD_DISTILL_MAX_TOP = 32, 64, 1024
+GPD_HEAD_MAX_DIM, GPD_HEAD_MAX_AXES, GPD_HEAD_NORM_MAX_PARTS, GPD_GRAD_NORM_WORKSPACE = 256, 4, 512, 16384
 _BLOCK = 128
 
 _vp, _i32, _i64, _f, _e = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_int
@@ -47,8 +48,16 @@ lib.gpd_token_logprobs_backward.argtypes = [_e, _vp, _i64, _i32, _vp, _i32, _f, 
                                             _vp]
 lib.gpd_distill_topk.argtypes = [_e, _vp, _i64, _i32, _vp, _i64, _e, _vp, _i64, _i32, _vp, _f, _vp, _vp, _i64, _i64, _i64,
                                  _vp]
+lib.gpd_head_norm_rope.argtypes = [_e, _vp, _i64, _i32, _vp, _i64, _i32, _i32, _e, _vp, _vp, _f, _vp, _i64, _i64, _i32, _i32, _i32,
+                                   _vp, _i64, _i32, _vp, _vp, _i64, _vp, _i64, _i64, _vp]
+lib.gpd_head_norm_rope_backward.argtypes = [_e, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _i32, _i32, _e, _vp, _vp, _f, _vp,
+                                            _i64, _i64, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64,
+                                            _vp, _i64, _vp]
+lib.gpd_grad_norm.argtypes = [_i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp]
+lib.gpd_clip_grads.argtypes = [_i32, _vp, _vp, _vp, _vp, _vp, _vp, _f, _vp]
 _NAMES = ["gpd_rmsnorm_quant", "gpd_rmsnorm_backward", "gpd_quantize_blocks", "gpd_gemm_fp8", "gpd_token_logprobs",
-          "gpd_token_logprobs_backward", "gpd_distill_topk"]
+          "gpd_token_logprobs_backward", "gpd_distill_topk", "gpd_head_norm_rope", "gpd_head_norm_rope_backward", "gpd_grad_norm",
+          "gpd_clip_grads"]
 for _name in _NAMES:
     getattr(lib, _name).restype = C.c_int
 EXPORTED += _NAMES
@@ -117,3 +126,46 @@ def gpd_distill_topk(logits, teacher_ids, teacher_logits, weights, loss, dlogits
     status = _lm.distill_topk(logits, teacher_ids, teacher_logits, weights, loss, dlogits, temperature, stream)
     if status:
         _check(status, "gpd_distill_topk")
+
+
+def new_rope_table(positions: int, rotated: int, base: float = 10000.0, device="cuda"):
+    """Cosines and sines of the angles position * base^(-2 j / rotated) for gpd_head_norm_rope: [positions, rotated] FP32, pair
+    j in columns j and rotated / 2 + j.  Angles are taken in FP64: far positions lose them in FP32."""
+    j = torch.arange(rotated // 2, dtype=torch.float64, device=device)
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * torch.pow(float(base), -2.0 * j / rotated)
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def gpd_head_norm_rope(q, k, table, positions, q_out, k_out, head_dim: int, q_weight=None, k_weight=None, eps: float = 1e-6,
+                       axes=None, neighbours: bool = False, stream=None):
+    """q, k: [T, heads * head_dim], either may be None with its output; table: [positions, rotated columns] FP32 or None for no
+    rotation; positions: [T], or [T, axes] with axes (uint8, one for each pair); weights None: rotation alone."""
+    status = _lm.head_norm_rope(q, k, table, positions, axes, q_out, k_out, head_dim, q_weight, k_weight, eps, neighbours, stream)
+    if status:
+        _check(status, "gpd_head_norm_rope")
+
+
+def gpd_head_norm_rope_backward(dq, dk, q, k, table, positions, dq_in, dk_in, head_dim: int, q_weight=None, k_weight=None,
+                                dq_weight=None, dk_weight=None, workspace=None, eps: float = 1e-6, axes=None,
+                                neighbours: bool = False, stream=None):
+    """dq, dk: gradients of the forward call's outputs; q, k: its inputs; dq_in, dk_in: theirs.  With weights: dq_weight,
+    dk_weight ([head_dim] FP32) and workspace, 2 * GPD_HEAD_NORM_MAX_PARTS * head_dim * 4 bytes."""
+    status = _lm.head_norm_rope_backward(dq, dk, table, positions, axes, q, k, dq_in, dk_in, head_dim, q_weight, k_weight, dq_weight,
+                                         dk_weight, workspace, eps, neighbours, stream)
+    if status:
+        _check(status, "gpd_head_norm_rope_backward")
+
+
+def gpd_grad_norm(grads, norm, workspace, stream=None):
+    """grads: list of dense tensors, FP32, BF16 and FP16 mixed as they come; norm: [1] FP32; workspace:
+    GPD_GRAD_NORM_WORKSPACE bytes."""
+    status = _lm.grad_norm(grads, norm, workspace, stream)
+    if status:
+        _check(status, "gpd_grad_norm")
+
+
+def gpd_clip_grads(grads, norm, max_norm: float, out=None, stream=None):
+    """out: list of the gradients' shapes, of any of the three types; None: in place."""
+    status = _lm.clip_grads(grads, norm, max_norm, out, stream)
+    if status:
+        _check(status, "gpd_clip_grads")
