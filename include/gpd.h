@@ -601,6 +601,45 @@ gpd_status gpd_grad_norm(int32_t n, const int32_t* types_host, const void* const
 gpd_status gpd_clip_grads(int32_t n, const int32_t* types_host, const void* const* grads_host, const int32_t* out_types_host,
                           void* const* out_host, const int64_t* counts_host, const float* norm_dev, float max_norm, void* stream);
 
+#define GPD_ADAPTER_MAX_RANK 128
+
+/*
+ * gpd_adapter - low-rank adapters of many requests at once beside a projection that they share:
+ *   h[t] = A_i x[t],   out[t] = base[t] + scale[i] B_i h[t]      for the rows t of every segment, i its adapter
+ * Segment s covers the rows offsets[s] .. offsets[s + 1] - 1 of the batch and has the adapter index[s]; offsets (S + 1 numbers,
+ * not decreasing, from 0 to T at most) and index (S) have index_bytes 4 or 8 and lie in device memory.  Segments may be
+ * empty, of one row, or share adapters.  index -1 (any negative number): no adapter, out = base and h = 0.  An index >= n makes
+ * its rows of h and out NaN.  Rows before the first segment and behind the last are left as they were.
+ * x: T rows of K; A: n matrices of r x K (rows lda apart, matrices next_a), B: n matrices of N x r; all of `type`, BF16 or FP16.
+ * scale: n floats or NULL (1).  base and out: T rows of N of out_type (`type` or FP32); base NULL: zero; out may be base with the
+ * same stride.  h: T x r floats, contiguous: written, and what gpd_adapter_backward needs.  Sums are FP32, h goes into the second
+ * product with 16 bits (BF16) or 22 (FP16) or more, 24 where out is FP32; out is rounded once.  1 <= r <= GPD_ADAPTER_MAX_RANK.
+ * Rows on 16-byte boundaries (of A and B too: r a multiple of 8) are much faster.
+ */
+gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n, int32_t r, const void* A_dev, int64_t lda,
+                       int64_t next_a, const void* B_dev, int64_t ldb, int64_t next_b, const float* scale_dev,
+                       int32_t index_bytes, const void* offsets_dev, const void* index_dev, int32_t S, float* h_dev,
+                       gpd_dtype out_type, const void* base_dev, int64_t ldbase, void* out_dev, int64_t ldo, int64_t T,
+                       int64_t K, int64_t N, void* stream);
+/*
+ * gpd_adapter_backward - gradients of it, with u[t] = scale[i] B_i^T dout[t]:
+ *   dx[t] = dbase[t] + A_i^T u[t],   dA_i = sum over the rows of adapter i of u[t] x[t]^T,   dB_i = scale[i] sum of dout[t] h[t]^T
+ * dout: T rows of N of `type`; h as the forward call left it.  dx (of dx_type, `type` or FP32) and dbase as out and base above;
+ * dx NULL: not wanted.  dA (n matrices of r x K) and dB (n of N x r) of grad_type (`type` or FP32), both or neither; every
+ * adapter's are written, zeros where it has no rows, or added to what is there (accumulate != 0).  Rows without an adapter
+ * have dx = dbase and give no gradient; rows outside the segments are not looked at and their dx is left as it was.
+ * Sums are taken in a fixed order.  workspace_dev: the bytes that gpd_adapter_backward_workspace gives, on a 16-byte boundary.
+ */
+gpd_status gpd_adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int32_t n, int32_t r, int64_t* bytes_host);
+gpd_status gpd_adapter_backward(gpd_dtype type, const void* dout_dev, int64_t lddo, const void* x_dev, int64_t ldx, int32_t n,
+                                int32_t r, const void* A_dev, int64_t lda, int64_t next_a, const void* B_dev, int64_t ldb,
+                                int64_t next_b, const float* scale_dev, const float* h_dev, int32_t index_bytes,
+                                const void* offsets_dev, const void* index_dev, int32_t S, gpd_dtype dx_type,
+                                const void* dbase_dev, int64_t lddb, void* dx_dev, int64_t lddx, gpd_dtype grad_type,
+                                void* dA_dev, int64_t ldda, int64_t next_da, void* dB_dev, int64_t lddB, int64_t next_db,
+                                int32_t accumulate, int64_t T, int64_t K, int64_t N, void* workspace_dev,
+                                int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,199 @@
+// Shared by the kernels of low-rank adapters (adapter_shrink.cu, adapter_expand.cu, adapter_grad.cu).
+//
+// The rows of a batch are cut into segments; segment s covers the rows offsets[s] .. offsets[s + 1] - 1 and has the
+// adapter index[s].  Products run on the tensor cores as 16 x 8 x 16 steps with FP32 sums; what they accumulate in one
+// chain is cut every few steps and added to nearest, because the chain itself truncates.
+#pragma once
+
+#include "lm_common.h"
+
+namespace gpd {
+namespace adapter {
+
+using namespace lm;
+
+constexpr int kMaxRank = GPD_ADAPTER_MAX_RANK;
+
+struct Segments {
+    const void *offsets, *index;
+    int64_t T;
+    int S, n;                                          // segments, adapters
+    bool wide;                                         // 8-byte numbers
+};
+// A row tile: rows of one segment.  rows 0: none.  adapter -1: the segment has none; >= n: there is no such adapter.
+struct RowTile {
+    int64_t row;
+    int rows;
+    int64_t id;
+};
+__device__ __forceinline__ int64_t number(const void* p, int64_t i, bool wide) {
+    return wide ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
+}
+__device__ __forceinline__ int64_t offset_at(const Segments& s, int64_t i) {
+    const int64_t v = number(s.offsets, i, s.wide);
+    return v < 0 ? 0 : v > s.T ? s.T : v;              // whatever stands there, rows stay inside the batch
+}
+// Tile number `tile` of the segments' tiles of TM rows.  Every warp works it out by itself: 128 segments per round.
+template <int TM>
+__device__ __forceinline__ RowTile find_tile(const Segments& s, int64_t tile) {
+    const int lane = threadIdx.x & 31;
+    RowTile r{0, 0, -1};
+    int64_t before = 0;
+    for (int64_t base = 0; base < s.S; base += 128) {
+        int64_t at[5], id[4];
+        int n[4], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 5; ++j) {
+            const int64_t i = base + lane * 4 + j;
+            at[j] = offset_at(s, i < s.S ? i : s.S);
+            if (j < 4) id[j] = i < s.S ? number(s.index, i, s.wide) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            n[j] = at[j + 1] > at[j] ? (int)((at[j + 1] - at[j] + TM - 1) / TM) : 0;
+            sum += n[j];
+        }
+        int scan = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += v;
+        }
+        const int total = __shfl_sync(0xffffffffu, scan, 31);
+        if (tile < before + total) {
+            int64_t from = before + scan - sum;
+            const uint32_t has = __ballot_sync(0xffffffffu, tile < before + scan);
+            const int who = __ffs(has) - 1;            // the first lane whose segments reach the tile
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (tile >= from && tile < from + n[j]) {
+                    r.row = at[j] + (tile - from) * TM;
+                    const int64_t left = at[j + 1] - r.row;
+                    r.rows = left < TM ? (int)left : TM;
+                    r.id = id[j];
+                }
+                from += n[j];
+            }
+            r.row = __shfl_sync(0xffffffffu, r.row, who);
+            r.rows = __shfl_sync(0xffffffffu, r.rows, who);
+            r.id = __shfl_sync(0xffffffffu, r.id, who);
+            return r;
+        }
+        before += total;
+    }
+    return r;
+}
+
+// ---- tensor core steps ---------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+template <bool TRANS>
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+    if constexpr (TRANS)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// ---- asynchronous copies ---------------------------------------------------------------------------------
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {     // what is missing is zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Eight 16-bit elements to shared memory, of which n (may be <= 0) exist; vec: from is on a 16-byte boundary (and
+// an address of the tensor, whether or not anything is there).
+template <typename T>
+__device__ __forceinline__ void stage8(uint32_t to, const T* from, int n, bool vec) {
+    if (vec) {
+        copy16(to, from, n <= 0 ? 0 : n >= 8 ? 16 : 2 * n);
+    } else {
+        const unsigned short* s = reinterpret_cast<const unsigned short*>(from);
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) w[i / 2] |= (uint32_t)s[i] << (16 * (i & 1));
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+}
+// ROWS x COLS elements (COLS a multiple of 8) from p, of which rows x cols exist; rows are `pitch` bytes apart in shared memory.
+template <typename T, int ROWS, int COLS, int THREADS>
+__device__ __forceinline__ void stage_tile(uint32_t to, int pitch, const T* p, int64_t ld, int64_t rows, int64_t cols, bool vec) {
+    constexpr int per = COLS / 8;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < ROWS * per; i += THREADS) {
+        const int r = i / per, c = i % per * 8;
+        const int n = r < rows ? (int)min((int64_t)8, cols - c) : 0;
+        stage8<T>(to + r * pitch + 2 * c, n > 0 ? p + (int64_t)r * ld + c : p, n, vec);
+    }
+}
+
+// ---- numbers of FP32 as sums of 16-bit ones ----------------------------------------------------------------
+// x = parts[0] + parts[1] (+ parts[2]) up to 2^-17 (two parts) or 2^-25 of it in BF16, two at a time.  An infinity or a NaN
+// is its first part, the others are then zero.  FP16: two parts, 2^-22 of numbers within its range.
+template <typename T, int PARTS>
+__device__ __forceinline__ void split2(float x, float y, uint32_t (&parts)[PARTS]) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        parts[i] = pack2(x, y, T());
+        const float2 f = unpack2(parts[i], T());
+        x = fabsf(f.x) <= 3.4e38f ? x - f.x : 0.f;
+        y = fabsf(f.y) <= 3.4e38f ? y - f.y : 0.f;
+    }
+}
+// e with m * 2^-e below 4 (FP16 parts of numbers of any size) and both 2^e and 2^-e normal; 0 for zeros, infinities and NaN.
+__device__ __forceinline__ int exponent_of(float m) {
+    const int e = (int)(__float_as_uint(m) >> 23 & 0xff);
+    return e == 0xff || m == 0.f ? 0 : min(max(e - 127, -126), 126);
+}
+__device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // |e| <= 126
+
+// ---- launches (host) -----------------------------------------------------------------------------------
+struct ShrinkArgs {                                    // h[t] = scale_i W_i x[t]
+    Segments seg;
+    const void* x; int64_t ldx;
+    const void* w; int64_t ldw, next;                  // rows of W, adapters apart; transposed: W_i is [C][r]
+    const float* scale;
+    float* h;                                          // [T][r]
+    int64_t C;                                         // columns of x
+    int r;
+    bool x_vec, w_vec;
+};
+struct ExpandArgs {                                    // out[t] = base[t] + scale_i W_i h[t]
+    Segments seg;
+    const float* h;
+    const void* w; int64_t ldw, next;                  // W_i is [C][r]; transposed: [r][C]
+    const float* scale;
+    const void* base; int64_t ldb;
+    void* out; int64_t ldo;
+    int64_t C;                                         // columns of out
+    int r;
+    bool w_vec, io_vec;
+};
+struct GradArgs {                                      // dW_i[c][k] = scale_i sum_t y[t][c] h[t][k], over the rows of adapter i
+    const void* y; int64_t ldy;
+    const float* h;
+    const float* scale;
+    void* dw; int64_t ldw, next;                       // [C][r]; transposed: [r][C]
+    int64_t C;
+    bool y_vec, transposed;
+};
+gpd_status shrink(int type, bool transposed, const ShrinkArgs& a, cudaStream_t st);
+gpd_status expand(int type, int out_type, bool transposed, const ExpandArgs& a, cudaStream_t st);
+int64_t grad_workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N);
+gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& seg, int r, const GradArgs (&two)[2], void* workspace,
+                     cudaStream_t st);
+
+inline int64_t tiles_of(const Segments& s, int TM) { return s.T / TM + (s.S < s.T ? s.S : s.T); }
+
+}  // namespace adapter
+}  // namespace gpd

@@ -1,0 +1,158 @@
+// First factor of low-rank adapters: h[t] = scale_i W_i x[t] for the rows of every segment, i its adapter.
+//
+// Bound by reading x (many rows) or the adapters (one row per segment); the r columns of the result are few.  A CTA takes
+// 64 rows of one segment, or 16 where segments are short, and a part of the columns of x; the CTAs of a cluster have the
+// other parts and add up their sums over distributed shared memory, in a fixed order.  Tiles of x and W come through a
+// ring of asynchronous copies.
+#include <cooperative_groups.h>
+
+#include "adapter_common.h"
+
+namespace gpd {
+namespace adapter {
+
+namespace {
+
+constexpr int kThreads = 128, kDeep = 64, kXPitch = 2 * kDeep + 16;    // columns of x per stage
+
+template <int NT, int WM, bool TRANS>
+struct Shape {
+    static constexpr int TM = 16 * WM, RP = 8 * NT, STAGES = WM == 1 ? 6 : 4;
+    static constexpr int W_ROWS = TRANS ? kDeep : RP, W_COLS = TRANS ? RP : kDeep, W_PITCH = 2 * W_COLS + 16;
+    static constexpr int STAGE = TM * kXPitch + W_ROWS * W_PITCH;
+    static constexpr int SUMS = 64 * RP * 4;           // FP32 sums: of 64 rows, or of 16 rows four times
+    static constexpr int SMEM = STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS;
+};
+
+// WM = 4: a warp has 16 rows of the tile.  WM = 1: all warps have the same 16 rows, and each a quarter of every stage.
+template <typename T, int NT, int WM, bool TRANS>
+__global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant__ ShrinkArgs a, int splits) {
+    using S = Shape<NT, WM, TRANS>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    after_previous();
+    const int rank = blockIdx.x % splits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x / splits);
+    if (tile.rows == 0) return;                        // the whole cluster
+    float* out = a.h + tile.row * a.r;
+    if (tile.id < 0 || tile.id >= a.seg.n) {
+        const float v = tile.id < 0 ? 0.f : __int_as_float(0x7fffffff);
+        if (rank == 0)
+            for (int i = threadIdx.x; i < tile.rows * a.r; i += kThreads) out[i] = v;
+        return;
+    }
+    const T* x = static_cast<const T*>(a.x) + tile.row * a.ldx;
+    const T* w = static_cast<const T*>(a.w) + tile.id * a.next;
+    const int64_t stages = (a.C + kDeep - 1) / kDeep;
+    const int64_t from = stages * rank / splits, to = stages * (rank + 1) / splits;
+    const uint32_t ring = smem_at(smem);
+    auto fetch = [&](int64_t k) {
+        if (k < to) {
+            const uint32_t at = ring + (uint32_t)((k - from) % S::STAGES) * S::STAGE;
+            const int64_t c = k * kDeep;
+            stage_tile<T, S::TM, kDeep, kThreads>(at, kXPitch, x + c, a.ldx, tile.rows, a.C - c, a.x_vec);
+            if (TRANS) stage_tile<T, S::W_ROWS, S::W_COLS, kThreads>(at + S::TM * kXPitch, S::W_PITCH, w + c * a.ldw, a.ldw, a.C - c, a.r, a.w_vec);
+            else stage_tile<T, S::W_ROWS, S::W_COLS, kThreads>(at + S::TM * kXPitch, S::W_PITCH, w + c, a.ldw, a.r, a.C - c, a.w_vec);
+        }
+        copies_end();
+    };
+    float sum[NT][4], acc[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[n][i] = acc[n][i] = 0.f;
+    auto cut = [&]() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[n][i] += acc[n][i];
+                acc[n][i] = 0.f;
+            }
+    };
+    for (int i = 0; i < S::STAGES - 1; ++i) fetch(from + i);
+    for (int64_t k = from; k < to; ++k) {
+        copies_wait<S::STAGES - 2>();
+        __syncthreads();
+        fetch(k + S::STAGES - 1);
+        const uint32_t xs = ring + (uint32_t)((k - from) % S::STAGES) * S::STAGE, ws = xs + S::TM * kXPitch;
+        auto step = [&](int ks) {
+            uint32_t xa[4];
+            ldmatrix4<false>(xa, xs + ((WM == 4 ? 16 * warp : 0) + (lane & 15)) * kXPitch + 2 * (16 * ks + (lane >> 4) * 8));
+#pragma unroll
+            for (int p = 0; p < NT / 2; ++p) {
+                uint32_t b[4];
+                if (TRANS) ldmatrix4<true>(b, ws + (16 * ks + (lane & 15)) * S::W_PITCH + 2 * (16 * p + (lane >> 4) * 8));
+                else ldmatrix4<false>(b, ws + (16 * p + (lane & 7) + (lane >> 4) * 8) * S::W_PITCH + 2 * (16 * ks + (lane >> 3 & 1) * 8));
+                mma(acc[2 * p], xa, b[0], b[1], T());
+                mma(acc[2 * p + 1], xa, b[2], b[3], T());
+            }
+        };
+        if (WM == 4) {
+#pragma unroll
+            for (int ks = 0; ks < kDeep / 16; ++ks) step(ks);
+            cut();
+        } else {
+            step(warp);
+            if (((k - from) & 3) == 3) cut();
+        }
+    }
+    cut();
+    copies_wait<0>();
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float* s = sums + (16 * warp + (lane >> 2)) * S::RP + 8 * n + 2 * (lane & 3);
+        *reinterpret_cast<float2*>(s) = make_float2(sum[n][0], sum[n][1]);
+        *reinterpret_cast<float2*>(s + 8 * S::RP) = make_float2(sum[n][2], sum[n][3]);
+    }
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    if (splits > 1) cluster.sync();
+    else __syncthreads();
+    const float scale = a.scale ? a.scale[tile.id] : 1.f;
+    for (int e = rank * kThreads + threadIdx.x; e < S::TM * S::RP; e += splits * kThreads) {
+        const int row = e / S::RP, c = e % S::RP;
+        if (row >= tile.rows || c >= a.r) continue;
+        float v = 0.f;
+        for (int s = 0; s < splits; ++s) {
+            const float* other = splits > 1 ? cluster.map_shared_rank(sums, s) : sums;
+#pragma unroll
+            for (int q = 0; q < (WM == 1 ? 4 : 1); ++q) v += other[e + q * 16 * S::RP];
+        }
+        out[(int64_t)row * a.r + c] = v * scale;
+    }
+    if (splits > 1) cluster.sync();                    // the others have read this CTA's sums
+}
+
+template <typename T, int NT, int WM, bool TRANS>
+gpd_status launch(const ShrinkArgs& a, cudaStream_t st) {
+    using S = Shape<NT, WM, TRANS>;
+    const int64_t tiles = tiles_of(a.seg, S::TM), stages = (a.C + kDeep - 1) / kDeep;
+    int splits = 1;                                    // until two CTAs per SM are busy, but four stages each at least
+    while (splits < 8 && tiles * splits < 2 * sm_count() && stages >= 8 * splits) splits *= 2;
+    if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
+    auto kernel = shrink_kernel<T, NT, WM, TRANS>;
+    if (S::SMEM > 49152 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), S::SMEM, splits, st, a, splits);
+}
+template <typename T, int NT, bool TRANS>
+gpd_status launch_rows(const ShrinkArgs& a, cudaStream_t st) {
+    // Segments of 16 rows and less on average: tiles of 16 rows.
+    return a.seg.T <= 16 * (int64_t)a.seg.S ? launch<T, NT, 1, TRANS>(a, st) : launch<T, NT, 4, TRANS>(a, st);
+}
+template <typename T, bool TRANS>
+gpd_status launch_rank(const ShrinkArgs& a, cudaStream_t st) {
+    if (a.r <= 16) return launch_rows<T, 2, TRANS>(a, st);
+    if (a.r <= 32) return launch_rows<T, 4, TRANS>(a, st);
+    return a.r <= 64 ? launch_rows<T, 8, TRANS>(a, st) : launch_rows<T, 16, TRANS>(a, st);
+}
+
+}  // namespace
+
+gpd_status shrink(int type, bool transposed, const ShrinkArgs& a, cudaStream_t st) {
+    if (type == GPD_DT_BF16) return transposed ? launch_rank<__nv_bfloat16, true>(a, st) : launch_rank<__nv_bfloat16, false>(a, st);
+    return transposed ? launch_rank<__half, true>(a, st) : launch_rank<__half, false>(a, st);
+}
+
+}  // namespace adapter
+}  // namespace gpd

@@ -427,6 +427,108 @@ gpd_status head_norm_rope_backward(PyObject* const* args, Py_ssize_t n) {
                                        c.stream(17));
 }
 
+// n matrices of rows x cols
+struct Cube {
+    void* p = nullptr;
+    int64_t ld = 0, next = 0;
+    unsigned type = 0;
+};
+Cube cube(const Call& c, const char* name, int i, unsigned types, int64_t n, int64_t rows, int64_t cols) {
+    Cube m;
+    if (c.absent(i)) return m;
+    const at::Tensor& t = c.tensor(name, i);
+    m.type = c.check_type(name, t, types);
+    c.check_device(name, t);
+    if (t.dim() != 3 || t.size(0) != n || t.size(1) != rows || t.size(2) != cols)
+        refuse(name, "shape (" + std::to_string(n) + ", " + std::to_string(rows) + ", " + std::to_string(cols) + ") expected, got " + shape_text(t));
+    if (cols > 1 && t.stride(2) != 1) refuse(name, "columns have to be adjacent");
+    m.ld = rows > 1 ? t.stride(1) : cols;
+    if (m.ld < cols) refuse(name, "rows overlap");
+    const int64_t size = m.ld * (rows - 1) + cols;
+    m.next = n > 1 ? t.stride(0) : size;
+    if (m.next < size) refuse(name, "matrices overlap");
+    m.p = t.data_ptr();
+    return m;
+}
+// The segments of a batch: offsets [S + 1] and index [S], of one type.
+struct Parts {
+    const void *offsets, *index;
+    int32_t S, index_bytes;
+    Parts(const Call& c, int at) {
+        const at::Tensor &o = c.tensor("offsets", at), &i = c.tensor("index", at + 1);
+        if (i.dim() != 1 || i.size(0) >= 0x7fffffff) refuse("index", "vector expected, got shape " + shape_text(i));
+        S = (int32_t)i.size(0);
+        offsets = c.vec("offsets", at, kIndex, (int64_t)S + 1);
+        index = c.vec("index", at + 1, kIndex, S);
+        if (o.scalar_type() != i.scalar_type()) throw Refusal("offsets and index: one type expected");
+        index_bytes = (int32_t)o.element_size();
+    }
+};
+// Sizes that A [n, r, K] and B [n, N, r] give.
+struct Factors {
+    int64_t n, r, N;
+    Cube A, B;
+    Factors(const Call& c, int at, unsigned type, int64_t K) {
+        const at::Tensor &a = c.tensor("A", at), &b = c.tensor("B", at + 1);
+        if (a.dim() != 3 || a.size(0) > 0x7fffffff || a.size(1) < 1 || a.size(1) > GPD_ADAPTER_MAX_RANK)
+            refuse("A", "[adapters, rank of at most " + std::to_string(GPD_ADAPTER_MAX_RANK) + ", K] expected, got shape " + shape_text(a));
+        if (b.dim() != 3) refuse("B", "[adapters, N, rank] expected, got shape " + shape_text(b));
+        n = a.size(0);
+        r = a.size(1);
+        N = b.size(1);
+        if (K < 1 || N < 1) throw Refusal("A, B: K and N of at least 1 expected");
+        A = cube(c, "A", at, type, n, r, K);
+        B = cube(c, "B", at + 1, type, n, N, r);
+    }
+};
+
+gpd_status adapter(PyObject* const* args, Py_ssize_t n) {
+    // x, A, B, offsets, index, out, h, base, scale, stream
+    Call c(args, n, 10);
+    const at::Tensor& x = c.lead("x", 0, kBF16 | kF16);
+    const int64_t T = x.size(0), K = x.size(1);
+    const unsigned same = type_bit(x.scalar_type());
+    const auto mx = c.mat("x", 0, same, T, K);
+    const Factors f(c, 1, same, K);
+    const Parts p(c, 3);
+    const auto mo = c.need_mat("out", 5, same | kF32, T, f.N);
+    const auto mb = c.mat("base", 7, mo.type, T, f.N);
+    if (c.absent(6)) refuse("h", "needed");
+    float* h = static_cast<float*>(c.per_row("h", 6, kF32, T, f.r));
+    const float* scale = static_cast<float*>(c.vec("scale", 8, kF32, f.n));
+    return gpd_adapter(gpd_type(same), mx.p, mx.ld, (int32_t)f.n, (int32_t)f.r, f.A.p, f.A.ld, f.A.next, f.B.p, f.B.ld, f.B.next, scale,
+                       p.index_bytes, p.offsets, p.index, p.S, h, gpd_type(mo.type), mb.p, mb.ld, mo.p, mo.ld, T, K, f.N, c.stream(9));
+}
+
+gpd_status adapter_backward(PyObject* const* args, Py_ssize_t n) {
+    // dout, x, A, B, h, offsets, index, dx, dA, dB, workspace, dbase, scale, accumulate, stream
+    Call c(args, n, 15);
+    const at::Tensor& x = c.lead("x", 1, kBF16 | kF16);
+    const int64_t T = x.size(0), K = x.size(1);
+    const unsigned same = type_bit(x.scalar_type());
+    const auto mx = c.mat("x", 1, same, T, K);
+    const Factors f(c, 2, same, K);
+    const auto md = c.need_mat("dout", 0, same, T, f.N);
+    const Parts p(c, 5);
+    if (c.absent(4)) refuse("h", "needed");
+    const float* h = static_cast<float*>(c.per_row("h", 4, kF32, T, f.r));
+    const auto mdx = c.mat("dx", 7, same | kF32, T, K);
+    if (!mdx.type && !c.absent(11)) throw Refusal("dbase: dx is needed with it");
+    const auto mdb = c.mat("dbase", 11, mdx.type, T, K);
+    if (c.absent(8) != c.absent(9)) throw Refusal("dA and dB go together");
+    const Cube dA = cube(c, "dA", 8, same | kF32, f.n, f.r, K), dB = cube(c, "dB", 9, same | kF32, f.n, f.N, f.r);
+    if (dA.type != dB.type) throw Refusal("dA and dB: one type expected");
+    int64_t ws_bytes = 0;
+    void* ws = c.buffer("workspace", 10, &ws_bytes);
+    const float* scale = static_cast<float*>(c.vec("scale", 12, kF32, f.n));
+    const int acc = PyObject_IsTrue(args[13]);
+    if (acc < 0) throw PythonError();
+    return gpd_adapter_backward(gpd_type(same), md.p, md.ld, mx.p, mx.ld, (int32_t)f.n, (int32_t)f.r, f.A.p, f.A.ld, f.A.next, f.B.p, f.B.ld,
+                                f.B.next, scale, h, p.index_bytes, p.offsets, p.index, p.S, mdx.type ? gpd_type(mdx.type) : GPD_DT_F32, mdb.p,
+                                mdb.ld, mdx.p, mdx.ld, dA.type ? gpd_type(dA.type) : GPD_DT_F32, dA.p, dA.ld, dA.next, dB.p, dB.ld, dB.next,
+                                acc, T, K, f.N, ws, ws_bytes, c.stream(14));
+}
+
 // Tensors of a list: floating types, on the call's device, dense (in any order of their dimensions).
 struct TensorList {
     std::vector<int32_t> types;
@@ -523,7 +625,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(rmsnorm_quant), ENTRY(rmsnorm_backward), ENTRY(quantize_blocks), ENTRY(gemm_fp8), ENTRY(token_logprobs),
                          ENTRY(token_logprobs_backward), ENTRY(distill_topk), ENTRY(head_norm_rope), ENTRY(head_norm_rope_backward),
-                         ENTRY(grad_norm), ENTRY(clip_grads), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(grad_norm), ENTRY(clip_grads), ENTRY(adapter), ENTRY(adapter_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lm", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -33,6 +33,7 @@ GPD_DT_F32, GPD_DT_BF16, GPD_DT_F16, GPD_DT_E4M3, GPD_DT_E5M2 = range(5)
 GPD_RMSNORM_MAX_PARTS = 512
 GPD_LOGPROBS_MAX_TOP, GPD_LOGPROBS_MAX_TOKENS, GPD_DISTILL_MAX_TOP = 32, 64, 1024
 GPD_HEAD_MAX_DIM, GPD_HEAD_MAX_AXES, GPD_HEAD_NORM_MAX_PARTS, GPD_GRAD_NORM_WORKSPACE = 256, 4, 512, 16384
+GPD_ADAPTER_MAX_RANK = 128
 _BLOCK = 128
 
 _vp, _i32, _i64, _f, _e = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_int
@@ -55,9 +56,15 @@ lib.gpd_head_norm_rope_backward.argtypes = [_e, _vp, _i64, _vp, _i64, _vp, _i64,
                                             _vp, _i64, _vp]
 lib.gpd_grad_norm.argtypes = [_i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp]
 lib.gpd_clip_grads.argtypes = [_i32, _vp, _vp, _vp, _vp, _vp, _vp, _f, _vp]
+lib.gpd_adapter.argtypes = [_e, _vp, _i64, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i32, _vp, _vp, _i32, _vp, _e, _vp, _i64,
+                            _vp, _i64, _i64, _i64, _i64, _vp]
+lib.gpd_adapter_backward_workspace.argtypes = [_i64, _i64, _i64, _i32, _i32, C.POINTER(_i64)]
+lib.gpd_adapter_backward.argtypes = [_e, _vp, _i64, _vp, _i64, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i32, _vp, _vp,
+                                     _i32, _e, _vp, _i64, _vp, _i64, _e, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _i64, _i64, _i64,
+                                     _vp, _i64, _vp]
 _NAMES = ["gpd_rmsnorm_quant", "gpd_rmsnorm_backward", "gpd_quantize_blocks", "gpd_gemm_fp8", "gpd_token_logprobs",
           "gpd_token_logprobs_backward", "gpd_distill_topk", "gpd_head_norm_rope", "gpd_head_norm_rope_backward", "gpd_grad_norm",
-          "gpd_clip_grads"]
+          "gpd_clip_grads", "gpd_adapter", "gpd_adapter_backward_workspace", "gpd_adapter_backward"]
 for _name in _NAMES:
     getattr(lib, _name).restype = C.c_int
 EXPORTED += _NAMES
@@ -169,3 +176,28 @@ def gpd_clip_grads(grads, norm, max_norm: float, out=None, stream=None):
     status = _lm.clip_grads(grads, norm, max_norm, out, stream)
     if status:
         _check(status, "gpd_clip_grads")
+
+
+def gpd_adapter(x, A, B, offsets, index, out, h, base=None, scale=None, stream=None):
+    """x: [T, K] BF16 or FP16; A: [adapters, rank, K], B: [adapters, N, rank] of its type; offsets: [S + 1], index: [S] (int32 or
+    int64, -1: no adapter); out, base: [T, N] of x's type or FP32; h: [T, rank] FP32, kept for the backward call; scale: [adapters]
+    FP32."""
+    status = _lm.adapter(x, A, B, offsets, index, out, h, base, scale, stream)
+    if status:
+        _check(status, "gpd_adapter")
+
+
+def gpd_adapter_backward_workspace(T: int, K: int, N: int, adapters: int, rank: int) -> int:
+    """Bytes of workspace that gpd_adapter_backward needs for these sizes."""
+    n = C.c_int64()
+    _check(lib.gpd_adapter_backward_workspace(T, K, N, adapters, rank, C.byref(n)), "gpd_adapter_backward_workspace")
+    return n.value
+
+
+def gpd_adapter_backward(dout, x, A, B, h, offsets, index, dx, dA, dB, workspace, dbase=None, scale=None, accumulate: bool = False,
+                         stream=None):
+    """dx, dbase: [T, K] of x's type or FP32, dx may be None; dA, dB: the shapes of A and B, of x's type or FP32, both may be None;
+    accumulate: dA and dB are added to."""
+    status = _lm.adapter_backward(dout, x, A, B, h, offsets, index, dx, dA, dB, workspace, dbase, scale, accumulate, stream)
+    if status:
+        _check(status, "gpd_adapter_backward")
