@@ -1,5 +1,6 @@
 // Entry points of low-rank adapters beside a shared projection: argument checks, and the order of the kernels.
 #include "adapter_common.h"
+#include "gemm_common.h"
 
 using namespace gpd;
 using namespace gpd::adapter;
@@ -21,6 +22,11 @@ int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace
 
+int gpd::adapter_status_fetch_and_clear() {
+    const int a = shrink_status_fetch_and_clear(), b = expand_status_fetch_and_clear();
+    return a != 0 ? a : b;
+}
+
 extern "C" gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n, int32_t r, const void* A_dev, int64_t lda,
                                   int64_t next_a, const void* B_dev, int64_t ldb, int64_t next_b, const float* scale_dev,
                                   int32_t index_bytes, const void* offsets_dev, const void* index_dev, int32_t S, float* h_dev,
@@ -40,7 +46,8 @@ extern "C" gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx
     const gpd_status first = shrink(type, false, down, st);
     if (first != GPD_OK) return first;
     const ExpandArgs above{seg, h_dev, B_dev, ldb, next_b, scale_dev, base_dev, ldbase, out_dev, ldo, N, r, weights_aligned(B_dev, ldb, next_b),
-                           lm::rows_aligned(base_dev, ldbase, e, wide) && lm::rows_aligned(out_dev, ldo, e, wide)};
+                           lm::rows_aligned(base_dev, ldbase, e, wide) && lm::rows_aligned(out_dev, ldo, e, wide),
+                           lm::rows_aligned(base_dev, ldbase, e) && lm::rows_aligned(out_dev, ldo, e)};
     return expand(type, out_type, false, above, st);
 }
 
@@ -85,7 +92,8 @@ extern "C" gpd_status gpd_adapter_backward(gpd_dtype type, const void* dout_dev,
         if (dx_dev) {
             const int e = lm::dtype_size(dx_type), wide = e == 4 ? 8 : 16;
             const ExpandArgs above{seg, u, A_dev, lda, next_a, nullptr, dbase_dev, lddb, dx_dev, lddx, K, r, weights_aligned(A_dev, lda, next_a),
-                                   lm::rows_aligned(dbase_dev, lddb, e, wide) && lm::rows_aligned(dx_dev, lddx, e, wide)};
+                                   lm::rows_aligned(dbase_dev, lddb, e, wide) && lm::rows_aligned(dx_dev, lddx, e, wide),
+                                   lm::rows_aligned(dbase_dev, lddb, e) && lm::rows_aligned(dx_dev, lddx, e)};
             const gpd_status s2 = expand(type, dx_type, true, above, st);
             if (s2 != GPD_OK) return s2;
         }

@@ -6,6 +6,7 @@
 #pragma once
 
 #include "lm_common.h"
+#include "tc_common.h"
 
 namespace gpd {
 namespace adapter {
@@ -137,6 +138,61 @@ __device__ __forceinline__ void stage_tile(uint32_t to, int pitch, const T* p, i
     }
 }
 
+// ---- tiles by TMA ------------------------------------------------------------------------------------------
+// A ring of stages that one warp fills and four empty.  Waits are bounded: on expiry the CTA gives up and raises the
+// kernel's status word (gpd_device_status).
+template <int STAGES>
+struct Ring {
+    uint64_t full[STAGES], empty[STAGES];
+    int abort;
+    // one thread; arrivals that fill a stage (beside the copies' bytes) and that empty it
+    __device__ __forceinline__ void init(int fills, int empties) {
+        for (int i = 0; i < STAGES; ++i) {
+            tc::mbar_init(&full[i], fills);
+            tc::mbar_init(&empty[i], empties);
+        }
+        abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __device__ __forceinline__ bool wait_full(int k, int* status) { return tc::mbar_wait(&full[k % STAGES], (k / STAGES) & 1, &abort, status); }
+    __device__ __forceinline__ bool wait_empty(int k, int* status) { return tc::mbar_wait(&empty[k % STAGES], ((k / STAGES) & 1) ^ 1, &abort, status); }
+    // After giving up: copies in flight land before the CTA's memory is another's.  `issued` stages were begun.
+    __device__ __forceinline__ void drain(int issued, int* status) {
+        int never = 0;
+        if (*static_cast<volatile int*>(&abort))
+            for (int k = issued > STAGES ? issued - STAGES : 0; k < issued; ++k)
+                tc::mbar_wait(&full[k % STAGES], (k / STAGES) & 1, &never, status);
+    }
+};
+// Byte of a tile whose rows are PITCH (32, 64 or 128) bytes, as TMA's swizzle of that width places it (the tile starts on a
+// 1024-byte boundary): eight rows' pieces of 16 bytes at one column lie in different banks.
+template <int PITCH>
+__device__ __forceinline__ uint32_t swizzled(uint32_t byte) { return byte ^ ((byte >> 7 & (PITCH / 16 - 1)) << 4); }
+// Factors' tiles of ROWS x COLS elements: columns in parts of 64 (128 bytes), one behind the other.
+template <int ROWS, int COLS>
+struct WTile {
+    static constexpr int PITCH = COLS >= 64 ? 128 : 2 * COLS, PARTS = COLS > 64 ? COLS / 64 : 1, BYTES = ROWS * COLS * 2;
+    static __device__ __forceinline__ uint32_t at(int row, int col) {
+        return (uint32_t)(col / 64 * ROWS * 128) + swizzled<PITCH>((uint32_t)(row * PITCH + col % 64 * 2));
+    }
+    static __device__ __forceinline__ void load(unsigned char* to, const CUtensorMap* map, int col, int row, int id, uint64_t* bar) {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) tc::tma_load_3d(to + i * ROWS * 128, map, col + 64 * i, row, id, bar);
+    }
+    // element by element, by one warp: rows off 16-byte boundaries.  What lies outside is zero already, or is written so.
+    template <typename T>
+    static __device__ __forceinline__ void copy(unsigned char* to, const T* p, int64_t ld, int64_t rows, int64_t cols, int used_rows, int used_cols) {
+        const int n = used_rows * used_cols, lane = threadIdx.x & 31;
+#pragma unroll 8
+        for (int i = lane; i < n; i += 32) {
+            const int r = i / used_cols, c = i % used_cols;
+            T v = from_f32<T>(0.f);
+            if (r < rows && c < cols) v = p[r * ld + c];
+            *reinterpret_cast<T*>(to + at(r, c)) = v;
+        }
+    }
+};
+
 // ---- numbers of FP32 as sums of 16-bit ones ----------------------------------------------------------------
 // x = parts[0] + parts[1] (+ parts[2]) up to 2^-17 (two parts) or 2^-25 of it in BF16, two at a time.  An infinity or a NaN
 // is its first part, the others are then zero.  FP16: two parts, 2^-22 of numbers within its range.
@@ -177,7 +233,7 @@ struct ExpandArgs {                                    // out[t] = base[t] + sca
     void* out; int64_t ldo;
     int64_t C;                                         // columns of out
     int r;
-    bool w_vec, io_vec;
+    bool w_vec, io_vec, tma;                           // W on 16-byte boundaries; base and out: pairs or eights; both on 16 bytes
 };
 struct GradArgs {                                      // dW_i[c][k] = scale_i sum_t y[t][c] h[t][k], over the rows of adapter i
     const void* y; int64_t ldy;
@@ -192,6 +248,26 @@ gpd_status expand(int type, int out_type, bool transposed, const ExpandArgs& a, 
 int64_t grad_workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N);
 gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& seg, int r, const GradArgs (&two)[2], void* workspace,
                      cudaStream_t st);
+
+int shrink_status_fetch_and_clear();                   // synchronous reads of the kernels' status words
+int expand_status_fetch_and_clear();
+
+// n matrices of rows x cols (rows ld apart, matrices next) in boxes of box_rows x box_cols; rows of a box are swizzled over
+// their whole width; elements outside read as zero and are not written.
+inline bool make_map(CUtensorMap* map, const void* base, int elem, int64_t n, int64_t rows, int64_t cols, int64_t ld, int64_t next, int box_rows,
+                     int box_cols) {
+    tc::EncodeTiledFn fn = tc::encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)n};
+    cuuint64_t strides[2] = {(cuuint64_t)(ld * elem), (cuuint64_t)((n > 1 ? next : ld) * elem)};
+    cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const int width = box_cols * elem;
+    return fn(map, elem == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 inline int64_t tiles_of(const Segments& s, int TM) { return s.T / TM + (s.S < s.T ? s.S : s.T); }
 

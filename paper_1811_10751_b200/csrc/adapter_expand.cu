@@ -53,6 +53,49 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
 template <typename O> struct Share { uint4 v[2][2]; };                 // [32 columns][row g, g + 8]: eight elements
 template <> struct Share<float> { float2 v[8][2]; };                   // [8 columns][row]: two elements
 
+// The warp's rows of h (those that there are) times scale, as operands of the tensor cores; undo[i]: what FP16 parts of
+// row g + 8 i have to be multiplied with.
+template <typename T, int KT, int PARTS>
+__device__ __forceinline__ void load_parts(const float* h, int r, float scale, const bool (&has)[2], uint32_t (&ha)[PARTS][KT][4], float (&undo)[2]) {
+    const int q = threadIdx.x & 3;
+    float v[KT][2][4];                                 // [16 columns][row][2 q, 2 q + 1, 2 q + 8, 2 q + 9]
+    float most[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = 16 * k + 2 * q + (j & 1) + (j >> 1) * 8;
+                v[k][i][j] = has[i] && c < r ? h[(int64_t)8 * i * r + c] * scale : 0.f;
+                most[i] = fmaxf(most[i], fabsf(v[k][i][j]));
+            }
+    undo[0] = undo[1] = 1.f;
+    if (std::is_same<T, __half>::value) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            most[i] = fmaxf(most[i], __shfl_xor_sync(0xffffffffu, most[i], 1));
+            most[i] = fmaxf(most[i], __shfl_xor_sync(0xffffffffu, most[i], 2));
+            const int e = exponent_of(most[i]);
+            undo[i] = power2(e);
+            const float by = power2(-e);
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[k][i][j] *= by;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {                  // rows g, g + 8, then the same eight columns on
+            uint32_t parts[PARTS];
+            split2<T, PARTS>(v[k][f & 1][2 * (f >> 1)], v[k][f & 1][2 * (f >> 1) + 1], parts);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) ha[p][k][f] = parts[p];
+        }
+}
+
 // WM = 4: a warp has 16 rows of the tile and all columns.  WM = 1: all warps have the same 16 rows, 64 columns each.
 template <typename T, typename O, int KT, int PARTS, int WM, bool TRANS>
 __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant__ ExpandArgs a) {
@@ -83,47 +126,8 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant_
     const int row0 = (WM == 4 ? 16 * warp : 0) + g;
     const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows};
     uint32_t ha[PARTS][KT][4];
-    float undo[2] = {1.f, 1.f};
-    {
-        float v[KT][2][4];                             // [16 columns][row][2 q, 2 q + 1, 2 q + 8, 2 q + 9]
-        const float scale = none || !a.scale ? 1.f : a.scale[tile.id];
-        float most[2] = {0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float* h = a.h + (tile.row + row0 + 8 * i) * a.r;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int c = 16 * k + 2 * q + (j & 1) + (j >> 1) * 8;
-                    v[k][i][j] = !none && has[i] && c < a.r ? h[c] * scale : 0.f;
-                    most[i] = fmaxf(most[i], fabsf(v[k][i][j]));
-                }
-            }
-        if (sizeof(T) == 2 && std::is_same<T, __half>::value) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                most[i] = fmaxf(most[i], __shfl_xor_sync(0xffffffffu, most[i], 1));
-                most[i] = fmaxf(most[i], __shfl_xor_sync(0xffffffffu, most[i], 2));
-                const int e = exponent_of(most[i]);
-                undo[i] = power2(e);
-                const float by = power2(-e);
-#pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[k][i][j] *= by;
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int f = 0; f < 4; ++f) {              // rows g, g + 8, then the same eight columns on
-                uint32_t parts[PARTS];
-                split2<T, PARTS>(v[k][f & 1][2 * (f >> 1)], v[k][f & 1][2 * (f >> 1) + 1], parts);
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) ha[p][k][f] = parts[p];
-            }
-    }
+    float undo[2];
+    load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
     const O* base = a.base ? static_cast<const O*>(a.base) + (tile.row + row0) * a.ldb : nullptr;
     O* out = static_cast<O*>(a.out) + (tile.row + row0) * a.ldo;
 
@@ -250,10 +254,193 @@ gpd_status launch(const ExpandArgs& a, cudaStream_t st) {
     if (S::SMEM > 49152 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
     return launch_after(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads), S::SMEM, 1, st, a);
 }
+// ---- the same with tiles by TMA: many rows, base and out on 16-byte boundaries ---------------------------------
+// Tiles of base arrive in shared memory, a lane adds its products to its elements there, and a warp's 16 rows leave from
+// there: as one copy if all of them are the segment's, row by row where it ends among them.
+__device__ int g_expand_status = 0;                    // GPD_ERR_TIMEOUT if a bounded wait expired
+
+template <typename O, int KT, bool TRANS>
+struct TmaShape {
+    static constexpr int TM = 64, RP = 16 * KT, STAGES = KT == 8 && sizeof(O) == 4 ? 3 : 4;
+    static constexpr int BOX = 128 / sizeof(O), BOXES = kCols / BOX;   // columns of a box of 128 bytes
+    using W = WTile<TRANS ? RP : kCols, TRANS ? kCols : RP>;
+    static constexpr int BASE = TM * 128 * BOXES, STAGE = BASE + W::BYTES, SMEM = STAGES * STAGE + 1024;
+};
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t from, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(from), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+template <typename T, typename O, int KT, int PARTS, bool TRANS>
+__global__ void __launch_bounds__(kThreads + 32) expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_base,
+                                                                   const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ExpandArgs a) {
+    using S = TmaShape<O, KT, TRANS>;
+    extern __shared__ unsigned char raw[];
+    __shared__ Ring<S::STAGES> ring;
+    unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    if (threadIdx.x == 0) ring.init(a.w_vec ? 1 : 33, 4);
+    after_previous();
+    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x);
+    if (tile.rows == 0) return;
+    const bool none = tile.id < 0 || tile.id >= a.seg.n;
+    if (tile.id < 0 && a.base == a.out) return;
+    const int64_t chunks = (a.C + kCols - 1) / kCols, from = chunks * blockIdx.y / gridDim.y;
+    const int n = (int)(chunks * (blockIdx.y + 1) / gridDim.y - from);
+    if (!a.w_vec) {                                    // columns and rows of W that do not exist
+        for (int i = threadIdx.x; i < S::STAGES * S::STAGE / 16; i += kThreads + 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    if (warp == kThreads / 32) {
+        int k = 0;
+        const uint32_t bytes = (a.base ? S::BASE : 0) + (none || !a.w_vec ? 0 : S::W::BYTES);
+        for (; k < n && ring.wait_empty(k, &g_expand_status); ++k) {
+            unsigned char *at = smem + k % S::STAGES * S::STAGE, *ws = at + S::BASE;
+            const int64_t c = (from + k) * kCols;
+            uint64_t* bar = &ring.full[k % S::STAGES];
+            if (lane == 0) {
+                if (bytes) tc::mbar_expect_tx(bar, bytes);
+                else tc::mbar_arrive(bar);
+                if (a.base)
+#pragma unroll
+                    for (int i = 0; i < S::BOXES; ++i) tc::tma_load_3d(at + i * S::TM * 128, &map_base, (int)c + i * S::BOX, (int)tile.row, 0, bar);
+                if (!none && a.w_vec) S::W::load(ws, &map_w, TRANS ? (int)c : 0, TRANS ? 0 : (int)c, (int)tile.id, bar);
+            }
+            if (!a.w_vec) {
+                if (!none) {
+                    const T* w = static_cast<const T*>(a.w) + tile.id * a.next + (TRANS ? c : c * a.ldw);
+                    if (TRANS) S::W::copy(ws, w, a.ldw, a.r, a.C - c, a.r, kCols);
+                    else S::W::copy(ws, w, a.ldw, a.C - c, a.r, kCols, a.r);
+                }
+                tc::mbar_arrive(bar);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) ring.drain(k, &g_expand_status);
+        return;
+    }
+    const int row0 = 16 * warp + g;
+    const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows}, whole = 16 * warp + 16 <= tile.rows, any = 16 * warp < tile.rows;
+    uint32_t ha[PARTS][KT][4];
+    float undo[2];
+    load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
+    const float nothing = tile.id >= a.seg.n ? __int_as_float(0x7fffffff) : 0.f;
+    for (int k = 0; k < n && ring.wait_full(k, &g_expand_status); ++k) {
+        const uint32_t at = smem_at(smem + k % S::STAGES * S::STAGE), ws = at + S::BASE, mine = at + 16 * warp * 128;
+        if (any) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {              // 16 columns
+                float acc[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = nothing;
+                if (!none) {
+#pragma unroll
+                    for (int s = 0; s < KT; ++s) {
+                        uint32_t b[4];
+                        if (TRANS) ldmatrix4<true>(b, ws + S::W::at(16 * s + (lane & 15), 16 * p + (lane >> 4) * 8));
+                        else ldmatrix4<false>(b, ws + S::W::at(16 * p + (lane & 7) + (lane >> 4) * 8, 16 * s + (lane >> 3 & 1) * 8));
+#pragma unroll
+                        for (int i = PARTS - 1; i >= 0; --i) {         // the small parts first
+                            mma(acc[0], ha[i][s], b[0], b[1], T());
+                            mma(acc[1], ha[i][s], b[2], b[3], T());
+                        }
+                    }
+                    if (std::is_same<T, __half>::value) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[i][j] *= undo[j >> 1];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {      // row g + 8 j, columns c and c + 1
+                        const int c = 16 * p + 8 * i + 2 * q;
+                        const uint32_t to = mine + c / S::BOX * S::TM * 128 + swizzled<128>((g + 8 * j) * 128 + c % S::BOX * (int)sizeof(O));
+                        if constexpr (sizeof(O) == 4) {
+                            float x = 0.f, y = 0.f;
+                            if (a.base) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(to) : "memory");
+                            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x + acc[i][2 * j]), "f"(y + acc[i][2 * j + 1]) : "memory");
+                        } else {
+                            uint32_t w = 0;
+                            if (a.base) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(to) : "memory");
+                            const float2 f = unpack2(w, O());
+                            w = pack2(f.x + acc[i][2 * j], f.y + acc[i][2 * j + 1], O());
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(w) : "memory");
+                        }
+                    }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            const int64_t c0 = (from + k) * kCols;
+            if (whole) {
+                if (lane == 0) {
+#pragma unroll
+                    for (int i = 0; i < S::BOXES; ++i)
+                        if (c0 + i * S::BOX < a.C) tma_store_3d(&map_out, mine + i * S::TM * 128, (int)c0 + i * S::BOX, (int)tile.row + 16 * warp, 0);
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < S::BOXES; ++b)
+                    for (int i = lane; i < 128; i += 32) {             // a row's pieces of 16 bytes
+                        const int r = i >> 3;
+                        const int64_t c = c0 + b * S::BOX + (i & 7) * (16 / (int)sizeof(O));
+                        if (16 * warp + r >= tile.rows || c >= a.C) continue;
+                        uint4 v;
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                                     : "r"(mine + b * S::TM * 128 + swizzled<128>(r * 128 + (i & 7) * 16)) : "memory");
+                        O* p = static_cast<O*>(a.out) + (tile.row + 16 * warp + r) * a.ldo + c;
+                        if (c + 16 / (int)sizeof(O) <= a.C) {
+                            *reinterpret_cast<uint4*>(p) = v;
+                        } else {
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int j = 0; j < 16 / (int)sizeof(O); ++j)
+                                if (c + j < a.C) {
+                                    if constexpr (sizeof(O) == 4) p[j] = __uint_as_float(w[j]);
+                                    else reinterpret_cast<unsigned short*>(p)[j] = (unsigned short)(w[j / 2] >> (16 * (j & 1)));
+                                }
+                        }
+                    }
+            }
+        }
+        // the stage before this one is free once its copy has left
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && k > 0) tc::mbar_arrive(&ring.empty[(k - 1) % S::STAGES]);
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+template <typename T, typename O, int KT, int PARTS, bool TRANS>
+gpd_status launch_tma(const ExpandArgs& a, cudaStream_t st) {
+    using S = TmaShape<O, KT, TRANS>;
+    const int64_t tiles = tiles_of(a.seg, S::TM), chunks = (a.C + kCols - 1) / kCols;
+    if (tiles > 0x7fffffff) return GPD_ERR_SHAPE;
+    int64_t splits = (8 * sm_count() + tiles - 1) / tiles;
+    splits = std::max<int64_t>(1, std::min({splits, chunks, (int64_t)65535}));
+    CUtensorMap map_w, map_base, map_out;
+    if (!make_map(&map_out, a.out, sizeof(O), 1, a.seg.T, a.C, a.ldo, 0, 16, S::BOX)) return GPD_ERR_CUDA;
+    map_w = map_base = map_out;                        // where they are not used
+    if (a.base && !make_map(&map_base, a.base, sizeof(O), 1, a.seg.T, a.C, a.ldb, 0, S::TM, S::BOX)) return GPD_ERR_CUDA;
+    if (a.w_vec && a.seg.n > 0) {
+        const bool ok = TRANS ? make_map(&map_w, a.w, 2, a.seg.n, a.r, a.C, a.ldw, a.next, S::RP, kCols)
+                              : make_map(&map_w, a.w, 2, a.seg.n, a.C, a.r, a.ldw, a.next, kCols, S::W::PITCH / 2);
+        if (!ok) return GPD_ERR_CUDA;
+    }
+    auto kernel = expand_tma_kernel<T, O, KT, PARTS, TRANS>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_after(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads + 32), S::SMEM, 1, st, map_w, map_base, map_out, a);
+}
 template <typename T, typename O, int KT, bool TRANS>
 gpd_status launch_rows(const ExpandArgs& a, cudaStream_t st) {
     constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
-    return a.seg.T <= 16 * (int64_t)a.seg.S ? launch<T, O, KT, PARTS, 1, TRANS>(a, st) : launch<T, O, KT, PARTS, 4, TRANS>(a, st);
+    if (a.seg.T <= 16 * (int64_t)a.seg.S) return launch<T, O, KT, PARTS, 1, TRANS>(a, st);
+    return a.tma ? launch_tma<T, O, KT, PARTS, TRANS>(a, st) : launch<T, O, KT, PARTS, 4, TRANS>(a, st);
 }
 template <typename T, typename O, bool TRANS>
 gpd_status launch_rank(const ExpandArgs& a, cudaStream_t st) {
@@ -268,6 +455,13 @@ gpd_status launch_type(int out_type, bool transposed, const ExpandArgs& a, cudaS
 }
 
 }  // namespace
+
+int expand_status_fetch_and_clear() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_expand_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
+    if (v != 0) cudaMemcpyToSymbol(g_expand_status, &zero, sizeof(int));
+    return v;
+}
 
 gpd_status expand(int type, int out_type, bool transposed, const ExpandArgs& a, cudaStream_t st) {
     return type == GPD_DT_BF16 ? launch_type<__nv_bfloat16>(out_type, transposed, a, st) : launch_type<__half>(out_type, transposed, a, st);

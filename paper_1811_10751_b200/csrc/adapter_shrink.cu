@@ -135,10 +135,149 @@ gpd_status launch(const ShrinkArgs& a, cudaStream_t st) {
     if (S::SMEM > 49152 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
     return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), S::SMEM, splits, st, a, splits);
 }
+// ---- the same with tiles by TMA: many rows, x on 16-byte boundaries --------------------------------------------
+__device__ int g_shrink_status = 0;                    // GPD_ERR_TIMEOUT if a bounded wait expired
+
+template <int NT, bool TRANS>
+struct TmaShape {
+    static constexpr int TM = 64, RP = 8 * NT, STAGES = NT <= 4 ? 6 : 4, X_BYTES = TM * 128;
+    using W = WTile<TRANS ? kDeep : RP, TRANS ? RP : kDeep>;
+    static constexpr int STAGE = X_BYTES + W::BYTES, SUMS = TM * RP * 4;
+    static constexpr int SMEM = (STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS) + 1024;
+};
+
+// Four warps with 16 rows each, and one that issues the copies.
+template <typename T, int NT, bool TRANS>
+__global__ void __launch_bounds__(kThreads + 32) shrink_tma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                                                                   const __grid_constant__ ShrinkArgs a, int splits) {
+    using S = TmaShape<NT, TRANS>;
+    extern __shared__ unsigned char raw[];
+    __shared__ Ring<S::STAGES> ring;
+    unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
+    const int rank = blockIdx.x % splits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) ring.init(a.w_vec ? 1 : 33, 4);
+    after_previous();
+    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x / splits);
+    if (tile.rows == 0) return;                        // the whole cluster
+    float* out = a.h + tile.row * a.r;
+    if (tile.id < 0 || tile.id >= a.seg.n) {
+        const float v = tile.id < 0 ? 0.f : __int_as_float(0x7fffffff);
+        if (rank == 0)
+            for (int i = threadIdx.x; i < tile.rows * a.r; i += kThreads + 32) out[i] = v;
+        return;
+    }
+    const int64_t stages = (a.C + kDeep - 1) / kDeep;
+    const int64_t from = stages * rank / splits;
+    const int n = (int)(stages * (rank + 1) / splits - from);
+    if (!a.w_vec)                                      // columns and rows of W that do not exist
+        for (int i = threadIdx.x; i < S::STAGES * S::STAGE / 16; i += kThreads + 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    if (!a.w_vec) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    float sum[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[i][j] = 0.f;
+    if (warp == kThreads / 32) {
+        int k = 0;
+        for (; k < n && ring.wait_empty(k, &g_shrink_status); ++k) {
+            unsigned char* at = smem + k % S::STAGES * S::STAGE;
+            const int64_t c = (from + k) * kDeep;
+            uint64_t* bar = &ring.full[k % S::STAGES];
+            if (lane == 0) {
+                tc::mbar_expect_tx(bar, S::X_BYTES + (a.w_vec ? S::W::BYTES : 0));
+                tc::tma_load_3d(at, &map_x, (int)c, (int)tile.row, 0, bar);
+                if (a.w_vec) S::W::load(at + S::X_BYTES, &map_w, TRANS ? 0 : (int)c, TRANS ? (int)c : 0, (int)tile.id, bar);
+            }
+            if (!a.w_vec) {
+                const T* w = static_cast<const T*>(a.w) + tile.id * a.next + (TRANS ? c * a.ldw : c);
+                if (TRANS) S::W::copy(at + S::X_BYTES, w, a.ldw, a.C - c, a.r, kDeep, a.r);
+                else S::W::copy(at + S::X_BYTES, w, a.ldw, a.r, a.C - c, a.r, kDeep);
+                tc::mbar_arrive(bar);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) ring.drain(k, &g_shrink_status);
+    } else {
+        const int row = 16 * warp + (lane & 15);
+        for (int k = 0; k < n && ring.wait_full(k, &g_shrink_status); ++k) {
+            const uint32_t xs = smem_at(smem + k % S::STAGES * S::STAGE), ws = xs + S::X_BYTES;
+            float acc[NT][4];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < kDeep / 16; ++ks) {
+                uint32_t xa[4];
+                ldmatrix4<false>(xa, xs + swizzled<128>(row * 128 + 32 * ks + (lane >> 4) * 16));
+#pragma unroll
+                for (int p = 0; p < NT / 2; ++p) {
+                    uint32_t b[4];
+                    if (TRANS) ldmatrix4<true>(b, ws + S::W::at(16 * ks + (lane & 15), 16 * p + (lane >> 4) * 8));
+                    else ldmatrix4<false>(b, ws + S::W::at(16 * p + (lane & 7) + (lane >> 4) * 8, 16 * ks + (lane >> 3 & 1) * 8));
+                    mma(acc[2 * p], xa, b[0], b[1], T());
+                    mma(acc[2 * p + 1], xa, b[2], b[3], T());
+                }
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&ring.empty[k % S::STAGES]);
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[i][j] += acc[i][j];
+        }
+    }
+    __syncthreads();                                   // every stage has been read
+    float* sums = reinterpret_cast<float*>(smem);
+    if (warp < kThreads / 32) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            float* s = sums + (16 * warp + (lane >> 2)) * S::RP + 8 * i + 2 * (lane & 3);
+            *reinterpret_cast<float2*>(s) = make_float2(sum[i][0], sum[i][1]);
+            *reinterpret_cast<float2*>(s + 8 * S::RP) = make_float2(sum[i][2], sum[i][3]);
+        }
+    }
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    if (splits > 1) cluster.sync();
+    else __syncthreads();
+    const float scale = a.scale ? a.scale[tile.id] : 1.f;
+    for (int e = rank * (kThreads + 32) + threadIdx.x; e < S::TM * S::RP; e += splits * (kThreads + 32)) {
+        const int r = e / S::RP, c = e % S::RP;
+        if (r >= tile.rows || c >= a.r) continue;
+        float v = 0.f;
+        for (int s = 0; s < splits; ++s) v += (splits > 1 ? cluster.map_shared_rank(sums, s) : sums)[e];
+        out[(int64_t)r * a.r + c] = v * scale;
+    }
+    if (splits > 1) cluster.sync();                    // the others have read this CTA's sums
+}
+
+template <typename T, int NT, bool TRANS>
+gpd_status launch_tma(const ShrinkArgs& a, cudaStream_t st) {
+    using S = TmaShape<NT, TRANS>;
+    const int64_t tiles = tiles_of(a.seg, S::TM), stages = (a.C + kDeep - 1) / kDeep;
+    int splits = 1;                                    // until two CTAs per SM are busy, but four stages each at least
+    while (splits < 8 && tiles * splits < 2 * sm_count() && stages >= 8 * splits) splits *= 2;
+    if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
+    CUtensorMap map_x, map_w;
+    if (!make_map(&map_x, a.x, 2, 1, a.seg.T, a.C, a.ldx, 0, S::TM, kDeep)) return GPD_ERR_CUDA;
+    if (a.w_vec && a.seg.n > 0) {
+        const bool ok = TRANS ? make_map(&map_w, a.w, 2, a.seg.n, a.C, a.r, a.ldw, a.next, kDeep, S::W::PITCH / 2)
+                              : make_map(&map_w, a.w, 2, a.seg.n, a.r, a.C, a.ldw, a.next, S::RP, kDeep);
+        if (!ok) return GPD_ERR_CUDA;
+    } else {
+        map_w = map_x;                                 // not used
+    }
+    auto kernel = shrink_tma_kernel<T, NT, TRANS>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads + 32), S::SMEM, splits, st, map_x, map_w, a, splits);
+}
+
 template <typename T, int NT, bool TRANS>
 gpd_status launch_rows(const ShrinkArgs& a, cudaStream_t st) {
     // Segments of 16 rows and less on average: tiles of 16 rows.
-    return a.seg.T <= 16 * (int64_t)a.seg.S ? launch<T, NT, 1, TRANS>(a, st) : launch<T, NT, 4, TRANS>(a, st);
+    if (a.seg.T <= 16 * (int64_t)a.seg.S) return launch<T, NT, 1, TRANS>(a, st);
+    return a.x_vec ? launch_tma<T, NT, TRANS>(a, st) : launch<T, NT, 4, TRANS>(a, st);
 }
 template <typename T, bool TRANS>
 gpd_status launch_rank(const ShrinkArgs& a, cudaStream_t st) {
@@ -148,6 +287,13 @@ gpd_status launch_rank(const ShrinkArgs& a, cudaStream_t st) {
 }
 
 }  // namespace
+
+int shrink_status_fetch_and_clear() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_shrink_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
+    if (v != 0) cudaMemcpyToSymbol(g_shrink_status, &zero, sizeof(int));
+    return v;
+}
 
 gpd_status shrink(int type, bool transposed, const ShrinkArgs& a, cudaStream_t st) {
     if (type == GPD_DT_BF16) return transposed ? launch_rank<__nv_bfloat16, true>(a, st) : launch_rank<__nv_bfloat16, false>(a, st);
