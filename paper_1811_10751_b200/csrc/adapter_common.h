@@ -34,6 +34,19 @@ __device__ __forceinline__ int64_t offset_at(const Segments& s, int64_t i) {
     const int64_t v = number(s.offsets, i, s.wide);
     return v < 0 ? 0 : v > s.T ? s.T : v;              // whatever stands there, rows stay inside the batch
 }
+// How many tiles of TM rows the segments have.  Every warp works it out by itself.
+template <int TM>
+__device__ __forceinline__ int64_t count_tiles(const Segments& s) {
+    int64_t n = 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x & 31; i < s.S; i += 32) {
+        const int64_t rows = offset_at(s, i + 1) - offset_at(s, i);
+        if (rows > 0) n += (rows + TM - 1) / TM;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+    return n;
+}
 // Tile number `tile` of the segments' tiles of TM rows.  Every warp works it out by itself: 128 segments per round.
 template <int TM>
 __device__ __forceinline__ RowTile find_tile(const Segments& s, int64_t tile) {
@@ -93,6 +106,9 @@ __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
     else
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void stmatrix4(const uint32_t (&r)[4], uint32_t at) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -164,6 +180,7 @@ struct Ring {
                 tc::mbar_wait(&full[k % STAGES], (k / STAGES) & 1, &never, status);
     }
 };
+constexpr int per_sm(int smem) { return 227 * 1024 / (smem + 1536) < 5 ? 227 * 1024 / (smem + 1536) : 5; }     // CTAs that shared memory has room for
 // Byte of a tile whose rows are PITCH (32, 64 or 128) bytes, as TMA's swizzle of that width places it (the tile starts on a
 // 1024-byte boundary): eight rows' pieces of 16 bytes at one column lie in different banks.
 template <int PITCH>

@@ -270,159 +270,189 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t fr
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(from), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
+// The CTAs share out the (tile, chunk of columns) pairs in contiguous runs of equal length.  Four warps have 16 rows of a tile
+// each, one issues the copies.
 template <typename T, typename O, int KT, int PARTS, bool TRANS>
-__global__ void __launch_bounds__(kThreads + 32) expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_base,
-                                                                   const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ExpandArgs a) {
+__global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<O, KT, TRANS>::SMEM))
+expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_base, const __grid_constant__ CUtensorMap map_out,
+                  const __grid_constant__ ExpandArgs a) {
     using S = TmaShape<O, KT, TRANS>;
     extern __shared__ unsigned char raw[];
     __shared__ Ring<S::STAGES> ring;
     unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) ring.init(a.w_vec ? 1 : 33, 4);
     after_previous();
-    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x);
-    if (tile.rows == 0) return;
-    const bool none = tile.id < 0 || tile.id >= a.seg.n;
-    if (tile.id < 0 && a.base == a.out) return;
-    const int64_t chunks = (a.C + kCols - 1) / kCols, from = chunks * blockIdx.y / gridDim.y;
-    const int n = (int)(chunks * (blockIdx.y + 1) / gridDim.y - from);
     if (!a.w_vec) {                                    // columns and rows of W that do not exist
         for (int i = threadIdx.x; i < S::STAGES * S::STAGE / 16; i += kThreads + 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    if (warp == kThreads / 32) {
-        int k = 0;
-        const uint32_t bytes = (a.base ? S::BASE : 0) + (none || !a.w_vec ? 0 : S::W::BYTES);
-        for (; k < n && ring.wait_empty(k, &g_expand_status); ++k) {
-            unsigned char *at = smem + k % S::STAGES * S::STAGE, *ws = at + S::BASE;
-            const int64_t c = (from + k) * kCols;
-            uint64_t* bar = &ring.full[k % S::STAGES];
-            if (lane == 0) {
-                if (bytes) tc::mbar_expect_tx(bar, bytes);
-                else tc::mbar_arrive(bar);
-                if (a.base)
-#pragma unroll
-                    for (int i = 0; i < S::BOXES; ++i) tc::tma_load_3d(at + i * S::TM * 128, &map_base, (int)c + i * S::BOX, (int)tile.row, 0, bar);
-                if (!none && a.w_vec) S::W::load(ws, &map_w, TRANS ? (int)c : 0, TRANS ? 0 : (int)c, (int)tile.id, bar);
-            }
-            if (!a.w_vec) {
-                if (!none) {
-                    const T* w = static_cast<const T*>(a.w) + tile.id * a.next + (TRANS ? c : c * a.ldw);
-                    if (TRANS) S::W::copy(ws, w, a.ldw, a.r, a.C - c, a.r, kCols);
-                    else S::W::copy(ws, w, a.ldw, a.C - c, a.r, kCols, a.r);
-                }
-                tc::mbar_arrive(bar);
-            }
-        }
-        __syncwarp();
-        if (lane == 0) ring.drain(k, &g_expand_status);
-        return;
-    }
-    const int row0 = 16 * warp + g;
-    const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows}, whole = 16 * warp + 16 <= tile.rows, any = 16 * warp < tile.rows;
-    uint32_t ha[PARTS][KT][4];
-    float undo[2];
-    load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
-    const float nothing = tile.id >= a.seg.n ? __int_as_float(0x7fffffff) : 0.f;
-    for (int k = 0; k < n && ring.wait_full(k, &g_expand_status); ++k) {
-        const uint32_t at = smem_at(smem + k % S::STAGES * S::STAGE), ws = at + S::BASE, mine = at + 16 * warp * 128;
-        if (any) {
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {              // 16 columns
-                float acc[2][4];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = nothing;
-                if (!none) {
-#pragma unroll
-                    for (int s = 0; s < KT; ++s) {
-                        uint32_t b[4];
-                        if (TRANS) ldmatrix4<true>(b, ws + S::W::at(16 * s + (lane & 15), 16 * p + (lane >> 4) * 8));
-                        else ldmatrix4<false>(b, ws + S::W::at(16 * p + (lane & 7) + (lane >> 4) * 8, 16 * s + (lane >> 3 & 1) * 8));
-#pragma unroll
-                        for (int i = PARTS - 1; i >= 0; --i) {         // the small parts first
-                            mma(acc[0], ha[i][s], b[0], b[1], T());
-                            mma(acc[1], ha[i][s], b[2], b[3], T());
-                        }
-                    }
-                    if (std::is_same<T, __half>::value) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[i][j] *= undo[j >> 1];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {      // row g + 8 j, columns c and c + 1
-                        const int c = 16 * p + 8 * i + 2 * q;
-                        const uint32_t to = mine + c / S::BOX * S::TM * 128 + swizzled<128>((g + 8 * j) * 128 + c % S::BOX * (int)sizeof(O));
-                        if constexpr (sizeof(O) == 4) {
-                            float x = 0.f, y = 0.f;
-                            if (a.base) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(to) : "memory");
-                            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x + acc[i][2 * j]), "f"(y + acc[i][2 * j + 1]) : "memory");
-                        } else {
-                            uint32_t w = 0;
-                            if (a.base) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(to) : "memory");
-                            const float2 f = unpack2(w, O());
-                            w = pack2(f.x + acc[i][2 * j], f.y + acc[i][2 * j + 1], O());
-                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(w) : "memory");
-                        }
-                    }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            const int64_t c0 = (from + k) * kCols;
-            if (whole) {
+    const int64_t chunks = (a.C + kCols - 1) / kCols, all = count_tiles<S::TM>(a.seg) * chunks;
+    const int64_t last = all * (blockIdx.x + 1) / gridDim.x;
+    int k = 0;                                         // stages so far
+    for (int64_t at = all * blockIdx.x / gridDim.x, end; at < last; at = end) {
+        const int64_t number = at / chunks;
+        end = min(last, (number + 1) * chunks);
+        const int first = (int)(at - number * chunks), n = (int)(end - at);
+        const RowTile tile = find_tile<S::TM>(a.seg, number);
+        const bool none = tile.id < 0 || tile.id >= a.seg.n;
+        if (tile.id < 0 && a.base == a.out) continue;
+        if (warp == kThreads / 32) {
+            const uint32_t bytes = (a.base ? S::BASE : 0) + (none || !a.w_vec ? 0 : S::W::BYTES);
+            for (int i = 0; i < n; ++i, ++k) {
+                if (!ring.wait_empty(k, &g_expand_status)) break;
+                unsigned char *stage = smem + k % S::STAGES * S::STAGE, *ws = stage + S::BASE;
+                const int c = (first + i) * kCols;
+                uint64_t* bar = &ring.full[k % S::STAGES];
                 if (lane == 0) {
+                    if (bytes) tc::mbar_expect_tx(bar, bytes);
+                    else tc::mbar_arrive(bar);
+                    if (a.base)
 #pragma unroll
-                    for (int i = 0; i < S::BOXES; ++i)
-                        if (c0 + i * S::BOX < a.C) tma_store_3d(&map_out, mine + i * S::TM * 128, (int)c0 + i * S::BOX, (int)tile.row + 16 * warp, 0);
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        for (int j = 0; j < S::BOXES; ++j) tc::tma_load_3d(stage + j * S::TM * 128, &map_base, c + j * S::BOX, (int)tile.row, 0, bar);
+                    if (!none && a.w_vec) S::W::load(ws, &map_w, TRANS ? c : 0, TRANS ? 0 : c, (int)tile.id, bar);
                 }
-            } else {
+                if (!a.w_vec) {
+                    if (!none) {
+                        const T* w = static_cast<const T*>(a.w) + tile.id * a.next + (TRANS ? c : c * a.ldw);
+                        if (TRANS) S::W::copy(ws, w, a.ldw, a.r, a.C - c, a.r, kCols);
+                        else S::W::copy(ws, w, a.ldw, a.C - c, a.r, kCols, a.r);
+                    }
+                    tc::mbar_arrive(bar);
+                }
+            }
+            __syncwarp();
+            if (*static_cast<volatile int*>(&ring.abort)) break;
+            continue;
+        }
+        const int g = lane >> 2, q = lane & 3, row0 = 16 * warp + g;
+        const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows}, whole = 16 * warp + 16 <= tile.rows, any = 16 * warp < tile.rows;
+        uint32_t ha[PARTS][KT][4];
+        float undo[2];
+        load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
+        for (int i = 0; i < n; ++i, ++k) {
+            if (!ring.wait_full(k, &g_expand_status)) break;
+            const uint32_t stage = smem_at(smem + k % S::STAGES * S::STAGE), ws = stage + S::BASE, mine = stage + 16 * warp * 128;
+            if (any) {
 #pragma unroll
-                for (int b = 0; b < S::BOXES; ++b)
-                    for (int i = lane; i < 128; i += 32) {             // a row's pieces of 16 bytes
-                        const int r = i >> 3;
-                        const int64_t c = c0 + b * S::BOX + (i & 7) * (16 / (int)sizeof(O));
-                        if (16 * warp + r >= tile.rows || c >= a.C) continue;
-                        uint4 v;
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                                     : "r"(mine + b * S::TM * 128 + swizzled<128>(r * 128 + (i & 7) * 16)) : "memory");
-                        O* p = static_cast<O*>(a.out) + (tile.row + 16 * warp + r) * a.ldo + c;
-                        if (c + 16 / (int)sizeof(O) <= a.C) {
-                            *reinterpret_cast<uint4*>(p) = v;
-                        } else {
-                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                for (int p = 0; p < 4; ++p) {          // 16 columns
+                    // the sums begin with base where the result has 16 bits, whose rounding hides the tensor cores' truncation
+                    constexpr bool kOnBase = sizeof(O) == 2 && std::is_same<T, __nv_bfloat16>::value;
+                    float acc[2][4], own[2][4];        // [8 columns][row g: 2 q, 2 q + 1; row g + 8]
+                    const uint32_t block = mine + swizzled<128>((lane & 15) * 128 + 32 * p + (lane >> 4) * 16);
+                    uint32_t b16[4] = {0, 0, 0, 0};
+                    if (sizeof(O) == 2) {
+                        if (a.base) ldmatrix4<false>(b16, block);
 #pragma unroll
-                            for (int j = 0; j < 16 / (int)sizeof(O); ++j)
-                                if (c + j < a.C) {
-                                    if constexpr (sizeof(O) == 4) p[j] = __uint_as_float(w[j]);
-                                    else reinterpret_cast<unsigned short*>(p)[j] = (unsigned short)(w[j / 2] >> (16 * (j & 1)));
-                                }
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 f = unpack2(b16[j], T());
+                            own[j >> 1][2 * (j & 1)] = f.x;
+                            own[j >> 1][2 * (j & 1) + 1] = f.y;
                         }
                     }
+#pragma unroll
+                    for (int i2 = 0; i2 < 2; ++i2)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[i2][j] = kOnBase ? own[i2][j] : 0.f;
+                    if (!none) {
+#pragma unroll
+                        for (int s = 0; s < KT; ++s) {
+                            uint32_t b[4];
+                            if (TRANS) ldmatrix4<true>(b, ws + S::W::at(16 * s + (lane & 15), 16 * p + (lane >> 4) * 8));
+                            else ldmatrix4<false>(b, ws + S::W::at(16 * p + (lane & 7) + (lane >> 4) * 8, 16 * s + (lane >> 3 & 1) * 8));
+#pragma unroll
+                            for (int i2 = PARTS - 1; i2 >= 0; --i2) {  // the small parts first
+                                mma(acc[0], ha[i2][s], b[0], b[1], T());
+                                mma(acc[1], ha[i2][s], b[2], b[3], T());
+                            }
+                        }
+                    } else if (tile.id >= 0) {         // there is no such adapter
+#pragma unroll
+                        for (int i2 = 0; i2 < 2; ++i2)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[i2][j] = __int_as_float(0x7fffffff);
+                    }
+                    if constexpr (sizeof(O) == 2) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float x = acc[j >> 1][2 * (j & 1)], y = acc[j >> 1][2 * (j & 1) + 1];
+                            if (!kOnBase) {
+                                x = fmaf(x, undo[j & 1], own[j >> 1][2 * (j & 1)]);
+                                y = fmaf(y, undo[j & 1], own[j >> 1][2 * (j & 1) + 1]);
+                            }
+                            b16[j] = pack2(x, y, O());
+                        }
+                        stmatrix4(b16, block);
+                    } else {
+#pragma unroll
+                        for (int i2 = 0; i2 < 2; ++i2)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {              // row g + 8 j, columns c and c + 1
+                                const int c = 16 * p + 8 * i2 + 2 * q;
+                                const uint32_t to = mine + c / S::BOX * S::TM * 128 + swizzled<128>((g + 8 * j) * 128 + c % S::BOX * 4);
+                                float x = 0.f, y = 0.f;
+                                if (a.base) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(to) : "memory");
+                                x = fmaf(acc[i2][2 * j], undo[j], x);
+                                y = fmaf(acc[i2][2 * j + 1], undo[j], y);
+                                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
+                            }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                const int64_t c0 = (int64_t)(first + i) * kCols;
+                if (whole) {
+                    if (lane == 0) {
+#pragma unroll
+                        for (int j = 0; j < S::BOXES; ++j)
+                            if (c0 + j * S::BOX < a.C) tma_store_3d(&map_out, mine + j * S::TM * 128, (int)c0 + j * S::BOX, (int)tile.row + 16 * warp, 0);
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < S::BOXES; ++b)
+                        for (int j = lane; j < 128; j += 32) {         // a row's pieces of 16 bytes
+                            const int r = j >> 3;
+                            const int64_t c = c0 + b * S::BOX + (j & 7) * (16 / (int)sizeof(O));
+                            if (16 * warp + r >= tile.rows || c >= a.C) continue;
+                            uint4 v;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                                         : "r"(mine + b * S::TM * 128 + swizzled<128>(r * 128 + (j & 7) * 16)) : "memory");
+                            O* p = static_cast<O*>(a.out) + (tile.row + 16 * warp + r) * a.ldo + c;
+                            if (c + 16 / (int)sizeof(O) <= a.C) {
+                                *reinterpret_cast<uint4*>(p) = v;
+                            } else {
+                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                for (int e = 0; e < 16 / (int)sizeof(O); ++e)
+                                    if (c + e < a.C) {
+                                        if constexpr (sizeof(O) == 4) p[e] = __uint_as_float(w[e]);
+                                        else reinterpret_cast<unsigned short*>(p)[e] = (unsigned short)(w[e / 2] >> (16 * (e & 1)));
+                                    }
+                            }
+                        }
+                }
             }
+            // the stage before this one is free once its copy has left
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && k > 0) tc::mbar_arrive(&ring.empty[(k - 1) % S::STAGES]);
         }
-        // the stage before this one is free once its copy has left
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-        __syncwarp();
-        if (lane == 0 && k > 0) tc::mbar_arrive(&ring.empty[(k - 1) % S::STAGES]);
+        if (*static_cast<volatile int*>(&ring.abort)) break;
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (warp == kThreads / 32) {
+        if (lane == 0) ring.drain(k, &g_expand_status);
+    } else if (lane == 0) {
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
 }
 
 template <typename T, typename O, int KT, int PARTS, bool TRANS>
 gpd_status launch_tma(const ExpandArgs& a, cudaStream_t st) {
     using S = TmaShape<O, KT, TRANS>;
     const int64_t tiles = tiles_of(a.seg, S::TM), chunks = (a.C + kCols - 1) / kCols;
-    if (tiles > 0x7fffffff) return GPD_ERR_SHAPE;
-    int64_t splits = (8 * sm_count() + tiles - 1) / tiles;
-    splits = std::max<int64_t>(1, std::min({splits, chunks, (int64_t)65535}));
+    const int64_t ctas = std::min<int64_t>(tiles * chunks, (int64_t)per_sm(S::SMEM) * sm_count());
     CUtensorMap map_w, map_base, map_out;
     if (!make_map(&map_out, a.out, sizeof(O), 1, a.seg.T, a.C, a.ldo, 0, 16, S::BOX)) return GPD_ERR_CUDA;
     map_w = map_base = map_out;                        // where they are not used
@@ -434,7 +464,7 @@ gpd_status launch_tma(const ExpandArgs& a, cudaStream_t st) {
     }
     auto kernel = expand_tma_kernel<T, O, KT, PARTS, TRANS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
-    return launch_after(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(kThreads + 32), S::SMEM, 1, st, map_w, map_base, map_out, a);
+    return launch_after(kernel, dim3((unsigned)ctas), dim3(kThreads + 32), S::SMEM, 1, st, map_w, map_base, map_out, a);
 }
 template <typename T, typename O, int KT, bool TRANS>
 gpd_status launch_rows(const ExpandArgs& a, cudaStream_t st) {

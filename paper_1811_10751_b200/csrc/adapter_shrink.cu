@@ -6,6 +6,8 @@
 // ring of asynchronous copies.
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "adapter_common.h"
 
 namespace gpd {
@@ -140,7 +142,7 @@ __device__ int g_shrink_status = 0;                    // GPD_ERR_TIMEOUT if a b
 
 template <int NT, bool TRANS>
 struct TmaShape {
-    static constexpr int TM = 64, RP = 8 * NT, STAGES = NT <= 4 ? 6 : 4, X_BYTES = TM * 128;
+    static constexpr int TM = 64, RP = 8 * NT, STAGES = 4, X_BYTES = TM * 128;
     using W = WTile<TRANS ? kDeep : RP, TRANS ? RP : kDeep>;
     static constexpr int STAGE = X_BYTES + W::BYTES, SUMS = TM * RP * 4;
     static constexpr int SMEM = (STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS) + 1024;
@@ -148,7 +150,7 @@ struct TmaShape {
 
 // Four warps with 16 rows each, and one that issues the copies.
 template <typename T, int NT, bool TRANS>
-__global__ void __launch_bounds__(kThreads + 32) shrink_tma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+__global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SMEM)) shrink_tma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                                                                    const __grid_constant__ ShrinkArgs a, int splits) {
     using S = TmaShape<NT, TRANS>;
     extern __shared__ unsigned char raw[];
@@ -256,8 +258,17 @@ template <typename T, int NT, bool TRANS>
 gpd_status launch_tma(const ShrinkArgs& a, cudaStream_t st) {
     using S = TmaShape<NT, TRANS>;
     const int64_t tiles = tiles_of(a.seg, S::TM), stages = (a.C + kDeep - 1) / kDeep;
-    int splits = 1;                                    // until two CTAs per SM are busy, but four stages each at least
-    while (splits < 8 && tiles * splits < 2 * sm_count() && stages >= 8 * splits) splits *= 2;
+    // The parts of a tile's columns with which the busiest SM is done first, a CTA costing about six stages beside its own:
+    // an SM that has one CTA more than the others holds all up.
+    int splits = 1;
+    int64_t best = 0;
+    for (int s = 1; s <= 8; s *= 2) {
+        const int64_t per = (tiles * s + sm_count() - 1) / sm_count(), time = std::max<int64_t>(per, 2) * ((stages + s - 1) / s + 6);
+        if (s == 1 || time < best) {
+            best = time;
+            splits = s;
+        }
+    }
     if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
     CUtensorMap map_x, map_w;
     if (!make_map(&map_x, a.x, 2, 1, a.seg.T, a.C, a.ldx, 0, S::TM, kDeep)) return GPD_ERR_CUDA;
