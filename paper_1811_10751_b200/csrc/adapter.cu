@@ -23,8 +23,8 @@ int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 }  // namespace
 
 int gpd::adapter_status_fetch_and_clear() {
-    const int a = shrink_status_fetch_and_clear(), b = expand_status_fetch_and_clear();
-    return a != 0 ? a : b;
+    const int a = shrink_status_fetch_and_clear(), b = expand_status_fetch_and_clear(), c = grad_status_fetch_and_clear();
+    return a != 0 ? a : b != 0 ? b : c;
 }
 
 extern "C" gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n, int32_t r, const void* A_dev, int64_t lda,
@@ -89,17 +89,17 @@ extern "C" gpd_status gpd_adapter_backward(gpd_dtype type, const void* dout_dev,
                               weights_aligned(B_dev, ldb, next_b)};
         const gpd_status s = shrink(type, true, down, st);
         if (s != GPD_OK) return s;
-        if (dx_dev) {
-            const int e = lm::dtype_size(dx_type), wide = e == 4 ? 8 : 16;
-            const ExpandArgs above{seg, u, A_dev, lda, next_a, nullptr, dbase_dev, lddb, dx_dev, lddx, K, r, weights_aligned(A_dev, lda, next_a),
-                                   lm::rows_aligned(dbase_dev, lddb, e, wide) && lm::rows_aligned(dx_dev, lddx, e, wide),
-                                   lm::rows_aligned(dbase_dev, lddb, e) && lm::rows_aligned(dx_dev, lddx, e)};
-            const gpd_status s2 = expand(type, dx_type, true, above, st);
-            if (s2 != GPD_OK) return s2;
-        }
     }
-    if (!grads) return GPD_OK;
-    const GradArgs two[2] = {{x_dev, ldx, u, nullptr, dA_dev, ldda, next_da, K, lm::rows_aligned(x_dev, ldx, 2), true},
-                             {dout_dev, lddo, h_dev, scale_dev, dB_dev, lddB, next_db, N, lm::rows_aligned(dout_dev, lddo, 2), false}};
-    return gradients(type, grad_type, accumulate != 0, seg, r, two, static_cast<unsigned char*>(workspace_dev) + own, st);
+    if (grads) {                                       // before dx: dout may still be in L2
+        const GradArgs two[2] = {{x_dev, ldx, u, nullptr, dA_dev, ldda, next_da, K, lm::rows_aligned(x_dev, ldx, 2), true},
+                                 {dout_dev, lddo, h_dev, scale_dev, dB_dev, lddB, next_db, N, lm::rows_aligned(dout_dev, lddo, 2), false}};
+        const gpd_status s = gradients(type, grad_type, accumulate != 0, seg, r, two, static_cast<unsigned char*>(workspace_dev) + own, st);
+        if (s != GPD_OK) return s;
+    }
+    if (!rows || !dx_dev) return GPD_OK;
+    const int e = lm::dtype_size(dx_type), wide = e == 4 ? 8 : 16;
+    const ExpandArgs above{seg, u, A_dev, lda, next_a, nullptr, dbase_dev, lddb, dx_dev, lddx, K, r, weights_aligned(A_dev, lda, next_a),
+                           lm::rows_aligned(dbase_dev, lddb, e, wide) && lm::rows_aligned(dx_dev, lddx, e, wide),
+                           lm::rows_aligned(dbase_dev, lddb, e) && lm::rows_aligned(dx_dev, lddx, e)};
+    return expand(type, dx_type, true, above, st);
 }

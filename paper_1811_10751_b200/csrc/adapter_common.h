@@ -268,6 +268,7 @@ gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& s
 
 int shrink_status_fetch_and_clear();                   // synchronous reads of the kernels' status words
 int expand_status_fetch_and_clear();
+int grad_status_fetch_and_clear();
 
 // n matrices of rows x cols (rows ld apart, matrices next) in boxes of box_rows x box_cols; rows of a box are swizzled over
 // their whole width; elements outside read as zero and are not written.

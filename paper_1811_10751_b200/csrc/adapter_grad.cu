@@ -3,8 +3,11 @@
 // Bound by reading y, 128 columns of which a CTA takes over a run of the adapter's rows (its segments' rows one after the
 // other); the r columns of h are few.  Long adapters are cut into runs, whose sums meet in a second kernel in a fixed order.  h is
 // FP32 and goes through the tensor cores as a sum of 16-bit parts, two for 16-bit gradients and FP16, three for FP32
-// gradients of BF16; FP16 parts are taken of a column of 64 rows over a power of two.  The chain of the tensor cores'
-// additions is cut every 64 rows.
+// gradients of BF16.  The chain of the tensor cores' additions is cut every 64 rows.
+// Two forms.  Rows on 16-byte boundaries and segments that are not short: a first kernel cuts h into its parts, once for all
+// columns of y, and tiles of both come by TMA, 64 rows of one segment each; FP16 parts are taken of an adapter's column over a
+// power of two.  Otherwise rows are gathered by their numbers, and h is cut by every CTA; FP16 parts are then taken of a
+// column of 64 rows over a power of two.
 #include <algorithm>
 #include <type_traits>
 
@@ -15,7 +18,7 @@ namespace adapter {
 
 namespace {
 
-constexpr int kThreads = 256, kCols = 128, kRows = 64, kStages = 3, kMostRows = 2048;
+constexpr int kThreads = 256, kCols = 128, kRows = 64, kStages = 3, kMostRows = 2048, kMostChunks = 256;
 constexpr int kYPitch = 2 * kCols + 16, kYStage = kRows * kYPitch;
 
 struct Job {
@@ -23,23 +26,22 @@ struct Job {
     Segments seg;
     const int32_t* slots;                              // [n + 1]: adapter i has the runs slots[i] .. slots[i + 1] - 1
     float* parts;                                      // [runs][part_size]
-    int64_t part_size, run;                            // floats of a run's sums; rows of a run
+    int64_t part_size, run;                            // floats of a run's sums; rows of a run, a multiple of 64
+    const int32_t* most;                               // FP16: bits of the largest magnitudes of h's columns, [2][n][RP]
     unsigned first_tiles;                              // column tiles of two[0]
     int r, max_slots;
     bool accumulate;
 };
 
-// Runs of every adapter.  One CTA; counts: n numbers of scratch.
-__global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Segments s, int64_t run, int max_slots, unsigned long long* counts,
-                                                   int32_t* slots) {
+// Runs of every adapter.  One CTA; counts: n numbers of scratch.  Segments take up whole multiples of `unit` rows.
+__device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int unit, int max_slots, unsigned long long* counts, int32_t* slots) {
     __shared__ int warp_sum[8];
     __shared__ int carry;
-    after_previous();
     for (int i = threadIdx.x; i < s.n; i += 256) counts[i] = 0;
     if (threadIdx.x == 0) carry = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < s.S; i += 256) {
-        const int64_t id = number(s.index, i, s.wide), rows = offset_at(s, i + 1) - offset_at(s, i);
+        const int64_t id = number(s.index, i, s.wide), rows = (offset_at(s, i + 1) - offset_at(s, i) + unit - 1) / unit * unit;
         if (id >= 0 && id < s.n && rows > 0) atomicAdd(counts + id, (unsigned long long)rows);     // whole numbers: any order
     }
     __threadfence_block();
@@ -66,6 +68,11 @@ __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Segme
     }
     if (threadIdx.x == 0) slots[s.n] = carry;
 }
+__global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Segments s, int64_t run, int max_slots, unsigned long long* counts,
+                                                   int32_t* slots) {
+    after_previous();
+    plan_runs(s, run, 1, max_slots, counts, slots);
+}
 
 // Rows v0 .. v0 + count - 1 of the adapter's rows, in `rows`; returns how many there are.  One warp.
 __device__ __forceinline__ int list_rows(const Segments& s, int64_t id, int64_t v0, int count, int32_t* rows) {
@@ -89,6 +96,17 @@ __device__ __forceinline__ int list_rows(const Segments& s, int64_t id, int64_t 
         }
     }
     return (int)min((int64_t)count, max((int64_t)0, seen - v0));
+}
+
+// The last adapter whose first run is <= slot
+__device__ __forceinline__ int adapter_of(const Job& job, int slot) {
+    int lo = 0, hi = job.seg.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (job.slots[mid] <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
 }
 
 __device__ __forceinline__ void add_to(float* p, float v, bool accumulate) { *p = accumulate ? *p + v : v; }
@@ -115,13 +133,7 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int slot = blockIdx.y, n = job.seg.n;
     if (slot >= job.slots[n]) return;
-    int lo = 0, hi = n - 1;                            // the last adapter whose first run is <= slot
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (job.slots[mid] <= slot) lo = mid;
-        else hi = mid - 1;
-    }
-    const int first = job.slots[lo], runs = job.slots[lo + 1] - first;
+    const int lo = adapter_of(job, slot), first = job.slots[lo], runs = job.slots[lo + 1] - first;
     const bool second = blockIdx.x >= job.first_tiles;
     const GradArgs& a = job.two[second];
     const int64_t c0 = (int64_t)(blockIdx.x - (second ? job.first_tiles : 0)) * kCols;
@@ -238,85 +250,381 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
             }
 }
 
-// Sums of the runs of the adapters that have several.
-template <typename O>
+// Sums of the runs of the adapters that have several.  FLAT: the results lie as the sums do, four at a time.
+template <typename O, bool FLAT>
 __global__ void __launch_bounds__(256) runs_kernel(const __grid_constant__ Job job) {
     after_previous();
     const int i = blockIdx.y, first = job.slots[i], runs = job.slots[i + 1] - first;
     if (runs == 1) return;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < job.part_size; e += (int64_t)gridDim.x * 256) {
-        float v = 0.f;
+    constexpr int V = FLAT ? 4 : 1;
+    const int64_t edge = job.two[0].C * job.r;
+    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; e < job.part_size; e += (int64_t)gridDim.x * 256 * V) {
         const float* p = job.parts + first * job.part_size + e;
-#pragma unroll 4
-        for (int k = 0; k < runs; ++k) v += p[k * job.part_size];
-        const bool second = e >= job.two[0].C * job.r;
+        const bool second = e >= edge;
         const GradArgs& a = job.two[second];
-        const int64_t at = e - (second ? job.two[0].C * job.r : 0), width = a.transposed ? a.C : job.r;
-        add_to(static_cast<O*>(a.dw) + i * a.next + at / width * a.ldw + at % width, v, job.accumulate);
+        const int64_t at = e - (second ? edge : 0);
+        if (FLAT) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int k = 0; k < runs; ++k) {
+                const float4 x = *reinterpret_cast<const float4*>(p + k * job.part_size);
+                v.x += x.x;
+                v.y += x.y;
+                v.z += x.z;
+                v.w += x.w;
+            }
+            O* to = static_cast<O*>(a.dw) + i * a.next + at;
+            add_to(to, v.x, job.accumulate);
+            add_to(to + 1, v.y, job.accumulate);
+            add_to(to + 2, v.z, job.accumulate);
+            add_to(to + 3, v.w, job.accumulate);
+        } else {
+            float v = 0.f;
+#pragma unroll 4
+            for (int k = 0; k < runs; ++k) v += p[k * job.part_size];
+            const int64_t width = a.transposed ? a.C : job.r;
+            add_to(static_cast<O*>(a.dw) + i * a.next + at / width * a.ldw + at % width, v, job.accumulate);
+        }
     }
 }
 
-// Rows of a run: enough runs that three CTAs per SM (of 148) are busy, of 256 rows at least.
-int64_t run_rows(int64_t T, int64_t K, int64_t N) {
-    const int64_t tiles = (K + kCols - 1) / kCols + (N + kCols - 1) / kCols, runs = std::max<int64_t>(1, (3 * 148 + tiles - 1) / std::max<int64_t>(tiles, 1));
-    const int64_t rows = ((T + runs - 1) / runs + kRows - 1) / kRows * kRows;
-    return std::min<int64_t>(kMostRows, std::max<int64_t>(256, rows));
+// ---- parts of h made once, tiles by TMA ----------------------------------------------------------------------
+__device__ int g_grad_status = 0;                      // GPD_ERR_TIMEOUT if a bounded wait expired
+
+// FP16: the largest magnitudes of the columns of u and h (blockIdx.y), for every adapter; `most` is zero before.
+__global__ void __launch_bounds__(256) most_kernel(const __grid_constant__ Job job, int RP, int32_t* most) {
+    after_previous();
+    const float* h = job.two[blockIdx.y].h;
+    const int r = job.r;
+    for (int s = blockIdx.z; s < job.seg.S; s += gridDim.z) {
+        const int64_t id = number(job.seg.index, s, job.seg.wide);
+        if (id < 0 || id >= job.seg.n) continue;
+        const int64_t from = offset_at(job.seg, s), to = offset_at(job.seg, s + 1);
+        // a thread keeps to one column
+        const int c = threadIdx.x % RP, step = 256 / RP;
+        float m = 0.f;
+        if (c < r)
+            for (int64_t t = from + (int64_t)blockIdx.x * step + threadIdx.x / RP; t < to; t += (int64_t)gridDim.x * step) m = fmaxf(m, fabsf(h[t * r + c]));
+        if (m > 0.f) atomicMax(most + ((int64_t)blockIdx.y * job.seg.n + id) * RP + c, __float_as_int(m));     // order does not matter
+    }
 }
-int64_t slots_of(int64_t T, int64_t n, int64_t K, int64_t N) { return T / run_rows(T, K, N) + n; }
+// planes[2][PARTS][T][RP]: u and h as parts.  The last CTA plans the runs.
+template <typename T, int PARTS>
+__global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job job, int RP, T* planes, int max_slots, unsigned long long* counts, int32_t* slots) {
+    after_previous();
+    if (blockIdx.x == gridDim.x - 1) {
+        plan_runs(job.seg, job.run, kRows, max_slots, counts, slots);
+        return;
+    }
+    constexpr bool kScaled = std::is_same<T, __half>::value;
+    const int64_t n = job.seg.T * (RP / 2), all = 2 * n;               // pairs
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)(gridDim.x - 1) * 256) {
+        const bool second = e >= n;
+        const int64_t at = e - (second ? n : 0), t = at / (RP / 2);
+        const int c = (int)(at - t * (RP / 2)) * 2;
+        const float* h = job.two[second].h + t * job.r + c;
+        float x = c < job.r ? h[0] : 0.f, y = c + 1 < job.r ? h[1] : 0.f;
+        if (kScaled) {
+            // the row's adapter: the last segment that begins at or before it (rows of no segment: anything will do)
+            int lo = 0, hi = job.seg.S - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (offset_at(job.seg, mid) <= t) lo = mid;
+                else hi = mid - 1;
+            }
+            const int64_t id = job.seg.S > 0 ? number(job.seg.index, lo, job.seg.wide) : -1;
+            if (id >= 0 && id < job.seg.n) {
+                const int32_t* m = job.most + ((int64_t)second * job.seg.n + id) * RP + c;
+                x *= power2(-exponent_of(__int_as_float(m[0])));
+                y *= power2(-exponent_of(__int_as_float(m[1])));
+            }
+        }
+        uint32_t parts[PARTS];
+        split2<T, PARTS>(x, y, parts);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint32_t*>(planes + ((second * PARTS + p) * job.seg.T + t) * RP + c) = parts[p];
+    }
+}
+
+// The chunks (of up to 64 rows of one segment) number c0 .. c0 + count - 1 of the adapter; returns how many there are.  One warp.
+__device__ __forceinline__ int list_chunks(const Segments& s, int64_t id, int64_t c0, int count, int2* list) {
+    const int lane = threadIdx.x & 31;
+    int64_t seen = 0;
+    for (int64_t base = 0; base < s.S && seen < c0 + count; base += 32) {
+        const int64_t i = base + lane;
+        int64_t at = 0, len = 0;
+        if (i < s.S && number(s.index, i, s.wide) == id) {
+            at = offset_at(s, i);
+            len = max((int64_t)0, offset_at(s, i + 1) - at);
+        }
+        uint32_t mine = __ballot_sync(0xffffffffu, len > 0);
+        while (mine) {
+            const int who = __ffs(mine) - 1;
+            mine &= mine - 1;
+            const int64_t start = __shfl_sync(0xffffffffu, at, who), rows = __shfl_sync(0xffffffffu, len, who), n = (rows + kRows - 1) / kRows;
+            const int64_t lo = max((int64_t)0, c0 - seen), hi = min(n, c0 + count - seen);
+            for (int64_t j = lo + lane; j < hi; j += 32)
+                list[seen + j - c0] = make_int2((int)(start + j * kRows), (int)min((int64_t)kRows, rows - j * kRows));
+            seen += n;
+        }
+    }
+    return (int)min((int64_t)count, max((int64_t)0, seen - c0));
+}
+
+template <int MT, int PARTS>
+struct TmaShape {
+    static constexpr int RP = 16 * MT, WARPS = MT <= 4 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
+    using Y = WTile<kRows, kCols>;
+    using H = WTile<kRows, RP>;
+    static constexpr int STAGE = Y::BYTES + PARTS * H::BYTES, SMEM = STAGES * STAGE + 1024;
+};
+struct GradMaps { CUtensorMap y[2], h[2]; };
+
+template <typename T, typename O, int MT, int PARTS>
+__global__ void __launch_bounds__(TmaShape<MT, PARTS>::WARPS * 32 + 32, MT <= 4 ? (per_sm(TmaShape<MT, PARTS>::SMEM) < 3 ? per_sm(TmaShape<MT, PARTS>::SMEM) : 3) : 1)
+grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ Job job) {
+    using S = TmaShape<MT, PARTS>;
+    constexpr int WARPS = S::WARPS, NT = S::NT;
+    constexpr bool kScaled = std::is_same<T, __half>::value;
+    extern __shared__ unsigned char raw[];
+    __shared__ Ring<S::STAGES> ring;
+    __shared__ int2 list[kMostChunks];
+    __shared__ int listed;
+    unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) ring.init(1, WARPS);
+    after_previous();
+    const int slot = blockIdx.y;
+    if (slot >= job.slots[job.seg.n]) return;
+    const int id = adapter_of(job, slot), first = job.slots[id], runs = job.slots[id + 1] - first;
+    const bool second = blockIdx.x >= job.first_tiles;
+    const GradArgs& a = job.two[second];
+    const int c0 = (int)(blockIdx.x - (second ? job.first_tiles : 0)) * kCols;
+    if (warp == 0) {
+        const int per = (int)(job.run / kRows), have = list_chunks(job.seg, id, (int64_t)(slot - first) * per, per, list);
+        if (lane == 0) listed = have;
+    }
+    __syncthreads();
+    const int n = listed;
+    if (warp == WARPS) {
+        int k = 0;
+        if (lane == 0) {
+            for (; k < n && ring.wait_empty(k, &g_grad_status); ++k) {
+                unsigned char* at = smem + k % S::STAGES * S::STAGE;
+                uint64_t* bar = &ring.full[k % S::STAGES];
+                tc::mbar_expect_tx(bar, S::STAGE);
+                S::Y::load(at, &maps.y[second], c0, list[k].x, 0, bar);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) S::H::load(at + S::Y::BYTES + p * S::H::BYTES, &maps.h[second], 0, list[k].x, p, bar);
+            }
+            ring.drain(k, &g_grad_status);
+        }
+        return;
+    }
+    float sum[MT][NT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[m][j][i] = 0.f;
+    for (int k = 0; k < n && ring.wait_full(k, &g_grad_status); ++k) {
+        const uint32_t ys = smem_at(smem + k % S::STAGES * S::STAGE), hs = ys + S::Y::BYTES;
+        const int rows = list[k].y;
+        float acc[MT][NT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.f;
+        // rows behind the segment's end, whatever they hold, are taken out of both operands
+        auto chunk = [&](auto masked) {
+#pragma unroll
+            for (int s = 0; s < kRows / 16; ++s) {
+                uint32_t low = 0xffffffffu, high = 0xffffffffu;        // rows 16 s + 2 q and the next; and eight rows on
+                if (masked.value) {
+                    const int t = 16 * s + 2 * (lane & 3);
+                    low = (t < rows ? 0xffffu : 0u) | (t + 1 < rows ? 0xffff0000u : 0u);
+                    high = (t + 8 < rows ? 0xffffu : 0u) | (t + 9 < rows ? 0xffff0000u : 0u);
+                }
+                uint32_t b[NT / 2][4];
+#pragma unroll
+                for (int j = 0; j < NT / 2; ++j) {
+                    ldmatrix4<true>(b[j], ys + S::Y::at(16 * s + (lane & 15), 8 * NT * warp + 16 * j + (lane >> 4) * 8));
+                    if (masked.value) {
+                        b[j][0] &= low;
+                        b[j][1] &= high;
+                        b[j][2] &= low;
+                        b[j][3] &= high;
+                    }
+                }
+#pragma unroll
+                for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        uint32_t h[4];
+                        ldmatrix4<true>(h, hs + p * S::H::BYTES + S::H::at(16 * s + (lane & 7) + (lane >> 4) * 8, 16 * m + (lane >> 3 & 1) * 8));
+                        if (masked.value) {
+                            h[0] &= low;
+                            h[1] &= low;
+                            h[2] &= high;
+                            h[3] &= high;
+                        }
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) mma(acc[m][j], h, b[j / 2][2 * (j & 1)], b[j / 2][2 * (j & 1) + 1], T());
+                    }
+            }
+        };
+        if (rows == kRows) chunk(std::false_type());
+        else chunk(std::true_type());
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ring.empty[k % S::STAGES]);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[m][j][i] += acc[m][j][i];
+    }
+    const float scale = a.scale ? a.scale[id] : 1.f;
+    O* dw = static_cast<O*>(a.dw) + id * a.next;
+    float* part = job.parts + slot * job.part_size + (second ? job.two[0].C * job.r : 0);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int kr = 16 * m + (lane >> 2) + 8 * (i >> 1);
+            if (kr >= job.r) continue;
+            const float by = kScaled ? scale * power2(exponent_of(__int_as_float(job.most[((int64_t)second * job.seg.n + id) * S::RP + kr]))) : scale;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int64_t c = c0 + 8 * (NT * warp + j) + 2 * (lane & 3) + (i & 1);
+                if (c >= a.C) continue;
+                const float v = sum[m][j][i] * by;
+                if (runs == 1) add_to(dw + (a.transposed ? kr * a.ldw + c : c * a.ldw + kr), v, job.accumulate);
+                else part[a.transposed ? kr * a.C + c : c * job.r + kr] = v;
+            }
+        }
+}
+
+// Rows of a run: so many runs that three CTAs per SM (of 148) are busy and none is left over, of 256 rows at least.
+int64_t run_rows(int64_t T, int64_t K, int64_t N, bool tma) {
+    const int64_t tiles = (K + kCols - 1) / kCols + (N + kCols - 1) / kCols, runs = std::max<int64_t>(1, 3 * 148 / std::max<int64_t>(tiles, 1));
+    const int64_t rows = ((T + runs - 1) / runs + kRows - 1) / kRows * kRows;
+    return std::min<int64_t>(tma ? kMostChunks * kRows : kMostRows, std::max<int64_t>(256, rows));
+}
+// Segments of less than 32 rows on average would leave half of their tiles empty.
+bool long_segments(int64_t T, int64_t S) { return S > 0 && T >= 32 * S; }
+// Most runs there can be.  By TMA a segment may end in a chunk of less than 64 rows, which takes up as much of a run.
+int64_t slots_of(int64_t T, int64_t n, int64_t S, int64_t K, int64_t N, bool tma) {
+    return (T + (tma ? (kRows - 1) * S : 0)) / run_rows(T, K, N, tma) + n;
+}
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
 
 template <typename T, typename O, int MT>
-gpd_status launch(const Job& job, cudaStream_t st) {
+gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t* slots, int32_t* most, bool tma, cudaStream_t st) {
     constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
-    using S = Shape<MT, PARTS>;
-    auto kernel = grad_kernel<T, O, MT, PARTS>;
-    if (S::SMEM > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
     const int64_t tiles = job.first_tiles + (job.two[1].C + kCols - 1) / kCols;
-    if (tiles == 0 || job.seg.n == 0) return GPD_OK;
-    gpd_status rc = launch_after(kernel, dim3((unsigned)tiles, (unsigned)job.max_slots), dim3(kThreads), S::SMEM, 1, st, job);
+    const dim3 grid((unsigned)tiles, (unsigned)job.max_slots);
+    gpd_status rc;
+    if (tma) {
+        using S = TmaShape<MT, PARTS>;
+        auto kernel = grad_tma_kernel<T, O, MT, PARTS>;
+        GradMaps maps;
+        for (int i = 0; i < 2; ++i)
+            if (!make_map(&maps.y[i], job.two[i].y, 2, 1, job.seg.T, job.two[i].C, job.two[i].ldy, 0, kRows, 64) ||
+                !make_map(&maps.h[i], planes + i * PARTS * job.seg.T * S::RP, 2, PARTS, job.seg.T, S::RP, S::RP, job.seg.T * S::RP, kRows, S::H::PITCH / 2))
+                return GPD_ERR_CUDA;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
+        if (std::is_same<T, __half>::value) {
+            const int RP = S::RP;
+            const unsigned z = (unsigned)std::min<int64_t>(job.seg.S, 64), x = (unsigned)std::max<int64_t>(1, std::min<int64_t>(256 / z, job.seg.T / z / 64));
+            rc = launch_after(most_kernel, dim3(x, 2, z), dim3(256), 0, 1, st, job, RP, most);
+            if (rc != GPD_OK) return rc;
+        }
+        const unsigned blocks = (unsigned)std::min<int64_t>((job.seg.T * S::RP + 255) / 256, 8 * sm_count()) + 1;
+        const int RP = S::RP;
+        rc = launch_after(split_kernel<T, PARTS>, dim3(blocks), dim3(256), 0, 1, st, job, RP, planes, job.max_slots, counts, slots);
+        if (rc != GPD_OK) return rc;
+        rc = launch_after(kernel, grid, dim3(S::WARPS * 32 + 32), S::SMEM, 1, st, maps, job);
+    } else {
+        using S = Shape<MT, PARTS>;
+        auto kernel = grad_kernel<T, O, MT, PARTS>;
+        if (S::SMEM > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
+        rc = launch_after(plan_kernel, dim3(1), dim3(256), 0, 1, st, job.seg, job.run, job.max_slots, counts, slots);
+        if (rc != GPD_OK) return rc;
+        rc = launch_after(kernel, grid, dim3(kThreads), S::SMEM, 1, st, job);
+    }
     if (rc != GPD_OK || job.max_slots == job.seg.n) return rc;         // as many runs as adapters: each has one
-    const unsigned blocks = (unsigned)std::min<int64_t>((job.part_size + 255) / 256, 16 * sm_count());
-    return launch_after(runs_kernel<O>, dim3(blocks, (unsigned)job.seg.n), dim3(256), 0, 1, st, job);
+    bool flat = job.two[0].C * job.r % 4 == 0 && job.part_size % 4 == 0;
+    for (const GradArgs& a : job.two) flat = flat && a.ldw == (a.transposed ? a.C : job.r) && (job.seg.n == 1 || a.next % 4 == 0);
+    const unsigned blocks = (unsigned)std::min<int64_t>((job.part_size / (flat ? 4 : 1) + 255) / 256, 16 * sm_count());
+    return launch_after(flat ? runs_kernel<O, true> : runs_kernel<O, false>, dim3(blocks, (unsigned)job.seg.n), dim3(256), 0, 1, st, job);
 }
-template <typename T, typename O>
-gpd_status launch_rank(const Job& job, cudaStream_t st) {
-    if (job.r <= 16) return launch<T, O, 1>(job, st);
-    if (job.r <= 32) return launch<T, O, 2>(job, st);
-    return job.r <= 64 ? launch<T, O, 4>(job, st) : launch<T, O, 8>(job, st);
+template <typename T, typename O, typename... A>
+gpd_status launch_rank(const Job& job, T* planes, A... more) {
+    if (job.r <= 16) return launch<T, O, 1>(job, planes, more...);
+    if (job.r <= 32) return launch<T, O, 2>(job, planes, more...);
+    return job.r <= 64 ? launch<T, O, 4>(job, planes, more...) : launch<T, O, 8>(job, planes, more...);
 }
+
+// Parts of the workspace, in bytes from its beginning
+struct Workspace {
+    int64_t counts, slots, most, planes, parts, bytes;
+    Workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N) {
+        const int64_t RP = padded_rank(r), runs = std::max(slots_of(T, n, 0, K, N, false), slots_of(T, n, T / 32, K, N, true));
+        counts = 0;
+        slots = counts + up(8 * n);
+        most = slots + up(4 * (n + 1));
+        planes = most + up(8 * n * RP);
+        parts = planes + up(2 * 3 * 2 * T * RP);
+        bytes = parts + (runs > n ? up(4 * runs * r * (K + N)) : 0);
+    }
+};
 
 }  // namespace
 
-// Counts, runs, their sums
-int64_t grad_workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N) {
-    const int64_t slots = slots_of(T, n, K, N);
-    return up(8 * n) + up(4 * (n + 1)) + (slots > n ? up(4 * slots * r * (K + N)) : 0);
+int64_t grad_workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N) { return Workspace(T, n, r, K, N).bytes; }
+
+int grad_status_fetch_and_clear() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_grad_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
+    if (v != 0) cudaMemcpyToSymbol(g_grad_status, &zero, sizeof(int));
+    return v;
 }
 
 gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& seg, int r, const GradArgs (&two)[2], void* workspace,
                      cudaStream_t st) {
+    const Workspace at(seg.T, seg.n, r, two[0].C, two[1].C);
+    const bool tma = two[0].y_vec && two[1].y_vec && long_segments(seg.T, seg.S);
     Job job;
     job.two[0] = two[0];
     job.two[1] = two[1];
     job.seg = seg;
     job.r = r;
     job.accumulate = accumulate;
-    job.run = run_rows(seg.T, two[0].C, two[1].C);
-    const int64_t slots = slots_of(seg.T, seg.n, two[0].C, two[1].C);
-    if (slots > 65535) return GPD_ERR_SHAPE;
-    job.max_slots = (int)slots;
+    job.run = run_rows(seg.T, two[0].C, two[1].C, tma);
+    const int64_t runs = slots_of(seg.T, seg.n, seg.S, two[0].C, two[1].C, tma);
+    if (runs > 65535) return GPD_ERR_SHAPE;
+    job.max_slots = (int)runs;
     job.part_size = (two[0].C + two[1].C) * r;
     job.first_tiles = (unsigned)((two[0].C + kCols - 1) / kCols);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
-    unsigned long long* counts = reinterpret_cast<unsigned long long*>(ws);
-    int32_t* runs = reinterpret_cast<int32_t*>(ws + up(8 * seg.n));
-    job.slots = runs;
-    job.parts = reinterpret_cast<float*>(ws + up(8 * seg.n) + up(4 * ((int64_t)seg.n + 1)));
-    const gpd_status rc = launch_after(plan_kernel, dim3(1), dim3(256), 0, 1, st, seg, job.run, job.max_slots, counts, runs);
-    if (rc != GPD_OK) return rc;
+    auto* counts = reinterpret_cast<unsigned long long*>(ws + at.counts);
+    int32_t *slots = reinterpret_cast<int32_t*>(ws + at.slots), *most = reinterpret_cast<int32_t*>(ws + at.most);
+    job.slots = slots;
+    job.most = most;
+    job.parts = reinterpret_cast<float*>(ws + at.parts);
+    if (tma && type == GPD_DT_F16 && cudaMemsetAsync(most, 0, 8 * (size_t)seg.n * padded_rank(r), st) != cudaSuccess) return GPD_ERR_CUDA;
+    auto* bf16 = reinterpret_cast<__nv_bfloat16*>(ws + at.planes);
+    auto* f16 = reinterpret_cast<__half*>(ws + at.planes);
     if (type == GPD_DT_BF16)
-        return grad_type == GPD_DT_F32 ? launch_rank<__nv_bfloat16, float>(job, st) : launch_rank<__nv_bfloat16, __nv_bfloat16>(job, st);
-    return grad_type == GPD_DT_F32 ? launch_rank<__half, float>(job, st) : launch_rank<__half, __half>(job, st);
+        return grad_type == GPD_DT_F32 ? launch_rank<__nv_bfloat16, float>(job, bf16, counts, slots, most, tma, st)
+                                       : launch_rank<__nv_bfloat16, __nv_bfloat16>(job, bf16, counts, slots, most, tma, st);
+    return grad_type == GPD_DT_F32 ? launch_rank<__half, float>(job, f16, counts, slots, most, tma, st)
+                                   : launch_rank<__half, __half>(job, f16, counts, slots, most, tma, st);
 }
 
 }  // namespace adapter

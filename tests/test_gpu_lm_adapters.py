@@ -160,6 +160,8 @@ CASES = {
     "many rows, several runs": dict(lens=[1500, 700, 900, 2100], index=[1, 0, 1, 2], n=3, r=40, K=264, N=136, grad=BF16),
     "many segments": dict(**ragged(900, 300, 11, 10, True), r=16, K=128, N=128),
     "several runs f16": dict(lens=[900, 1300], index=[0, 1], n=2, r=16, K=128, N=256, type=F16, grad=F16),
+    "several runs each, ends in tiles": dict(lens=[700, 1, 1290, 0, 333, 65], index=[1, 0, 1, 0, 0, 1], n=2, r=64, K=520, N=1160, grad=F32),
+    "rank 128, runs": dict(lens=[650, 1001], index=[0, 1], n=2, r=128, K=256, N=136, type=F16),
     "long sums": dict(lens=[60], index=[0], n=1, r=16, K=20000, N=16),
     "wide": dict(lens=[50], index=[0], n=1, r=16, K=16, N=20000),
     "tiny f16": dict(**ragged(150, 3, 2, 11), r=16, K=128, N=128, type=F16, size=2e-6),
@@ -255,6 +257,24 @@ def test_infinities_and_nans_stay_in_their_rows():
         bad[[3, 40, 41]] = True
         assert torch.equal(~torch.isfinite(h).any(1), bad) and torch.equal(out[~bad], clean[~bad])
         assert torch.isnan(out[3]).all() and not torch.isfinite(out[40:42]).any()
+
+
+@pytest.mark.parametrize("type", [BF16, F16])
+@pytest.mark.parametrize("lens", [[70, 90, 61], [5, 9, 3]])
+def test_gradients_of_an_adapter_do_not_see_the_rows_of_others(type, lens):
+    c = Case(lens=lens, index=[0, 1, 2], n=3, r=16, K=128, N=192, type=type)
+    _, h = c.forward()
+    c.backward(h)
+    dx, dA, dB = c.dx.clone(), c.dA.clone(), c.dB.clone()
+    a, b = lens[0], lens[0] + lens[1]
+    c.x[a, 3], c.x[b - 1, 100], c.dout[a, 5], c.dout[b - 1, 191], h[a, 2], h[b - 1, 7] = math.nan, math.inf, -math.inf, math.nan, math.nan, math.inf
+    c.backward(h)
+    others = torch.ones(c.T, dtype=torch.bool, device="cuda")
+    others[a:b] = False
+    assert torch.equal(c.dx[others], dx[others])
+    for i in (0, 2):
+        assert torch.equal(c.dA[i], dA[i]) and torch.equal(c.dB[i], dB[i])
+    assert not torch.isfinite(c.dA[1]).all() and not torch.isfinite(c.dB[1]).all()
 
 
 def test_gradients_agree_with_differences():
