@@ -180,6 +180,12 @@ struct Ring {
                 tc::mbar_wait(&full[k % STAGES], (k / STAGES) & 1, &never, status);
     }
 };
+// A lane's row and column in the 16 x 16 block that four matrices of a load make up: rows first (the two halves of an operand's
+// depth in neighbouring registers where the block is transposed), or columns first.
+__device__ __forceinline__ int row_first() { return threadIdx.x & 15; }
+__device__ __forceinline__ int row_first_col() { return (threadIdx.x >> 4 & 1) * 8; }
+__device__ __forceinline__ int col_first_row() { return (threadIdx.x & 7) + (threadIdx.x >> 4 & 1) * 8; }
+__device__ __forceinline__ int col_first() { return (threadIdx.x >> 3 & 1) * 8; }
 constexpr int per_sm(int smem) { return 227 * 1024 / (smem + 1536) < 5 ? 227 * 1024 / (smem + 1536) : 5; }     // CTAs that shared memory has room for
 // Byte of a tile whose rows are PITCH (32, 64 or 128) bytes, as TMA's swizzle of that width places it (the tile starts on a
 // 1024-byte boundary): eight rows' pieces of 16 bytes at one column lie in different banks.
@@ -191,6 +197,12 @@ struct WTile {
     static constexpr int PITCH = COLS >= 64 ? 128 : 2 * COLS, PARTS = COLS > 64 ? COLS / 64 : 1, BYTES = ROWS * COLS * 2;
     static __device__ __forceinline__ uint32_t at(int row, int col) {
         return (uint32_t)(col / 64 * ROWS * 128) + swizzled<PITCH>((uint32_t)(row * PITCH + col % 64 * 2));
+    }
+    // The same in two steps, for addresses of matrix loads: a lane's place (row below 16, column 0 or 8) in the tile at `tile`,
+    // and from there, by one operation, the place `row` (a multiple of 8) rows and `col` (a multiple of 16) columns on.
+    static __device__ __forceinline__ uint32_t lane_at(uint32_t tile, int row, int col) { return tile + swizzled<PITCH>((uint32_t)(row * PITCH + col * 2)); }
+    static __device__ __forceinline__ uint32_t on(uint32_t lane, int row, int col) {
+        return (lane ^ (uint32_t)(col % 64 * 2)) + (uint32_t)(row * PITCH + col / 64 * ROWS * 128);
     }
     static __device__ __forceinline__ void load(unsigned char* to, const CUtensorMap* map, int col, int row, int id, uint64_t* bar) {
 #pragma unroll

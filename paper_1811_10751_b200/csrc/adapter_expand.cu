@@ -282,12 +282,14 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) ring.init(a.w_vec ? 1 : 33, 4);
-    after_previous();
     if (!a.w_vec) {                                    // columns and rows of W that do not exist
         for (int i = threadIdx.x; i < S::STAGES * S::STAGE / 16; i += kThreads + 32) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
+    // The kernel before this one is the same call's: it began its work, and let this one start, when all before it had
+    // completed, and it writes h alone.  So only the warps that read h wait for it; segments, W and base are there.
+    if (warp < kThreads / 32) after_previous();
     const int64_t chunks = (a.C + kCols - 1) / kCols, all = count_tiles<S::TM>(a.seg) * chunks;
     const int64_t last = all * (blockIdx.x + 1) / gridDim.x;
     int k = 0;                                         // stages so far
@@ -333,14 +335,17 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
         for (int i = 0; i < n; ++i, ++k) {
             if (!ring.wait_full(k, &g_expand_status)) break;
-            const uint32_t stage = smem_at(smem + k % S::STAGES * S::STAGE), ws = stage + S::BASE, mine = stage + 16 * warp * 128;
+            const uint32_t stage = smem_at(smem) + k % S::STAGES * S::STAGE, mine = stage + 16 * warp * 128;
+            const uint32_t ws = TRANS ? S::W::lane_at(stage + S::BASE, row_first(), row_first_col())
+                                      : S::W::lane_at(stage + S::BASE, col_first_row(), col_first());
+            const uint32_t block0 = WTile<S::TM, kCols>::lane_at(mine, row_first(), row_first_col());
             if (any) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {          // 16 columns
                     // the sums begin with base where the result has 16 bits, whose rounding hides the tensor cores' truncation
                     constexpr bool kOnBase = sizeof(O) == 2 && std::is_same<T, __nv_bfloat16>::value;
                     float acc[2][4], own[2][4];        // [8 columns][row g: 2 q, 2 q + 1; row g + 8]
-                    const uint32_t block = mine + swizzled<128>((lane & 15) * 128 + 32 * p + (lane >> 4) * 16);
+                    const uint32_t block = WTile<S::TM, kCols>::on(block0, 0, 16 * p);
                     uint32_t b16[4] = {0, 0, 0, 0};
                     if (sizeof(O) == 2) {
                         if (a.base) ldmatrix4<false>(b16, block);
@@ -359,8 +364,8 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 #pragma unroll
                         for (int s = 0; s < KT; ++s) {
                             uint32_t b[4];
-                            if (TRANS) ldmatrix4<true>(b, ws + S::W::at(16 * s + (lane & 15), 16 * p + (lane >> 4) * 8));
-                            else ldmatrix4<false>(b, ws + S::W::at(16 * p + (lane & 7) + (lane >> 4) * 8, 16 * s + (lane >> 3 & 1) * 8));
+                            if (TRANS) ldmatrix4<true>(b, S::W::on(ws, 16 * s, 16 * p));
+                            else ldmatrix4<false>(b, S::W::on(ws, 16 * p, 16 * s));
 #pragma unroll
                             for (int i2 = PARTS - 1; i2 >= 0; --i2) {  // the small parts first
                                 mma(acc[0], ha[i2][s], b[0], b[1], T());

@@ -25,10 +25,12 @@ struct Job {
     GradArgs two[2];
     Segments seg;
     const int32_t* slots;                              // [n + 1]: adapter i has the runs slots[i] .. slots[i + 1] - 1
-    float* parts;                                      // [runs][part_size]
-    int64_t part_size, run;                            // floats of a run's sums; rows of a run, a multiple of 64
+    int4* info;                                        // by TMA: [runs]: adapter, its runs, chunks of this one
+    int2* chunks;                                      // by TMA: [runs][run / 64]: first row, rows
+    float* parts;                                      // [runs][tiles]: a tile's sums, as the threads hold them
+    int64_t run;                                       // rows of a run, a multiple of 64
     const int32_t* most;                               // FP16: bits of the largest magnitudes of h's columns, [2][n][RP]
-    unsigned first_tiles;                              // column tiles of two[0]
+    unsigned first_tiles, tiles;                       // column tiles of two[0], of both
     int r, max_slots;
     bool accumulate;
 };
@@ -112,6 +114,65 @@ __device__ __forceinline__ int adapter_of(const Job& job, int slot) {
 __device__ __forceinline__ void add_to(float* p, float v, bool accumulate) { *p = accumulate ? *p + v : v; }
 __device__ __forceinline__ void add_to(__nv_bfloat16* p, float v, bool accumulate) { *p = from_f32<__nv_bfloat16>(accumulate ? to_f32(*p) + v : v); }
 __device__ __forceinline__ void add_to(__half* p, float v, bool accumulate) { *p = from_f32<__half>(accumulate ? to_f32(*p) + v : v); }
+
+// A tile's sums: sum[m][j] are rows 16 m + g and g + 8 (columns of h), columns 8 (NT warp + j) + 2 q and the next, of 128.
+template <int WARPS>
+__device__ __forceinline__ void tile_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
+// Writes them where they belong, through shared memory (16 MT rows of 132 floats), so that neighbours leave together.  The
+// first 32 WARPS threads call it.
+template <typename O, int MT, int NT, int WARPS>
+__device__ __forceinline__ void finish_tile(const float (&sum)[MT][NT][4], const Job& job, const GradArgs& a, int id, int64_t c0, float* tile) {
+    constexpr int W = kCols + 4, THREADS = 32 * WARPS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = job.r;
+    tile_barrier<WARPS>();                             // what was in the memory has been read
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float* p = tile + (16 * m + (lane >> 2)) * W + 8 * (NT * warp + j) + 2 * (lane & 3);
+            *reinterpret_cast<float2*>(p) = make_float2(sum[m][j][0], sum[m][j][1]);
+            *reinterpret_cast<float2*>(p + 8 * W) = make_float2(sum[m][j][2], sum[m][j][3]);
+        }
+    tile_barrier<WARPS>();
+    const int cols = (int)min((int64_t)kCols, a.C - c0);
+    O* dw = static_cast<O*>(a.dw) + id * a.next;
+    if (a.transposed) {
+        O* to = dw + c0;
+        const bool vec = a.ldw % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & (4 * sizeof(O) - 1)) == 0;
+#pragma unroll 1
+        for (int e = threadIdx.x; e < r * (kCols / 4); e += THREADS) {
+            const int k = e / (kCols / 4), c = e % (kCols / 4) * 4;
+            const float4 v = *reinterpret_cast<const float4*>(tile + k * W + c);
+            O* p = to + k * a.ldw + c;
+            if (vec && c + 4 <= cols && !job.accumulate) {
+                if constexpr (sizeof(O) == 4) *reinterpret_cast<float4*>(p) = v;
+                else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v.x, v.y, O()), pack2(v.z, v.w, O()));
+            } else {
+                const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c + i < cols) add_to(p + i, f[i], job.accumulate);
+            }
+        }
+    } else {
+#pragma unroll 2
+        for (int e = threadIdx.x; e < r * cols; e += THREADS) {
+            const int c = e / r, k = e - c * r;
+            add_to(dw + (c0 + c) * a.ldw + k, tile[k * W + c], job.accumulate);
+        }
+    }
+}
+template <int MT, int NT, int WARPS>
+__device__ __forceinline__ float4* part_of(const Job& job, int slot, unsigned tile) {
+    return reinterpret_cast<float4*>(job.parts) + ((int64_t)slot * job.tiles + tile) * (MT * NT * 32 * WARPS) + threadIdx.x;
+}
+template <int MT, int NT, int WARPS>
+__device__ __forceinline__ void keep_tile(const float (&sum)[MT][NT][4], float4* part) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[(m * NT + j) * 32 * WARPS] = make_float4(sum[m][j][0], sum[m][j][1], sum[m][j][2], sum[m][j][3]);
+}
 
 template <int MT, int PARTS>
 struct Shape {
@@ -233,59 +294,46 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
     }
     copies_wait<0>();
     const float scale = a.scale ? a.scale[lo] : 1.f;
-    O* dw = static_cast<O*>(a.dw) + lo * a.next;
-    float* part = job.parts + slot * job.part_size + (second ? job.two[0].C * job.r : 0);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int kr = 16 * m + (lane >> 2) + 8 * (i >> 1);
-                const int64_t c = c0 + 16 * warp + 8 * j + 2 * (lane & 3) + (i & 1);
-                if (kr >= job.r || c >= a.C) continue;
-                const float v = sum[m][j][i] * scale;
-                if (runs == 1) add_to(dw + (a.transposed ? kr * a.ldw + c : c * a.ldw + kr), v, job.accumulate);
-                else part[a.transposed ? kr * a.C + c : c * job.r + kr] = v;
-            }
+            for (int i = 0; i < 4; ++i) sum[m][j][i] *= scale;
+    if (runs == 1) finish_tile<O, MT, 2, kThreads / 32>(sum, job, a, lo, c0, reinterpret_cast<float*>(smem));
+    else keep_tile<MT, 2, kThreads / 32>(sum, part_of<MT, 2, kThreads / 32>(job, slot, blockIdx.x));
 }
 
-// Sums of the runs of the adapters that have several.  FLAT: the results lie as the sums do, four at a time.
-template <typename O, bool FLAT>
-__global__ void __launch_bounds__(256) runs_kernel(const __grid_constant__ Job job) {
+// Sums of the runs of the adapters that have several.
+template <typename O, int MT, int NT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) runs_kernel(const __grid_constant__ Job job) {
+    extern __shared__ __align__(128) unsigned char smem[];
     after_previous();
-    const int i = blockIdx.y, first = job.slots[i], runs = job.slots[i + 1] - first;
-    if (runs == 1) return;
-    constexpr int V = FLAT ? 4 : 1;
-    const int64_t edge = job.two[0].C * job.r;
-    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; e < job.part_size; e += (int64_t)gridDim.x * 256 * V) {
-        const float* p = job.parts + first * job.part_size + e;
-        const bool second = e >= edge;
-        const GradArgs& a = job.two[second];
-        const int64_t at = e - (second ? edge : 0);
-        if (FLAT) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-            for (int k = 0; k < runs; ++k) {
-                const float4 x = *reinterpret_cast<const float4*>(p + k * job.part_size);
-                v.x += x.x;
-                v.y += x.y;
-                v.z += x.z;
-                v.w += x.w;
+    const int id = blockIdx.y, first = job.slots[id], runs = job.slots[id + 1] - first;
+    if (runs <= 1) return;
+    const bool second = blockIdx.x >= job.first_tiles;
+    float sum[MT][NT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[m][j][i] = 0.f;
+    const float4* part = part_of<MT, NT, WARPS>(job, first, blockIdx.x);
+#pragma unroll 1
+    for (int k = 0; k < runs; ++k, part += (int64_t)job.tiles * (MT * NT * 32 * WARPS))
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const float4 v = part[(m * NT + j) * 32 * WARPS];
+                sum[m][j][0] += v.x;
+                sum[m][j][1] += v.y;
+                sum[m][j][2] += v.z;
+                sum[m][j][3] += v.w;
             }
-            O* to = static_cast<O*>(a.dw) + i * a.next + at;
-            add_to(to, v.x, job.accumulate);
-            add_to(to + 1, v.y, job.accumulate);
-            add_to(to + 2, v.z, job.accumulate);
-            add_to(to + 3, v.w, job.accumulate);
-        } else {
-            float v = 0.f;
-#pragma unroll 4
-            for (int k = 0; k < runs; ++k) v += p[k * job.part_size];
-            const int64_t width = a.transposed ? a.C : job.r;
-            add_to(static_cast<O*>(a.dw) + i * a.next + at / width * a.ldw + at % width, v, job.accumulate);
-        }
-    }
+    finish_tile<O, MT, NT, WARPS>(sum, job, job.two[second], id, (int64_t)(blockIdx.x - (second ? job.first_tiles : 0)) * kCols,
+                                  reinterpret_cast<float*>(smem));
 }
 
 // ---- parts of h made once, tiles by TMA ----------------------------------------------------------------------
@@ -308,12 +356,44 @@ __global__ void __launch_bounds__(256) most_kernel(const __grid_constant__ Job j
         if (m > 0.f) atomicMax(most + ((int64_t)blockIdx.y * job.seg.n + id) * RP + c, __float_as_int(m));     // order does not matter
     }
 }
+// The chunks (of up to 64 rows of one segment) number c0 .. c0 + count - 1 of the adapter; returns how many there are.  One warp.
+__device__ __forceinline__ int list_chunks(const Segments& s, int64_t id, int64_t c0, int count, int2* list) {
+    const int lane = threadIdx.x & 31;
+    int64_t seen = 0;
+    for (int64_t base = 0; base < s.S && seen < c0 + count; base += 32) {
+        const int64_t i = base + lane;
+        int64_t at = 0, len = 0;
+        if (i < s.S && number(s.index, i, s.wide) == id) {
+            at = offset_at(s, i);
+            len = max((int64_t)0, offset_at(s, i + 1) - at);
+        }
+        uint32_t mine = __ballot_sync(0xffffffffu, len > 0);
+        while (mine) {
+            const int who = __ffs(mine) - 1;
+            mine &= mine - 1;
+            const int64_t start = __shfl_sync(0xffffffffu, at, who), rows = __shfl_sync(0xffffffffu, len, who), n = (rows + kRows - 1) / kRows;
+            const int64_t lo = max((int64_t)0, c0 - seen), hi = min(n, c0 + count - seen);
+            for (int64_t j = lo + lane; j < hi; j += 32)
+                list[seen + j - c0] = make_int2((int)(start + j * kRows), (int)min((int64_t)kRows, rows - j * kRows));
+            seen += n;
+        }
+    }
+    return (int)min((int64_t)count, max((int64_t)0, seen - c0));
+}
+
 // planes[2][PARTS][T][RP]: u and h as parts.  The last CTA plans the runs.
 template <typename T, int PARTS>
 __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job job, int RP, T* planes, int max_slots, unsigned long long* counts, int32_t* slots) {
     after_previous();
     if (blockIdx.x == gridDim.x - 1) {
         plan_runs(job.seg, job.run, kRows, max_slots, counts, slots);
+        __syncthreads();
+        const int per = (int)(job.run / kRows);
+        for (int slot = threadIdx.x >> 5; slot < slots[job.seg.n]; slot += 8) {
+            const int id = adapter_of(job, slot), first = slots[id];
+            const int have = list_chunks(job.seg, id, (int64_t)(slot - first) * per, per, job.chunks + (int64_t)slot * per);
+            if ((threadIdx.x & 31) == 0) job.info[slot] = make_int4(id, slots[id + 1] - first, have, 0);
+        }
         return;
     }
     constexpr bool kScaled = std::is_same<T, __half>::value;
@@ -346,31 +426,6 @@ __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job 
     }
 }
 
-// The chunks (of up to 64 rows of one segment) number c0 .. c0 + count - 1 of the adapter; returns how many there are.  One warp.
-__device__ __forceinline__ int list_chunks(const Segments& s, int64_t id, int64_t c0, int count, int2* list) {
-    const int lane = threadIdx.x & 31;
-    int64_t seen = 0;
-    for (int64_t base = 0; base < s.S && seen < c0 + count; base += 32) {
-        const int64_t i = base + lane;
-        int64_t at = 0, len = 0;
-        if (i < s.S && number(s.index, i, s.wide) == id) {
-            at = offset_at(s, i);
-            len = max((int64_t)0, offset_at(s, i + 1) - at);
-        }
-        uint32_t mine = __ballot_sync(0xffffffffu, len > 0);
-        while (mine) {
-            const int who = __ffs(mine) - 1;
-            mine &= mine - 1;
-            const int64_t start = __shfl_sync(0xffffffffu, at, who), rows = __shfl_sync(0xffffffffu, len, who), n = (rows + kRows - 1) / kRows;
-            const int64_t lo = max((int64_t)0, c0 - seen), hi = min(n, c0 + count - seen);
-            for (int64_t j = lo + lane; j < hi; j += 32)
-                list[seen + j - c0] = make_int2((int)(start + j * kRows), (int)min((int64_t)kRows, rows - j * kRows));
-            seen += n;
-        }
-    }
-    return (int)min((int64_t)count, max((int64_t)0, seen - c0));
-}
-
 template <int MT, int PARTS>
 struct TmaShape {
     static constexpr int RP = 16 * MT, WARPS = MT <= 4 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
@@ -389,23 +444,19 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
     extern __shared__ unsigned char raw[];
     __shared__ Ring<S::STAGES> ring;
     __shared__ int2 list[kMostChunks];
-    __shared__ int listed;
     unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) ring.init(1, WARPS);
     after_previous();
-    const int slot = blockIdx.y;
-    if (slot >= job.slots[job.seg.n]) return;
-    const int id = adapter_of(job, slot), first = job.slots[id], runs = job.slots[id + 1] - first;
+    const int slot = blockIdx.y, per = (int)(job.run / kRows);
+    for (int i = threadIdx.x; i < per; i += 32 * WARPS + 32) list[i] = job.chunks[(int64_t)slot * per + i];
+    const int4 info = job.info[slot];
+    if (slot >= job.slots[job.seg.n]) return;          // nor is there a list or an info
+    const int id = info.x, runs = info.y, n = info.z;
     const bool second = blockIdx.x >= job.first_tiles;
     const GradArgs& a = job.two[second];
     const int c0 = (int)(blockIdx.x - (second ? job.first_tiles : 0)) * kCols;
-    if (warp == 0) {
-        const int per = (int)(job.run / kRows), have = list_chunks(job.seg, id, (int64_t)(slot - first) * per, per, list);
-        if (lane == 0) listed = have;
-    }
     __syncthreads();
-    const int n = listed;
     if (warp == WARPS) {
         int k = 0;
         if (lane == 0) {
@@ -429,7 +480,10 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[m][j][i] = 0.f;
     for (int k = 0; k < n && ring.wait_full(k, &g_grad_status); ++k) {
-        const uint32_t ys = smem_at(smem + k % S::STAGES * S::STAGE), hs = ys + S::Y::BYTES;
+        const uint32_t stage = smem_at(smem) + k % S::STAGES * S::STAGE;
+        // a warp's columns: 32 (half of a part of 64) or 16
+        const uint32_t ys = S::Y::on(S::Y::lane_at(stage, row_first(), row_first_col()), 0, 8 * NT * warp);
+        const uint32_t hs = S::H::lane_at(stage + S::Y::BYTES, col_first_row(), col_first());
         const int rows = list[k].y;
         float acc[MT][NT][4];
 #pragma unroll
@@ -440,7 +494,7 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
                 for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.f;
         // rows behind the segment's end, whatever they hold, are taken out of both operands
         auto chunk = [&](auto masked) {
-#pragma unroll
+#pragma unroll (masked.value ? 1 : 2)
             for (int s = 0; s < kRows / 16; ++s) {
                 uint32_t low = 0xffffffffu, high = 0xffffffffu;        // rows 16 s + 2 q and the next; and eight rows on
                 if (masked.value) {
@@ -451,7 +505,7 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
                 uint32_t b[NT / 2][4];
 #pragma unroll
                 for (int j = 0; j < NT / 2; ++j) {
-                    ldmatrix4<true>(b[j], ys + S::Y::at(16 * s + (lane & 15), 8 * NT * warp + 16 * j + (lane >> 4) * 8));
+                    ldmatrix4<true>(b[j], S::Y::on(ys, 16 * s, 16 * j));
                     if (masked.value) {
                         b[j][0] &= low;
                         b[j][1] &= high;
@@ -464,7 +518,7 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
 #pragma unroll
                     for (int m = 0; m < MT; ++m) {
                         uint32_t h[4];
-                        ldmatrix4<true>(h, hs + p * S::H::BYTES + S::H::at(16 * s + (lane & 7) + (lane >> 4) * 8, 16 * m + (lane >> 3 & 1) * 8));
+                        ldmatrix4<true>(h, S::H::on(hs, 16 * s, 16 * m) + p * S::H::BYTES);
                         if (masked.value) {
                             h[0] &= low;
                             h[1] &= low;
@@ -488,29 +542,23 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
                 for (int i = 0; i < 4; ++i) sum[m][j][i] += acc[m][j][i];
     }
     const float scale = a.scale ? a.scale[id] : 1.f;
-    O* dw = static_cast<O*>(a.dw) + id * a.next;
-    float* part = job.parts + slot * job.part_size + (second ? job.two[0].C * job.r : 0);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int kr = 16 * m + (lane >> 2) + 8 * (i >> 1);
-            if (kr >= job.r) continue;
             const float by = kScaled ? scale * power2(exponent_of(__int_as_float(job.most[((int64_t)second * job.seg.n + id) * S::RP + kr]))) : scale;
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int64_t c = c0 + 8 * (NT * warp + j) + 2 * (lane & 3) + (i & 1);
-                if (c >= a.C) continue;
-                const float v = sum[m][j][i] * by;
-                if (runs == 1) add_to(dw + (a.transposed ? kr * a.ldw + c : c * a.ldw + kr), v, job.accumulate);
-                else part[a.transposed ? kr * a.C + c : c * job.r + kr] = v;
-            }
+            for (int j = 0; j < NT; ++j) sum[m][j][i] *= by;
         }
+    if (runs == 1) finish_tile<O, MT, NT, WARPS>(sum, job, a, id, c0, reinterpret_cast<float*>(smem));
+    else keep_tile<MT, NT, WARPS>(sum, part_of<MT, NT, WARPS>(job, slot, blockIdx.x));
 }
 
+int64_t tiles_of(int64_t K, int64_t N) { return (K + kCols - 1) / kCols + (N + kCols - 1) / kCols; }
 // Rows of a run: so many runs that three CTAs per SM (of 148) are busy and none is left over, of 256 rows at least.
 int64_t run_rows(int64_t T, int64_t K, int64_t N, bool tma) {
-    const int64_t tiles = (K + kCols - 1) / kCols + (N + kCols - 1) / kCols, runs = std::max<int64_t>(1, 3 * 148 / std::max<int64_t>(tiles, 1));
+    const int64_t runs = std::max<int64_t>(1, 3 * 148 / tiles_of(K, N));
     const int64_t rows = ((T + runs - 1) / runs + kRows - 1) / kRows * kRows;
     return std::min<int64_t>(tma ? kMostChunks * kRows : kMostRows, std::max<int64_t>(256, rows));
 }
@@ -526,8 +574,8 @@ int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 :
 template <typename T, typename O, int MT>
 gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t* slots, int32_t* most, bool tma, cudaStream_t st) {
     constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
-    const int64_t tiles = job.first_tiles + (job.two[1].C + kCols - 1) / kCols;
-    const dim3 grid((unsigned)tiles, (unsigned)job.max_slots);
+    constexpr int TILE = 16 * MT * (kCols + 4) * 4;    // a tile's sums on their way out
+    const dim3 grid(job.tiles, (unsigned)job.max_slots);
     gpd_status rc;
     if (tma) {
         using S = TmaShape<MT, PARTS>;
@@ -551,6 +599,7 @@ gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t
         rc = launch_after(kernel, grid, dim3(S::WARPS * 32 + 32), S::SMEM, 1, st, maps, job);
     } else {
         using S = Shape<MT, PARTS>;
+        static_assert(S::SMEM >= TILE && TmaShape<MT, PARTS>::SMEM - 1024 >= TILE, "a tile's sums leave through the stages' memory");
         auto kernel = grad_kernel<T, O, MT, PARTS>;
         if (S::SMEM > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
         rc = launch_after(plan_kernel, dim3(1), dim3(256), 0, 1, st, job.seg, job.run, job.max_slots, counts, slots);
@@ -558,10 +607,10 @@ gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t
         rc = launch_after(kernel, grid, dim3(kThreads), S::SMEM, 1, st, job);
     }
     if (rc != GPD_OK || job.max_slots == job.seg.n) return rc;         // as many runs as adapters: each has one
-    bool flat = job.two[0].C * job.r % 4 == 0 && job.part_size % 4 == 0;
-    for (const GradArgs& a : job.two) flat = flat && a.ldw == (a.transposed ? a.C : job.r) && (job.seg.n == 1 || a.next % 4 == 0);
-    const unsigned blocks = (unsigned)std::min<int64_t>((job.part_size / (flat ? 4 : 1) + 255) / 256, 16 * sm_count());
-    return launch_after(flat ? runs_kernel<O, true> : runs_kernel<O, false>, dim3(blocks, (unsigned)job.seg.n), dim3(256), 0, 1, st, job);
+    constexpr int WARPS = TmaShape<MT, PARTS>::WARPS, NT = TmaShape<MT, PARTS>::NT;
+    auto join = tma ? runs_kernel<O, MT, NT, WARPS> : runs_kernel<O, MT, 2, kThreads / 32>;
+    if (TILE > 49152 && cudaFuncSetAttribute(join, cudaFuncAttributeMaxDynamicSharedMemorySize, TILE) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_after(join, dim3(job.tiles, (unsigned)job.seg.n), dim3(tma ? 32 * WARPS : kThreads), TILE, 1, st, job);
 }
 template <typename T, typename O, typename... A>
 gpd_status launch_rank(const Job& job, T* planes, A... more) {
@@ -572,15 +621,17 @@ gpd_status launch_rank(const Job& job, T* planes, A... more) {
 
 // Parts of the workspace, in bytes from its beginning
 struct Workspace {
-    int64_t counts, slots, most, planes, parts, bytes;
+    int64_t counts, slots, most, planes, info, chunks, parts, bytes;
     Workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N) {
-        const int64_t RP = padded_rank(r), runs = std::max(slots_of(T, n, 0, K, N, false), slots_of(T, n, T / 32, K, N, true));
+        const int64_t RP = padded_rank(r), by_tma = slots_of(T, n, T / 32, K, N, true), runs = std::max(slots_of(T, n, 0, K, N, false), by_tma);
         counts = 0;
         slots = counts + up(8 * n);
         most = slots + up(4 * (n + 1));
         planes = most + up(8 * n * RP);
-        parts = planes + up(2 * 3 * 2 * T * RP);
-        bytes = parts + (runs > n ? up(4 * runs * r * (K + N)) : 0);
+        info = planes + up(2 * 3 * 2 * T * RP);
+        chunks = info + up(16 * by_tma);
+        parts = chunks + up(8 * by_tma * (run_rows(T, K, N, true) / kRows));
+        bytes = parts + (runs > n ? up(4 * runs * tiles_of(K, N) * RP * kCols) : 0);
     }
 };
 
@@ -609,13 +660,15 @@ gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& s
     const int64_t runs = slots_of(seg.T, seg.n, seg.S, two[0].C, two[1].C, tma);
     if (runs > 65535) return GPD_ERR_SHAPE;
     job.max_slots = (int)runs;
-    job.part_size = (two[0].C + two[1].C) * r;
     job.first_tiles = (unsigned)((two[0].C + kCols - 1) / kCols);
+    job.tiles = (unsigned)tiles_of(two[0].C, two[1].C);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     auto* counts = reinterpret_cast<unsigned long long*>(ws + at.counts);
     int32_t *slots = reinterpret_cast<int32_t*>(ws + at.slots), *most = reinterpret_cast<int32_t*>(ws + at.most);
     job.slots = slots;
     job.most = most;
+    job.info = reinterpret_cast<int4*>(ws + at.info);
+    job.chunks = reinterpret_cast<int2*>(ws + at.chunks);
     job.parts = reinterpret_cast<float*>(ws + at.parts);
     if (tma && type == GPD_DT_F16 && cudaMemsetAsync(most, 0, 8 * (size_t)seg.n * padded_rank(r), st) != cudaSuccess) return GPD_ERR_CUDA;
     auto* bf16 = reinterpret_cast<__nv_bfloat16*>(ws + at.planes);

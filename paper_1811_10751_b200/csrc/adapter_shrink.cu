@@ -201,9 +201,11 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
         __syncwarp();
         if (lane == 0) ring.drain(k, &g_shrink_status);
     } else {
-        const int row = 16 * warp + (lane & 15);
         for (int k = 0; k < n && ring.wait_full(k, &g_shrink_status); ++k) {
-            const uint32_t xs = smem_at(smem + k % S::STAGES * S::STAGE), ws = xs + S::X_BYTES;
+            const uint32_t stage = smem_at(smem) + k % S::STAGES * S::STAGE;
+            const uint32_t xs = WTile<S::TM, kDeep>::lane_at(stage, row_first(), row_first_col()) + 16 * warp * 128;
+            const uint32_t ws = TRANS ? S::W::lane_at(stage + S::X_BYTES, row_first(), row_first_col())
+                                      : S::W::lane_at(stage + S::X_BYTES, col_first_row(), col_first());
             float acc[NT][4];
 #pragma unroll
             for (int i = 0; i < NT; ++i)
@@ -212,12 +214,12 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
 #pragma unroll
             for (int ks = 0; ks < kDeep / 16; ++ks) {
                 uint32_t xa[4];
-                ldmatrix4<false>(xa, xs + swizzled<128>(row * 128 + 32 * ks + (lane >> 4) * 16));
+                ldmatrix4<false>(xa, WTile<S::TM, kDeep>::on(xs, 0, 16 * ks));
 #pragma unroll
                 for (int p = 0; p < NT / 2; ++p) {
                     uint32_t b[4];
-                    if (TRANS) ldmatrix4<true>(b, ws + S::W::at(16 * ks + (lane & 15), 16 * p + (lane >> 4) * 8));
-                    else ldmatrix4<false>(b, ws + S::W::at(16 * p + (lane & 7) + (lane >> 4) * 8, 16 * ks + (lane >> 3 & 1) * 8));
+                    if (TRANS) ldmatrix4<true>(b, S::W::on(ws, 16 * ks, 16 * p));
+                    else ldmatrix4<false>(b, S::W::on(ws, 16 * p, 16 * ks));
                     mma(acc[2 * p], xa, b[0], b[1], T());
                     mma(acc[2 * p + 1], xa, b[2], b[3], T());
                 }
