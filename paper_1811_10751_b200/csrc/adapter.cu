@@ -90,9 +90,9 @@ extern "C" gpd_status gpd_adapter_backward(gpd_dtype type, const void* dout_dev,
         const gpd_status s = shrink(type, true, down, st);
         if (s != GPD_OK) return s;
     }
-    if (grads) {                                       // before dx: dout may still be in L2
-        const GradArgs two[2] = {{x_dev, ldx, u, nullptr, dA_dev, ldda, next_da, K, lm::rows_aligned(x_dev, ldx, 2), true},
-                                 {dout_dev, lddo, h_dev, scale_dev, dB_dev, lddB, next_db, N, lm::rows_aligned(dout_dev, lddo, 2), false}};
+    if (grads) {                                       // before dx, and dB first: dout may still be in L2
+        const GradArgs two[2] = {{dout_dev, lddo, h_dev, scale_dev, dB_dev, lddB, next_db, N, lm::rows_aligned(dout_dev, lddo, 2), false},
+                                 {x_dev, ldx, u, nullptr, dA_dev, ldda, next_da, K, lm::rows_aligned(x_dev, ldx, 2), true}};
         const gpd_status s = gradients(type, grad_type, accumulate != 0, seg, r, two, static_cast<unsigned char*>(workspace_dev) + own, st);
         if (s != GPD_OK) return s;
     }

@@ -1,13 +1,16 @@
 // Gradients of low-rank adapters' factors: dW_i[c][k] = scale_i sum_t y[t][c] h[t][k] over the rows t of adapter i.
 //
-// Bound by reading y, 128 columns of which a CTA takes over a run of the adapter's rows (its segments' rows one after the
-// other); the r columns of h are few.  Long adapters are cut into runs, whose sums meet in a second kernel in a fixed order.  h is
+// Bound by reading y, 128 columns of which a CTA takes over a part of the adapter's rows (its segments' rows one after the
+// other); the r columns of h are few.  The parts' sums meet in a fixed order.  h is
 // FP32 and goes through the tensor cores as a sum of 16-bit parts, two for 16-bit gradients and FP16, three for FP32
 // gradients of BF16.  The chain of the tensor cores' additions is cut every 64 rows.
 // Two forms.  Rows on 16-byte boundaries and segments that are not short: a first kernel cuts h into its parts, once for all
-// columns of y, and tiles of both come by TMA, 64 rows of one segment each; FP16 parts are taken of an adapter's column over a
-// power of two.  Otherwise rows are gathered by their numbers, and h is cut by every CTA; FP16 parts are then taken of a
-// column of 64 rows over a power of two.
+// columns of y, and tiles of both come by TMA, 64 rows of one segment each; the CTAs of a cluster share an adapter's rows and
+// add up over distributed shared memory; FP16 parts are taken of an adapter's column over a power of two.  Otherwise
+// rows are gathered by their numbers in runs, whose sums go through memory, and h is cut by every CTA; FP16 parts are then taken
+// of a column of 64 rows over a power of two.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -18,15 +21,14 @@ namespace adapter {
 
 namespace {
 
-constexpr int kThreads = 256, kCols = 128, kRows = 64, kStages = 3, kMostRows = 2048, kMostChunks = 256;
+constexpr int kThreads = 256, kCols = 128, kRows = 64, kStages = 3, kMostRows = 2048;
 constexpr int kYPitch = 2 * kCols + 16, kYStage = kRows * kYPitch;
 
 struct Job {
     GradArgs two[2];
     Segments seg;
-    const int32_t* slots;                              // [n + 1]: adapter i has the runs slots[i] .. slots[i + 1] - 1
-    int4* info;                                        // by TMA: [runs]: adapter, its runs, chunks of this one
-    int2* chunks;                                      // by TMA: [runs][run / 64]: first row, rows
+    const int32_t* slots;                              // [n + 1]: adapter i has the runs (chunks) slots[i] .. slots[i + 1] - 1
+    int2* chunks;                                      // by TMA: first row and rows of the adapters' chunks, up to 64 rows of a segment
     float* parts;                                      // [runs][tiles]: a tile's sums, as the threads hold them
     int64_t run;                                       // rows of a run, a multiple of 64
     const int32_t* most;                               // FP16: bits of the largest magnitudes of h's columns, [2][n][RP]
@@ -35,8 +37,8 @@ struct Job {
     bool accumulate;
 };
 
-// Runs of every adapter.  One CTA; counts: n numbers of scratch.  Segments take up whole multiples of `unit` rows.
-__device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int unit, int max_slots, unsigned long long* counts, int32_t* slots) {
+// Runs of every adapter, `least` or more.  One CTA; counts: n numbers of scratch.  Segments take up whole multiples of `unit` rows.
+__device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int unit, int least, int max_slots, unsigned long long* counts, int32_t* slots) {
     __shared__ int warp_sum[8];
     __shared__ int carry;
     for (int i = threadIdx.x; i < s.n; i += 256) counts[i] = 0;
@@ -51,7 +53,7 @@ __device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int un
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int base = 0; base < s.n; base += 256) {
         const int i = base + threadIdx.x;
-        const int64_t want = i < s.n ? max((int64_t)1, ((int64_t)counts[i] + run - 1) / run) : 0;
+        const int64_t want = i < s.n ? max((int64_t)least, ((int64_t)counts[i] + run - 1) / run) : 0;
         const int own = (int)min(want, (int64_t)max_slots);
         int scan = own;
 #pragma unroll
@@ -73,7 +75,7 @@ __device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int un
 __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Segments s, int64_t run, int max_slots, unsigned long long* counts,
                                                    int32_t* slots) {
     after_previous();
-    plan_runs(s, run, 1, max_slots, counts, slots);
+    plan_runs(s, run, 1, 1, max_slots, counts, slots);
 }
 
 // Rows v0 .. v0 + count - 1 of the adapter's rows, in `rows`; returns how many there are.  One warp.
@@ -100,17 +102,6 @@ __device__ __forceinline__ int list_rows(const Segments& s, int64_t id, int64_t 
     return (int)min((int64_t)count, max((int64_t)0, seen - v0));
 }
 
-// The last adapter whose first run is <= slot
-__device__ __forceinline__ int adapter_of(const Job& job, int slot) {
-    int lo = 0, hi = job.seg.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (job.slots[mid] <= slot) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
-
 __device__ __forceinline__ void add_to(float* p, float v, bool accumulate) { *p = accumulate ? *p + v : v; }
 __device__ __forceinline__ void add_to(__nv_bfloat16* p, float v, bool accumulate) { *p = from_f32<__nv_bfloat16>(accumulate ? to_f32(*p) + v : v); }
 __device__ __forceinline__ void add_to(__half* p, float v, bool accumulate) { *p = from_f32<__half>(accumulate ? to_f32(*p) + v : v); }
@@ -118,33 +109,36 @@ __device__ __forceinline__ void add_to(__half* p, float v, bool accumulate) { *p
 // A tile's sums: sum[m][j] are rows 16 m + g and g + 8 (columns of h), columns 8 (NT warp + j) + 2 q and the next, of 128.
 template <int WARPS>
 __device__ __forceinline__ void tile_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
-// Writes them where they belong, through shared memory (16 MT rows of 132 floats), so that neighbours leave together.  The
-// first 32 WARPS threads call it.
-template <typename O, int MT, int NT, int WARPS>
-__device__ __forceinline__ void finish_tile(const float (&sum)[MT][NT][4], const Job& job, const GradArgs& a, int id, int64_t c0, float* tile) {
-    constexpr int W = kCols + 4, THREADS = 32 * WARPS;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = job.r;
-    tile_barrier<WARPS>();                             // what was in the memory has been read
+// They leave through shared memory (16 MT rows of 132 floats), so that neighbours leave together.
+constexpr int kTileWidth = kCols + 4;
+template <int MT, int NT>
+__device__ __forceinline__ void put_tile(const float (&sum)[MT][NT][4], float* tile) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            float* p = tile + (16 * m + (lane >> 2)) * W + 8 * (NT * warp + j) + 2 * (lane & 3);
+            float* p = tile + (16 * m + (lane >> 2)) * kTileWidth + 8 * (NT * warp + j) + 2 * (lane & 3);
             *reinterpret_cast<float2*>(p) = make_float2(sum[m][j][0], sum[m][j][1]);
-            *reinterpret_cast<float2*>(p + 8 * W) = make_float2(sum[m][j][2], sum[m][j][3]);
+            *reinterpret_cast<float2*>(p + 8 * kTileWidth) = make_float2(sum[m][j][2], sum[m][j][3]);
         }
-    tile_barrier<WARPS>();
-    const int cols = (int)min((int64_t)kCols, a.C - c0);
+}
+// Writes a tile where it belongs: four of its numbers at (row k of h, column c) come from get(k, c).  Of `threads` threads this is
+// number `first`.
+template <typename O, typename F>
+__device__ __forceinline__ void write_tile(const Job& job, const GradArgs& a, int64_t id, int64_t c0, int first, int threads, F get) {
+    const int cols = (int)min((int64_t)kCols, a.C - c0), r = job.r;
     O* dw = static_cast<O*>(a.dw) + id * a.next;
     if (a.transposed) {
         O* to = dw + c0;
-        const bool vec = a.ldw % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & (4 * sizeof(O) - 1)) == 0;
+        const bool vec = a.ldw % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & (4 * sizeof(O) - 1)) == 0 && !job.accumulate;
 #pragma unroll 1
-        for (int e = threadIdx.x; e < r * (kCols / 4); e += THREADS) {
+        for (int e = first; e < r * (kCols / 4); e += threads) {
             const int k = e / (kCols / 4), c = e % (kCols / 4) * 4;
-            const float4 v = *reinterpret_cast<const float4*>(tile + k * W + c);
+            if (c >= cols) continue;
+            const float4 v = get(k, c);
             O* p = to + k * a.ldw + c;
-            if (vec && c + 4 <= cols && !job.accumulate) {
+            if (vec && c + 4 <= cols) {
                 if constexpr (sizeof(O) == 4) *reinterpret_cast<float4*>(p) = v;
                 else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v.x, v.y, O()), pack2(v.z, v.w, O()));
             } else {
@@ -155,12 +149,27 @@ __device__ __forceinline__ void finish_tile(const float (&sum)[MT][NT][4], const
             }
         }
     } else {
-#pragma unroll 2
-        for (int e = threadIdx.x; e < r * cols; e += THREADS) {
-            const int c = e / r, k = e - c * r;
-            add_to(dw + (c0 + c) * a.ldw + k, tile[k * W + c], job.accumulate);
+        // four columns of y (rows of dW) at one column of h
+#pragma unroll 1
+        for (int e = first; e < r * (kCols / 4); e += threads) {
+            const int g = e / r, k = e - g * r, c = 4 * g;
+            if (c >= cols) continue;
+            const float4 v = get(k, c);
+            const float f[4] = {v.x, v.y, v.z, v.w};
+            O* p = dw + (c0 + c) * a.ldw + k;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < cols) add_to(p + i * a.ldw, f[i], job.accumulate);
         }
     }
+}
+// The first 32 WARPS threads call it: a tile that is whole in their registers.
+template <typename O, int MT, int NT, int WARPS>
+__device__ __forceinline__ void finish_tile(const float (&sum)[MT][NT][4], const Job& job, const GradArgs& a, int id, int64_t c0, float* tile) {
+    tile_barrier<WARPS>();                             // what was in the memory has been read
+    put_tile<MT, NT>(sum, tile);
+    tile_barrier<WARPS>();
+    write_tile<O>(job, a, id, c0, threadIdx.x, 32 * WARPS, [&](int k, int c) { return *reinterpret_cast<const float4*>(tile + k * kTileWidth + c); });
 }
 template <int MT, int NT, int WARPS>
 __device__ __forceinline__ float4* part_of(const Job& job, int slot, unsigned tile) {
@@ -194,7 +203,13 @@ __global__ void __launch_bounds__(kThreads) grad_kernel(const __grid_constant__ 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int slot = blockIdx.y, n = job.seg.n;
     if (slot >= job.slots[n]) return;
-    const int lo = adapter_of(job, slot), first = job.slots[lo], runs = job.slots[lo + 1] - first;
+    int lo = 0, hi = n - 1;                            // the last adapter whose first run is <= slot
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (job.slots[mid] <= slot) lo = mid;
+        else hi = mid - 1;
+    }
+    const int first = job.slots[lo], runs = job.slots[lo + 1] - first;
     const bool second = blockIdx.x >= job.first_tiles;
     const GradArgs& a = job.two[second];
     const int64_t c0 = (int64_t)(blockIdx.x - (second ? job.first_tiles : 0)) * kCols;
@@ -356,11 +371,11 @@ __global__ void __launch_bounds__(256) most_kernel(const __grid_constant__ Job j
         if (m > 0.f) atomicMax(most + ((int64_t)blockIdx.y * job.seg.n + id) * RP + c, __float_as_int(m));     // order does not matter
     }
 }
-// The chunks (of up to 64 rows of one segment) number c0 .. c0 + count - 1 of the adapter; returns how many there are.  One warp.
-__device__ __forceinline__ int list_chunks(const Segments& s, int64_t id, int64_t c0, int count, int2* list) {
+// The adapter's chunks, `count` at most.  One warp.
+__device__ __forceinline__ void list_chunks(const Segments& s, int64_t id, int count, int2* list) {
     const int lane = threadIdx.x & 31;
     int64_t seen = 0;
-    for (int64_t base = 0; base < s.S && seen < c0 + count; base += 32) {
+    for (int64_t base = 0; base < s.S && seen < count; base += 32) {
         const int64_t i = base + lane;
         int64_t at = 0, len = 0;
         if (i < s.S && number(s.index, i, s.wide) == id) {
@@ -372,28 +387,21 @@ __device__ __forceinline__ int list_chunks(const Segments& s, int64_t id, int64_
             const int who = __ffs(mine) - 1;
             mine &= mine - 1;
             const int64_t start = __shfl_sync(0xffffffffu, at, who), rows = __shfl_sync(0xffffffffu, len, who), n = (rows + kRows - 1) / kRows;
-            const int64_t lo = max((int64_t)0, c0 - seen), hi = min(n, c0 + count - seen);
-            for (int64_t j = lo + lane; j < hi; j += 32)
-                list[seen + j - c0] = make_int2((int)(start + j * kRows), (int)min((int64_t)kRows, rows - j * kRows));
+            for (int64_t j = lane; j < n && seen + j < count; j += 32)
+                list[seen + j] = make_int2((int)(start + j * kRows), (int)min((int64_t)kRows, rows - j * kRows));
             seen += n;
         }
     }
-    return (int)min((int64_t)count, max((int64_t)0, seen - c0));
 }
 
-// planes[2][PARTS][T][RP]: u and h as parts.  The last CTA plans the runs.
+// planes[2][PARTS][T][RP]: u and h as parts.  The last CTA lists the chunks.
 template <typename T, int PARTS>
-__global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job job, int RP, T* planes, int max_slots, unsigned long long* counts, int32_t* slots) {
+__global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job job, int RP, T* planes, int max_chunks, unsigned long long* counts, int32_t* slots) {
     after_previous();
     if (blockIdx.x == gridDim.x - 1) {
-        plan_runs(job.seg, job.run, kRows, max_slots, counts, slots);
+        plan_runs(job.seg, kRows, kRows, 0, max_chunks, counts, slots);
         __syncthreads();
-        const int per = (int)(job.run / kRows);
-        for (int slot = threadIdx.x >> 5; slot < slots[job.seg.n]; slot += 8) {
-            const int id = adapter_of(job, slot), first = slots[id];
-            const int have = list_chunks(job.seg, id, (int64_t)(slot - first) * per, per, job.chunks + (int64_t)slot * per);
-            if ((threadIdx.x & 31) == 0) job.info[slot] = make_int4(id, slots[id + 1] - first, have, 0);
-        }
+        for (int id = threadIdx.x >> 5; id < job.seg.n; id += 8) list_chunks(job.seg, id, slots[id + 1] - slots[id], job.chunks + slots[id]);
         return;
     }
     constexpr bool kScaled = std::is_same<T, __half>::value;
@@ -428,7 +436,7 @@ __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job 
 
 template <int MT, int PARTS>
 struct TmaShape {
-    static constexpr int RP = 16 * MT, WARPS = MT <= 4 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
+    static constexpr int RP = 16 * MT, WARPS = MT <= 2 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
     using Y = WTile<kRows, kCols>;
     using H = WTile<kRows, RP>;
     static constexpr int STAGE = Y::BYTES + PARTS * H::BYTES, SMEM = STAGES * STAGE + 1024;
@@ -437,41 +445,24 @@ struct GradMaps { CUtensorMap y[2], h[2]; };
 
 template <typename T, typename O, int MT, int PARTS>
 __global__ void __launch_bounds__(TmaShape<MT, PARTS>::WARPS * 32 + 32, MT <= 4 ? (per_sm(TmaShape<MT, PARTS>::SMEM) < 3 ? per_sm(TmaShape<MT, PARTS>::SMEM) : 3) : 1)
-grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ Job job) {
+grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ Job job, int splits) {
     using S = TmaShape<MT, PARTS>;
     constexpr int WARPS = S::WARPS, NT = S::NT;
     constexpr bool kScaled = std::is_same<T, __half>::value;
     extern __shared__ unsigned char raw[];
     __shared__ Ring<S::STAGES> ring;
-    __shared__ int2 list[kMostChunks];
+    __shared__ int rows_of[S::STAGES];                 // rows of the stages' chunks
     unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) ring.init(1, WARPS);
     after_previous();
-    const int slot = blockIdx.y, per = (int)(job.run / kRows);
-    for (int i = threadIdx.x; i < per; i += 32 * WARPS + 32) list[i] = job.chunks[(int64_t)slot * per + i];
-    const int4 info = job.info[slot];
-    if (slot >= job.slots[job.seg.n]) return;          // nor is there a list or an info
-    const int id = info.x, runs = info.y, n = info.z;
-    const bool second = blockIdx.x >= job.first_tiles;
+    // the cluster's adapter; this CTA's chunks of it
+    const int id = blockIdx.x / splits, rank = blockIdx.x % splits, first = job.slots[id], have = job.slots[id + 1] - first;
+    const int from = (int)((int64_t)have * rank / splits), n = (int)((int64_t)have * (rank + 1) / splits) - from;
+    const bool second = blockIdx.y >= job.first_tiles;
     const GradArgs& a = job.two[second];
-    const int c0 = (int)(blockIdx.x - (second ? job.first_tiles : 0)) * kCols;
+    const int c0 = (int)(blockIdx.y - (second ? job.first_tiles : 0)) * kCols;
     __syncthreads();
-    if (warp == WARPS) {
-        int k = 0;
-        if (lane == 0) {
-            for (; k < n && ring.wait_empty(k, &g_grad_status); ++k) {
-                unsigned char* at = smem + k % S::STAGES * S::STAGE;
-                uint64_t* bar = &ring.full[k % S::STAGES];
-                tc::mbar_expect_tx(bar, S::STAGE);
-                S::Y::load(at, &maps.y[second], c0, list[k].x, 0, bar);
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p) S::H::load(at + S::Y::BYTES + p * S::H::BYTES, &maps.h[second], 0, list[k].x, p, bar);
-            }
-            ring.drain(k, &g_grad_status);
-        }
-        return;
-    }
     float sum[MT][NT][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -479,12 +470,32 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[m][j][i] = 0.f;
+    if (warp == WARPS) {
+        int k = 0;
+        int2 next = make_int2(0, 0);
+        for (; k < n; ++k) {
+            if (k % 32 == 0 && k + lane < n) next = job.chunks[first + from + k + lane];
+            const int row = __shfl_sync(0xffffffffu, next.x, k % 32), rows = __shfl_sync(0xffffffffu, next.y, k % 32);
+            if (!ring.wait_empty(k, &g_grad_status)) break;
+            if (lane == 0) {
+                unsigned char* at = smem + k % S::STAGES * S::STAGE;
+                uint64_t* bar = &ring.full[k % S::STAGES];
+                rows_of[k % S::STAGES] = rows;
+                tc::mbar_expect_tx(bar, S::STAGE);
+                S::Y::load(at, &maps.y[second], c0, row, 0, bar);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) S::H::load(at + S::Y::BYTES + p * S::H::BYTES, &maps.h[second], 0, row, p, bar);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) ring.drain(k, &g_grad_status);
+    } else
     for (int k = 0; k < n && ring.wait_full(k, &g_grad_status); ++k) {
         const uint32_t stage = smem_at(smem) + k % S::STAGES * S::STAGE;
         // a warp's columns: 32 (half of a part of 64) or 16
         const uint32_t ys = S::Y::on(S::Y::lane_at(stage, row_first(), row_first_col()), 0, 8 * NT * warp);
         const uint32_t hs = S::H::lane_at(stage + S::Y::BYTES, col_first_row(), col_first());
-        const int rows = list[k].y;
+        const int rows = rows_of[k % S::STAGES];
         float acc[MT][NT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -551,22 +562,43 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
 #pragma unroll
             for (int j = 0; j < NT; ++j) sum[m][j][i] *= by;
         }
-    if (runs == 1) finish_tile<O, MT, NT, WARPS>(sum, job, a, id, c0, reinterpret_cast<float*>(smem));
-    else keep_tile<MT, NT, WARPS>(sum, part_of<MT, NT, WARPS>(job, slot, blockIdx.x));
+    float* tile = reinterpret_cast<float*>(smem);
+    __syncthreads();                                   // every stage has been read
+    if (warp < WARPS) put_tile<MT, NT>(sum, tile);
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    if (splits > 1) cluster.sync();
+    else __syncthreads();
+    constexpr int THREADS = 32 * WARPS + 32;
+    write_tile<O>(job, a, id, c0, rank * THREADS + threadIdx.x, splits * THREADS, [&](int k, int c) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < splits; ++s) {
+            const float4 x = *reinterpret_cast<const float4*>((splits > 1 ? cluster.map_shared_rank(tile, s) : tile) + k * kTileWidth + c);
+            v.x += x.x;
+            v.y += x.y;
+            v.z += x.z;
+            v.w += x.w;
+        }
+        return v;
+    });
+    if (splits > 1) cluster.sync();                    // the others have read this CTA's sums
 }
 
 int64_t tiles_of(int64_t K, int64_t N) { return (K + kCols - 1) / kCols + (N + kCols - 1) / kCols; }
-// Rows of a run: so many runs that three CTAs per SM (of 148) are busy and none is left over, of 256 rows at least.
-int64_t run_rows(int64_t T, int64_t K, int64_t N, bool tma) {
-    const int64_t runs = std::max<int64_t>(1, 3 * 148 / tiles_of(K, N));
+// Rows of a run where rows are gathered: so many runs that two CTAs per SM (of 148) are busy, of 256 rows at least.
+int64_t run_rows(int64_t T, int64_t K, int64_t N) {
+    const int64_t runs = std::max<int64_t>(1, 2 * 148 / tiles_of(K, N));
     const int64_t rows = ((T + runs - 1) / runs + kRows - 1) / kRows * kRows;
-    return std::min<int64_t>(tma ? kMostChunks * kRows : kMostRows, std::max<int64_t>(256, rows));
+    return std::min<int64_t>(kMostRows, std::max<int64_t>(256, rows));
 }
+int64_t slots_of(int64_t T, int64_t n, int64_t K, int64_t N) { return T / run_rows(T, K, N) + n; }    // most runs there can be
 // Segments of less than 32 rows on average would leave half of their tiles empty.
 bool long_segments(int64_t T, int64_t S) { return S > 0 && T >= 32 * S; }
-// Most runs there can be.  By TMA a segment may end in a chunk of less than 64 rows, which takes up as much of a run.
-int64_t slots_of(int64_t T, int64_t n, int64_t S, int64_t K, int64_t N, bool tma) {
-    return (T + (tma ? (kRows - 1) * S : 0)) / run_rows(T, K, N, tma) + n;
+int64_t chunks_of(int64_t T, int64_t S) { return T / kRows + S; }      // most chunks there can be
+// CTAs that share an adapter's rows: as many as are resident at once, if as many adapters as there are segments have rows, and
+// no more than leaves each of them four chunks.
+int splits_of(int64_t T, int64_t S, int64_t n, int64_t tiles, int resident) {
+    const int64_t active = std::min(n, S), most = std::min<int64_t>(8, std::max<int64_t>(1, T / active / (4 * kRows)));
+    return (int)std::max<int64_t>(1, std::min(most, (int64_t)resident / (tiles * active)));
 }
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
@@ -574,8 +606,7 @@ int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 :
 template <typename T, typename O, int MT>
 gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t* slots, int32_t* most, bool tma, cudaStream_t st) {
     constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
-    constexpr int TILE = 16 * MT * (kCols + 4) * 4;    // a tile's sums on their way out
-    const dim3 grid(job.tiles, (unsigned)job.max_slots);
+    constexpr int TILE = 16 * MT * kTileWidth * 4;     // a tile's sums on their way out
     gpd_status rc;
     if (tma) {
         using S = TmaShape<MT, PARTS>;
@@ -594,23 +625,26 @@ gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t
         }
         const unsigned blocks = (unsigned)std::min<int64_t>((job.seg.T * S::RP + 255) / 256, 8 * sm_count()) + 1;
         const int RP = S::RP;
-        rc = launch_after(split_kernel<T, PARTS>, dim3(blocks), dim3(256), 0, 1, st, job, RP, planes, job.max_slots, counts, slots);
+        const int most_chunks = (int)chunks_of(job.seg.T, job.seg.S);
+        rc = launch_after(split_kernel<T, PARTS>, dim3(blocks), dim3(256), 0, 1, st, job, RP, planes, most_chunks, counts, slots);
         if (rc != GPD_OK) return rc;
-        rc = launch_after(kernel, grid, dim3(S::WARPS * 32 + 32), S::SMEM, 1, st, maps, job);
-    } else {
+        const int per = MT <= 4 ? std::min(3, per_sm(S::SMEM)) : 1, splits = splits_of(job.seg.T, job.seg.S, job.seg.n, job.tiles, per * sm_count());
+        if (job.tiles > 65535 || (int64_t)job.seg.n * splits > 0x7fffffff) return GPD_ERR_SHAPE;
+        return launch_after(kernel, dim3((unsigned)(job.seg.n * splits), job.tiles), dim3(S::WARPS * 32 + 32), S::SMEM, splits, st, maps, job, splits);
+    }
+    {
         using S = Shape<MT, PARTS>;
         static_assert(S::SMEM >= TILE && TmaShape<MT, PARTS>::SMEM - 1024 >= TILE, "a tile's sums leave through the stages' memory");
         auto kernel = grad_kernel<T, O, MT, PARTS>;
         if (S::SMEM > 40960 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
         rc = launch_after(plan_kernel, dim3(1), dim3(256), 0, 1, st, job.seg, job.run, job.max_slots, counts, slots);
         if (rc != GPD_OK) return rc;
-        rc = launch_after(kernel, grid, dim3(kThreads), S::SMEM, 1, st, job);
+        rc = launch_after(kernel, dim3(job.tiles, (unsigned)job.max_slots), dim3(kThreads), S::SMEM, 1, st, job);
     }
     if (rc != GPD_OK || job.max_slots == job.seg.n) return rc;         // as many runs as adapters: each has one
-    constexpr int WARPS = TmaShape<MT, PARTS>::WARPS, NT = TmaShape<MT, PARTS>::NT;
-    auto join = tma ? runs_kernel<O, MT, NT, WARPS> : runs_kernel<O, MT, 2, kThreads / 32>;
+    auto join = runs_kernel<O, MT, 2, kThreads / 32>;
     if (TILE > 49152 && cudaFuncSetAttribute(join, cudaFuncAttributeMaxDynamicSharedMemorySize, TILE) != cudaSuccess) return GPD_ERR_CUDA;
-    return launch_after(join, dim3(job.tiles, (unsigned)job.seg.n), dim3(tma ? 32 * WARPS : kThreads), TILE, 1, st, job);
+    return launch_after(join, dim3(job.tiles, (unsigned)job.seg.n), dim3(kThreads), TILE, 1, st, job);
 }
 template <typename T, typename O, typename... A>
 gpd_status launch_rank(const Job& job, T* planes, A... more) {
@@ -621,16 +655,15 @@ gpd_status launch_rank(const Job& job, T* planes, A... more) {
 
 // Parts of the workspace, in bytes from its beginning
 struct Workspace {
-    int64_t counts, slots, most, planes, info, chunks, parts, bytes;
+    int64_t counts, slots, most, planes, chunks, parts, bytes;
     Workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N) {
-        const int64_t RP = padded_rank(r), by_tma = slots_of(T, n, T / 32, K, N, true), runs = std::max(slots_of(T, n, 0, K, N, false), by_tma);
+        const int64_t RP = padded_rank(r), runs = slots_of(T, n, K, N);
         counts = 0;
         slots = counts + up(8 * n);
         most = slots + up(4 * (n + 1));
         planes = most + up(8 * n * RP);
-        info = planes + up(2 * 3 * 2 * T * RP);
-        chunks = info + up(16 * by_tma);
-        parts = chunks + up(8 * by_tma * (run_rows(T, K, N, true) / kRows));
+        chunks = planes + up(2 * 3 * 2 * T * RP);
+        parts = chunks + up(8 * chunks_of(T, T / 32));
         bytes = parts + (runs > n ? up(4 * runs * tiles_of(K, N) * RP * kCols) : 0);
     }
 };
@@ -656,8 +689,8 @@ gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& s
     job.seg = seg;
     job.r = r;
     job.accumulate = accumulate;
-    job.run = run_rows(seg.T, two[0].C, two[1].C, tma);
-    const int64_t runs = slots_of(seg.T, seg.n, seg.S, two[0].C, two[1].C, tma);
+    job.run = run_rows(seg.T, two[0].C, two[1].C);
+    const int64_t runs = slots_of(seg.T, seg.n, two[0].C, two[1].C);
     if (runs > 65535) return GPD_ERR_SHAPE;
     job.max_slots = (int)runs;
     job.first_tiles = (unsigned)((two[0].C + kCols - 1) / kCols);
@@ -667,7 +700,6 @@ gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& s
     int32_t *slots = reinterpret_cast<int32_t*>(ws + at.slots), *most = reinterpret_cast<int32_t*>(ws + at.most);
     job.slots = slots;
     job.most = most;
-    job.info = reinterpret_cast<int4*>(ws + at.info);
     job.chunks = reinterpret_cast<int2*>(ws + at.chunks);
     job.parts = reinterpret_cast<float*>(ws + at.parts);
     if (tma && type == GPD_DT_F16 && cudaMemsetAsync(most, 0, 8 * (size_t)seg.n * padded_rank(r), st) != cudaSuccess) return GPD_ERR_CUDA;
