@@ -23,8 +23,8 @@ int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 }  // namespace
 
 int gpd::adapter_status_fetch_and_clear() {
-    const int a = shrink_status_fetch_and_clear(), b = expand_status_fetch_and_clear(), c = grad_status_fetch_and_clear();
-    return a != 0 ? a : b != 0 ? b : c;
+    const int a = shrink_status_fetch_and_clear(), b = expand_status_fetch_and_clear(), c = grad_status_fetch_and_clear(), d = short_status_fetch_and_clear();
+    return a != 0 ? a : b != 0 ? b : c != 0 ? c : d;
 }
 
 extern "C" gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n, int32_t r, const void* A_dev, int64_t lda,
@@ -43,12 +43,14 @@ extern "C" gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx
     cudaStream_t st = as_stream(stream);
     const ShrinkArgs down{seg, x_dev, ldx, A_dev, lda, next_a, nullptr, h_dev, K, r, lm::rows_aligned(x_dev, ldx, 2),
                           weights_aligned(A_dev, lda, next_a)};
-    const gpd_status first = shrink(type, false, down, st);
-    if (first != GPD_OK) return first;
     const ExpandArgs above{seg, h_dev, B_dev, ldb, next_b, scale_dev, base_dev, ldbase, out_dev, ldo, N, r, weights_aligned(B_dev, ldb, next_b),
                            lm::rows_aligned(base_dev, ldbase, e, wide) && lm::rows_aligned(out_dev, ldo, e, wide),
                            lm::rows_aligned(base_dev, ldbase, e) && lm::rows_aligned(out_dev, ldo, e)};
-    return expand(type, out_type, false, above, st);
+    bool taken = false;
+    const gpd_status both = short_segments(type, out_type, down, above, &taken, st);
+    if (both != GPD_OK || taken) return both;
+    const gpd_status first = shrink(type, false, down, st);
+    return first != GPD_OK ? first : expand(type, out_type, false, above, st);
 }
 
 extern "C" gpd_status gpd_adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int32_t n, int32_t r, int64_t* bytes_host) {

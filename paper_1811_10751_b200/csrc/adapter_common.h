@@ -274,12 +274,14 @@ struct GradArgs {                                      // dW_i[c][k] = scale_i s
 };
 gpd_status shrink(int type, bool transposed, const ShrinkArgs& a, cudaStream_t st);
 gpd_status expand(int type, int out_type, bool transposed, const ExpandArgs& a, cudaStream_t st);
+gpd_status short_segments(int type, int out_type, const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st);
 int64_t grad_workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N);
 gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& seg, int r, const GradArgs (&two)[2], void* workspace,
                      cudaStream_t st);
 
 int shrink_status_fetch_and_clear();                   // synchronous reads of the kernels' status words
 int expand_status_fetch_and_clear();
+int short_status_fetch_and_clear();
 int grad_status_fetch_and_clear();
 
 // n matrices of rows x cols (rows ld apart, matrices next) in boxes of box_rows x box_cols; rows of a box are swizzled over

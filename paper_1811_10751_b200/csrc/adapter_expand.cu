@@ -10,7 +10,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "adapter_common.h"
+#include "adapter_rows.h"
 
 namespace gpd {
 namespace adapter {
@@ -26,83 +26,13 @@ struct Shape {
     static constexpr int STAGE = W_ROWS * W_PITCH, SMEM = STAGES * STAGE;
 };
 
-// Word j of lane t of four becomes word t of lane j.
-__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
-    const int lane = threadIdx.x & 31;
-    const bool odd = lane & 1, high = lane & 2;
-    uint32_t r0 = __shfl_xor_sync(0xffffffffu, odd ? w[0] : w[1], 1), r1 = __shfl_xor_sync(0xffffffffu, odd ? w[2] : w[3], 1);
-    if (odd) {
-        w[0] = r0;
-        w[2] = r1;
-    } else {
-        w[1] = r0;
-        w[3] = r1;
-    }
-    r0 = __shfl_xor_sync(0xffffffffu, high ? w[0] : w[2], 2);
-    r1 = __shfl_xor_sync(0xffffffffu, high ? w[1] : w[3], 2);
-    if (high) {
-        w[0] = r0;
-        w[1] = r1;
-    } else {
-        w[2] = r0;
-        w[3] = r1;
-    }
-}
-
-// A thread's share of base in a chunk, as it is in memory
-template <typename O> struct Share { uint4 v[2][2]; };                 // [32 columns][row g, g + 8]: eight elements
-template <> struct Share<float> { float2 v[8][2]; };                   // [8 columns][row]: two elements
-
-// The warp's rows of h (those that there are) times scale, as operands of the tensor cores; undo[i]: what FP16 parts of
-// row g + 8 i have to be multiplied with.
-template <typename T, int KT, int PARTS>
-__device__ __forceinline__ void load_parts(const float* h, int r, float scale, const bool (&has)[2], uint32_t (&ha)[PARTS][KT][4], float (&undo)[2]) {
-    const int q = threadIdx.x & 3;
-    float v[KT][2][4];                                 // [16 columns][row][2 q, 2 q + 1, 2 q + 8, 2 q + 9]
-    float most[2] = {0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < KT; ++k)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = 16 * k + 2 * q + (j & 1) + (j >> 1) * 8;
-                v[k][i][j] = has[i] && c < r ? h[(int64_t)8 * i * r + c] * scale : 0.f;
-                most[i] = fmaxf(most[i], fabsf(v[k][i][j]));
-            }
-    undo[0] = undo[1] = 1.f;
-    if (std::is_same<T, __half>::value) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            most[i] = fmaxf(most[i], __shfl_xor_sync(0xffffffffu, most[i], 1));
-            most[i] = fmaxf(most[i], __shfl_xor_sync(0xffffffffu, most[i], 2));
-            const int e = exponent_of(most[i]);
-            undo[i] = power2(e);
-            const float by = power2(-e);
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[k][i][j] *= by;
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < KT; ++k)
-#pragma unroll
-        for (int f = 0; f < 4; ++f) {                  // rows g, g + 8, then the same eight columns on
-            uint32_t parts[PARTS];
-            split2<T, PARTS>(v[k][f & 1][2 * (f >> 1)], v[k][f & 1][2 * (f >> 1) + 1], parts);
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) ha[p][k][f] = parts[p];
-        }
-}
-
 // WM = 4: a warp has 16 rows of the tile and all columns.  WM = 1: all warps have the same 16 rows, 64 columns each.
 template <typename T, typename O, int KT, int PARTS, int WM, bool TRANS>
 __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant__ ExpandArgs a) {
     using S = Shape<KT, WM, TRANS>;
     extern __shared__ __align__(128) unsigned char smem[];
     after_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
     const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x);
     if (tile.rows == 0) return;
     const bool none = tile.id < 0 || tile.id >= a.seg.n;
@@ -133,31 +63,8 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant_
 
     Share<O> next;
     auto load_base = [&](int64_t k, Share<O>& s) {
-        const int64_t c0 = k * S::COLS + (WM == 1 ? kCols * warp : 0);
-        if constexpr (sizeof(O) == 4) {
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int64_t c = c0 + 8 * n + 2 * q;
-                    s.v[n][i] = make_float2(0.f, 0.f);
-                    if (!base || !has[i] || k >= to || c >= a.C) continue;
-                    const float* p = base + 8 * i * a.ldb + c;
-                    if (a.io_vec && c + 2 <= a.C) s.v[n][i] = *reinterpret_cast<const float2*>(p);
-                    else s.v[n][i] = make_float2(p[0], c + 1 < a.C ? p[1] : 0.f);
-                }
-        } else {
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int64_t c = c0 + 32 * n + 8 * q;
-                    s.v[n][i] = make_uint4(0, 0, 0, 0);
-                    if (!base || !has[i] || k >= to || c >= a.C) continue;
-                    const O* p = base + 8 * i * a.ldb + c;
-                    s.v[n][i] = a.io_vec ? load8<O, true>(p, (int)min((int64_t)8, a.C - c)).v : load8<O, false>(p, (int)min((int64_t)8, a.C - c)).v;
-                }
-        }
+        const int64_t c = k * S::COLS + (WM == 1 ? kCols * warp : 0);
+        load_share<O>(s, base ? base + c : nullptr, a.ldb, has, k < to ? a.C - c : 0, a.io_vec);
     };
     load_base(from, next);
     const float nan = __int_as_float(0x7fffffff);
@@ -195,49 +102,8 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant_
                     for (int i = 0; i < 4; ++i) acc[n][i] *= undo[i >> 1];
             }
         }
-        const int64_t c0 = k * S::COLS + wc;
-        if constexpr (sizeof(O) == 4) {
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int64_t c = c0 + 8 * n + 2 * q;
-                    if (!has[i] || c >= a.C) continue;
-                    float* p = out + 8 * i * a.ldo + c;
-                    const float2 v = make_float2(share.v[n][i].x + acc[n][2 * i], share.v[n][i].y + acc[n][2 * i + 1]);
-                    if (a.io_vec && c + 2 <= a.C) {
-                        *reinterpret_cast<float2*>(p) = v;
-                    } else {
-                        p[0] = v.x;
-                        if (c + 1 < a.C) p[1] = v.y;
-                    }
-                }
-        } else {
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t b[4] = {share.v[n][i].x, share.v[n][i].y, share.v[n][i].z, share.v[n][i].w};
-                    transpose4(b);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 f = unpack2(b[j], O());
-                        b[j] = pack2(f.x + acc[4 * n + j][2 * i], f.y + acc[4 * n + j][2 * i + 1], O());
-                    }
-                    transpose4(b);
-                    const int64_t c = c0 + 32 * n + 8 * q;
-                    if (!has[i] || c >= a.C) continue;
-                    O* p = out + 8 * i * a.ldo + c;
-                    if (a.io_vec && c + 8 <= a.C) {
-                        *reinterpret_cast<uint4*>(p) = make_uint4(b[0], b[1], b[2], b[3]);
-                    } else {
-                        unsigned short* s = reinterpret_cast<unsigned short*>(p);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (c + j < a.C) s[j] = (unsigned short)(b[j / 2] >> (16 * (j & 1)));
-                    }
-                }
-        }
+        const int64_t c = k * S::COLS + wc;
+        store_sum<O>(share, acc, out + c, a.ldo, has, a.C - c, a.io_vec);
     }
     copies_wait<0>();
 }

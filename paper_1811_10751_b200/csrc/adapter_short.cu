@@ -1,0 +1,250 @@
+// Low-rank adapters over short segments (a token each, or a few), both products in one launch:
+//   h[t] = A_i x[t],   out[t] = base[t] + scale_i B_i h[t]
+//
+// Bound by reading the adapters, and where that is little by latency.  A cluster takes 16 rows of one segment.  Each of its CTAs
+// has a part of the columns of A and of the rows of B, all of which it asks for at once (they fit in shared memory); it
+// computes its share of h, gives it to every CTA of the cluster, and after one barrier each has h and computes its columns of out.
+// Nothing but that barrier and the segment's numbers stands between the launch and the loads.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "adapter_rows.h"
+
+namespace gpd {
+namespace adapter {
+
+namespace {
+
+constexpr int kThreads = 128, kWarps = 4, kBlockCols = 64, kMostSplits = 8;
+
+__device__ int g_short_status = 0;                     // GPD_ERR_TIMEOUT if a bounded wait expired
+
+struct ShortArgs {
+    ShrinkArgs down;
+    ExpandArgs above;
+    int blocks_a, blocks_b;                            // blocks of 64 columns of A and rows of B that a CTA has at most
+};
+template <int NT>
+struct Shape {
+    static constexpr int RP = 8 * NT, X = 16 * 128;
+    using A = WTile<RP, kBlockCols>;
+    using B = WTile<kBlockCols, RP>;
+    static constexpr int SUMS = (kWarps + kMostSplits + 1) * 16 * RP * 4;              // the warps' shares, the CTAs', h
+    static int bytes(int blocks_a, int blocks_b) { return blocks_a * (X + A::BYTES) + blocks_b * B::BYTES + SUMS + 1024; }
+};
+
+template <typename T, typename O, int NT, int PARTS>
+__global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
+                                                         const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ShortArgs s, int splits) {
+    using S = Shape<NT>;
+    constexpr int KT = S::RP / 16;
+    extern __shared__ unsigned char raw[];
+    __shared__ uint64_t ready_a[kWarps], ready_b[kWarps];
+    __shared__ int abort;
+    unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
+    const int rank = blockIdx.x % splits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
+    if (threadIdx.x < kWarps) {
+        tc::mbar_init(&ready_a[threadIdx.x], 1);
+        tc::mbar_init(&ready_b[threadIdx.x], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 0) abort = 0;
+    __syncthreads();
+    after_previous();
+    const ShrinkArgs& down = s.down;
+    const ExpandArgs& above = s.above;
+    const RowTile tile = find_tile<16>(down.seg, blockIdx.x / splits);
+    if (tile.rows == 0) return;                        // the whole cluster
+    const bool none = tile.id < 0 || tile.id >= down.seg.n;
+    // the CTAs of a cluster write to each other only when all of them have come this far
+    if (!none) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const bool has[2] = {g < tile.rows, g + 8 < tile.rows};
+    // this CTA's blocks of A's columns and of B's rows; a warp has every fourth
+    const int all_a = (int)((down.C + kBlockCols - 1) / kBlockCols), all_b = (int)((above.C + kBlockCols - 1) / kBlockCols);
+    const int a0 = (int)((int64_t)all_a * rank / splits), a1 = (int)((int64_t)all_a * (rank + 1) / splits);
+    const int b0 = (int)((int64_t)all_b * rank / splits), b1 = (int)((int64_t)all_b * (rank + 1) / splits);
+    unsigned char* xs = smem;
+    unsigned char* as = xs + s.blocks_a * S::X;
+    unsigned char* bs = as + s.blocks_a * S::A::BYTES;
+    float* shares = reinterpret_cast<float*>(bs + s.blocks_b * S::B::BYTES);           // [4][16][RP]
+    float* given = shares + kWarps * 16 * S::RP;       // [splits][16][RP]
+    float* h = given + kMostSplits * 16 * S::RP;       // [16][RP]
+    if (!none && lane == 0) {
+        const int na = a0 + warp < a1 ? (a1 - a0 - warp + kWarps - 1) / kWarps : 0, nb = b0 + warp < b1 ? (b1 - b0 - warp + kWarps - 1) / kWarps : 0;
+        tc::mbar_expect_tx(&ready_a[warp], na * (S::X + S::A::BYTES));
+        tc::mbar_expect_tx(&ready_b[warp], nb * S::B::BYTES);
+        for (int i = warp; i < a1 - a0; i += kWarps) {
+            S::A::load(as + i * S::A::BYTES, &map_a, (a0 + i) * kBlockCols, 0, (int)tile.id, &ready_a[warp]);
+            tc::tma_load_3d(xs + i * S::X, &map_x, (a0 + i) * kBlockCols, (int)tile.row, 0, &ready_a[warp]);
+        }
+        for (int i = warp; i < b1 - b0; i += kWarps) S::B::load(bs + i * S::B::BYTES, &map_b, 0, (b0 + i) * kBlockCols, (int)tile.id, &ready_b[warp]);
+    }
+    const O* base = above.base ? static_cast<const O*>(above.base) + (tile.row + g) * above.ldb : nullptr;
+    O* out = static_cast<O*>(above.out) + (tile.row + g) * above.ldo;
+    auto columns = [&](int i) { return b0 + i < b1 ? above.C - (int64_t)(b0 + i) * kBlockCols : 0; };
+    Share<O> next;
+    load_share<O>(next, base ? base + (int64_t)(b0 + warp) * kBlockCols : nullptr, above.ldb, has, columns(warp), above.io_vec);
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    if (!none) {
+        float sum[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[n][i] = 0.f;
+        bool live = tc::mbar_wait(&ready_a[warp], 0, &abort, &g_short_status);
+        for (int i = warp; live && i < a1 - a0; i += kWarps) {
+            const uint32_t xa = WTile<16, kBlockCols>::lane_at(smem_at(xs + i * S::X), row_first(), row_first_col());
+            const uint32_t aa = S::A::lane_at(smem_at(as + i * S::A::BYTES), col_first_row(), col_first());
+            float acc[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[n][j] = 0.f;
+#pragma unroll
+            for (int k = 0; k < kBlockCols / 16; ++k) {
+                uint32_t x[4];
+                ldmatrix4<false>(x, WTile<16, kBlockCols>::on(xa, 0, 16 * k));
+#pragma unroll
+                for (int p = 0; p < NT / 2; ++p) {
+                    uint32_t b[4];
+                    ldmatrix4<false>(b, S::A::on(aa, 16 * p, 16 * k));
+                    mma(acc[2 * p], x, b[0], b[1], T());
+                    mma(acc[2 * p + 1], x, b[2], b[3], T());
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[n][j] += acc[n][j];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float* p = shares + (16 * warp + g) * S::RP + 8 * n + 2 * (lane & 3);
+            *reinterpret_cast<float2*>(p) = make_float2(sum[n][0], sum[n][1]);
+            *reinterpret_cast<float2*>(p + 8 * S::RP) = make_float2(sum[n][2], sum[n][3]);
+        }
+        __syncthreads();
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        for (int e = threadIdx.x; e < tile.rows * S::RP; e += kThreads) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) v += shares[w * 16 * S::RP + e];
+            for (int c = 0; c < splits; ++c) *cluster.map_shared_rank(given + rank * 16 * S::RP + e, c) = v;
+        }
+        // no CTA writes to another after this barrier, so none has to wait for the others at its end
+        cluster.sync();
+        for (int e = threadIdx.x; e < 16 * S::RP; e += kThreads) {
+            float v = 0.f;
+            if (e < tile.rows * S::RP)
+                for (int c = 0; c < splits; ++c) v += given[c * 16 * S::RP + e];
+            h[e] = v;
+        }
+        __syncthreads();
+    }
+    if (rank == 0)
+        for (int e = threadIdx.x; e < tile.rows * down.r; e += kThreads) {
+            const int row = e / down.r, c = e - row * down.r;
+            down.h[tile.row * down.r + e] = none ? (tile.id < 0 ? 0.f : __int_as_float(0x7fffffff)) : h[row * S::RP + c];
+        }
+    uint32_t ha[PARTS][KT][4];
+    float undo[2];
+    load_parts<T, KT, PARTS>(h + g * S::RP, none ? 0 : S::RP, none || !above.scale ? 1.f : above.scale[tile.id], has, ha, undo);
+    const float nothing = tile.id >= down.seg.n ? __int_as_float(0x7fffffff) : 0.f;
+    const bool live = none || tc::mbar_wait(&ready_b[warp], 0, &abort, &g_short_status);
+    for (int i = warp; live && i < b1 - b0; i += kWarps) {
+        const Share<O> share = next;
+        load_share<O>(next, base ? base + (int64_t)(b0 + i + kWarps) * kBlockCols : nullptr, above.ldb, has, columns(i + kWarps), above.io_vec);
+        float acc[8][4];
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[n][j] = nothing;
+        if (!none) {
+            const uint32_t bb = S::B::lane_at(smem_at(bs + i * S::B::BYTES), col_first_row(), col_first());
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    uint32_t b[4];
+                    ldmatrix4<false>(b, S::B::on(bb, 16 * p, 16 * k));
+#pragma unroll
+                    for (int j = PARTS - 1; j >= 0; --j) {             // the small parts first
+                        mma(acc[2 * p], ha[j][k], b[0], b[1], T());
+                        mma(acc[2 * p + 1], ha[j][k], b[2], b[3], T());
+                    }
+                }
+            if (std::is_same<T, __half>::value) {
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[n][j] *= undo[j >> 1];
+            }
+        }
+        const int64_t c = (int64_t)(b0 + i) * kBlockCols;
+        store_sum<O>(share, acc, out + c, above.ldo, has, above.C - c, above.io_vec);
+    }
+    if (!none && *static_cast<volatile int*>(&abort)) {                // given up: copies in flight land before the CTA ends
+        int never = 0;
+        tc::mbar_wait(&ready_a[warp], 0, &never, &g_short_status);
+        tc::mbar_wait(&ready_b[warp], 0, &never, &g_short_status);
+    }
+}
+
+template <typename T, typename O, int NT>
+gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st) {
+    using S = Shape<NT>;
+    constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
+    const int64_t tiles = tiles_of(down.seg, 16), all_a = (down.C + kBlockCols - 1) / kBlockCols, all_b = (above.C + kBlockCols - 1) / kBlockCols;
+    // Eight CTAs per tile while all of them are resident at once, fewer for more tiles as long as their parts fit.
+    constexpr int kRoom = 220 * 1024;
+    auto bytes = [&](int n) {
+        const int64_t a = (all_a + n - 1) / n, b = (all_b + n - 1) / n;
+        return a > 4096 || b > 4096 ? INT32_MAX : S::bytes((int)a, (int)b);
+    };
+    int splits = kMostSplits;
+    while (splits > 1 && tiles * splits > 4 * sm_count() && bytes(splits / 2) <= kRoom / 3) splits /= 2;
+    while (splits > 1 && (all_a < splits || all_b < splits)) splits /= 2;
+    const int smem = bytes(splits);
+    *taken = smem <= kRoom;
+    if (!*taken) return GPD_OK;
+    if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
+    ShortArgs s{down, above, (int)((all_a + splits - 1) / splits), (int)((all_b + splits - 1) / splits)};
+    CUtensorMap map_x, map_a, map_b;
+    if (!make_map(&map_x, down.x, 2, 1, down.seg.T, down.C, down.ldx, 0, 16, kBlockCols)) return GPD_ERR_CUDA;
+    map_a = map_b = map_x;                             // without adapters they are not used
+    if (down.seg.n > 0 && (!make_map(&map_a, down.w, 2, down.seg.n, down.r, down.C, down.ldw, down.next, S::RP, kBlockCols) ||
+                           !make_map(&map_b, above.w, 2, down.seg.n, above.C, above.r, above.ldw, above.next, kBlockCols, S::B::PITCH / 2)))
+        return GPD_ERR_CUDA;
+    auto kernel = short_kernel<T, O, NT, PARTS>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), smem, splits, st, map_x, map_a, map_b, s, splits);
+}
+template <typename T, typename O>
+gpd_status launch_rank(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st) {
+    if (down.r <= 16) return launch<T, O, 2>(down, above, taken, st);
+    if (down.r <= 32) return launch<T, O, 4>(down, above, taken, st);
+    return down.r <= 64 ? launch<T, O, 8>(down, above, taken, st) : launch<T, O, 16>(down, above, taken, st);
+}
+
+}  // namespace
+
+int short_status_fetch_and_clear() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_short_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
+    if (v != 0) cudaMemcpyToSymbol(g_short_status, &zero, sizeof(int));
+    return v;
+}
+
+// Segments of 16 rows and less on average, everything but base and out on 16-byte boundaries; *taken: it was done here.
+gpd_status short_segments(int type, int out_type, const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st) {
+    *taken = false;
+    if (down.seg.T > 16 * (int64_t)down.seg.S || !down.x_vec || !down.w_vec || !above.w_vec) return GPD_OK;
+    if (type == GPD_DT_BF16)
+        return out_type == GPD_DT_F32 ? launch_rank<__nv_bfloat16, float>(down, above, taken, st)
+                                      : launch_rank<__nv_bfloat16, __nv_bfloat16>(down, above, taken, st);
+    return out_type == GPD_DT_F32 ? launch_rank<__half, float>(down, above, taken, st) : launch_rank<__half, __half>(down, above, taken, st);
+}
+
+}  // namespace adapter
+}  // namespace gpd

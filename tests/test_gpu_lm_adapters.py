@@ -143,6 +143,10 @@ CASES = {
     "one row": dict(lens=[1], index=[0], n=1, r=16, K=256, N=256),
     "one row each": dict(lens=[1] * 37, index=[(7 * i) % 40 for i in range(37)], n=40, r=16, K=1024, N=512),
     "one row each f16, adapters shared": dict(lens=[1] * 20, index=[i % 3 for i in range(20)], n=3, r=8, K=512, N=1000, type=F16),
+    "one row each, many, wide factors": dict(**ragged(300, 290, 17, 20, True), r=32, K=1416, N=2000),
+    "one row each, too wide to be held": dict(lens=[1, 2, 1], index=[2, 0, 1], n=3, r=128, K=8192, N=4096),
+    "few rows each f32 out": dict(**ragged(90, 13, 5, 21), r=64, K=200, N=72, out=F32, before=3, behind=4),
+    "few rows each rank 128": dict(**ragged(60, 9, 5, 22), r=128, K=512, N=576, type=F16),
     "short": dict(lens=[3, 0, 16, 17, 1, 40, 2], index=[1, 0, -1, 2, 2, 0, 1], n=3, r=32, K=320, N=704, wide=True),
     "ragged": dict(**ragged(700, 5, 3, 1, True), r=64, K=512, N=768),
     "ragged f16, f32 out": dict(**ragged(515, 4, 2, 2), r=16, K=640, N=256, type=F16, out=F32),
