@@ -27,16 +27,16 @@ struct ShortArgs {
 };
 template <int NT>
 struct Shape {
-    static constexpr int RP = 8 * NT, X = 16 * 128;
+    static constexpr int RP = 8 * NT;
     using A = WTile<RP, kBlockCols>;
     using B = WTile<kBlockCols, RP>;
     static constexpr int SUMS = (kWarps + kMostSplits + 1) * 16 * RP * 4;              // the warps' shares, the CTAs', h
-    static int bytes(int blocks_a, int blocks_b) { return blocks_a * (X + A::BYTES) + blocks_b * B::BYTES + SUMS + 1024; }
+    static int bytes(int blocks_a, int blocks_b) { return blocks_a * A::BYTES + blocks_b * B::BYTES + SUMS + 1024; }
 };
 
 template <typename T, typename O, int NT, int PARTS>
-__global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
-                                                         const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ShortArgs s, int splits) {
+__global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                         const __grid_constant__ ShortArgs s, int splits) {
     using S = Shape<NT>;
     constexpr int KT = S::RP / 16;
     extern __shared__ unsigned char raw[];
@@ -64,20 +64,16 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
     const int all_a = (int)((down.C + kBlockCols - 1) / kBlockCols), all_b = (int)((above.C + kBlockCols - 1) / kBlockCols);
     const int a0 = (int)((int64_t)all_a * rank / splits), a1 = (int)((int64_t)all_a * (rank + 1) / splits);
     const int b0 = (int)((int64_t)all_b * rank / splits), b1 = (int)((int64_t)all_b * (rank + 1) / splits);
-    unsigned char* xs = smem;
-    unsigned char* as = xs + s.blocks_a * S::X;
+    unsigned char* as = smem;
     unsigned char* bs = as + s.blocks_a * S::A::BYTES;
     float* shares = reinterpret_cast<float*>(bs + s.blocks_b * S::B::BYTES);           // [4][16][RP]
     float* given = shares + kWarps * 16 * S::RP;       // [splits][16][RP]
     float* h = given + kMostSplits * 16 * S::RP;       // [16][RP]
     if (!none && lane == 0) {
         const int na = a0 + warp < a1 ? (a1 - a0 - warp + kWarps - 1) / kWarps : 0, nb = b0 + warp < b1 ? (b1 - b0 - warp + kWarps - 1) / kWarps : 0;
-        tc::mbar_expect_tx(&ready_a[warp], na * (S::X + S::A::BYTES));
+        tc::mbar_expect_tx(&ready_a[warp], na * S::A::BYTES);
         tc::mbar_expect_tx(&ready_b[warp], nb * S::B::BYTES);
-        for (int i = warp; i < a1 - a0; i += kWarps) {
-            S::A::load(as + i * S::A::BYTES, &map_a, (a0 + i) * kBlockCols, 0, (int)tile.id, &ready_a[warp]);
-            tc::tma_load_3d(xs + i * S::X, &map_x, (a0 + i) * kBlockCols, (int)tile.row, 0, &ready_a[warp]);
-        }
+        for (int i = warp; i < a1 - a0; i += kWarps) S::A::load(as + i * S::A::BYTES, &map_a, (a0 + i) * kBlockCols, 0, (int)tile.id, &ready_a[warp]);
         for (int i = warp; i < b1 - b0; i += kWarps) S::B::load(bs + i * S::B::BYTES, &map_b, 0, (b0 + i) * kBlockCols, (int)tile.id, &ready_b[warp]);
     }
     const O* base = above.base ? static_cast<const O*>(above.base) + (tile.row + g) * above.ldb : nullptr;
@@ -92,9 +88,26 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[n][i] = 0.f;
+        // the lane's elements of x: rows g and g + 8, columns 2 q and the next, and eight on, of sixteen; a block ahead
+        uint32_t x[2][kBlockCols / 16][4];
+        const T* row = static_cast<const T*>(down.x) + (tile.row + g) * down.ldx + 2 * (lane & 3);
+        auto load_x = [&](int i, uint32_t (&to)[kBlockCols / 16][4]) {
+#pragma unroll
+            for (int k = 0; k < kBlockCols / 16; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int64_t c = (int64_t)(a0 + i) * kBlockCols + 16 * k + 8 * (j >> 1);
+                    const int64_t left = a0 + i < a1 ? down.C - c - 2 * (lane & 3) : 0;
+                    const T* p = row + 8 * (j & 1) * down.ldx + c;
+                    to[k][j] = 0;
+                    if (has[j & 1] && left > 1) to[k][j] = *reinterpret_cast<const uint32_t*>(p);
+                    else if (has[j & 1] && left == 1) to[k][j] = *reinterpret_cast<const unsigned short*>(p);
+                }
+        };
+        load_x(warp, x[0]);
         bool live = tc::mbar_wait(&ready_a[warp], 0, &abort, &g_short_status);
         for (int i = warp; live && i < a1 - a0; i += kWarps) {
-            const uint32_t xa = WTile<16, kBlockCols>::lane_at(smem_at(xs + i * S::X), row_first(), row_first_col());
+            load_x(i + kWarps, x[1]);
             const uint32_t aa = S::A::lane_at(smem_at(as + i * S::A::BYTES), col_first_row(), col_first());
             float acc[NT][4];
 #pragma unroll
@@ -103,20 +116,22 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
                 for (int j = 0; j < 4; ++j) acc[n][j] = 0.f;
 #pragma unroll
             for (int k = 0; k < kBlockCols / 16; ++k) {
-                uint32_t x[4];
-                ldmatrix4<false>(x, WTile<16, kBlockCols>::on(xa, 0, 16 * k));
 #pragma unroll
                 for (int p = 0; p < NT / 2; ++p) {
                     uint32_t b[4];
                     ldmatrix4<false>(b, S::A::on(aa, 16 * p, 16 * k));
-                    mma(acc[2 * p], x, b[0], b[1], T());
-                    mma(acc[2 * p + 1], x, b[2], b[3], T());
+                    mma(acc[2 * p], x[0][k], b[0], b[1], T());
+                    mma(acc[2 * p + 1], x[0][k], b[2], b[3], T());
                 }
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum[n][j] += acc[n][j];
+#pragma unroll
+            for (int k = 0; k < kBlockCols / 16; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[0][k][j] = x[1][k][j];
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -197,7 +212,7 @@ gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, 
     constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
     const int64_t tiles = tiles_of(down.seg, 16), all_a = (down.C + kBlockCols - 1) / kBlockCols, all_b = (above.C + kBlockCols - 1) / kBlockCols;
     // Eight CTAs per tile while all of them are resident at once, fewer for more tiles as long as their parts fit.
-    constexpr int kRoom = 220 * 1024;
+    constexpr int kRoom = 220 * 1024;                  // of shared memory, and a third of it
     auto bytes = [&](int n) {
         const int64_t a = (all_a + n - 1) / n, b = (all_b + n - 1) / n;
         return a > 4096 || b > 4096 ? INT32_MAX : S::bytes((int)a, (int)b);
@@ -210,15 +225,13 @@ gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, 
     if (!*taken) return GPD_OK;
     if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
     ShortArgs s{down, above, (int)((all_a + splits - 1) / splits), (int)((all_b + splits - 1) / splits)};
-    CUtensorMap map_x, map_a, map_b;
-    if (!make_map(&map_x, down.x, 2, 1, down.seg.T, down.C, down.ldx, 0, 16, kBlockCols)) return GPD_ERR_CUDA;
-    map_a = map_b = map_x;                             // without adapters they are not used
+    CUtensorMap map_a{}, map_b{};                      // without adapters they are not used
     if (down.seg.n > 0 && (!make_map(&map_a, down.w, 2, down.seg.n, down.r, down.C, down.ldw, down.next, S::RP, kBlockCols) ||
                            !make_map(&map_b, above.w, 2, down.seg.n, above.C, above.r, above.ldw, above.next, kBlockCols, S::B::PITCH / 2)))
         return GPD_ERR_CUDA;
     auto kernel = short_kernel<T, O, NT, PARTS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
-    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), smem, splits, st, map_x, map_a, map_b, s, splits);
+    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), smem, splits, st, map_a, map_b, s, splits);
 }
 template <typename T, typename O>
 gpd_status launch_rank(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st) {
