@@ -21,50 +21,49 @@ struct Segments {
     int S, n;                                          // segments, adapters
     bool wide;                                         // 8-byte numbers
 };
-// A row tile: rows of one segment.  rows 0: none.  adapter -1: the segment has none; >= n: there is no such adapter.
+// A row tile: rows of one segment.  rows 0: none.  adapter -1: the segment has none; n: there is no such adapter.  Rows and
+// adapters are below 2^31.
 struct RowTile {
-    int64_t row;
-    int rows;
-    int64_t id;
+    int row, rows, id;
 };
 __device__ __forceinline__ int64_t number(const void* p, int64_t i, bool wide) {
     return wide ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
 }
-__device__ __forceinline__ int64_t offset_at(const Segments& s, int64_t i) {
+__device__ __forceinline__ int offset_at(const Segments& s, int64_t i) {
     const int64_t v = number(s.offsets, i, s.wide);
-    return v < 0 ? 0 : v > s.T ? s.T : v;              // whatever stands there, rows stay inside the batch
+    return (int)(v < 0 ? 0 : v > s.T ? s.T : v);       // whatever stands there, rows stay inside the batch
+}
+__device__ __forceinline__ int adapter_at(const Segments& s, int64_t i) {
+    const int64_t v = number(s.index, i, s.wide);
+    return v < 0 ? -1 : v >= s.n ? s.n : (int)v;
 }
 // How many tiles of TM rows the segments have.  Every warp works it out by itself.
 template <int TM>
 __device__ __forceinline__ int64_t count_tiles(const Segments& s) {
-    int64_t n = 0;
+    int n = 0;
 #pragma unroll 4
-    for (int64_t i = threadIdx.x & 31; i < s.S; i += 32) {
-        const int64_t rows = offset_at(s, i + 1) - offset_at(s, i);
+    for (int i = threadIdx.x & 31; i < s.S; i += 32) {
+        const int rows = offset_at(s, i + 1) - offset_at(s, i);
         if (rows > 0) n += (rows + TM - 1) / TM;
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-    return n;
+    return __reduce_add_sync(0xffffffffu, n);
 }
 // Tile number `tile` of the segments' tiles of TM rows.  Every warp works it out by itself: 128 segments per round.
 template <int TM>
-__device__ __forceinline__ RowTile find_tile(const Segments& s, int64_t tile) {
+__device__ __forceinline__ RowTile find_tile(const Segments& s, int tile) {
     const int lane = threadIdx.x & 31;
     RowTile r{0, 0, -1};
-    int64_t before = 0;
-    for (int64_t base = 0; base < s.S; base += 128) {
-        int64_t at[5], id[4];
-        int n[4], sum = 0;
+    for (int base = 0; base < s.S; base += 128) {
+        int at[5], id[4], n[4], sum = 0;
 #pragma unroll
         for (int j = 0; j < 5; ++j) {
-            const int64_t i = base + lane * 4 + j;
-            at[j] = offset_at(s, i < s.S ? i : s.S);
-            if (j < 4) id[j] = i < s.S ? number(s.index, i, s.wide) : -1;
+            const int i = base + lane * 4 + j;
+            at[j] = offset_at(s, min(i, s.S));
+            if (j < 4) id[j] = i < s.S ? adapter_at(s, i) : -1;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            n[j] = at[j + 1] > at[j] ? (int)((at[j + 1] - at[j] + TM - 1) / TM) : 0;
+            n[j] = at[j + 1] > at[j] ? (at[j + 1] - at[j] + TM - 1) / TM : 0;
             sum += n[j];
         }
         int scan = sum;
@@ -73,27 +72,25 @@ __device__ __forceinline__ RowTile find_tile(const Segments& s, int64_t tile) {
             const int v = __shfl_up_sync(0xffffffffu, scan, o);
             if (lane >= o) scan += v;
         }
-        const int total = __shfl_sync(0xffffffffu, scan, 31);
-        if (tile < before + total) {
-            int64_t from = before + scan - sum;
-            const uint32_t has = __ballot_sync(0xffffffffu, tile < before + scan);
-            const int who = __ffs(has) - 1;            // the first lane whose segments reach the tile
+        const uint32_t has = __ballot_sync(0xffffffffu, tile < scan);
+        if (has) {
+            int from = scan - sum;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (tile >= from && tile < from + n[j]) {
                     r.row = at[j] + (tile - from) * TM;
-                    const int64_t left = at[j + 1] - r.row;
-                    r.rows = left < TM ? (int)left : TM;
+                    r.rows = min(TM, at[j + 1] - r.row);
                     r.id = id[j];
                 }
                 from += n[j];
             }
+            const int who = __ffs(has) - 1;            // the first lane whose segments reach the tile
             r.row = __shfl_sync(0xffffffffu, r.row, who);
             r.rows = __shfl_sync(0xffffffffu, r.rows, who);
             r.id = __shfl_sync(0xffffffffu, r.id, who);
             return r;
         }
-        before += total;
+        tile -= __shfl_sync(0xffffffffu, scan, 31);
     }
     return r;
 }

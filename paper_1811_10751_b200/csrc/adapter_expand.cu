@@ -33,11 +33,11 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant_
     extern __shared__ __align__(128) unsigned char smem[];
     after_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
-    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x);
+    const RowTile tile = find_tile<S::TM>(a.seg, (int)blockIdx.x);
     if (tile.rows == 0) return;
     const bool none = tile.id < 0 || tile.id >= a.seg.n;
     if (tile.id < 0 && a.base == a.out) return;
-    const T* w = none ? nullptr : static_cast<const T*>(a.w) + tile.id * a.next;
+    const T* w = none ? nullptr : static_cast<const T*>(a.w) + (int64_t)tile.id * a.next;
     const int64_t chunks = (a.C + S::COLS - 1) / S::COLS;
     const int64_t from = chunks * blockIdx.y / gridDim.y, to = chunks * (blockIdx.y + 1) / gridDim.y;
     const uint32_t ring = smem_at(smem);
@@ -57,14 +57,14 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant_
     const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows};
     uint32_t ha[PARTS][KT][4];
     float undo[2];
-    load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
-    const O* base = a.base ? static_cast<const O*>(a.base) + (tile.row + row0) * a.ldb : nullptr;
-    O* out = static_cast<O*>(a.out) + (tile.row + row0) * a.ldo;
+    load_parts<T, KT, PARTS>(a.h + (int64_t)(tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
+    const O* base = a.base ? static_cast<const O*>(a.base) + (int64_t)(tile.row + row0) * a.ldb : nullptr;
+    O* out = static_cast<O*>(a.out) + (int64_t)(tile.row + row0) * a.ldo;
 
     Share<O> next;
     auto load_base = [&](int64_t k, Share<O>& s) {
         const int64_t c = k * S::COLS + (WM == 1 ? kCols * warp : 0);
-        load_share<O>(s, base ? base + c : nullptr, a.ldb, has, k < to ? a.C - c : 0, a.io_vec);
+        load_share<O>(s, base ? base + c : nullptr, a.ldb, has, k < to ? (int)min((int64_t)kCols, a.C - c) : 0, a.io_vec);
     };
     load_base(from, next);
     const float nan = __int_as_float(0x7fffffff);
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const __grid_constant_
             }
         }
         const int64_t c = k * S::COLS + wc;
-        store_sum<O>(share, acc, out + c, a.ldo, has, a.C - c, a.io_vec);
+        store_sum<O>(share, acc, out + c, a.ldo, has, (int)min((int64_t)kCols, a.C - c), a.io_vec, true);
     }
     copies_wait<0>();
 }
@@ -160,9 +160,9 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     const int64_t last = all * (blockIdx.x + 1) / gridDim.x;
     int k = 0;                                         // stages so far
     for (int64_t at = all * blockIdx.x / gridDim.x, end; at < last; at = end) {
-        const int64_t number = at / chunks;
-        end = min(last, (number + 1) * chunks);
-        const int first = (int)(at - number * chunks), n = (int)(end - at);
+        const int number = (int)(at / chunks);
+        end = min(last, (int64_t)(number + 1) * chunks);
+        const int first = (int)(at - (int64_t)number * chunks), n = (int)(end - at);
         const RowTile tile = find_tile<S::TM>(a.seg, number);
         const bool none = tile.id < 0 || tile.id >= a.seg.n;
         if (tile.id < 0 && a.base == a.out) continue;
@@ -183,7 +183,7 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                 }
                 if (!a.w_vec) {
                     if (!none) {
-                        const T* w = static_cast<const T*>(a.w) + tile.id * a.next + (TRANS ? c : c * a.ldw);
+                        const T* w = static_cast<const T*>(a.w) + (int64_t)tile.id * a.next + (TRANS ? c : c * a.ldw);
                         if (TRANS) S::W::copy(ws, w, a.ldw, a.r, a.C - c, a.r, kCols);
                         else S::W::copy(ws, w, a.ldw, a.C - c, a.r, kCols, a.r);
                     }
@@ -198,7 +198,7 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows}, whole = 16 * warp + 16 <= tile.rows, any = 16 * warp < tile.rows;
         uint32_t ha[PARTS][KT][4];
         float undo[2];
-        load_parts<T, KT, PARTS>(a.h + (tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
+        load_parts<T, KT, PARTS>(a.h + (int64_t)(tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
         for (int i = 0; i < n; ++i, ++k) {
             if (!ring.wait_full(k, &g_expand_status)) break;
             const uint32_t stage = smem_at(smem) + k % S::STAGES * S::STAGE, mine = stage + 16 * warp * 128;
@@ -290,7 +290,7 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                             uint4 v;
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                                          : "r"(mine + b * S::TM * 128 + swizzled<128>(r * 128 + (j & 7) * 16)) : "memory");
-                            O* p = static_cast<O*>(a.out) + (tile.row + 16 * warp + r) * a.ldo + c;
+                            O* p = static_cast<O*>(a.out) + (int64_t)(tile.row + 16 * warp + r) * a.ldo + c;
                             if (c + 16 / (int)sizeof(O) <= a.C) {
                                 *reinterpret_cast<uint4*>(p) = v;
                             } else {

@@ -37,7 +37,7 @@ template <typename O> struct Share { uint4 v[2][2]; };                 // [32 co
 template <> struct Share<float> { float2 v[8][2]; };                   // [8 columns][row]: two elements
 // base: row g, from column c0 - of which `cols` exist (<= 0: none); null: zeros.  vec: 16-byte (FP32: 8-byte) boundaries.
 template <typename O>
-__device__ __forceinline__ void load_share(Share<O>& s, const O* base, int64_t ld, const bool (&has)[2], int64_t cols, bool vec) {
+__device__ __forceinline__ void load_share(Share<O>& s, const O* base, int64_t ld, const bool (&has)[2], int cols, bool vec) {
     const int q = threadIdx.x & 3;
     if constexpr (sizeof(O) == 4) {
 #pragma unroll
@@ -60,14 +60,15 @@ __device__ __forceinline__ void load_share(Share<O>& s, const O* base, int64_t l
                 s.v[n][i] = make_uint4(0, 0, 0, 0);
                 if (!base || !has[i] || c >= cols) continue;
                 const O* p = base + 8 * i * ld + c;
-                const int left = (int)min((int64_t)8, cols - c);
-                s.v[n][i] = vec ? load8<O, true>(p, left).v : load8<O, false>(p, left).v;
+                s.v[n][i] = vec ? load8<O, true>(p, cols - c).v : load8<O, false>(p, cols - c).v;
             }
     }
 }
-// out = share + acc, acc[n]: columns 8 n + 2 q and the next of row g, and of row g + 8.  All lanes call it.
+// out = share + acc, acc[n]: columns 8 n + 2 q and the next of row g, and of row g + 8 (`both`: any lane has one).  All lanes
+// call it.
 template <typename O>
-__device__ __forceinline__ void store_sum(const Share<O>& s, const float (&acc)[8][4], O* out, int64_t ld, const bool (&has)[2], int64_t cols, bool vec) {
+__device__ __forceinline__ void store_sum(const Share<O>& s, const float (&acc)[8][4], O* out, int64_t ld, const bool (&has)[2], int cols, bool vec,
+                                          bool both) {
     const int q = threadIdx.x & 3;
     if constexpr (sizeof(O) == 4) {
 #pragma unroll
@@ -87,9 +88,10 @@ __device__ __forceinline__ void store_sum(const Share<O>& s, const float (&acc)[
             }
     } else {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int i = 0; i < 2; ++i) {
+            if (i == 1 && !both) break;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int n = 0; n < 2; ++n) {
                 uint32_t b[4] = {s.v[n][i].x, s.v[n][i].y, s.v[n][i].z, s.v[n][i].w};
                 transpose4(b);
 #pragma unroll
@@ -110,6 +112,7 @@ __device__ __forceinline__ void store_sum(const Share<O>& s, const float (&acc)[
                         if (c + j < cols) to[j] = (unsigned short)(b[j / 2] >> (16 * (j & 1)));
                 }
             }
+        }
     }
 }
 

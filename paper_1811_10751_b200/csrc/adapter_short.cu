@@ -24,6 +24,7 @@ struct ShortArgs {
     ShrinkArgs down;
     ExpandArgs above;
     int blocks_a, blocks_b;                            // blocks of 64 columns of A and rows of B that a CTA has at most
+    int all_a, all_b;                                  // and all of them
 };
 template <int NT>
 struct Shape {
@@ -36,14 +37,14 @@ struct Shape {
 
 template <typename T, typename O, int NT, int PARTS>
 __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                         const __grid_constant__ ShortArgs s, int splits) {
+                                                         const __grid_constant__ ShortArgs s, int log_splits) {
     using S = Shape<NT>;
     constexpr int KT = S::RP / 16;
     extern __shared__ unsigned char raw[];
     __shared__ uint64_t ready_a[kWarps], ready_b[kWarps];
     __shared__ int abort;
     unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
-    const int rank = blockIdx.x % splits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
+    const int splits = 1 << log_splits, rank = blockIdx.x & (splits - 1), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
     if (threadIdx.x < kWarps) {
         tc::mbar_init(&ready_a[threadIdx.x], 1);
         tc::mbar_init(&ready_b[threadIdx.x], 1);
@@ -54,31 +55,32 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
     after_previous();
     const ShrinkArgs& down = s.down;
     const ExpandArgs& above = s.above;
-    const RowTile tile = find_tile<16>(down.seg, blockIdx.x / splits);
+    const RowTile tile = find_tile<16>(down.seg, blockIdx.x >> log_splits);
     if (tile.rows == 0) return;                        // the whole cluster
     const bool none = tile.id < 0 || tile.id >= down.seg.n;
     // the CTAs of a cluster write to each other only when all of them have come this far
     if (!none) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const bool has[2] = {g < tile.rows, g + 8 < tile.rows};
     // this CTA's blocks of A's columns and of B's rows; a warp has every fourth
-    const int all_a = (int)((down.C + kBlockCols - 1) / kBlockCols), all_b = (int)((above.C + kBlockCols - 1) / kBlockCols);
-    const int a0 = (int)((int64_t)all_a * rank / splits), a1 = (int)((int64_t)all_a * (rank + 1) / splits);
-    const int b0 = (int)((int64_t)all_b * rank / splits), b1 = (int)((int64_t)all_b * (rank + 1) / splits);
+    const int a0 = s.all_a * rank >> log_splits, na = (s.all_a * (rank + 1) >> log_splits) - a0;
+    const int b0 = s.all_b * rank >> log_splits, nb = (s.all_b * (rank + 1) >> log_splits) - b0;
     unsigned char* as = smem;
     unsigned char* bs = as + s.blocks_a * S::A::BYTES;
     float* shares = reinterpret_cast<float*>(bs + s.blocks_b * S::B::BYTES);           // [4][16][RP]
     float* given = shares + kWarps * 16 * S::RP;       // [splits][16][RP]
     float* h = given + kMostSplits * 16 * S::RP;       // [16][RP]
     if (!none && lane == 0) {
-        const int na = a0 + warp < a1 ? (a1 - a0 - warp + kWarps - 1) / kWarps : 0, nb = b0 + warp < b1 ? (b1 - b0 - warp + kWarps - 1) / kWarps : 0;
-        tc::mbar_expect_tx(&ready_a[warp], na * S::A::BYTES);
-        tc::mbar_expect_tx(&ready_b[warp], nb * S::B::BYTES);
-        for (int i = warp; i < a1 - a0; i += kWarps) S::A::load(as + i * S::A::BYTES, &map_a, (a0 + i) * kBlockCols, 0, (int)tile.id, &ready_a[warp]);
-        for (int i = warp; i < b1 - b0; i += kWarps) S::B::load(bs + i * S::B::BYTES, &map_b, 0, (b0 + i) * kBlockCols, (int)tile.id, &ready_b[warp]);
+        tc::mbar_expect_tx(&ready_a[warp], (na - warp + kWarps - 1) / kWarps * S::A::BYTES);
+        tc::mbar_expect_tx(&ready_b[warp], (nb - warp + kWarps - 1) / kWarps * S::B::BYTES);
+#pragma unroll 1
+        for (int i = warp; i < na; i += kWarps) S::A::load(as + i * S::A::BYTES, &map_a, (a0 + i) * kBlockCols, 0, tile.id, &ready_a[warp]);
+#pragma unroll 1
+        for (int i = warp; i < nb; i += kWarps) S::B::load(bs + i * S::B::BYTES, &map_b, 0, (b0 + i) * kBlockCols, tile.id, &ready_b[warp]);
     }
-    const O* base = above.base ? static_cast<const O*>(above.base) + (tile.row + g) * above.ldb : nullptr;
-    O* out = static_cast<O*>(above.out) + (tile.row + g) * above.ldo;
-    auto columns = [&](int i) { return b0 + i < b1 ? above.C - (int64_t)(b0 + i) * kBlockCols : 0; };
+    __syncwarp();
+    const O* base = above.base ? static_cast<const O*>(above.base) + (int64_t)(tile.row + g) * above.ldb : nullptr;
+    O* out = static_cast<O*>(above.out) + (int64_t)(tile.row + g) * above.ldo;
+    auto columns = [&](int i) { return i < nb ? (int)min((int64_t)kBlockCols, above.C - (int64_t)(b0 + i) * kBlockCols) : 0; };
     Share<O> next;
     load_share<O>(next, base ? base + (int64_t)(b0 + warp) * kBlockCols : nullptr, above.ldb, has, columns(warp), above.io_vec);
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
@@ -90,24 +92,33 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
             for (int i = 0; i < 4; ++i) sum[n][i] = 0.f;
         // the lane's elements of x: rows g and g + 8, columns 2 q and the next, and eight on, of sixteen; a block ahead
         uint32_t x[2][kBlockCols / 16][4];
-        const T* row = static_cast<const T*>(down.x) + (tile.row + g) * down.ldx + 2 * (lane & 3);
+        const T* row = static_cast<const T*>(down.x) + (int64_t)(tile.row + g) * down.ldx + 2 * (lane & 3);
         auto load_x = [&](int i, uint32_t (&to)[kBlockCols / 16][4]) {
+            const int64_t c = (int64_t)(a0 + i) * kBlockCols;
+            const T* p = row + c;
+            if (i < na && c + kBlockCols <= down.C) {
 #pragma unroll
-            for (int k = 0; k < kBlockCols / 16; ++k)
+                for (int k = 0; k < kBlockCols / 16; ++k)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int64_t c = (int64_t)(a0 + i) * kBlockCols + 16 * k + 8 * (j >> 1);
-                    const int64_t left = a0 + i < a1 ? down.C - c - 2 * (lane & 3) : 0;
-                    const T* p = row + 8 * (j & 1) * down.ldx + c;
-                    to[k][j] = 0;
-                    if (has[j & 1] && left > 1) to[k][j] = *reinterpret_cast<const uint32_t*>(p);
-                    else if (has[j & 1] && left == 1) to[k][j] = *reinterpret_cast<const unsigned short*>(p);
-                }
+                    for (int j = 0; j < 4; ++j)
+                        to[k][j] = has[j & 1] ? *reinterpret_cast<const uint32_t*>(p + 8 * (j & 1) * down.ldx + 16 * k + 8 * (j >> 1)) : 0u;
+            } else {
+                const int left = i < na ? (int)(down.C - c) - 2 * (lane & 3) : 0;
+#pragma unroll
+                for (int k = 0; k < kBlockCols / 16; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = 16 * k + 8 * (j >> 1);
+                        const unsigned short* e = reinterpret_cast<const unsigned short*>(p + 8 * (j & 1) * down.ldx + at);
+                        to[k][j] = has[j & 1] && at < left ? e[0] : 0u;
+                        if (has[j & 1] && at + 1 < left) to[k][j] |= (uint32_t)e[1] << 16;
+                    }
+            }
         };
         load_x(warp, x[0]);
         bool live = tc::mbar_wait(&ready_a[warp], 0, &abort, &g_short_status);
-        for (int i = warp; live && i < a1 - a0; i += kWarps) {
-            load_x(i + kWarps, x[1]);
+        for (int i = warp; live && i < na; i += kWarps) {
+            if (i + kWarps < na) load_x(i + kWarps, x[1]);
             const uint32_t aa = S::A::lane_at(smem_at(as + i * S::A::BYTES), col_first_row(), col_first());
             float acc[NT][4];
 #pragma unroll
@@ -160,16 +171,16 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
     if (rank == 0)
         for (int e = threadIdx.x; e < tile.rows * down.r; e += kThreads) {
             const int row = e / down.r, c = e - row * down.r;
-            down.h[tile.row * down.r + e] = none ? (tile.id < 0 ? 0.f : __int_as_float(0x7fffffff)) : h[row * S::RP + c];
+            down.h[(int64_t)tile.row * down.r + e] = none ? (tile.id < 0 ? 0.f : __int_as_float(0x7fffffff)) : h[row * S::RP + c];
         }
     uint32_t ha[PARTS][KT][4];
     float undo[2];
     load_parts<T, KT, PARTS>(h + g * S::RP, none ? 0 : S::RP, none || !above.scale ? 1.f : above.scale[tile.id], has, ha, undo);
     const float nothing = tile.id >= down.seg.n ? __int_as_float(0x7fffffff) : 0.f;
     const bool live = none || tc::mbar_wait(&ready_b[warp], 0, &abort, &g_short_status);
-    for (int i = warp; live && i < b1 - b0; i += kWarps) {
+    for (int i = warp; live && i < nb; i += kWarps) {
         const Share<O> share = next;
-        load_share<O>(next, base ? base + (int64_t)(b0 + i + kWarps) * kBlockCols : nullptr, above.ldb, has, columns(i + kWarps), above.io_vec);
+        if (i + kWarps < nb) load_share<O>(next, base ? base + (int64_t)(b0 + i + kWarps) * kBlockCols : nullptr, above.ldb, has, columns(i + kWarps), above.io_vec);
         float acc[8][4];
 #pragma unroll
         for (int n = 0; n < 8; ++n)
@@ -197,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
             }
         }
         const int64_t c = (int64_t)(b0 + i) * kBlockCols;
-        store_sum<O>(share, acc, out + c, above.ldo, has, above.C - c, above.io_vec);
+        store_sum<O>(share, acc, out + c, above.ldo, has, columns(i), above.io_vec, tile.rows > 8);
     }
     if (!none && *static_cast<volatile int*>(&abort)) {                // given up: copies in flight land before the CTA ends
         int never = 0;
@@ -217,21 +228,22 @@ gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, 
         const int64_t a = (all_a + n - 1) / n, b = (all_b + n - 1) / n;
         return a > 4096 || b > 4096 ? INT32_MAX : S::bytes((int)a, (int)b);
     };
-    int splits = kMostSplits;
+    int splits = kMostSplits, log_splits = 0;
     while (splits > 1 && tiles * splits > 4 * sm_count() && bytes(splits / 2) <= kRoom / 3) splits /= 2;
     while (splits > 1 && (all_a < splits || all_b < splits)) splits /= 2;
+    while (1 << log_splits < splits) ++log_splits;
     const int smem = bytes(splits);
     *taken = smem <= kRoom;
     if (!*taken) return GPD_OK;
     if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
-    ShortArgs s{down, above, (int)((all_a + splits - 1) / splits), (int)((all_b + splits - 1) / splits)};
+    ShortArgs s{down, above, (int)((all_a + splits - 1) / splits), (int)((all_b + splits - 1) / splits), (int)all_a, (int)all_b};
     CUtensorMap map_a{}, map_b{};                      // without adapters they are not used
     if (down.seg.n > 0 && (!make_map(&map_a, down.w, 2, down.seg.n, down.r, down.C, down.ldw, down.next, S::RP, kBlockCols) ||
                            !make_map(&map_b, above.w, 2, down.seg.n, above.C, above.r, above.ldw, above.next, kBlockCols, S::B::PITCH / 2)))
         return GPD_ERR_CUDA;
     auto kernel = short_kernel<T, O, NT, PARTS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
-    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), smem, splits, st, map_a, map_b, s, splits);
+    return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), smem, splits, st, map_a, map_b, s, log_splits);
 }
 template <typename T, typename O>
 gpd_status launch_rank(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st) {

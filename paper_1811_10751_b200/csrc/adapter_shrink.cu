@@ -33,17 +33,17 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
     extern __shared__ __align__(128) unsigned char smem[];
     after_previous();
     const int rank = blockIdx.x % splits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x / splits);
+    const RowTile tile = find_tile<S::TM>(a.seg, (int)(blockIdx.x / splits));
     if (tile.rows == 0) return;                        // the whole cluster
-    float* out = a.h + tile.row * a.r;
+    float* out = a.h + (int64_t)tile.row * a.r;
     if (tile.id < 0 || tile.id >= a.seg.n) {
         const float v = tile.id < 0 ? 0.f : __int_as_float(0x7fffffff);
         if (rank == 0)
             for (int i = threadIdx.x; i < tile.rows * a.r; i += kThreads) out[i] = v;
         return;
     }
-    const T* x = static_cast<const T*>(a.x) + tile.row * a.ldx;
-    const T* w = static_cast<const T*>(a.w) + tile.id * a.next;
+    const T* x = static_cast<const T*>(a.x) + (int64_t)tile.row * a.ldx;
+    const T* w = static_cast<const T*>(a.w) + (int64_t)tile.id * a.next;
     const int64_t stages = (a.C + kDeep - 1) / kDeep;
     const int64_t from = stages * rank / splits, to = stages * (rank + 1) / splits;
     const uint32_t ring = smem_at(smem);
@@ -159,9 +159,9 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
     const int rank = blockIdx.x % splits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) ring.init(a.w_vec ? 1 : 33, 4);
     after_previous();
-    const RowTile tile = find_tile<S::TM>(a.seg, blockIdx.x / splits);
+    const RowTile tile = find_tile<S::TM>(a.seg, (int)(blockIdx.x / splits));
     if (tile.rows == 0) return;                        // the whole cluster
-    float* out = a.h + tile.row * a.r;
+    float* out = a.h + (int64_t)tile.row * a.r;
     if (tile.id < 0 || tile.id >= a.seg.n) {
         const float v = tile.id < 0 ? 0.f : __int_as_float(0x7fffffff);
         if (rank == 0)
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
                 if (a.w_vec) S::W::load(at + S::X_BYTES, &map_w, TRANS ? 0 : (int)c, TRANS ? (int)c : 0, (int)tile.id, bar);
             }
             if (!a.w_vec) {
-                const T* w = static_cast<const T*>(a.w) + tile.id * a.next + (TRANS ? c * a.ldw : c);
+                const T* w = static_cast<const T*>(a.w) + (int64_t)tile.id * a.next + (TRANS ? c * a.ldw : c);
                 if (TRANS) S::W::copy(at + S::X_BYTES, w, a.ldw, a.C - c, a.r, kDeep, a.r);
                 else S::W::copy(at + S::X_BYTES, w, a.ldw, a.r, a.C - c, a.r, kDeep);
                 tc::mbar_arrive(bar);
