@@ -538,7 +538,7 @@ gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, int64_t ld, 
                             void* stream);
 
 #define GPD_HEAD_MAX_DIM 256          /* columns of a head */
-#define GPD_HEAD_MAX_HEADS 65536
+#define GPD_HEAD_MAX_HEADS 1024
 #define GPD_HEAD_MAX_AXES 4           /* axes that positions have */
 #define GPD_HEAD_NORM_MAX_PARTS 512   /* gpd_head_norm_rope_backward: partial rows of each weight's gradient */
 

@@ -7,9 +7,11 @@
 // Every element is read once and written once, with a handful of operations: HBM bounds both directions.  A head of D
 // columns is cut into units of V pairs: the two vectors of V elements that hold them, so that a pair's halves are in one
 // thread's registers in either pairing and loads are 16 bytes (or 8) per lane.  G lanes hold a head, 32 / G heads are in a
-// warp; the norm is a butterfly over the G lanes, no shared memory and no barrier.  A warp stays with one token, whose
-// angles it loads once, for up to U steps of 32 / G heads, all of whose loads are issued before the first use.
+// warp; the norm is a butterfly over the G lanes, no shared memory and no barrier.  A piece of work is one token, whose
+// angles are loaded once, and up to U * 32 / G of its heads; warps walk over the pieces, and load the next one before they
+// work on the present one.  Arithmetic is on pairs of numbers.
 #include <algorithm>
+#include <numeric>
 
 #include "lm_common.h"
 
@@ -39,7 +41,7 @@ struct HeadArgs {
     float* parts;                                      // gradient: [gridDim.x][D]
     int64_t T;
     int D, R, A, lanes;                                // lanes: G
-    float eps;
+    float eps, inv_d;                                  // 1 / D
     bool wide_pos, w_f32, neighbours, inverse, table_vec;
 };
 
@@ -148,21 +150,30 @@ __device__ __forceinline__ void load_floats(const float* p, bool vec, float (&f)
     }
 }
 
-// Cosines and sines of unit u for token t.  Several axes: the rows of all of them are loaded, and every pair takes its
+// Cosines and sines of unit u at the positions `pos`, one for each axis.  Several axes: the rows of all of them are loaded, and every pair takes its
 // axis's; positions outside the table, and axes that there are none of, give NaN.
 template <int V>
-__device__ __forceinline__ void angles(const HeadArgs& a, int64_t t, int u, float (&cs)[V], float (&sn)[V]) {
+__device__ __forceinline__ void angles(const HeadArgs& a, const int (&pos)[GPD_HEAD_MAX_AXES], int u, float (&cs)[V], float (&sn)[V]) {
+    if (a.A == 1 && pos[0] >= 0) {
+        const float* row = a.table + pos[0] * a.ldt + V * u;
+        load_floats<V>(row, a.table_vec, cs);
+        load_floats<V>(row + a.R / 2, a.table_vec, sn);
+        if (a.inverse) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) sn[i] = -sn[i];
+        }
+        return;
+    }
     unsigned long long axis = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         cs[i] = sn[i] = __int_as_float(0x7fffffff);
         if (a.axes) axis |= (unsigned long long)__ldg(a.axes + V * u + i) << (8 * i);
     }
-    for (int x = 0; x < a.A; ++x) {
-        const int64_t i = t * a.ldp + x;
-        const int64_t at = a.wide_pos ? static_cast<const int64_t*>(a.pos)[i] : static_cast<const int32_t*>(a.pos)[i];
-        if (at < 0 || at >= a.P) continue;
-        const float* row = a.table + at * a.ldt + V * u;
+#pragma unroll
+    for (int x = 0; x < GPD_HEAD_MAX_AXES; ++x) {
+        if (x >= a.A || pos[x] < 0) continue;
+        const float* row = a.table + pos[x] * a.ldt + V * u;
         float c[V], s[V];
         load_floats<V>(row, a.table_vec, c);
         load_floats<V>(row + a.R / 2, a.table_vec, s);
@@ -172,6 +183,15 @@ __device__ __forceinline__ void angles(const HeadArgs& a, int64_t t, int u, floa
             cs[j] = mine ? c[j] : cs[j];
             sn[j] = mine ? (a.inverse ? -s[j] : s[j]) : sn[j];
         }
+    }
+}
+// Rows of the table for token t, one for each axis; -1: none
+__device__ __forceinline__ void positions(const HeadArgs& a, int64_t t, int (&at)[GPD_HEAD_MAX_AXES]) {
+#pragma unroll
+    for (int x = 0; x < GPD_HEAD_MAX_AXES; ++x) {
+        if (x >= a.A || a.R == 0) continue;
+        const int64_t v = a.wide_pos ? static_cast<const int64_t*>(a.pos)[t * a.ldp + x] : static_cast<const int32_t*>(a.pos)[t * a.ldp + x];
+        at[x] = v < 0 || v >= a.P ? -1 : (int)v;
     }
 }
 template <typename T, int V>
@@ -194,13 +214,16 @@ __device__ __forceinline__ void weights(const HeadArgs& a, const void* w, const 
 }
 // Sum over the G lanes of a head
 __device__ __forceinline__ float lanes_sum(float v, int G) {
-    for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < G) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// N units per lane (N > 1 only with V = 1: rows that no vector fits)
-template <typename T, int V, int N, int U>
+// Rows that no vector fits: element by element, N units per lane.
+template <typename T, int N>
 __global__ void __launch_bounds__(32 * kWarps) heads_kernel(const __grid_constant__ HeadArgs a) {
+    constexpr int V = 1, U = 1;
     after_previous();
     const bool second = blockIdx.x >= a.split;
     const Part& p = a.part[second];
@@ -225,11 +248,13 @@ __global__ void __launch_bounds__(32 * kWarps) heads_kernel(const __grid_constan
                 r2[i][n] = load_vec<T, V>(x + (int64_t)h * a.D + u.c2);
             }
         }
+    int at[GPD_HEAD_MAX_AXES];
+    positions(a, t, at);
     float cs[N][V], sn[N][V], wa[N][V], wb[N][V];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const Unit<V> u(lane % G + n * G, a);
-        if (u.there && u.turned) angles<V>(a, t, lane % G + n * G, cs[n], sn[n]);
+        if (u.there && u.turned) angles<V>(a, at, lane % G + n * G, cs[n], sn[n]);
         if (u.there && p.w) weights<T, V>(a, p.w, u, wa[n], wb[n]);
     }
 #pragma unroll
@@ -246,7 +271,7 @@ __global__ void __launch_bounds__(32 * kWarps) heads_kernel(const __grid_constan
 #pragma unroll
             for (int j = 0; j < V; ++j) sum = fmaf(fa[n][j], fa[n][j], fmaf(fb[n][j], fb[n][j], sum));
         }
-        const float s = p.w ? rsqrtf(lanes_sum(sum, G) / (float)a.D + a.eps) : 1.f;
+        const float s = p.w ? rsqrtf(lanes_sum(sum, G) * a.inv_d + a.eps) : 1.f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Unit<V> u(lane % G + n * G, a);
@@ -275,8 +300,9 @@ __global__ void __launch_bounds__(32 * kWarps) heads_kernel(const __grid_constan
 }
 
 // Gradient with norm: warps walk over the tokens and add up their lanes' share of dw in registers.
-template <typename T, int V, int N, int U>
+template <typename T, int N>
 __global__ void __launch_bounds__(32 * kWarps) heads_backward_kernel(const __grid_constant__ HeadArgs a) {
+    constexpr int V = 1, U = 1;
     __shared__ float shares[kWarps][kMaxHead];
     after_previous();
     const bool second = blockIdx.x >= a.split;
@@ -313,11 +339,13 @@ __global__ void __launch_bounds__(32 * kWarps) heads_backward_kernel(const __gri
                     y2[i][n] = load_vec<T, V>(dy + at + u.c2);
                 }
             }
+        int where[GPD_HEAD_MAX_AXES];
+        positions(a, t, where);
         float cs[N][V], sn[N][V];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Unit<V> u(lane % G + n * G, a);
-            if (u.there && u.turned) angles<V>(a, t, lane % G + n * G, cs[n], sn[n]);
+            if (u.there && u.turned) angles<V>(a, where, lane % G + n * G, cs[n], sn[n]);
         }
 #pragma unroll
         for (int i = 0; i < U; ++i) {
@@ -349,8 +377,8 @@ __global__ void __launch_bounds__(32 * kWarps) heads_backward_kernel(const __gri
                     dot = fmaf(ga[n][j] * wa[n][j], xa[n][j], fmaf(gb[n][j] * wb[n][j], xb[n][j], dot));
                 }
             }
-            const float s = rsqrtf(lanes_sum(squares, G) / (float)a.D + a.eps);
-            const float k = s * s * (lanes_sum(dot, G) / (float)a.D);
+            const float s = rsqrtf(lanes_sum(squares, G) * a.inv_d + a.eps);
+            const float k = s * s * (lanes_sum(dot, G) * a.inv_d);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const Unit<V> u(lane % G + n * G, a);
@@ -407,12 +435,243 @@ __global__ void __launch_bounds__(1024) heads_dweight_kernel(const float* parts,
     float* dw = blockIdx.y ? dkw : dqw;
     float v = 0.f;
     if (c < D)
+#pragma unroll 8
         for (int p = from + threadIdx.y; p < to; p += 32) v += parts[(int64_t)p * D + c];
     s[threadIdx.y][threadIdx.x] = v;
     __syncthreads();
-    if (threadIdx.y == 0 && c < D && dw) {
-        for (int i = 1; i < 32; ++i) v += s[i][threadIdx.x];
-        dw[c] = v;
+    // a warp per column now, the same tree for every column
+    v = warp_sum(s[threadIdx.x][threadIdx.y]);
+    const int mine = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && mine < D && dw) dw[mine] = v;
+}
+
+// ---- the same with whole vectors: warps walk over the work, the next piece's loads under way --------------------------
+// Halves of a unit's pairs, two at a time
+template <typename T, int V, bool NEAR>
+__device__ __forceinline__ void pairs(const Vec<T, V>& r1, const Vec<T, V>& r2, F2 (&a)[V / 2], F2 (&b)[V / 2]) {
+    float2 w[V];                                       // neighbours in memory
+    const uint32_t *u1 = reinterpret_cast<const uint32_t*>(&r1.r), *u2 = reinterpret_cast<const uint32_t*>(&r2.r);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = make_float2(__uint_as_float(u1[2 * i]), __uint_as_float(u1[2 * i + 1]));
+            w[V / 2 + i] = make_float2(__uint_as_float(u2[2 * i]), __uint_as_float(u2[2 * i + 1]));
+        } else {
+            w[i] = unpack2(u1[i], T());
+            w[V / 2 + i] = unpack2(u2[i], T());
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        a[i] = NEAR ? f2(w[2 * i].x, w[2 * i + 1].x) : f2(w[i].x, w[i].y);
+        b[i] = NEAR ? f2(w[2 * i].y, w[2 * i + 1].y) : f2(w[V / 2 + i].x, w[V / 2 + i].y);
+    }
+}
+template <typename T, int V, bool NEAR>
+__device__ __forceinline__ void store_pairs(T* p1, T* p2, const F2 (&a)[V / 2], const F2 (&b)[V / 2]) {
+    float x[V], y[V];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        const float2 u = f2(a[i]), v = f2(b[i]);
+        if (NEAR) {
+            float* q = i < V / 4 ? x : y;
+            const int at = 4 * i % V;
+            q[at] = u.x;
+            q[at + 1] = v.x;
+            q[at + 2] = u.y;
+            q[at + 3] = v.y;
+        } else {
+            x[2 * i] = u.x;
+            x[2 * i + 1] = u.y;
+            y[2 * i] = v.x;
+            y[2 * i + 1] = v.y;
+        }
+    }
+    store_vec<T, V>(p1, x);
+    store_vec<T, V>(p2, y);
+}
+template <int V>
+__device__ __forceinline__ void two_by_two(const float (&f)[V], F2 (&o)[V / 2]) {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) o[i] = f2(f[2 * i], f[2 * i + 1]);
+}
+// (a, b) turned; ns: the sines negated
+template <int N>
+__device__ __forceinline__ void turn(F2 (&a)[N], F2 (&b)[N], const F2 (&c)[N], const F2 (&s)[N], const F2 (&ns)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const F2 x = a[i];
+        a[i] = fma2(b[i], ns[i], mul2(x, c[i]));
+        b[i] = fma2(x, s[i], mul2(b[i], c[i]));
+    }
+}
+__device__ __forceinline__ float both(F2 v) {
+    const float2 f = f2(v);
+    return f.x + f.y;
+}
+
+// U: heads of a lane in one piece of work.  BACK: the gradient with norm; otherwise the forward pass, or the gradient without.
+template <typename T, int V, int U, bool NEAR, bool BACK>
+__global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(const __grid_constant__ HeadArgs a) {
+    constexpr int P = V / 2;
+    __shared__ float shares[BACK ? kWarps : 1][BACK ? kMaxHead : 1];
+    after_previous();
+    const bool second = blockIdx.x >= a.split;
+    const Part& p = a.part[second];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.lanes, per = 32 / G;
+    // a warp keeps to one chunk of heads and walks over the tokens: the part's warps are a multiple of its chunks
+    const int warps = (int)(second ? gridDim.x - a.split : a.split) * kWarps, index = (int)(blockIdx.x - (second ? a.split : 0)) * kWarps + warp;
+    const int step = warps / p.chunks, h0 = index % p.chunks * per * U + lane / G, T_all = (int)a.T;
+    const Unit<V> u(lane % G, a);
+    const bool turned = u.there && u.turned;
+    F2 wa[P], wb[P], da[BACK ? P : 1], db[BACK ? P : 1];
+    if (p.w && u.there) {
+        float x[V], y[V];
+        weights<T, V>(a, p.w, u, x, y);
+        two_by_two<V>(x, wa);
+        two_by_two<V>(y, wb);
+    } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) wa[i] = wb[i] = f2(0.f, 0.f);
+    }
+    if (BACK) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) da[i] = db[i] = f2(0.f, 0.f);
+    }
+    Vec<T, V> x1[U], x2[U], y1[BACK ? U : 1], y2[BACK ? U : 1];        // the next piece, as it comes
+    int at[GPD_HEAD_MAX_AXES];                     // its positions
+    auto fetch = [&](int t) {
+        const T* x = static_cast<const T*>(p.x) + t * p.ldx + h0 * a.D;
+        const T* dy = static_cast<const T*>(p.dy) + t * p.lddy + h0 * a.D;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool here = u.there && h0 + i * per < p.heads;
+            const int d = i * per * a.D;
+            x1[i] = x2[i] = Vec<T, V>{};
+            if (here) {
+                x1[i] = load_vec<T, V>(x + d + u.c1);
+                x2[i] = load_vec<T, V>(x + d + u.c2);
+            }
+            if (BACK) {
+                y1[i] = y2[i] = Vec<T, V>{};
+                if (here) {
+                    y1[i] = load_vec<T, V>(dy + d + u.c1);
+                    y2[i] = load_vec<T, V>(dy + d + u.c2);
+                }
+            }
+        }
+        positions(a, t, at);
+    };
+    int t = index / p.chunks;
+    if (t < T_all) fetch(t);
+    for (; t < T_all; t += step) {
+        F2 c[P], s[P], ns[P];
+        if (turned) {
+            float cs[V], sn[V];
+            angles<V>(a, at, lane % G, cs, sn);
+            two_by_two<V>(cs, c);
+            two_by_two<V>(sn, s);
+#pragma unroll
+            for (int i = 0; i < P; ++i) ns[i] = s[i] ^ 0x8000000080000000ull;
+        }
+        Vec<T, V> r1[U], r2[U], g1[BACK ? U : 1], g2[BACK ? U : 1];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            r1[i] = x1[i];
+            r2[i] = x2[i];
+            if (BACK) {
+                g1[i] = y1[i];
+                g2[i] = y2[i];
+            }
+        }
+        if (t < T_all - step) fetch(t + step);
+        T* out = static_cast<T*>(p.out) + t * p.ldo + h0 * a.D;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool here = u.there && h0 + i * per < p.heads;
+            T* o = out + i * per * a.D;
+            F2 xa[P], xb[P];
+            pairs<T, V, NEAR>(r1[i], r2[i], xa, xb);
+            F2 squares = f2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < P; ++j) squares = fma2(xa[j], xa[j], fma2(xb[j], xb[j], squares));
+            if constexpr (!BACK) {
+                if (p.w) {
+                    const float f = rsqrtf(lanes_sum(both(squares), G) * a.inv_d + a.eps);
+                    const F2 f_2 = f2(f, f);
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        xa[j] = mul2(mul2(xa[j], f_2), wa[j]);
+                        xb[j] = mul2(mul2(xb[j], f_2), wb[j]);
+                    }
+                }
+                if (turned) turn<P>(xa, xb, c, s, ns);
+                if (here) store_pairs<T, V, NEAR>(o + u.c1, o + u.c2, xa, xb);
+            } else {
+                F2 ga[P], gb[P];
+                pairs<T, V, NEAR>(g1[i], g2[i], ga, gb);
+                if (turned && here) turn<P>(ga, gb, c, s, ns);         // heads and units that do not exist are zeros and stay so
+                F2 dot = f2(0.f, 0.f), ta[P], tb[P];
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    ta[j] = mul2(ga[j], xa[j]);
+                    tb[j] = mul2(gb[j], xb[j]);
+                    dot = fma2(ta[j], wa[j], fma2(tb[j], wb[j], dot));
+                }
+                float sq = both(squares), dt = both(dot);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    if (o < G) {
+                        sq += __shfl_xor_sync(0xffffffffu, sq, o);
+                        dt += __shfl_xor_sync(0xffffffffu, dt, o);
+                    }
+                const float f = rsqrtf(sq * a.inv_d + a.eps), k = f * f * f * (dt * a.inv_d);
+                const F2 f_2 = f2(f, f), k_2 = f2(-k, -k);
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    da[j] = fma2(ta[j], f_2, da[j]);
+                    db[j] = fma2(tb[j], f_2, db[j]);
+                    ga[j] = fma2(xa[j], k_2, mul2(mul2(ga[j], wa[j]), f_2));
+                    gb[j] = fma2(xb[j], k_2, mul2(mul2(gb[j], wb[j]), f_2));
+                }
+                if (here) store_pairs<T, V, NEAR>(o + u.c1, o + u.c2, ga, gb);
+            }
+        }
+    }
+    if constexpr (BACK) {
+        // the warp's heads, then the CTA's warps, in a fixed order
+        float fa[V], fb[V];
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const float2 v = f2(da[j]), w = f2(db[j]);
+            fa[2 * j] = v.x;
+            fa[2 * j + 1] = v.y;
+            fb[2 * j] = w.x;
+            fb[2 * j + 1] = w.y;
+        }
+        for (int o = G; o < 32; o <<= 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                fa[j] += __shfl_xor_sync(0xffffffffu, fa[j], o);
+                fb[j] += __shfl_xor_sync(0xffffffffu, fb[j], o);
+            }
+        }
+        if (u.there && lane < G) {
+            float f[V], h[V];
+            from_pairs<V>(fa, fb, NEAR, f, h);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                shares[warp][u.c1 + j] = f[j];
+                shares[warp][u.c2 + j] = h[j];
+            }
+        }
+        __syncthreads();
+        for (int d = threadIdx.x; d < a.D; d += 32 * kWarps) {
+            float v = shares[0][d];
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) v += shares[w][d];
+            a.parts[(int64_t)blockIdx.x * a.D + d] = v;
+        }
     }
 }
 
@@ -435,69 +694,65 @@ int pow2_lanes(int units) {
     return g;
 }
 
-template <typename T, int V, int U>
-gpd_status launch_forward(HeadArgs a, cudaStream_t st) {
-    constexpr int N = V == 1 ? kMaxHead / 64 : 1;
-    int64_t ctas = 0;
+// Gives each part its chunks and CTAs: as many as there is work, about `most` at most in all, shared out by the amount of it;
+// fixed: so many that their warps are a multiple of the chunks.
+int share_out(HeadArgs& a, int U, int64_t most, bool fixed) {
+    const int step = 32 / a.lanes * U;
+    int64_t work[2], n[2], unit[2];
     for (int i = 0; i < 2; ++i) {
-        Part& p = a.part[i];
-        const int step = 32 / a.lanes * U;
-        p.chunks = std::max(1, (p.heads + step - 1) / step);
-        const int64_t n = p.heads > 0 ? (a.T * p.chunks + kWarps - 1) / kWarps : 0;
-        if (i == 0) a.split = (unsigned)n;
-        ctas += n;
+        const int chunks = std::max(1, (a.part[i].heads + step - 1) / step);
+        a.part[i].chunks = chunks;
+        work[i] = a.part[i].heads > 0 ? (a.T * chunks + kWarps - 1) / kWarps : 0;
+        unit[i] = fixed ? chunks / std::gcd(chunks, kWarps) : 1;       // CTAs
     }
-    if (ctas > 0x7fffffff) return GPD_ERR_SHAPE;
-    return launch_after(heads_kernel<T, V, N, U>, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, a);
+    const int64_t sum = work[0] + work[1];
+    for (int i = 0; i < 2; ++i) {
+        const int64_t share = sum > most ? most * work[i] / sum : work[i];
+        n[i] = work[i] == 0 ? 0 : std::max<int64_t>(1, std::min((work[i] + unit[i] - 1) / unit[i], share / unit[i])) * unit[i];
+    }
+    a.split = (unsigned)n[0];
+    return (int)(n[0] + n[1]);
+}
+template <typename T, int V, int U>
+gpd_status launch_walk(HeadArgs a, bool back, cudaStream_t st) {
+    const int ctas = share_out(a, U, (back ? 3 : 4) * sm_count(), true);
+    auto kernel = back ? (a.neighbours ? heads_walk_kernel<T, V, 2, true, true> : heads_walk_kernel<T, V, 2, false, true>)
+                       : (a.neighbours ? heads_walk_kernel<T, V, U, true, false> : heads_walk_kernel<T, V, U, false, false>);
+    return launch_after(kernel, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, a);
 }
 template <typename T, int V>
-gpd_status launch_forward_steps(HeadArgs a, cudaStream_t st) {
+gpd_status launch_forward(HeadArgs a, cudaStream_t st) {
     a.lanes = pow2_lanes(a.D / (2 * V));
-    if (V == 1) return launch_forward<T, V, 1>(a, st);
-    // Few tokens: one step per warp, so that the heads are spread over the SMs.
+    // Few tokens: one head per lane and piece, so that the heads are spread over the SMs.
     const int64_t steps = a.T * ((a.part[0].heads + a.part[1].heads) / (32 / a.lanes) + 1);
-    return steps < 8 * (int64_t)sm_count() * kWarps ? launch_forward<T, V, 1>(a, st) : launch_forward<T, V, 4>(a, st);
+    return steps < 8 * (int64_t)sm_count() * kWarps ? launch_walk<T, V, 1>(a, false, st) : launch_walk<T, V, 4>(a, false, st);
 }
 template <typename T>
-gpd_status launch_heads(const HeadArgs& a, cudaStream_t st) {
+gpd_status launch_heads(HeadArgs a, cudaStream_t st) {
     switch (vector_width(a, sizeof(T))) {
-        case sizeof(T) == 2 ? 8 : -1: return launch_forward_steps<T, 16 / sizeof(T)>(a, st);
-        case 4: return launch_forward_steps<T, 4>(a, st);
-        default: return launch_forward_steps<T, 1>(a, st);
+        case sizeof(T) == 2 ? 8 : -1: return launch_forward<T, 16 / sizeof(T)>(a, st);
+        case 4: return launch_forward<T, 4>(a, st);
     }
+    a.lanes = pow2_lanes(a.D / 2);
+    const int ctas = share_out(a, 1, INT32_MAX, false);
+    return launch_after(heads_kernel<T, kMaxHead / 64>, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, a);
 }
 
-template <typename T, int V>
-gpd_status launch_backward(HeadArgs a, float* dqw, float* dkw, cudaStream_t st) {
-    constexpr int N = V == 1 ? kMaxHead / 64 : 1, U = V == 1 ? 1 : 2;
+template <typename T>
+gpd_status launch_heads_backward(HeadArgs a, float* dqw, float* dkw, cudaStream_t st) {
+    const int V = vector_width(a, sizeof(T));
     a.lanes = pow2_lanes(a.D / (2 * V));
-    const int step = 32 / a.lanes * U;
-    int64_t work[2];
-    for (int i = 0; i < 2; ++i) {
-        a.part[i].chunks = std::max(1, (a.part[i].heads + step - 1) / step);
-        work[i] = a.part[i].heads > 0 ? (a.T * a.part[i].chunks + kWarps - 1) / kWarps : 0;
-    }
-    // four CTAs per SM, shared out by the amount of work
-    const int64_t most = std::min<int64_t>(4 * sm_count(), 2 * GPD_HEAD_NORM_MAX_PARTS), sum = work[0] + work[1];
-    int64_t n[2];
-    for (int i = 0; i < 2; ++i)
-        n[i] = work[i] == 0 ? 0 : std::max<int64_t>(1, std::min({work[i], most * work[i] / sum, (int64_t)GPD_HEAD_NORM_MAX_PARTS}));
-    a.split = (unsigned)n[0];
-    const int split = (int)n[0], total = (int)(n[0] + n[1]);
-    if (total > 0) {
-        const gpd_status rc = launch_after(heads_backward_kernel<T, V, N, U>, dim3((unsigned)total), dim3(32 * kWarps), 0, 1, st, a);
+    HeadArgs shared = a;                               // the CTAs of either part, for the sum over them
+    const int ctas = share_out(shared, V == 1 ? 1 : 2, 3 * sm_count(), V > 1);
+    if (ctas > 0) {
+        gpd_status rc;
+        if (V == 1) rc = launch_after(heads_backward_kernel<T, kMaxHead / 64>, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, shared);
+        else rc = V == 4 ? launch_walk<T, 4, 2>(a, true, st) : launch_walk<T, 16 / sizeof(T), 2>(a, true, st);
         if (rc != GPD_OK) return rc;
     }
     const float* parts = a.parts;
-    return launch_after(heads_dweight_kernel, dim3((unsigned)((a.D + 31) / 32), 2), dim3(32, 32), 0, 1, st, parts, split, total, a.D, dqw, dkw);
-}
-template <typename T>
-gpd_status launch_heads_backward(const HeadArgs& a, float* dqw, float* dkw, cudaStream_t st) {
-    switch (vector_width(a, sizeof(T))) {
-        case sizeof(T) == 2 ? 8 : -1: return launch_backward<T, 16 / sizeof(T)>(a, dqw, dkw, st);
-        case 4: return launch_backward<T, 4>(a, dqw, dkw, st);
-        default: return launch_backward<T, 1>(a, dqw, dkw, st);
-    }
+    const int split = (int)shared.split;
+    return launch_after(heads_dweight_kernel, dim3((unsigned)((a.D + 31) / 32), 2), dim3(32, 32), 0, 1, st, parts, split, ctas, a.D, dqw, dkw);
 }
 
 // What both directions check.  GPD_OK with a.T = 0: nothing to do.
@@ -508,7 +763,7 @@ gpd_status check_heads(int type, int weight_type, const HeadArgs& a, int index_b
     const Part *q = &a.part[0], *k = &a.part[1];
     if (q->heads < 0 || k->heads < 0 || q->heads > GPD_HEAD_MAX_HEADS || k->heads > GPD_HEAD_MAX_HEADS) return GPD_ERR_SHAPE;
     if (a.R > 0) {
-        if (a.A < 1 || a.A > GPD_HEAD_MAX_AXES || a.P < 0 || (a.P > 1 && a.ldt < a.R) || (a.T > 1 && a.ldp < a.A)) return GPD_ERR_SHAPE;
+        if (a.A < 1 || a.A > GPD_HEAD_MAX_AXES || a.P < 0 || a.P > 0x7fffffff || (a.P > 1 && a.ldt < a.R) || (a.T > 1 && a.ldp < a.A)) return GPD_ERR_SHAPE;
         if ((index_bytes != 4 && index_bytes != 8) || (a.A > 1 && !a.axes)) return GPD_ERR_ARG;
         if ((a.P > 0 && !a.table) || (a.T > 0 && !a.pos)) return GPD_ERR_ARG;
     }
@@ -535,7 +790,7 @@ extern "C" gpd_status gpd_head_norm_rope(gpd_dtype type, const void* q_dev, int6
                                          int32_t n_axes, const uint8_t* axes_dev, void* q_out_dev, int64_t ldqo, void* k_out_dev,
                                          int64_t ldko, int64_t T, void* stream) {
     HeadArgs a{{{q_dev, ldq, nullptr, 0, q_out_dev, ldqo, q_weight_dev, q_heads, 0}, {k_dev, ldk, nullptr, 0, k_out_dev, ldko, k_weight_dev, k_heads, 0}},
-               0, table_dev, ldt, positions, pos_dev, ldp, n_axes > 1 ? axes_dev : nullptr, nullptr, T, head_dim, rotated, n_axes, 0, eps,
+               0, table_dev, ldt, positions, pos_dev, ldp, n_axes > 1 ? axes_dev : nullptr, nullptr, T, head_dim, rotated, n_axes, 0, eps, head_dim > 0 ? 1.f / (float)head_dim : 0.f,
                index_bytes == 8, weight_type == GPD_DT_F32, neighbours != 0, false, lm::rows_aligned(table_dev, ldt, 4)};
     const bool norm = q_weight_dev || k_weight_dev;
     const gpd_status rc = check_heads(type, weight_type, a, index_bytes, norm);
@@ -563,7 +818,7 @@ extern "C" gpd_status gpd_head_norm_rope_backward(gpd_dtype type, const void* dq
     HeadArgs a{{{xq, norm ? ldq : lddq, norm ? dq_dev : nullptr, lddq, dq_in_dev, lddqi, q_weight_dev, q_heads, 0},
                 {xk, norm ? ldk : lddk, norm ? dk_dev : nullptr, lddk, dk_in_dev, lddki, k_weight_dev, k_heads, 0}},
                0, table_dev, ldt, positions, pos_dev, ldp, n_axes > 1 ? axes_dev : nullptr, static_cast<float*>(workspace_dev), T, head_dim,
-               rotated, n_axes, 0, eps, index_bytes == 8, weight_type == GPD_DT_F32, neighbours != 0, true,
+               rotated, n_axes, 0, eps, head_dim > 0 ? 1.f / (float)head_dim : 0.f, index_bytes == 8, weight_type == GPD_DT_F32, neighbours != 0, true,
                lm::rows_aligned(table_dev, ldt, 4)};
     const gpd_status rc = check_heads(type, weight_type, a, index_bytes, norm);
     if (rc != GPD_OK) return rc;
