@@ -212,12 +212,21 @@ __device__ __forceinline__ void weights(const HeadArgs& a, const void* w, const 
     }
     to_pairs<V>(x, y, a.neighbours, wa, wb);
 }
-// Sum over the G lanes of a head
+// Sum over the G lanes of a head: a power of two, or any number (then every lane adds them up in the same order).
 __device__ __forceinline__ float lanes_sum(float v, int G) {
+    if (G == 8) {                                      // 128 columns of 16 bits
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (o < G) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+        for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    if ((G & (G - 1)) == 0) {
+        for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    const int first = (threadIdx.x & 31) / G * G;
+    float sum = 0.f;
+    for (int i = 0; i < G; ++i) sum += __shfl_sync(0xffffffffu, v, (first + i) & 31);
+    return sum;
 }
 
 // Rows that no vector fits: element by element, N units per lane.
@@ -522,7 +531,8 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
     // a warp keeps to one chunk of heads and walks over the tokens: the part's warps are a multiple of its chunks
     const int warps = (int)(second ? gridDim.x - a.split : a.split) * kWarps, index = (int)(blockIdx.x - (second ? a.split : 0)) * kWarps + warp;
     const int step = warps / p.chunks, h0 = index % p.chunks * per * U + lane / G, T_all = (int)a.T;
-    const Unit<V> u(lane % G, a);
+    Unit<V> u(lane % G, a);
+    u.there = u.there && lane < per * G;               // 32 need not be a multiple of G
     const bool turned = u.there && u.turned;
     F2 wa[P], wb[P], da[BACK ? P : 1], db[BACK ? P : 1];
     if (p.w && u.there) {
@@ -618,13 +628,7 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
                     tb[j] = mul2(gb[j], xb[j]);
                     dot = fma2(ta[j], wa[j], fma2(tb[j], wb[j], dot));
                 }
-                float sq = both(squares), dt = both(dot);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    if (o < G) {
-                        sq += __shfl_xor_sync(0xffffffffu, sq, o);
-                        dt += __shfl_xor_sync(0xffffffffu, dt, o);
-                    }
+                const float sq = lanes_sum(both(squares), G), dt = lanes_sum(both(dot), G);
                 const float f = rsqrtf(sq * a.inv_d + a.eps), k = f * f * f * (dt * a.inv_d);
                 const F2 f_2 = f2(f, f), k_2 = f2(-k, -k);
 #pragma unroll
@@ -649,12 +653,15 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
             fb[2 * j] = w.x;
             fb[2 * j + 1] = w.y;
         }
-        for (int o = G; o < 32; o <<= 1) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                fa[j] += __shfl_xor_sync(0xffffffffu, fa[j], o);
-                fb[j] += __shfl_xor_sync(0xffffffffu, fb[j], o);
+        for (int j = 0; j < V; ++j) {
+            float x = 0.f, y = 0.f;
+            for (int i = 0; i < per; ++i) {
+                x += __shfl_sync(0xffffffffu, fa[j], (lane + i * G) & 31);
+                y += __shfl_sync(0xffffffffu, fb[j], (lane + i * G) & 31);
             }
+            fa[j] = x;
+            fb[j] = y;
         }
         if (u.there && lane < G) {
             float f[V], h[V];
@@ -688,11 +695,14 @@ int vector_width(const HeadArgs& a, int elem) {
     }
     return 1;
 }
+// Lanes of a head: the next power of two, whose sums take fewer steps, unless more heads find room without (80 columns: six
+// instead of four).
 int pow2_lanes(int units) {
     int g = 1;
     while (g < units && g < 32) g *= 2;
     return g;
 }
+int head_lanes(int units) { return units < 32 && 32 / units > 32 / pow2_lanes(units) ? units : pow2_lanes(units); }
 
 // Gives each part its chunks and CTAs: as many as there is work, about `most` at most in all, shared out by the amount of it;
 // fixed: so many that their warps are a multiple of the chunks.
@@ -722,7 +732,7 @@ gpd_status launch_walk(HeadArgs a, bool back, cudaStream_t st) {
 }
 template <typename T, int V>
 gpd_status launch_forward(HeadArgs a, cudaStream_t st) {
-    a.lanes = pow2_lanes(a.D / (2 * V));
+    a.lanes = head_lanes(a.D / (2 * V));
     // Few tokens: one head per lane and piece, so that the heads are spread over the SMs.
     const int64_t steps = a.T * ((a.part[0].heads + a.part[1].heads) / (32 / a.lanes) + 1);
     return steps < 8 * (int64_t)sm_count() * kWarps ? launch_walk<T, V, 1>(a, false, st) : launch_walk<T, V, 4>(a, false, st);
@@ -741,7 +751,7 @@ gpd_status launch_heads(HeadArgs a, cudaStream_t st) {
 template <typename T>
 gpd_status launch_heads_backward(HeadArgs a, float* dqw, float* dkw, cudaStream_t st) {
     const int V = vector_width(a, sizeof(T));
-    a.lanes = pow2_lanes(a.D / (2 * V));
+    a.lanes = V == 1 ? pow2_lanes(a.D / 2) : head_lanes(a.D / (2 * V));
     HeadArgs shared = a;                               // the CTAs of either part, for the sum over them
     const int ctas = share_out(shared, V == 1 ? 1 : 2, 3 * sm_count(), V > 1);
     if (ctas > 0) {

@@ -113,7 +113,8 @@ CASES = [dict(T=1, Hq=1, Hk=1, D=128, R=128), dict(T=8, Hq=32, Hk=8, D=128, R=12
          dict(T=37, Hq=3, Hk=2, D=130, R=62, neighbours=True), dict(T=44, Hq=4, Hk=2, D=72, R=40, wtype=F32),
          dict(T=29, Hq=4, Hk=2, D=128, R=128, pad=1), dict(T=29, Hq=4, Hk=2, D=128, R=128, pad=4, offset=4),
          dict(T=31, Hq=4, Hk=2, D=128, R=128, offset=3, axes=2, index=torch.int64), dict(T=31, Hq=4, Hk=2, D=64, R=64, type=F32, pad=2),
-         dict(T=70, Hq=6, Hk=2, D=128, R=0), dict(T=3, Hq=2, Hk=64, D=64, R=64, wtype=F32, type=F16),
+         dict(T=70, Hq=6, Hk=2, D=128, R=0), dict(T=77, Hq=13, Hk=5, D=80, R=40, type=F32),
+         dict(T=130, Hq=7, Hk=3, D=96, R=96, wtype=F32), dict(T=600, Hq=12, Hk=12, D=48, R=48), dict(T=3, Hq=2, Hk=64, D=64, R=64, wtype=F32, type=F16),
          dict(T=65, Hq=8, Hk=8, D=80, R=80, norm=False, axes=3, neighbours=True, type=F16), dict(T=9, Hq=4, Hk=2, D=128, R=96, norm=False),
          dict(T=12, Hq=3, Hk=1, D=10, R=6, norm=False, type=F32)]
 IDS = ["-".join(f"{k}{str(v).replace('torch.', '')}" for k, v in c.items()) for c in CASES]
