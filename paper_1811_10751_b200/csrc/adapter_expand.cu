@@ -155,7 +155,7 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     __syncthreads();
     // The kernel before this one is the same call's: it began its work, and let this one start, when all before it had
     // completed, and it writes h alone.  So only the warps that read h wait for it; segments, W and base are there.
-    if (warp < kThreads / 32) after_previous();
+    bool waited = warp == kThreads / 32;
     const int64_t chunks = (a.C + kCols - 1) / kCols, all = count_tiles<S::TM>(a.seg) * chunks;
     const int64_t last = all * (blockIdx.x + 1) / gridDim.x;
     int k = 0;                                         // stages so far
@@ -198,6 +198,8 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         const bool has[2] = {row0 < tile.rows, row0 + 8 < tile.rows}, whole = 16 * warp + 16 <= tile.rows, any = 16 * warp < tile.rows;
         uint32_t ha[PARTS][KT][4];
         float undo[2];
+        if (!waited) after_previous();
+        waited = true;
         load_parts<T, KT, PARTS>(a.h + (int64_t)(tile.row + row0) * a.r, none ? 0 : a.r, none || !a.scale ? 1.f : a.scale[tile.id], has, ha, undo);
         for (int i = 0; i < n; ++i, ++k) {
             if (!ring.wait_full(k, &g_expand_status)) break;
@@ -206,68 +208,80 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                                       : S::W::lane_at(stage + S::BASE, col_first_row(), col_first());
             const uint32_t block0 = WTile<S::TM, kCols>::lane_at(mine, row_first(), row_first_col());
             if (any) {
+                // the sums begin with base where the result has 16 bits, whose rounding hides the tensor cores' truncation
+                constexpr bool kOnBase = sizeof(O) == 2 && std::is_same<T, __nv_bfloat16>::value;
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {          // 16 columns
-                    // the sums begin with base where the result has 16 bits, whose rounding hides the tensor cores' truncation
-                    constexpr bool kOnBase = sizeof(O) == 2 && std::is_same<T, __nv_bfloat16>::value;
-                    float acc[2][4], own[2][4];        // [8 columns][row g: 2 q, 2 q + 1; row g + 8]
-                    const uint32_t block = WTile<S::TM, kCols>::on(block0, 0, 16 * p);
-                    uint32_t b16[4] = {0, 0, 0, 0};
+                for (int half = 0; half < 2; ++half) { // 32 columns: four chains of additions side by side
+                    float acc[2][2][4];                // [16 columns][8 columns][row g: 2 q, 2 q + 1; row g + 8]
+                    uint32_t b16[2][4];
+                    auto block = [&](int i) { return WTile<S::TM, kCols>::on(block0, 0, 32 * half + 16 * i); };
                     if (sizeof(O) == 2) {
-                        if (a.base) ldmatrix4<false>(b16, block);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 f = unpack2(b16[j], T());
-                            own[j >> 1][2 * (j & 1)] = f.x;
-                            own[j >> 1][2 * (j & 1) + 1] = f.y;
+                        for (int i2 = 0; i2 < 2; ++i2) {
+                            b16[i2][0] = b16[i2][1] = b16[i2][2] = b16[i2][3] = 0;
+                            if (a.base) ldmatrix4<false>(b16[i2], block(i2));
                         }
                     }
 #pragma unroll
                     for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[i2][j] = kOnBase ? own[i2][j] : 0.f;
+                        for (int j = 0; j < 4; ++j) {
+                            float2 f = make_float2(0.f, 0.f);
+                            if (kOnBase) f = unpack2(b16[i2][j], T());
+                            acc[i2][j >> 1][2 * (j & 1)] = f.x;
+                            acc[i2][j >> 1][2 * (j & 1) + 1] = f.y;
+                        }
                     if (!none) {
 #pragma unroll
                         for (int s = 0; s < KT; ++s) {
-                            uint32_t b[4];
-                            if (TRANS) ldmatrix4<true>(b, S::W::on(ws, 16 * s, 16 * p));
-                            else ldmatrix4<false>(b, S::W::on(ws, 16 * p, 16 * s));
+                            uint32_t b[2][4];
 #pragma unroll
-                            for (int i2 = PARTS - 1; i2 >= 0; --i2) {  // the small parts first
-                                mma(acc[0], ha[i2][s], b[0], b[1], T());
-                                mma(acc[1], ha[i2][s], b[2], b[3], T());
+                            for (int i2 = 0; i2 < 2; ++i2) {
+                                if (TRANS) ldmatrix4<true>(b[i2], S::W::on(ws, 16 * s, 32 * half + 16 * i2));
+                                else ldmatrix4<false>(b[i2], S::W::on(ws, 32 * half + 16 * i2, 16 * s));
                             }
+#pragma unroll
+                            for (int j = PARTS - 1; j >= 0; --j)       // the small parts first
+#pragma unroll
+                                for (int i2 = 0; i2 < 2; ++i2) {
+                                    mma(acc[i2][0], ha[j][s], b[i2][0], b[i2][1], T());
+                                    mma(acc[i2][1], ha[j][s], b[i2][2], b[i2][3], T());
+                                }
                         }
                     } else if (tile.id >= 0) {         // there is no such adapter
 #pragma unroll
-                        for (int i2 = 0; i2 < 2; ++i2)
+                        for (int i2 = 0; i2 < 8; ++i2)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[i2][j] = __int_as_float(0x7fffffff);
+                            for (int j = 0; j < 2; ++j) acc[i2 >> 2][j][i2 & 3] = __int_as_float(0x7fffffff);
                     }
-                    if constexpr (sizeof(O) == 2) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float x = acc[j >> 1][2 * (j & 1)], y = acc[j >> 1][2 * (j & 1) + 1];
-                            if (!kOnBase) {
-                                x = fmaf(x, undo[j & 1], own[j >> 1][2 * (j & 1)]);
-                                y = fmaf(y, undo[j & 1], own[j >> 1][2 * (j & 1) + 1]);
+                    for (int i2 = 0; i2 < 2; ++i2) {
+                        if constexpr (sizeof(O) == 2) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float x = acc[i2][j >> 1][2 * (j & 1)], y = acc[i2][j >> 1][2 * (j & 1) + 1];
+                                if (!kOnBase) {
+                                    const float2 f = unpack2(b16[i2][j], O());
+                                    x = fmaf(x, undo[j & 1], f.x);
+                                    y = fmaf(y, undo[j & 1], f.y);
+                                }
+                                b16[i2][j] = pack2(x, y, O());
                             }
-                            b16[j] = pack2(x, y, O());
+                            stmatrix4(b16[i2], block(i2));
+                        } else {
+#pragma unroll
+                            for (int n2 = 0; n2 < 2; ++n2)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {          // row g + 8 j, columns c and c + 1
+                                    const int c = 32 * half + 16 * i2 + 8 * n2 + 2 * q;
+                                    const uint32_t to = mine + c / S::BOX * S::TM * 128 + swizzled<128>((g + 8 * j) * 128 + c % S::BOX * 4);
+                                    float x = 0.f, y = 0.f;
+                                    if (a.base) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(to) : "memory");
+                                    x = fmaf(acc[i2][n2][2 * j], undo[j], x);
+                                    y = fmaf(acc[i2][n2][2 * j + 1], undo[j], y);
+                                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
+                                }
                         }
-                        stmatrix4(b16, block);
-                    } else {
-#pragma unroll
-                        for (int i2 = 0; i2 < 2; ++i2)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {              // row g + 8 j, columns c and c + 1
-                                const int c = 16 * p + 8 * i2 + 2 * q;
-                                const uint32_t to = mine + c / S::BOX * S::TM * 128 + swizzled<128>((g + 8 * j) * 128 + c % S::BOX * 4);
-                                float x = 0.f, y = 0.f;
-                                if (a.base) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(to) : "memory");
-                                x = fmaf(acc[i2][2 * j], undo[j], x);
-                                y = fmaf(acc[i2][2 * j + 1], undo[j], y);
-                                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
-                            }
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
