@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job 
 
 template <int MT, int PARTS>
 struct TmaShape {
-    static constexpr int RP = 16 * MT, WARPS = MT <= 2 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
+    static constexpr int RP = 16 * MT, WARPS = MT <= 4 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
     using Y = WTile<kRows, kCols>;
     using H = WTile<kRows, RP>;
     static constexpr int STAGE = Y::BYTES + PARTS * H::BYTES, SMEM = STAGES * STAGE + 1024;
@@ -462,6 +462,7 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
     const bool second = blockIdx.y >= job.first_tiles;
     const GradArgs& a = job.two[second];
     const int c0 = (int)(blockIdx.y - (second ? job.first_tiles : 0)) * kCols;
+    const float scale = a.scale ? a.scale[id] : 1.f;
     __syncthreads();
     float sum[MT][NT][4];
 #pragma unroll
@@ -552,7 +553,6 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[m][j][i] += acc[m][j][i];
     }
-    const float scale = a.scale ? a.scale[id] : 1.f;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -570,13 +570,20 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
     else __syncthreads();
     constexpr int THREADS = 32 * WARPS + 32;
     write_tile<O>(job, a, id, c0, rank * THREADS + threadIdx.x, splits * THREADS, [&](int k, int c) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < splits; ++s) {
-            const float4 x = *reinterpret_cast<const float4*>((splits > 1 ? cluster.map_shared_rank(tile, s) : tile) + k * kTileWidth + c);
-            v.x += x.x;
-            v.y += x.y;
-            v.z += x.z;
-            v.w += x.w;
+        const int at = k * kTileWidth + c;
+        float4 v = *reinterpret_cast<const float4*>(tile + at);
+        if (splits > 1) {                              // all CTAs' numbers under way before the first is added
+            float4 x[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) x[s] = s < splits ? *reinterpret_cast<const float4*>(cluster.map_shared_rank(tile, s) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v = x[0];
+#pragma unroll
+            for (int s = 1; s < 8; ++s) {
+                v.x += x[s].x;
+                v.y += x[s].y;
+                v.z += x[s].z;
+                v.w += x[s].w;
+            }
         }
         return v;
     });
@@ -594,11 +601,12 @@ int64_t slots_of(int64_t T, int64_t n, int64_t K, int64_t N) { return T / run_ro
 // Segments of less than 32 rows on average would leave half of their tiles empty.
 bool long_segments(int64_t T, int64_t S) { return S > 0 && T >= 32 * S; }
 int64_t chunks_of(int64_t T, int64_t S) { return T / kRows + S; }      // most chunks there can be
-// CTAs that share an adapter's rows: as many as are resident at once, if as many adapters as there are segments have rows, and
-// no more than leaves each of them four chunks.
+// CTAs that share an adapter's rows: as many as are resident at once, if as many adapters as there are segments have rows; where
+// those would be too few for two, four, which evens out adapters of unequal size.  Each has four chunks at least.
 int splits_of(int64_t T, int64_t S, int64_t n, int64_t tiles, int resident) {
     const int64_t active = std::min(n, S), most = std::min<int64_t>(8, std::max<int64_t>(1, T / active / (4 * kRows)));
-    return (int)std::max<int64_t>(1, std::min(most, (int64_t)resident / (tiles * active)));
+    const int64_t fit = resident / (tiles * active);
+    return (int)std::min(most, fit >= 2 ? fit : 4);
 }
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }

@@ -116,6 +116,7 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
         const int row = e / S::RP, c = e % S::RP;
         if (row >= tile.rows || c >= a.r) continue;
         float v = 0.f;
+#pragma unroll 2
         for (int s = 0; s < splits; ++s) {
             const float* other = splits > 1 ? cluster.map_shared_rank(sums, s) : sums;
 #pragma unroll
@@ -249,8 +250,15 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
     for (int e = rank * (kThreads + 32) + threadIdx.x; e < S::TM * S::RP; e += splits * (kThreads + 32)) {
         const int r = e / S::RP, c = e % S::RP;
         if (r >= tile.rows || c >= a.r) continue;
-        float v = 0.f;
-        for (int s = 0; s < splits; ++s) v += (splits > 1 ? cluster.map_shared_rank(sums, s) : sums)[e];
+        float v = sums[e];
+        if (splits > 1) {                              // all CTAs' numbers under way before the first is added
+            float x[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s) x[s] = s < splits ? cluster.map_shared_rank(sums, s)[e] : 0.f;
+            v = x[0];
+#pragma unroll
+            for (int s = 1; s < 8; ++s) v += x[s];
+        }
         out[(int64_t)r * a.r + c] = v * scale;
     }
     if (splits > 1) cluster.sync();                    // the others have read this CTA's sums
