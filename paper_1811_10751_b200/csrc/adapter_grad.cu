@@ -434,27 +434,64 @@ __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job 
     }
 }
 
+// The tensor cores take both tiles as TMA leaves them, rows of y and h being the depth of the product: D (128 columns of y x
+// RP columns of h) in tensor memory, two accumulators in turn.  One warp issues copies, one the products, four pull a finished
+// accumulator into registers and add it up to nearest: the chain of truncating additions in tensor memory is cut every chunk (FP32
+// gradients of three parts: 12 steps) or every fourth.
 template <int MT, int PARTS>
 struct TmaShape {
-    static constexpr int RP = 16 * MT, WARPS = MT <= 4 ? 4 : 8, NT = 16 / WARPS, STAGES = MT == 8 && PARTS == 3 ? 2 : 3;   // NT: 8 columns each, of a warp
+    static constexpr int RP = 16 * MT, GROUP = PARTS == 3 ? 1 : 4, COLS = 2 * RP < 32 ? 32 : 2 * RP;      // columns of tensor memory
     using Y = WTile<kRows, kCols>;
     using H = WTile<kRows, RP>;
-    static constexpr int STAGE = Y::BYTES + PARTS * H::BYTES, SMEM = STAGES * STAGE + 1024;
+    static constexpr int STAGE = Y::BYTES + PARTS * H::BYTES;
+    static constexpr int STAGES = MT == 8 ? (PARTS == 3 ? 3 : 4) : MT == 4 && PARTS == 3 ? 2 : 3;
+    static constexpr int SMEM = STAGES * STAGE + 1024, PER_SM = per_sm(SMEM) < 3 ? per_sm(SMEM) : 3;
 };
 struct GradMaps { CUtensorMap y[2], h[2]; };
+constexpr int kTmaThreads = 192;
+
+// Tile of [depth][PITCH / 2 elements] rows: eight rows of PITCH bytes make a swizzled group, the next eight follow; further
+// columns lie `part` bytes on.
+template <int PITCH>
+__device__ __forceinline__ uint64_t depth_first(uint32_t at, uint32_t part) {
+    const uint64_t layout = PITCH == 128 ? 2 : PITCH == 64 ? 4 : 6;
+    return (uint64_t)(at >> 4 & 0x3fff) | (uint64_t)(part >> 4 & 0x3fff) << 16 | (uint64_t)(8 * PITCH >> 4) << 32 | (uint64_t)1 << 46 | layout << 61;
+}
+__device__ __forceinline__ void umma_16(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+}
 
 template <typename T, typename O, int MT, int PARTS>
-__global__ void __launch_bounds__(TmaShape<MT, PARTS>::WARPS * 32 + 32, MT <= 4 ? (per_sm(TmaShape<MT, PARTS>::SMEM) < 3 ? per_sm(TmaShape<MT, PARTS>::SMEM) : 3) : 1)
+__global__ void __launch_bounds__(kTmaThreads, TmaShape<MT, PARTS>::PER_SM)
 grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ Job job, int splits) {
     using S = TmaShape<MT, PARTS>;
-    constexpr int WARPS = S::WARPS, NT = S::NT;
+    constexpr int RP = S::RP;
     constexpr bool kScaled = std::is_same<T, __half>::value;
     extern __shared__ unsigned char raw[];
     __shared__ Ring<S::STAGES> ring;
+    __shared__ uint64_t acc_full[2], acc_empty[2], done;
+    __shared__ uint32_t tmem_slot;
     __shared__ int rows_of[S::STAGES];                 // rows of the stages' chunks
     unsigned char* smem = raw + (1024 - (smem_at(raw) & 1023)) % 1024;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) ring.init(1, WARPS);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&acc_full[i], 1);
+            tc::mbar_init(&acc_empty[i], 4);
+        }
+        tc::mbar_init(&done, 1);
+        ring.init(1, 1);
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_slot)), "r"(S::COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
     after_previous();
     // the cluster's adapter; this CTA's chunks of it
     const int id = blockIdx.x / splits, rank = blockIdx.x % splits, first = job.slots[id], have = job.slots[id + 1] - first;
@@ -463,15 +500,12 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
     const GradArgs& a = job.two[second];
     const int c0 = (int)(blockIdx.y - (second ? job.first_tiles : 0)) * kCols;
     const float scale = a.scale ? a.scale[id] : 1.f;
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    float sum[MT][NT][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[m][j][i] = 0.f;
-    if (warp == WARPS) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_slot;
+    float sum[RP];
+    if (warp == 0) {
         int k = 0;
         int2 next = make_int2(0, 0);
         for (; k < n; ++k) {
@@ -490,86 +524,84 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
         }
         __syncwarp();
         if (lane == 0) ring.drain(k, &g_grad_status);
-    } else
-    for (int k = 0; k < n && ring.wait_full(k, &g_grad_status); ++k) {
-        const uint32_t stage = smem_at(smem) + k % S::STAGES * S::STAGE;
-        // a warp's columns: 32 (half of a part of 64) or 16
-        const uint32_t ys = S::Y::on(S::Y::lane_at(stage, row_first(), row_first_col()), 0, 8 * NT * warp);
-        const uint32_t hs = S::H::lane_at(stage + S::Y::BYTES, col_first_row(), col_first());
-        const int rows = rows_of[k % S::STAGES];
-        float acc[MT][NT][4];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.f;
-        // rows behind the segment's end, whatever they hold, are taken out of both operands
-        auto chunk = [&](auto masked) {
-#pragma unroll (masked.value ? 1 : 2)
-            for (int s = 0; s < kRows / 16; ++s) {
-                uint32_t low = 0xffffffffu, high = 0xffffffffu;        // rows 16 s + 2 q and the next; and eight rows on
-                if (masked.value) {
-                    const int t = 16 * s + 2 * (lane & 3);
-                    low = (t < rows ? 0xffffu : 0u) | (t + 1 < rows ? 0xffff0000u : 0u);
-                    high = (t + 8 < rows ? 0xffffu : 0u) | (t + 9 < rows ? 0xffff0000u : 0u);
-                }
-                uint32_t b[NT / 2][4];
-#pragma unroll
-                for (int j = 0; j < NT / 2; ++j) {
-                    ldmatrix4<true>(b[j], S::Y::on(ys, 16 * s, 16 * j));
-                    if (masked.value) {
-                        b[j][0] &= low;
-                        b[j][1] &= high;
-                        b[j][2] &= low;
-                        b[j][3] &= high;
-                    }
-                }
-#pragma unroll
-                for (int p = PARTS - 1; p >= 0; --p)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        uint32_t h[4];
-                        ldmatrix4<true>(h, S::H::on(hs, 16 * s, 16 * m) + p * S::H::BYTES);
-                        if (masked.value) {
-                            h[0] &= low;
-                            h[1] &= low;
-                            h[2] &= high;
-                            h[3] &= high;
-                        }
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) mma(acc[m][j], h, b[j / 2][2 * (j & 1)], b[j / 2][2 * (j & 1) + 1], T());
-                    }
+    } else if (warp == 1) {
+        // FP32 sums of two BF16 or FP16 operands, both depth first, 128 x RP
+        constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+        constexpr uint32_t what = 1u << 4 | kType << 7 | kType << 10 | 1u << 15 | 1u << 16 | (uint32_t)(RP >> 3) << 17 | (uint32_t)(kCols >> 4) << 24;
+        for (int k = 0; k < n; ++k) {
+            const int buf = k / S::GROUP & 1, s = k % S::STAGES;
+            const bool fresh = k % S::GROUP == 0;
+            bool live = ring.wait_full(k, &g_grad_status);
+            if (live && fresh) live = tc::mbar_wait(&acc_empty[buf], (k / S::GROUP >> 1 & 1) ^ 1, &ring.abort, &g_grad_status);
+            if (!__all_sync(0xffffffffu, live)) break;
+            unsigned char* stage = smem + s * S::STAGE;
+            const int rows = rows_of[s];
+            if (rows < kRows) {                        // rows behind the segment's end are another's, whatever they hold
+                auto clear = [&](unsigned char* part, int pitch) {
+                    for (int i = rows * pitch / 16 + lane; i < kRows * pitch / 16; i += 32) reinterpret_cast<uint4*>(part)[i] = make_uint4(0, 0, 0, 0);
+                };
+                for (int i = 0; i < S::Y::PARTS; ++i) clear(stage + i * kRows * 128, 128);
+                for (int p = 0; p < PARTS; ++p)
+                    for (int i = 0; i < S::H::PARTS; ++i) clear(stage + S::Y::BYTES + p * S::H::BYTES + i * kRows * 128, S::H::PITCH);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
             }
-        };
-        if (rows == kRows) chunk(std::false_type());
-        else chunk(std::true_type());
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&ring.empty[k % S::STAGES]);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (lane == 0) {
+                const uint32_t ys = smem_at(stage), hs = ys + S::Y::BYTES;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+                for (int d = 0; d < kRows / 16; ++d)
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[m][j][i] += acc[m][j][i];
-    }
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int kr = 16 * m + (lane >> 2) + 8 * (i >> 1);
-            const float by = kScaled ? scale * power2(exponent_of(__int_as_float(job.most[((int64_t)second * job.seg.n + id) * S::RP + kr]))) : scale;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sum[m][j][i] *= by;
+                    for (int p = PARTS - 1; p >= 0; --p)               // the small parts first
+                        umma_16(tmem + buf * RP, depth_first<128>(ys + d * 16 * 128, kRows * 128),
+                                depth_first<S::H::PITCH>(hs + p * S::H::BYTES + d * 16 * S::H::PITCH, kRows * 128), what, !(fresh && d == 0 && p == PARTS - 1));
+                tc::umma_commit(&ring.empty[s]);
+                if (k % S::GROUP == S::GROUP - 1 || k == n - 1) tc::umma_commit(&acc_full[buf]);
+            }
+            __syncwarp();
         }
+        if (lane == 0) {                               // nothing is under way when the memory gets another use
+            int never = 0;
+            tc::umma_commit(&done);
+            tc::mbar_wait(&done, 0, &never, &g_grad_status);
+        }
+        __syncwarp();
+    } else {
+#pragma unroll
+        for (int c = 0; c < RP; ++c) sum[c] = 0.f;
+        const uint32_t mine = tmem + ((uint32_t)(warp & 3) * 32 << 16);
+        for (int i = 0; i * S::GROUP < n; ++i) {
+            const int buf = i & 1;
+            const bool live = tc::mbar_wait(&acc_full[buf], i >> 1 & 1, &ring.abort, &g_grad_status);
+            if (!__all_sync(0xffffffffu, live)) break; // loads from tensor memory are the whole warp's
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int c = 0; c < RP; c += 16) {
+                uint32_t r[16];
+                tmem_ld16(mine + buf * RP + c, r);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[c + j] += __uint_as_float(r[j]);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&acc_empty[buf]);
+        }
+    }
     float* tile = reinterpret_cast<float*>(smem);
-    __syncthreads();                                   // every stage has been read
-    if (warp < WARPS) put_tile<MT, NT>(sum, tile);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();                                   // every stage and accumulator has been read
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::COLS) : "memory");
+    if (warp >= 2) {
+        const int32_t* most = job.most + ((int64_t)second * job.seg.n + id) * RP;
+#pragma unroll
+        for (int c = 0; c < RP; ++c) tile[c * kTileWidth + (warp & 3) * 32 + lane] = sum[c] * (kScaled ? scale * power2(exponent_of(__int_as_float(most[c]))) : scale);
+    }
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     if (splits > 1) cluster.sync();
     else __syncthreads();
-    constexpr int THREADS = 32 * WARPS + 32;
-    write_tile<O>(job, a, id, c0, rank * THREADS + threadIdx.x, splits * THREADS, [&](int k, int c) {
+    write_tile<O>(job, a, id, c0, rank * kTmaThreads + threadIdx.x, splits * kTmaThreads, [&](int k, int c) {
         const int at = k * kTileWidth + c;
         float4 v = *reinterpret_cast<const float4*>(tile + at);
         if (splits > 1) {                              // all CTAs' numbers under way before the first is added
@@ -636,9 +668,9 @@ gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t
         const int most_chunks = (int)chunks_of(job.seg.T, job.seg.S);
         rc = launch_after(split_kernel<T, PARTS>, dim3(blocks), dim3(256), 0, 1, st, job, RP, planes, most_chunks, counts, slots);
         if (rc != GPD_OK) return rc;
-        const int per = MT <= 4 ? std::min(3, per_sm(S::SMEM)) : 1, splits = splits_of(job.seg.T, job.seg.S, job.seg.n, job.tiles, per * sm_count());
+        const int splits = splits_of(job.seg.T, job.seg.S, job.seg.n, job.tiles, S::PER_SM * sm_count());
         if (job.tiles > 65535 || (int64_t)job.seg.n * splits > 0x7fffffff) return GPD_ERR_SHAPE;
-        return launch_after(kernel, dim3((unsigned)(job.seg.n * splits), job.tiles), dim3(S::WARPS * 32 + 32), S::SMEM, splits, st, maps, job, splits);
+        return launch_after(kernel, dim3((unsigned)(job.seg.n * splits), job.tiles), dim3(kTmaThreads), S::SMEM, splits, st, maps, job, splits);
     }
     {
         using S = Shape<MT, PARTS>;
