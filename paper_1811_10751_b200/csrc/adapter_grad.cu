@@ -444,7 +444,7 @@ struct TmaShape {
     using Y = WTile<kRows, kCols>;
     using H = WTile<kRows, RP>;
     static constexpr int STAGE = Y::BYTES + PARTS * H::BYTES;
-    static constexpr int STAGES = MT == 8 ? (PARTS == 3 ? 3 : 4) : MT == 4 && PARTS == 3 ? 2 : 3;
+    static constexpr int STAGES = MT == 8 ? (PARTS == 3 ? 3 : 4) : MT == 4 ? 2 : 3;
     static constexpr int SMEM = STAGES * STAGE + 1024, PER_SM = per_sm(SMEM) < 3 ? per_sm(SMEM) : 3;
 };
 struct GradMaps { CUtensorMap y[2], h[2]; };
@@ -633,12 +633,11 @@ int64_t slots_of(int64_t T, int64_t n, int64_t K, int64_t N) { return T / run_ro
 // Segments of less than 32 rows on average would leave half of their tiles empty.
 bool long_segments(int64_t T, int64_t S) { return S > 0 && T >= 32 * S; }
 int64_t chunks_of(int64_t T, int64_t S) { return T / kRows + S; }      // most chunks there can be
-// CTAs that share an adapter's rows: as many as are resident at once, if as many adapters as there are segments have rows; where
-// those would be too few for two, four, which evens out adapters of unequal size.  Each has four chunks at least.
+// CTAs that share an adapter's rows: as many as are resident at once, if as many adapters as there are segments have rows; each has
+// four chunks at least.
 int splits_of(int64_t T, int64_t S, int64_t n, int64_t tiles, int resident) {
     const int64_t active = std::min(n, S), most = std::min<int64_t>(8, std::max<int64_t>(1, T / active / (4 * kRows)));
-    const int64_t fit = resident / (tiles * active);
-    return (int)std::min(most, fit >= 2 ? fit : 4);
+    return (int)std::min(most, std::max<int64_t>(1, resident / (tiles * active)));
 }
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 : 128; }
