@@ -269,11 +269,12 @@ gpd_status launch_tma(const ShrinkArgs& a, cudaStream_t st) {
     using S = TmaShape<NT, TRANS>;
     const int64_t tiles = tiles_of(a.seg, S::TM), stages = (a.C + kDeep - 1) / kDeep;
     // The parts of a tile's columns with which the busiest SM is done first, a CTA costing about six stages beside its own:
-    // an SM that has one CTA more than the others holds all up.
+    // an SM that has one CTA more than the others holds all up, and one that has less than three does not reach its share
+    // of the bandwidth (16384 x 8192, rank 32, 280 tiles: two parts 165 us for both products, one 175).
     int splits = 1;
     int64_t best = 0;
     for (int s = 1; s <= 8; s *= 2) {
-        const int64_t per = (tiles * s + sm_count() - 1) / sm_count(), time = std::max<int64_t>(per, 2) * ((stages + s - 1) / s + 6);
+        const int64_t per = (tiles * s + sm_count() - 1) / sm_count(), time = std::max<int64_t>(per, 3) * ((stages + s - 1) / s + 6);
         if (s == 1 || time < best) {
             best = time;
             splits = s;

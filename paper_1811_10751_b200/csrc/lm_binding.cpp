@@ -529,17 +529,20 @@ gpd_status adapter_backward(PyObject* const* args, Py_ssize_t n) {
                                 acc, T, K, f.N, ws, ws_bytes, c.stream(14));
 }
 
-// Tensors of a list: floating types, on the call's device, dense (in any order of their dimensions).
+// Tensors of a list or tuple: floating types, on the call's device, dense (in any order of their dimensions).
 struct TensorList {
-    std::vector<int32_t> types;
-    std::vector<void*> at;
+    PyObject* items = nullptr;                         // keeps the tensors
+    int32_t n = 0;
     std::vector<int64_t> counts;
-    std::vector<const at::Tensor*> tensors;            // borrowed from the list's items, which `items` keeps
-    PyObject* items = nullptr;
+    std::vector<void*> at;
+    std::vector<int32_t> types;
     TensorList(const Call& c, const char* name, PyObject* list) {
         if (THPVariable_Check(list)) refuse(name, "list of tensors expected");
-        items = PySequence_Tuple(list);
-        if (!items) throw PythonError();
+        items = PySequence_Fast(list, "list of tensors expected");
+        if (!items) {
+            PyErr_Clear();
+            refuse(name, "list of tensors expected");
+        }
         try {
             fill(c, name);
         } catch (...) {
@@ -550,25 +553,25 @@ struct TensorList {
     ~TensorList() { Py_DECREF(items); }
     TensorList(const TensorList&) = delete;
     TensorList& operator=(const TensorList&) = delete;
+    const at::Tensor& tensor(int32_t i) const { return THPVariable_Unpack(PySequence_Fast_GET_ITEM(items, i)); }
 
 private:
     void fill(const Call& c, const char* name) {
-        const Py_ssize_t n = PyTuple_GET_SIZE(items);
-        if (n > 0x7fffffff) refuse(name, "too many tensors");
-        types.reserve(n);
-        at.reserve(n);
-        counts.reserve(n);
-        tensors.reserve(n);
-        for (Py_ssize_t i = 0; i < n; ++i) {
-            PyObject* o = PyTuple_GET_ITEM(items, i);
+        const Py_ssize_t size = PySequence_Fast_GET_SIZE(items);
+        if (size > 0x7fffffff) refuse(name, "too many tensors");
+        n = (int32_t)size;
+        counts.resize(n);
+        at.resize(n);
+        types.resize(n);
+        for (int32_t i = 0; i < n; ++i) {
+            PyObject* o = PySequence_Fast_GET_ITEM(items, i);
             if (!THPVariable_Check(o)) refuse(name, "list of tensors expected");
             const at::Tensor& t = THPVariable_Unpack(o);
-            types.push_back(gpd_type(c.check_type(name, t, kFloats)));
+            types[i] = gpd_type(c.check_type(name, t, kFloats));
             c.check_device(name, t);
             if (!t.is_non_overlapping_and_dense()) refuse(name, "dense tensors expected, item " + std::to_string(i) + " is not");
-            at.push_back(t.numel() ? t.data_ptr() : nullptr);
-            counts.push_back(t.numel());
-            tensors.push_back(&t);
+            counts[i] = t.numel();
+            at[i] = counts[i] ? t.data_ptr() : nullptr;
         }
     }
 };
@@ -581,7 +584,7 @@ gpd_status grad_norm(PyObject* const* args, Py_ssize_t n) {
     const TensorList g(c, "grads", args[0]);
     int64_t ws_bytes = 0;
     void* ws = c.buffer("workspace", 2, &ws_bytes);
-    return gpd_grad_norm((int32_t)g.at.size(), g.types.data(), g.at.data(), g.counts.data(), norm, ws, ws_bytes, c.stream(3));
+    return gpd_grad_norm(g.n, g.types.data(), g.at.data(), g.counts.data(), norm, ws, ws_bytes, c.stream(3));
 }
 
 gpd_status clip_grads(PyObject* const* args, Py_ssize_t n) {
@@ -592,17 +595,17 @@ gpd_status clip_grads(PyObject* const* args, Py_ssize_t n) {
     const TensorList g(c, "grads", args[0]);
     const float max_norm = (float)c.number(2);
     if (c.absent(3))
-        return gpd_clip_grads((int32_t)g.at.size(), g.types.data(), g.at.data(), g.types.data(), g.at.data(), g.counts.data(), norm, max_norm,
+        return gpd_clip_grads(g.n, g.types.data(), g.at.data(), g.types.data(), g.at.data(), g.counts.data(), norm, max_norm,
                               c.stream(4));
     const TensorList o(c, "out", args[3]);
-    if (o.at.size() != g.at.size()) refuse("out", std::to_string(g.at.size()) + " tensors expected, got " + std::to_string(o.at.size()));
-    for (size_t i = 0; i < g.at.size(); ++i) {
-        const at::Tensor &a = *g.tensors[i], &b = *o.tensors[i];
+    if (o.n != g.n) refuse("out", std::to_string(g.n) + " tensors expected, got " + std::to_string(o.n));
+    for (int32_t i = 0; i < g.n; ++i) {
+        const at::Tensor &a = g.tensor(i), &b = o.tensor(i);
         if (a.sizes() != b.sizes()) refuse("out", "item " + std::to_string(i) + " has shape " + shape_text(b) + " for a gradient of shape " + shape_text(a));
         if (a.strides() != b.strides() && !(a.is_contiguous() && b.is_contiguous()))
             refuse("out", "item " + std::to_string(i) + " has its dimensions in another order than its gradient");
     }
-    return gpd_clip_grads((int32_t)g.at.size(), g.types.data(), g.at.data(), o.types.data(), o.at.data(), g.counts.data(), norm, max_norm,
+    return gpd_clip_grads(g.n, g.types.data(), g.at.data(), o.types.data(), o.at.data(), g.counts.data(), norm, max_norm,
                           c.stream(4));
 }
 
