@@ -39,8 +39,7 @@ struct Job {
 
 // Runs of every adapter, `least` or more.  One CTA; counts: n numbers of scratch.  Segments take up whole multiples of `unit` rows.
 __device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int unit, int least, int max_slots, unsigned long long* counts, int32_t* slots) {
-    __shared__ int warp_sum[8];
-    __shared__ int carry;
+    __shared__ long long warp_sum[8], carry;           // offsets that mean nothing may add up to anything
     for (int i = threadIdx.x; i < s.n; i += 256) counts[i] = 0;
     if (threadIdx.x == 0) carry = 0;
     __syncthreads();
@@ -53,24 +52,24 @@ __device__ __forceinline__ void plan_runs(const Segments& s, int64_t run, int un
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int base = 0; base < s.n; base += 256) {
         const int i = base + threadIdx.x;
-        const int64_t want = i < s.n ? max((int64_t)least, ((int64_t)counts[i] + run - 1) / run) : 0;
-        const int own = (int)min(want, (int64_t)max_slots);
-        int scan = own;
+        const int64_t want = i < s.n ? max((int64_t)least, ((int64_t)__ldcg(counts + i) + run - 1) / run) : 0;
+        const long long own = min(want, (int64_t)max_slots);
+        long long scan = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, scan, o);
+            const long long v = __shfl_up_sync(0xffffffffu, scan, o);
             if (lane >= o) scan += v;
         }
         if (lane == 31) warp_sum[warp] = scan;
         __syncthreads();
-        int before = carry;
+        long long before = carry;
         for (int k = 0; k < warp; ++k) before += warp_sum[k];
-        if (i < s.n) slots[i] = min(before + scan - own, max_slots);
+        if (i < s.n) slots[i] = (int)min(before + scan - own, (long long)max_slots);
         __syncthreads();
-        if (threadIdx.x == 255) carry = min(before + scan, max_slots);
+        if (threadIdx.x == 255) carry = min(before + scan, (long long)max_slots);
         __syncthreads();
     }
-    if (threadIdx.x == 0) slots[s.n] = carry;
+    if (threadIdx.x == 0) slots[s.n] = (int)carry;
 }
 __global__ void __launch_bounds__(256) plan_kernel(const __grid_constant__ Segments s, int64_t run, int max_slots, unsigned long long* counts,
                                                    int32_t* slots) {
