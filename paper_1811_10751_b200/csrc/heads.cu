@@ -150,39 +150,33 @@ __device__ __forceinline__ void load_floats(const float* p, bool vec, float (&f)
     }
 }
 
-// Cosines and sines of unit u at the positions `pos`, one for each axis.  Several axes: the rows of all of them are loaded, and every pair takes its
-// axis's; positions outside the table, and axes that there are none of, give NaN.
+// Cosines and sines of unit u at the rows `pos` of the table, one for each axis.  Several axes: every pair takes its own
+// from its axis's row, all loads at once.  Positions outside the table (-1), and axes that there are none of, give NaN.
 template <int V>
 __device__ __forceinline__ void angles(const HeadArgs& a, const int (&pos)[GPD_HEAD_MAX_AXES], int u, float (&cs)[V], float (&sn)[V]) {
-    if (a.A == 1 && pos[0] >= 0) {
-        const float* row = a.table + pos[0] * a.ldt + V * u;
-        load_floats<V>(row, a.table_vec, cs);
-        load_floats<V>(row + a.R / 2, a.table_vec, sn);
-        if (a.inverse) {
+    const float* first = a.table + V * u;
+    if (!a.axes) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) sn[i] = -sn[i];
+        for (int i = 0; i < V; ++i) cs[i] = sn[i] = __int_as_float(0x7fffffff);
+        if (pos[0] < 0) return;
+        load_floats<V>(first + pos[0] * a.ldt, a.table_vec, cs);
+        load_floats<V>(first + pos[0] * a.ldt + a.R / 2, a.table_vec, sn);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int x = __ldg(a.axes + V * u + i);
+            const int row = x >= a.A ? -1 : x == 0 ? pos[0] : x == 1 ? pos[1] : x == 2 ? pos[2] : pos[3];
+            cs[i] = sn[i] = __int_as_float(0x7fffffff);
+            if (row >= 0) {
+                const float* p = first + row * a.ldt + i;
+                cs[i] = __ldg(p);
+                sn[i] = __ldg(p + a.R / 2);
+            }
         }
-        return;
     }
-    unsigned long long axis = 0;
+    if (a.inverse) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        cs[i] = sn[i] = __int_as_float(0x7fffffff);
-        if (a.axes) axis |= (unsigned long long)__ldg(a.axes + V * u + i) << (8 * i);
-    }
-#pragma unroll
-    for (int x = 0; x < GPD_HEAD_MAX_AXES; ++x) {
-        if (x >= a.A || pos[x] < 0) continue;
-        const float* row = a.table + pos[x] * a.ldt + V * u;
-        float c[V], s[V];
-        load_floats<V>(row, a.table_vec, c);
-        load_floats<V>(row + a.R / 2, a.table_vec, s);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const bool mine = !a.axes || (int)(axis >> (8 * j) & 0xff) == x;
-            cs[j] = mine ? c[j] : cs[j];
-            sn[j] = mine ? (a.inverse ? -s[j] : s[j]) : sn[j];
-        }
+        for (int i = 0; i < V; ++i) sn[i] = -sn[i];
     }
 }
 // Rows of the table for token t, one for each axis; -1: none
