@@ -205,16 +205,28 @@ struct WTile {
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) tc::tma_load_3d(to + i * ROWS * 128, map, col + 64 * i, row, id, bar);
     }
-    // element by element, by one warp: rows off 16-byte boundaries.  What lies outside is zero already, or is written so.
-    template <typename T>
-    static __device__ __forceinline__ void copy(unsigned char* to, const T* p, int64_t ld, int64_t rows, int64_t cols, int used_rows, int used_cols) {
-        const int n = used_rows * used_cols, lane = threadIdx.x & 31;
-#pragma unroll 8
-        for (int i = lane; i < n; i += 32) {
-            const int r = i / used_cols, c = i % used_cols;
-            T v = from_f32<T>(0.f);
-            if (r < rows && c < cols) v = p[r * ld + c];
-            *reinterpret_cast<T*>(to + at(r, c)) = v;
+    // Element by element, by one warp: rows off 16-byte boundaries.  What lies outside is zero already, or is written so.
+    // BY_ROW: a lane has two of the 64 rows, and `rank` columns of them are used; otherwise two of the 64 columns, and `rank`
+    // rows.  All loads of eight of these before the first store.
+    template <bool BY_ROW, typename T>
+    static __device__ __forceinline__ void copy(unsigned char* to, const T* p, int64_t ld, int64_t rows, int64_t cols, int rank) {
+        const int lane = threadIdx.x & 31;
+        constexpr int N = 8;
+        for (int first = 0; first < rank; first += N) {
+            T v[N][2];
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = BY_ROW ? lane + 32 * i : first + j, c = BY_ROW ? first + j : lane + 32 * i;
+                    v[j][i] = from_f32<T>(0.f);
+                    if (first + j < rank && r < rows && c < cols) v[j][i] = p[r * ld + c];
+                }
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (first + j < rank) *reinterpret_cast<T*>(to + (BY_ROW ? at(lane + 32 * i, first + j) : at(first + j, lane + 32 * i))) = v[j][i];
         }
     }
 };

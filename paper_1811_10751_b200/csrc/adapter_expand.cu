@@ -184,8 +184,8 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                 if (!a.w_vec) {
                     if (!none) {
                         const T* w = static_cast<const T*>(a.w) + (int64_t)tile.id * a.next + (TRANS ? c : c * a.ldw);
-                        if (TRANS) S::W::copy(ws, w, a.ldw, a.r, a.C - c, a.r, kCols);
-                        else S::W::copy(ws, w, a.ldw, a.C - c, a.r, kCols, a.r);
+                        if (TRANS) S::W::template copy<false>(ws, w, a.ldw, a.r, a.C - c, a.r);
+                        else S::W::template copy<true>(ws, w, a.ldw, a.C - c, a.r, a.r);
                     }
                     tc::mbar_arrive(bar);
                 }

@@ -355,9 +355,12 @@ __device__ int g_grad_status = 0;                      // GPD_ERR_TIMEOUT if a b
 
 // FP16: the largest magnitudes of the columns of u and h (blockIdx.y), for every adapter; `most` is zero before.
 __global__ void __launch_bounds__(256) most_kernel(const __grid_constant__ Job job, int RP, int32_t* most) {
+    __shared__ int32_t here[kMaxRank];
     after_previous();
     const float* h = job.two[blockIdx.y].h;
     const int r = job.r;
+    if (threadIdx.x < RP) here[threadIdx.x] = 0;
+    __syncthreads();
     for (int s = blockIdx.z; s < job.seg.S; s += gridDim.z) {
         const int64_t id = number(job.seg.index, s, job.seg.wide);
         if (id < 0 || id >= job.seg.n) continue;
@@ -366,8 +369,16 @@ __global__ void __launch_bounds__(256) most_kernel(const __grid_constant__ Job j
         const int c = threadIdx.x % RP, step = 256 / RP;
         float m = 0.f;
         if (c < r)
+#pragma unroll 4
             for (int64_t t = from + (int64_t)blockIdx.x * step + threadIdx.x / RP; t < to; t += (int64_t)gridDim.x * step) m = fmaxf(m, fabsf(h[t * r + c]));
-        if (m > 0.f) atomicMax(most + ((int64_t)blockIdx.y * job.seg.n + id) * RP + c, __float_as_int(m));     // order does not matter
+        if (m > 0.f) atomicMax(here + c, __float_as_int(m));           // order does not matter
+        __syncthreads();
+        if (threadIdx.x < RP) {
+            const int32_t all = here[threadIdx.x];
+            if (all > 0) atomicMax(most + ((int64_t)blockIdx.y * job.seg.n + id) * RP + threadIdx.x, all);
+            here[threadIdx.x] = 0;
+        }
+        __syncthreads();
     }
 }
 // The adapter's chunks, `count` at most.  One warp.
@@ -657,7 +668,7 @@ gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
         if (std::is_same<T, __half>::value) {
             const int RP = S::RP;
-            const unsigned z = (unsigned)std::min<int64_t>(job.seg.S, 64), x = (unsigned)std::max<int64_t>(1, std::min<int64_t>(256 / z, job.seg.T / z / 64));
+            const unsigned z = (unsigned)std::min<int64_t>(job.seg.S, 64), x = (unsigned)std::max<int64_t>(1, std::min<int64_t>(1024 / z, job.seg.T / z * RP / 1024));
             rc = launch_after(most_kernel, dim3(x, 2, z), dim3(256), 0, 1, st, job, RP, most);
             if (rc != GPD_OK) return rc;
         }

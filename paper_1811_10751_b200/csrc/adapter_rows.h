@@ -72,9 +72,10 @@ __device__ __forceinline__ void store_sum(const Share<O>& s, const float (&acc)[
     const int q = threadIdx.x & 3;
     if constexpr (sizeof(O) == 4) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int i = 0; i < 2; ++i) {
+            if (i == 1 && !both) break;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int n = 0; n < 8; ++n) {
                 const int c = 8 * n + 2 * q;
                 if (!has[i] || c >= cols) continue;
                 float* p = out + 8 * i * ld + c;
@@ -86,6 +87,7 @@ __device__ __forceinline__ void store_sum(const Share<O>& s, const float (&acc)[
                     if (c + 1 < cols) p[1] = v.y;
                 }
             }
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {

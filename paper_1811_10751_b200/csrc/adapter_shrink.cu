@@ -194,8 +194,8 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
             }
             if (!a.w_vec) {
                 const T* w = static_cast<const T*>(a.w) + (int64_t)tile.id * a.next + (TRANS ? c * a.ldw : c);
-                if (TRANS) S::W::copy(at + S::X_BYTES, w, a.ldw, a.C - c, a.r, kDeep, a.r);
-                else S::W::copy(at + S::X_BYTES, w, a.ldw, a.r, a.C - c, a.r, kDeep);
+                if (TRANS) S::W::template copy<true>(at + S::X_BYTES, w, a.ldw, a.C - c, a.r, a.r);
+                else S::W::template copy<false>(at + S::X_BYTES, w, a.ldw, a.r, a.C - c, a.r);
                 tc::mbar_arrive(bar);
             }
         }

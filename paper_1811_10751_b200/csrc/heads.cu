@@ -219,7 +219,9 @@ __device__ __forceinline__ float lanes_sum(float v, int G) {
     }
     const int first = (threadIdx.x & 31) / G * G;
     float sum = 0.f;
-    for (int i = 0; i < G; ++i) sum += __shfl_sync(0xffffffffu, v, (first + i) & 31);
+#pragma unroll
+    for (int i = 0; i < 10; ++i)                       // from eleven on the next power of two has as many heads
+        if (i < G) sum += __shfl_sync(0xffffffffu, v, (first + i) & 31);
     return sum;
 }
 
