@@ -37,6 +37,7 @@ int64_t sgemm_3xtf32_scratch_bytes(int64_t pieces);
 gpd_status bounded_wait_selftest_launch(long long limit_cycles, cudaStream_t st);
 int tf32_device_status_fetch_and_clear();   // synchronous read of the tensor-path status word
 int fp8_device_status_fetch_and_clear();    // the same for the 8-bit product
-int adapter_status_fetch_and_clear();       // and for the adapters' kernels
+int adapter_status_fetch_and_clear();       // for the adapters' kernels
+int heads_status_fetch_and_clear();         // and for those of the head norms
 
 }  // namespace gpd

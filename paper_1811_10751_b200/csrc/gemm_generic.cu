@@ -217,6 +217,7 @@ extern "C" gpd_status gpd_device_status(int32_t* status_host) {
     if (cudaDeviceSynchronize() != cudaSuccess) return GPD_ERR_CUDA;
     const int a = tf32_device_status_fetch_and_clear(), b = i8_device_status_fetch_and_clear();
     const int c = fp8_device_status_fetch_and_clear(), d = adapter_status_fetch_and_clear();
-    *status_host = a != 0 ? a : b != 0 ? b : c != 0 ? c : d;
+    const int e = heads_status_fetch_and_clear();
+    *status_host = a != 0 ? a : b != 0 ? b : c != 0 ? c : d != 0 ? d : e;
     return GPD_OK;
 }

@@ -13,7 +13,9 @@
 #include <algorithm>
 #include <numeric>
 
+#include "gemm_common.h"
 #include "lm_common.h"
+#include "tc_common.h"
 
 namespace gpd {
 
@@ -21,7 +23,7 @@ namespace {
 
 using namespace lm;
 
-constexpr int kWarps = 4;                              // of a CTA
+constexpr int kWarps = 4, kWalkPerSm = 4;              // warps of a CTA; CTAs of the forward pass on an SM
 constexpr int kMaxHead = GPD_HEAD_MAX_DIM;
 
 // Queries or keys
@@ -206,23 +208,15 @@ __device__ __forceinline__ void weights(const HeadArgs& a, const void* w, const 
     }
     to_pairs<V>(x, y, a.neighbours, wa, wb);
 }
-// Sum over the G lanes of a head: a power of two, or any number (then every lane adds them up in the same order).
+// Sum over the G lanes of a head
 __device__ __forceinline__ float lanes_sum(float v, int G) {
     if (G == 8) {                                      // 128 columns of 16 bits
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
-    }
-    if ((G & (G - 1)) == 0) {
+    } else {
         for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
     }
-    const int first = (threadIdx.x & 31) / G * G;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 10; ++i)                       // from eleven on the next power of two has as many heads
-        if (i < G) sum += __shfl_sync(0xffffffffu, v, (first + i) & 31);
-    return sum;
+    return v;
 }
 
 // Rows that no vector fits: element by element, N units per lane.
@@ -451,6 +445,17 @@ __global__ void __launch_bounds__(1024) heads_dweight_kernel(const float* parts,
 }
 
 // ---- the same with whole vectors: warps walk over the work, the next piece's loads under way --------------------------
+template <typename T, int V>
+__device__ __forceinline__ void write_vec(uint32_t to, const float (&f)[V]) {
+    uint32_t w[V * sizeof(T) / 4];
+#pragma unroll
+    for (int i = 0; i < (int)(V * sizeof(T) / 4); ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+        else w[i] = pack2(f[2 * i], f[2 * i + 1], T());
+    }
+    if constexpr (V * sizeof(T) == 16) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    else asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(w[0]), "r"(w[1]) : "memory");
+}
 // Halves of a unit's pairs, two at a time
 template <typename T, int V, bool NEAR>
 __device__ __forceinline__ void pairs(const Vec<T, V>& r1, const Vec<T, V>& r2, F2 (&a)[V / 2], F2 (&b)[V / 2]) {
@@ -472,9 +477,8 @@ __device__ __forceinline__ void pairs(const Vec<T, V>& r1, const Vec<T, V>& r2, 
         b[i] = NEAR ? f2(w[2 * i].y, w[2 * i + 1].y) : f2(w[V / 2 + i].x, w[V / 2 + i].y);
     }
 }
-template <typename T, int V, bool NEAR>
-__device__ __forceinline__ void store_pairs(T* p1, T* p2, const F2 (&a)[V / 2], const F2 (&b)[V / 2]) {
-    float x[V], y[V];
+template <int V, bool NEAR>
+__device__ __forceinline__ void from_pairs2(const F2 (&a)[V / 2], const F2 (&b)[V / 2], float (&x)[V], float (&y)[V]) {
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
         const float2 u = f2(a[i]), v = f2(b[i]);
@@ -492,21 +496,33 @@ __device__ __forceinline__ void store_pairs(T* p1, T* p2, const F2 (&a)[V / 2], 
             y[2 * i + 1] = v.y;
         }
     }
+}
+template <typename T, int V, bool NEAR>
+__device__ __forceinline__ void store_pairs(T* p1, T* p2, const F2 (&a)[V / 2], const F2 (&b)[V / 2]) {
+    float x[V], y[V];
+    from_pairs2<V, NEAR>(a, b, x, y);
     store_vec<T, V>(p1, x);
     store_vec<T, V>(p2, y);
+}
+template <typename T, int V, bool NEAR>
+__device__ __forceinline__ void write_pairs(uint32_t p1, uint32_t p2, const F2 (&a)[V / 2], const F2 (&b)[V / 2]) {
+    float x[V], y[V];
+    from_pairs2<V, NEAR>(a, b, x, y);
+    write_vec<T, V>(p1, x);
+    write_vec<T, V>(p2, y);
 }
 template <int V>
 __device__ __forceinline__ void two_by_two(const float (&f)[V], F2 (&o)[V / 2]) {
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) o[i] = f2(f[2 * i], f[2 * i + 1]);
 }
-// (a, b) turned; ns: the sines negated
+// (a, b) turned
 template <int N>
-__device__ __forceinline__ void turn(F2 (&a)[N], F2 (&b)[N], const F2 (&c)[N], const F2 (&s)[N], const F2 (&ns)[N]) {
+__device__ __forceinline__ void turn(F2 (&a)[N], F2 (&b)[N], const F2 (&c)[N], const F2 (&s)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const F2 x = a[i];
-        a[i] = fma2(b[i], ns[i], mul2(x, c[i]));
+        a[i] = fma2(b[i] ^ 0x8000000080000000ull, s[i], mul2(x, c[i]));
         b[i] = fma2(x, s[i], mul2(b[i], c[i]));
     }
 }
@@ -515,11 +531,10 @@ __device__ __forceinline__ float both(F2 v) {
     return f.x + f.y;
 }
 
-// U: heads of a lane in one piece of work.  BACK: the gradient with norm; otherwise the forward pass, or the gradient without.
-template <typename T, int V, int U, bool NEAR, bool BACK>
-__global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(const __grid_constant__ HeadArgs a) {
+// The forward pass, or the gradient without norm.  U: heads of a lane in one piece of work.
+template <typename T, int V, int U, bool NEAR>
+__global__ void __launch_bounds__(32 * kWarps, kWalkPerSm) heads_walk_kernel(const __grid_constant__ HeadArgs a) {
     constexpr int P = V / 2;
-    __shared__ float shares[BACK ? kWarps : 1][BACK ? kMaxHead : 1];
     after_previous();
     const bool second = blockIdx.x >= a.split;
     const Part& p = a.part[second];
@@ -527,10 +542,9 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
     // a warp keeps to one chunk of heads and walks over the tokens: the part's warps are a multiple of its chunks
     const int warps = (int)(second ? gridDim.x - a.split : a.split) * kWarps, index = (int)(blockIdx.x - (second ? a.split : 0)) * kWarps + warp;
     const int step = warps / p.chunks, h0 = index % p.chunks * per * U + lane / G, T_all = (int)a.T;
-    Unit<V> u(lane % G, a);
-    u.there = u.there && lane < per * G;               // 32 need not be a multiple of G
+    const Unit<V> u(lane % G, a);
     const bool turned = u.there && u.turned;
-    F2 wa[P], wb[P], da[BACK ? P : 1], db[BACK ? P : 1];
+    F2 wa[P], wb[P];
     if (p.w && u.there) {
         float x[V], y[V];
         weights<T, V>(a, p.w, u, x, y);
@@ -540,15 +554,10 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
 #pragma unroll
         for (int i = 0; i < P; ++i) wa[i] = wb[i] = f2(0.f, 0.f);
     }
-    if (BACK) {
-#pragma unroll
-        for (int i = 0; i < P; ++i) da[i] = db[i] = f2(0.f, 0.f);
-    }
-    Vec<T, V> x1[U], x2[U], y1[BACK ? U : 1], y2[BACK ? U : 1];        // the next piece, as it comes
+    Vec<T, V> x1[U], x2[U];                            // the next piece, as it comes
     int at[GPD_HEAD_MAX_AXES];                     // its positions
     auto fetch = [&](int t) {
         const T* x = static_cast<const T*>(p.x) + t * p.ldx + h0 * a.D;
-        const T* dy = static_cast<const T*>(p.dy) + t * p.lddy + h0 * a.D;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const bool here = u.there && h0 + i * per < p.heads;
@@ -558,37 +567,24 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
                 x1[i] = load_vec<T, V>(x + d + u.c1);
                 x2[i] = load_vec<T, V>(x + d + u.c2);
             }
-            if (BACK) {
-                y1[i] = y2[i] = Vec<T, V>{};
-                if (here) {
-                    y1[i] = load_vec<T, V>(dy + d + u.c1);
-                    y2[i] = load_vec<T, V>(dy + d + u.c2);
-                }
-            }
         }
         positions(a, t, at);
     };
     int t = index / p.chunks;
     if (t < T_all) fetch(t);
     for (; t < T_all; t += step) {
-        F2 c[P], s[P], ns[P];
+        F2 c[P], s[P];
         if (turned) {
             float cs[V], sn[V];
             angles<V>(a, at, lane % G, cs, sn);
             two_by_two<V>(cs, c);
             two_by_two<V>(sn, s);
-#pragma unroll
-            for (int i = 0; i < P; ++i) ns[i] = s[i] ^ 0x8000000080000000ull;
         }
-        Vec<T, V> r1[U], r2[U], g1[BACK ? U : 1], g2[BACK ? U : 1];
+        Vec<T, V> r1[U], r2[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             r1[i] = x1[i];
             r2[i] = x2[i];
-            if (BACK) {
-                g1[i] = y1[i];
-                g2[i] = y2[i];
-            }
         }
         if (t < T_all - step) fetch(t + step);
         T* out = static_cast<T*>(p.out) + t * p.ldo + h0 * a.D;
@@ -598,107 +594,265 @@ __global__ void __launch_bounds__(32 * kWarps, BACK ? 3 : 4) heads_walk_kernel(c
             T* o = out + i * per * a.D;
             F2 xa[P], xb[P];
             pairs<T, V, NEAR>(r1[i], r2[i], xa, xb);
-            F2 squares = f2(0.f, 0.f);
+            if (p.w) {
+                F2 squares = f2(0.f, 0.f);
 #pragma unroll
-            for (int j = 0; j < P; ++j) squares = fma2(xa[j], xa[j], fma2(xb[j], xb[j], squares));
-            if constexpr (!BACK) {
-                if (p.w) {
-                    const float f = rsqrtf(lanes_sum(both(squares), G) * a.inv_d + a.eps);
-                    const F2 f_2 = f2(f, f);
-#pragma unroll
-                    for (int j = 0; j < P; ++j) {
-                        xa[j] = mul2(mul2(xa[j], f_2), wa[j]);
-                        xb[j] = mul2(mul2(xb[j], f_2), wb[j]);
-                    }
-                }
-                if (turned) turn<P>(xa, xb, c, s, ns);
-                if (here) store_pairs<T, V, NEAR>(o + u.c1, o + u.c2, xa, xb);
-            } else {
-                F2 ga[P], gb[P];
-                pairs<T, V, NEAR>(g1[i], g2[i], ga, gb);
-                if (turned && here) turn<P>(ga, gb, c, s, ns);         // heads and units that do not exist are zeros and stay so
-                F2 dot = f2(0.f, 0.f), ta[P], tb[P];
+                for (int j = 0; j < P; ++j) squares = fma2(xa[j], xa[j], fma2(xb[j], xb[j], squares));
+                const float f = rsqrtf(lanes_sum(both(squares), G) * a.inv_d + a.eps);
+                const F2 f_2 = f2(f, f);
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
-                    ta[j] = mul2(ga[j], xa[j]);
-                    tb[j] = mul2(gb[j], xb[j]);
-                    dot = fma2(ta[j], wa[j], fma2(tb[j], wb[j], dot));
+                    xa[j] = mul2(mul2(xa[j], f_2), wa[j]);
+                    xb[j] = mul2(mul2(xb[j], f_2), wb[j]);
                 }
-                const float sq = lanes_sum(both(squares), G), dt = lanes_sum(both(dot), G);
-                const float f = rsqrtf(sq * a.inv_d + a.eps), k = f * f * f * (dt * a.inv_d);
-                const F2 f_2 = f2(f, f), k_2 = f2(-k, -k);
-#pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    da[j] = fma2(ta[j], f_2, da[j]);
-                    db[j] = fma2(tb[j], f_2, db[j]);
-                    ga[j] = fma2(xa[j], k_2, mul2(mul2(ga[j], wa[j]), f_2));
-                    gb[j] = fma2(xb[j], k_2, mul2(mul2(gb[j], wb[j]), f_2));
-                }
-                if (here) store_pairs<T, V, NEAR>(o + u.c1, o + u.c2, ga, gb);
             }
-        }
-    }
-    if constexpr (BACK) {
-        // the warp's heads, then the CTA's warps, in a fixed order
-        float fa[V], fb[V];
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const float2 v = f2(da[j]), w = f2(db[j]);
-            fa[2 * j] = v.x;
-            fa[2 * j + 1] = v.y;
-            fb[2 * j] = w.x;
-            fb[2 * j + 1] = w.y;
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float x = 0.f, y = 0.f;
-            for (int i = 0; i < per; ++i) {
-                x += __shfl_sync(0xffffffffu, fa[j], (lane + i * G) & 31);
-                y += __shfl_sync(0xffffffffu, fb[j], (lane + i * G) & 31);
-            }
-            fa[j] = x;
-            fb[j] = y;
-        }
-        if (u.there && lane < G) {
-            float f[V], h[V];
-            from_pairs<V>(fa, fb, NEAR, f, h);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                shares[warp][u.c1 + j] = f[j];
-                shares[warp][u.c2 + j] = h[j];
-            }
-        }
-        __syncthreads();
-        for (int d = threadIdx.x; d < a.D; d += 32 * kWarps) {
-            float v = shares[0][d];
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) v += shares[w][d];
-            a.parts[(int64_t)blockIdx.x * a.D + d] = v;
+            if (turned) turn<P>(xa, xb, c, s);
+            if (here) store_pairs<T, V, NEAR>(o + u.c1, o + u.c2, xa, xb);
         }
     }
 }
 
+// ---- gradient with norm, rows and heads on 16-byte boundaries ------------------------------------------------------
+// Pieces, which are whole stretches of a row, come into a ring in shared memory by bulk copies of the warp's own, with the
+// table's row where one is enough, and leave from there: what two inputs and the sums of dw need in registers leaves no room
+// to load ahead (4096 x 40 heads of 128 BF16: 33 us, loading ahead into registers 38; the forward pass gains nothing, 120
+// and 118 us at 16384 x 72 heads).
+__device__ int g_heads_status = 0;                     // GPD_ERR_TIMEOUT if a bounded wait expired
+
+constexpr int kBackHeads = 2, kBackStages = 3, kBackPerSm = 3;         // heads of a lane in a piece; stages; CTAs per SM
+struct Stage {
+    static constexpr int X = kBackHeads * 1024, BYTES = 2 * X + kMaxHead * 4;          // inputs, gradients, angles
+};
+__device__ __forceinline__ void bulk_load(uint32_t to, const void* from, int bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(to), "l"(from), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* to, uint32_t from, int bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> read_vec(uint32_t at) {
+    Vec<T, V> v;
+    if constexpr (V * sizeof(T) == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.r.x), "=r"(v.r.y), "=r"(v.r.z), "=r"(v.r.w) : "r"(at) : "memory");
+    else asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.r.x), "=r"(v.r.y) : "r"(at) : "memory");
+    return v;
+}
+
+template <typename T, int V, bool NEAR>
+__global__ void __launch_bounds__(32 * kWarps, kBackPerSm) heads_back_kernel(const __grid_constant__ HeadArgs a) {
+    constexpr int P = V / 2, U = kBackHeads, STAGES = kBackStages;
+    using S = Stage;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ float shares[kWarps][kMaxHead];
+    __shared__ uint64_t full[kWarps][STAGES];
+    __shared__ int row_of[kWarps][STAGES], abort;      // the table's row; -1: none
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lane == 0) {
+        for (int i = 0; i < STAGES; ++i) tc::mbar_init(&full[warp][i], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 0) abort = 0;
+    __syncthreads();
+    after_previous();
+    const bool second = blockIdx.x >= a.split;
+    const Part& p = a.part[second];
+    const int G = a.lanes, per = 32 / G;
+    // a warp keeps to one chunk of heads and walks over the tokens: the part's warps are a multiple of its chunks
+    const int warps = (int)(second ? gridDim.x - a.split : a.split) * kWarps, index = (int)(blockIdx.x - (second ? a.split : 0)) * kWarps + warp;
+    const int step = warps / p.chunks, h0 = index % p.chunks * per * U, T_all = (int)a.T, first = index / p.chunks;
+    const int here = min(per * U, p.heads - h0), bytes = here * a.D * (int)sizeof(T);  // heads of the chunk
+    const Unit<V> u(lane % G, a);
+    const bool turned = u.there && u.turned, by_row = a.R > 0 && a.A == 1 && a.table_vec && a.R % 4 == 0;
+    F2 wa[P], wb[P], da[P], db[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) wa[i] = wb[i] = da[i] = db[i] = f2(0.f, 0.f);
+    if (u.there) {
+        float x[V], y[V];
+        weights<T, V>(a, p.w, u, x, y);
+        two_by_two<V>(x, wa);
+        two_by_two<V>(y, wb);
+    }
+    const uint32_t mine = tc::smem_u32(ring) + warp * (STAGES * S::BYTES);
+    const T *x_at = static_cast<const T*>(p.x) + (int64_t)first * p.ldx + h0 * a.D, *dy_at = static_cast<const T*>(p.dy) + (int64_t)first * p.lddy + h0 * a.D;
+    T* out_at = static_cast<T*>(p.out) + (int64_t)first * p.ldo + h0 * a.D;
+    const int64_t x_step = step * p.ldx, dy_step = step * p.lddy, out_step = step * p.ldo;
+    int at[GPD_HEAD_MAX_AXES] = {-1, -1, -1, -1};      // rows of the table for the token that is asked for next (one row), or worked on next
+    // asks for a token's piece; lane 0
+    auto fetch = [&](int stage) {
+        uint64_t* bar = &full[warp][stage];
+        const uint32_t to = mine + stage * S::BYTES;
+        const bool row = by_row && at[0] >= 0;
+        row_of[warp][stage] = at[0];
+        tc::mbar_expect_tx(bar, bytes * 2 + (row ? a.R * 4 : 0));
+        bulk_load(to, x_at, bytes, bar);
+        bulk_load(to + S::X, dy_at, bytes, bar);
+        if (row) bulk_load(to + S::BYTES - kMaxHead * 4, a.table + at[0] * a.ldt, a.R * 4, bar);
+        x_at += x_step;
+        dy_at += dy_step;
+    };
+    auto later = [&](int t, int n) { return t < T_all - n * (int64_t)step; };          // whether there is a token n on
+    int asked = 0;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (later(first, i)) {
+            if (by_row) positions(a, first + i * step, at);
+            if (lane == 0) fetch(i);
+            ++asked;
+        }
+    if (by_row && later(first, STAGES - 1)) positions(a, first + (STAGES - 1) * step, at);
+    if (!by_row && a.R > 0 && first < T_all) positions(a, first, at);
+    int k = 0, done = 0;
+    uint32_t phase = 0;
+    for (int t = first; t < T_all; t += step, ++done) {
+        float cs[V], sn[V];
+        if (!by_row && turned) angles<V>(a, at, lane % G, cs, sn);     // under way while the piece is awaited
+        const bool live = tc::mbar_wait(&full[warp][k], phase, &abort, &g_heads_status);
+        if (!__all_sync(0xffffffffu, live)) break;
+        const uint32_t piece = mine + k * S::BYTES + lane / G * a.D * (int)sizeof(T);
+        F2 c[P], s[P];
+        if (turned) {
+            if (by_row) {
+                const uint32_t row = mine + k * S::BYTES + S::BYTES - kMaxHead * 4 + V * (lane % G) * 4;
+                const bool there = row_of[warp][k] >= 0;
+#pragma unroll
+                for (int i = 0; i < V / 4; ++i) {
+                    const Vec<float, 4> x = read_vec<float, 4>(row + 16 * i), y = read_vec<float, 4>(row + a.R * 2 + 16 * i);
+                    c[2 * i] = f2(__uint_as_float(x.r.x), __uint_as_float(x.r.y));
+                    c[2 * i + 1] = f2(__uint_as_float(x.r.z), __uint_as_float(x.r.w));
+                    s[2 * i] = f2(__uint_as_float(y.r.x), __uint_as_float(y.r.y));
+                    s[2 * i + 1] = f2(__uint_as_float(y.r.z), __uint_as_float(y.r.w));
+                }
+                const float nan = __int_as_float(0x7fffffff);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    s[i] ^= 0x8000000080000000ull;     // back
+                    if (!there) c[i] = s[i] = f2(nan, nan);
+                }
+            } else {
+                two_by_two<V>(cs, c);
+                two_by_two<V>(sn, s);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (i * per >= here) break;                // the same for the warp
+            const bool mine_too = u.there && i * per + lane / G < here;
+            const uint32_t from = piece + i * per * a.D * (int)sizeof(T), at1 = from + u.c1 * (int)sizeof(T), at2 = from + u.c2 * (int)sizeof(T);
+            Vec<T, V> r1{}, r2{};
+            if (mine_too) {
+                r1 = read_vec<T, V>(at1);
+                r2 = read_vec<T, V>(at2);
+            }
+            F2 xa[P], xb[P];
+            pairs<T, V, NEAR>(r1, r2, xa, xb);
+            Vec<T, V> g1{}, g2{};
+            if (mine_too) {
+                g1 = read_vec<T, V>(at1 + S::X);
+                g2 = read_vec<T, V>(at2 + S::X);
+            }
+            F2 ga[P], gb[P];
+            pairs<T, V, NEAR>(g1, g2, ga, gb);
+            if (turned && mine_too) turn<P>(ga, gb, c, s);         // heads and units that do not exist are zeros and stay so
+            F2 squares = f2(0.f, 0.f), dot = f2(0.f, 0.f), ta[P], tb[P];
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                squares = fma2(xa[j], xa[j], fma2(xb[j], xb[j], squares));
+                ta[j] = mul2(ga[j], xa[j]);
+                tb[j] = mul2(gb[j], xb[j]);
+                dot = fma2(ta[j], wa[j], fma2(tb[j], wb[j], dot));
+            }
+            const float sq = lanes_sum(both(squares), G), dt = lanes_sum(both(dot), G);
+            const float f = rsqrtf(sq * a.inv_d + a.eps), q = f * f * f * (dt * a.inv_d);
+            const F2 f_2 = f2(f, f), q_2 = f2(-q, -q);
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                da[j] = fma2(ta[j], f_2, da[j]);
+                db[j] = fma2(tb[j], f_2, db[j]);
+                ga[j] = fma2(xa[j], q_2, mul2(mul2(ga[j], wa[j]), f_2));
+                gb[j] = fma2(xb[j], q_2, mul2(mul2(gb[j], wb[j]), f_2));
+            }
+            if (mine_too) write_pairs<T, V, NEAR>(at1, at2, ga, gb);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            bulk_store(out_at, mine + k * S::BYTES, bytes);
+            // the stage before this one has left: it takes the token that is asked for next
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            if (later(t, STAGES - 1)) fetch(k == 0 ? STAGES - 1 : k - 1);
+        }
+        asked += later(t, STAGES - 1);
+        if (by_row && later(t, STAGES)) positions(a, t + STAGES * step, at);
+        if (!by_row && a.R > 0 && later(t, 1)) positions(a, t + step, at);
+        out_at += out_step;
+        if (++k == STAGES) {
+            k = 0;
+            phase ^= 1;
+        }
+    }
+    if (lane == 0) {
+        int never = 0;                                 // given up: copies in flight land before the CTA ends
+        if (*static_cast<volatile int*>(&abort))
+            for (int i = done; i < asked; ++i) tc::mbar_wait(&full[warp][i % STAGES], i / STAGES & 1, &never, &g_heads_status);
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    // the warp's heads, then the CTA's warps, in a fixed order
+    float fa[V], fb[V];
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        const float2 v = f2(da[j]), w = f2(db[j]);
+        fa[2 * j] = v.x;
+        fa[2 * j + 1] = v.y;
+        fb[2 * j] = w.x;
+        fb[2 * j + 1] = w.y;
+    }
+    for (int o = G; o < 32; o <<= 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            fa[j] += __shfl_xor_sync(0xffffffffu, fa[j], o);
+            fb[j] += __shfl_xor_sync(0xffffffffu, fb[j], o);
+        }
+    }
+    if (u.there && lane < G) {
+        float f[V], h[V];
+        from_pairs<V>(fa, fb, NEAR, f, h);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            shares[warp][u.c1 + j] = f[j];
+            shares[warp][u.c2 + j] = h[j];
+        }
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < a.D; d += 32 * kWarps) {
+        float v = shares[0][d];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) v += shares[w][d];
+        a.parts[(int64_t)blockIdx.x * a.D + d] = v;
+    }
+}
+
 // ---- host side ---------------------------------------------------------------------------------------
-// Largest vector that the layout allows: whole units (turned and not), and every row on a boundary of it.
-int vector_width(const HeadArgs& a, int elem) {
+// Largest vector that the layout allows: whole units (turned and not), and every row on a boundary of it, or of 16 bytes where
+// bulk copies take whole heads; else 1.
+int vector_width(const HeadArgs& a, int elem, bool bulk) {
+    if (bulk && a.D * elem % 16 != 0) return 1;
     for (int V = 16 / elem; V >= 4; V /= 2) {
         bool ok = a.D % (2 * V) == 0 && a.R % (2 * V) == 0;
+        const int bytes = bulk ? 16 : V * elem;
         for (const Part& p : a.part)
             if (p.heads > 0)
-                ok = ok && rows_aligned(p.x, p.ldx, elem, V * elem) && rows_aligned(p.dy, p.lddy, elem, V * elem) &&
-                     rows_aligned(p.out, p.ldo, elem, V * elem);
+                ok = ok && rows_aligned(p.x, p.ldx, elem, bytes) && rows_aligned(p.dy, p.lddy, elem, bytes) && rows_aligned(p.out, p.ldo, elem, bytes);
         if (ok) return V;
     }
     return 1;
 }
-// Lanes of a head: the next power of two, whose sums take fewer steps, unless more heads find room without (80 columns: six
-// instead of four).
 int pow2_lanes(int units) {
     int g = 1;
     while (g < units && g < 32) g *= 2;
     return g;
 }
-int head_lanes(int units) { return units < 32 && 32 / units > 32 / pow2_lanes(units) ? units : pow2_lanes(units); }
 
 // Gives each part its chunks and CTAs: as many as there is work, about `most` at most in all, shared out by the amount of it;
 // fixed: so many that their warps are a multiple of the chunks.
@@ -720,22 +874,29 @@ int share_out(HeadArgs& a, int U, int64_t most, bool fixed) {
     return (int)(n[0] + n[1]);
 }
 template <typename T, int V, int U>
-gpd_status launch_walk(HeadArgs a, bool back, cudaStream_t st) {
-    const int ctas = share_out(a, U, (back ? 3 : 4) * sm_count(), true);
-    auto kernel = back ? (a.neighbours ? heads_walk_kernel<T, V, 2, true, true> : heads_walk_kernel<T, V, 2, false, true>)
-                       : (a.neighbours ? heads_walk_kernel<T, V, U, true, false> : heads_walk_kernel<T, V, U, false, false>);
+gpd_status launch_walk(HeadArgs a, cudaStream_t st) {
+    const int ctas = share_out(a, U, kWalkPerSm * sm_count(), true);
+    auto kernel = a.neighbours ? heads_walk_kernel<T, V, U, true> : heads_walk_kernel<T, V, U, false>;
     return launch_after(kernel, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, a);
 }
 template <typename T, int V>
+gpd_status launch_back(const HeadArgs& a, int ctas, cudaStream_t st) {
+    constexpr int smem = kWarps * kBackStages * Stage::BYTES;
+    static_assert(kBackPerSm * (smem + kWarps * kMaxHead * 4 + 2048) <= 227 * 1024, "the CTAs of an SM find room");
+    auto kernel = a.neighbours ? heads_back_kernel<T, V, true> : heads_back_kernel<T, V, false>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
+    return launch_after(kernel, dim3((unsigned)ctas), dim3(32 * kWarps), smem, 1, st, a);
+}
+template <typename T, int V>
 gpd_status launch_forward(HeadArgs a, cudaStream_t st) {
-    a.lanes = head_lanes(a.D / (2 * V));
+    a.lanes = pow2_lanes(a.D / (2 * V));
     // Few tokens: one head per lane and piece, so that the heads are spread over the SMs.
     const int64_t steps = a.T * ((a.part[0].heads + a.part[1].heads) / (32 / a.lanes) + 1);
-    return steps < 8 * (int64_t)sm_count() * kWarps ? launch_walk<T, V, 1>(a, false, st) : launch_walk<T, V, 4>(a, false, st);
+    return steps < 8 * (int64_t)sm_count() * kWarps ? launch_walk<T, V, 1>(a, st) : launch_walk<T, V, 4>(a, st);
 }
 template <typename T>
 gpd_status launch_heads(HeadArgs a, cudaStream_t st) {
-    switch (vector_width(a, sizeof(T))) {
+    switch (vector_width(a, sizeof(T), false)) {
         case sizeof(T) == 2 ? 8 : -1: return launch_forward<T, 16 / sizeof(T)>(a, st);
         case 4: return launch_forward<T, 4>(a, st);
     }
@@ -746,18 +907,17 @@ gpd_status launch_heads(HeadArgs a, cudaStream_t st) {
 
 template <typename T>
 gpd_status launch_heads_backward(HeadArgs a, float* dqw, float* dkw, cudaStream_t st) {
-    const int V = vector_width(a, sizeof(T));
-    a.lanes = V == 1 ? pow2_lanes(a.D / 2) : head_lanes(a.D / (2 * V));
-    HeadArgs shared = a;                               // the CTAs of either part, for the sum over them
-    const int ctas = share_out(shared, V == 1 ? 1 : 2, 3 * sm_count(), V > 1);
+    const int V = vector_width(a, sizeof(T), true);
+    a.lanes = pow2_lanes(a.D / (2 * V));
+    const int ctas = share_out(a, V == 1 ? 1 : kBackHeads, kBackPerSm * sm_count(), V > 1);
     if (ctas > 0) {
         gpd_status rc;
-        if (V == 1) rc = launch_after(heads_backward_kernel<T, kMaxHead / 64>, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, shared);
-        else rc = V == 4 ? launch_walk<T, 4, 2>(a, true, st) : launch_walk<T, 16 / sizeof(T), 2>(a, true, st);
+        if (V == 1) rc = launch_after(heads_backward_kernel<T, kMaxHead / 64>, dim3((unsigned)ctas), dim3(32 * kWarps), 0, 1, st, a);
+        else rc = V == 4 ? launch_back<T, 4>(a, ctas, st) : launch_back<T, 16 / sizeof(T)>(a, ctas, st);
         if (rc != GPD_OK) return rc;
     }
     const float* parts = a.parts;
-    const int split = (int)shared.split;
+    const int split = (int)a.split;
     return launch_after(heads_dweight_kernel, dim3((unsigned)((a.D + 31) / 32), 2), dim3(32, 32), 0, 1, st, parts, split, ctas, a.D, dqw, dkw);
 }
 
@@ -783,6 +943,13 @@ gpd_status check_heads(int type, int weight_type, const HeadArgs& a, int index_b
 }
 
 }  // namespace
+
+int heads_status_fetch_and_clear() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_heads_status, sizeof(int)) != cudaSuccess) return (int)GPD_ERR_CUDA;
+    if (v != 0) cudaMemcpyToSymbol(g_heads_status, &zero, sizeof(int));
+    return v;
+}
 
 }  // namespace gpd
 
