@@ -225,6 +225,9 @@ __global__ void __launch_bounds__(kThreads + 32, per_sm(TmaShape<NT, TRANS>::SME
                     mma(acc[2 * p + 1], xa, b[2], b[3], T());
                 }
             }
+            // every load of the stage has its data before copies may write there: an arrival alone does not hold matrix loads
+            // back that nothing has waited for yet
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&ring.empty[k % S::STAGES]);
 #pragma unroll

@@ -326,6 +326,18 @@ def test_other_stream_and_graph():
     assert all(torch.equal(a, b) for a, b in zip(results, want))
 
 
+@pytest.mark.parametrize("type", [BF16, F16])
+@pytest.mark.parametrize("r", [32, 64, 128])
+def test_long_sums_while_their_stages_are_filled_again(r, type):
+    """16384 rows of 8192 columns, so that the copies run ahead of the products all the time: every row is right, in every run."""
+    c = Case([700] * 23 + [284], [i % 4 for i in range(24)], 4, r, 8192, 256, type, seed=r)
+    out, h = c.forward()
+    c.check_forward(out, h)
+    for _ in range(12):
+        again = c.forward(out=c.mat(c.T, c.N, c.out_type, 77.0))
+        assert torch.equal(again[1], h) and torch.equal(again[0], out)
+
+
 def test_refusals():
     c = Case(lens=[10, 6], index=[0, 1], n=2, r=8, K=64, N=48)
     h, out = torch.zeros((16, 8), device="cuda"), torch.zeros((16, 48), device="cuda", dtype=BF16)
