@@ -276,14 +276,21 @@ struct Range {
 bool overlapping(int32_t n, const int32_t* types, const void* const* in, const int32_t* out_types, void* const* out, const int64_t* counts) {
     std::vector<Range> r;
     r.reserve(2 * (size_t)n);
-    for (int32_t i = 0; i < n; ++i) {
-        if (counts[i] == 0) continue;
-        const auto o = reinterpret_cast<uintptr_t>(out[i]), x = reinterpret_cast<uintptr_t>(in[i]);
-        r.push_back({o, o + (uintptr_t)counts[i] * dtype_size(out_types[i]), true});
-        if (o != x) r.push_back({x, x + (uintptr_t)counts[i] * dtype_size(types[i]), false});
-    }
+    auto add = [&](const void* p, int64_t count, int type, bool written) {
+        const auto from = reinterpret_cast<uintptr_t>(p);
+        r.push_back({from, from + (uintptr_t)count * dtype_size(type), written});
+    };
+    for (int32_t i = 0; i < n; ++i)
+        if (counts[i] > 0) add(out[i], counts[i], out_types[i], true);
+    const auto outs = (std::ptrdiff_t)r.size();
+    for (int32_t i = 0; i < n; ++i)
+        if (counts[i] > 0 && out[i] != in[i]) add(in[i], counts[i], types[i], false);
+    // most often each half is in order: then one merging pass
     auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
-    if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
+    const auto middle = r.begin() + outs;
+    if (!std::is_sorted(r.begin(), middle, before)) std::sort(r.begin(), middle, before);
+    if (!std::is_sorted(middle, r.end(), before)) std::sort(middle, r.end(), before);
+    std::inplace_merge(r.begin(), middle, r.end(), before);
     uintptr_t end = 0, written_end = 0;
     for (const Range& x : r) {
         if (x.from < written_end || (x.written && x.from < end)) return true;
