@@ -338,6 +338,22 @@ def test_long_sums_while_their_stages_are_filled_again(r, type):
         assert torch.equal(again[1], h) and torch.equal(again[0], out)
 
 
+def test_what_follows_a_batch_without_adapters_sees_its_zeros():
+    """In place and without adapters the second product has nothing to do; the next call still comes after the first one."""
+    T, r, K, N = 300000, 128, 8, 64
+    x, out = torch.ones(T, K, dtype=BF16, device="cuda"), torch.ones(T, N, dtype=BF16, device="cuda")
+    A, B = torch.ones(1, r, K, dtype=BF16, device="cuda"), torch.ones(1, N, r, dtype=BF16, device="cuda")
+    offsets, index = torch.tensor([0, T // 3, T], device="cuda"), torch.tensor([-1, -1], device="cuda")
+    h = torch.empty(T, r, device="cuda")
+    norm, ws = torch.empty(1, device="cuda"), torch.empty(g.GPD_GRAD_NORM_WORKSPACE, dtype=torch.uint8, device="cuda")
+    for _ in range(5):
+        h.fill_(55)
+        g.gpd_adapter(x, A, B, offsets, index, out, h, base=out)
+        g.gpd_grad_norm([h], norm, ws)
+        assert float(norm) == 0
+        assert not h.any() and bool((out == 1).all())
+
+
 def test_refusals():
     c = Case(lens=[10, 6], index=[0, 1], n=2, r=8, K=64, N=48)
     h, out = torch.zeros((16, 8), device="cuda"), torch.zeros((16, 48), device="cuda", dtype=BF16)
