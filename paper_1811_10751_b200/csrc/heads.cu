@@ -10,6 +10,10 @@
 // warp; the norm is a butterfly over the G lanes, no shared memory and no barrier.  A piece of work is one token, whose
 // angles are loaded once, and up to U * 32 / G of its heads; warps walk over the pieces, and load the next one before they
 // work on the present one.  Arithmetic is on pairs of numbers.
+//
+// Measured: 16384 tokens x 72 heads of 128 BF16 115 us of 95 at the copy bandwidth (issue 54 %, two thirds of it conversions, the norm's butterfly
+// and the turn); 8 tokens 3.4 us; the gradient of 4096 x 40 heads 33 us of 20 (issue 48 %), 4 of them the sum of the
+// weights' gradients.
 #include <algorithm>
 #include <numeric>
 
