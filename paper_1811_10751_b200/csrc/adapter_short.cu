@@ -35,8 +35,12 @@ struct Shape {
     static constexpr int RP = 8 * NT;
     using A = WTile<RP, kBlockCols>;
     using B = WTile<kBlockCols, RP>;
-    static constexpr int SUMS = (kWarps + kMostSplits + 1) * 16 * RP * 4;              // the warps' shares, the CTAs', h
-    static int bytes(int blocks_a, int blocks_b) { return blocks_a * A::BYTES + blocks_b * B::BYTES + SUMS + 1024; }
+    static constexpr int SUMS = 16 * RP;               // floats: a share of h
+    static_assert(A::BYTES >= SUMS * 4, "a warp's share fits in its first block of A");
+    // A (a block for every warp at least), B, the CTAs' shares and h
+    static int bytes(int blocks_a, int blocks_b, int splits) {
+        return std::max(blocks_a, kWarps) * A::BYTES + blocks_b * B::BYTES + (splits + 1) * SUMS * 4 + 1024;
+    }
 };
 
 template <typename T, typename O, int NT, int PARTS>
@@ -69,10 +73,11 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
     const int a0 = s.all_a * rank >> log_splits, na = (s.all_a * (rank + 1) >> log_splits) - a0;
     const int b0 = s.all_b * rank >> log_splits, nb = (s.all_b * (rank + 1) >> log_splits) - b0;
     unsigned char* as = smem;
-    unsigned char* bs = as + s.blocks_a * S::A::BYTES;
-    float* shares = reinterpret_cast<float*>(bs + s.blocks_b * S::B::BYTES);           // [4][16][RP]
-    float* given = shares + kWarps * 16 * S::RP;       // [splits][16][RP]
-    float* h = given + kMostSplits * 16 * S::RP;       // [16][RP]
+    unsigned char* bs = as + max(s.blocks_a, kWarps) * S::A::BYTES;
+    float* given = reinterpret_cast<float*>(bs + s.blocks_b * S::B::BYTES);            // [splits][16][RP]
+    float* h = given + splits * S::SUMS;               // [16][RP]
+    // A warp's share of h takes the place of its first block of A, which no other warp reads.
+    auto share_of = [&](int w) { return reinterpret_cast<float*>(as + w * S::A::BYTES); };
     if (!none && lane == 0) {
         tc::mbar_expect_tx(&ready_a[warp], (na - warp + kWarps - 1) / kWarps * S::A::BYTES);
         tc::mbar_expect_tx(&ready_b[warp], (nb - warp + kWarps - 1) / kWarps * S::B::BYTES);
@@ -148,9 +153,10 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[0][k][j] = x[1][k][j];
         }
+        __syncwarp();                                  // its blocks have been read
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float* p = shares + (16 * warp + g) * S::RP + 8 * n + 2 * (lane & 3);
+            float* p = share_of(warp) + g * S::RP + 8 * n + 2 * (lane & 3);
             *reinterpret_cast<float2*>(p) = make_float2(sum[n][0], sum[n][1]);
             *reinterpret_cast<float2*>(p + 8 * S::RP) = make_float2(sum[n][2], sum[n][3]);
         }
@@ -159,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
         for (int e = threadIdx.x; e < tile.rows * S::RP; e += kThreads) {
             float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) v += shares[w * 16 * S::RP + e];
+            for (int w = 0; w < kWarps; ++w) v += share_of(w)[e];
             for (int c = 0; c < splits; ++c) *cluster.map_shared_rank(given + rank * 16 * S::RP + e, c) = v;
         }
         // no CTA writes to another after this barrier, so none has to wait for the others at its end
@@ -227,19 +233,24 @@ gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, 
     constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
     const int64_t tiles = tiles_of(down.seg, 16), all_a = (down.C + kBlockCols - 1) / kBlockCols, all_b = (above.C + kBlockCols - 1) / kBlockCols;
     // Eight CTAs per tile while all of them are resident at once, fewer for more tiles as long as their parts fit.
-    constexpr int kRoom = 220 * 1024;                  // of shared memory, and a third of it
+    constexpr int kRoom = 220 * 1024;                  // of shared memory, and a fifth of it
     auto bytes = [&](int n) {
         const int64_t a = (all_a + n - 1) / n, b = (all_b + n - 1) / n;
-        return a > 4096 || b > 4096 ? INT32_MAX : S::bytes((int)a, (int)b);
+        return a > 4096 || b > 4096 ? INT32_MAX : S::bytes((int)a, (int)b, n);
     };
     int splits = kMostSplits, log_splits = 0;
-    while (splits > 1 && tiles * splits > 4 * sm_count() && bytes(splits / 2) <= kRoom / 3) splits /= 2;
+    while (splits > 1 && tiles * splits > 4 * sm_count() && bytes(splits / 2) <= kRoom / 5) splits /= 2;
     while (splits > 1 && (all_a < splits || all_b < splits)) splits /= 2;
     while (1 << log_splits < splits) ++log_splits;
-    const int smem = bytes(splits);
-    *taken = smem <= kRoom;
+    // One CTA per SM waits for its loads alone: where that makes many waves, the pipelines of two launches are faster (256 segments
+    // of a row, 4096 x 4096, rank 64: 118 us, in waves 147).
+    int smem = bytes(splits);
+    *taken = smem <= kRoom / 2 || (smem <= kRoom && tiles * splits <= 4 * sm_count());
     if (!*taken) return GPD_OK;
     if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
+    // Where all CTAs are resident at once, no SM gets more of them than an even share (64 segments: 8.1 us, else 9.0).
+    const int64_t even = (tiles * splits + sm_count() - 1) / sm_count();
+    if (even < kRoom / smem) smem = (int)(kRoom / even);
     ShortArgs s{down, above, (int)((all_a + splits - 1) / splits), (int)((all_b + splits - 1) / splits), (int)all_a, (int)all_b};
     CUtensorMap map_a{}, map_b{};                      // without adapters they are not used
     if (down.seg.n > 0 && (!make_map(&map_a, down.w, 2, down.seg.n, down.r, down.C, down.ldw, down.next, S::RP, kBlockCols) ||
