@@ -25,7 +25,7 @@ constexpr int kThreads = 128, kCols = 64;              // columns of a warp and 
 
 template <int KT, int WM, bool TRANS>
 struct Shape {
-    static constexpr int TM = 16 * WM, RP = 16 * KT, COLS = WM == 4 ? kCols : 4 * kCols, STAGES = WM == 1 && KT == 8 ? 2 : 3;
+    static constexpr int TM = 16 * WM, RP = 16 * KT, COLS = WM == 4 ? kCols : 4 * kCols, STAGES = WM == 1 && KT >= 4 ? 2 : 3;
     static constexpr int W_ROWS = TRANS ? RP : COLS, W_COLS = TRANS ? COLS : RP, W_PITCH = 2 * W_COLS + 16;
     static constexpr int STAGE = W_ROWS * W_PITCH, SMEM = STAGES * STAGE;
 };

@@ -8,7 +8,7 @@
 //
 // Measured: 64 rows with an adapter each, 4096 x 4096, rank 16, BF16: 8.1 us, in two launches 21; reading the adapters takes 2.8.
 // The columns' loads, the meeting of the CTAs and the rows' loads are 2 to 3 us each.  Many more segments run in waves of clusters: 256
-// of them 29 us, reading takes 10.4.
+// of them 31 us, reading takes 10.4.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -242,10 +242,11 @@ gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, 
     while (splits > 1 && tiles * splits > 4 * sm_count() && bytes(splits / 2) <= kRoom / 5) splits /= 2;
     while (splits > 1 && (all_a < splits || all_b < splits)) splits /= 2;
     while (1 << log_splits < splits) ++log_splits;
-    // One CTA per SM waits for its loads alone: where that makes many waves, the pipelines of two launches are faster (256 segments
-    // of a row, 4096 x 4096, rank 64: 118 us, in waves 147).
+    // One CTA per SM waits for its loads alone: beyond two waves of such the pipelines of two launches are faster (4096 x 4096, rank
+    // 64, segments of a row, this and two launches: 24 of them 15 and 20 us, 32 24 and 25, 48 34 and 28, 256 147 and 81; two CTAs per SM, rank
+    // 32: 64 of them 20 and 28 us, 256 70 and 69).
     int smem = bytes(splits);
-    *taken = smem <= kRoom / 2 || (smem <= kRoom && tiles * splits <= 4 * sm_count());
+    *taken = smem <= kRoom / 2 || (smem <= kRoom && tiles * splits <= 2 * sm_count());
     if (!*taken) return GPD_OK;
     if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
     // Where all CTAs are resident at once, no SM gets more of them than an even share (64 segments: 8.1 us, else 9.0).

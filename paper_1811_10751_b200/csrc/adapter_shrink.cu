@@ -22,7 +22,7 @@ constexpr int kThreads = 128, kDeep = 64, kXPitch = 2 * kDeep + 16;    // column
 
 template <int NT, int WM, bool TRANS>
 struct Shape {
-    static constexpr int TM = 16 * WM, RP = 8 * NT, STAGES = WM == 1 ? 6 : 4;
+    static constexpr int TM = 16 * WM, RP = 8 * NT, STAGES = WM == 4 ? 4 : NT == 16 ? 3 : NT == 8 ? 4 : 6;     // room for three CTAs per SM or more
     static constexpr int W_ROWS = TRANS ? kDeep : RP, W_COLS = TRANS ? RP : kDeep, W_PITCH = 2 * W_COLS + 16;
     static constexpr int STAGE = TM * kXPitch + W_ROWS * W_PITCH;
     static constexpr int SUMS = 64 * RP * 4;           // FP32 sums: of 64 rows, or of 16 rows four times
