@@ -158,7 +158,7 @@ __device__ __forceinline__ void stage8(uint32_t to, const T* from, int n, bool v
     }
 }
 // ROWS x COLS elements (COLS a multiple of 8) from p, of which rows x cols exist; rows are `pitch` bytes apart in shared memory.
-// Off 16-byte boundaries all loads of four pieces come before their stores (2246 rows x 8535, rank 128: 297 -> 281 us).
+// Off 16-byte boundaries all loads of four pieces come before their stores (2246 rows x 8535, rank 128: 281 us, piece by piece 297).
 template <typename T, int ROWS, int COLS, int THREADS>
 __device__ __forceinline__ void stage_tile(uint32_t to, int pitch, const T* p, int64_t ld, int64_t rows, int64_t cols, bool vec) {
     constexpr int per = COLS / 8, N = 4;

@@ -134,8 +134,10 @@ template <typename T, int NT, int WM, bool TRANS>
 gpd_status launch(const ShrinkArgs& a, cudaStream_t st) {
     using S = Shape<NT, WM, TRANS>;
     const int64_t tiles = tiles_of(a.seg, S::TM), stages = (a.C + kDeep - 1) / kDeep;
-    int splits = 1;                                    // until two CTAs per SM are busy, but four stages each at least
-    while (splits < 8 && tiles * splits < 2 * sm_count() && stages >= 8 * splits) splits *= 2;
+    // until two CTAs per SM are busy, or four where loads are awaited in line, but four stages each at least
+    const int64_t busy = (a.x_vec && a.w_vec ? 2 : 4) * sm_count();
+    int splits = 1;
+    while (splits < 8 && tiles * splits < busy && stages >= 8 * splits) splits *= 2;
     if (tiles * splits > 0x7fffffff) return GPD_ERR_SHAPE;
     auto kernel = shrink_kernel<T, NT, WM, TRANS>;
     if (S::SMEM > 49152 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return GPD_ERR_CUDA;
