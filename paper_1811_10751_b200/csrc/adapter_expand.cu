@@ -127,7 +127,8 @@ gpd_status launch(const ExpandArgs& a, cudaStream_t st) {
 // ---- the same with tiles by TMA: many rows, base and out on 16-byte boundaries ---------------------------------
 // Tiles of base arrive in shared memory, a lane adds its products to its elements there, and a warp's 16 rows leave from
 // there: as one copy if all of them are the segment's, row by row where it ends among them.  A stage is handed back one step
-// late, when its copy has left and every load from it has long had its data.
+// late, when its copy has left and every load from it has long had its data: a warp ends every step with a group of copies,
+// an empty one where it has none, so that all but the newest group are those of the steps before.
 __device__ int g_expand_status = 0;                    // GPD_ERR_TIMEOUT if a bounded wait expired
 
 template <typename O, int KT, bool TRANS>
@@ -297,7 +298,6 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 #pragma unroll
                         for (int j = 0; j < S::BOXES; ++j)
                             if (c0 + j * S::BOX < a.C) tma_store_3d(&map_out, mine + j * S::TM * 128, (int)c0 + j * S::BOX, (int)tile.row + 16 * warp, 0);
-                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 } else {
 #pragma unroll
@@ -324,8 +324,11 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                         }
                 }
             }
-            // the stage before this one is free once its copy has left
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            // the stage before this one is free once its copy has left; this step's group, empty or not, may be under way
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            }
             __syncwarp();
             if (lane == 0 && k > 0) tc::mbar_arrive(&ring.empty[(k - 1) % S::STAGES]);
         }
