@@ -269,7 +269,8 @@ struct WTile {
 
 // ---- numbers of FP32 as sums of 16-bit ones ----------------------------------------------------------------
 // x = parts[0] + parts[1] (+ parts[2]) up to 2^-17 (two parts) or 2^-25 of it in BF16, two at a time.  An infinity or a NaN
-// is its first part, the others are then zero.  FP16: two parts, 2^-22 of numbers within its range.
+// is its first part, the others are then zero.  FP16: 2^-23 (two parts) or 2^-34 of it, or 2^-25 where that is more: its
+// smallest numbers are 2^-24 apart.
 template <typename T, int PARTS>
 __device__ __forceinline__ void split2(float x, float y, uint32_t (&parts)[PARTS]) {
 #pragma unroll
@@ -280,11 +281,14 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&parts)[PARTS
         y = fabsf(f.y) <= 3.4e38f ? y - f.y : 0.f;
     }
 }
-// e with m * 2^-e below 4 (FP16 parts of numbers of any size) and both 2^e and 2^-e normal; 0 for zeros, infinities and NaN.
+// e with m * 2^-e below 2^15 (FP16 parts of numbers of any size) and both 2^e and 2^-e normal; 0 for zeros, infinities and NaN.
+// So near the top of FP16's range that three parts hold all 24 bits of what is down to 2^-14 of m, and 2^-39 of m of the rest.
 __device__ __forceinline__ int exponent_of(float m) {
     const int e = (int)(__float_as_uint(m) >> 23 & 0xff);
-    return e == 0xff || m == 0.f ? 0 : min(max(e - 127, -126), 126);
+    return e == 0xff || m == 0.f ? 0 : max(e - 127 - 14, -126);
 }
+// Parts that an FP32 factor is cut into: two for 16-bit results, three for FP32 ones, which lose nothing of its 24 bits.
+template <typename T, typename O> constexpr int kParts = sizeof(O) == 4 ? 3 : 2;
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // |e| <= 126
 
 // ---- launches (host) -----------------------------------------------------------------------------------

@@ -1,8 +1,8 @@
 // Second factor of low-rank adapters: out[t] = base[t] + scale_i W_i h[t] for the rows of every segment, i its adapter.
 //
 // Bound by reading base and writing out (many rows) or by reading the adapters (one row per segment).  h is FP32 and goes
-// through the tensor cores as a sum of two or three 16-bit numbers, its parts: two lose 2^-17 (BF16) or 2^-22 (FP16) of
-// it, far below the rounding of a 16-bit result; FP32 results of BF16 adapters take three.  FP16 parts are taken of a row
+// through the tensor cores as a sum of two or three 16-bit numbers, its parts: two lose 2^-17 (BF16) or 2^-23 (FP16) of
+// it, far below the rounding of a 16-bit result; FP32 results take three.  FP16 parts are taken of a row
 // over a power of two, so that h may be of any size.  A warp has its 16 rows of h as operands in registers, and W comes in chunks
 // of columns through a ring of asynchronous copies; base is read a chunk ahead.  The tensor cores leave a lane two
 // neighbouring columns of a tile of eight: the four lanes of a row exchange words, so that each reads and writes eight
@@ -362,7 +362,7 @@ gpd_status launch_tma(const ExpandArgs& a, cudaStream_t st) {
 }
 template <typename T, typename O, int KT, bool TRANS>
 gpd_status launch_rows(const ExpandArgs& a, cudaStream_t st) {
-    constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
+    constexpr int PARTS = kParts<T, O>;
     if (a.seg.T <= 16 * (int64_t)a.seg.S) return launch<T, O, KT, PARTS, 1, TRANS>(a, st);
     return a.tma ? launch_tma<T, O, KT, PARTS, TRANS>(a, st) : launch<T, O, KT, PARTS, 4, TRANS>(a, st);
 }

@@ -2,8 +2,8 @@
 //
 // Bound by reading y, 128 columns of which a CTA takes over a part of the adapter's rows (its segments' rows one after the
 // other); the r columns of h are few.  The parts' sums meet in a fixed order.  h is
-// FP32 and goes through the tensor cores as a sum of 16-bit parts, two for 16-bit gradients and FP16, three for FP32
-// gradients of BF16.  The chain of the tensor cores' additions is cut every 64 rows.
+// FP32 and goes through the tensor cores as a sum of 16-bit parts, two for 16-bit gradients, three for FP32
+// ones.  The chain of the tensor cores' additions is cut every 64 rows.
 // Two forms.  Rows on 16-byte boundaries and segments that are not short: a first kernel cuts h into its parts, once for all
 // columns of y, and tiles of both come by TMA, 64 rows of one segment each; the CTAs of a cluster share an adapter's rows and
 // add up over distributed shared memory; FP16 parts are taken of an adapter's column over a power of two.  Otherwise
@@ -610,7 +610,7 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
     if (warp >= 2) {
         const int32_t* most = job.most + ((int64_t)second * job.seg.n + id) * RP;
 #pragma unroll
-        for (int c = 0; c < RP; ++c) tile[c * kTileWidth + (warp & 3) * 32 + lane] = sum[c] * (kScaled ? scale * power2(exponent_of(__int_as_float(most[c]))) : scale);
+        for (int c = 0; c < RP; ++c) tile[c * kTileWidth + (warp & 3) * 32 + lane] = (kScaled ? sum[c] * power2(exponent_of(__int_as_float(most[c]))) : sum[c]) * scale;
     }
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     if (splits > 1) cluster.sync();
@@ -658,7 +658,7 @@ int padded_rank(int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : r <= 64 ? 64 :
 
 template <typename T, typename O, int MT>
 gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t* slots, int32_t* most, bool tma, cudaStream_t st) {
-    constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
+    constexpr int PARTS = kParts<T, O>;
     constexpr int TILE = 16 * MT * kTileWidth * 4;     // a tile's sums on their way out
     gpd_status rc;
     if (tma) {

@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
 template <typename T, typename O, int NT>
 gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st) {
     using S = Shape<NT>;
-    constexpr int PARTS = sizeof(O) == 4 && std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
+    constexpr int PARTS = kParts<T, O>;
     const int64_t tiles = tiles_of(down.seg, 16), all_a = (down.C + kBlockCols - 1) / kBlockCols, all_b = (above.C + kBlockCols - 1) / kBlockCols;
     // Eight CTAs per tile while all of them are resident at once, fewer for more tiles as long as their parts fit.
     constexpr int kRoom = 220 * 1024;                  // of shared memory, and a fifth of it
