@@ -5,6 +5,8 @@
 // chain is cut every few steps and added to nearest, because the chain itself truncates.
 #pragma once
 
+#include <type_traits>
+
 #include "lm_common.h"
 #include "tc_common.h"
 
@@ -268,7 +270,7 @@ struct WTile {
 };
 
 // ---- numbers of FP32 as sums of 16-bit ones ----------------------------------------------------------------
-// x = parts[0] + parts[1] (+ parts[2]) up to 2^-17 (two parts) or 2^-25 of it in BF16, two at a time.  An infinity or a NaN
+// x = parts[0] + parts[1] + parts[2] up to 2^-25 of it in BF16, two at a time.  An infinity or a NaN
 // is its first part, the others are then zero.  FP16: 2^-23 (two parts) or 2^-34 of it, or 2^-25 where that is more: its
 // smallest numbers are 2^-24 apart.
 template <typename T, int PARTS>
@@ -287,8 +289,9 @@ __device__ __forceinline__ int exponent_of(float m) {
     const int e = (int)(__float_as_uint(m) >> 23 & 0xff);
     return e == 0xff || m == 0.f ? 0 : max(e - 127 - 14, -126);
 }
-// Parts that an FP32 factor is cut into: two for 16-bit results, three for FP32 ones, which lose nothing of its 24 bits.
-template <typename T, typename O> constexpr int kParts = sizeof(O) == 4 ? 3 : 2;
+// Parts that an FP32 factor is cut into.  Three lose nothing of its 24 bits.  Two of FP16, 22 bits, are enough for results of FP16;
+// two of BF16 would be 16 bits, which 16-bit results hide only until terms cancel (and flip one rounding in 400 where they do not).
+template <typename T, typename O> constexpr int kParts = sizeof(O) == 4 || std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // |e| <= 126
 
 // ---- launches (host) -----------------------------------------------------------------------------------

@@ -1,12 +1,11 @@
 // Second factor of low-rank adapters: out[t] = base[t] + scale_i W_i h[t] for the rows of every segment, i its adapter.
 //
 // Bound by reading base and writing out (many rows) or by reading the adapters (one row per segment).  h is FP32 and goes
-// through the tensor cores as a sum of two or three 16-bit numbers, its parts: two lose 2^-17 (BF16) or 2^-23 (FP16) of
-// it, far below the rounding of a 16-bit result; FP32 results take three.  FP16 parts are taken of a row
-// over a power of two, so that h may be of any size.  A warp has its 16 rows of h as operands in registers, and W comes in chunks
-// of columns through a ring of asynchronous copies; base is read a chunk ahead.  The tensor cores leave a lane two
-// neighbouring columns of a tile of eight: the four lanes of a row exchange words, so that each reads and writes eight
-// columns, 16 bytes, of it.
+// through the tensor cores as a sum of 16-bit numbers, its parts: three, which hold all of it, or two of FP16 for FP16 results,
+// which lose 2^-23.  FP16 parts are taken of a row over a power of two, so that h may be of any size.  A warp has its 16 rows of
+// h as operands in registers, and W comes in chunks of columns through a ring of asynchronous copies; base is read a chunk
+// ahead.  The tensor cores leave a lane two neighbouring columns of a tile of eight: the four lanes of a row exchange words, so
+// that each reads and writes eight columns, 16 bytes, of it.
 //
 // Measured (BF16, many rows, base read and out written; the first product is not in these times): 16384 x 8192, rank 32, 103 us
 // of 83 at the copy bandwidth (tensor pipe 37 %, DRAM 61 %); 4001 x 6144, rank 64, 33 us (tensor pipe 44 %): the products of

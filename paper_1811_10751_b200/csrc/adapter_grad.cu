@@ -2,8 +2,7 @@
 //
 // Bound by reading y, 128 columns of which a CTA takes over a part of the adapter's rows (its segments' rows one after the
 // other); the r columns of h are few.  The parts' sums meet in a fixed order.  h is
-// FP32 and goes through the tensor cores as a sum of 16-bit parts, two for 16-bit gradients, three for FP32
-// ones.  The chain of the tensor cores' additions is cut every 64 rows.
+// FP32 and goes through the tensor cores as a sum of 16-bit parts, three, or two for FP16 gradients of FP16.  The chain of the tensor cores' additions is cut every 64 rows.
 // Two forms.  Rows on 16-byte boundaries and segments that are not short: a first kernel cuts h into its parts, once for all
 // columns of y, and tiles of both come by TMA, 64 rows of one segment each; the CTAs of a cluster share an adapter's rows and
 // add up over distributed shared memory; FP16 parts are taken of an adapter's column over a power of two.  Otherwise

@@ -9,8 +9,17 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("needs a CUDA device", allow_module_level=True)
 
-from lm_reference import check_close                           # noqa: E402
+from lm_reference import HALF_ULP, TINY                        # noqa: E402
 from test_gpu_lm_adapters import BF16, F16, F32, STEP, Case    # noqa: E402
+
+
+
+def check(got, ref, lost):
+    """`lost`: before the result's one rounding."""
+    bound = lost + ref.abs() * HALF_ULP[got.dtype] * (1 + 1e-6) + TINY[got.dtype]
+    d = (got.double() - ref).abs()
+    assert bool((d <= bound).all()), float((d / bound).max())
+
 
 # aligned rows and long segments, rows off 16-byte boundaries, single rows
 FORMS = {"long": dict(lens=[130, 70]), "off boundaries": dict(lens=[130, 70], pad=1, offset=1), "single": dict(lens=[1, 1, 2, 1] * 5)}
@@ -37,7 +46,7 @@ def test_small_numbers_of_a_row_beside_a_large_one(form, type):
         s, B, hd = float(c.scale[i]), c.B[i].double(), h[a:b].double()
         top = hd.abs().amax(1, keepdim=True)
         size = s * (hd.abs() @ B.abs().t())
-        check_close(out[a:b], s * (hd @ B.t()), 1.0, (3 * STEP + 2.0 ** -23) * size + FAR * s * top * B.abs().sum(1))
+        check(out[a:b], s * (hd @ B.t()), (3 * STEP + 2.0 ** -23) * size + FAR * s * top * B.abs().sum(1))
 
 
 @pytest.mark.parametrize("form", FORMS)
@@ -54,7 +63,7 @@ def test_small_gradients_of_a_row_beside_a_large_one(form, type):
     for a, b, i in c.segments:
         s, A, B, d = float(c.scale[i]), c.A[i].double(), c.B[i].double(), c.dout[a:b].double()
         u, us = s * (d @ B), s * (d.abs() @ B.abs())
-        check_close(c.dx[a:b], u @ A, 1.0, (lost_u + 3 * STEP + 2.0 ** -23) * (us @ A.abs()) + FAR * us.amax(1, keepdim=True) * A.abs().sum(0))
+        check(c.dx[a:b], u @ A, (lost_u + 3 * STEP + 2.0 ** -23) * (us @ A.abs()) + FAR * us.amax(1, keepdim=True) * A.abs().sum(0))
 
 
 @pytest.mark.parametrize("form", FORMS)
@@ -75,7 +84,7 @@ def test_small_numbers_of_a_column_beside_a_large_one(form, type):
         top[i] += s * d.abs().sum(0)[:, None]
     for i in range(2):
         top[i] *= torch.cat([h[a:b] for a, b, j in c.segments if j == i]).abs().amax(0).double()
-    check_close(c.dB, dB, 1.0, (12 * STEP + (c.T / 64 + 8) * 2.0 ** -24) * size + FAR * top)
+    check(c.dB, dB, (12 * STEP + (c.T / 64 + 8) * 2.0 ** -24) * size + FAR * top)
 
     c = case(form, type)
     _, h = c.forward()
@@ -92,4 +101,56 @@ def test_small_numbers_of_a_column_beside_a_large_one(form, type):
         size[i] += us.t() @ x.abs()
         top[i] += x.abs().sum(0)
         most[i] = torch.maximum(most[i], us.amax(0)[:, None])
-    check_close(c.dA, dA, 1.0, (lost_u + 12 * STEP + (c.T / 64 + 8) * 2.0 ** -24) * size + FAR * top * most)
+    check(c.dA, dA, (lost_u + 12 * STEP + (c.T / 64 + 8) * 2.0 ** -24) * size + FAR * top * most)
+
+
+# 16-bit results: of a term, what the parts of its FP32 factor lose (nothing of three BF16 parts, 2^-23 of two FP16 ones) and the steps
+# of the tensor cores that have more than zeros to add, one for each part
+CANCEL = {BF16: 2.0 ** -24 + 3 * STEP, F16: 2.0 ** -22 + 2 * STEP}
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("type", [BF16, F16])
+def test_sixteen_bit_results_of_terms_that_cancel(form, type):
+    """Two numbers of h (and of u) that are nearly alike, one of them subtracted: the difference is rounded once."""
+    c = case(form, type, out=type, r=2)
+    c.A[:, 1] = c.A[:, 0]
+    c.A[:, 1, 7] *= 1.03125
+    c.B[:, :, 1] = -c.B[:, :, 0]
+    out, h = c.forward(base=None)
+    assert float((h[:, 0] - h[:, 1]).abs().median()) < float(h.abs().median()) / 256
+    for a, b, i in c.segments:
+        s, B, hd = float(c.scale[i]), c.B[i].double(), h[a:b].double()
+        check(out[a:b], s * (hd @ B.t()), (CANCEL[type] + 2.0 ** -23) * s * (hd.abs() @ B.abs().t()))
+
+    c = case(form, type, out=type, r=2)
+    c.B[:, :, 1] = c.B[:, :, 0]
+    c.B[:, 7, 1] *= 1.03125
+    c.A[:, 1] = -c.A[:, 0]
+    c.backward(h, dbase=None)
+    lost_u = 4 * STEP + (c.N / 64 + 16) * 2.0 ** -24
+    for a, b, i in c.segments:
+        s, A, B, d = float(c.scale[i]), c.A[i].double(), c.B[i].double(), c.dout[a:b].double()
+        u, us = s * (d @ B), s * (d.abs() @ B.abs())
+        check(c.dx[a:b], u @ A, lost_u * (us @ A.abs()) + (CANCEL[type] + 2.0 ** -23) * (u.abs() @ A.abs()))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("type", [BF16, F16])
+def test_sixteen_bit_gradients_of_rows_that_cancel(form, type):
+    """Two rows with nearly the same h and the opposite gradients, all others without: dB is rounded once."""
+    c = case(form, type)
+    c.grad = type
+    _, h = c.forward()
+    pairs = []
+    for i in range(2):
+        rows = [t for a, b, j in c.segments if j == i for t in range(a, b)]
+        c.dout[rows[2:]] = 0
+        c.dout[rows[1]] = -c.dout[rows[0]]
+        h[rows[1]] = h[rows[0]] * (1 - 2.0 ** -11)
+        pairs.append(rows[:2])
+    c.backward(h)
+    for i, (t, u) in enumerate(pairs):
+        d, s = c.dout[t].double()[:, None], float(c.scale[i])
+        size = s * d.abs() * (h[t].abs() + h[u].abs()).double()
+        check(c.dB[i], s * d * (h[t].double() - h[u].double()), (CANCEL[type] + 2 * 2.0 ** -24) * size)
