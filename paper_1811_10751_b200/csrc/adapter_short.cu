@@ -258,7 +258,8 @@ gpd_status launch(const ShrinkArgs& down, const ExpandArgs& above, bool* taken, 
                            !make_map(&map_b, above.w, 2, down.seg.n, above.C, above.r, above.ldw, above.next, kBlockCols, S::B::PITCH / 2)))
         return GPD_ERR_CUDA;
     auto kernel = short_kernel<T, O, NT, PARTS>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return GPD_ERR_CUDA;
+    // the limit is the kernel's, not the call's: always the largest, so that calls of other host threads do not meet a lower one
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom) != cudaSuccess) return GPD_ERR_CUDA;
     return launch_after(kernel, dim3((unsigned)(tiles * splits)), dim3(kThreads), smem, splits, st, map_a, map_b, s, log_splits);
 }
 template <typename T, typename O>
