@@ -775,7 +775,8 @@ __global__ void __launch_bounds__(32 * kWarps, kBackPerSm) heads_back_kernel(con
                 dot = fma2(ta[j], wa[j], fma2(tb[j], wb[j], dot));
             }
             const float sq = lanes_sum(both(squares), G), dt = lanes_sum(both(dot), G);
-            const float f = rsqrtf(sq * a.inv_d + a.eps), q = f * f * f * (dt * a.inv_d);
+            // each product is about one of the terms below, so that none leaves FP32 where they do not (f^3 would for x of 1e13)
+            const float f = rsqrtf(sq * a.inv_d + a.eps), q = f * (dt * a.inv_d) * f * f;
             const F2 f_2 = f2(f, f), q_2 = f2(-q, -q);
 #pragma unroll
             for (int j = 0; j < P; ++j) {
