@@ -776,7 +776,8 @@ __global__ void __launch_bounds__(32 * kWarps, kBackPerSm) heads_back_kernel(con
             }
             const float sq = lanes_sum(both(squares), G), dt = lanes_sum(both(dot), G);
             // each product is about one of the terms below, so that none leaves FP32 where they do not (f^3 would for x of 1e13)
-            const float f = rsqrtf(sq * a.inv_d + a.eps), q = f * (dt * a.inv_d) * f * f;
+            // Heads that do not exist are zeros, whose root is an infinity without eps: they get 0.
+            const float f = mine_too ? rsqrtf(sq * a.inv_d + a.eps) : 0.f, q = f * (dt * a.inv_d) * f * f;
             const F2 f_2 = f2(f, f), q_2 = f2(-q, -q);
 #pragma unroll
             for (int j = 0; j < P; ++j) {

@@ -17,7 +17,8 @@ from test_gpu_lm_heads import BF16, F32, STEPS, Case, turn     # noqa: E402
 
 @pytest.mark.parametrize("type", [BF16, F32])
 @pytest.mark.parametrize("pad", [0, 1])                        # whole vectors, element by element
-@pytest.mark.parametrize("size,eps", [(1e15, 1e-6), (1e13, 1e-36), (1e-14, 1e-36), (1e-17, 1e-36)])
+@pytest.mark.parametrize("size,eps", [(1e15, 1e-6), (1e13, 1e-36), (1e-14, 1e-36), (1e-17, 1e-36), (1e13, 0.0), (1e-14, 0.0),
+                                      (1e-17, 0.0), (1.0, 0.0)])
 def test_heads_of_any_size(type, pad, size, eps):
     """dx is of the size of dy / x, whatever x is: neither term of it may be lost on the way."""
     c = Case(T=50, Hq=5, Hk=2, D=128, R=64, type=type, pad=pad)
