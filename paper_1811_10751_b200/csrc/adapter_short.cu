@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__
         cluster.sync();
         for (int e = threadIdx.x; e < 16 * S::RP; e += kThreads) {
             float v = 0.f;
-            if (e < tile.rows * S::RP)
+            if (e < tile.rows * S::RP && e % S::RP < down.r)           // behind the rank: zeros, where x has infinities too
                 for (int c = 0; c < splits; ++c) v += given[c * 16 * S::RP + e];
             h[e] = v;
         }
