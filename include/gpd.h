@@ -595,8 +595,8 @@ gpd_status gpd_grad_norm(int32_t n, const int32_t* types_host, const void* const
 /*
  * gpd_clip_grads - out = grad * min(1, max_norm / norm) for every one of n tensors, FP32 inside and rounded once.
  * norm_dev: one float, as gpd_grad_norm leaves it; max_norm > 0.  out[i] may be grads[i] (of the same type; if all are,
- * nothing is moved where the norm is within the bound); otherwise an output must not overlap any other tensor of the call
- * (GPD_ERR_ARG).  An infinite norm gives 0 (NaN where the gradient is infinite), a norm that is NaN gives NaN.
+ * nothing is moved where the norm is within the bound); otherwise an output must not overlap any other tensor of the call, the norm
+ * among them (GPD_ERR_ARG).  An infinite norm gives 0 (NaN where the gradient is infinite), a norm that is NaN gives NaN.
  */
 gpd_status gpd_clip_grads(int32_t n, const int32_t* types_host, const void* const* grads_host, const int32_t* out_types_host,
                           void* const* out_host, const int64_t* counts_host, const float* norm_dev, float max_norm, void* stream);

@@ -271,14 +271,15 @@ gpd_status launch_clip(int32_t n, const int32_t* types, const void* const* grads
     });
 }
 
-// Whether an output shares memory with another output or with another tensor's input.
+// Whether an output shares memory with another output, with another tensor's input or with the norm.
 struct Range {
     uintptr_t from, to;
     bool written;
 };
-bool overlapping(int32_t n, const int32_t* types, const void* const* in, const int32_t* out_types, void* const* out, const int64_t* counts) {
+bool overlapping(int32_t n, const int32_t* types, const void* const* in, const int32_t* out_types, void* const* out, const int64_t* counts,
+                 const float* norm) {
     std::vector<Range> r;
-    r.reserve(2 * (size_t)n);
+    r.reserve(2 * (size_t)n + 1);
     auto add = [&](const void* p, int64_t count, int type, bool written) {
         const auto from = reinterpret_cast<uintptr_t>(p);
         r.push_back({from, from + (uintptr_t)count * dtype_size(type), written});
@@ -288,6 +289,7 @@ bool overlapping(int32_t n, const int32_t* types, const void* const* in, const i
     const auto outs = (std::ptrdiff_t)r.size();
     for (int32_t i = 0; i < n; ++i)
         if (counts[i] > 0 && out[i] != in[i]) add(in[i], counts[i], types[i], false);
+    add(norm, 1, GPD_DT_F32, false);
     // most often each half is in order: then one merging pass
     auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
     const auto middle = r.begin() + outs;
@@ -338,7 +340,7 @@ extern "C" gpd_status gpd_clip_grads(int32_t n, const int32_t* types_host, const
         in_place = in_place && (same || counts_host[i] == 0);
     }
     try {
-        if (overlapping(n, types_host, grads_host, out_types_host, out_host, counts_host)) return GPD_ERR_ARG;
+        if (overlapping(n, types_host, grads_host, out_types_host, out_host, counts_host, norm_dev)) return GPD_ERR_ARG;
     } catch (const std::bad_alloc&) {
         return GPD_ERR_SHAPE;
     }
