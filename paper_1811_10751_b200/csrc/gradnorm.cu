@@ -192,6 +192,25 @@ __device__ __forceinline__ void scale_to(const Tensor& t, int64_t chunk, float b
     else if (t.out_type == GPD_DT_BF16) scale_chunk<T, __nv_bfloat16>(t, chunk, by);
     else scale_chunk<T, __half>(t, chunk, by);
 }
+// A factor below 2^-100, of which FP32 may hold less than 24 bits, in two steps: 2^-64 first, which is exact wherever the result is not
+// zero (a gradient below 2^-62 would be scaled to less than 2^-162).  Element by element: it is rare, and within the registers
+// of the other form.
+constexpr float kFirst = 5.421010862427522e-20f, kFar = 7.9e-31f;      // 2^-64, 2^-100
+__device__ __forceinline__ void scale_far(const Tensor& t, int64_t chunk, float by) {
+    const int64_t from = chunk * kChunk - misaligned(t.in, t.in_type);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < kChunk; i += kThreads) {
+        const int64_t e = from + i;
+        if (e < 0 || e >= t.count) continue;
+        const float f = t.in_type == GPD_DT_F32    ? static_cast<const float*>(t.in)[e]
+                        : t.in_type == GPD_DT_BF16 ? to_f32(static_cast<const __nv_bfloat16*>(t.in)[e])
+                                                   : to_f32(static_cast<const __half*>(t.in)[e]);
+        const float v = f * kFirst * by;
+        if (t.out_type == GPD_DT_F32) static_cast<float*>(t.out)[e] = v;
+        else if (t.out_type == GPD_DT_BF16) static_cast<__nv_bfloat16*>(t.out)[e] = from_f32<__nv_bfloat16>(v);
+        else static_cast<__half*>(t.out)[e] = from_f32<__half>(v);
+    }
+}
 // in_place: every tensor's output is itself; nothing to do where the norm is within the bound
 template <int N>
 __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ Tensors<N> a, const float* norm, float max_norm, bool in_place) {
@@ -199,6 +218,11 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
     const float n = *norm;
     if (in_place && n <= max_norm) return;
     const float by = n <= max_norm ? 1.f : max_norm / n;               // NaN: NaN
+    if (by < kFar && n <= 3.4e38f) {
+        const float rest = max_norm / (n * kFirst);
+        for_chunks<N, true>(a, [&](const Tensor& t, int64_t chunk) { scale_far(t, chunk, rest); });
+        return;
+    }
     for_chunks<N, true>(a, [&](const Tensor& t, int64_t chunk) {
         if (t.in_type == GPD_DT_F32) scale_to<float>(t, chunk, by);
         else if (t.in_type == GPD_DT_BF16) scale_to<__nv_bfloat16>(t, chunk, by);
