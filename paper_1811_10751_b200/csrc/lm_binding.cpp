@@ -576,6 +576,14 @@ private:
     }
 };
 
+// Whether two dense tensors of one shape have their elements in the same order; dimensions of one element have no order.
+bool same_order(const at::Tensor& a, const at::Tensor& b) {
+    if (a.numel() == 0) return true;
+    for (int64_t i = 0; i < a.dim(); ++i)
+        if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+    return true;
+}
+
 gpd_status grad_norm(PyObject* const* args, Py_ssize_t n) {
     // grads, norm, workspace, stream
     Call c(args, n, 4);
@@ -602,7 +610,7 @@ gpd_status clip_grads(PyObject* const* args, Py_ssize_t n) {
     for (int32_t i = 0; i < g.n; ++i) {
         const at::Tensor &a = g.tensor(i), &b = o.tensor(i);
         if (a.sizes() != b.sizes()) refuse("out", "item " + std::to_string(i) + " has shape " + shape_text(b) + " for a gradient of shape " + shape_text(a));
-        if (a.strides() != b.strides() && !(a.is_contiguous() && b.is_contiguous()))
+        if (!same_order(a, b))
             refuse("out", "item " + std::to_string(i) + " has its dimensions in another order than its gradient");
     }
     return gpd_clip_grads(g.n, g.types.data(), g.at.data(), o.types.data(), o.at.data(), g.counts.data(), norm, max_norm,
