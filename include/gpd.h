@@ -537,6 +537,7 @@ gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, int64_t ld, 
                             float temperature, float* loss_dev, void* dlogits_dev, int64_t ldd, int64_t T, int64_t V,
                             void* stream);
 
+#define GPD_LM_MAX_ROWS 2147418112LL   /* 2^31 - 2^16: rows and columns of the operators from here on */
 #define GPD_HEAD_MAX_DIM 256          /* columns of a head */
 #define GPD_HEAD_MAX_HEADS 1024
 #define GPD_HEAD_MAX_AXES 4           /* axes that positions have */
@@ -548,7 +549,7 @@ gpd_status gpd_distill_topk(gpd_dtype type, const void* logits_dev, int64_t ld, 
  * q: T rows of q_heads * head_dim columns, k: of k_heads * head_dim; both may be parts of one wider matrix (ldq, ldk), and
  * either may have no heads.  Weights have head_dim elements of weight_type (`type` or GPD_DT_F32), shared by the heads of q
  * and of k; both NULL: no norm, rotation alone.  FP32 inside, y is rounded once.  q_out may be q and k_out may be k, with the
- * same stride.  head_dim is even and at most GPD_HEAD_MAX_DIM.
+ * same stride.  head_dim is even and at most GPD_HEAD_MAX_DIM, T at most GPD_LM_MAX_ROWS (GPD_ERR_SHAPE).
  * Rotation: with half = rotated / 2, pair j is (z_j, z_(j + half)), or (z_2j, z_(2j + 1)) where neighbours != 0, and becomes
  *   (a c - b s, b c + a s)  with  c = table[pos][j], s = table[pos][half + j]
  * table: `positions` rows of at least `rotated` floats, ldt apart (angles belong in 64 bits before their cosines are taken);
@@ -610,6 +611,7 @@ gpd_status gpd_clip_grads(int32_t n, const int32_t* types_host, const void* cons
  * not decreasing, from 0 to T at most) and index (S) have index_bytes 4 or 8 and lie in device memory.  Segments may be
  * empty, of one row, or share adapters.  index -1 (any negative number): no adapter, out = base and h = 0.  An index >= n makes
  * its rows of h and out NaN.  Rows before the first segment and behind the last are left as they were.
+ * T, K and N are at most GPD_LM_MAX_ROWS, n and S at most 2^30 (GPD_ERR_SHAPE).
  * x: T rows of K; A: n matrices of r x K (rows lda apart, matrices next_a), B: n matrices of N x r; all of `type`, BF16 or FP16.
  * scale: n floats or NULL (1).  base and out: T rows of N of out_type (`type` or FP32); base NULL: zero; out may be base with the
  * same stride.  h: T x r floats, contiguous: written, and what gpd_adapter_backward needs.  Sums are FP32, h goes into the second

@@ -7,10 +7,15 @@ using namespace gpd::adapter;
 
 namespace {
 
+// Rows, segments and adapters are counted in 32 bits: there is room for the steps of the loops over them.
+constexpr int32_t kMost = 1 << 30;
+bool sizes_fit(int64_t T, int64_t K, int64_t N, int32_t n, int32_t r) {
+    return T >= 0 && T <= GPD_LM_MAX_ROWS && K > 0 && N > 0 && K <= GPD_LM_MAX_ROWS && N <= GPD_LM_MAX_ROWS && n >= 0 && n <= kMost && r > 0 && r <= kMaxRank;
+}
 gpd_status check_adapters(int type, int64_t T, int64_t K, int64_t N, int32_t n, int32_t r, const void* A, int64_t lda, int64_t next_a,
                           const void* B, int64_t ldb, int64_t next_b, int32_t index_bytes, const void* offsets, const void* index, int32_t S) {
     if (type != GPD_DT_BF16 && type != GPD_DT_F16) return GPD_ERR_ARG;
-    if (T < 0 || T > 0x7fffffff || K <= 0 || N <= 0 || K > 0x7fffffff || N > 0x7fffffff || n < 0 || r <= 0 || r > kMaxRank || S < 0) return GPD_ERR_SHAPE;
+    if (!sizes_fit(T, K, N, n, r) || S < 0 || S > kMost) return GPD_ERR_SHAPE;
     if (lda < K || ldb < r || (n > 1 && (next_a < lda * (r - 1) + K || next_b < ldb * (N - 1) + r))) return GPD_ERR_SHAPE;
     if (index_bytes != 4 && index_bytes != 8) return GPD_ERR_ARG;
     if (n > 0 && (!A || !B)) return GPD_ERR_ARG;
@@ -55,7 +60,7 @@ extern "C" gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx
 
 extern "C" gpd_status gpd_adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int32_t n, int32_t r, int64_t* bytes_host) {
     if (!bytes_host) return GPD_ERR_ARG;
-    if (T < 0 || T > 0x7fffffff || K <= 0 || N <= 0 || K > 0x7fffffff || N > 0x7fffffff || n < 0 || r <= 0 || r > kMaxRank) return GPD_ERR_SHAPE;
+    if (!sizes_fit(T, K, N, n, r)) return GPD_ERR_SHAPE;
     *bytes_host = up(4 * T * r) + grad_workspace(T, n, r, K, N);
     return GPD_OK;
 }

@@ -939,7 +939,7 @@ gpd_status launch_heads_backward(HeadArgs a, float* dqw, float* dkw, cudaStream_
 // What both directions check.  GPD_OK with a.T = 0: nothing to do.
 gpd_status check_heads(int type, int weight_type, const HeadArgs& a, int index_bytes, bool norm) {
     if (!is_float_type(type) || (norm && weight_type != type && weight_type != GPD_DT_F32)) return GPD_ERR_ARG;
-    if (a.T < 0 || a.T > 0x7fffffff || a.D <= 0 || a.D % 2 || a.D > kMaxHead || a.R < 0 || a.R % 2 || a.R > a.D) return GPD_ERR_SHAPE;
+    if (a.T < 0 || a.T > GPD_LM_MAX_ROWS || a.D <= 0 || a.D % 2 || a.D > kMaxHead || a.R < 0 || a.R % 2 || a.R > a.D) return GPD_ERR_SHAPE;
     if (!norm && a.R == 0) return GPD_ERR_ARG;
     const Part *q = &a.part[0], *k = &a.part[1];
     if (q->heads < 0 || k->heads < 0 || q->heads > GPD_HEAD_MAX_HEADS || k->heads > GPD_HEAD_MAX_HEADS) return GPD_ERR_SHAPE;
