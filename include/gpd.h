@@ -631,6 +631,9 @@ gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n
  * dx NULL: not wanted.  dA (n matrices of r x K) and dB (n of N x r) of grad_type (`type` or FP32), both or neither; every
  * adapter's are written, zeros where it has no rows, or added to what is there (accumulate != 0).  Rows without an adapter
  * have dx = dbase and give no gradient; rows outside the segments are not looked at and their dx is left as it was.
+ * An infinity in x or dout makes the gradients that it enters infinite or NaN.  dA and dB of more than about 65000 adapters want rows
+ * of x and dout on 16-byte boundaries and segments of 32 rows and more on average (GPD_ERR_SHAPE: adapters and T / 2048 are more
+ * than 65535).  Outputs overlap nothing else of the call but what is named here.
  * Sums are taken in a fixed order.  workspace_dev: the bytes that gpd_adapter_backward_workspace gives, on a 16-byte boundary.
  */
 gpd_status gpd_adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int32_t n, int32_t r, int64_t* bytes_host);

@@ -91,15 +91,17 @@ extern "C" gpd_status gpd_adapter_backward(gpd_dtype type, const void* dout_dev,
     const Segments seg{offsets_dev, index_dev, T, rows ? S : 0, n, index_bytes == 8};
     cudaStream_t st = as_stream(stream);
     float* u = static_cast<float*>(workspace_dev);     // scale_i B_i^T dout, [T][r]
+    // dB first: dout may still be in L2
+    const GradArgs two[2] = {{dout_dev, lddo, h_dev, scale_dev, dB_dev, lddB, next_db, N, lm::rows_aligned(dout_dev, lddo, 2), false},
+                             {x_dev, ldx, u, nullptr, dA_dev, ldda, next_da, K, lm::rows_aligned(x_dev, ldx, 2), true}};
+    if (grads && !gradients_fit(seg, two)) return GPD_ERR_SHAPE;
     if (rows) {
         const ShrinkArgs down{seg, dout_dev, lddo, B_dev, ldb, next_b, scale_dev, u, N, r, lm::rows_aligned(dout_dev, lddo, 2),
                               weights_aligned(B_dev, ldb, next_b)};
         const gpd_status s = shrink(type, true, down, st);
         if (s != GPD_OK) return s;
     }
-    if (grads) {                                       // before dx, and dB first: dout may still be in L2
-        const GradArgs two[2] = {{dout_dev, lddo, h_dev, scale_dev, dB_dev, lddB, next_db, N, lm::rows_aligned(dout_dev, lddo, 2), false},
-                                 {x_dev, ldx, u, nullptr, dA_dev, ldda, next_da, K, lm::rows_aligned(x_dev, ldx, 2), true}};
+    if (grads) {                                       // before dx
         const gpd_status s = gradients(type, grad_type, accumulate != 0, seg, r, two, static_cast<unsigned char*>(workspace_dev) + own, st);
         if (s != GPD_OK) return s;
     }

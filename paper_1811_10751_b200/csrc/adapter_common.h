@@ -328,6 +328,7 @@ gpd_status shrink(int type, bool transposed, const ShrinkArgs& a, cudaStream_t s
 gpd_status expand(int type, int out_type, bool transposed, const ExpandArgs& a, cudaStream_t st);
 gpd_status short_segments(int type, int out_type, const ShrinkArgs& down, const ExpandArgs& above, bool* taken, cudaStream_t st);
 int64_t grad_workspace(int64_t T, int64_t n, int64_t r, int64_t K, int64_t N);
+bool gradients_fit(const Segments& seg, const GradArgs (&two)[2]);
 gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& seg, int r, const GradArgs (&two)[2], void* workspace,
                      cudaStream_t st);
 

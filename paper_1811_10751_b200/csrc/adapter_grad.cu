@@ -645,6 +645,7 @@ int64_t run_rows(int64_t T, int64_t K, int64_t N) {
 int64_t slots_of(int64_t T, int64_t n, int64_t K, int64_t N) { return T / run_rows(T, K, N) + n; }    // most runs there can be
 // Segments of less than 32 rows on average would leave half of their tiles empty.
 bool long_segments(int64_t T, int64_t S) { return S > 0 && T >= 32 * S; }
+bool by_tma(const Segments& s, const GradArgs (&two)[2]) { return two[0].y_vec && two[1].y_vec && long_segments(s.T, s.S); }
 int64_t chunks_of(int64_t T, int64_t S) { return T / kRows + S; }      // most chunks there can be
 // CTAs that share an adapter's rows: as many as are resident at once, if as many adapters as there are segments have rows; each has
 // four chunks at least.
@@ -681,7 +682,6 @@ gpd_status launch(const Job& job, T* planes, unsigned long long* counts, int32_t
         rc = launch_after(split_kernel<T, PARTS>, dim3(blocks), dim3(256), 0, 1, st, job, RP, planes, most_chunks, counts, slots);
         if (rc != GPD_OK) return rc;
         const int splits = splits_of(job.seg.T, job.seg.S, job.seg.n, job.tiles, S::PER_SM * sm_count());
-        if (job.tiles > 65535 || (int64_t)job.seg.n * splits > 0x7fffffff) return GPD_ERR_SHAPE;
         return launch_after(kernel, dim3((unsigned)(job.seg.n * splits), job.tiles), dim3(kTmaThreads), S::SMEM, splits, st, maps, job, splits);
     }
     {
@@ -731,10 +731,16 @@ int grad_status_fetch_and_clear() {
     return v;
 }
 
+// Whether a launch's grid has room: all column tiles beside all adapters (by TMA), or beside all runs.
+bool gradients_fit(const Segments& seg, const GradArgs (&two)[2]) {
+    const int64_t K = two[0].C, N = two[1].C;
+    return by_tma(seg, two) ? tiles_of(K, N) <= 65535 && (int64_t)seg.n * 8 <= 0x7fffffff : slots_of(seg.T, seg.n, K, N) <= 65535;
+}
+
 gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& seg, int r, const GradArgs (&two)[2], void* workspace,
                      cudaStream_t st) {
     const Workspace at(seg.T, seg.n, r, two[0].C, two[1].C);
-    const bool tma = two[0].y_vec && two[1].y_vec && long_segments(seg.T, seg.S);
+    const bool tma = by_tma(seg, two);
     Job job;
     job.two[0] = two[0];
     job.two[1] = two[1];
@@ -742,9 +748,7 @@ gpd_status gradients(int type, int grad_type, bool accumulate, const Segments& s
     job.r = r;
     job.accumulate = accumulate;
     job.run = run_rows(seg.T, two[0].C, two[1].C);
-    const int64_t runs = slots_of(seg.T, seg.n, two[0].C, two[1].C);
-    if (runs > 65535) return GPD_ERR_SHAPE;
-    job.max_slots = (int)runs;
+    job.max_slots = (int)slots_of(seg.T, seg.n, two[0].C, two[1].C);
     job.first_tiles = (unsigned)((two[0].C + kCols - 1) / kCols);
     job.tiles = (unsigned)tiles_of(two[0].C, two[1].C);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
