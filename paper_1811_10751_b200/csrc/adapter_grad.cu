@@ -505,6 +505,11 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&tmem_slot)), "r"(S::COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    // The kernel behind this one may want tensor memory too, and hold it while it waits for this one's end: it is let in only when
+    // this CTA has its own.
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     after_previous();
     // the cluster's adapter; this CTA's chunks of it
     const int id = blockIdx.x / splits, rank = blockIdx.x % splits, first = job.slots[id], have = job.slots[id + 1] - first;
@@ -513,9 +518,6 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
     const GradArgs& a = job.two[second];
     const int c0 = (int)(blockIdx.y - (second ? job.first_tiles : 0)) * kCols;
     const float scale = a.scale ? a.scale[id] : 1.f;
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_slot;
     float sum[RP];
     if (warp == 0) {
