@@ -44,7 +44,7 @@ struct Shape {
 };
 
 template <typename T, typename O, int NT, int PARTS>
-__global__ void __launch_bounds__(kThreads) short_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+__global__ void __launch_bounds__(kThreads, NT == 2 && sizeof(O) == 2 ? 5 : 1) short_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                          const __grid_constant__ ShortArgs s, int log_splits) {
     using S = Shape<NT>;
     constexpr int KT = S::RP / 16;
