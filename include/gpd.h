@@ -630,7 +630,8 @@ gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n
  * dout: T rows of N of `type`; h as the forward call left it.  dx (of dx_type, `type` or FP32) and dbase as out and base above;
  * dx NULL: not wanted.  dA (n matrices of r x K) and dB (n of N x r) of grad_type (`type` or FP32), both or neither; every
  * adapter's are written, zeros where it has no rows, or added to what is there (accumulate != 0).  Rows without an adapter
- * have dx = dbase and give no gradient; rows outside the segments are not looked at and their dx is left as it was.
+ * have dx = dbase and give no gradient; rows outside the segments are not looked at and their dx is left as it was.  u enters dx and
+ * dA, h dB with as many bits as h does out.
  * An infinity in x or dout makes the gradients that it enters infinite or NaN.  dA and dB of more than about 65000 adapters want rows
  * of x and dout on 16-byte boundaries and segments of 32 rows and more on average (GPD_ERR_SHAPE: adapters and T / 2048 are more
  * than 65535).  Outputs overlap nothing else of the call but what is named here.

@@ -7,9 +7,9 @@
 // ahead.  The tensor cores leave a lane two neighbouring columns of a tile of eight: the four lanes of a row exchange words, so
 // that each reads and writes eight columns, 16 bytes, of it.
 //
-// Measured (BF16, many rows, base read and out written; the first product is not in these times): 16384 x 8192, rank 32, 103 us
-// of 83 at the copy bandwidth (tensor pipe 37 %, DRAM 61 %); 4001 x 6144, rank 64, 33 us (tensor pipe 44 %): the products of
-// two parts, the reads and writes of a tile in shared memory and the copies take turns in a warp.
+// Measured (BF16, many rows, base read and out written; the first product is not in these times): 16384 x 8192, rank 32, 104 us
+// of 83 at the copy bandwidth (tensor pipe 54 %, DRAM 60 %); 4001 x 6144, rank 64, 40 us cold (tensor pipe 53 %; 33 with two parts):
+// the products of three parts, the reads and writes of a tile in shared memory and the copies take turns in a warp.
 #include <algorithm>
 #include <type_traits>
 
@@ -159,7 +159,8 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     }
     __syncthreads();
     // The kernel before this one is the same call's: it began its work, and let this one start, when all before it had
-    // completed, and it writes h alone.  So only the warps that read h wait for it; segments, W and base are there.
+    // completed.  It is the first product, which writes h alone, or that of the factors' gradients, which writes dA and dB, and these
+    // overlap nothing else of the call.  So only the warps that read h wait for it; segments, W and base are there.
     bool waited = warp == kThreads / 32;
     const int64_t chunks = (a.C + kCols - 1) / kCols, all = count_tiles<S::TM>(a.seg) * chunks;
     const int64_t last = all * (blockIdx.x + 1) / gridDim.x;
@@ -213,7 +214,8 @@ expand_tma_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                                       : S::W::lane_at(stage + S::BASE, col_first_row(), col_first());
             const uint32_t block0 = WTile<S::TM, kCols>::lane_at(mine, row_first(), row_first_col());
             if (any) {
-                // the sums begin with base where the result has 16 bits, whose rounding hides the tensor cores' truncation
+                // the sums begin with base where the result has 16 bits: their chain's steps lose at most 2^-22 of it each, the
+                // rounding 2^-8 (adding it behind the chain: 4001 x 4096 -> 6144, rank 64, 58.7 us for both products, so 55.9)
                 constexpr bool kOnBase = sizeof(O) == 2 && std::is_same<T, __nv_bfloat16>::value;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) { // 32 columns: four chains of additions side by side

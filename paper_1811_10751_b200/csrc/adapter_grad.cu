@@ -1,8 +1,9 @@
 // Gradients of low-rank adapters' factors: dW_i[c][k] = scale_i sum_t y[t][c] h[t][k] over the rows t of adapter i.
 //
 // Bound by reading y, 128 columns of which a CTA takes over a part of the adapter's rows (its segments' rows one after the
-// other); the r columns of h are few.  The parts' sums meet in a fixed order.  h is
-// FP32 and goes through the tensor cores as a sum of 16-bit parts, three, or two for FP16 gradients of FP16.  The chain of the tensor cores' additions is cut every 64 rows.
+// other); the r columns of h are few.  The parts' sums meet in a fixed order.  h is FP32 and goes through the tensor cores as a
+// sum of 16-bit parts, three, or two for FP16 gradients of FP16.  The chain of the tensor cores' additions is cut every 64 rows
+// (every 256 for FP16 gradients of FP16 by TMA: 32 steps, of at most 2^-22 each).
 // Two forms.  Rows on 16-byte boundaries and segments that are not short: a first kernel cuts h into its parts, once for all
 // columns of y, and tiles of both come by TMA, 64 rows of one segment each; the CTAs of a cluster share an adapter's rows and
 // add up over distributed shared memory; FP16 parts are taken of an adapter's column over a power of two.  Otherwise
@@ -449,8 +450,8 @@ __global__ void __launch_bounds__(256) split_kernel(const __grid_constant__ Job 
 
 // The tensor cores take both tiles as TMA leaves them, rows of y and h being the depth of the product: D (128 columns of y x
 // RP columns of h) in tensor memory, two accumulators in turn.  One warp issues copies, one the products, four pull a finished
-// accumulator into registers and add it up to nearest: the chain of truncating additions in tensor memory is cut every chunk (FP32
-// gradients of three parts: 12 steps) or every fourth.
+// accumulator into registers and add it up to nearest: the chain of truncating additions in tensor memory is cut every chunk (three
+// parts: 12 steps) or every fourth (two: 32).
 template <int MT, int PARTS>
 struct TmaShape {
     static constexpr int RP = 16 * MT, GROUP = PARTS == 3 ? 1 : 4, COLS = 2 * RP < 32 ? 32 : 2 * RP;      // columns of tensor memory
@@ -638,7 +639,8 @@ grad_tma_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ J
 }
 
 int64_t tiles_of(int64_t K, int64_t N) { return (K + kCols - 1) / kCols + (N + kCols - 1) / kCols; }
-// Rows of a run where rows are gathered: so many runs that two CTAs per SM (of 148) are busy, of 256 rows at least.
+// Rows of a run where rows are gathered: so many runs that two CTAs per SM are busy, of 256 rows at least.  148 SMs as a constant: the
+// workspace's size is asked for without a device.
 int64_t run_rows(int64_t T, int64_t K, int64_t N) {
     const int64_t runs = std::max<int64_t>(1, 2 * 148 / tiles_of(K, N));
     const int64_t rows = ((T + runs - 1) / runs + kRows - 1) / kRows * kRows;
