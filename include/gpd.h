@@ -615,8 +615,8 @@ gpd_status gpd_clip_grads(int32_t n, const int32_t* types_host, const void* cons
  * x: T rows of K; A: n matrices of r x K (rows lda apart, matrices next_a), B: n matrices of N x r; all of `type`, BF16 or FP16.
  * scale: n floats or NULL (1).  base and out: T rows of N of out_type (`type` or FP32); base NULL: zero; out may be base with the
  * same stride.  h: T x r floats, contiguous: written, and what gpd_adapter_backward needs.  Sums are FP32, h goes into the second
- * product with 24 bits, 22 where all of it is FP16 (FP16: numbers below 2^-14 of their row's largest up to 2^-39 of that); out is
- * rounded once.  1 <= r <= GPD_ADAPTER_MAX_RANK.
+ * product with 24 bits, 22 where all of it is FP16 (FP16: numbers below 2^-14 of their row's largest up to 2^-39 of that; BF16: times
+ * their scale up to 2^-134); out is rounded once.  1 <= r <= GPD_ADAPTER_MAX_RANK.
  * Rows on 16-byte boundaries (of A and B too: r a multiple of 8) are much faster.
  */
 gpd_status gpd_adapter(gpd_dtype type, const void* x_dev, int64_t ldx, int32_t n, int32_t r, const void* A_dev, int64_t lda,
